@@ -531,6 +531,172 @@ spec_status_t spec_lm_head_stats(const spec_lm_head_args_t* lm, void* ws, size_t
 spec_status_t spec_accept_block_noalloc(const spec_accept_args_t* accept, spec_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------
+ * A KV cache held in 8 bits
+ *
+ * Layout of one layer's cache, shared by the two calls below:
+ *   kv_cache: e4m3 [num_pages][Hkv][2][page_size][D], 16-byte aligned; [..][0] are a
+ *             page's keys, [..][1] its values. Keys and values of a page and head are
+ *             adjacent so that one copy brings both.
+ *   kv_scale: fp32 [num_pages][Hkv][2]; an element stands for its e4m3 value times the
+ *             scale of its page, head and kind.
+ * spec_append_kv_fp8 writes scales that are powers of two in [2^-32, 2^32].
+ * ------------------------------------------------------------------------------------- */
+
+/*
+ * Pages and cache slots for the new tokens of a ragged batch (the block of a verify step,
+ * a prompt, or a mix). Sequence b holds kv_len[b] tokens and gets num_new[b] >= 0 more. Its
+ * table row already holds the pages of its first kv_len[b] + reserved tokens (reserved =
+ * gamma after spec_commit_kv with reserve = 1, else 0); the ones it lacks come from the top
+ * of the free list, in order. As in spec_commit_kv, requests are served in batch order
+ * while their running total fits the list, and a refused request still counts against the
+ * later ones; a sequence that needs no page is never refused.
+ *   - row_start[b] = num_new[0] + .. + num_new[b-1] (negative counts as 0, saturated at
+ *     INT32_MAX): the first row of b in the packed batch; row_start[batch] is the total.
+ *   - Row r of sequence b is its token at position kv_len[b] + r - row_start[b]:
+ *     slots[r] = page * page_size + position % page_size, or -1 where the sequence was not
+ *     served or a page id is outside [0, num_pages). Rows from the total up to max_rows
+ *     get -1 in slots, positions and row_seq; rows past max_rows are not written.
+ *   - new_len[b] = kv_len[b] + num_new[b] where served, else kv_len[b]; new_free_count: the
+ *     pages left. Either may be the array that is read (kv_len, free_count).
+ *   - flags[b]: 0 served; 1 kv_len or num_new negative, or their sum above
+ *     max_pages_per_seq * page_size; 2 the pages did not fit the free list.
+ * One launch; batch <= SPEC_SLOTS_MAX_BATCH. The workspace holds one counter (zero-filled
+ * once when new, zero again after each call).
+ */
+#define SPEC_SLOTS_MAX_BATCH 8192
+typedef struct {
+  int32_t batch, page_size, max_pages_per_seq, num_pages;
+  int32_t reserved;             /* >= 0: tokens past kv_len whose pages the table holds       */
+  int32_t max_rows;             /* >= 1: entries of slots, positions and row_seq              */
+  int32_t free_capacity;        /* entries of free_pages                                      */
+  const int32_t* num_new;       /* [batch]                                                    */
+  const int32_t* kv_len;        /* [batch]                                                    */
+  int32_t* new_len;             /* [batch], written; may be kv_len                            */
+  int32_t* page_table;          /* [batch][max_pages_per_seq], new pages written              */
+  const int32_t* free_pages;    /* [free_capacity]                                            */
+  const int32_t* free_count;    /* [1], clamped to [0, free_capacity]                         */
+  int32_t* new_free_count;      /* [1], written; may be free_count                            */
+  int32_t* row_start;           /* [batch + 1], written                                       */
+  int32_t* slots;               /* [max_rows], written                                        */
+  int32_t* positions;           /* [max_rows], written, or NULL                               */
+  int32_t* row_seq;             /* [max_rows], written, or NULL                               */
+  int32_t* flags;               /* [batch], written, or NULL                                  */
+} spec_slot_args_t;
+
+size_t spec_slot_workspace_size(const spec_slot_args_t* slots);
+spec_status_t spec_map_slots(const spec_slot_args_t* slots, void* ws, size_t ws_bytes,
+                             spec_stream_t stream);
+
+/*
+ * Writes new keys and values into the 8-bit cache: row r goes to slot slots[r] (page
+ * slots[r] / page_size, place slots[r] % page_size); negative slots are skipped. For each
+ * page, head and kind (K or V) that the call writes to:
+ *   - need = the smallest power of two, at least 2^-32 and at most 2^32, with
+ *     max |x| <= 448 * need over the finite new values x;
+ *   - a page whose place 0 is written starts anew: its scale becomes need, and its places
+ *     that are not written hold nothing of use (tokens of a sequence are written in order);
+ *   - any other page goes on: its scale becomes max(old scale, need), and if that is more
+ *     than the old one its unwritten places are rounded again to the new scale;
+ *   - x is stored as the nearest e4m3 value of x / scale (ties to even, beyond +-448, so
+ *     also infinities, as +-448, NaN as NaN).
+ * A scale never falls while a page goes on, so a rejected block leaves it as it made it.
+ * Rows written to one page lie within SPEC_APPEND_WINDOW consecutive rows, and no two rows
+ * of a call have one slot (else the affected pages hold unspecified values). Keeping a
+ * candidate tree's accepted path is this call too: the path's rows with the slots of
+ * their final positions, every other row's slot negative. A slot at or past
+ * num_pages * page_size is skipped and sets SPEC_FLAG_BAD_PAGE in *status (if given).
+ * One launch, no workspace; with rows = 0 nothing is read (k, v and slots may be NULL).
+ */
+#define SPEC_APPEND_WINDOW 128
+typedef struct {
+  int32_t rows, num_kv_heads, head_dim, page_size, num_pages;  /* head_dim 64 or 128;
+                                   page_size 16, 32 or 64                                     */
+  int64_t k_row_stride, v_row_stride;  /* elements from one row to the next, multiples of 8;
+                                   0: num_kv_heads * head_dim                                 */
+  const void* k;                /* bf16 rows of [num_kv_heads][head_dim], 16-byte aligned     */
+  const void* v;                /* likewise                                                   */
+  const int32_t* slots;         /* [rows]                                                     */
+  void* kv_cache;               /* updated                                                    */
+  float* kv_scale;              /* updated                                                    */
+  uint32_t* status;             /* a status word (e.g. a workspace's first word), or NULL     */
+} spec_append_fp8_args_t;
+
+spec_status_t spec_append_kv_fp8(const spec_append_fp8_args_t* append, spec_stream_t stream);
+
+/*
+ * spec_verify_attention over the 8-bit cache: the same masks, sequence rules, flags and
+ * outputs, with key k of head g standing for kv_scale[page][g][0] * its e4m3 values and its
+ * value for kv_scale[page][g][1] * its e4m3 values. Scales are positive and finite; value
+ * scales are read clamped to [2^-32, 2^32]. A query row that sees no key (an empty tree
+ * mask over an empty prefix) gets out = 0 and lse = -inf. What a row's mask hides (keys past
+ * kv_len, or hidden block keys) does not reach it, whatever the bytes there. Scores,
+ * softmax statistics and accumulators are fp32. path: SPEC_ATTN_AUTO or
+ * SPEC_ATTN_CUDA_CORES. The workspace rules are spec_verify_attention's.
+ */
+typedef struct {
+  int32_t batch;              /* >= 1                                                       */
+  int32_t gamma;              /* 1 .. 64                                                    */
+  int32_t num_q_heads;        /* a multiple of num_kv_heads                                 */
+  int32_t num_kv_heads;
+  int32_t head_dim;           /* 64 or 128                                                  */
+  int32_t page_size;          /* 16, 32 or 64                                               */
+  int32_t max_pages_per_seq;
+  int32_t num_pages;
+  float softmax_scale;        /* 0 => 1/sqrt(head_dim)                                      */
+  int32_t path;               /* SPEC_ATTN_AUTO or SPEC_ATTN_CUDA_CORES                      */
+  const void* q;              /* bf16 [batch][gamma][Hq][D], 16-byte aligned                */
+  const void* kv_cache;       /* as above                                                   */
+  const float* kv_scale;      /* as above, 8-byte aligned                                   */
+  const int32_t* page_table;  /* [batch][max_pages_per_seq]; entries past the sequence unread */
+  const int32_t* kv_len;      /* [batch]: keys in the cache, the block's own included       */
+  void* out;                  /* bf16 [batch][gamma][Hq][D], 16-byte aligned                */
+  float* lse;                 /* fp32 [batch][gamma][Hq], or NULL                           */
+  const uint64_t* tree_mask;  /* [batch][gamma], or NULL                                    */
+} spec_attn_fp8_args_t;
+
+size_t spec_attn_fp8_workspace_size(const spec_attn_fp8_args_t* attn);
+spec_status_t spec_verify_attention_fp8(const spec_attn_fp8_args_t* attn, void* ws,
+                                        size_t ws_bytes, spec_stream_t stream);
+
+/*
+ * Penalties for repeated tokens, biases and grammar masks on the logits of a verify step,
+ * before the acceptance (or the draft sampling) reads them. For row j of sequence b, with
+ * prompt = history[b][0 .. prompt_len[b]), output = history[b][prompt_len[b] ..
+ * history_len[b]), and, if block_tokens is given, the block's tokens t_i with i <= j
+ * (block_shift = 0: target row j is the distribution after t_j) or i < j (block_shift = 1:
+ * drafter row j is the one that t_j was drawn from) counted as output too:
+ *   1. x = logit; if the token is in prompt or output: x = x > 0 ? x / r : x * r,
+ *      r = repetition[b];
+ *   2. c = how often the token is in output: x -= frequency[b] * c; x -= presence[b] if c > 0;
+ *   3. if the token is in bias_tokens[b]: x += the value beside it (its first place there);
+ *   4. if allowed is given and bit v % 32 of allowed[b][j][v / 32] is 0: x = -inf.
+ * Each step is one fp32 operation, the result rounded once to the logits' type. Tokens
+ * outside [0, vocab) in history, block or bias are ignored. history_len is clamped to
+ * [0, max_history], prompt_len to [0, history_len]. A masked entry is -inf
+ * whatever its logit; a row may end with no finite entry (the acceptance flags it).
+ * out may be logits itself. One launch, no workspace.
+ */
+typedef struct {
+  int32_t batch, gamma, vocab, logits_dtype;  /* gamma 1 .. 64, batch <= 65535                */
+  int32_t block_shift;          /* 0 or 1                                                     */
+  int32_t max_history, max_bias;  /* row lengths of history and bias_*; 0: none               */
+  const void* logits;           /* [batch][gamma][vocab]                                      */
+  void* out;                    /* the same type and shape, written                           */
+  const int32_t* block_tokens;  /* [batch][gamma], or NULL                                    */
+  const int32_t* history;       /* [batch][max_history], or NULL                              */
+  const int32_t* history_len;   /* [batch] (with history)                                     */
+  const int32_t* prompt_len;    /* [batch], or NULL: no prompt, all of history is output      */
+  const float* repetition;      /* [batch], or NULL: 1                                        */
+  const float* frequency;       /* [batch], or NULL: 0                                        */
+  const float* presence;        /* [batch], or NULL: 0                                        */
+  const int32_t* bias_tokens;   /* [batch][max_bias], or NULL                                 */
+  const float* bias_values;     /* [batch][max_bias] (with bias_tokens)                       */
+  const uint32_t* allowed;      /* [batch][gamma][ceil(vocab / 32)], or NULL                  */
+} spec_adjust_args_t;
+
+spec_status_t spec_adjust_logits(const spec_adjust_args_t* adjust, spec_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
  * Test hooks for the timeout path (not part of the verify step)
  *
  * The kernels' internal waits on asynchronous copies and tensor-core operations are

@@ -119,6 +119,52 @@ class LmHeadArgs(ctypes.Structure):
                 ("token_logit", ctypes.c_void_p), ("logits", ctypes.c_void_p)]
 
 
+class SlotArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("free_capacity", ctypes.c_int32), ("num_new", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("new_len", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("free_count", ctypes.c_void_p), ("new_free_count", ctypes.c_void_p),
+                ("row_start", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("row_seq", ctypes.c_void_p),
+                ("flags", ctypes.c_void_p)]
+
+
+class AppendFp8Args(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("k_row_stride", ctypes.c_int64),
+                ("v_row_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("kv_cache", ctypes.c_void_p),
+                ("kv_scale", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class AttnFp8Args(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("gamma", ctypes.c_int32),
+                ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("path", ctypes.c_int32),
+                ("q", ctypes.c_void_p), ("kv_cache", ctypes.c_void_p),
+                ("kv_scale", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("tree_mask", ctypes.c_void_p)]
+
+
+class AdjustArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("gamma", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("logits_dtype", ctypes.c_int32), ("block_shift", ctypes.c_int32),
+                ("max_history", ctypes.c_int32), ("max_bias", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("block_tokens", ctypes.c_void_p), ("history", ctypes.c_void_p),
+                ("history_len", ctypes.c_void_p), ("prompt_len", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("bias_tokens", ctypes.c_void_p),
+                ("bias_values", ctypes.c_void_p), ("allowed", ctypes.c_void_p)]
+
+
 HEADER = os.path.join(_build.ROOT, "include", "spec_verify.h")
 
 
@@ -181,6 +227,15 @@ def lib(build_if_missing: bool = True):
             L.spec_tree_build_workspace_size.restype = ctypes.c_size_t
             L.spec_build_tree.argtypes = [P, P, ctypes.c_size_t, P]
             L.spec_build_tree.restype = ctypes.c_int
+            for f in ("spec_slot_workspace_size", "spec_attn_fp8_workspace_size"):
+                getattr(L, f).argtypes = [P]
+                getattr(L, f).restype = ctypes.c_size_t
+            for f in ("spec_map_slots", "spec_verify_attention_fp8"):
+                getattr(L, f).argtypes = [P, P, ctypes.c_size_t, P]
+                getattr(L, f).restype = ctypes.c_int
+            for f in ("spec_append_kv_fp8", "spec_adjust_logits"):
+                getattr(L, f).argtypes = [P, P]
+                getattr(L, f).restype = ctypes.c_int
             for f in ("spec_test_attention_wait_timeout", "spec_test_lm_head_wait_timeout"):
                 getattr(L, f).argtypes = [P, P, ctypes.c_size_t, P]
                 getattr(L, f).restype = ctypes.c_int
@@ -664,6 +719,223 @@ def lm_head_stats(hidden_states, weight, temperature, rows_per_seq: int, tokens=
         ws = new_workspace(lm_head_workspace_size(a), dev)
     lm_head_stats_args(a, ws, stream)
     return {k: v for k, v in out.items() if v is not None}
+
+
+# ----------------------------------------------------------------------------------
+# The KV cache held in 8 bits
+# ----------------------------------------------------------------------------------
+def new_kv_cache_fp8(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, device=None):
+    """One layer's empty 8-bit cache: (kv_cache e4m3 [num_pages][Hkv][2][page_size][D],
+    kv_scale fp32 [num_pages][Hkv][2])."""
+    dev = device or "cuda"
+    cache = torch.zeros(num_pages, num_kv_heads, 2, page_size, head_dim, dtype=torch.uint8, device=dev)
+    return (cache.view(torch.float8_e4m3fn),
+            torch.full((num_pages, num_kv_heads, 2), 2.0 ** -32, dtype=torch.float32, device=dev))
+
+
+def slot_args(num_new, kv_len, new_len, page_table, page_size: int, num_pages: int, free_pages,
+              free_count, new_free_count, row_start, slots, positions=None, row_seq=None,
+              flags=None, reserved: int = 0) -> SlotArgs:
+    B, MP = page_table.shape
+    R = slots.numel()
+    for t, name, shape in ((num_new, "num_new", (B,)), (kv_len, "kv_len", (B,)),
+                           (new_len, "new_len", (B,)), (page_table, "page_table", (B, MP)),
+                           (free_pages, "free_pages", None), (free_count, "free_count", (1,)),
+                           (new_free_count, "new_free_count", (1,)),
+                           (row_start, "row_start", (B + 1,)), (slots, "slots", (R,))):
+        _check(t, name, torch.int32, shape)
+    for t, name, shape in ((positions, "positions", (R,)), (row_seq, "row_seq", (R,)),
+                           (flags, "flags", (B,))):
+        if t is not None:
+            _check(t, name, torch.int32, shape)
+    return SlotArgs(B, int(page_size), MP, int(num_pages), int(reserved), R, free_pages.numel(),
+                    num_new.data_ptr(), kv_len.data_ptr(), new_len.data_ptr(),
+                    page_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                    new_free_count.data_ptr(), row_start.data_ptr(), slots.data_ptr(),
+                    None if positions is None else positions.data_ptr(),
+                    None if row_seq is None else row_seq.data_ptr(),
+                    None if flags is None else flags.data_ptr())
+
+
+def slot_workspace_size(a: SlotArgs) -> int:
+    n = lib().spec_slot_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise SpecError(1, "spec_slot_workspace_size")
+    return int(n)
+
+
+def map_slots_args(a: SlotArgs, ws: torch.Tensor, stream=None):
+    _raise(lib().spec_map_slots(ctypes.byref(a), _ptr(ws), ws.numel(), _stream(stream)),
+           "spec_map_slots")
+
+
+def map_slots(num_new, kv_len, page_table, page_size: int, num_pages: int, free_pages, free_count,
+              max_rows: int, reserved: int = 0, ws=None, stream=None) -> Dict[str, torch.Tensor]:
+    """Pages and cache slots for num_new[b] more tokens of each sequence (spec_map_slots).
+    kv_len, page_table and free_count are updated in place. Returns row_start, the slots,
+    positions and row_seq of a batch packed by sequence (-1 past its total), and flags."""
+    B = page_table.shape[0]
+    dev = page_table.device
+    res = {k: torch.empty(n, dtype=torch.int32, device=dev)
+           for k, n in (("row_start", B + 1), ("slots", max_rows), ("positions", max_rows),
+                        ("row_seq", max_rows), ("flags", B))}
+    a = slot_args(num_new, kv_len, kv_len, page_table, page_size, num_pages, free_pages, free_count,
+                  free_count, res["row_start"], res["slots"], res["positions"], res["row_seq"],
+                  res["flags"], reserved)
+    if ws is None:
+        ws = new_workspace(slot_workspace_size(a), dev)
+    map_slots_args(a, ws, stream)
+    return res
+
+
+def _check_cache_fp8(kv_cache, kv_scale):
+    _check(kv_cache, "kv_cache", torch.float8_e4m3fn)
+    if kv_cache.dim() != 5 or kv_cache.shape[2] != 2:
+        raise ValueError("kv_cache must have shape [num_pages][Hkv][2][page_size][D]")
+    _check(kv_scale, "kv_scale", torch.float32, kv_cache.shape[:3])
+
+
+def append_fp8_args(k, v, slots, kv_cache, kv_scale, status_ws=None) -> AppendFp8Args:
+    _check_cache_fp8(kv_cache, kv_scale)
+    num_pages, Hkv, _, P, D = kv_cache.shape
+    R = slots.numel()
+    _check(slots, "slots", torch.int32, (R,))
+    strides = []
+    for t, name in ((k, "k"), (v, "v")):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+            raise TypeError(f"{name} must be a torch.bfloat16 tensor")
+        if not t.is_cuda or tuple(t.shape) != (R, Hkv, D):
+            raise ValueError(f"{name} must be a CUDA tensor of shape {(R, Hkv, D)}")
+        # rows may be strided (a column range of a wider projection), heads are dense
+        if R and t[0].stride() != (D, 1) and t[0].numel() != 1:
+            raise ValueError(f"{name} must have dense [Hkv][D] rows")
+        strides.append(t.stride(0) if R > 1 else 0)
+    return AppendFp8Args(R, Hkv, D, P, num_pages, strides[0], strides[1], k.data_ptr(),
+                         v.data_ptr(), slots.data_ptr(), kv_cache.data_ptr(), kv_scale.data_ptr(),
+                         None if status_ws is None else status_ws.data_ptr())
+
+
+def append_kv_fp8_args(a: AppendFp8Args, stream=None):
+    _raise(lib().spec_append_kv_fp8(ctypes.byref(a), _stream(stream)), "spec_append_kv_fp8")
+
+
+def append_kv_fp8(k, v, slots, kv_cache, kv_scale, status_ws=None, stream=None):
+    """Write rows k, v (bf16 [rows][Hkv][D], row stride free) into the 8-bit cache at slots
+    (spec_append_kv_fp8; kv_cache and kv_scale are updated in place)."""
+    append_kv_fp8_args(append_fp8_args(k, v, slots, kv_cache, kv_scale, status_ws), stream)
+
+
+def attn_fp8_args(q, kv_cache, kv_scale, page_table, kv_len, out, lse=None, softmax_scale=0.0,
+                  path=ATTN_AUTO, tree_mask=None) -> AttnFp8Args:
+    B, G, Hq, D = q.shape
+    _check(q, "q", torch.bfloat16)
+    _check_cache_fp8(kv_cache, kv_scale)
+    num_pages, Hkv, _, P, D2 = kv_cache.shape
+    _check(page_table, "page_table", torch.int32)
+    _check(kv_len, "kv_len", torch.int32, (B,))
+    _check(out, "out", torch.bfloat16, q.shape)
+    if lse is not None:
+        _check(lse, "lse", torch.float32, (B, G, Hq))
+    if tree_mask is not None:
+        _check(tree_mask, "tree_mask", torch.int64, (B, G))
+    if D2 != D or page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError("inconsistent attention shapes")
+    return AttnFp8Args(B, G, Hq, Hkv, D, P, page_table.shape[1], num_pages, float(softmax_scale),
+                       int(path), q.data_ptr(), kv_cache.data_ptr(), kv_scale.data_ptr(),
+                       page_table.data_ptr(), kv_len.data_ptr(), out.data_ptr(),
+                       None if lse is None else lse.data_ptr(),
+                       None if tree_mask is None else tree_mask.data_ptr())
+
+
+def attn_fp8_workspace_size(a: AttnFp8Args) -> int:
+    n = lib().spec_attn_fp8_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise SpecError(1, "spec_attn_fp8_workspace_size")
+    return int(n)
+
+
+def verify_attention_fp8_args(a: AttnFp8Args, ws: torch.Tensor, stream=None):
+    _raise(lib().spec_verify_attention_fp8(ctypes.byref(a), _ptr(ws), ws.numel(), _stream(stream)),
+           "spec_verify_attention_fp8")
+
+
+def verify_attention_fp8(q, kv_cache, kv_scale, page_table, kv_len, softmax_scale=0.0,
+                         path=ATTN_AUTO, want_lse=True, ws=None, stream=None, tree_mask=None):
+    """verify_attention over the 8-bit cache (spec_verify_attention_fp8). Returns
+    (out bf16, lse fp32 or None)."""
+    out = torch.empty_like(q)
+    lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
+    a = attn_fp8_args(q, kv_cache, kv_scale, page_table, kv_len, out, lse, softmax_scale, path,
+                      tree_mask)
+    if ws is None:
+        ws = new_workspace(attn_fp8_workspace_size(a), q.device)
+    verify_attention_fp8_args(a, ws, stream)
+    return out, lse
+
+
+# ----------------------------------------------------------------------------------
+# Penalties, biases and grammar masks
+# ----------------------------------------------------------------------------------
+def adjust_args(logits, out, block_tokens=None, history=None, history_len=None, prompt_len=None,
+                repetition=None, frequency=None, presence=None, bias_tokens=None, bias_values=None,
+                allowed=None, block_shift: int = 0) -> AdjustArgs:
+    B, G, V = logits.shape
+    if logits.dtype == torch.bfloat16:
+        dt = SPEC_BF16
+    elif logits.dtype == torch.float32:
+        dt = SPEC_F32
+    else:
+        raise TypeError("logits must be bfloat16 or float32")
+    _check(logits, "logits", logits.dtype)
+    _check(out, "out", logits.dtype, logits.shape)
+    if (history is None) != (history_len is None) or (bias_tokens is None) != (bias_values is None):
+        raise ValueError("history and history_len, bias_tokens and bias_values go together")
+    if prompt_len is not None and history is None:
+        raise ValueError("prompt_len needs a history")
+    H = N = 0
+    if history is not None:
+        H = history.shape[-1]
+        _check(history, "history", torch.int32, (B, H))
+    if bias_tokens is not None:
+        N = bias_tokens.shape[-1]
+        _check(bias_tokens, "bias_tokens", torch.int32, (B, N))
+        _check(bias_values, "bias_values", torch.float32, (B, N))
+    for t, name, dtype, shape in (
+            (block_tokens, "block_tokens", torch.int32, (B, G)),
+            (history_len, "history_len", torch.int32, (B,)),
+            (prompt_len, "prompt_len", torch.int32, (B,)),
+            (repetition, "repetition", torch.float32, (B,)),
+            (frequency, "frequency", torch.float32, (B,)),
+            (presence, "presence", torch.float32, (B,)),
+            (allowed, "allowed", torch.int32, (B, G, (V + 31) // 32))):
+        if t is not None:
+            _check(t, name, dtype, shape)
+
+    def ptr(t):
+        return None if t is None else t.data_ptr()
+    return AdjustArgs(B, G, V, dt, int(block_shift), H, N, logits.data_ptr(), out.data_ptr(),
+                      ptr(block_tokens), ptr(history), ptr(history_len), ptr(prompt_len),
+                      ptr(repetition), ptr(frequency), ptr(presence), ptr(bias_tokens),
+                      ptr(bias_values), ptr(allowed))
+
+
+def adjust_logits_args(a: AdjustArgs, stream=None):
+    _raise(lib().spec_adjust_logits(ctypes.byref(a), _stream(stream)), "spec_adjust_logits")
+
+
+def adjust_logits(logits, block_tokens=None, history=None, history_len=None, prompt_len=None,
+                  repetition=None, frequency=None, presence=None, bias_tokens=None,
+                  bias_values=None, allowed=None, block_shift: int = 0, out=None,
+                  stream=None) -> torch.Tensor:
+    """Repetition, frequency and presence penalties, biases and grammar masks (allowed: int32
+    bit words [batch][gamma][ceil(vocab / 32)]) on logits rows (spec_adjust_logits). block_shift
+    is 0 for target rows and 1 for drafter rows; out may be logits."""
+    if out is None:
+        out = torch.empty_like(logits)
+    adjust_logits_args(adjust_args(logits, out, block_tokens, history, history_len, prompt_len,
+                                   repetition, frequency, presence, bias_tokens, bias_values,
+                                   allowed, block_shift), stream)
+    return out
 
 
 def philox_uniforms(seed: int, n: int, offset: int = 0, device=None, stream=None) -> torch.Tensor:

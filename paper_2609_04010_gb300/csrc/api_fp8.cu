@@ -1,0 +1,158 @@
+// The C ABI of the 8-bit KV cache and the logit constraints (include/spec_verify.h):
+// host-side argument checks, workspace layout and launches.
+#include <climits>
+
+#include "kv_fp8.cuh"
+
+using namespace specv;
+
+namespace {
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+bool bad_ws(const void* ws) { return !ws || !aligned(ws, kWsAlign); }
+bool head_dim_ok(int d) { return d == 64 || d == 128; }
+bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64; }
+
+spec_status_t check_slots(const spec_slot_args_t* a) {
+  if (!a || a->batch < 1 || a->page_size < 1 || a->max_pages_per_seq < 1 || a->num_pages < 1 ||
+      a->reserved < 0 || a->max_rows < 1 || a->free_capacity < 0)
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (!a->num_new || !a->kv_len || !a->new_len || !a->page_table || !a->free_pages ||
+      !a->free_count || !a->new_free_count || !a->row_start || !a->slots)
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (a->batch > SPEC_SLOTS_MAX_BATCH || a->reserved > (1 << 30) ||
+      static_cast<int64_t>(a->max_pages_per_seq) * a->page_size > (1 << 30) ||
+      static_cast<int64_t>(a->num_pages) * a->page_size > INT32_MAX)
+    return SPEC_ERR_UNSUPPORTED;
+  return SPEC_OK;
+}
+
+spec_status_t check_append(const spec_append_fp8_args_t* a) {
+  if (!a || a->rows < 0 || a->num_kv_heads < 1 || a->num_pages < 1 || a->head_dim < 1 ||
+      a->page_size < 1)
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (!a->kv_cache || !a->kv_scale || (a->rows > 0 && (!a->k || !a->v || !a->slots)))
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (!head_dim_ok(a->head_dim) || !page_size_ok(a->page_size) || a->num_kv_heads > 65535 ||
+      static_cast<int64_t>(a->num_pages) * a->page_size > INT32_MAX)
+    return SPEC_ERR_UNSUPPORTED;
+  const int64_t dense = static_cast<int64_t>(a->num_kv_heads) * a->head_dim;
+  for (int64_t s : {a->k_row_stride, a->v_row_stride})
+    if (s != 0 && (s < dense || s % 8 != 0)) return SPEC_ERR_INVALID_ARGUMENT;
+  if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->kv_cache, 16) || !aligned(a->kv_scale, 4))
+    return SPEC_ERR_INVALID_ARGUMENT;
+  return SPEC_OK;
+}
+
+spec_status_t check_attn_fp8(const spec_attn_fp8_args_t* a) {
+  if (!a || a->batch < 1 || a->gamma < 1 || a->num_q_heads < 1 || a->num_kv_heads < 1 ||
+      a->max_pages_per_seq < 1 || a->num_pages < 1 || a->page_size < 1 || a->head_dim < 1 ||
+      a->num_q_heads % a->num_kv_heads != 0)
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (!a->q || !a->kv_cache || !a->kv_scale || !a->page_table || !a->kv_len || !a->out)
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (!aligned(a->q, 16) || !aligned(a->kv_cache, 16) || !aligned(a->out, 16) || !aligned(a->kv_scale, 8))
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (!(a->softmax_scale == 0.f || (a->softmax_scale > 0.f && a->softmax_scale < 1e30f)))
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (a->path != SPEC_ATTN_AUTO && a->path != SPEC_ATTN_CUDA_CORES) return SPEC_ERR_INVALID_ARGUMENT;
+  if (a->gamma > 64 || !head_dim_ok(a->head_dim) || !page_size_ok(a->page_size))
+    return SPEC_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(a->max_pages_per_seq) * a->page_size > (1 << 30) ||
+      static_cast<int64_t>(a->num_pages) * a->page_size > INT32_MAX)
+    return SPEC_ERR_UNSUPPORTED;
+  const int64_t rows = static_cast<int64_t>(a->num_q_heads / a->num_kv_heads) * a->gamma;
+  const int64_t z = static_cast<int64_t>(a->batch) * ((rows + kSimtRowTile - 1) / kSimtRowTile);
+  if (z > 65535 || a->num_kv_heads > 65535) return SPEC_ERR_UNSUPPORTED;
+  return SPEC_OK;
+}
+
+spec_status_t check_adjust(const spec_adjust_args_t* a) {
+  if (!a || a->batch < 1 || a->gamma < 1 || a->vocab < 1 || a->max_history < 0 || a->max_bias < 0)
+    return SPEC_ERR_INVALID_ARGUMENT;
+  if (a->logits_dtype != SPEC_F32 && a->logits_dtype != SPEC_BF16) return SPEC_ERR_INVALID_ARGUMENT;
+  if (a->block_shift != 0 && a->block_shift != 1) return SPEC_ERR_INVALID_ARGUMENT;
+  if (!a->logits || !a->out || (a->history && !a->history_len) || (a->max_history > 0 && !a->history) ||
+      (a->bias_tokens && !a->bias_values) || (a->max_bias > 0 && !a->bias_tokens))
+    return SPEC_ERR_INVALID_ARGUMENT;
+  const uintptr_t esz = a->logits_dtype == SPEC_BF16 ? 2 : 4;
+  if (!aligned(a->logits, esz) || !aligned(a->out, esz)) return SPEC_ERR_INVALID_ARGUMENT;
+  if (a->gamma > 64 || a->batch > 65535) return SPEC_ERR_UNSUPPORTED;
+  return SPEC_OK;
+}
+
+size_t attn_fp8_bytes(const spec_attn_fp8_args_t& a, int sms) {
+  return attn_fp8_plan(a, kWsHeader, sms, a.path).end;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t spec_slot_workspace_size(const spec_slot_args_t* a) {
+  return check_slots(a) == SPEC_OK ? kWsHeader + kWsAlign : 0;
+}
+
+spec_status_t spec_map_slots(const spec_slot_args_t* a, void* ws, size_t ws_bytes, spec_stream_t stream) {
+  const spec_status_t st = check_slots(a);
+  if (st != SPEC_OK) return st;
+  if (bad_ws(ws)) return SPEC_ERR_INVALID_ARGUMENT;
+  if (ws_bytes < kWsHeader + kWsAlign) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  if (!scope.ok) return SPEC_ERR_CUDA;
+  return launch_map_slots(*a, static_cast<char*>(ws), s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+}
+
+spec_status_t spec_append_kv_fp8(const spec_append_fp8_args_t* a, spec_stream_t stream) {
+  const spec_status_t st = check_append(a);
+  if (st != SPEC_OK) return st;
+  if (a->rows == 0) return SPEC_OK;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  if (!scope.ok) return SPEC_ERR_CUDA;
+  return launch_append_fp8(*a, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+}
+
+size_t spec_attn_fp8_workspace_size(const spec_attn_fp8_args_t* a) {
+  if (check_attn_fp8(a) != SPEC_OK) return 0;
+  // the split count depends on the SM count: size for every device it may meet
+  int dev = 0, sms = 160;
+  if (cudaGetDevice(&dev) == cudaSuccess) {
+    const int n = device_sm_count(dev);
+    if (n > sms) sms = n;
+  } else {
+    cudaGetLastError();
+  }
+  size_t need = 0;
+  for (int s : {148, 152, sms}) {
+    const size_t x = attn_fp8_bytes(*a, s);
+    if (x > need) need = x;
+  }
+  return need;
+}
+
+spec_status_t spec_verify_attention_fp8(const spec_attn_fp8_args_t* a, void* ws, size_t ws_bytes,
+                                        spec_stream_t stream) {
+  const spec_status_t st = check_attn_fp8(a);
+  if (st != SPEC_OK) return st;
+  if (bad_ws(ws)) return SPEC_ERR_INVALID_ARGUMENT;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  if (!scope.ok) return SPEC_ERR_CUDA;
+  (void)cudaGetLastError();
+  const AttnFp8Plan P = attn_fp8_plan(*a, kWsHeader, scope.sms, a->path);
+  if (P.end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+  return launch_attn_fp8_simt(*a, P, static_cast<char*>(ws), s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+}
+
+spec_status_t spec_adjust_logits(const spec_adjust_args_t* a, spec_stream_t stream) {
+  const spec_status_t st = check_adjust(a);
+  if (st != SPEC_OK) return st;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  if (!scope.ok) return SPEC_ERR_CUDA;
+  return launch_adjust(*a, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,105 @@
+// Internal helpers of the attention kernels over the 8-bit cache: launch parameters, and
+// the merge of split-KV partials (each keeps an unnormalised fp32 output, its base-2
+// maximum m and its sum l).
+#pragma once
+
+#include "attn_common.cuh"
+#include "kv_fp8.cuh"
+
+namespace specv {
+
+// AttnParams with k_cache = the 8-bit cache (v_cache unused) and its scales.
+struct AttnFp8Params : AttnParams {
+  const float* kv_scale;  // [num_pages][Hkv][2]
+};
+
+inline AttnFp8Params make_attn_fp8_params(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws) {
+  AttnFp8Params p{};
+  p.batch = a.batch;
+  p.gamma = a.gamma;
+  p.hq = a.num_q_heads;
+  p.hkv = a.num_kv_heads;
+  p.hunits = a.num_kv_heads;
+  p.group = a.num_q_heads / a.num_kv_heads;
+  p.rows = P.rows;
+  p.row_tiles = P.row_tiles;
+  p.page_size = a.page_size;
+  p.max_pages = a.max_pages_per_seq;
+  p.num_pages = a.num_pages;
+  p.nsplit = P.nsplit;
+  p.tiles_per_split = P.tiles_per_split;
+  p.slot_rows = P.slot_rows;
+  p.max_keys = a.max_pages_per_seq * a.page_size;
+  const float scale = a.softmax_scale != 0.f ? a.softmax_scale : 1.f / sqrtf(static_cast<float>(a.head_dim));
+  p.scale_log2 = scale * kLog2e;
+  p.q = a.q;
+  p.k_cache = a.kv_cache;
+  p.kv_scale = a.kv_scale;
+  p.page_table = a.page_table;
+  p.kv_len = a.kv_len;
+  p.out = a.out;
+  p.lse = a.lse;
+  p.status = reinterpret_cast<uint32_t*>(ws);
+  p.tickets = reinterpret_cast<uint32_t*>(ws + P.tickets);
+  p.partial_o = reinterpret_cast<float*>(ws + P.partial_o);
+  p.partial_ml = reinterpret_cast<float2*>(ws + P.partial_ml);
+  p.tree_mask = a.tree_mask;
+  return p;
+}
+
+#ifdef __CUDACC__
+// 1 / l for a row's output: 0 for a bad sequence (l = -1) or a row that saw no key (l = 0);
+// NaN stays NaN.
+__device__ __forceinline__ float fp8_inv(float l) { return l <= 0.f ? 0.f : 1.f / l; }
+
+// lse of a row from its base-2 maximum and sum.
+__device__ __forceinline__ float fp8_lse(float m, float l) {
+  return l <= 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+__device__ __forceinline__ void write_fp8_lse(const AttnParams& p, int b, int g, int row, float m, float l) {
+  if (!p.lse) return;
+  const int j = row / p.group, h = g * p.group + row % p.group;
+  p.lse[(static_cast<int64_t>(b) * p.gamma + j) * p.hq + h] = fp8_lse(m, l);
+}
+
+// The partials of one unit in slots [slot0, slot0 + nslots): rows [row0, row0 + nrows) of
+// KV head g are merged and written, row r from slot row prow0 + r.
+template <int D>
+__device__ void merge_fp8_unit(const AttnParams& p, int b, int g, int row0, int nrows, int64_t slot0,
+                               int nslots, int tid, int nthreads, int prow0 = 0) {
+  constexpr int C8 = D / 8;
+  for (int idx = tid; idx < nrows * C8; idx += nthreads) {
+    const int r = idx / C8, c8 = idx % C8;
+    float M = -INFINITY, L = 0.f, acc[8];
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    for (int s = 0; s < nslots; ++s) {
+      const int64_t row = (slot0 + s) * p.slot_rows + prow0 + r;
+      const float2 ml = __ldcg(&p.partial_ml[row]);
+      const float4* src = reinterpret_cast<const float4*>(p.partial_o + row * D) + 2 * c8;
+      const float4 lo = __ldcg(src), hi = __ldcg(src + 1);
+      if (ml.y < 0.f) bad = true;
+      if (ml.y == 0.f) continue;
+      const float m = fmaxf(M, ml.x);
+      const float old = M == -INFINITY ? 0.f : ex2(M - m), w = m == -INFINITY ? ml.y : ex2(ml.x - m);
+      L = L * old + ml.y * w;
+      const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = acc[e] * old + x[e] * w;
+      M = m;
+    }
+    if (bad) L = -1.f;
+    const float inv = fp8_inv(L);
+    if (inv == 0.f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    }
+    write_out_row<D>(p, b, g, row0 + r, c8 * 8, acc, inv);
+    if (c8 == 0) write_fp8_lse(p, b, g, row0 + r, M, L);
+  }
+}
+#endif
+
+}  // namespace specv

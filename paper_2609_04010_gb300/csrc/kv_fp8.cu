@@ -1,0 +1,365 @@
+// The 8-bit KV cache: pages and slots for new tokens, and the quantising write of their
+// keys and values (spec_map_slots, spec_append_kv_fp8).
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "kv_fp8.cuh"
+
+namespace specv {
+namespace {
+
+// ---------------------------------------------------------------------------------
+// Pages and slots
+// ---------------------------------------------------------------------------------
+// Every block scans the whole batch (its request sizes and page needs) into shared memory
+// and then maps its share of the rows, so that one launch does what would otherwise take a
+// scan and a dependent expansion. No block waits: the state that may be updated in place
+// (kv_len, free_count) is written by the block that takes the last ticket, after every
+// block has read it. New pages are read from the free list, never from the table entries
+// that other blocks are writing.
+constexpr int kSlotThreads = 512;
+constexpr int kSlotRowsPerBlock = 4096;  // rows the grid is sized for, per block
+
+struct SlotParams {
+  spec_slot_args_t a;
+  uint32_t* ticket;
+};
+
+struct SeqSlots {
+  int32_t len;     // tokens held; -1: not served
+  int32_t first;   // table entry of its first new page
+  int32_t before;  // pages taken by earlier sequences
+};
+
+__device__ __forceinline__ int64_t block_excl_scan(int64_t x, int64_t* sh, int64_t* total) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  int64_t in = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, in, o);
+    if (lane >= o) in += y;
+  }
+  if (lane == 31) sh[w] = in;
+  __syncthreads();
+  if (w == 0) {
+    int64_t v = lane < kSlotThreads / 32 ? sh[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    if (lane < kSlotThreads / 32) sh[lane] = v;
+  }
+  __syncthreads();
+  const int64_t ex = (w > 0 ? sh[w - 1] : 0) + in - x;
+  *total = sh[kSlotThreads / 32 - 1];
+  __syncthreads();
+  return ex;
+}
+
+__global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  const spec_slot_args_t& a = p.a;
+  int32_t* start = reinterpret_cast<int32_t*>(smem_raw);                // [batch + 1]
+  SeqSlots* seq = reinterpret_cast<SeqSlots*>(start + a.batch + 1);      // [batch]
+  __shared__ int64_t sh[kSlotThreads / 32];
+  __shared__ int s_last, s_taken;
+  const int tid = threadIdx.x;
+  const int P = a.page_size, MP = a.max_pages_per_seq;
+  const int64_t cap = static_cast<int64_t>(MP) * P;
+  const int count0 = min(max(*a.free_count, 0), a.free_capacity);
+  if (tid == 0) s_taken = 0;
+  int64_t row_carry = 0, page_carry = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kSlotThreads) {
+    const int b = b0 + tid;
+    int len = -1, n = 0, need = 0, first = 0;
+    if (b < a.batch) {
+      n = a.num_new[b];
+      len = a.kv_len[b];
+      const bool fits = len >= 0 && n >= 0 && static_cast<int64_t>(len) + n <= cap;
+      if (fits) {
+        first = static_cast<int>((static_cast<int64_t>(len) + a.reserved + P - 1) / P);
+        need = max(0, (len + n + P - 1) / P - first);
+      } else {
+        len = -1;
+      }
+      n = max(n, 0);
+    }
+    int64_t rows, pages;
+    const int64_t r = row_carry + block_excl_scan(n, sh, &rows);
+    const int64_t before = page_carry + block_excl_scan(need, sh, &pages);
+    row_carry += rows;
+    page_carry += pages;
+    if (b < a.batch) {
+      start[b] = static_cast<int32_t>(min(r, static_cast<int64_t>(INT32_MAX)));
+      const bool served = len >= 0 && (need == 0 || before + need <= count0);
+      if (served && need > 0) atomicMax(&s_taken, static_cast<int>(before) + need);
+      seq[b] = {served ? len : -1, first, served ? static_cast<int32_t>(before) : 0};
+    }
+  }
+  if (tid == 0) start[a.batch] = static_cast<int32_t>(min(row_carry, static_cast<int64_t>(INT32_MAX)));
+  __syncthreads();
+  const int total = start[a.batch];
+
+  // rows past max_rows only put their new pages into the table
+  const int rows_end = max(total, a.max_rows);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kSlotThreads;
+  for (int64_t r64 = static_cast<int64_t>(blockIdx.x) * kSlotThreads + tid; r64 < rows_end; r64 += step) {
+    const int r = static_cast<int>(r64);
+    int slot = -1, pos = -1, b = -1;
+    if (r < total) {
+      int lo = 0, hi = a.batch;  // largest b with start[b] <= r
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= r) lo = mid; else hi = mid;
+      }
+      b = lo;
+      const SeqSlots s = seq[b];
+      const int i = r - start[b];
+      if (s.len >= 0) {
+        pos = s.len + i;
+        const int idx = pos / P;
+        int32_t* entry = a.page_table + static_cast<int64_t>(b) * MP + idx;
+        int page;
+        if (idx >= s.first) {
+          page = a.free_pages[count0 - 1 - s.before - (idx - s.first)];
+          if (pos % P == 0) *entry = page;  // the page's first token is new: first * P >= len
+        } else {
+          page = *entry;
+        }
+        if (page >= 0 && page < a.num_pages) slot = page * P + pos % P;
+      } else {
+        pos = a.kv_len[b] + i;
+      }
+    }
+    if (r >= a.max_rows) continue;
+    a.slots[r] = slot;
+    if (a.positions) a.positions[r] = pos;
+    if (a.row_seq) a.row_seq[r] = b;
+  }
+
+  // the last block to get here updates the state
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+    if (s_last) *p.ticket = 0;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  for (int b = tid; b < a.batch; b += kSlotThreads) {
+    const int len = a.kv_len[b], n = a.num_new[b];
+    const bool served = seq[b].len >= 0;
+    const bool fits = len >= 0 && n >= 0 && static_cast<int64_t>(len) + n <= cap;
+    a.new_len[b] = served ? len + n : len;
+    if (a.flags) a.flags[b] = served ? 0 : (fits ? 2 : 1);
+  }
+  for (int b = tid; b <= a.batch; b += kSlotThreads) a.row_start[b] = start[b];
+  if (tid == 0) *a.new_free_count = count0 - s_taken;
+}
+
+// ---------------------------------------------------------------------------------
+// Quantising write
+// ---------------------------------------------------------------------------------
+// A block takes kAppendRows rows of one KV head. A row that is the first of its page in
+// the window before it leads that page's rows; one warp per 16 places of the page (a group)
+// then holds the page's new keys or values in registers: one pass finds their largest
+// magnitude, from it the page's scale, and the same registers are rounded and stored.
+// HBM traffic is the new rows once and their 8-bit form once (a page whose scale grows is
+// read and written once more).
+constexpr int kAppendThreads = 256;
+constexpr int kAppendRows = 32;
+constexpr int kWin = SPEC_APPEND_WINDOW;
+
+struct AppendParams {
+  int rows, hkv, num_pages;
+  int64_t k_stride, v_stride;
+  const __nv_bfloat16* k;
+  const __nv_bfloat16* v;
+  const int32_t* slots;
+  uint8_t* cache;
+  float* scale;
+  uint32_t* status;
+};
+
+// The largest finite magnitude of two packed bf16 values, as its bits.
+__device__ __forceinline__ uint32_t finite_max2(uint32_t w, uint32_t m) {
+  const uint32_t a = w & 0x7fffu, b = (w >> 16) & 0x7fffu;
+  m = max(m, a < 0x7f80u ? a : 0u);
+  return max(m, b < 0x7f80u ? b : 0u);
+}
+
+template <int D, int P>
+__global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams p) {
+  constexpr int GW = P / 16;                        // warps per group
+  constexpr int GROUPS = kAppendThreads / 32 / GW;  // groups per block
+  constexpr int LPR = D / 8;                        // lanes per row of 8-element pieces
+  constexpr int RPI = 32 / LPR;                     // rows per warp and step
+  constexpr int STEPS = 16 / RPI;
+  __shared__ int32_t win[kAppendRows + 2 * kWin];   // slots of the rows around the block's
+  __shared__ int32_t leaders[kAppendRows];
+  __shared__ int nlead;
+  __shared__ int32_t row_of[GROUPS][P];             // row written to each place, or -1
+  __shared__ uint32_t amax[GROUPS][GW];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int r0 = blockIdx.x * kAppendRows, head = blockIdx.y;
+  const int64_t max_slot = static_cast<int64_t>(p.num_pages) * P;
+  if (tid == 0) nlead = 0;
+  for (int i = tid; i < kAppendRows + 2 * kWin; i += kAppendThreads) {
+    const int64_t r = static_cast<int64_t>(r0) - kWin + i;
+    int s = r >= 0 && r < p.rows ? p.slots[r] : -1;
+    if (s >= max_slot) {
+      if (p.status && head == 0 && i >= kWin && i < kWin + kAppendRows)
+        set_status(p.status, SPEC_FLAG_BAD_PAGE);
+      s = -1;
+    }
+    win[i] = s;
+  }
+  __syncthreads();
+  for (int i = warp; i < kAppendRows; i += kAppendThreads / 32) {
+    const int s = win[kWin + i];
+    if (s < 0) continue;  // warp-uniform
+    bool earlier = false;
+    for (int q = lane; q < kWin - 1; q += 32) {
+      const int t = win[i + 1 + q];
+      earlier |= t >= 0 && t / P == s / P;
+    }
+    if (!__any_sync(0xffffffffu, earlier) && lane == 0) leaders[atomicAdd(&nlead, 1)] = i;
+  }
+  __syncthreads();
+  const int items = nlead * 2;  // (leader, K or V)
+  const int group = warp / GW, gwarp = warp % GW;
+  const int sub = lane / LPR, piece = lane % LPR;
+  for (int it0 = 0; it0 < items; it0 += GROUPS) {
+    const int it = it0 + group;
+    const bool live = it < items;
+    const int li = live ? leaders[it >> 1] : 0, kind = it & 1;
+    const int page = live ? win[kWin + li] / P : 0;
+    for (int q = gwarp * 32 + lane; q < P; q += GW * 32) row_of[group][q] = -1;
+    __syncthreads();
+    if (live)
+      for (int q = gwarp * 32 + lane; q < kWin; q += GW * 32) {
+        const int s = win[kWin + li + q];
+        if (s >= 0 && s / P == page) row_of[group][s % P] = r0 + li + q;
+      }
+    __syncthreads();
+    uint4 x[STEPS];
+    uint32_t m = 0;
+    const __nv_bfloat16* src = kind ? p.v : p.k;
+    const int64_t stride = kind ? p.v_stride : p.k_stride;
+    uint32_t written = 0;
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int row = row_of[group][gwarp * 16 + i * RPI + sub];
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (row >= 0) {
+          written |= 1u << i;
+          x[i] = __ldg(reinterpret_cast<const uint4*>(src + row * stride + head * D + piece * 8));
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i)
+        m = finite_max2(x[i].w, finite_max2(x[i].z, finite_max2(x[i].y, finite_max2(x[i].x, m))));
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (GW > 1) {
+      if (lane == 0) amax[group][gwarp] = m;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < GW; ++w) m = max(m, amax[group][w]);
+    }
+    if (live) {
+      float* sp = p.scale + (static_cast<int64_t>(page) * p.hkv + head) * 2 + kind;
+      float sc = fp8_scale_of(m), grow = 1.f;
+      if (row_of[group][0] < 0) {  // the page goes on
+        const float old = clamp_scale(*sp);
+        if (old >= sc) sc = old;
+        else grow = old / sc;
+      }
+      const float inv = 1.f / sc;
+      uint8_t* dst = p.cache + ((static_cast<int64_t>(page) * p.hkv + head) * 2 + kind) * (P * D);
+      const bool anew = row_of[group][0] >= 0;
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        uint2* d = reinterpret_cast<uint2*>(dst + (gwarp * 16 + i * RPI + sub) * D + piece * 8);
+        if (written >> i & 1) {
+          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          uint32_t o[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[e] = to_e4m3x2(__uint_as_float(w[e] << 16) * inv, __uint_as_float(w[e] & 0xffff0000u) * inv);
+          *d = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+        } else if (!anew && grow != 1.f) {
+          const uint2 held = *d;
+          const uint32_t w[4] = {held.x & 0xffffu, held.x >> 16, held.y & 0xffffu, held.y >> 16};
+          uint32_t o[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = from_e4m3x2(w[e]);
+            o[e] = to_e4m3x2(f.x * grow, f.y * grow);
+          }
+          *d = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+        }
+      }
+    }
+    __syncthreads();  // every warp of the group has read the old scale
+    if (live && gwarp == 0 && lane == 0) {
+      float* sp = p.scale + (static_cast<int64_t>(page) * p.hkv + head) * 2 + kind;
+      float sc = fp8_scale_of(m);
+      if (row_of[group][0] < 0) sc = fmaxf(sc, clamp_scale(*sp));
+      *sp = sc;
+    }
+    __syncthreads();
+  }
+}
+
+template <int D>
+cudaError_t launch_append_d(const AppendParams& p, int page_size, cudaStream_t stream) {
+  const dim3 grid((p.rows + kAppendRows - 1) / kAppendRows, p.hkv);
+  if (page_size == 16) append_fp8_kernel<D, 16><<<grid, kAppendThreads, 0, stream>>>(p);
+  else if (page_size == 32) append_fp8_kernel<D, 32><<<grid, kAppendThreads, 0, stream>>>(p);
+  else append_fp8_kernel<D, 64><<<grid, kAppendThreads, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t slot_smem(int batch) { return (batch + 1) * 4 + batch * sizeof(SeqSlots); }
+
+cudaError_t launch_map_slots(const spec_slot_args_t& a, char* ws, cudaStream_t stream) {
+  SlotParams p{a, reinterpret_cast<uint32_t*>(ws + kWsHeader)};
+  const size_t smem = slot_smem(a.batch);
+  (void)cudaGetLastError();
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(
+        map_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+  }
+  const int grid = (a.max_rows - 1) / kSlotRowsPerBlock + 1;
+  map_slots_kernel<<<grid, kSlotThreads, smem, stream>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_append_fp8(const spec_append_fp8_args_t& a, cudaStream_t stream) {
+  AppendParams p;
+  const int64_t dense = static_cast<int64_t>(a.num_kv_heads) * a.head_dim;
+  p.rows = a.rows;
+  p.hkv = a.num_kv_heads;
+  p.num_pages = a.num_pages;
+  p.k_stride = a.k_row_stride ? a.k_row_stride : dense;
+  p.v_stride = a.v_row_stride ? a.v_row_stride : dense;
+  p.k = static_cast<const __nv_bfloat16*>(a.k);
+  p.v = static_cast<const __nv_bfloat16*>(a.v);
+  p.slots = a.slots;
+  p.cache = static_cast<uint8_t*>(a.kv_cache);
+  p.scale = a.kv_scale;
+  p.status = a.status;
+  (void)cudaGetLastError();
+  return a.head_dim == 128 ? launch_append_d<128>(p, a.page_size, stream)
+                           : launch_append_d<64>(p, a.page_size, stream);
+}
+
+}  // namespace specv
