@@ -630,8 +630,14 @@ spec_status_t spec_append_kv_fp8(const spec_append_fp8_args_t* append, spec_stre
  * scales are read clamped to [2^-32, 2^32]. A query row that sees no key (an empty tree
  * mask over an empty prefix) gets out = 0 and lse = -inf. What a row's mask hides (keys past
  * kv_len, or hidden block keys) does not reach it, whatever the bytes there. Scores,
- * softmax statistics and accumulators are fp32. path: SPEC_ATTN_AUTO or
- * SPEC_ATTN_CUDA_CORES. The workspace rules are spec_verify_attention's.
+ * softmax statistics and accumulators are fp32. On the tensor cores the queries and the
+ * weights enter as sums of two e4m3 terms, exact to 2^-18 of the largest |q| of up to 64
+ * rows of one KV head, and to 2^-8 of each weight.
+ * path: SPEC_ATTN_AUTO takes the tensor cores where the call fits them (the batch's prefix
+ * sums in a block's shared memory: batches up to 4,096; 32-bit counts of key tiles and
+ * cache rows), else CUDA cores; SPEC_ATTN_TENSOR_CORES is SPEC_ERR_UNSUPPORTED where it
+ * does not fit. The workspace rules
+ * are spec_verify_attention's.
  */
 typedef struct {
   int32_t batch;              /* >= 1                                                       */
@@ -643,7 +649,7 @@ typedef struct {
   int32_t max_pages_per_seq;
   int32_t num_pages;
   float softmax_scale;        /* 0 => 1/sqrt(head_dim)                                      */
-  int32_t path;               /* SPEC_ATTN_AUTO or SPEC_ATTN_CUDA_CORES                      */
+  int32_t path;               /* spec_attn_path_t, without KEYS_ON_LANES                    */
   const void* q;              /* bf16 [batch][gamma][Hq][D], 16-byte aligned                */
   const void* kv_cache;       /* as above                                                   */
   const float* kv_scale;      /* as above, 8-byte aligned                                   */
@@ -701,7 +707,7 @@ spec_status_t spec_adjust_logits(const spec_adjust_args_t* adjust, spec_stream_t
  *
  * The kernels' internal waits on asynchronous copies and tensor-core operations are
  * bounded (about 1 s of SM clock); one that runs out sets SPEC_FLAG_TIMEOUT, the block
- * releases its resources and returns, and the context stays usable. These two calls make
+ * releases its resources and returns, and the context stays usable. These calls make
  * that happen on purpose, so that it can be tested: each is the launch of its product
  * call (spec_verify_attention on the tensor-core row-tile path, spec_lm_head_stats), with
  * the same arguments, workspace rules and errors, except that the kernel's copy producer
@@ -710,10 +716,13 @@ spec_status_t spec_adjust_logits(const spec_adjust_args_t* adjust, spec_stream_t
  * SPEC_ERR_TIMEOUT and clears it), the outputs are undefined, and the workspace's
  * counters are still zero, so the same workspace serves the next product call.
  * spec_test_attention_wait_timeout returns SPEC_ERR_UNSUPPORTED for shapes the
- * tensor-core row-tile kernel does not take. Nothing traps, faults or waits without bound.
+ * tensor-core row-tile kernel does not take; spec_test_attention_fp8_wait_timeout does the
+ * same for spec_verify_attention_fp8 and its tensor-core kernel. Nothing traps, faults or waits without bound.
  * ------------------------------------------------------------------------------------- */
 spec_status_t spec_test_attention_wait_timeout(const spec_attn_args_t* attn, void* ws,
                                                size_t ws_bytes, spec_stream_t stream);
+spec_status_t spec_test_attention_fp8_wait_timeout(const spec_attn_fp8_args_t* attn, void* ws,
+                                                   size_t ws_bytes, spec_stream_t stream);
 spec_status_t spec_test_lm_head_wait_timeout(const spec_lm_head_args_t* lm, void* ws,
                                              size_t ws_bytes, spec_stream_t stream);
 

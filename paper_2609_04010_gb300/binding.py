@@ -236,7 +236,8 @@ def lib(build_if_missing: bool = True):
             for f in ("spec_append_kv_fp8", "spec_adjust_logits"):
                 getattr(L, f).argtypes = [P, P]
                 getattr(L, f).restype = ctypes.c_int
-            for f in ("spec_test_attention_wait_timeout", "spec_test_lm_head_wait_timeout"):
+            for f in ("spec_test_attention_wait_timeout", "spec_test_attention_fp8_wait_timeout",
+                      "spec_test_lm_head_wait_timeout"):
                 getattr(L, f).argtypes = [P, P, ctypes.c_size_t, P]
                 getattr(L, f).restype = ctypes.c_int
             for f in ("spec_workspace_init", "spec_verify_attention", "spec_accept_block",
@@ -857,6 +858,14 @@ def attn_fp8_workspace_size(a: AttnFp8Args) -> int:
 def verify_attention_fp8_args(a: AttnFp8Args, ws: torch.Tensor, stream=None):
     _raise(lib().spec_verify_attention_fp8(ctypes.byref(a), _ptr(ws), ws.numel(), _stream(stream)),
            "spec_verify_attention_fp8")
+
+
+def test_attention_fp8_wait_timeout_args(a: AttnFp8Args, ws: torch.Tensor, stream=None):
+    """Test hook: spec_verify_attention_fp8's tensor-core kernel with its copy producer idle,
+    so that its bounded waits run out (about 1 s) and it returns with SPEC_FLAG_TIMEOUT set."""
+    _raise(lib().spec_test_attention_fp8_wait_timeout(ctypes.byref(a), _ptr(ws), ws.numel(),
+                                                      _stream(stream)),
+           "spec_test_attention_fp8_wait_timeout")
 
 
 def verify_attention_fp8(q, kv_cache, kv_scale, page_table, kv_len, softmax_scale=0.0,

@@ -44,6 +44,13 @@ spec_status_t check_append(const spec_append_fp8_args_t* a) {
   return SPEC_OK;
 }
 
+// Two KV heads per block when each has at most 64 query rows: a page of both is one copy of
+// twice the size.
+int heads_per_block(const spec_attn_fp8_args_t& a) {
+  const int rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
+  return rows <= 64 && a.num_kv_heads % 2 == 0 ? 2 : 1;
+}
+
 spec_status_t check_attn_fp8(const spec_attn_fp8_args_t* a) {
   if (!a || a->batch < 1 || a->gamma < 1 || a->num_q_heads < 1 || a->num_kv_heads < 1 ||
       a->max_pages_per_seq < 1 || a->num_pages < 1 || a->page_size < 1 || a->head_dim < 1 ||
@@ -55,7 +62,8 @@ spec_status_t check_attn_fp8(const spec_attn_fp8_args_t* a) {
     return SPEC_ERR_INVALID_ARGUMENT;
   if (!(a->softmax_scale == 0.f || (a->softmax_scale > 0.f && a->softmax_scale < 1e30f)))
     return SPEC_ERR_INVALID_ARGUMENT;
-  if (a->path != SPEC_ATTN_AUTO && a->path != SPEC_ATTN_CUDA_CORES) return SPEC_ERR_INVALID_ARGUMENT;
+  if (a->path != SPEC_ATTN_AUTO && a->path != SPEC_ATTN_CUDA_CORES && a->path != SPEC_ATTN_TENSOR_CORES)
+    return SPEC_ERR_INVALID_ARGUMENT;
   if (a->gamma > 64 || !head_dim_ok(a->head_dim) || !page_size_ok(a->page_size))
     return SPEC_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(a->max_pages_per_seq) * a->page_size > (1 << 30) ||
@@ -63,7 +71,10 @@ spec_status_t check_attn_fp8(const spec_attn_fp8_args_t* a) {
     return SPEC_ERR_UNSUPPORTED;
   const int64_t rows = static_cast<int64_t>(a->num_q_heads / a->num_kv_heads) * a->gamma;
   const int64_t z = static_cast<int64_t>(a->batch) * ((rows + kSimtRowTile - 1) / kSimtRowTile);
-  if (z > 65535 || a->num_kv_heads > 65535) return SPEC_ERR_UNSUPPORTED;
+  const bool tc = attn_fp8_tc_fits(*a, heads_per_block(*a), static_cast<int>(rows));
+  if (a->path == SPEC_ATTN_TENSOR_CORES && !tc) return SPEC_ERR_UNSUPPORTED;
+  if ((a->path == SPEC_ATTN_CUDA_CORES || !tc) && (z > 65535 || a->num_kv_heads > 65535))
+    return SPEC_ERR_UNSUPPORTED;
   return SPEC_OK;
 }
 
@@ -83,6 +94,65 @@ spec_status_t check_adjust(const spec_adjust_args_t* a) {
 
 size_t attn_fp8_bytes(const spec_attn_fp8_args_t& a, int sms) {
   return attn_fp8_plan(a, kWsHeader, sms, a.path).end;
+}
+
+}  // namespace
+
+namespace specv {
+
+AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path) {
+  AttnFp8Plan P{};
+  P.rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
+  P.heads = heads_per_block(a);
+  P.path = path != SPEC_ATTN_CUDA_CORES && attn_fp8_tc_fits(a, P.heads, P.rows) ? SPEC_ATTN_TENSOR_CORES
+                                                                                : SPEC_ATTN_CUDA_CORES;
+  int64_t units;
+  if (P.path == SPEC_ATTN_TENSOR_CORES) {
+    // persistent grid; a unit has a slot of its own and one per block that starts inside it
+    P.row_tiles = (P.rows + kFp8MaxRows - 1) / kFp8MaxRows;
+    units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / P.heads) * P.row_tiles;
+    P.grid = num_sms;
+    P.nsplit = 1;
+    P.slot_rows = P.heads == 2 ? 2 * P.rows : (P.rows < kFp8MaxRows ? P.rows : kFp8MaxRows);
+    P.slots = units + P.grid;
+  } else {
+    P.row_tiles = (P.rows + kSimtRowTile - 1) / kSimtRowTile;
+    const int max_tiles = (a.max_pages_per_seq * a.page_size + kSimtKeyTile - 1) / kSimtKeyTile;
+    units = static_cast<int64_t>(a.batch) * a.num_kv_heads * P.row_tiles;
+    int64_t nsplit = static_cast<int64_t>(num_sms) * 4 / units;  // two blocks fit an SM
+    nsplit = nsplit < 1 ? 1 : (nsplit > max_tiles ? max_tiles : nsplit);
+    P.tiles_per_split = static_cast<int>((max_tiles + nsplit - 1) / nsplit);
+    P.nsplit = (max_tiles + P.tiles_per_split - 1) / P.tiles_per_split;
+    P.slot_rows = kSimtRowTile;
+    P.slots = P.nsplit > 1 ? units * P.nsplit : 0;
+  }
+  P.tickets = base;
+  P.partial_o = ws_round(P.tickets + sizeof(uint32_t) * units);
+  P.partial_ml = ws_round(P.partial_o + static_cast<size_t>(P.slots) * P.slot_rows * a.head_dim * 4);
+  P.end = ws_round(P.partial_ml + static_cast<size_t>(P.slots) * P.slot_rows * sizeof(float2));
+  return P;
+}
+
+}  // namespace specv
+
+namespace {
+
+spec_status_t run_attn_fp8(const spec_attn_fp8_args_t* a, void* ws, size_t ws_bytes, spec_stream_t stream,
+                           bool starve) {
+  const spec_status_t st = check_attn_fp8(a);
+  if (st != SPEC_OK) return st;
+  if (bad_ws(ws)) return SPEC_ERR_INVALID_ARGUMENT;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  if (!scope.ok) return SPEC_ERR_CUDA;
+  (void)cudaGetLastError();
+  const AttnFp8Plan P = attn_fp8_plan(*a, kWsHeader, scope.sms, a->path);
+  if (P.end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+  char* w = static_cast<char*>(ws);
+  if (P.path == SPEC_ATTN_TENSOR_CORES)
+    return launch_attn_fp8_tc(*a, P, w, s, starve) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+  if (starve) return SPEC_ERR_UNSUPPORTED;
+  return launch_attn_fp8_simt(*a, P, w, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }
 
 }  // namespace
@@ -134,16 +204,12 @@ size_t spec_attn_fp8_workspace_size(const spec_attn_fp8_args_t* a) {
 
 spec_status_t spec_verify_attention_fp8(const spec_attn_fp8_args_t* a, void* ws, size_t ws_bytes,
                                         spec_stream_t stream) {
-  const spec_status_t st = check_attn_fp8(a);
-  if (st != SPEC_OK) return st;
-  if (bad_ws(ws)) return SPEC_ERR_INVALID_ARGUMENT;
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  DeviceScope scope(s);
-  if (!scope.ok) return SPEC_ERR_CUDA;
-  (void)cudaGetLastError();
-  const AttnFp8Plan P = attn_fp8_plan(*a, kWsHeader, scope.sms, a->path);
-  if (P.end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
-  return launch_attn_fp8_simt(*a, P, static_cast<char*>(ws), s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+  return run_attn_fp8(a, ws, ws_bytes, stream, false);
+}
+
+spec_status_t spec_test_attention_fp8_wait_timeout(const spec_attn_fp8_args_t* a, void* ws, size_t ws_bytes,
+                                                   spec_stream_t stream) {
+  return run_attn_fp8(a, ws, ws_bytes, stream, true);
 }
 
 spec_status_t spec_adjust_logits(const spec_adjust_args_t* a, spec_stream_t stream) {

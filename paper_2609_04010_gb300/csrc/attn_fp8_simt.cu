@@ -215,27 +215,6 @@ cudaError_t launch_simt_d(const AttnFp8Params& p, const dim3& grid, cudaStream_t
 
 }  // namespace
 
-AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path) {
-  AttnFp8Plan P{};
-  P.rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
-  P.path = SPEC_ATTN_CUDA_CORES;
-  (void)path;
-  P.row_tiles = (P.rows + RT - 1) / RT;
-  const int max_tiles = (a.max_pages_per_seq * a.page_size + TK - 1) / TK;
-  const int64_t units = static_cast<int64_t>(a.batch) * a.num_kv_heads * P.row_tiles;
-  int64_t nsplit = static_cast<int64_t>(num_sms) * 4 / units;  // two blocks fit an SM
-  nsplit = nsplit < 1 ? 1 : (nsplit > max_tiles ? max_tiles : nsplit);
-  P.tiles_per_split = static_cast<int>((max_tiles + nsplit - 1) / nsplit);
-  P.nsplit = (max_tiles + P.tiles_per_split - 1) / P.tiles_per_split;
-  P.slot_rows = RT;
-  P.slots = P.nsplit > 1 ? units * P.nsplit : 0;
-  P.tickets = base;
-  P.partial_o = ws_round(P.tickets + sizeof(uint32_t) * units);
-  P.partial_ml = ws_round(P.partial_o + static_cast<size_t>(P.slots) * P.slot_rows * a.head_dim * 4);
-  P.end = ws_round(P.partial_ml + static_cast<size_t>(P.slots) * P.slot_rows * sizeof(float2));
-  return P;
-}
-
 cudaError_t launch_attn_fp8_simt(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
                                  cudaStream_t stream) {
   const AttnFp8Params p = make_attn_fp8_params(a, P, ws);

@@ -2,7 +2,7 @@
 
 Tolerances. With s the scores, p the weights and o the outputs:
   * a query enters a tensor-core score as the sum of two e4m3 terms, exact to 2^-18 of the
-    row's largest |q|, and a score is an fp32 sum of at most 128 products; so
+    largest |q| of its KV group, and a score is an fp32 sum of at most 128 products; so
     |ds| <= scale * kmax * (2^-18 + 128 * 2^-24) * max|q|, kmax = max_t sum_d |k_td|;
   * a weight enters as two e4m3 terms, exact to 2^-8 of itself, or to 2^-13 of the row's
     largest weighted value 2^m where it is small; ds moves it by another (e^|2 ds| - 1);
@@ -19,8 +19,8 @@ import fp8_reference as ref
 
 pytestmark = pytest.mark.gpu
 
-CUDA_CORES = 1
-PATHS = [CUDA_CORES]
+CUDA_CORES, TENSOR_CORES = 1, 2
+PATHS = [CUDA_CORES, TENSOR_CORES]
 
 
 def i32(a):
@@ -82,7 +82,10 @@ class Case:
         ro, rl, mass, kmax = ref.attention(q, self.codes, self.scale, self.table, self.kv_len,
                                            self.G, self.P, softmax_scale, self.tree)
         sc = softmax_scale or q.shape[-1] ** -0.5
-        ds = (sc * kmax * (2.0 ** -18 + 128 * 2.0 ** -24) * np.abs(q).max(-1))[..., None]
+        B, G, Hq, _ = q.shape
+        H = self.codes.shape[1]
+        qmax = np.repeat(np.abs(q).reshape(B, G, H, -1).max((1, 3)), Hq // H, 1)[:, None]
+        ds = (sc * kmax * (2.0 ** -18 + 128 * 2.0 ** -24) * qmax)[..., None]
         used = self.codes[(self.codes & 0x7f) != 0x7f]
         vmax = np.abs(ref.decode(used)).max() * np.clip(self.scale[:, :, 1], 2.0 ** -32, 2.0 ** 32).max()
         tol = (2.0 ** -8 + 2 * ds) * mass + 2.0 ** -12 * vmax + 2.0 ** -9 * np.abs(ro) + 1e-30
@@ -294,3 +297,23 @@ def test_no_lse_and_auto():
     o2, _ = b.verify_attention_fp8(*t)
     assert l is None and torch.equal(o, o2)
     c.check(0)
+
+
+def test_wait_timeout_is_reported_and_survived():
+    """The kernel with an idle copy producer: its bounded waits run out, it reports, and the
+    same workspace serves the next call."""
+    from paper_2609_04010_gb300 import binding as b
+    c = Case(3, 4, 8, 2, 128, 16, [300, 5, 1000], seed=8)
+    want = c.run(TENSOR_CORES)
+    t, _ = c.device()
+    out, lse = torch.zeros_like(t[0]), torch.zeros(t[0].shape[:3], device="cuda")
+    a = b.attn_fp8_args(*t, out, lse, path=TENSOR_CORES)
+    ws = b.new_workspace(b.attn_fp8_workspace_size(a))
+    b.test_attention_fp8_wait_timeout_args(a, ws)
+    assert b.read_device_status(ws) == (6, b.FLAG_TIMEOUT)
+    assert int(ws[256:256 + 64].sum()) == 0
+    b.verify_attention_fp8_args(a, ws)
+    torch.cuda.synchronize()
+    assert b.read_device_status(ws) == (0, 0)
+    assert np.array_equal(out.float().cpu().numpy().astype(np.float64), want[0])
+    assert np.array_equal(lse.cpu().numpy().astype(np.float64), want[1])
