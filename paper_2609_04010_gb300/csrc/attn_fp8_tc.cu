@@ -16,8 +16,9 @@
 // With sk, sv the scales of a key's page, m_r the row's reference and the weights
 //   P = 2^(s + log2(sv) - m_r),  s = sk * S^T * softmax_scale * log2(e),
 // O^T accumulates the weighted values with their scales, and sum P / sv is the softmax sum.
-// m_r is chosen so that 32 <= the row's largest P <= 256 and rises only when P would pass
-// 256 (e4m3 ends at 448), which after a unit's first tile is rare.
+// m_r is chosen so that 4 <= the row's largest P <= 256 and rises only when P would pass 256
+// (e4m3 ends at 448), which after a unit's first tile is rare. The second term of P is kept
+// times 16, which puts its smallest step at 2^-13.
 //
 // A block serves NH = 2 (or 1) sub-units of at most 64 query rows: two adjacent KV heads
 // (HP = 2, one box brings K and V of both: 8 KB with 16-token pages and D = 128), or two
@@ -25,7 +26,7 @@
 //   warp 0       producer: page ids and scales 32 pages ahead, one TMA box per page
 //   warp 1       issues S^T = K Q^T into a ring of four S buffers in TMEM
 //   warp 3       issues O^T += V^T P^T; clears V of keys past the sequence's end
-//   warps 4..11  softmax: lane quadrant = 32 keys, two warps per quadrant share the rows;
+//   warps 4..    softmax: lane quadrant = 32 keys, NG warps per quadrant share the rows;
 //                they also convert Q and write the outputs
 // The tiles of all units form one list that is cut into equal ranges, one per block; a unit
 // split between blocks is merged from fp32 partials by the last block to finish it (atomic
@@ -47,7 +48,8 @@ constexpr int TK = kFp8KeyTile;  // keys per tile
 template <int D, int HP, int NH, int NR>
 struct Cfg {
   static_assert(HP <= NH, "two heads are two sub-units");
-  static constexpr int NC = NR / 2;                        // rows per softmax warp
+  static constexpr int NC = NR == 64 ? 16 : 8;             // rows per softmax warp
+  static constexpr int NG = NR / NC;                       // softmax warps per lane quadrant
   static constexpr uint32_t ATOM = 8 * D;                  // 8 rows of D bytes, swizzled
   static constexpr uint32_t SG = 2 * HP * ATOM;            // 8-key group: K, V of each head
   static constexpr uint32_t STAGE = (TK / 8) * SG;
@@ -61,23 +63,28 @@ struct Cfg {
   static constexpr uint32_t OFF_Q = OFF_P + NH * PB * P_BUF;
   static constexpr uint32_t OFF_SCL = OFF_Q + NH * 2 * Q_TERM;     // float4 [NST][8 pages][HP]
   static constexpr uint32_t OFF_NAN = OFF_SCL + NST * 8 * HP * 16;  // uint64 [HP][D]: NaN block values
-  static constexpr uint32_t OFF_VIS = OFF_NAN + HP * D * 8;        // uint64 [NH][NR]: visible block keys
-  static constexpr uint32_t OFF_M = OFF_VIS + NH * NR * 8;         // float [NH][NR]
-  static constexpr uint32_t OFF_X = OFF_M + NH * NR * 4;           // float [NH][4][NR]: cross-quadrant
-  static constexpr uint32_t OFF_BAR = OFF_X + NH * 4 * NR * 4;
+  // of the current and the next segment: the block keys each row sees, the rows that see
+  // each block key, the rows' references
+  static constexpr uint32_t OFF_VIS = OFF_NAN + HP * D * 8;           // uint64 [2][NH][NR]
+  static constexpr uint32_t OFF_SEEN = OFF_VIS + 2 * NH * NR * 8;     // uint32 [2][NH][NG][64]
+  static constexpr uint32_t OFF_M = OFF_SEEN + 2 * NH * NG * 64 * 4;  // float [2][NH][NR]
+  static constexpr uint32_t OFF_X = OFF_M + 2 * NH * NR * 4;          // float [NH][4][NR]: cross-quadrant
+  static constexpr uint32_t OFF_ROW = OFF_X + NH * 4 * NR * 4;        // int64 [NH][NR]: rows' outputs
+  static constexpr uint32_t OFF_INV = OFF_ROW + NH * NR * 8;          // float [NH][NR]: their factors
+  static constexpr uint32_t OFF_BAR = OFF_INV + NH * NR * 4;
   // full[NST], empty[NST], s_full[SB], s_free[SB], p_full[NH*PB], pv_done[NH*PB], seg_ready,
   // drain[2], flag_ready[8]
   static constexpr int NBAR = 2 * NST + 2 * SB + 2 * NH * PB + 1 + 2 + 8;
   static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, pending, NaN flag
   static constexpr uint32_t OFF_FLAG = OFF_MISC + 16;       // int [8]: bad flags of segments
   static constexpr uint32_t OFF_PEND = OFF_FLAG + 32;       // int [2][8]
-  static constexpr uint32_t OFF_QMAX = OFF_PEND + 64;       // uint32 [NH][8]
-  static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 32;    // int [batch + 1]
+  static constexpr uint32_t OFF_QMAX = OFF_PEND + 64;       // uint32 [NH][16]
+  static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 64;    // int [batch + 1]
   static constexpr uint32_t S_COL = 0;
   static constexpr uint32_t O_COL = SB * NR;
   static constexpr uint32_t TMEM_COLS = (SB + 2 * NH) * NR <= 128 ? 128 : ((SB + 2 * NH) * NR <= 256 ? 256 : 512);
   static_assert((SB + 2 * NH) * NR <= 512, "TMEM holds 512 columns");
-  static constexpr int THREADS = 384;
+  static constexpr int THREADS = 128 + 128 * NG;
   static size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
 };
 
@@ -124,15 +131,8 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
 }
 template <int N>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* r) {
-  if constexpr (N == 32) tmem_ld32(taddr, r);
-  else if constexpr (N == 16) tmem_ld16(taddr, r);
+  if constexpr (N == 16) tmem_ld16(taddr, r);
   else tmem_ld8(taddr, r);
-}
-template <int N>
-__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t* r) {
-  if constexpr (N == 32) tmem_st32(taddr, r);
-  else if constexpr (N == 16) tmem_st16(taddr, r);
-  else tmem_st8(taddr, r);
 }
 // Named barrier of the four softmax warps that share a set of rows; or-reduces `v`.
 __device__ __forceinline__ bool group_any(int id, bool v) {
@@ -172,12 +172,13 @@ __device__ __forceinline__ float sum_columns(float* v, int lane) {
 }
 // The warp's largest x (NaN ignored).
 __device__ __forceinline__ float warp_max(float x) {
-  int i = __float_as_int(x == x ? x : -INFINITY);
-  i ^= (i >> 31) & 0x7fffffff;
-  i = __reduce_max_sync(0xffffffffu, i);
-  return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
 }
-// The two terms of a pair of values, each term packed with a's in the low byte.
+// The two terms of a pair of values, each term packed with a's in the low byte; UP: the
+// second term times 16.
+template <bool UP>
 __device__ __forceinline__ void split_e4m3x2(float a, float b, uint32_t& hi, uint32_t& lo) {
   hi = to_e4m3x2(a, b);
   uint32_t x;
@@ -185,6 +186,7 @@ __device__ __forceinline__ void split_e4m3x2(float a, float b, uint32_t& hi, uin
   const uint32_t h = e4m3x2_to_f16x2(hi);
   uint32_t d;
   asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(h));
+  if (UP) asm("mul.f16x2 %0, %1, %2;" : "=r"(d) : "r"(d), "r"(0x4c004c00u));
   uint16_t l;
   asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(l) : "r"(d));
   lo = l;
@@ -196,10 +198,10 @@ constexpr float kNoKey = -1e30f;  // a row's reference before it has seen a key
 // The kernel
 // ---------------------------------------------------------------------------------
 template <int D, int HP, int NH, int NR>
-__global__ void __launch_bounds__(384, 1)
+__global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
     attn_fp8_tc_kernel(const __grid_constant__ CUtensorMap tmap, AttnFp8Params p) {
   using C = Cfg<D, HP, NH, NR>;
-  constexpr int NC = C::NC, NST = C::NST, PB = C::PB, SB = C::SB;
+  constexpr int NC = C::NC, NG = C::NG, NST = C::NST, PB = C::PB, SB = C::SB;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -216,8 +218,6 @@ __global__ void __launch_bounds__(384, 1)
   auto flag_bar = [&](int i) { return seg_ready + 24 + 8u * i; };
   float4* scl = reinterpret_cast<float4*>(smem + C::OFF_SCL);
   unsigned long long* nanv = reinterpret_cast<unsigned long long*>(smem + C::OFF_NAN);
-  unsigned long long* vis = reinterpret_cast<unsigned long long*>(smem + C::OFF_VIS);
-  float* mref = reinterpret_cast<float*>(smem + C::OFF_M);
   float* xch = reinterpret_cast<float*>(smem + C::OFF_X);
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(384, 1)
   const int tile_rows = HP == 2 ? NR : NH * NR;
   // softmax warps whose rows are all padding take no part
   const int max_rows = min(p.rows, NR);
-  const int ngroup = max_rows > NC ? 2 : 1;
+  const int ngroup = (max_rows + NC - 1) / NC;
   const int nsoft = 4 * ngroup;
 
   if (threadIdx.x == 0) {
@@ -506,9 +506,11 @@ __global__ void __launch_bounds__(384, 1)
   } else if (warp >= 4 && (warp - 4) / 4 < ngroup) {
     // ============================ softmax ============================
     const int q4 = (warp - 4) & 3, ch = (warp - 4) >> 2;  // 32 keys; rows [ch * NC, + NC)
-    const int gbar = 1 + ch;                              // named barrier of this row group
-    const int stid = threadIdx.x - 128;                   // thread among the softmax warps
+    const int gbar = 2 + ch;                              // named barrier of this row group
+    const int nthr = nsoft * 32, stid = threadIdx.x - 128;  // threads of all groups
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
+    const int psh = __ffs(p.page_size) - 1;
+    const int pg = (q4 * 32 + lane) >> psh;  // this lane's page of a tile
     uint32_t it = 0, seg_no = 0;
     bool dead = false;  // after a timeout: run on without waiting
     auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -516,97 +518,117 @@ __global__ void __launch_bounds__(384, 1)
       const bool ok = mbar_wait(bar, parity, abort_flag, p.status);
       dead = !__all_sync(0xffffffffu, ok);
     };
-    for (Seg s = locate<TK>(t0, t1, p, pb, OVH); s.ntile > 0; ++seg_no) {
-      const int row_base = s.rt * tile_rows;
-      // rows of sub-unit h: unit row of its row r, and how many are real
-      auto unit_row = [&](int h, int r) { return row_base + (HP == 2 ? 0 : h * NR) + r; };
-      auto real_rows = [&](int h) { return min(NR, p.rows - unit_row(h, 0)); };
-      const int ctx = s.kv_len - p.gamma;
-      // ---- Q: the group's largest finite magnitude, then its two terms ----
-      float qf[NH];
-      {
-        constexpr int kPieces = D / 16;  // 16 elements per piece: 32 B in, 16 B per term
-        constexpr int kItems = NR * kPieces > 256 ? NR * kPieces / 256 : 1;  // NR > 16 has 256 threads
-        const int nthr = nsoft * 32;
-        uint4 x[NH][kItems][2];
+    // per-segment state, by the segment's parity
+    auto vis_of = [&](uint32_t par) { return reinterpret_cast<unsigned long long*>(smem + C::OFF_VIS) + par * NH * NR; };
+    auto seen_of = [&](uint32_t par) { return reinterpret_cast<uint32_t*>(smem + C::OFF_SEEN) + par * NH * NG * 64; };
+    auto mref_of = [&](uint32_t par) { return reinterpret_cast<float*>(smem + C::OFF_M) + par * NH * NR; };
+    // rows of sub-unit h: the unit row of its row r, and how many are real
+    auto unit_row = [&](const Seg& sg, int h, int r) { return sg.rt * tile_rows + (HP == 2 ? 0 : h * NR) + r; };
+    auto real_rows = [&](const Seg& sg, int h) { return min(NR, p.rows - unit_row(sg, h, 0)); };
+
+    // Brings a segment's Q into shared memory as two e4m3 terms, scaled by the power of two
+    // that takes the sub-unit's largest finite magnitude into (224, 448], and sets its
+    // row state. Returns the scales in qf.
+    auto start_segment = [&](const Seg& sg, uint32_t par, float* qf) {
+      constexpr int kPieces = D / 16;  // 16 elements per piece: 32 B in, 16 B per term
+      constexpr int kTotal = NR * kPieces;
+      constexpr int kLoops = NR == 64 ? (kTotal + 383) / 384 : 1;  // rows 33.. and 17.. have 384 threads
+      uint4 x[NH][kLoops][2];
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          uint32_t mx = 0;
+      for (int h = 0; h < NH; ++h) {
 #pragma unroll
-          for (int i = 0; i < kItems; ++i) {
-            const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
-            x[h][i][0] = x[h][i][1] = make_uint4(0, 0, 0, 0);
-            if (r < real_rows(h)) {
-              const int ur = unit_row(h, r), j = ur / p.group;
-              const int head = (s.g * HP + (HP == 2 ? h : 0)) * p.group + ur % p.group;
-              const uint4* src = reinterpret_cast<const uint4*>(
-                  static_cast<const __nv_bfloat16*>(p.q) +
-                  ((static_cast<int64_t>(s.b) * p.gamma + j) * p.hq + head) * D + piece * 16);
-              x[h][i][0] = __ldg(src);
-              x[h][i][1] = __ldg(src + 1);
-            }
+        for (int i = 0; i < kLoops; ++i) {
+          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+          x[h][i][0] = x[h][i][1] = make_uint4(0, 0, 0, 0);
+          if (r < real_rows(sg, h)) {
+            const int ur = unit_row(sg, h, r), j = ur / p.group;
+            const int head = (sg.g * HP + (HP == 2 ? h : 0)) * p.group + ur - j * p.group;
+            const uint4* src = reinterpret_cast<const uint4*>(
+                static_cast<const __nv_bfloat16*>(p.q) +
+                ((static_cast<int64_t>(sg.b) * p.gamma + j) * p.hq + head) * D + piece * 16);
+            x[h][i][0] = __ldg(src);
+            x[h][i][1] = __ldg(src + 1);
           }
-#pragma unroll
-          for (int i = 0; i < kItems; ++i)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t w[4] = {x[h][i][e].x, x[h][i][e].y, x[h][i][e].z, x[h][i][e].w};
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const uint32_t a = w[c] & 0x7fffu, b = (w[c] >> 16) & 0x7fffu;
-                mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
-              }
-            }
-          mx = __reduce_max_sync(0xffffffffu, mx);
-          if (lane == 0) qmax[h * 8 + warp - 4] = mx;
         }
-        bar_sync(3, nthr);
+      }
+      // meanwhile the rows' visible block keys, and the rows that see each block key
+      const unsigned long long all = p.gamma >= 64 ? ~0ull : (1ull << p.gamma) - 1;
+      unsigned long long* vis = vis_of(par);
+      for (int i = stid; i < NH * NR; i += nthr) {
+        const int h = i / NR, r = i % NR;
+        const int j = min(unit_row(sg, h, r), p.rows - 1) / p.group;
+        vis[i] = all & (p.tree_mask ? __ldg(p.tree_mask + static_cast<int64_t>(sg.b) * p.gamma + j) : (2ull << j) - 1);
+        mref_of(par)[i] = kNoKey;
+      }
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          uint32_t mx = 0;
-          for (int w = 0; w < nsoft; ++w) mx = max(mx, qmax[h * 8 + w]);
-          // the power of two that brings the largest magnitude into (224, 448]
-          const int e = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
-          qf[h] = __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
-          const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+      for (int h = 0; h < NH; ++h) {
+        uint32_t mx = 0;
 #pragma unroll
-          for (int i = 0; i < kItems; ++i) {
-            const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
-            if (r >= NR) continue;
-            uint32_t t1w[4], t2w[4];
+        for (int i = 0; i < kLoops; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t w[4] = {x[h][i][e].x, x[h][i][e].y, x[h][i][e].z, x[h][i][e].w};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const uint4 u = x[h][i][c >> 1];
-              const uint32_t w[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
-              uint32_t a[2], b[2];
-#pragma unroll
-              for (int d = 0; d < 2; ++d) {
-                float lo = __uint_as_float(w[d] << 16) * inv, hi = __uint_as_float(w[d] & 0xffff0000u) * inv;
-                lo = fabsf(lo) < INFINITY ? lo : __int_as_float(0x7fc00000);  // an infinite query is NaN
-                hi = fabsf(hi) < INFINITY ? hi : __int_as_float(0x7fc00000);
-                split_e4m3x2(lo, hi, a[d], b[d]);
-              }
-              t1w[c] = a[0] | a[1] << 16;
-              t2w[c] = b[0] | b[1] << 16;
+              const uint32_t a = w[c] & 0x7fffu, b = (w[c] >> 16) & 0x7fffu;
+              mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
             }
-            const int ph = D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3);
-            unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + r * D + ph * 16;
-            *reinterpret_cast<uint4*>(dst) = make_uint4(t1w[0], t1w[1], t1w[2], t1w[3]);
-            *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
           }
-        }
-        // the rows' visible block keys and references
-        for (int i = stid; i < NH * NR; i += nthr) {
-          const int h = i / NR, r = i % NR;
-          const int j = min(unit_row(h, r), p.rows - 1) / p.group;
-          const unsigned long long all = p.gamma >= 64 ? ~0ull : (1ull << p.gamma) - 1;
-          vis[i] = all & (p.tree_mask ? __ldg(p.tree_mask + static_cast<int64_t>(s.b) * p.gamma + j) : (2ull << j) - 1);
-          mref[i] = kNoKey;
-        }
-        fence_async_smem();
-        bar_sync(3, nthr);  // vis and mref are set
-        if (lane == 0) mbar_arrive(seg_ready);
+        mx = __reduce_max_sync(0xffffffffu, mx);
+        if (lane == 0) qmax[h * 16 + warp - 4] = mx;
       }
+      bar_sync(1, nthr);
+      for (int i = warp - 4; i < NH * ngroup * 64; i += nsoft) {  // lane = row of the group
+        const int key = i & 63, hg = i >> 6, h = hg / ngroup, g = hg - h * ngroup;
+        const bool v = lane < NC && (vis[h * NR + g * NC + (lane & (NC - 1))] >> key & 1);
+        const uint32_t m = __ballot_sync(0xffffffffu, v);
+        if (lane == 0) seen_of(par)[(h * NG + g) * 64 + key] = m;
+      }
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        uint32_t mx = 0;
+        for (int w = 0; w < nsoft; ++w) mx = max(mx, qmax[h * 16 + w]);
+        const int e = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
+        qf[h] = __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+        const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+#pragma unroll
+        for (int i = 0; i < kLoops; ++i) {
+          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+          if (r >= NR) continue;
+          uint32_t t1w[4], t2w[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint4 u = x[h][i][c >> 1];
+            const uint32_t w[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
+            uint32_t a[2], b[2];
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+              float lo = __uint_as_float(w[d] << 16) * inv, hi = __uint_as_float(w[d] & 0xffff0000u) * inv;
+              lo = fabsf(lo) < INFINITY ? lo : __int_as_float(0x7fc00000);  // an infinite query is NaN
+              hi = fabsf(hi) < INFINITY ? hi : __int_as_float(0x7fc00000);
+              split_e4m3x2<false>(lo, hi, a[d], b[d]);
+            }
+            t1w[c] = a[0] | a[1] << 16;
+            t2w[c] = b[0] | b[1] << 16;
+          }
+          const int ph = D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3);
+          unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + r * D + ph * 16;
+          *reinterpret_cast<uint4*>(dst) = make_uint4(t1w[0], t1w[1], t1w[2], t1w[3]);
+          *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
+        }
+      }
+      fence_async_smem();
+      bar_sync(1, nthr);  // the row state is set
+      if (lane == 0) mbar_arrive(seg_ready);
+    };
+
+    Seg s = locate<TK>(t0, t1, p, pb, OVH);
+    float qf[NH];
+    if (s.ntile > 0) start_segment(s, 0, qf);
+    while (s.ntile > 0) {
+      const uint32_t par = seg_no & 1;
+      const int ctx = s.kv_len - p.gamma;
+      float* mref = mref_of(par);
       float l[NH][NC];
 #pragma unroll
       for (int h = 0; h < NH; ++h)
@@ -615,9 +637,9 @@ __global__ void __launch_bounds__(384, 1)
 
       for (int k = 0; k < s.ntile; ++k) {
         const uint32_t x = it + k, st = x % NST;
-        const int key0 = (s.tile0 + k) * TK, key = key0 + q4 * 32 + lane;
+        const int key0 = (s.tile0 + k) * TK;
         const bool masked = key0 + TK > ctx;
-        const int pg = (q4 * 32 + lane) / p.page_size;
+        const int rel = key0 + q4 * 32 + lane - ctx;  // block position (negative: the prefix)
         const int buf = static_cast<int>(x % PB);
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
@@ -630,46 +652,41 @@ __global__ void __launch_bounds__(384, 1)
           if (h == 0) wait(full(st), (x / NST) & 1);  // orders the producer's scales before this
           const float4 sc = scl[(st * 8 + pg) * HP + (HP == 2 ? h : 0)];
           const float ks = sc.x * qf[h];
-          tmem_wait_ld();
-          // e = log2 of the key's weighted value for each row; hidden keys have none
-          float e[NC];
-          auto exponents = [&]() {
-#pragma unroll
-            for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(raw[c]), ks, sc.y);
-            if (masked) {
-              const int rel = key - ctx;
-#pragma unroll
-              for (int c = 0; c < NC; ++c) {
-                const bool see = rel < 0 || (rel < 64 && (vis[h * NR + ch * NC + c] >> (rel & 63) & 1));
-                e[c] = see ? e[c] : -INFINITY;
-              }
-            }
-          };
-          exponents();
+          // e = log2 of the key's weight and value scale for each row, over the row's
+          // reference; hidden keys have none
           const float* mr = mref + h * NR + ch * NC;
-          float top = -INFINITY;
+          uint32_t seen = ~0u;
+          if (masked && rel >= 0) seen = rel < 64 ? seen_of(par)[(h * NG + ch) * 64 + rel] : 0u;
+          float e[NC];
+          for (bool raised = false;; raised = true) {
+            tmem_wait_ld();
+            float top = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            e[c] -= mr[c];
-            top = fmaxf(top, e[c]);
-          }
-          if (group_any(gbar, top > 8.f)) {
-            // some weight would pass 256: raise the references of the rows concerned
+            for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(raw[c]), ks, sc.y) - mr[c];
+            if (masked) {
+#pragma unroll
+              for (int c = 0; c < NC; ++c) e[c] = (seen >> c & 1) ? e[c] : -INFINITY;
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) top = fmaxf(top, e[c]);
+            if (raised || !group_any(gbar, top > 8.f)) break;
+            // Some weight would pass 2^8: raise the references, so that each row's largest
+            // weight so far becomes 2^2 where it was more.
+            float* xc = xch + h * 4 * NR;
+            float mx = -INFINITY;
             tmem_ld<NC>(s_tmem, raw);
             tmem_wait_ld();
-            exponents();
-            float mx = -INFINITY;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-              const float m = warp_max(e[c]);
+              const float v = fmaf(__uint_as_float(raw[c]), ks, sc.y);
+              const float m = warp_max((seen >> c & 1) ? v : -INFINITY);
               if (lane % NC == c) mx = m;
             }
-            float* xc = xch + h * 4 * NR;
             if (lane < NC) xc[q4 * NR + ch * NC + lane] = mx;
             bar_sync(gbar, 128);
             const int c0 = ch * NC + lane % NC;
             const float old = mref[h * NR + c0];
-            mx = fmaxf(fmaxf(xc[c0], xc[NR + c0]), fmaxf(xc[2 * NR + c0], xc[3 * NR + c0])) - 5.f;
+            mx = fmaxf(fmaxf(xc[c0], xc[NR + c0]), fmaxf(xc[2 * NR + c0], xc[3 * NR + c0])) - 2.f;
             const float now = fmaxf(old, mx);
             const float alpha = ex2(old - now);
             bar_sync(gbar, 128);
@@ -677,23 +694,23 @@ __global__ void __launch_bounds__(384, 1)
             if (k > 0) {  // O holds every earlier tile before it is scaled
               wait(pv_done(h, (x - 1) % PB), ((x - 1) / PB) & 1);
               tc_fence_after();
-#pragma unroll
-              for (int t = 0; t < 2; ++t) {
-                const uint32_t col = lane_base + C::O_COL + (h * 2 + t) * NR + ch * NC;
-                tmem_ld<NC>(col, raw);
+#pragma unroll 1
+              for (int c8 = 0; c8 < 2 * NC; c8 += 8) {
+                const int t = c8 / NC, c1 = c8 % NC;
+                const uint32_t col = lane_base + C::O_COL + (h * 2 + t) * NR + ch * NC + c1;
+                tmem_ld8(col, raw);
                 tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-                  raw[c] = __float_as_uint(__uint_as_float(raw[c]) * __shfl_sync(0xffffffffu, alpha, c));
-                tmem_st<NC>(col, raw);
+                for (int c = 0; c < 8; ++c)
+                  raw[c] = __float_as_uint(__uint_as_float(raw[c]) * __shfl_sync(0xffffffffu, alpha, c1 + c));
+                tmem_st8(col, raw);
               }
               tmem_wait_st();
             }
 #pragma unroll
             for (int c = 0; c < NC; ++c) l[h][c] *= __shfl_sync(0xffffffffu, alpha, c);
+            tmem_ld<NC>(s_tmem, raw);
             bar_sync(gbar, 128);
-#pragma unroll
-            for (int c = 0; c < NC; ++c) e[c] -= mr[c];
           }
           tc_fence_before();
           __syncwarp();
@@ -708,26 +725,22 @@ __global__ void __launch_bounds__(384, 1)
               l[h][c + i] = fmaf(pr[i], sc.z, l[h][c + i]);
             }
             uint32_t a0, a1, b0, b1;
-            split_e4m3x2(pr[0], pr[1], a0, b0);
-            split_e4m3x2(pr[2], pr[3], a1, b1);
+            split_e4m3x2<true>(pr[0], pr[1], a0, b0);
+            split_e4m3x2<true>(pr[2], pr[3], a1, b1);
             w1[c / 4] = a0 | a1 << 16;
             w2[c / 4] = b0 | b1 << 16;
           }
-          if (x >= static_cast<uint32_t>(PB) && k >= PB) {  // the buffer's last products are done
-            wait(pv_done(h, buf), ((x / PB) - 1) & 1);
-          }
+          if (k >= PB) wait(pv_done(h, buf), ((x / PB) - 1) & 1);  // the buffer's last products are done
           unsigned char* prow = smem + C::OFF_P + (h * PB + buf) * C::P_BUF + (q4 * 32 + lane) * 128;
           const int sw = lane & 7;
-          if constexpr (NC >= 16) {
-#pragma unroll
-            for (int c = 0; c < NC / 16; ++c) {
-              const int a = (ch * NC) / 16 + c, b = (NR + ch * NC) / 16 + c;
-              *reinterpret_cast<uint4*>(prow + ((a ^ sw) << 4)) = make_uint4(w1[4 * c], w1[4 * c + 1], w1[4 * c + 2], w1[4 * c + 3]);
-              *reinterpret_cast<uint4*>(prow + ((b ^ sw) << 4)) = make_uint4(w2[4 * c], w2[4 * c + 1], w2[4 * c + 2], w2[4 * c + 3]);
-            }
-          } else {  // NR = 16: bytes [ch * 8, + 8) of chunks 0 and 1
-            *reinterpret_cast<uint2*>(prow + ((0 ^ sw) << 4) + ch * 8) = make_uint2(w1[0], w1[1]);
-            *reinterpret_cast<uint2*>(prow + ((1 ^ sw) << 4) + ch * 8) = make_uint2(w2[0], w2[1]);
+          if constexpr (NC == 16) {
+            const int a = ch, b = NR / 16 + ch;
+            *reinterpret_cast<uint4*>(prow + ((a ^ sw) << 4)) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+            *reinterpret_cast<uint4*>(prow + ((b ^ sw) << 4)) = make_uint4(w2[0], w2[1], w2[2], w2[3]);
+          } else {  // eight bytes of a 16-byte chunk
+            const int a = ch >> 1, b = NR / 16 + (ch >> 1);
+            *reinterpret_cast<uint2*>(prow + ((a ^ sw) << 4) + (ch & 1) * 8) = make_uint2(w1[0], w1[1]);
+            *reinterpret_cast<uint2*>(prow + ((b ^ sw) << 4) + (ch & 1) * 8) = make_uint2(w2[0], w2[1]);
           }
           fence_async_smem();
           tc_fence_before();
@@ -735,70 +748,100 @@ __global__ void __launch_bounds__(384, 1)
           if (lane == 0) mbar_arrive(p_full(h, buf));
         }
       }
-      // ---- the unit's (or the part's) sums and outputs ----
-      const uint32_t xl = it + s.ntile - 1;
-      wait(flag_bar(seg_no & 7), (seg_no >> 3) & 1);
-      const bool bad = seg_flag[seg_no & 7] != 0;
-      const bool whole = s.tile0 == 0 && s.ntile == s.unit_tiles;
-      const int c_first = owner_of(s.unit_start, total, ctas);
-      const int c_last = owner_of(s.unit_start + s.unit_tiles - 1, total, ctas);
-      const int64_t slot = s.u + cta;
-      if (bad && warp == 4 && lane == 0)
-        set_status(p.status, s.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
         const float sum = sum_columns<NC>(l[h], lane);
         if (lane % (32 / NC) == 0) xch[(h * 4 + q4) * NR + ch * NC + lane / (32 / NC)] = sum;
       }
-      bar_sync(gbar, 128);
+      // The next segment's Q takes the place of this one's: every S of this segment has been
+      // read. Its first scores are computed while this segment's outputs are written.
+      const Seg c = s;
+      const uint32_t xl = it + c.ntile - 1;
+      it += c.ntile;
+      float qn[NH];
 #pragma unroll
+      for (int h = 0; h < NH; ++h) qn[h] = 0.f;
+      if (has_more(c, t1, OVH)) {
+        s = locate<TK>(c.vnext, t1, p, pb, OVH);
+        start_segment(s, par ^ 1, qn);
+      } else {
+        s.ntile = 0;
+      }
+      // ---- the unit's (or the part's) sums and outputs ----
+      wait(flag_bar(seg_no & 7), (seg_no >> 3) & 1);
+      const bool bad = seg_flag[seg_no & 7] != 0;
+      const bool whole = c.tile0 == 0 && c.ntile == c.unit_tiles;
+      const int64_t slot = c.u + cta;
+      if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
+      bar_sync(1, nthr);
+      // a thread per row: its sum, factor and place
+      int64_t* row_at = reinterpret_cast<int64_t*>(smem + C::OFF_ROW);
+      float* row_inv = reinterpret_cast<float*>(smem + C::OFF_INV);
+      for (int i = stid; i < NH * NR; i += nthr) {
+        const int h = i / NR, r = i % NR;
+        if (r >= real_rows(c, h)) continue;
+        const float* xs = xch + h * 4 * NR + r;
+        const float L = bad ? -1.f : xs[0] + xs[NR] + xs[2 * NR] + xs[3 * NR];
+        const float m = mref[i];
+        if (whole) {
+          const int ur = unit_row(c, h, r), j = ur / p.group;
+          const int head = (c.g * HP + (HP == 2 ? h : 0)) * p.group + ur - j * p.group;
+          const int64_t at = (static_cast<int64_t>(c.b) * p.gamma + j) * p.hq + head;
+          row_at[i] = at * D;
+          row_inv[i] = fp8_inv(L);
+          if (p.lse) p.lse[at] = fp8_lse(m, L);
+        } else {
+          const int64_t at = slot * p.slot_rows + (HP == 2 ? h * p.rows + r : h * NR + r);
+          row_at[i] = at * D;
+          row_inv[i] = L <= 0.f ? 0.f : 1.f;
+          p.partial_ml[at] = make_float2(m, L);
+        }
+      }
+      bar_sync(1, nthr);
+      const int d = q4 * 32 + lane;  // this lane's dim
+#pragma unroll 1
       for (int h = 0; h < NH; ++h) {
         wait(pv_done(h, xl % PB), (xl / PB) & 1);
         tc_fence_after();
-        uint32_t a[NC], b[NC];
-        tmem_ld<NC>(lane_base + C::O_COL + h * 2 * NR + ch * NC, a);
-        tmem_ld<NC>(lane_base + C::O_COL + (h * 2 + 1) * NR + ch * NC, b);
-        tmem_wait_ld();
-        const int nreal = real_rows(h) - ch * NC;  // of this warp's rows
-        const int d = q4 * 32 + lane;              // this lane's dim
-        const int kvh = s.g * HP + (HP == 2 ? h : 0);
-        const bool has_nan = *nan_flag != 0;
+        const bool has_nan = *nan_flag != 0;  // noted before the products just waited for
+        const int nreal = min(NC, real_rows(c, h) - ch * NC);  // of this warp's rows
+#pragma unroll 1
+        for (int c8 = 0; c8 < nreal; c8 += 8) {
+          uint32_t a[8], b[8];
+          const uint32_t col = lane_base + C::O_COL + h * 2 * NR + ch * NC + c8;
+          tmem_ld8(col, a);
+          tmem_ld8(col + NR, b);
+          tmem_wait_ld();
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          if (c >= nreal) continue;
-          const int r = ch * NC + c, ur = unit_row(h, r);
-          const float* xs = xch + h * 4 * NR + r;
-          const float L = bad ? -1.f : xs[0] + xs[NR] + xs[2 * NR] + xs[3 * NR];
-          const float m = mref[h * NR + r];
-          float o = __uint_as_float(a[c]) + __uint_as_float(b[c]);
-          if (has_nan && d < D && (nanv[(HP == 2 ? h : 0) * D + d] & vis[h * NR + r])) o = __int_as_float(0x7fc00000);
-          const int j = ur / p.group, head = kvh * p.group + ur % p.group;
-          const int64_t at = (static_cast<int64_t>(s.b) * p.gamma + j) * p.hq + head;
-          if (whole) {
-            const float inv = fp8_inv(L);
-            if (d < D) static_cast<__nv_bfloat16*>(p.out)[at * D + d] = __float2bfloat16_rn(inv == 0.f ? 0.f : o * inv);
-            if (d == 0 && p.lse) p.lse[at] = fp8_lse(m, L);
-          } else {
-            const int64_t prow = slot * p.slot_rows + (HP == 2 ? h * p.rows + r : h * NR + r);
-            if (d < D) p.partial_o[prow * D + d] = bad || L == 0.f ? 0.f : o;
-            if (d == 0) p.partial_ml[prow] = make_float2(m, L);
+          for (int i = 0; i < 8; ++i) {
+            if (c8 + i >= nreal || d >= D) continue;
+            const int r = h * NR + ch * NC + c8 + i;
+            const float inv = row_inv[r];
+            float o = fmaf(__uint_as_float(b[i]), 0.0625f, __uint_as_float(a[i])) * inv;
+            if (inv == 0.f) o = 0.f;
+            if (has_nan && inv != 0.f && (nanv[(HP == 2 ? h : 0) * D + d] & vis_of(par)[r])) o = __int_as_float(0x7fc00000);
+            if (whole) static_cast<__nv_bfloat16*>(p.out)[row_at[r] + d] = __float2bfloat16_rn(o);
+            else p.partial_o[row_at[r] + d] = o;
           }
         }
       }
-      if (!whole && warp == 4 && lane == 0) {
+      if (!whole && stid == 0) {
+        const int c_first = owner_of(c.unit_start, total, ctas);
+        const int c_last = owner_of(c.unit_start + c.unit_tiles - 1, total, ctas);
         int* e = pend + 8 * (*pend_count);
-        e[0] = s.b; e[1] = s.g; e[2] = row_base; e[3] = min(tile_rows, p.rows - row_base);
-        e[4] = static_cast<int>(s.u + c_first); e[5] = c_last - c_first + 1;
-        e[6] = static_cast<int>(s.u); e[7] = 0;
+        const int row_base = c.rt * tile_rows;
+        e[0] = c.b; e[1] = c.g; e[2] = row_base; e[3] = min(tile_rows, p.rows - row_base);
+        e[4] = static_cast<int>(c.u + c_first); e[5] = c_last - c_first + 1;
+        e[6] = static_cast<int>(c.u); e[7] = 0;
         *pend_count = *pend_count + 1;
       }
       tc_fence_before();
-      bar_sync(3, nsoft * 32);  // xch, vis, mref and nanv are read; the next segment may set them
-      for (int i = stid; i < HP * D; i += nsoft * 32) nanv[i] = 0ull;
+      bar_sync(1, nthr);  // xch, the row state and nanv are read; the next segment may set them
+      for (int i = stid; i < HP * D; i += nthr) nanv[i] = 0ull;
       if (stid == 0) *nan_flag = 0;
-      it += s.ntile;
-      if (!has_more(s, t1, OVH)) break;
-      s = locate<TK>(s.vnext, t1, p, pb, OVH);
+#pragma unroll
+      for (int h = 0; h < NH; ++h) qf[h] = qn[h];
+      ++seg_no;
     }
     tc_fence_before();
   }
