@@ -44,11 +44,21 @@ spec_status_t check_append(const spec_append_fp8_args_t* a) {
   return SPEC_OK;
 }
 
-// Two KV heads per block when each has at most 64 query rows: a page of both is one copy of
-// twice the size.
-int heads_per_block(const spec_attn_fp8_args_t& a) {
+// The tensor-core kernel's form of a call. A block serves two sub-units of at most 64 query
+// rows: two adjacent KV heads where each has that many (a page of both is one copy of twice
+// the size), else two halves of one KV head's rows, in tiles of up to 128.
+struct TcForm {
+  int heads, sub_rows, row_tiles;
+  bool fits;
+};
+TcForm tc_form(const spec_attn_fp8_args_t& a) {
   const int rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
-  return rows <= 64 && a.num_kv_heads % 2 == 0 ? 2 : 1;
+  TcForm f;
+  f.heads = rows <= kFp8SubRows && a.num_kv_heads % 2 == 0 ? 2 : 1;
+  f.row_tiles = f.heads == 2 ? 1 : (rows + 2 * kFp8SubRows - 1) / (2 * kFp8SubRows);
+  f.sub_rows = f.heads == 2 ? rows : (rows > 2 * kFp8SubRows ? kFp8SubRows : (rows + 1) / 2);
+  f.fits = attn_fp8_tc_fits(a, f.heads, f.sub_rows, f.row_tiles);
+  return f;
 }
 
 spec_status_t check_attn_fp8(const spec_attn_fp8_args_t* a) {
@@ -71,7 +81,7 @@ spec_status_t check_attn_fp8(const spec_attn_fp8_args_t* a) {
     return SPEC_ERR_UNSUPPORTED;
   const int64_t rows = static_cast<int64_t>(a->num_q_heads / a->num_kv_heads) * a->gamma;
   const int64_t z = static_cast<int64_t>(a->batch) * ((rows + kSimtRowTile - 1) / kSimtRowTile);
-  const bool tc = attn_fp8_tc_fits(*a, heads_per_block(*a), static_cast<int>(rows));
+  const bool tc = tc_form(*a).fits;
   if (a->path == SPEC_ATTN_TENSOR_CORES && !tc) return SPEC_ERR_UNSUPPORTED;
   if ((a->path == SPEC_ATTN_CUDA_CORES || !tc) && (z > 65535 || a->num_kv_heads > 65535))
     return SPEC_ERR_UNSUPPORTED;
@@ -103,17 +113,18 @@ namespace specv {
 AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path) {
   AttnFp8Plan P{};
   P.rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
-  P.heads = heads_per_block(a);
-  P.path = path != SPEC_ATTN_CUDA_CORES && attn_fp8_tc_fits(a, P.heads, P.rows) ? SPEC_ATTN_TENSOR_CORES
-                                                                                : SPEC_ATTN_CUDA_CORES;
+  const TcForm f = tc_form(a);
+  P.path = path != SPEC_ATTN_CUDA_CORES && f.fits ? SPEC_ATTN_TENSOR_CORES : SPEC_ATTN_CUDA_CORES;
   int64_t units;
   if (P.path == SPEC_ATTN_TENSOR_CORES) {
     // persistent grid; a unit has a slot of its own and one per block that starts inside it
-    P.row_tiles = (P.rows + kFp8MaxRows - 1) / kFp8MaxRows;
+    P.heads = f.heads;
+    P.sub_rows = f.sub_rows;
+    P.row_tiles = f.row_tiles;
     units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / P.heads) * P.row_tiles;
     P.grid = num_sms;
     P.nsplit = 1;
-    P.slot_rows = P.heads == 2 ? 2 * P.rows : (P.rows < kFp8MaxRows ? P.rows : kFp8MaxRows);
+    P.slot_rows = 2 * P.sub_rows;
     P.slots = units + P.grid;
   } else {
     P.row_tiles = (P.rows + kSimtRowTile - 1) / kSimtRowTile;

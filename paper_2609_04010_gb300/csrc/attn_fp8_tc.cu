@@ -20,14 +20,16 @@
 // (e4m3 ends at 448), which after a unit's first tile is rare. The second term of P is kept
 // times 16, which puts its smallest step at 2^-13.
 //
-// A block serves NH = 2 (or 1) sub-units of at most 64 query rows: two adjacent KV heads
-// (HP = 2, one box brings K and V of both: 8 KB with 16-token pages and D = 128), or two
-// row halves of one KV head. Warp roles (persistent, one block per SM):
-//   warp 0       producer: page ids and scales 32 pages ahead, one TMA box per page
-//   warp 1       issues S^T = K Q^T into a ring of four S buffers in TMEM
-//   warp 3       issues O^T += V^T P^T; clears V of keys past the sequence's end
-//   warps 4..    softmax: lane quadrant = 32 keys, NG warps per quadrant share the rows;
-//                they also convert Q and write the outputs
+// A block serves two sub-units of at most 64 query rows: two adjacent KV heads (HP = 2, one
+// box brings K and V of both: 8 KB with 16-token pages and D = 128), or two halves of one KV
+// head's rows (HP = 1). Warp roles (persistent, one block per SM):
+//   warp 16      producer: page ids and scales 32 pages ahead, one TMA box per page
+//   warp 17      issues S^T = K Q^T into two S buffers per sub-unit in TMEM
+//   warp 18      issues O^T += V^T P^T; clears V of keys past the sequence's end
+//   warps 0..15  softmax, eight per sub-unit: lane quadrant = 32 keys, two warps per quadrant
+//                share the rows. The sub-units' warps run free of each other, so that the
+//                waits of one are filled by the other's arithmetic. They also convert Q and
+//                write the outputs.
 // The tiles of all units form one list that is cut into equal ranges, one per block; a unit
 // split between blocks is merged from fp32 partials by the last block to finish it (atomic
 // ticket, no waiting). Every mbarrier wait is bounded; after a timeout the softmax warps run
@@ -44,47 +46,47 @@ using namespace tcx;
 
 constexpr int TK = kFp8KeyTile;  // keys per tile
 
+constexpr int NH = 2;  // sub-units of a block
+constexpr int kSoftWarps = 8 * NH;
+constexpr int kThreads = 32 * (kSoftWarps + 3);  // 19 warps: 104 registers a thread
+
 // NR: query rows of a sub-unit (N of the first product), 16, 32 or 64.
-template <int D, int HP, int NH, int NR>
+template <int D, int HP, int NR>
 struct Cfg {
-  static_assert(HP <= NH, "two heads are two sub-units");
-  static constexpr int NC = NR == 64 ? 16 : 8;             // rows per softmax warp
-  static constexpr int NG = NR / NC;                       // softmax warps per lane quadrant
+  static constexpr int NC = NR / 2;                        // rows per softmax warp
   static constexpr uint32_t ATOM = 8 * D;                  // 8 rows of D bytes, swizzled
   static constexpr uint32_t SG = 2 * HP * ATOM;            // 8-key group: K, V of each head
   static constexpr uint32_t STAGE = (TK / 8) * SG;
   static constexpr int NST = (HP == 2 ? 2 : 4) * (128 / D);  // 128 KB in stages
-  static constexpr int PB = NH == 1 ? 2 : 1;               // P buffers per sub-unit
-  static constexpr int SB = 4;                             // S buffers
+  static constexpr int SB = 2;                             // S buffers per sub-unit
   static constexpr uint32_t Q_TERM = NR * D;               // one term of one sub-unit's Q
   static constexpr uint32_t P_BUF = TK * 128;              // [key][128 B]: first terms, second terms
   static constexpr uint32_t OFF_STAGE = 0;
   static constexpr uint32_t OFF_P = OFF_STAGE + NST * STAGE;
-  static constexpr uint32_t OFF_Q = OFF_P + NH * PB * P_BUF;
-  static constexpr uint32_t OFF_SCL = OFF_Q + NH * 2 * Q_TERM;     // float4 [NST][8 pages][HP]
-  static constexpr uint32_t OFF_NAN = OFF_SCL + NST * 8 * HP * 16;  // uint64 [HP][D]: NaN block values
+  static constexpr uint32_t OFF_Q = OFF_P + NH * P_BUF;
+  static constexpr uint32_t OFF_SCL = OFF_Q + NH * 2 * Q_TERM;      // float4 [NST][8 pages][HP]
+  static constexpr uint32_t OFF_NAN = OFF_SCL + NST * 8 * HP * 16;  // uint64 [NH][D]: NaN block values
   // of the current and the next segment: the block keys each row sees, the rows that see
   // each block key, the rows' references
-  static constexpr uint32_t OFF_VIS = OFF_NAN + HP * D * 8;           // uint64 [2][NH][NR]
-  static constexpr uint32_t OFF_SEEN = OFF_VIS + 2 * NH * NR * 8;     // uint32 [2][NH][NG][64]
-  static constexpr uint32_t OFF_M = OFF_SEEN + 2 * NH * NG * 64 * 4;  // float [2][NH][NR]
-  static constexpr uint32_t OFF_X = OFF_M + 2 * NH * NR * 4;          // float [NH][4][NR]: cross-quadrant
-  static constexpr uint32_t OFF_ROW = OFF_X + NH * 4 * NR * 4;        // int64 [NH][NR]: rows' outputs
-  static constexpr uint32_t OFF_INV = OFF_ROW + NH * NR * 8;          // float [NH][NR]: their factors
+  static constexpr uint32_t OFF_VIS = OFF_NAN + NH * D * 8;          // uint64 [2][NH][NR]
+  static constexpr uint32_t OFF_SEEN = OFF_VIS + 2 * NH * NR * 8;    // uint32 [2][NH][2][64]
+  static constexpr uint32_t OFF_M = OFF_SEEN + 2 * NH * 2 * 64 * 4;  // float [2][NH][NR]
+  static constexpr uint32_t OFF_X = OFF_M + 2 * NH * NR * 4;         // float [NH][4][NR]: cross-quadrant
+  static constexpr uint32_t OFF_ROW = OFF_X + NH * 4 * NR * 4;       // int64 [NH][NR]: rows' outputs
+  static constexpr uint32_t OFF_INV = OFF_ROW + NH * NR * 8;         // float [NH][NR]: their factors
   static constexpr uint32_t OFF_BAR = OFF_INV + NH * NR * 4;
-  // full[NST], empty[NST], s_full[SB], s_free[SB], p_full[NH*PB], pv_done[NH*PB], seg_ready,
-  // drain[2], flag_ready[8]
-  static constexpr int NBAR = 2 * NST + 2 * SB + 2 * NH * PB + 1 + 2 + 8;
-  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, pending, NaN flag
-  static constexpr uint32_t OFF_FLAG = OFF_MISC + 16;       // int [8]: bad flags of segments
+  // full[NST], empty[NST], s_full[NH][SB], s_free[NH][SB], p_full[NH], pv_done[NH],
+  // seg_ready[NH], drain[2], flag_ready[8]
+  static constexpr int NBAR = 2 * NST + 2 * NH * SB + 3 * NH + 2 + 8;
+  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, pending, -, NaN flags
+  static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;       // int [8]: bad flags of segments
   static constexpr uint32_t OFF_PEND = OFF_FLAG + 32;       // int [2][8]
-  static constexpr uint32_t OFF_QMAX = OFF_PEND + 64;       // uint32 [NH][16]
-  static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 64;    // int [batch + 1]
-  static constexpr uint32_t S_COL = 0;
-  static constexpr uint32_t O_COL = SB * NR;
-  static constexpr uint32_t TMEM_COLS = (SB + 2 * NH) * NR <= 128 ? 128 : ((SB + 2 * NH) * NR <= 256 ? 256 : 512);
-  static_assert((SB + 2 * NH) * NR <= 512, "TMEM holds 512 columns");
-  static constexpr int THREADS = 128 + 128 * NG;
+  static constexpr uint32_t OFF_QMAX = OFF_PEND + 64;       // uint32 [NH][8]
+  static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 32;    // int [batch + 1]
+  static constexpr uint32_t S_COL = 0;                      // [NH][SB][NR]
+  static constexpr uint32_t O_COL = NH * SB * NR;           // [NH][first, second terms][NR]
+  static constexpr uint32_t TMEM_COLS = NH * (SB + 2) * NR;
+  static_assert(TMEM_COLS <= 512, "TMEM holds 512 columns");
   static size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
 };
 
@@ -131,7 +133,8 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
 }
 template <int N>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* r) {
-  if constexpr (N == 16) tmem_ld16(taddr, r);
+  if constexpr (N == 32) tmem_ld32(taddr, r);
+  else if constexpr (N == 16) tmem_ld16(taddr, r);
   else tmem_ld8(taddr, r);
 }
 // Named barrier of the four softmax warps that share a set of rows; or-reduces `v`.
@@ -197,11 +200,11 @@ constexpr float kNoKey = -1e30f;  // a row's reference before it has seen a key
 // ---------------------------------------------------------------------------------
 // The kernel
 // ---------------------------------------------------------------------------------
-template <int D, int HP, int NH, int NR>
-__global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
+template <int D, int HP, int NR>
+__global__ void __launch_bounds__(kThreads, 1)
     attn_fp8_tc_kernel(const __grid_constant__ CUtensorMap tmap, AttnFp8Params p) {
-  using C = Cfg<D, HP, NH, NR>;
-  constexpr int NC = C::NC, NG = C::NG, NST = C::NST, PB = C::PB, SB = C::SB;
+  using C = Cfg<D, HP, NR>;
+  constexpr int NC = C::NC, NST = C::NST, SB = C::SB;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -209,59 +212,55 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
   const uint32_t bar0 = sbase + C::OFF_BAR;
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (NST + s); };
-  auto s_full = [&](int s) { return bar0 + 8u * (2 * NST + s); };
-  auto s_free = [&](int s) { return bar0 + 8u * (2 * NST + SB + s); };
-  auto p_full = [&](int h, int b) { return bar0 + 8u * (2 * NST + 2 * SB + h * PB + b); };
-  auto pv_done = [&](int h, int b) { return bar0 + 8u * (2 * NST + 2 * SB + NH * PB + h * PB + b); };
-  const uint32_t seg_ready = bar0 + 8u * (2 * NST + 2 * SB + 2 * NH * PB);
-  auto drain_bar = [&](int i) { return seg_ready + 8 + 8u * i; };
-  auto flag_bar = [&](int i) { return seg_ready + 24 + 8u * i; };
+  auto s_full = [&](int h, int b) { return bar0 + 8u * (2 * NST + h * SB + b); };
+  auto s_free = [&](int h, int b) { return bar0 + 8u * (2 * NST + NH * SB + h * SB + b); };
+  auto p_full = [&](int h) { return bar0 + 8u * (2 * NST + 2 * NH * SB + h); };
+  auto pv_done = [&](int h) { return bar0 + 8u * (2 * NST + 2 * NH * SB + NH + h); };
+  auto seg_ready = [&](int h) { return bar0 + 8u * (2 * NST + 2 * NH * SB + 2 * NH + h); };
+  auto drain_bar = [&](int i) { return bar0 + 8u * (2 * NST + 2 * NH * SB + 3 * NH + i); };
+  auto flag_bar = [&](int i) { return bar0 + 8u * (2 * NST + 2 * NH * SB + 3 * NH + 2 + i); };
   float4* scl = reinterpret_cast<float4*>(smem + C::OFF_SCL);
   unsigned long long* nanv = reinterpret_cast<unsigned long long*>(smem + C::OFF_NAN);
-  float* xch = reinterpret_cast<float*>(smem + C::OFF_X);
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
   volatile int* pend_count = reinterpret_cast<volatile int*>(misc + 2);
-  volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 3);
+  volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 4);  // [NH]
   volatile int* seg_flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);
   int* pend = reinterpret_cast<int*>(smem + C::OFF_PEND);
-  uint32_t* qmax = reinterpret_cast<uint32_t*>(smem + C::OFF_QMAX);
   int* pb = reinterpret_cast<int*>(smem + C::OFF_PB);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // rows of each sub-unit: one head's, or a half of a row tile's
-  const int tile_rows = HP == 2 ? NR : NH * NR;
+  // a unit's row tile: one sub-unit's rows for each of two heads, or two sub-units' rows
+  const int sub_rows = p.rows_per_cta;
+  const int tile_rows = HP == 2 ? sub_rows : NH * sub_rows;
   // softmax warps whose rows are all padding take no part
-  const int max_rows = min(p.rows, NR);
-  const int ngroup = (max_rows + NC - 1) / NC;
-  const int nsoft = 4 * ngroup;
+  const int nsoft = sub_rows > NC ? 8 : 4;  // per sub-unit
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < NST; ++s) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    for (int s = 0; s < SB; ++s) {
-      mbar_init(s_full(s), 1);
-      mbar_init(s_free(s), nsoft);
-    }
-    for (int h = 0; h < NH; ++h)
-      for (int b = 0; b < PB; ++b) {
-        mbar_init(p_full(h, b), nsoft);
-        mbar_init(pv_done(h, b), 1);
+    for (int h = 0; h < NH; ++h) {
+      for (int b = 0; b < SB; ++b) {
+        mbar_init(s_full(h, b), 1);
+        mbar_init(s_free(h, b), nsoft);
       }
-    mbar_init(seg_ready, nsoft);
+      mbar_init(p_full(h), nsoft);
+      mbar_init(pv_done(h), 1);
+      mbar_init(seg_ready(h), nsoft);
+      nan_flag[h] = 0;
+    }
     mbar_init(drain_bar(0), 1);
     mbar_init(drain_bar(1), 1);
     for (int i = 0; i < 8; ++i) mbar_init(flag_bar(i), 1);
     *abort_flag = 0;
     *pend_count = 0;
-    *nan_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int i = threadIdx.x; i < HP * D; i += C::THREADS) nanv[i] = 0ull;
-  if (warp == 1) tmem_alloc(smem_u32(misc), C::TMEM_COLS);
-  if (warp == 0) {
+  for (int i = threadIdx.x; i < NH * D; i += kThreads) nanv[i] = 0ull;
+  if (warp == kSoftWarps + 1) tmem_alloc(smem_u32(misc), C::TMEM_COLS);
+  if (warp == kSoftWarps) {
     const int per_b = p.hunits * p.row_tiles;
     int carry = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
@@ -297,7 +296,7 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
   const int64_t t1 = cta < ctas ? static_cast<int64_t>(cta + 1) * total / ctas : 0;
   const int OVH = p.unit_overhead;
 
-  if (warp == 0) {
+  if (warp == kSoftWarps) {
     // ============================ producer ============================
     uint32_t it = 0, seg_no = 0;
     bool ok = true;
@@ -380,19 +379,18 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
         }
       }
     }
-  } else if (warp == 1) {
+  } else if (warp == kSoftWarps + 1) {
     // ============================ S^T = K Q^T ============================
     constexpr uint32_t kIdesc = idesc_e4m3(128, NR, false, false);
     uint32_t it = 0, seg_no = 0;
     bool ok = true, issued = false;
     for (Seg s = locate<TK>(t0, t1, p, pb, OVH); s.ntile > 0 && ok; ++seg_no) {
-      ok = mbar_wait(seg_ready, seg_no & 1, abort_flag, p.status);
       for (int k = 0; k < s.ntile && ok; ++k, ++it) {
-        const uint32_t st = it % NST;
+        const uint32_t st = it % NST, sb = it % SB;
         ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
         for (int h = 0; h < NH && ok; ++h) {
-          const uint32_t y = it * NH + h, sb = y % SB;
-          if (y >= SB) ok = mbar_wait(s_free(sb), ((y / SB) - 1) & 1, abort_flag, p.status);
+          if (k == 0) ok = mbar_wait(seg_ready(h), seg_no & 1, abort_flag, p.status);
+          if (ok && it >= SB) ok = mbar_wait(s_free(h, sb), ((it / SB) - 1) & 1, abort_flag, p.status);
           if (!ok) break;
           tc_fence_after();
           if (lane == 0) {
@@ -401,10 +399,10 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
             for (int t = 0; t < 2; ++t)
 #pragma unroll
               for (int kk = 0; kk < D / 32; ++kk)
-                mma_e4m3(tmem + C::S_COL + sb * NR, desc_rows<D>(kb + kk * 32u, 16, C::SG),
+                mma_e4m3(tmem + C::S_COL + (h * SB + sb) * NR, desc_rows<D>(kb + kk * 32u, 16, C::SG),
                          desc_rows<D>(sbase + C::OFF_Q + (h * 2 + t) * C::Q_TERM + kk * 32u, 16, C::ATOM), kIdesc,
                          t > 0 || kk > 0);
-            mma_commit(s_full(sb));
+            mma_commit(s_full(h, sb));
             issued = true;
           }
           __syncwarp();
@@ -420,7 +418,7 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
       while (!mbar_try(drain_bar(0), 0) && clock64() - c0 < kWaitCycles) {
       }
     }
-  } else if (warp == 3) {
+  } else if (warp == kSoftWarps + 2) {
     // ============================ O^T += V^T P^T ============================
     constexpr uint32_t kIdesc = idesc_e4m3(128, 2 * NR, true, true);
     uint32_t it = 0;
@@ -455,10 +453,12 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
             const uint32_t sh = (e & 3) * 8;
             if ((w[e >> 2] >> sh & 0x7fu) == 0x7fu) {
               atomicOr(nanv + h * D + piece * 16 + e, bit);
+              if (HP == 1) atomicOr(nanv + D + piece * 16 + e, bit);
               w[e >> 2] &= ~(0xffu << sh);
             }
           }
-          *nan_flag = 1;
+          nan_flag[h] = 1;
+          if (HP == 1) nan_flag[1] = 1;
           *at = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
@@ -472,21 +472,22 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
         if (!ok) break;
         // a unit's first tile waits for its weights first: they follow the outputs of the unit
         // before, whose NaN notes are then read
-        if (k > 0) fix_values(st, s, k);
-        const int buf = static_cast<int>(it % PB);
+        if (k == 0)
+          for (int h = 0; h < NH && ok; ++h) ok = mbar_wait(p_full(h), it & 1, abort_flag, p.status);
+        if (!ok) break;
+        fix_values(st, s, k);
         for (int h = 0; h < NH && ok; ++h) {
-          ok = mbar_wait(p_full(h, buf), (it / PB) & 1, abort_flag, p.status);
+          ok = mbar_wait(p_full(h), it & 1, abort_flag, p.status);
           if (!ok) break;
-          if (k == 0 && h == 0) fix_values(st, s, k);
           tc_fence_after();
           if (lane == 0) {
             const uint32_t vb = sbase + C::OFF_STAGE + st * C::STAGE + ((HP == 2 ? h : 0) * 2 + 1) * C::ATOM;
-            const uint32_t pa = sbase + C::OFF_P + (h * PB + buf) * C::P_BUF;
+            const uint32_t pa = sbase + C::OFF_P + h * C::P_BUF;
 #pragma unroll
             for (int kk = 0; kk < TK / 32; ++kk)
               mma_e4m3(tmem + C::O_COL + h * 2 * NR, desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG),
                        desc_rows<128>(pa + kk * 4096u, 0, 1024), kIdesc, k > 0 || kk > 0);
-            mma_commit(pv_done(h, buf));
+            mma_commit(pv_done(h));
             if (h == NH - 1) mma_commit(empty(st));
             issued = true;
           }
@@ -503,226 +504,216 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
       while (!mbar_try(drain_bar(1), 0) && clock64() - c0 < kWaitCycles) {
       }
     }
-  } else if (warp >= 4 && (warp - 4) / 4 < ngroup) {
+  } else if ((warp & 7) < nsoft) {
     // ============================ softmax ============================
-    const int q4 = (warp - 4) & 3, ch = (warp - 4) >> 2;  // 32 keys; rows [ch * NC, + NC)
-    const int gbar = 2 + ch;                              // named barrier of this row group
-    const int nthr = nsoft * 32, stid = threadIdx.x - 128;  // threads of all groups
+    // sub-unit h; lane quadrant q4 = 32 keys; rows [ch * NC, + NC)
+    const int h = warp >> 3, ch = (warp >> 2) & 1, q4 = warp & 3;
+    const int sbar = 1 + h, gbar = 3 + 2 * h + ch;  // named barriers of the sub-unit and of the row group
+    const int nthr = nsoft * 32, stid = threadIdx.x & 255;  // threads of the sub-unit
+    const int swarp = warp & 7, kvh = HP == 2 ? h : 0;
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
-    const int psh = __ffs(p.page_size) - 1;
-    const int pg = (q4 * 32 + lane) >> psh;  // this lane's page of a tile
+    const uint32_t o_col = lane_base + C::O_COL + h * 2 * NR + ch * NC;
+    const int pg = (q4 * 32 + lane) / p.page_size;  // this lane's page of a tile
+    float* xch = reinterpret_cast<float*>(smem + C::OFF_X) + h * 4 * NR;  // [4][NR]
+    uint32_t* qmax = reinterpret_cast<uint32_t*>(smem + C::OFF_QMAX) + h * 8;
+    unsigned char* const pbuf = smem + C::OFF_P + h * C::P_BUF + (q4 * 32 + lane) * 128;
     uint32_t it = 0, seg_no = 0;
-    bool dead = false;  // after a timeout: run on without waiting
+    // After a timeout the warp runs its loops to the end without waiting (nothing else
+    // depends on `dead`), so that it passes every named barrier.
+    bool dead = false;
     auto wait = [&](uint32_t bar, uint32_t parity) {
-      if (dead) return;
-      const bool ok = mbar_wait(bar, parity, abort_flag, p.status);
-      dead = !__all_sync(0xffffffffu, ok);
+      if (!dead && !mbar_wait(bar, parity, abort_flag, p.status)) dead = true;
+      __syncwarp();
     };
     // per-segment state, by the segment's parity
-    auto vis_of = [&](uint32_t par) { return reinterpret_cast<unsigned long long*>(smem + C::OFF_VIS) + par * NH * NR; };
-    auto seen_of = [&](uint32_t par) { return reinterpret_cast<uint32_t*>(smem + C::OFF_SEEN) + par * NH * NG * 64; };
-    auto mref_of = [&](uint32_t par) { return reinterpret_cast<float*>(smem + C::OFF_M) + par * NH * NR; };
-    // rows of sub-unit h: the unit row of its row r, and how many are real
-    auto unit_row = [&](const Seg& sg, int h, int r) { return sg.rt * tile_rows + (HP == 2 ? 0 : h * NR) + r; };
-    auto real_rows = [&](const Seg& sg, int h) { return min(NR, p.rows - unit_row(sg, h, 0)); };
+    auto vis_of = [&](uint32_t par) {
+      return reinterpret_cast<unsigned long long*>(smem + C::OFF_VIS) + (par * NH + h) * NR;
+    };
+    auto seen_of = [&](uint32_t par) { return reinterpret_cast<uint32_t*>(smem + C::OFF_SEEN) + (par * NH + h) * 128; };
+    auto mref_of = [&](uint32_t par) { return reinterpret_cast<float*>(smem + C::OFF_M) + (par * NH + h) * NR; };
+    // the unit row of row r, and how many are real
+    auto unit_row = [&](const Seg& sg, int r) { return sg.rt * tile_rows + (HP == 2 ? 0 : h * sub_rows) + r; };
+    auto real_rows = [&](const Seg& sg) { return min(sub_rows, p.rows - unit_row(sg, 0)); };
 
     // Brings a segment's Q into shared memory as two e4m3 terms, scaled by the power of two
     // that takes the sub-unit's largest finite magnitude into (224, 448], and sets its
-    // row state. Returns the scales in qf.
-    auto start_segment = [&](const Seg& sg, uint32_t par, float* qf) {
+    // row state. Returns the scale.
+    auto start_segment = [&](const Seg& sg, uint32_t par) -> float {
       constexpr int kPieces = D / 16;  // 16 elements per piece: 32 B in, 16 B per term
-      constexpr int kTotal = NR * kPieces;
-      constexpr int kLoops = NR == 64 ? (kTotal + 383) / 384 : 1;  // rows 33.. and 17.. have 384 threads
-      uint4 x[NH][kLoops][2];
+      constexpr int kLoops = NR * kPieces > 256 ? NR * kPieces / 256 : 1;  // NR > 16 has 256 threads
+      const int nreal = real_rows(sg);
+      uint4 x[kLoops][2];
 #pragma unroll
-      for (int h = 0; h < NH; ++h) {
-#pragma unroll
-        for (int i = 0; i < kLoops; ++i) {
-          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
-          x[h][i][0] = x[h][i][1] = make_uint4(0, 0, 0, 0);
-          if (r < real_rows(sg, h)) {
-            const int ur = unit_row(sg, h, r), j = ur / p.group;
-            const int head = (sg.g * HP + (HP == 2 ? h : 0)) * p.group + ur - j * p.group;
-            const uint4* src = reinterpret_cast<const uint4*>(
-                static_cast<const __nv_bfloat16*>(p.q) +
-                ((static_cast<int64_t>(sg.b) * p.gamma + j) * p.hq + head) * D + piece * 16);
-            x[h][i][0] = __ldg(src);
-            x[h][i][1] = __ldg(src + 1);
-          }
+      for (int i = 0; i < kLoops; ++i) {
+        const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+        x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+        if (r < nreal) {
+          const int ur = unit_row(sg, r), j = ur / p.group;
+          const int head = (sg.g * HP + kvh) * p.group + ur - j * p.group;
+          const uint4* src = reinterpret_cast<const uint4*>(
+              static_cast<const __nv_bfloat16*>(p.q) +
+              ((static_cast<int64_t>(sg.b) * p.gamma + j) * p.hq + head) * D + piece * 16);
+          x[i][0] = __ldg(src);
+          x[i][1] = __ldg(src + 1);
         }
       }
       // meanwhile the rows' visible block keys, and the rows that see each block key
       const unsigned long long all = p.gamma >= 64 ? ~0ull : (1ull << p.gamma) - 1;
       unsigned long long* vis = vis_of(par);
-      for (int i = stid; i < NH * NR; i += nthr) {
-        const int h = i / NR, r = i % NR;
-        const int j = min(unit_row(sg, h, r), p.rows - 1) / p.group;
-        vis[i] = all & (p.tree_mask ? __ldg(p.tree_mask + static_cast<int64_t>(sg.b) * p.gamma + j) : (2ull << j) - 1);
-        mref_of(par)[i] = kNoKey;
+      for (int r = stid; r < NR; r += nthr) {
+        const int j = min(unit_row(sg, r), p.rows - 1) / p.group;
+        vis[r] = all & (p.tree_mask ? __ldg(p.tree_mask + static_cast<int64_t>(sg.b) * p.gamma + j) : (2ull << j) - 1);
+        mref_of(par)[r] = kNoKey;
       }
+      uint32_t mx = 0;
 #pragma unroll
-      for (int h = 0; h < NH; ++h) {
-        uint32_t mx = 0;
+      for (int i = 0; i < kLoops; ++i)
 #pragma unroll
-        for (int i = 0; i < kLoops; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t w[4] = {x[h][i][e].x, x[h][i][e].y, x[h][i][e].z, x[h][i][e].w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t a = w[c] & 0x7fffu, b = (w[c] >> 16) & 0x7fffu;
-              mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
-            }
-          }
-        mx = __reduce_max_sync(0xffffffffu, mx);
-        if (lane == 0) qmax[h * 16 + warp - 4] = mx;
-      }
-      bar_sync(1, nthr);
-      for (int i = warp - 4; i < NH * ngroup * 64; i += nsoft) {  // lane = row of the group
-        const int key = i & 63, hg = i >> 6, h = hg / ngroup, g = hg - h * ngroup;
-        const bool v = lane < NC && (vis[h * NR + g * NC + (lane & (NC - 1))] >> key & 1);
-        const uint32_t m = __ballot_sync(0xffffffffu, v);
-        if (lane == 0) seen_of(par)[(h * NG + g) * 64 + key] = m;
-      }
-#pragma unroll
-      for (int h = 0; h < NH; ++h) {
-        uint32_t mx = 0;
-        for (int w = 0; w < nsoft; ++w) mx = max(mx, qmax[h * 16 + w]);
-        const int e = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
-        qf[h] = __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
-        const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-#pragma unroll
-        for (int i = 0; i < kLoops; ++i) {
-          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
-          if (r >= NR) continue;
-          uint32_t t1w[4], t2w[4];
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t w[4] = {x[i][e].x, x[i][e].y, x[i][e].z, x[i][e].w};
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const uint4 u = x[h][i][c >> 1];
-            const uint32_t w[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
-            uint32_t a[2], b[2];
-#pragma unroll
-            for (int d = 0; d < 2; ++d) {
-              float lo = __uint_as_float(w[d] << 16) * inv, hi = __uint_as_float(w[d] & 0xffff0000u) * inv;
-              lo = fabsf(lo) < INFINITY ? lo : __int_as_float(0x7fc00000);  // an infinite query is NaN
-              hi = fabsf(hi) < INFINITY ? hi : __int_as_float(0x7fc00000);
-              split_e4m3x2<false>(lo, hi, a[d], b[d]);
-            }
-            t1w[c] = a[0] | a[1] << 16;
-            t2w[c] = b[0] | b[1] << 16;
+            const uint32_t a = w[c] & 0x7fffu, b = (w[c] >> 16) & 0x7fffu;
+            mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
           }
-          const int ph = D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3);
-          unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + r * D + ph * 16;
-          *reinterpret_cast<uint4*>(dst) = make_uint4(t1w[0], t1w[1], t1w[2], t1w[3]);
-          *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
         }
+      mx = __reduce_max_sync(0xffffffffu, mx);
+      if (lane == 0) qmax[swarp] = mx;
+      bar_sync(sbar, nthr);
+      for (int i = swarp; i < nsoft / 4 * 64; i += nsoft) {  // lane = row of group i / 64
+        const bool v = lane < NC && (vis[(i >> 6) * NC + (lane & (NC - 1))] >> (i & 63) & 1);
+        const uint32_t m = __ballot_sync(0xffffffffu, v);
+        if (lane == 0) seen_of(par)[i] = m;
+      }
+      mx = 0;
+      for (int w = 0; w < nsoft; ++w) mx = max(mx, qmax[w]);
+      const int ex = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
+      const float inv = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+#pragma unroll
+      for (int i = 0; i < kLoops; ++i) {
+        const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+        if (r >= NR) continue;
+        uint32_t t1w[4], t2w[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint4 u = x[i][c >> 1];
+          const uint32_t w[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
+          uint32_t a[2], b[2];
+#pragma unroll
+          for (int d = 0; d < 2; ++d) {
+            float lo = __uint_as_float(w[d] << 16) * inv, hi = __uint_as_float(w[d] & 0xffff0000u) * inv;
+            lo = fabsf(lo) < INFINITY ? lo : __int_as_float(0x7fc00000);  // an infinite query is NaN
+            hi = fabsf(hi) < INFINITY ? hi : __int_as_float(0x7fc00000);
+            split_e4m3x2<false>(lo, hi, a[d], b[d]);
+          }
+          t1w[c] = a[0] | a[1] << 16;
+          t2w[c] = b[0] | b[1] << 16;
+        }
+        const int ph = D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3);
+        unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + r * D + ph * 16;
+        *reinterpret_cast<uint4*>(dst) = make_uint4(t1w[0], t1w[1], t1w[2], t1w[3]);
+        *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
       }
       fence_async_smem();
-      bar_sync(1, nthr);  // the row state is set
-      if (lane == 0) mbar_arrive(seg_ready);
+      bar_sync(sbar, nthr);  // the row state is set
+      if (lane == 0) mbar_arrive(seg_ready(h));
+      return __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
     };
 
     Seg s = locate<TK>(t0, t1, p, pb, OVH);
-    float qf[NH];
-    if (s.ntile > 0) start_segment(s, 0, qf);
+    float qf = s.ntile > 0 ? start_segment(s, 0) : 1.f;
     while (s.ntile > 0) {
       const uint32_t par = seg_no & 1;
       const int ctx = s.kv_len - p.gamma;
-      float* mref = mref_of(par);
-      float l[NH][NC];
+      float* const mr = mref_of(par) + ch * NC;
+      float l[NC];
 #pragma unroll
-      for (int h = 0; h < NH; ++h)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) l[h][c] = 0.f;
+      for (int c = 0; c < NC; ++c) l[c] = 0.f;
 
       for (int k = 0; k < s.ntile; ++k) {
-        const uint32_t x = it + k, st = x % NST;
+        const uint32_t x = it + k, st = x % NST, sb = x % SB;
         const int key0 = (s.tile0 + k) * TK;
         const bool masked = key0 + TK > ctx;
         const int rel = key0 + q4 * 32 + lane - ctx;  // block position (negative: the prefix)
-        const int buf = static_cast<int>(x % PB);
+        wait(s_full(h, sb), (x / SB) & 1);
+        tc_fence_after();
+        uint32_t raw[NC];
+        const uint32_t s_tmem = lane_base + C::S_COL + (h * SB + sb) * NR + ch * NC;
+        tmem_ld<NC>(s_tmem, raw);
+        wait(full(st), (x / NST) & 1);  // orders the producer's scales before this
+        const float4 sc = scl[(st * 8 + pg) * HP + kvh];
+        const float ks = sc.x * qf;
+        uint32_t seen = ~0u;
+        if (masked && rel >= 0) seen = rel < 64 ? seen_of(par)[ch * 64 + rel] : 0u;
+        // e = log2 of the key's weight and value scale for each row, over the row's
+        // reference; hidden keys have none
+        float e[NC];
+        for (bool raised = false;; raised = true) {
+          tmem_wait_ld();
+          float top = -INFINITY;
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          const uint32_t y = x * NH + h, sb = y % SB;
-          wait(s_full(sb), (y / SB) & 1);
-          tc_fence_after();
-          uint32_t raw[NC];
-          const uint32_t s_tmem = lane_base + C::S_COL + sb * NR + ch * NC;
-          tmem_ld<NC>(s_tmem, raw);
-          if (h == 0) wait(full(st), (x / NST) & 1);  // orders the producer's scales before this
-          const float4 sc = scl[(st * 8 + pg) * HP + (HP == 2 ? h : 0)];
-          const float ks = sc.x * qf[h];
-          // e = log2 of the key's weight and value scale for each row, over the row's
-          // reference; hidden keys have none
-          const float* mr = mref + h * NR + ch * NC;
-          uint32_t seen = ~0u;
-          if (masked && rel >= 0) seen = rel < 64 ? seen_of(par)[(h * NG + ch) * 64 + rel] : 0u;
-          float e[NC];
-          for (bool raised = false;; raised = true) {
-            tmem_wait_ld();
-            float top = -INFINITY;
+          for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(raw[c]), ks, sc.y) - mr[c];
+          if (masked) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(raw[c]), ks, sc.y) - mr[c];
-            if (masked) {
-#pragma unroll
-              for (int c = 0; c < NC; ++c) e[c] = (seen >> c & 1) ? e[c] : -INFINITY;
-            }
-#pragma unroll
-            for (int c = 0; c < NC; ++c) top = fmaxf(top, e[c]);
-            if (raised || !group_any(gbar, top > 8.f)) break;
-            // Some weight would pass 2^8: raise the references, so that each row's largest
-            // weight so far becomes 2^2 where it was more.
-            float* xc = xch + h * 4 * NR;
-            float mx = -INFINITY;
-            tmem_ld<NC>(s_tmem, raw);
-            tmem_wait_ld();
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              const float v = fmaf(__uint_as_float(raw[c]), ks, sc.y);
-              const float m = warp_max((seen >> c & 1) ? v : -INFINITY);
-              if (lane % NC == c) mx = m;
-            }
-            if (lane < NC) xc[q4 * NR + ch * NC + lane] = mx;
-            bar_sync(gbar, 128);
-            const int c0 = ch * NC + lane % NC;
-            const float old = mref[h * NR + c0];
-            mx = fmaxf(fmaxf(xc[c0], xc[NR + c0]), fmaxf(xc[2 * NR + c0], xc[3 * NR + c0])) - 2.f;
-            const float now = fmaxf(old, mx);
-            const float alpha = ex2(old - now);
-            bar_sync(gbar, 128);
-            if (q4 == 0 && lane < NC) mref[h * NR + c0] = now;
-            if (k > 0) {  // O holds every earlier tile before it is scaled
-              wait(pv_done(h, (x - 1) % PB), ((x - 1) / PB) & 1);
-              tc_fence_after();
-#pragma unroll 1
-              for (int c8 = 0; c8 < 2 * NC; c8 += 8) {
-                const int t = c8 / NC, c1 = c8 % NC;
-                const uint32_t col = lane_base + C::O_COL + (h * 2 + t) * NR + ch * NC + c1;
-                tmem_ld8(col, raw);
-                tmem_wait_ld();
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                  raw[c] = __float_as_uint(__uint_as_float(raw[c]) * __shfl_sync(0xffffffffu, alpha, c1 + c));
-                tmem_st8(col, raw);
-              }
-              tmem_wait_st();
-            }
-#pragma unroll
-            for (int c = 0; c < NC; ++c) l[h][c] *= __shfl_sync(0xffffffffu, alpha, c);
-            tmem_ld<NC>(s_tmem, raw);
-            bar_sync(gbar, 128);
+            for (int c = 0; c < NC; ++c) e[c] = (seen >> c & 1) ? e[c] : -INFINITY;
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(s_free(sb));
-          uint32_t w1[NC / 4], w2[NC / 4];
 #pragma unroll
-          for (int c = 0; c < NC; c += 4) {
+          for (int c = 0; c < NC; ++c) top = fmaxf(top, e[c]);
+          if (raised || !group_any(gbar, top > 8.f)) break;
+          // Some weight would pass 2^8: raise the references, so that each row's largest
+          // weight so far becomes 2^2 where it was more.
+          float mx = -INFINITY;
+          tmem_ld<NC>(s_tmem, raw);
+          tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const float m = warp_max((seen >> c & 1) ? fmaf(__uint_as_float(raw[c]), ks, sc.y) : -INFINITY);
+            if (lane % NC == c) mx = m;
+          }
+          float* const xc = xch + ch * NC + lane % NC;
+          if (lane < NC) xc[q4 * NR] = mx;
+          bar_sync(gbar, 128);
+          const float old = mr[lane % NC];
+          const float now = fmaxf(old, fmaxf(fmaxf(xc[0], xc[NR]), fmaxf(xc[2 * NR], xc[3 * NR])) - 2.f);
+          const float alpha = ex2(old - now);
+          bar_sync(gbar, 128);
+          if (q4 == 0 && lane < NC) mr[lane] = now;
+          if (k > 0) {  // O holds every earlier tile before it is scaled
+            wait(pv_done(h), (x - 1) & 1);
+            tc_fence_after();
+#pragma unroll 1
+            for (int c8 = 0; c8 < 2 * NC; c8 += 8) {
+              const uint32_t col = o_col + (c8 / NC) * NR + c8 % NC;
+              tmem_ld8(col, raw);
+              tmem_wait_ld();
+#pragma unroll
+              for (int c = 0; c < 8; ++c)
+                raw[c] = __float_as_uint(__uint_as_float(raw[c]) * __shfl_sync(0xffffffffu, alpha, c8 % NC + c));
+              tmem_st8(col, raw);
+            }
+            tmem_wait_st();
+          }
+#pragma unroll
+          for (int c = 0; c < NC; ++c) l[c] *= __shfl_sync(0xffffffffu, alpha, c);
+          tmem_ld<NC>(s_tmem, raw);
+          bar_sync(gbar, 128);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_free(h, sb));
+        if (k > 0) wait(pv_done(h), (x - 1) & 1);  // the last products have read P
+        // weights, their sums, and their two terms into shared memory, 16 (8) rows at a time
+        constexpr int CB = NC >= 16 ? 16 : 8;
+#pragma unroll
+        for (int cb = 0; cb < NC; cb += CB) {
+          uint32_t w1[CB / 4], w2[CB / 4];
+#pragma unroll
+          for (int c = 0; c < CB; c += 4) {
             float pr[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              pr[i] = ex2(e[c + i]);
-              l[h][c + i] = fmaf(pr[i], sc.z, l[h][c + i]);
+              pr[i] = ex2(e[cb + c + i]);
+              l[cb + c + i] = fmaf(pr[i], sc.z, l[cb + c + i]);
             }
             uint32_t a0, a1, b0, b1;
             split_e4m3x2<true>(pr[0], pr[1], a0, b0);
@@ -730,40 +721,34 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
             w1[c / 4] = a0 | a1 << 16;
             w2[c / 4] = b0 | b1 << 16;
           }
-          if (k >= PB) wait(pv_done(h, buf), ((x / PB) - 1) & 1);  // the buffer's last products are done
-          unsigned char* prow = smem + C::OFF_P + (h * PB + buf) * C::P_BUF + (q4 * 32 + lane) * 128;
           const int sw = lane & 7;
-          if constexpr (NC == 16) {
-            const int a = ch, b = NR / 16 + ch;
-            *reinterpret_cast<uint4*>(prow + ((a ^ sw) << 4)) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
-            *reinterpret_cast<uint4*>(prow + ((b ^ sw) << 4)) = make_uint4(w2[0], w2[1], w2[2], w2[3]);
-          } else {  // eight bytes of a 16-byte chunk
-            const int a = ch >> 1, b = NR / 16 + (ch >> 1);
-            *reinterpret_cast<uint2*>(prow + ((a ^ sw) << 4) + (ch & 1) * 8) = make_uint2(w1[0], w1[1]);
-            *reinterpret_cast<uint2*>(prow + ((b ^ sw) << 4) + (ch & 1) * 8) = make_uint2(w2[0], w2[1]);
+          if constexpr (CB == 16) {
+            const int a = (ch * NC + cb) / 16, b = a + NR / 16;
+            *reinterpret_cast<uint4*>(pbuf + ((a ^ sw) << 4)) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+            *reinterpret_cast<uint4*>(pbuf + ((b ^ sw) << 4)) = make_uint4(w2[0], w2[1], w2[2], w2[3]);
+          } else {  // NR = 16: eight bytes of a 16-byte chunk
+            *reinterpret_cast<uint2*>(pbuf + ((0 ^ sw) << 4) + ch * 8) = make_uint2(w1[0], w1[1]);
+            *reinterpret_cast<uint2*>(pbuf + ((1 ^ sw) << 4) + ch * 8) = make_uint2(w2[0], w2[1]);
           }
-          fence_async_smem();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(p_full(h, buf));
         }
+        fence_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(h));
       }
-#pragma unroll
-      for (int h = 0; h < NH; ++h) {
-        const float sum = sum_columns<NC>(l[h], lane);
-        if (lane % (32 / NC) == 0) xch[(h * 4 + q4) * NR + ch * NC + lane / (32 / NC)] = sum;
+      {
+        const float sum = sum_columns<NC>(l, lane);
+        if (lane % (32 / NC) == 0) xch[q4 * NR + ch * NC + lane / (32 / NC)] = sum;
       }
       // The next segment's Q takes the place of this one's: every S of this segment has been
       // read. Its first scores are computed while this segment's outputs are written.
       const Seg c = s;
       const uint32_t xl = it + c.ntile - 1;
       it += c.ntile;
-      float qn[NH];
-#pragma unroll
-      for (int h = 0; h < NH; ++h) qn[h] = 0.f;
+      qf = 1.f;
       if (has_more(c, t1, OVH)) {
         s = locate<TK>(c.vnext, t1, p, pb, OVH);
-        start_segment(s, par ^ 1, qn);
+        qf = start_segment(s, par ^ 1);
       } else {
         s.ntile = 0;
       }
@@ -773,59 +758,53 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
       const bool whole = c.tile0 == 0 && c.ntile == c.unit_tiles;
       const int64_t slot = c.u + cta;
       if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
-      bar_sync(1, nthr);
+      const int nrows = real_rows(c);
+      bar_sync(sbar, nthr);
       // a thread per row: its sum, factor and place
-      int64_t* row_at = reinterpret_cast<int64_t*>(smem + C::OFF_ROW);
-      float* row_inv = reinterpret_cast<float*>(smem + C::OFF_INV);
-      for (int i = stid; i < NH * NR; i += nthr) {
-        const int h = i / NR, r = i % NR;
-        if (r >= real_rows(c, h)) continue;
-        const float* xs = xch + h * 4 * NR + r;
-        const float L = bad ? -1.f : xs[0] + xs[NR] + xs[2 * NR] + xs[3 * NR];
-        const float m = mref[i];
+      int64_t* row_at = reinterpret_cast<int64_t*>(smem + C::OFF_ROW) + h * NR;
+      float* row_inv = reinterpret_cast<float*>(smem + C::OFF_INV) + h * NR;
+      for (int r = stid; r < nrows; r += nthr) {
+        const float L = bad ? -1.f : xch[r] + xch[NR + r] + xch[2 * NR + r] + xch[3 * NR + r];
+        const float m = mref_of(par)[r];
         if (whole) {
-          const int ur = unit_row(c, h, r), j = ur / p.group;
-          const int head = (c.g * HP + (HP == 2 ? h : 0)) * p.group + ur - j * p.group;
+          const int ur = unit_row(c, r), j = ur / p.group;
+          const int head = (c.g * HP + kvh) * p.group + ur - j * p.group;
           const int64_t at = (static_cast<int64_t>(c.b) * p.gamma + j) * p.hq + head;
-          row_at[i] = at * D;
-          row_inv[i] = fp8_inv(L);
+          row_at[r] = at * D;
+          row_inv[r] = fp8_inv(L);
           if (p.lse) p.lse[at] = fp8_lse(m, L);
         } else {
-          const int64_t at = slot * p.slot_rows + (HP == 2 ? h * p.rows + r : h * NR + r);
-          row_at[i] = at * D;
-          row_inv[i] = L <= 0.f ? 0.f : 1.f;
+          const int64_t at = slot * p.slot_rows + h * sub_rows + r;
+          row_at[r] = at * D;
+          row_inv[r] = L <= 0.f ? 0.f : 1.f;
           p.partial_ml[at] = make_float2(m, L);
         }
       }
-      bar_sync(1, nthr);
-      const int d = q4 * 32 + lane;  // this lane's dim
+      bar_sync(sbar, nthr);
+      wait(pv_done(h), xl & 1);
+      tc_fence_after();
+      const bool has_nan = nan_flag[h] != 0;  // noted before the products just waited for
+      const int d = q4 * 32 + lane;           // this lane's dim
+      const int nreal = min(NC, nrows - ch * NC);  // of this warp's rows
 #pragma unroll 1
-      for (int h = 0; h < NH; ++h) {
-        wait(pv_done(h, xl % PB), (xl / PB) & 1);
-        tc_fence_after();
-        const bool has_nan = *nan_flag != 0;  // noted before the products just waited for
-        const int nreal = min(NC, real_rows(c, h) - ch * NC);  // of this warp's rows
-#pragma unroll 1
-        for (int c8 = 0; c8 < nreal; c8 += 8) {
-          uint32_t a[8], b[8];
-          const uint32_t col = lane_base + C::O_COL + h * 2 * NR + ch * NC + c8;
-          tmem_ld8(col, a);
-          tmem_ld8(col + NR, b);
-          tmem_wait_ld();
+      for (int c8 = 0; c8 < nreal; c8 += 8) {
+        uint32_t a[8], b[8];
+        tmem_ld8(o_col + c8, a);
+        tmem_ld8(o_col + NR + c8, b);
+        tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (c8 + i >= nreal || d >= D) continue;
-            const int r = h * NR + ch * NC + c8 + i;
-            const float inv = row_inv[r];
-            float o = fmaf(__uint_as_float(b[i]), 0.0625f, __uint_as_float(a[i])) * inv;
-            if (inv == 0.f) o = 0.f;
-            if (has_nan && inv != 0.f && (nanv[(HP == 2 ? h : 0) * D + d] & vis_of(par)[r])) o = __int_as_float(0x7fc00000);
-            if (whole) static_cast<__nv_bfloat16*>(p.out)[row_at[r] + d] = __float2bfloat16_rn(o);
-            else p.partial_o[row_at[r] + d] = o;
-          }
+        for (int i = 0; i < 8; ++i) {
+          if (c8 + i >= nreal || d >= D) continue;
+          const int r = ch * NC + c8 + i;
+          const float inv = row_inv[r];
+          float o = fmaf(__uint_as_float(b[i]), 0.0625f, __uint_as_float(a[i])) * inv;
+          if (inv == 0.f) o = 0.f;
+          if (has_nan && inv != 0.f && (nanv[h * D + d] & vis_of(par)[r])) o = __int_as_float(0x7fc00000);
+          if (whole) static_cast<__nv_bfloat16*>(p.out)[row_at[r] + d] = __float2bfloat16_rn(o);
+          else p.partial_o[row_at[r] + d] = o;
         }
       }
-      if (!whole && stid == 0) {
+      if (!whole && h == 0 && stid == 0) {
         const int c_first = owner_of(c.unit_start, total, ctas);
         const int c_last = owner_of(c.unit_start + c.unit_tiles - 1, total, ctas);
         int* e = pend + 8 * (*pend_count);
@@ -836,17 +815,15 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
         *pend_count = *pend_count + 1;
       }
       tc_fence_before();
-      bar_sync(1, nthr);  // xch, the row state and nanv are read; the next segment may set them
-      for (int i = stid; i < HP * D; i += nthr) nanv[i] = 0ull;
-      if (stid == 0) *nan_flag = 0;
-#pragma unroll
-      for (int h = 0; h < NH; ++h) qf[h] = qn[h];
+      bar_sync(sbar, nthr);  // xch, the row state and nanv are read; the next segment may set them
+      for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;
+      if (stid == 0) nan_flag[h] = 0;
       ++seg_no;
     }
     tc_fence_before();
   }
   __syncthreads();
-  if (warp == 1) {
+  if (warp == kSoftWarps + 1) {
     tc_fence_after();
     tmem_dealloc(tmem, C::TMEM_COLS);
   }
@@ -870,7 +847,7 @@ __global__ void __launch_bounds__(Cfg<D, HP, NH, NR>::THREADS, 1)
     if (!e[7]) continue;
     __threadfence();
     for (int h = 0; h < HP; ++h)
-      merge_fp8_unit<D>(p, e[0], e[1] * HP + h, e[2], e[3], e[4], e[5], threadIdx.x, C::THREADS, h * p.rows);
+      merge_fp8_unit<D>(p, e[0], e[1] * HP + h, e[2], e[3], e[4], e[5], threadIdx.x, kThreads, h * sub_rows);
   }
 }
 
@@ -892,65 +869,60 @@ bool encode_fp8_map(CUtensorMap* map, const spec_attn_fp8_args_t& a, int heads_p
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int HP, int NH, int NR>
+template <int D, int HP, int NR>
 cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
                          bool starve) {
-  using C = Cfg<D, HP, NH, NR>;
+  using C = Cfg<D, HP, NR>;
   CUtensorMap map;
   if (!encode_fp8_map(&map, a, HP)) return cudaErrorInvalidValue;
   AttnFp8Params p = make_attn_fp8_params(a, P, ws);
   p.hunits = a.num_kv_heads / HP;
+  p.rows_per_cta = P.sub_rows;
   p.starve = starve ? 1 : 0;
   // Starting a unit inside a block's range costs about this many tiles of time; charged
   // only where blocks hold several starts.
   p.unit_overhead = static_cast<int64_t>(a.batch) * p.hunits * P.row_tiles > P.grid ? 2 : 0;
   const size_t smem = C::smem_bytes(a.batch);
-  auto kernel = attn_fp8_tc_kernel<D, HP, NH, NR>;
+  auto kernel = attn_fp8_tc_kernel<D, HP, NR>;
   const cudaError_t e =
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  kernel<<<P.grid, C::THREADS, smem, stream>>>(map, p);
+  kernel<<<P.grid, kThreads, smem, stream>>>(map, p);
   return cudaGetLastError();
 }
 
-template <int D>
+template <int D, int HP>
 cudaError_t launch_d(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
                      bool starve) {
-  if (P.heads == 2) {
-    if (P.rows <= 16) return launch_typed<D, 2, 2, 16>(a, P, ws, stream, starve);
-    if (P.rows <= 32) return launch_typed<D, 2, 2, 32>(a, P, ws, stream, starve);
-    return launch_typed<D, 2, 2, 64>(a, P, ws, stream, starve);
-  }
-  if (P.rows <= 16) return launch_typed<D, 1, 1, 16>(a, P, ws, stream, starve);
-  if (P.rows <= 32) return launch_typed<D, 1, 1, 32>(a, P, ws, stream, starve);
-  if (P.rows <= 64) return launch_typed<D, 1, 1, 64>(a, P, ws, stream, starve);
-  return launch_typed<D, 1, 2, 64>(a, P, ws, stream, starve);
+  if (P.sub_rows <= 16) return launch_typed<D, HP, 16>(a, P, ws, stream, starve);
+  if (P.sub_rows <= 32) return launch_typed<D, HP, 32>(a, P, ws, stream, starve);
+  return launch_typed<D, HP, 64>(a, P, ws, stream, starve);
 }
 
-template <int D>
-size_t smem_of(int heads, int rows, int batch) {
-  if (heads == 2)
-    return rows <= 16 ? Cfg<D, 2, 2, 16>::smem_bytes(batch)
-                      : (rows <= 32 ? Cfg<D, 2, 2, 32>::smem_bytes(batch) : Cfg<D, 2, 2, 64>::smem_bytes(batch));
-  return rows <= 16   ? Cfg<D, 1, 1, 16>::smem_bytes(batch)
-         : rows <= 32 ? Cfg<D, 1, 1, 32>::smem_bytes(batch)
-         : rows <= 64 ? Cfg<D, 1, 1, 64>::smem_bytes(batch)
-                      : Cfg<D, 1, 2, 64>::smem_bytes(batch);
+template <int D, int HP>
+size_t smem_of(int sub_rows, int batch) {
+  return sub_rows <= 16   ? Cfg<D, HP, 16>::smem_bytes(batch)
+         : sub_rows <= 32 ? Cfg<D, HP, 32>::smem_bytes(batch)
+                          : Cfg<D, HP, 64>::smem_bytes(batch);
 }
 
 }  // namespace
 
-bool attn_fp8_tc_fits(const spec_attn_fp8_args_t& a, int heads, int rows) {
-  const size_t smem = a.head_dim == 128 ? smem_of<128>(heads, rows, a.batch) : smem_of<64>(heads, rows, a.batch);
+bool attn_fp8_tc_fits(const spec_attn_fp8_args_t& a, int heads, int sub_rows, int row_tiles) {
+  const bool d128 = a.head_dim == 128;
+  const size_t smem = heads == 2 ? (d128 ? smem_of<128, 2>(sub_rows, a.batch) : smem_of<64, 2>(sub_rows, a.batch))
+                                 : (d128 ? smem_of<128, 1>(sub_rows, a.batch) : smem_of<64, 1>(sub_rows, a.batch));
   const int64_t tiles = (static_cast<int64_t>(a.max_pages_per_seq) * a.page_size + TK - 1) / TK + 2;
-  const int64_t units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / heads) * ((rows + 127) / 128);
+  const int64_t units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / heads) * row_tiles;
   return smem <= kTcMaxSmem && tiles * units <= INT32_MAX &&
          2 * static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX;
 }
 
 cudaError_t launch_attn_fp8_tc(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
                                bool starve) {
-  return a.head_dim == 128 ? launch_d<128>(a, P, ws, stream, starve) : launch_d<64>(a, P, ws, stream, starve);
+  if (P.heads == 2)
+    return a.head_dim == 128 ? launch_d<128, 2>(a, P, ws, stream, starve) : launch_d<64, 2>(a, P, ws, stream, starve);
+  return a.head_dim == 128 ? launch_d<128, 1>(a, P, ws, stream, starve) : launch_d<64, 1>(a, P, ws, stream, starve);
 }
 
 }  // namespace specv

@@ -15,6 +15,7 @@ cudaError_t launch_adjust(const spec_adjust_args_t& a, cudaStream_t stream);
 struct AttnFp8Plan {
   int path;             // SPEC_ATTN_CUDA_CORES or SPEC_ATTN_TENSOR_CORES
   int heads;            // tensor cores: KV heads per block (2: adjacent ones)
+  int sub_rows;         // tensor cores: query rows of one of a block's two sub-units
   int grid;             // tensor cores: blocks
   int rows, row_tiles;  // (Hq/Hkv) * gamma query rows per KV head, in tiles
   int nsplit, tiles_per_split;  // CUDA cores: KV splits per unit and key tiles of a split
@@ -24,9 +25,9 @@ struct AttnFp8Plan {
 };
 AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path);
 constexpr int kFp8KeyTile = 128;   // keys per tile of the tensor-core kernel
-constexpr int kFp8MaxRows = 128;   // query rows of one of its units and KV head
-// Whether the tensor-core kernel takes the call with `heads` KV heads per block.
-bool attn_fp8_tc_fits(const spec_attn_fp8_args_t& a, int heads, int rows);
+constexpr int kFp8SubRows = 64;    // query rows of a sub-unit, at most
+// Whether the tensor-core kernel takes the call in this form.
+bool attn_fp8_tc_fits(const spec_attn_fp8_args_t& a, int heads, int sub_rows, int row_tiles);
 // starve (test hook only): the producer issues no copies, so the bounded waits run out.
 cudaError_t launch_attn_fp8_tc(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
                                cudaStream_t stream, bool starve = false);
