@@ -179,20 +179,23 @@ __device__ __forceinline__ float warp_max(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
-// The two terms of a pair of values, each term packed with a's in the low byte; UP: the
-// second term times 16.
+// The two e4m3 terms of four values, each packed in order from the low byte; UP: the second
+// terms times 16.
 template <bool UP>
-__device__ __forceinline__ void split_e4m3x2(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = to_e4m3x2(a, b);
-  uint32_t x;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(b), "f"(a));
-  const uint32_t h = e4m3x2_to_f16x2(hi);
-  uint32_t d;
-  asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(h));
-  if (UP) asm("mul.f16x2 %0, %1, %2;" : "=r"(d) : "r"(d), "r"(0x4c004c00u));
-  uint16_t l;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(l) : "r"(d));
-  lo = l;
+__device__ __forceinline__ void split_e4m3x4(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
+  asm("{\n .reg .b16 p, q, r, s;\n .reg .b32 x, y, h, g;\n"
+      " cvt.rn.satfinite.e4m3x2.f32 p, %3, %2;\n cvt.rn.satfinite.e4m3x2.f32 q, %5, %4;\n mov.b32 %0, {p, q};\n"
+      " cvt.rn.f16x2.f32 x, %3, %2;\n cvt.rn.f16x2.f32 y, %5, %4;\n"
+      " cvt.rn.f16x2.e4m3x2 h, p;\n cvt.rn.f16x2.e4m3x2 g, q;\n"
+      " sub.f16x2 x, x, h;\n sub.f16x2 y, y, g;\n mul.f16x2 x, x, %6;\n mul.f16x2 y, y, %6;\n"
+      " cvt.rn.satfinite.e4m3x2.f16x2 r, x;\n cvt.rn.satfinite.e4m3x2.f16x2 s, y;\n mov.b32 %1, {r, s};\n}"
+      : "=r"(hi), "=r"(lo)
+      : "f"(a), "f"(b), "f"(c), "f"(d), "r"(UP ? 0x4c004c00u : 0x3c003c00u));
+}
+
+// The slow part of a wait: polls until the phase completes, or gives up (mbar_wait).
+__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status) {
+  return mbar_wait(bar, parity, abort_flag, status);
 }
 
 constexpr float kNoKey = -1e30f;  // a row's reference before it has seen a key
@@ -206,8 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = Cfg<D, HP, NR>;
   constexpr int NC = C::NC, NST = C::NST, SB = C::SB;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  unsigned char* smem = reinterpret_cast<unsigned char*>(
-      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t sbase = smem_u32(smem);
   const uint32_t bar0 = sbase + C::OFF_BAR;
   auto full = [&](int s) { return bar0 + 8u * s; };
@@ -522,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // depends on `dead`), so that it passes every named barrier.
     bool dead = false;
     auto wait = [&](uint32_t bar, uint32_t parity) {
-      if (!dead && !mbar_wait(bar, parity, abort_flag, p.status)) dead = true;
+      if (!dead && !mbar_try(bar, parity)) dead = !wait_slow(bar, parity, abort_flag, p.status);
       __syncwarp();
     };
     // per-segment state, by the segment's parity
@@ -598,16 +600,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int c = 0; c < 4; ++c) {
           const uint4 u = x[i][c >> 1];
           const uint32_t w[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
-          uint32_t a[2], b[2];
+          float v[4];
 #pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            float lo = __uint_as_float(w[d] << 16) * inv, hi = __uint_as_float(w[d] & 0xffff0000u) * inv;
-            lo = fabsf(lo) < INFINITY ? lo : __int_as_float(0x7fc00000);  // an infinite query is NaN
-            hi = fabsf(hi) < INFINITY ? hi : __int_as_float(0x7fc00000);
-            split_e4m3x2<false>(lo, hi, a[d], b[d]);
+          for (int d = 0; d < 4; ++d) {
+            v[d] = __uint_as_float((d & 1) ? w[d >> 1] & 0xffff0000u : w[d >> 1] << 16) * inv;
+            if (!(fabsf(v[d]) < INFINITY)) v[d] = __int_as_float(0x7fc00000);  // an infinite query is NaN
           }
-          t1w[c] = a[0] | a[1] << 16;
-          t2w[c] = b[0] | b[1] << 16;
+          split_e4m3x4<false>(v[0], v[1], v[2], v[3], t1w[c], t2w[c]);
         }
         const int ph = D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3);
         unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + r * D + ph * 16;
@@ -715,11 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               pr[i] = ex2(e[cb + c + i]);
               l[cb + c + i] = fmaf(pr[i], sc.z, l[cb + c + i]);
             }
-            uint32_t a0, a1, b0, b1;
-            split_e4m3x2<true>(pr[0], pr[1], a0, b0);
-            split_e4m3x2<true>(pr[2], pr[3], a1, b1);
-            w1[c / 4] = a0 | a1 << 16;
-            w2[c / 4] = b0 | b1 << 16;
+            split_e4m3x4<true>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
           }
           const int sw = lane & 7;
           if constexpr (CB == 16) {
