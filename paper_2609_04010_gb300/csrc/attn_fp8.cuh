@@ -63,32 +63,48 @@ __device__ __forceinline__ void write_fp8_lse(const AttnParams& p, int b, int g,
   p.lse[(static_cast<int64_t>(b) * p.gamma + j) * p.hq + h] = fp8_lse(m, l);
 }
 
-// The partials of one unit in slots [slot0, slot0 + nslots): rows [row0, row0 + nrows) of
-// KV head g are merged and written, row r from slot row prow0 + r.
+// The partials of one unit in slots [slot0, slot0 + nslots): rows [row0, row0 + nrows) of KV
+// heads g .. g + nheads - 1 (a head's rows after another's in a slot) are merged and written.
+// A thread takes a (row, 8 columns) item; the loads of up to four slots are in flight
+// together.
 template <int D>
-__device__ void merge_fp8_unit(const AttnParams& p, int b, int g, int row0, int nrows, int64_t slot0,
-                               int nslots, int tid, int nthreads, int prow0 = 0) {
-  constexpr int C8 = D / 8;
-  for (int idx = tid; idx < nrows * C8; idx += nthreads) {
-    const int r = idx / C8, c8 = idx % C8;
+__device__ void merge_fp8_unit(const AttnParams& p, int b, int g, int nheads, int row0, int nrows,
+                               int64_t slot0, int nslots, int tid, int nthreads) {
+  constexpr int C8 = D / 8, SB = 4;
+  for (int idx = tid; idx < nheads * nrows * C8; idx += nthreads) {
+    const int hr = idx / C8, c8 = idx % C8;
+    const int head = hr / nrows, r = hr - head * nrows;
     float M = -INFINITY, L = 0.f, acc[8];
     bool bad = false;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    for (int s = 0; s < nslots; ++s) {
-      const int64_t row = (slot0 + s) * p.slot_rows + prow0 + r;
-      const float2 ml = __ldcg(&p.partial_ml[row]);
-      const float4* src = reinterpret_cast<const float4*>(p.partial_o + row * D) + 2 * c8;
-      const float4 lo = __ldcg(src), hi = __ldcg(src + 1);
-      if (ml.y < 0.f) bad = true;
-      if (ml.y == 0.f) continue;
-      const float m = fmaxf(M, ml.x);
-      const float old = M == -INFINITY ? 0.f : ex2(M - m), w = m == -INFINITY ? ml.y : ex2(ml.x - m);
-      L = L * old + ml.y * w;
-      const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    for (int s0 = 0; s0 < nslots; s0 += SB) {
+      float2 ml[SB];
+      float4 lo[SB], hi[SB];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = acc[e] * old + x[e] * w;
-      M = m;
+      for (int i = 0; i < SB; ++i) {
+        ml[i] = make_float2(-INFINITY, 0.f);
+        lo[i] = hi[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s0 + i < nslots) {
+          const int64_t row = (slot0 + s0 + i) * p.slot_rows + hr;
+          const float4* src = reinterpret_cast<const float4*>(p.partial_o + row * D) + 2 * c8;
+          ml[i] = __ldcg(&p.partial_ml[row]);
+          lo[i] = __ldcg(src);
+          hi[i] = __ldcg(src + 1);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < SB; ++i) {
+        if (ml[i].y < 0.f) bad = true;
+        if (ml[i].y == 0.f) continue;  // saw no key
+        const float m = fmaxf(M, ml[i].x);
+        const float old = M == -INFINITY ? 0.f : ex2(M - m), w = m == -INFINITY ? 1.f : ex2(ml[i].x - m);
+        L = L * old + ml[i].y * w;
+        const float x[8] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w, hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = acc[e] * old + x[e] * w;
+        M = m;
+      }
     }
     if (bad) L = -1.f;
     const float inv = fp8_inv(L);
@@ -96,8 +112,8 @@ __device__ void merge_fp8_unit(const AttnParams& p, int b, int g, int row0, int 
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = 0.f;
     }
-    write_out_row<D>(p, b, g, row0 + r, c8 * 8, acc, inv);
-    if (c8 == 0) write_fp8_lse(p, b, g, row0 + r, M, L);
+    write_out_row<D>(p, b, g + head, row0 + r, c8 * 8, acc, inv);
+    if (c8 == 0) write_fp8_lse(p, b, g + head, row0 + r, M, L);
   }
 }
 #endif

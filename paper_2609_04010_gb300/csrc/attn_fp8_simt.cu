@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(NT) attn_fp8_simt_kernel(AttnFp8Params p) {
   __syncthreads();
   if (!sm.last) return;
   __threadfence();
-  merge_fp8_unit<D>(p, b, g, row0, nrows, unit * p.nsplit, p.nsplit, tid, NT);
+  merge_fp8_unit<D>(p, b, g, 1, row0, nrows, unit * p.nsplit, p.nsplit, tid, NT);
 }
 
 template <int D>

@@ -23,7 +23,8 @@
 // A block serves two sub-units of at most 64 query rows: two adjacent KV heads (HP = 2, one
 // box brings K and V of both: 8 KB with 16-token pages and D = 128), or two halves of one KV
 // head's rows (HP = 1). Warp roles (persistent, one block per SM):
-//   warp 16      producer: page ids and scales 32 pages ahead, one TMA box per page
+//   warps 16,19  producers: page ids and scales 32 pages ahead, one TMA box per page, each
+//                the half of a tile's pages
 //   warp 17      issues S^T = K Q^T into two S buffers per sub-unit in TMEM
 //   warp 18      issues O^T += V^T P^T; clears V of keys past the sequence's end
 //   warps 0..15  softmax, eight per sub-unit: lane quadrant = 32 keys, two warps per quadrant
@@ -47,8 +48,9 @@ using namespace tcx;
 constexpr int TK = kFp8KeyTile;  // keys per tile
 
 constexpr int NH = 2;  // sub-units of a block
+constexpr int kFlagRing = 16;  // segments' flags: more than the stages that producers run ahead
 constexpr int kSoftWarps = 8 * NH;
-constexpr int kThreads = 32 * (kSoftWarps + 3);  // 19 warps: 104 registers a thread
+constexpr int kThreads = 32 * (kSoftWarps + 4);
 
 // NR: query rows of a sub-unit (N of the first product), 16, 32 or 64.
 template <int D, int HP, int NR>
@@ -76,11 +78,11 @@ struct Cfg {
   static constexpr uint32_t OFF_INV = OFF_ROW + NH * NR * 8;         // float [NH][NR]: their factors
   static constexpr uint32_t OFF_BAR = OFF_INV + NH * NR * 4;
   // full[NST], empty[NST], s_full[NH][SB], s_free[NH][SB], p_full[NH], pv_done[NH],
-  // seg_ready[NH], drain[2], flag_ready[8]
-  static constexpr int NBAR = 2 * NST + 2 * NH * SB + 3 * NH + 2 + 8;
+  // seg_ready[NH], drain[2], flag_ready[kFlagRing]
+  static constexpr int NBAR = 2 * NST + 2 * NH * SB + 3 * NH + 2 + kFlagRing;
   static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, pending, -, NaN flags
-  static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;       // int [8]: bad flags of segments
-  static constexpr uint32_t OFF_PEND = OFF_FLAG + 32;       // int [2][8]
+  static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;               // int [2][kFlagRing]: segments' bad flags
+  static constexpr uint32_t OFF_PEND = OFF_FLAG + 8 * kFlagRing;    // int [2][8]
   static constexpr uint32_t OFF_QMAX = OFF_PEND + 64;       // uint32 [NH][8]
   static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 32;    // int [batch + 1]
   static constexpr uint32_t S_COL = 0;                      // [NH][SB][NR]
@@ -93,6 +95,9 @@ struct Cfg {
 // ---------------------------------------------------------------------------------
 // PTX wrappers
 // ---------------------------------------------------------------------------------
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 // One page of HP KV heads, keys and values (encode_fp8_map's box).
 __device__ __forceinline__ void tma_load_page8(uint32_t dst, const CUtensorMap* map, int kind_head, uint32_t bar) {
   asm volatile(
@@ -227,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
   volatile int* pend_count = reinterpret_cast<volatile int*>(misc + 2);
   volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 4);  // [NH]
-  volatile int* seg_flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);
+  volatile int* seg_flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);  // [producer][kFlagRing]
   int* pend = reinterpret_cast<int*>(smem + C::OFF_PEND);
   int* pb = reinterpret_cast<int*>(smem + C::OFF_PB);
 
@@ -238,26 +243,19 @@ __global__ void __launch_bounds__(kThreads, 1)
   // softmax warps whose rows are all padding take no part
   const int nsoft = sub_rows > NC ? 8 : 4;  // per sub-unit
 
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < NST; ++s) {
-      mbar_init(full(s), 1);
-      mbar_init(empty(s), 1);
+  if (warp == 0) {
+    for (int i = lane; i < C::NBAR; i += 32) {
+      constexpr int b_sfree = 2 * NST + NH * SB, b_pfull = b_sfree + NH * SB, b_pv = b_pfull + NH, b_seg = b_pv + NH;
+      constexpr int b_drain = b_seg + NH, b_flag = b_drain + 2;
+      const int n = i < NST || i >= b_flag ? 2                                                       // full, flag_ready
+                    : (i >= b_sfree && i < b_pv) || (i >= b_seg && i < b_drain) ? nsoft : 1;  // s_free, p_full, seg_ready
+      mbar_init(bar0 + 8u * i, n);
     }
-    for (int h = 0; h < NH; ++h) {
-      for (int b = 0; b < SB; ++b) {
-        mbar_init(s_full(h, b), 1);
-        mbar_init(s_free(h, b), nsoft);
-      }
-      mbar_init(p_full(h), nsoft);
-      mbar_init(pv_done(h), 1);
-      mbar_init(seg_ready(h), nsoft);
-      nan_flag[h] = 0;
+    if (lane < NH) nan_flag[lane] = 0;
+    if (lane == 0) {
+      *abort_flag = 0;
+      *pend_count = 0;
     }
-    mbar_init(drain_bar(0), 1);
-    mbar_init(drain_bar(1), 1);
-    for (int i = 0; i < 8; ++i) mbar_init(flag_bar(i), 1);
-    *abort_flag = 0;
-    *pend_count = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = threadIdx.x; i < NH * D; i += kThreads) nanv[i] = 0ull;
@@ -298,8 +296,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int64_t t1 = cta < ctas ? static_cast<int64_t>(cta + 1) * total / ctas : 0;
   const int OVH = p.unit_overhead;
 
-  if (warp == kSoftWarps) {
-    // ============================ producer ============================
+  if (warp == kSoftWarps || warp == kSoftWarps + 3) {
+    // ============================ producers ============================
+    const int half = warp == kSoftWarps ? 0 : 1;
     uint32_t it = 0, seg_no = 0;
     bool ok = true;
     const int psh = __ffs(p.page_size) - 1;  // log2
@@ -321,11 +320,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int h = 0; h < HP; ++h) sc[h] = __ldg(src + h);
       };
-      int id = load_id(first), id1 = load_id(first + 32), base = first;
+      int base = first, id = load_id(first), id1 = load_id(first + 32), id2 = load_id(first + 64);
       float2 sc[HP], sc1[HP];
       load_scale(id, sc);
       load_scale(id1, sc1);
-      int id2 = load_id(first + 64);
       for (int k = 0; k < s.ntile && ok; ++k, ++it) {
         const uint32_t st = it % NST;
         const int pg0 = first + k * npg;
@@ -341,35 +339,35 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (it >= NST) ok = mbar_wait(empty(st), ((it / NST) - 1) & 1, abort_flag, p.status);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        // lanes [pg0 - base, + npg) hold this tile's pages
+        // lanes [pg0 - base, + npg) hold this tile's pages; this warp copies the half
+        // [q0, q1) of them
+        const int q0 = half * (npg >> 1), q1 = min(q0 + (npg >> 1), pages - pg0);
+        const uint32_t dst = sbase + C::OFF_STAGE + st * C::STAGE;
+        if (lane == 0 && q1 > q0) mbar_expect_tx(full(st), static_cast<uint32_t>(q1 - q0) * box_bytes);
+        for (int q = q0; q < q1; ++q) {
+          const int raw = __shfl_sync(0xffffffffu, id, pg0 - base + q);
+          const bool in_range = raw >= 0 && raw < p.num_pages;
+          flag |= !in_range;
+          if (lane == 0)
+            tma_load_page8(dst + static_cast<uint32_t>(q) * box_bytes, &tmap,
+                           2 * ((in_range ? raw : 0) * p.hkv + s.g * HP), full(st));
+        }
         const int q = base + lane - pg0;
-        const bool mine = q >= 0 && q < npg;
-        const bool valid = mine && pg0 + q < pages;
-        const bool in_range = id >= 0 && id < p.num_pages;
-        flag |= __any_sync(0xffffffffu, valid && !in_range);
-        if (mine) {
+        if (q >= q0 && q < q0 + (npg >> 1)) {
 #pragma unroll
           for (int h = 0; h < HP; ++h) {
             const float sv = clamp_scale(sc[h].y);
-            scl[(st * 8 + q) * HP + h] = valid ? make_float4(sc[h].x * p.scale_log2, log2f(sv), 1.f / sv, 0.f)
-                                               : make_float4(0.f, 0.f, 0.f, 0.f);
+            scl[(st * 8 + q) * HP + h] = q < q1 ? make_float4(sc[h].x * p.scale_log2, __log2f(sv), __frcp_rn(sv), 0.f)
+                                                : make_float4(0.f, 0.f, 0.f, 0.f);
           }
         }
-        const uint32_t nvalid = __popc(__ballot_sync(0xffffffffu, valid));
         __syncwarp();
-        if (lane == 0) {
-          if (nvalid) mbar_arrive_tx(full(st), nvalid * box_bytes);
-          else mbar_arrive(full(st));
-        }
-        __syncwarp();
-        if (valid)
-          tma_load_page8(sbase + C::OFF_STAGE + st * C::STAGE + static_cast<uint32_t>(q) * box_bytes, &tmap,
-                         2 * ((in_range ? id : 0) * p.hkv + s.g * HP), full(st));
+        if (lane == 0) mbar_arrive(full(st));
         __syncwarp();
       }
       if (ok && lane == 0) {
-        seg_flag[seg_no & 7] = flag ? 1 : 0;
-        mbar_arrive(flag_bar(seg_no & 7));
+        seg_flag[half * kFlagRing + seg_no % kFlagRing] = flag ? 1 : 0;
+        mbar_arrive(flag_bar(seg_no % kFlagRing));
       }
       if (!has_more(s, t1, OVH)) break;
       s = locate<TK>(s.vnext, t1, p, pb, OVH);
@@ -647,27 +645,33 @@ __global__ void __launch_bounds__(kThreads, 1)
         // e = log2 of the key's weight and value scale for each row, over the row's
         // reference; hidden keys have none
         float e[NC];
-        for (bool raised = false;; raised = true) {
-          tmem_wait_ld();
-          float top = -INFINITY;
+        auto exponents = [&](const uint32_t* r) {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(raw[c]), ks, sc.y) - mr[c];
+          for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(r[c]), ks, sc.y) - mr[c];
           if (masked) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) e[c] = (seen >> c & 1) ? e[c] : -INFINITY;
           }
+        };
+        tmem_wait_ld();
+        exponents(raw);
+        float top = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) top = fmaxf(top, e[c]);
-          if (raised || !group_any(gbar, top > 8.f)) break;
+        for (int c = 0; c < NC; ++c) top = fmaxf(top, e[c]);
+        if (group_any(gbar, top > 8.f)) {
           // Some weight would pass 2^8: raise the references, so that each row's largest
           // weight so far becomes 2^2 where it was more.
           float mx = -INFINITY;
-          tmem_ld<NC>(s_tmem, raw);
-          tmem_wait_ld();
+#pragma unroll 1
+          for (int c8 = 0; c8 < NC; c8 += 8) {
+            uint32_t t8[8];
+            tmem_ld8(s_tmem + c8, t8);
+            tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            const float m = warp_max((seen >> c & 1) ? fmaf(__uint_as_float(raw[c]), ks, sc.y) : -INFINITY);
-            if (lane % NC == c) mx = m;
+            for (int c = 0; c < 8; ++c) {
+              const float m = warp_max((seen >> (c8 + c) & 1) ? fmaf(__uint_as_float(t8[c]), ks, sc.y) : -INFINITY);
+              if (lane % NC == c8 + c) mx = m;
+            }
           }
           float* const xc = xch + ch * NC + lane % NC;
           if (lane < NC) xc[q4 * NR] = mx;
@@ -682,20 +686,24 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_after();
 #pragma unroll 1
             for (int c8 = 0; c8 < 2 * NC; c8 += 8) {
+              uint32_t t8[8];
               const uint32_t col = o_col + (c8 / NC) * NR + c8 % NC;
-              tmem_ld8(col, raw);
+              tmem_ld8(col, t8);
               tmem_wait_ld();
 #pragma unroll
               for (int c = 0; c < 8; ++c)
-                raw[c] = __float_as_uint(__uint_as_float(raw[c]) * __shfl_sync(0xffffffffu, alpha, c8 % NC + c));
-              tmem_st8(col, raw);
+                t8[c] = __float_as_uint(__uint_as_float(t8[c]) * __shfl_sync(0xffffffffu, alpha, c8 % NC + c));
+              tmem_st8(col, t8);
             }
             tmem_wait_st();
           }
 #pragma unroll
           for (int c = 0; c < NC; ++c) l[c] *= __shfl_sync(0xffffffffu, alpha, c);
-          tmem_ld<NC>(s_tmem, raw);
           bar_sync(gbar, 128);
+          uint32_t again[NC];
+          tmem_ld<NC>(s_tmem, again);
+          tmem_wait_ld();
+          exponents(again);
         }
         tc_fence_before();
         __syncwarp();
@@ -748,8 +756,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         s.ntile = 0;
       }
       // ---- the unit's (or the part's) sums and outputs ----
-      wait(flag_bar(seg_no & 7), (seg_no >> 3) & 1);
-      const bool bad = seg_flag[seg_no & 7] != 0;
+      wait(flag_bar(seg_no % kFlagRing), (seg_no / kFlagRing) & 1);
+      const bool bad = (seg_flag[seg_no % kFlagRing] | seg_flag[kFlagRing + seg_no % kFlagRing]) != 0;
       const bool whole = c.tile0 == 0 && c.ntile == c.unit_tiles;
       const int64_t slot = c.u + cta;
       if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
@@ -828,21 +836,18 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (np == 0) return;
   __threadfence();
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < np; ++i) {
-      int* e = pend + 8 * i;
-      const uint32_t prev = atomicAdd(&p.tickets[e[6]], 1u);
-      e[7] = prev == static_cast<uint32_t>(e[5] - 1);
-      if (e[7]) p.tickets[e[6]] = 0;
-    }
+  if (threadIdx.x < np) {
+    int* e = pend + 8 * threadIdx.x;
+    const uint32_t prev = atomicAdd(&p.tickets[e[6]], 1u);
+    e[7] = prev == static_cast<uint32_t>(e[5] - 1);
+    if (e[7]) p.tickets[e[6]] = 0;
   }
   __syncthreads();
   for (int i = 0; i < np; ++i) {
     const int* e = pend + 8 * i;
     if (!e[7]) continue;
     __threadfence();
-    for (int h = 0; h < HP; ++h)
-      merge_fp8_unit<D>(p, e[0], e[1] * HP + h, e[2], e[3], e[4], e[5], threadIdx.x, kThreads, h * sub_rows);
+    merge_fp8_unit<D>(p, e[0], e[1] * HP, HP, e[2], e[3], e[4], e[5], threadIdx.x, kThreads);
   }
 }
 
