@@ -1,12 +1,12 @@
 // Penalties for repeated tokens, biases and grammar masks on logits rows
 // (spec_adjust_logits).
 //
-// A block takes a slice of the vocabulary of one sequence, for all of its rows. It counts
-// the history's tokens of the slice in shared memory once (integer atomics, so the counts
-// do not depend on their order) and then streams the rows: almost every group of eight
-// logits has no counted and no biased token, which one bit per group says, and is copied
-// under its eight mask bits; the few others take the formula with the counts. A group that
-// the mask hides whole is written without being read. The logits are read and written once.
+// A block takes 2,048 tokens of the vocabulary of one sequence, for all of its rows, a thread
+// eight of them. It counts the history's tokens of its range in shared memory once (integer
+// atomics, so the counts do not depend on their order); a thread whose tokens are neither
+// counted nor biased, which is nearly every one, then only copies its logits under their mask
+// bits, the others take the formula. Eight logits that the mask hides together are written
+// without being read. The logits are read and written once; memory bounds it.
 #include <cuda_bf16.h>
 
 #include <cmath>
@@ -17,49 +17,63 @@ namespace specv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxSlice = 4096;  // tokens of a block: 32 KB of counts and bias places
-constexpr uint32_t kPrompt = 0x80000000u;
+constexpr int kSlice = kThreads * 8;  // tokens of a block
+constexpr uint32_t kPrompt = 0x80000000u, kBlock = 0x40000000u, kBias = 0x20000000u;  // beside a count
+constexpr uint32_t kCount = 0x1fffffffu;
 
-struct AdjustParams {
-  spec_adjust_args_t a;
-  int slice, nmask;
+template <typename T>
+__device__ __forceinline__ float to_f32(T x);
+template <>
+__device__ __forceinline__ float to_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// Eight logits of a thread, as the 16-byte words they are loaded and stored in.
+template <typename T>
+struct Eight {
+  static constexpr int kWords = static_cast<int>(sizeof(T)) / 2;
+  union {
+    uint4 w[kWords];
+    T x[8];
+  };
+  __device__ Eight() {}
 };
-
-__device__ __forceinline__ float load_logit(const float* p) { return *p; }
-__device__ __forceinline__ float load_logit(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void store_logit(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_logit(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
 struct Seq {
   float rep, freq, pres;
   const float* bias;  // the sequence's bias values
 };
 
-// The formula for one logit; c = count word, bi = place in the bias list (or none).
+// The formula for one logit; c = its count word, bi = its place in the bias list.
 __device__ __forceinline__ float adjust_one(float x, int v, uint32_t c, uint32_t bi, const Seq& q,
                                             const int* btok, int nblk) {
-  int cnt = static_cast<int>(c & ~kPrompt);
-  for (int i = 0; i < nblk; ++i) cnt += btok[i] == v;
+  int cnt = static_cast<int>(c & kCount);
+  if (c & kBlock)
+    for (int i = 0; i < nblk; ++i) cnt += btok[i] == v;
   if (cnt > 0 || (c & kPrompt)) x = x > 0.f ? __fdiv_rn(x, q.rep) : __fmul_rn(x, q.rep);
   if (cnt > 0) {
     x = __fsub_rn(x, __fmul_rn(q.freq, static_cast<float>(cnt)));
     x = __fsub_rn(x, q.pres);
   }
-  if (bi != 0xffffffffu) x = __fadd_rn(x, __ldg(q.bias + bi));
+  if (c & kBias) x = __fadd_rn(x, __ldg(q.bias + bi));
   return x;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) adjust_kernel(AdjustParams p) {
-  extern __shared__ __align__(16) uint32_t smem[];
-  const spec_adjust_args_t& a = p.a;
-  const int S = p.slice;
-  uint32_t* count = smem;              // [S]: output count, bit 31 = in the prompt
-  uint32_t* place = count + S;         // [S]: first place in the bias list
-  uint32_t* dirty = place + S;         // [S / 256]: one bit per eight tokens
+// VEC: rows are 16-byte aligned and a thread's eight tokens are consecutive; otherwise they
+// are 32 apart, so that a warp's loads of one element each are.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) {
+  __shared__ __align__(16) uint32_t count[kSlice];  // output count and flags
+  __shared__ uint32_t place[kSlice];                // first place in the bias list
   __shared__ int btok[64];
   const int tid = threadIdx.x, b = blockIdx.y;
-  const int v0 = blockIdx.x * S, nv = min(S, a.vocab - v0);
+  const int v0 = blockIdx.x * kSlice, nv = min(kSlice, a.vocab - v0);
   const int G = a.gamma;
   Seq q;
   q.rep = a.repetition ? a.repetition[b] : 1.f;
@@ -67,76 +81,141 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(AdjustParams p) {
   q.pres = a.presence ? a.presence[b] : 0.f;
   q.bias = a.bias_values + static_cast<int64_t>(b) * a.max_bias;
   const bool penal = q.rep != 1.f || q.freq != 0.f || q.pres != 0.f;
-  for (int i = tid; i < S; i += kThreads) {
-    count[i] = 0;
-    place[i] = 0xffffffffu;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    reinterpret_cast<uint4*>(count)[tid + i * kThreads] = make_uint4(0, 0, 0, 0);
   }
-  for (int i = tid; i < S / 256; i += kThreads) dirty[i] = 0;
-  if (tid < 64) btok[tid] = a.block_tokens && tid < G ? a.block_tokens[b * G + tid] : -1;
+  if (a.bias_tokens)
+    for (int i = tid; i < kSlice; i += kThreads) place[i] = 0xffffffffu;
+  if (tid < 64) btok[tid] = a.block_tokens && tid < G ? a.block_tokens[static_cast<int64_t>(b) * G + tid] : -1;
   __syncthreads();
-  auto mark = [&](int u) { atomicOr(&dirty[u >> 8], 1u << ((u >> 3) & 31)); };
+  const auto index = [&](int token) { return static_cast<uint32_t>(token) - static_cast<uint32_t>(v0); };
   if (penal && a.history) {
     const int hl = min(max(a.history_len[b], 0), a.max_history);
     const int pl = a.prompt_len ? min(max(a.prompt_len[b], 0), hl) : 0;
     const int32_t* h = a.history + static_cast<int64_t>(b) * a.max_history;
-    for (int i = tid; i < hl; i += kThreads) {
-      const uint32_t u = static_cast<uint32_t>(__ldg(h + i)) - static_cast<uint32_t>(v0);
-      if (u >= static_cast<uint32_t>(nv)) continue;
-      if (i < pl) atomicOr(&count[u], kPrompt); else atomicAdd(&count[u], 1u);
-      mark(u);
+    auto add = [&](int token, int i) {
+      const uint32_t u = index(token);
+      if (u >= static_cast<uint32_t>(nv)) return;
+      if (i < pl) atomicOr(&count[u], kPrompt);
+      else atomicAdd(&count[u], 1u);
+    };
+    int i = tid;
+    for (; i + 3 * kThreads < hl; i += 4 * kThreads) {  // four loads in flight
+      int t[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = __ldg(h + i + e * kThreads);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) add(t[e], i + e * kThreads);
     }
+    for (; i < hl; i += kThreads) add(__ldg(h + i), i);
   }
   if (penal && tid < G) {
-    const uint32_t u = static_cast<uint32_t>(btok[tid]) - static_cast<uint32_t>(v0);
-    if (u < static_cast<uint32_t>(nv)) mark(u);
+    const uint32_t u = index(btok[tid]);
+    if (u < static_cast<uint32_t>(nv)) atomicOr(&count[u], kBlock);
   }
   if (a.bias_tokens) {
     const int32_t* t = a.bias_tokens + static_cast<int64_t>(b) * a.max_bias;
     for (int i = tid; i < a.max_bias; i += kThreads) {
-      const uint32_t u = static_cast<uint32_t>(__ldg(t + i)) - static_cast<uint32_t>(v0);
+      const uint32_t u = index(__ldg(t + i));
       if (u >= static_cast<uint32_t>(nv)) continue;
       atomicMin(&place[u], static_cast<uint32_t>(i));
-      mark(u);
+      atomicOr(&count[u], kBias);
     }
   }
   __syncthreads();
-  const T* in = static_cast<const T*>(a.logits);
-  T* out = static_cast<T*>(a.out);
-  const int groups = (nv + 7) / 8;
-  for (int64_t it = tid; it < static_cast<int64_t>(groups) * G; it += kThreads) {
-    const int j = static_cast<int>(it / groups), g = static_cast<int>(it % groups);
-    const int64_t row = static_cast<int64_t>(b) * G + j;
-    const uint32_t* mask = a.allowed ? a.allowed + row * p.nmask : nullptr;
-    const bool slow = dirty[g >> 5] >> (g & 31) & 1;
-    const int nblk = penal ? (a.block_shift ? j : j + 1) : 0;
-    for (int e = 0; e < 8; ++e) {
-      const int u = g * 8 + e;
-      if (u >= nv) break;
-      const int v = v0 + u;
-      const int64_t at = row * a.vocab + v;
-      if (mask && !(__ldg(mask + (v >> 5)) >> (v & 31) & 1)) {
-        store_logit(out + at, -INFINITY);
-        continue;
+  // this thread's tokens u(e) of the range
+  const int u0 = VEC ? tid * 8 : (tid >> 5) * 256 + (tid & 31);
+  constexpr int kStep = VEC ? 1 : 32;
+  if (u0 >= nv) return;
+  uint32_t touched = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) touched |= count[u0 + e * kStep];
+  const int nmask = (a.vocab - 1) / 32 + 1;
+  const T* in = static_cast<const T*>(a.logits) + static_cast<int64_t>(b) * G * a.vocab + v0 + u0;
+  T* out = static_cast<T*>(a.out) + static_cast<int64_t>(b) * G * a.vocab + v0 + u0;
+  const uint32_t* mask = a.allowed ? a.allowed + static_cast<int64_t>(b) * G * nmask : nullptr;
+  const int word0 = (v0 + (VEC ? u0 : (tid >> 5) * 256)) >> 5;
+  constexpr int U = VEC ? 8 / Eight<T>::kWords : 2;  // rows in flight
+  for (int j0 = 0; j0 < G; j0 += U) {
+    uint32_t keep[U];  // the mask's eight bits for each row
+#pragma unroll
+    for (int r = 0; r < U; ++r) {
+      keep[r] = j0 + r < G ? 0xffu : 0u;
+      if (mask && j0 + r < G) {
+        const uint32_t* w = mask + static_cast<int64_t>(j0 + r) * nmask + word0;
+        if (VEC) {
+          keep[r] = __ldg(reinterpret_cast<const uint8_t*>(w) + ((u0 >> 3) & 3));
+        } else {
+          keep[r] = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (u0 + e * 32 < nv) keep[r] |= (__ldg(w + e) >> (tid & 31) & 1u) << e;
+        }
       }
-      float x = load_logit(in + at);
-      if (slow) x = adjust_one(x, v, count[u], place[u], q, btok, nblk);
-      store_logit(out + at, x);
+    }
+    Eight<T> x[U];
+#pragma unroll
+    for (int r = 0; r < U; ++r) {
+      if (!keep[r]) continue;
+      const T* src = in + static_cast<int64_t>(j0 + r) * a.vocab;
+      if (VEC) {
+#pragma unroll
+        for (int w = 0; w < Eight<T>::kWords; ++w) x[r].w[w] = __ldcs(reinterpret_cast<const uint4*>(src) + w);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (u0 + e * 32 < nv) x[r].x[e] = src[e * 32];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < U; ++r) {
+      if (j0 + r >= G) break;
+      if (touched && keep[r]) {
+        const int nblk = a.block_shift ? j0 + r : j0 + r + 1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int u = u0 + e * kStep;
+          const uint32_t c = count[u];
+          if (c && (keep[r] >> e & 1))
+            x[r].x[e] = from_f32<T>(adjust_one(to_f32<T>(x[r].x[e]), v0 + u, c, place[u], q, btok, nblk));
+        }
+      }
+      if (keep[r] != 0xffu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!(keep[r] >> e & 1)) x[r].x[e] = from_f32<T>(-INFINITY);
+      }
+      T* dst = out + static_cast<int64_t>(j0 + r) * a.vocab;
+      if (VEC) {
+#pragma unroll
+        for (int w = 0; w < Eight<T>::kWords; ++w) __stcs(reinterpret_cast<uint4*>(dst) + w, x[r].w[w]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (u0 + e * 32 < nv) dst[e * 32] = x[r].x[e];
+      }
     }
   }
+}
+
+template <typename T>
+void launch_typed(const spec_adjust_args_t& a, bool vec, cudaStream_t stream) {
+  const dim3 grid((a.vocab - 1) / kSlice + 1, a.batch);
+  if (vec) adjust_kernel<T, true><<<grid, kThreads, 0, stream>>>(a);
+  else adjust_kernel<T, false><<<grid, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
 
 cudaError_t launch_adjust(const spec_adjust_args_t& a, cudaStream_t stream) {
-  AdjustParams p;
-  p.a = a;
-  p.slice = kMaxSlice;
-  p.nmask = (a.vocab - 1) / 32 + 1;
-  const dim3 grid((a.vocab - 1) / p.slice + 1, a.batch);
-  const size_t smem = (2 * p.slice + p.slice / 256) * sizeof(uint32_t);
+  const size_t esz = a.logits_dtype == SPEC_BF16 ? 2 : 4;
+  // whole groups of eight in aligned rows
+  const bool vec = a.vocab % 8 == 0 &&
+                   ((reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.out)) & 15u) == 0;
   (void)cudaGetLastError();
-  if (a.logits_dtype == SPEC_BF16) adjust_kernel<__nv_bfloat16><<<grid, kThreads, smem, stream>>>(p);
-  else adjust_kernel<float><<<grid, kThreads, smem, stream>>>(p);
+  if (esz == 2) launch_typed<__nv_bfloat16>(a, vec, stream);
+  else launch_typed<float>(a, vec, stream);
   return cudaGetLastError();
 }
 
