@@ -1,12 +1,14 @@
 // Penalties for repeated tokens, biases and grammar masks on logits rows
 // (spec_adjust_logits).
 //
-// A block takes 2,048 tokens of the vocabulary of one sequence, for all of its rows, a thread
-// eight of them. It counts the history's tokens of its range in shared memory once (integer
-// atomics, so the counts do not depend on their order); a thread whose tokens are neither
-// counted nor biased, which is nearly every one, then only copies its logits under their mask
-// bits, the others take the formula. Eight logits that the mask hides together are written
-// without being read. The logits are read and written once; memory bounds it.
+// A block takes 2,048 tokens of the vocabulary of one sequence, for all of its rows. It counts
+// the history's tokens of its range in shared memory once (integer atomics, so the counts do
+// not depend on their order) and lists the tokens that are counted or biased. It then copies
+// its logits under their mask bits, eight a thread (eight that the mask hides together are
+// written without being read), and last rewrites the listed tokens, shared out over all
+// threads: a few in a hundred logits, but so spread that handled in the copy they would hold
+// up most warps (353 us at 64 x 16 x 128,256). The logits are read and written once; memory
+// bounds it.
 #include <cuda_bf16.h>
 
 #include <cmath>
@@ -71,6 +73,8 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) {
   __shared__ __align__(16) uint32_t count[kSlice];  // output count and flags
   __shared__ uint32_t place[kSlice];                // first place in the bias list
+  __shared__ uint16_t list[kSlice];                 // the tokens with a count or a bias
+  __shared__ int nlist;
   __shared__ int btok[64];
   const int tid = threadIdx.x, b = blockIdx.y;
   const int v0 = blockIdx.x * kSlice, nv = min(kSlice, a.vocab - v0);
@@ -87,6 +91,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
   }
   if (a.bias_tokens)
     for (int i = tid; i < kSlice; i += kThreads) place[i] = 0xffffffffu;
+  if (tid == 0) nlist = 0;
   if (tid < 64) btok[tid] = a.block_tokens && tid < G ? a.block_tokens[static_cast<int64_t>(b) * G + tid] : -1;
   __syncthreads();
   const auto index = [&](int token) { return static_cast<uint32_t>(token) - static_cast<uint32_t>(v0); };
@@ -124,20 +129,18 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
     }
   }
   __syncthreads();
-  // this thread's tokens u(e) of the range
-  const int u0 = VEC ? tid * 8 : (tid >> 5) * 256 + (tid & 31);
-  constexpr int kStep = VEC ? 1 : 32;
-  if (u0 >= nv) return;
-  uint32_t touched = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) touched |= count[u0 + e * kStep];
+  for (int e = 0; e < 8; ++e)
+    if (count[tid + e * kThreads]) list[atomicAdd(&nlist, 1)] = static_cast<uint16_t>(tid + e * kThreads);
   const int nmask = (a.vocab - 1) / 32 + 1;
-  const T* in = static_cast<const T*>(a.logits) + static_cast<int64_t>(b) * G * a.vocab + v0 + u0;
-  T* out = static_cast<T*>(a.out) + static_cast<int64_t>(b) * G * a.vocab + v0 + u0;
+  const T* in = static_cast<const T*>(a.logits) + static_cast<int64_t>(b) * G * a.vocab + v0;
+  T* out = static_cast<T*>(a.out) + static_cast<int64_t>(b) * G * a.vocab + v0;
   const uint32_t* mask = a.allowed ? a.allowed + static_cast<int64_t>(b) * G * nmask : nullptr;
+  // ---- the copy: this thread's tokens are u0 + e * (VEC ? 1 : 32) of the range ----
+  const int u0 = VEC ? tid * 8 : (tid >> 5) * 256 + (tid & 31);
   const int word0 = (v0 + (VEC ? u0 : (tid >> 5) * 256)) >> 5;
   constexpr int U = VEC ? 8 / Eight<T>::kWords : 2;  // rows in flight
-  for (int j0 = 0; j0 < G; j0 += U) {
+  for (int j0 = 0; j0 < (u0 < nv ? G : 0); j0 += U) {
     uint32_t keep[U];  // the mask's eight bits for each row
 #pragma unroll
     for (int r = 0; r < U; ++r) {
@@ -158,7 +161,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
 #pragma unroll
     for (int r = 0; r < U; ++r) {
       if (!keep[r]) continue;
-      const T* src = in + static_cast<int64_t>(j0 + r) * a.vocab;
+      const T* src = in + static_cast<int64_t>(j0 + r) * a.vocab + u0;
       if (VEC) {
 #pragma unroll
         for (int w = 0; w < Eight<T>::kWords; ++w) x[r].w[w] = __ldcs(reinterpret_cast<const uint4*>(src) + w);
@@ -171,22 +174,12 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
 #pragma unroll
     for (int r = 0; r < U; ++r) {
       if (j0 + r >= G) break;
-      if (touched && keep[r]) {
-        const int nblk = a.block_shift ? j0 + r : j0 + r + 1;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int u = u0 + e * kStep;
-          const uint32_t c = count[u];
-          if (c && (keep[r] >> e & 1))
-            x[r].x[e] = from_f32<T>(adjust_one(to_f32<T>(x[r].x[e]), v0 + u, c, place[u], q, btok, nblk));
-        }
-      }
       if (keep[r] != 0xffu) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (!(keep[r] >> e & 1)) x[r].x[e] = from_f32<T>(-INFINITY);
       }
-      T* dst = out + static_cast<int64_t>(j0 + r) * a.vocab;
+      T* dst = out + static_cast<int64_t>(j0 + r) * a.vocab + u0;
       if (VEC) {
 #pragma unroll
         for (int w = 0; w < Eight<T>::kWords; ++w) __stcs(reinterpret_cast<uint4*>(dst) + w, x[r].w[w]);
@@ -196,6 +189,16 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
           if (u0 + e * 32 < nv) dst[e * 32] = x[r].x[e];
       }
     }
+  }
+  // ---- the listed tokens (out already holds their logits, so it may be the input) ----
+  __syncthreads();
+  const int n = nlist;
+  for (int it = tid; it < n * G; it += kThreads) {
+    const int j = it / n, u = list[it - j * n];
+    if (mask && !(__ldg(mask + static_cast<int64_t>(j) * nmask + ((v0 + u) >> 5)) >> ((v0 + u) & 31) & 1u)) continue;
+    const int64_t at = static_cast<int64_t>(j) * a.vocab + u;
+    const int nblk = a.block_shift ? j : j + 1;
+    out[at] = from_f32<T>(adjust_one(to_f32<T>(out[at]), v0 + u, count[u], place[u], q, btok, nblk));
   }
 }
 

@@ -192,7 +192,7 @@ spec_status_t spec_append_kv_fp8(const spec_append_fp8_args_t* a, spec_stream_t 
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   DeviceScope scope(s);
   if (!scope.ok) return SPEC_ERR_CUDA;
-  return launch_append_fp8(*a, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+  return launch_append_fp8(*a, scope.sms, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }
 
 size_t spec_attn_fp8_workspace_size(const spec_attn_fp8_args_t* a) {

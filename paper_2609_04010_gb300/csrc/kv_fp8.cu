@@ -163,18 +163,19 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
 // ---------------------------------------------------------------------------------
 // Quantising write
 // ---------------------------------------------------------------------------------
-// A block takes kAppendRows rows of one KV head. A row that is the first of its page in
-// the window before it leads that page's rows; one warp per 16 places of the page (a group)
-// then holds the page's new keys or values in registers: one pass finds their largest
-// magnitude, from it the page's scale, and the same registers are rounded and stored.
-// HBM traffic is the new rows once and their 8-bit form once (a page whose scale grows is
-// read and written once more).
+// A block takes kAppendRows rows of some KV heads. A row that is the first of its page in the
+// window before it leads that page's rows; the block notes which row goes to each place of a
+// led page once, for all heads, K and V. A group of one warp per 16 places then holds a
+// page's new keys or values of one head in registers: one pass finds their largest
+// magnitude, from it the page's scale, and the same registers are rounded and stored. Groups
+// run free of each other. HBM traffic is the new rows once and their 8-bit form once (a page
+// whose scale grows is read and written once more); memory bounds it.
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 32;
 constexpr int kWin = SPEC_APPEND_WINDOW;
 
 struct AppendParams {
-  int rows, hkv, num_pages;
+  int rows, hkv, heads, num_pages;  // heads: per block
   int64_t k_stride, v_stride;
   const __nv_bfloat16* k;
   const __nv_bfloat16* v;
@@ -201,17 +202,18 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams
   __shared__ int32_t win[kAppendRows + 2 * kWin];   // slots of the rows around the block's
   __shared__ int32_t leaders[kAppendRows];
   __shared__ int nlead;
-  __shared__ int32_t row_of[GROUPS][P];             // row written to each place, or -1
-  __shared__ uint32_t amax[GROUPS][GW];
+  __shared__ int32_t row_of[kAppendRows][P];        // row written to each place of a led page, or -1
+  __shared__ uint32_t amax[GROUPS][2][GW];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int r0 = blockIdx.x * kAppendRows, head = blockIdx.y;
+  const int r0 = blockIdx.x * kAppendRows, head0 = blockIdx.y * p.heads;
+  const int nheads = min(p.heads, p.hkv - head0);
   const int64_t max_slot = static_cast<int64_t>(p.num_pages) * P;
   if (tid == 0) nlead = 0;
   for (int i = tid; i < kAppendRows + 2 * kWin; i += kAppendThreads) {
     const int64_t r = static_cast<int64_t>(r0) - kWin + i;
     int s = r >= 0 && r < p.rows ? p.slots[r] : -1;
     if (s >= max_slot) {
-      if (p.status && head == 0 && i >= kWin && i < kWin + kAppendRows)
+      if (p.status && head0 == 0 && i >= kWin && i < kWin + kAppendRows)
         set_status(p.status, SPEC_FLAG_BAD_PAGE);
       s = -1;
     }
@@ -226,99 +228,88 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams
       const int t = win[i + 1 + q];
       earlier |= t >= 0 && t / P == s / P;
     }
-    if (!__any_sync(0xffffffffu, earlier) && lane == 0) leaders[atomicAdd(&nlead, 1)] = i;
+    if (__any_sync(0xffffffffu, earlier)) continue;
+    int at = 0;
+    if (lane == 0) {
+      at = atomicAdd(&nlead, 1);
+      leaders[at] = s / P;
+    }
+    at = __shfl_sync(0xffffffffu, at, 0);
+    for (int q = lane; q < P; q += 32) row_of[at][q] = -1;
+    __syncwarp();
+    for (int q = lane; q < kWin; q += 32) {
+      const int t = win[kWin + i + q];
+      if (t >= 0 && t / P == s / P) row_of[at][t % P] = r0 + i + q;
+    }
   }
   __syncthreads();
-  const int items = nlead * 2;  // (leader, K or V)
+  const int items = nlead * nheads * 2;  // (leader, head, K or V)
   const int group = warp / GW, gwarp = warp % GW;
   const int sub = lane / LPR, piece = lane % LPR;
-  for (int it0 = 0; it0 < items; it0 += GROUPS) {
-    const int it = it0 + group;
-    const bool live = it < items;
-    const int li = live ? leaders[it >> 1] : 0, kind = it & 1;
-    const int page = live ? win[kWin + li] / P : 0;
-    for (int q = gwarp * 32 + lane; q < P; q += GW * 32) row_of[group][q] = -1;
-    __syncthreads();
-    if (live)
-      for (int q = gwarp * 32 + lane; q < kWin; q += GW * 32) {
-        const int s = win[kWin + li + q];
-        if (s >= 0 && s / P == page) row_of[group][s % P] = r0 + li + q;
-      }
-    __syncthreads();
-    uint4 x[STEPS];
-    uint32_t m = 0;
-    const __nv_bfloat16* src = kind ? p.v : p.k;
+  int turn = 0;
+  for (int it = group; it < items; it += GROUPS, turn ^= 1) {
+    const int kind = it & 1, lead = (it >> 1) / nheads, head = head0 + (it >> 1) - lead * nheads;
+    const int page = leaders[lead];
+    const int32_t* rows = row_of[lead];
+    const __nv_bfloat16* src = (kind ? p.v : p.k) + head * D + piece * 8;
     const int64_t stride = kind ? p.v_stride : p.k_stride;
-    uint32_t written = 0;
-    if (live) {
+    float* sp = p.scale + (static_cast<int64_t>(page) * p.hkv + head) * 2 + kind;
+    const bool anew = rows[0] >= 0;
+    const float old = anew ? kScaleMin : clamp_scale(*sp);
+    uint4 x[STEPS];
+    uint32_t written = 0, m = 0;
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int row = row_of[group][gwarp * 16 + i * RPI + sub];
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (row >= 0) {
-          written |= 1u << i;
-          x[i] = __ldg(reinterpret_cast<const uint4*>(src + row * stride + head * D + piece * 8));
-        }
+    for (int i = 0; i < STEPS; ++i) {
+      const int row = rows[gwarp * 16 + i * RPI + sub];
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (row >= 0) {
+        written |= 1u << i;
+        x[i] = __ldcs(reinterpret_cast<const uint4*>(src + row * stride));
       }
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i)
-        m = finite_max2(x[i].w, finite_max2(x[i].z, finite_max2(x[i].y, finite_max2(x[i].x, m))));
     }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i)
+      m = finite_max2(x[i].w, finite_max2(x[i].z, finite_max2(x[i].y, finite_max2(x[i].x, m))));
     m = __reduce_max_sync(0xffffffffu, m);
-    if (GW > 1) {
-      if (lane == 0) amax[group][gwarp] = m;
-      __syncthreads();
+    if (GW > 1) {  // over the group's warps; the two halves of amax take turns
+      if (lane == 0) amax[group][turn][gwarp] = m;
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(GW * 32) : "memory");
 #pragma unroll
-      for (int w = 0; w < GW; ++w) m = max(m, amax[group][w]);
+      for (int w = 0; w < GW; ++w) m = max(m, amax[group][turn][w]);
     }
-    if (live) {
-      float* sp = p.scale + (static_cast<int64_t>(page) * p.hkv + head) * 2 + kind;
-      float sc = fp8_scale_of(m), grow = 1.f;
-      if (row_of[group][0] < 0) {  // the page goes on
-        const float old = clamp_scale(*sp);
-        if (old >= sc) sc = old;
-        else grow = old / sc;
-      }
-      const float inv = 1.f / sc;
-      uint8_t* dst = p.cache + ((static_cast<int64_t>(page) * p.hkv + head) * 2 + kind) * (P * D);
-      const bool anew = row_of[group][0] >= 0;
+    const float need = fp8_scale_of(m), sc = fmaxf(need, old);
+    const float inv = 1.f / sc, grow = old / sc;
+    uint8_t* dst = p.cache + ((static_cast<int64_t>(page) * p.hkv + head) * 2 + kind) * (P * D) + piece * 8;
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        uint2* d = reinterpret_cast<uint2*>(dst + (gwarp * 16 + i * RPI + sub) * D + piece * 8);
-        if (written >> i & 1) {
-          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-          uint32_t o[4];
+    for (int i = 0; i < STEPS; ++i) {
+      uint2* d = reinterpret_cast<uint2*>(dst + (gwarp * 16 + i * RPI + sub) * D);
+      if (written >> i & 1) {
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        uint32_t o[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            o[e] = to_e4m3x2(__uint_as_float(w[e] << 16) * inv, __uint_as_float(w[e] & 0xffff0000u) * inv);
-          *d = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
-        } else if (!anew && grow != 1.f) {
-          const uint2 held = *d;
-          const uint32_t w[4] = {held.x & 0xffffu, held.x >> 16, held.y & 0xffffu, held.y >> 16};
-          uint32_t o[4];
+        for (int e = 0; e < 4; ++e)
+          o[e] = to_e4m3x2(__uint_as_float(w[e] << 16) * inv, __uint_as_float(w[e] & 0xffff0000u) * inv);
+        *d = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+      } else if (!anew && grow != 1.f) {  // the page goes on at a larger scale
+        const uint2 held = *d;
+        const uint32_t w[4] = {held.x & 0xffffu, held.x >> 16, held.y & 0xffffu, held.y >> 16};
+        uint32_t o[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 f = from_e4m3x2(w[e]);
-            o[e] = to_e4m3x2(f.x * grow, f.y * grow);
-          }
-          *d = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = from_e4m3x2(w[e]);
+          o[e] = to_e4m3x2(f.x * grow, f.y * grow);
         }
+        *d = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
       }
     }
-    __syncthreads();  // every warp of the group has read the old scale
-    if (live && gwarp == 0 && lane == 0) {
-      float* sp = p.scale + (static_cast<int64_t>(page) * p.hkv + head) * 2 + kind;
-      float sc = fp8_scale_of(m);
-      if (row_of[group][0] < 0) sc = fmaxf(sc, clamp_scale(*sp));
-      *sp = sc;
-    }
-    __syncthreads();
+    if (gwarp == 0 && lane == 0) *sp = sc;  // the group's warps read the old one before the barrier
+    __syncwarp();
   }
 }
 
 template <int D>
 cudaError_t launch_append_d(const AppendParams& p, int page_size, cudaStream_t stream) {
-  const dim3 grid((p.rows + kAppendRows - 1) / kAppendRows, p.hkv);
+  const dim3 grid((p.rows - 1) / kAppendRows + 1, (p.hkv - 1) / p.heads + 1);
   if (page_size == 16) append_fp8_kernel<D, 16><<<grid, kAppendThreads, 0, stream>>>(p);
   else if (page_size == 32) append_fp8_kernel<D, 32><<<grid, kAppendThreads, 0, stream>>>(p);
   else append_fp8_kernel<D, 64><<<grid, kAppendThreads, 0, stream>>>(p);
@@ -343,7 +334,7 @@ cudaError_t launch_map_slots(const spec_slot_args_t& a, char* ws, cudaStream_t s
   return cudaGetLastError();
 }
 
-cudaError_t launch_append_fp8(const spec_append_fp8_args_t& a, cudaStream_t stream) {
+cudaError_t launch_append_fp8(const spec_append_fp8_args_t& a, int sms, cudaStream_t stream) {
   AppendParams p;
   const int64_t dense = static_cast<int64_t>(a.num_kv_heads) * a.head_dim;
   p.rows = a.rows;
@@ -357,6 +348,12 @@ cudaError_t launch_append_fp8(const spec_append_fp8_args_t& a, cudaStream_t stre
   p.cache = static_cast<uint8_t*>(a.kv_cache);
   p.scale = a.kv_scale;
   p.status = a.status;
+  // several heads per block where the rows alone fill the GPU: the search for led pages is
+  // done once for all of them
+  p.heads = 1;
+  while (p.heads < 8 && p.heads < p.hkv &&
+         static_cast<int64_t>((p.rows - 1) / kAppendRows + 1) * ((p.hkv - 1) / (2 * p.heads) + 1) >= 4 * sms)
+    p.heads *= 2;
   (void)cudaGetLastError();
   return a.head_dim == 128 ? launch_append_d<128>(p, a.page_size, stream)
                            : launch_append_d<64>(p, a.page_size, stream);
