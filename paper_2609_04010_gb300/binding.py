@@ -178,6 +178,8 @@ def declared_functions():
 def lib(build_if_missing: bool = True):
     """The loaded library (built first if it is missing and the toolkit is present)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(_build.LIB):
@@ -251,7 +253,14 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+# torch.cuda.current_stream() builds a Stream object (about 3 us); its handle alone is read
+# where torch offers that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream=None):
+    if stream is None and _raw_stream is not None:
+        return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
 

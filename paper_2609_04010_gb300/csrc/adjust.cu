@@ -70,14 +70,14 @@ __device__ __forceinline__ float adjust_one(float x, int v, uint32_t c, uint32_t
 // VEC: rows are 16-byte aligned and a thread's eight tokens are consecutive; otherwise they
 // are 32 apart, so that a warp's loads of one element each are.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) {
+__global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t a) {
   __shared__ __align__(16) uint32_t count[kSlice];  // output count and flags
   __shared__ uint32_t place[kSlice];                // first place in the bias list
   __shared__ uint16_t list[kSlice];                 // the tokens with a count or a bias
   __shared__ int nlist;
   __shared__ int btok[64];
-  const int tid = threadIdx.x, b = blockIdx.y;
-  const int v0 = blockIdx.x * kSlice, nv = min(kSlice, a.vocab - v0);
+  const int tid = threadIdx.x, b = blockIdx.x;  // low token ids, which text uses most, start first
+  const int v0 = blockIdx.y * kSlice, nv = min(kSlice, a.vocab - v0);
   const int G = a.gamma;
   Seq q;
   q.rep = a.repetition ? a.repetition[b] : 1.f;
@@ -105,15 +105,32 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
       if (i < pl) atomicOr(&count[u], kPrompt);
       else atomicAdd(&count[u], 1u);
     };
-    int i = tid;
-    for (; i + 3 * kThreads < hl; i += 4 * kThreads) {  // four loads in flight
-      int t[4];
+    int i0 = 0;  // tokens taken four at a time, two loads in flight
+    if ((reinterpret_cast<uintptr_t>(h) & 15u) == 0) {
+      for (; i0 + 8 * kThreads <= hl; i0 += 8 * kThreads) {
+        int4 t[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) t[e] = __ldg(h + i + e * kThreads);
+        for (int e = 0; e < 2; ++e) t[e] = __ldg(reinterpret_cast<const int4*>(h + i0) + tid + e * kThreads);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) add(t[e], i + e * kThreads);
+        for (int e = 0; e < 2; ++e) {
+          const int at = i0 + (tid + e * kThreads) * 4;
+          add(t[e].x, at);
+          add(t[e].y, at + 1);
+          add(t[e].z, at + 2);
+          add(t[e].w, at + 3);
+        }
+      }
     }
-    for (; i < hl; i += kThreads) add(__ldg(h + i), i);
+    for (; i0 < hl; i0 += 8 * kThreads) {
+      int t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = i0 + tid + e * kThreads;
+        t[e] = at < hl ? __ldg(h + at) : -1;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) add(t[e], i0 + tid + e * kThreads);
+    }
   }
   if (penal && tid < G) {
     const uint32_t u = index(btok[tid]);
@@ -139,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
   // ---- the copy: this thread's tokens are u0 + e * (VEC ? 1 : 32) of the range ----
   const int u0 = VEC ? tid * 8 : (tid >> 5) * 256 + (tid & 31);
   const int word0 = (v0 + (VEC ? u0 : (tid >> 5) * 256)) >> 5;
-  constexpr int U = VEC ? 8 / Eight<T>::kWords : 2;  // rows in flight
+  constexpr int U = VEC ? 4 / Eight<T>::kWords : 2;  // rows in flight
   for (int j0 = 0; j0 < (u0 < nv ? G : 0); j0 += U) {
     uint32_t keep[U];  // the mask's eight bits for each row
 #pragma unroll
@@ -193,18 +210,35 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(spec_adjust_args_t a) 
   // ---- the listed tokens (out already holds their logits, so it may be the input) ----
   __syncthreads();
   const int n = nlist;
-  for (int it = tid; it < n * G; it += kThreads) {
-    const int j = it / n, u = list[it - j * n];
-    if (mask && !(__ldg(mask + static_cast<int64_t>(j) * nmask + ((v0 + u) >> 5)) >> ((v0 + u) & 31) & 1u)) continue;
-    const int64_t at = static_cast<int64_t>(j) * a.vocab + u;
-    const int nblk = a.block_shift ? j : j + 1;
-    out[at] = from_f32<T>(adjust_one(to_f32<T>(out[at]), v0 + u, count[u], place[u], q, btok, nblk));
+  constexpr int W = 4;  // in flight
+  for (int it0 = tid; it0 < n * G; it0 += W * kThreads) {
+    int64_t at[W];
+    int row[W], u[W];
+    float x[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const int it = it0 + e * kThreads;
+      at[e] = -1;
+      if (it >= n * G) continue;
+      row[e] = it / n;
+      u[e] = list[it - row[e] * n];
+      const int v = v0 + u[e];
+      if (mask && !(__ldg(mask + static_cast<int64_t>(row[e]) * nmask + (v >> 5)) >> (v & 31) & 1u)) continue;
+      at[e] = static_cast<int64_t>(row[e]) * a.vocab + u[e];
+      x[e] = to_f32<T>(out[at[e]]);
+    }
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      if (at[e] < 0) continue;
+      const int nblk = a.block_shift ? row[e] : row[e] + 1;
+      out[at[e]] = from_f32<T>(adjust_one(x[e], v0 + u[e], count[u[e]], place[u[e]], q, btok, nblk));
+    }
   }
 }
 
 template <typename T>
 void launch_typed(const spec_adjust_args_t& a, bool vec, cudaStream_t stream) {
-  const dim3 grid((a.vocab - 1) / kSlice + 1, a.batch);
+  const dim3 grid(a.batch, (a.vocab - 1) / kSlice + 1);
   if (vec) adjust_kernel<T, true><<<grid, kThreads, 0, stream>>>(a);
   else adjust_kernel<T, false><<<grid, kThreads, 0, stream>>>(a);
 }

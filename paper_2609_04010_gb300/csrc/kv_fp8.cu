@@ -20,7 +20,7 @@ namespace {
 // block has read it. New pages are read from the free list, never from the table entries
 // that other blocks are writing.
 constexpr int kSlotThreads = 512;
-constexpr int kSlotRowsPerBlock = 4096;  // rows the grid is sized for, per block
+constexpr int kSlotRowsPerBlock = 4 * kSlotThreads;  // rows the grid is sized for, per block
 
 struct SlotParams {
   spec_slot_args_t a;
@@ -33,30 +33,36 @@ struct SeqSlots {
   int32_t before;  // pages taken by earlier sequences
 };
 
-__device__ __forceinline__ int64_t block_excl_scan(int64_t x, int64_t* sh, int64_t* total) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  int64_t in = x;
+struct Two {  // rows and pages, summed together
+  int64_t rows, pages;
+};
+
+__device__ __forceinline__ Two warp_incl_scan(Two v, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, in, o);
-    if (lane >= o) in += y;
+    const int64_t r = __shfl_up_sync(0xffffffffu, v.rows, o), g = __shfl_up_sync(0xffffffffu, v.pages, o);
+    if (lane >= o) {
+      v.rows += r;
+      v.pages += g;
+    }
   }
+  return v;
+}
+
+// Sums over the earlier threads of the block; *total over all.
+__device__ __forceinline__ Two block_excl_scan(Two x, Two* sh, Two* total) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  constexpr int kWarps = kSlotThreads / 32;
+  const Two in = warp_incl_scan(x, lane);
   if (lane == 31) sh[w] = in;
   __syncthreads();
-  if (w == 0) {
-    int64_t v = lane < kSlotThreads / 32 ? sh[lane] : 0;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += y;
-    }
-    if (lane < kSlotThreads / 32) sh[lane] = v;
-  }
+  // every warp sums the warps' totals for itself
+  const Two all = warp_incl_scan(lane < kWarps ? sh[lane] : Two{0, 0}, lane);
+  *total = {__shfl_sync(0xffffffffu, all.rows, kWarps - 1), __shfl_sync(0xffffffffu, all.pages, kWarps - 1)};
+  const int64_t r = __shfl_sync(0xffffffffu, all.rows, w > 0 ? w - 1 : 0);
+  const int64_t g = __shfl_sync(0xffffffffu, all.pages, w > 0 ? w - 1 : 0);
   __syncthreads();
-  const int64_t ex = (w > 0 ? sh[w - 1] : 0) + in - x;
-  *total = sh[kSlotThreads / 32 - 1];
-  __syncthreads();
-  return ex;
+  return {(w > 0 ? r : 0) + in.rows - x.rows, (w > 0 ? g : 0) + in.pages - x.pages};
 }
 
 __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
@@ -64,14 +70,15 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
   const spec_slot_args_t& a = p.a;
   int32_t* start = reinterpret_cast<int32_t*>(smem_raw);                // [batch + 1]
   SeqSlots* seq = reinterpret_cast<SeqSlots*>(start + a.batch + 1);      // [batch]
-  __shared__ int64_t sh[kSlotThreads / 32];
+  __shared__ Two sh[kSlotThreads / 32];
   __shared__ int s_last, s_taken;
   const int tid = threadIdx.x;
   const int P = a.page_size, MP = a.max_pages_per_seq;
+  const int psh = (P & (P - 1)) == 0 ? __ffs(P) - 1 : -1;  // log2 of a power of two
   const int64_t cap = static_cast<int64_t>(MP) * P;
   const int count0 = min(max(*a.free_count, 0), a.free_capacity);
   if (tid == 0) s_taken = 0;
-  int64_t row_carry = 0, page_carry = 0;
+  Two carry = {0, 0};
   for (int b0 = 0; b0 < a.batch; b0 += kSlotThreads) {
     const int b = b0 + tid;
     int len = -1, n = 0, need = 0, first = 0;
@@ -80,78 +87,103 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
       len = a.kv_len[b];
       const bool fits = len >= 0 && n >= 0 && static_cast<int64_t>(len) + n <= cap;
       if (fits) {
-        first = static_cast<int>((static_cast<int64_t>(len) + a.reserved + P - 1) / P);
-        need = max(0, (len + n + P - 1) / P - first);
+        const int64_t held = static_cast<int64_t>(len) + a.reserved + P - 1;
+        first = static_cast<int>(psh >= 0 ? held >> psh : held / P);
+        const int end = len + n + P - 1;
+        need = max(0, (psh >= 0 ? end >> psh : end / P) - first);
       } else {
         len = -1;
       }
       n = max(n, 0);
     }
-    int64_t rows, pages;
-    const int64_t r = row_carry + block_excl_scan(n, sh, &rows);
-    const int64_t before = page_carry + block_excl_scan(need, sh, &pages);
-    row_carry += rows;
-    page_carry += pages;
+    Two all;
+    const Two before = block_excl_scan({n, need}, sh, &all);
     if (b < a.batch) {
-      start[b] = static_cast<int32_t>(min(r, static_cast<int64_t>(INT32_MAX)));
-      const bool served = len >= 0 && (need == 0 || before + need <= count0);
-      if (served && need > 0) atomicMax(&s_taken, static_cast<int>(before) + need);
-      seq[b] = {served ? len : -1, first, served ? static_cast<int32_t>(before) : 0};
+      const int64_t pages = carry.pages + before.pages;
+      start[b] = static_cast<int32_t>(min(carry.rows + before.rows, static_cast<int64_t>(INT32_MAX)));
+      const bool served = len >= 0 && (need == 0 || pages + need <= count0);
+      if (served && need > 0) atomicMax(&s_taken, static_cast<int>(pages) + need);
+      seq[b] = {served ? len : -1, first, served && need > 0 ? static_cast<int32_t>(pages) : 0};
     }
+    carry.rows += all.rows;
+    carry.pages += all.pages;
   }
-  if (tid == 0) start[a.batch] = static_cast<int32_t>(min(row_carry, static_cast<int64_t>(INT32_MAX)));
+  if (tid == 0) start[a.batch] = static_cast<int32_t>(min(carry.rows, static_cast<int64_t>(INT32_MAX)));
   __syncthreads();
   const int total = start[a.batch];
 
-  // rows past max_rows only put their new pages into the table
-  const int rows_end = max(total, a.max_rows);
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kSlotThreads;
-  for (int64_t r64 = static_cast<int64_t>(blockIdx.x) * kSlotThreads + tid; r64 < rows_end; r64 += step) {
-    const int r = static_cast<int>(r64);
-    int slot = -1, pos = -1, b = -1;
-    if (r < total) {
-      int lo = 0, hi = a.batch;  // largest b with start[b] <= r
+  // Four rows a thread, one search for their sequence; rows past max_rows only put their new
+  // pages into the table.
+  const int64_t rows_end = max(total, a.max_rows);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kSlotThreads * 4;
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.slots) | reinterpret_cast<uintptr_t>(a.positions) |
+                      reinterpret_cast<uintptr_t>(a.row_seq)) & 15u) == 0;
+  for (int64_t r0 = (static_cast<int64_t>(blockIdx.x) * kSlotThreads + tid) * 4; r0 < rows_end; r0 += step) {
+    int lo = 0;
+    if (r0 < total) {
+      int hi = a.batch;  // largest b with start[b] <= r0
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (start[mid] <= r) lo = mid; else hi = mid;
-      }
-      b = lo;
-      const SeqSlots s = seq[b];
-      const int i = r - start[b];
-      if (s.len >= 0) {
-        pos = s.len + i;
-        const int idx = pos / P;
-        int32_t* entry = a.page_table + static_cast<int64_t>(b) * MP + idx;
-        int page;
-        if (idx >= s.first) {
-          page = a.free_pages[count0 - 1 - s.before - (idx - s.first)];
-          if (pos % P == 0) *entry = page;  // the page's first token is new: first * P >= len
-        } else {
-          page = *entry;
-        }
-        if (page >= 0 && page < a.num_pages) slot = page * P + pos % P;
-      } else {
-        pos = a.kv_len[b] + i;
+        if (start[mid] <= r0) lo = mid; else hi = mid;
       }
     }
-    if (r >= a.max_rows) continue;
-    a.slots[r] = slot;
-    if (a.positions) a.positions[r] = pos;
-    if (a.row_seq) a.row_seq[r] = b;
+    int slot[4], pos[4], sq[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      slot[e] = pos[e] = sq[e] = -1;
+      const int64_t r = r0 + e;
+      if (r >= total) continue;
+      while (start[lo + 1] <= r) ++lo;
+      sq[e] = lo;
+      const SeqSlots s = seq[lo];
+      const int i = static_cast<int>(r) - start[lo];
+      if (s.len < 0) {
+        pos[e] = a.kv_len[lo] + i;
+        continue;
+      }
+      pos[e] = s.len + i;
+      const int idx = psh >= 0 ? pos[e] >> psh : pos[e] / P, place = pos[e] - idx * P;
+      int32_t* entry = a.page_table + static_cast<int64_t>(lo) * MP + idx;
+      int page;
+      if (idx >= s.first) {
+        page = __ldg(a.free_pages + (count0 - 1 - s.before - (idx - s.first)));
+        if (place == 0) *entry = page;  // the page's first token is new: first * P >= len
+      } else {
+        page = *entry;
+      }
+      if (page >= 0 && page < a.num_pages) slot[e] = page * P + place;
+    }
+    if (wide && r0 + 4 <= a.max_rows) {
+      *reinterpret_cast<int4*>(a.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      if (a.positions) *reinterpret_cast<int4*>(a.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      if (a.row_seq) *reinterpret_cast<int4*>(a.row_seq + r0) = make_int4(sq[0], sq[1], sq[2], sq[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (r0 + e >= a.max_rows) break;
+        a.slots[r0 + e] = slot[e];
+        if (a.positions) a.positions[r0 + e] = pos[e];
+        if (a.row_seq) a.row_seq[r0 + e] = sq[e];
+      }
+    }
   }
 
   // the last block to get here updates the state
-  __threadfence();
-  __syncthreads();
-  if (tid == 0) {
-    s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
-    if (s_last) *p.ticket = 0;
+  if (gridDim.x > 1) {
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+      s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+      if (s_last) *p.ticket = 0;
+    }
+    __syncthreads();
+    if (!s_last) return;
+  } else {
+    __syncthreads();  // every row has read kv_len
   }
-  __syncthreads();
-  if (!s_last) return;
   for (int b = tid; b < a.batch; b += kSlotThreads) {
-    const int len = a.kv_len[b], n = a.num_new[b];
     const bool served = seq[b].len >= 0;
+    const int len = a.kv_len[b], n = a.num_new[b];
     const bool fits = len >= 0 && n >= 0 && static_cast<int64_t>(len) + n <= cap;
     a.new_len[b] = served ? len + n : len;
     if (a.flags) a.flags[b] = served ? 0 : (fits ? 2 : 1);
