@@ -1,7 +1,7 @@
 // Penalties for repeated tokens, biases and grammar masks on logits rows
 // (spec_adjust_logits).
 //
-// A block takes 2,048 tokens of the vocabulary of one sequence, for all of its rows. It counts
+// A block takes 2,048 tokens of the vocabulary of one sequence, for some of its rows. It counts
 // the history's tokens of its range in shared memory once (integer atomics, so the counts do
 // not depend on their order) and lists the tokens that are counted or biased. It then copies
 // its logits under their mask bits, eight a thread (eight that the mask hides together are
@@ -11,6 +11,7 @@
 // bounds it.
 #include <cuda_bf16.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "kv_fp8.cuh"
@@ -70,7 +71,7 @@ __device__ __forceinline__ float adjust_one(float x, int v, uint32_t c, uint32_t
 // VEC: rows are 16-byte aligned and a thread's eight tokens are consecutive; otherwise they
 // are 32 apart, so that a warp's loads of one element each are.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t a) {
+__global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t a, int rows) {
   __shared__ __align__(16) uint32_t count[kSlice];  // output count and flags
   __shared__ uint32_t place[kSlice];                // first place in the bias list
   __shared__ uint16_t list[kSlice];                 // the tokens with a count or a bias
@@ -79,6 +80,7 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
   const int tid = threadIdx.x, b = blockIdx.x;  // low token ids, which text uses most, start first
   const int v0 = blockIdx.y * kSlice, nv = min(kSlice, a.vocab - v0);
   const int G = a.gamma;
+  const int row0 = blockIdx.z * rows, row1 = min(G, row0 + rows);  // this block's rows
   Seq q;
   q.rep = a.repetition ? a.repetition[b] : 1.f;
   q.freq = a.frequency ? a.frequency[b] : 0.f;
@@ -157,12 +159,12 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
   const int u0 = VEC ? tid * 8 : (tid >> 5) * 256 + (tid & 31);
   const int word0 = (v0 + (VEC ? u0 : (tid >> 5) * 256)) >> 5;
   constexpr int U = VEC ? 4 / Eight<T>::kWords : 2;  // rows in flight
-  for (int j0 = 0; j0 < (u0 < nv ? G : 0); j0 += U) {
+  for (int j0 = row0; j0 < (u0 < nv ? row1 : 0); j0 += U) {
     uint32_t keep[U];  // the mask's eight bits for each row
 #pragma unroll
     for (int r = 0; r < U; ++r) {
-      keep[r] = j0 + r < G ? 0xffu : 0u;
-      if (mask && j0 + r < G) {
+      keep[r] = j0 + r < row1 ? 0xffu : 0u;
+      if (mask && j0 + r < row1) {
         const uint32_t* w = mask + static_cast<int64_t>(j0 + r) * nmask + word0;
         if (VEC) {
           keep[r] = __ldg(reinterpret_cast<const uint8_t*>(w) + ((u0 >> 3) & 3));
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
     }
 #pragma unroll
     for (int r = 0; r < U; ++r) {
-      if (j0 + r >= G) break;
+      if (j0 + r >= row1) break;
       if (keep[r] != 0xffu) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -199,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
       T* dst = out + static_cast<int64_t>(j0 + r) * a.vocab + u0;
       if (VEC) {
 #pragma unroll
-        for (int w = 0; w < Eight<T>::kWords; ++w) __stcs(reinterpret_cast<uint4*>(dst) + w, x[r].w[w]);
+        for (int w = 0; w < Eight<T>::kWords; ++w) reinterpret_cast<uint4*>(dst)[w] = x[r].w[w];
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -210,8 +212,9 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
   // ---- the listed tokens (out already holds their logits, so it may be the input) ----
   __syncthreads();
   const int n = nlist;
-  constexpr int W = 4;  // in flight
-  for (int it0 = tid; it0 < n * G; it0 += W * kThreads) {
+  constexpr int W = 2;  // in flight
+  const int items = n * (row1 - row0);
+  for (int it0 = tid; it0 < items; it0 += W * kThreads) {
     int64_t at[W];
     int row[W], u[W];
     float x[W];
@@ -219,9 +222,9 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
     for (int e = 0; e < W; ++e) {
       const int it = it0 + e * kThreads;
       at[e] = -1;
-      if (it >= n * G) continue;
-      row[e] = it / n;
-      u[e] = list[it - row[e] * n];
+      if (it >= items) continue;
+      row[e] = row0 + it / n;
+      u[e] = list[it % n];
       const int v = v0 + u[e];
       if (mask && !(__ldg(mask + static_cast<int64_t>(row[e]) * nmask + (v >> 5)) >> (v & 31) & 1u)) continue;
       at[e] = static_cast<int64_t>(row[e]) * a.vocab + u[e];
@@ -237,22 +240,27 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
 }
 
 template <typename T>
-void launch_typed(const spec_adjust_args_t& a, bool vec, cudaStream_t stream) {
-  const dim3 grid(a.batch, (a.vocab - 1) / kSlice + 1);
-  if (vec) adjust_kernel<T, true><<<grid, kThreads, 0, stream>>>(a);
-  else adjust_kernel<T, false><<<grid, kThreads, 0, stream>>>(a);
+void launch_typed(const spec_adjust_args_t& a, bool vec, int sms, cudaStream_t stream) {
+  // rows are shared out among blocks (each counts the history again) until there are about two
+  // rounds of them
+  const int64_t blocks = static_cast<int64_t>(a.batch) * ((a.vocab - 1) / kSlice + 1);
+  const int64_t splits = std::min<int64_t>(a.gamma, std::max<int64_t>(1, 12 * sms / blocks));
+  const int rows = static_cast<int>((a.gamma + splits - 1) / splits);
+  const dim3 grid(a.batch, (a.vocab - 1) / kSlice + 1, (a.gamma - 1) / rows + 1);
+  if (vec) adjust_kernel<T, true><<<grid, kThreads, 0, stream>>>(a, rows);
+  else adjust_kernel<T, false><<<grid, kThreads, 0, stream>>>(a, rows);
 }
 
 }  // namespace
 
-cudaError_t launch_adjust(const spec_adjust_args_t& a, cudaStream_t stream) {
+cudaError_t launch_adjust(const spec_adjust_args_t& a, int sms, cudaStream_t stream) {
   const size_t esz = a.logits_dtype == SPEC_BF16 ? 2 : 4;
   // whole groups of eight in aligned rows
   const bool vec = a.vocab % 8 == 0 &&
                    ((reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.out)) & 15u) == 0;
   (void)cudaGetLastError();
-  if (esz == 2) launch_typed<__nv_bfloat16>(a, vec, stream);
-  else launch_typed<float>(a, vec, stream);
+  if (esz == 2) launch_typed<__nv_bfloat16>(a, vec, sms, stream);
+  else launch_typed<float>(a, vec, sms, stream);
   return cudaGetLastError();
 }
 

@@ -229,7 +229,7 @@ spec_status_t spec_adjust_logits(const spec_adjust_args_t* a, spec_stream_t stre
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   DeviceScope scope(s);
   if (!scope.ok) return SPEC_ERR_CUDA;
-  return launch_adjust(*a, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+  return launch_adjust(*a, scope.sms, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }
 
 }  // extern "C"
