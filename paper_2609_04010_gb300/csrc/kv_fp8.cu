@@ -20,7 +20,7 @@ namespace {
 // block has read it. New pages are read from the free list, never from the table entries
 // that other blocks are writing.
 constexpr int kSlotThreads = 512;
-constexpr int kSlotRowsPerBlock = 4 * kSlotThreads;  // rows the grid is sized for, per block
+constexpr int kSlotRowsPerBlock = 8 * kSlotThreads;  // rows the grid is sized for, per block
 
 struct SlotParams {
   spec_slot_args_t a;
@@ -168,9 +168,9 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
     }
   }
 
-  // the last block to get here updates the state
+  // The last block to get here updates the state. What the blocks before it read of it they
+  // have used, and nothing they wrote is read here, so the ticket needs no fence.
   if (gridDim.x > 1) {
-    __threadfence();
     __syncthreads();
     if (tid == 0) {
       s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams
       x[i] = make_uint4(0, 0, 0, 0);
       if (row >= 0) {
         written |= 1u << i;
-        x[i] = __ldcs(reinterpret_cast<const uint4*>(src + row * stride));
+        x[i] = __ldg(reinterpret_cast<const uint4*>(src + row * stride));
       }
     }
 #pragma unroll
