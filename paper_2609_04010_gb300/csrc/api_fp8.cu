@@ -44,20 +44,27 @@ spec_status_t check_append(const spec_append_fp8_args_t* a) {
   return SPEC_OK;
 }
 
-// The tensor-core kernel's form of a call. A block serves two sub-units of at most 64 query
-// rows: two adjacent KV heads where each has that many (a page of both is one copy of twice
-// the size), else two halves of one KV head's rows, in tiles of up to 128.
+// The tensor-core form of a call. A block serves two sub-units of query rows: two adjacent KV
+// heads where each fits one (a page of both is one copy of twice the size), else two halves
+// of one KV head's rows, in tiles. With the rows on the MMA's M side (up to 128 a sub-unit)
+// a thread owns a row, with the keys there (up to 64) few rows cost little.
+constexpr int kRowsFrom = 33;  // rows of a sub-unit from which they go to the M side
 struct TcForm {
-  int heads, sub_rows, row_tiles;
+  int rows_on_m, heads, sub_rows, row_tiles;
   bool fits;
 };
 TcForm tc_form(const spec_attn_fp8_args_t& a) {
   const int rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
   TcForm f;
-  f.heads = rows <= kFp8SubRows && a.num_kv_heads % 2 == 0 ? 2 : 1;
-  f.row_tiles = f.heads == 2 ? 1 : (rows + 2 * kFp8SubRows - 1) / (2 * kFp8SubRows);
-  f.sub_rows = f.heads == 2 ? rows : (rows > 2 * kFp8SubRows ? kFp8SubRows : (rows + 1) / 2);
-  f.fits = attn_fp8_tc_fits(a, f.heads, f.sub_rows, f.row_tiles);
+  f.heads = rows <= 128 && a.num_kv_heads % 2 == 0 ? 2 : 1;
+  f.row_tiles = f.heads == 2 ? 1 : (rows + 255) / 256;
+  f.sub_rows = f.heads == 2 ? rows : (rows > 256 ? 128 : (rows + 1) / 2);
+  f.rows_on_m = f.sub_rows >= kRowsFrom;
+  const size_t smem = f.rows_on_m ? attn_fp8_rows_smem(a, f.heads) : attn_fp8_keys_smem(a, f.heads, f.sub_rows);
+  const int64_t tiles = (static_cast<int64_t>(a.max_pages_per_seq) * a.page_size + kFp8KeyTile - 1) / kFp8KeyTile + 8;
+  const int64_t units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / f.heads) * f.row_tiles;
+  f.fits = smem <= kTcMaxSmem && tiles * units <= INT32_MAX &&
+           2 * static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX;
   return f;
 }
 
@@ -118,6 +125,7 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
   int64_t units;
   if (P.path == SPEC_ATTN_TENSOR_CORES) {
     // persistent grid; a unit has a slot of its own and one per block that starts inside it
+    P.rows_on_m = f.rows_on_m;
     P.heads = f.heads;
     P.sub_rows = f.sub_rows;
     P.row_tiles = f.row_tiles;
@@ -161,7 +169,10 @@ spec_status_t run_attn_fp8(const spec_attn_fp8_args_t* a, void* ws, size_t ws_by
   if (P.end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
   char* w = static_cast<char*>(ws);
   if (P.path == SPEC_ATTN_TENSOR_CORES)
-    return launch_attn_fp8_tc(*a, P, w, s, starve) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+    return (P.rows_on_m ? launch_attn_fp8_rows(*a, P, w, s, starve) : launch_attn_fp8_keys(*a, P, w, s, starve)) ==
+                   cudaSuccess
+               ? SPEC_OK
+               : SPEC_ERR_CUDA;
   if (starve) return SPEC_ERR_UNSUPPORTED;
   return launch_attn_fp8_simt(*a, P, w, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }

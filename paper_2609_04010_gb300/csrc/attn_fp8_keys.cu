@@ -35,20 +35,13 @@
 // split between blocks is merged from fp32 partials by the last block to finish it (atomic
 // ticket, no waiting). Every mbarrier wait is bounded; after a timeout the softmax warps run
 // their loops to the end without waiting, so that none is missed at a named barrier.
-#include <cuda.h>  // CUtensorMap
-
-#include "attn_fp8.cuh"
-#include "tc_ptx.cuh"
+#include "attn_fp8_tc.cuh"
 
 namespace specv {
 namespace {
 
-using namespace tcx;
+using namespace fp8tc;
 
-constexpr int TK = kFp8KeyTile;  // keys per tile
-
-constexpr int NH = 2;  // sub-units of a block
-constexpr int kFlagRing = 16;  // segments' flags: more than the stages that producers run ahead
 constexpr int kSoftWarps = 8 * NH;
 constexpr int kThreads = 32 * (kSoftWarps + 4);
 
@@ -56,9 +49,7 @@ constexpr int kThreads = 32 * (kSoftWarps + 4);
 template <int D, int HP, int NR>
 struct Cfg {
   static constexpr int NC = NR / 2;                        // rows per softmax warp
-  static constexpr uint32_t ATOM = 8 * D;                  // 8 rows of D bytes, swizzled
-  static constexpr uint32_t SG = 2 * HP * ATOM;            // 8-key group: K, V of each head
-  static constexpr uint32_t STAGE = (TK / 8) * SG;
+  static constexpr uint32_t ATOM = Stage<D, HP>::ATOM, SG = Stage<D, HP>::SG, STAGE = Stage<D, HP>::BYTES;
   static constexpr int NST = (HP == 2 ? 2 : 4) * (128 / D);  // 128 KB in stages
   static constexpr int SB = 2;                             // S buffers per sub-unit
   static constexpr uint32_t Q_TERM = NR * D;               // one term of one sub-unit's Q
@@ -95,47 +86,6 @@ struct Cfg {
 // ---------------------------------------------------------------------------------
 // PTX wrappers
 // ---------------------------------------------------------------------------------
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-// One page of HP KV heads, keys and values (encode_fp8_map's box).
-__device__ __forceinline__ void tma_load_page8(uint32_t dst, const CUtensorMap* map, int kind_head, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(0), "r"(kind_head), "r"(0), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
-                                         uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d_tmem),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// Matrix descriptor of a tile whose rows are W bytes (128 or 64) with the W-byte swizzle.
-template <int W>
-__device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>((lbo >> 4) & 0x3FFFu) << 16) |
-         (static_cast<uint64_t>((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46) |
-         (static_cast<uint64_t>(W == 128 ? 2 : 4) << 61);
-}
-// Instruction descriptor, kind::f8f6f4: fp32 accumulator, e4m3 A and B.
-__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn, bool b_mn) {
-  return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-         (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
-}
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
-               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
 template <int N>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* r) {
   if constexpr (N == 32) tmem_ld32(taddr, r);
@@ -152,10 +102,6 @@ __device__ __forceinline__ bool group_any(int id, bool v) {
       : "memory");
   return r != 0;
 }
-__device__ __forceinline__ void bar_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-
 // Sum over the warp's lanes of each of N columns: lane i ends with column i * N / 32.
 template <int N>
 __device__ __forceinline__ float sum_columns(float* v, int lane) {
@@ -184,25 +130,6 @@ __device__ __forceinline__ float warp_max(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
-// The two e4m3 terms of four values, each packed in order from the low byte; UP: the second
-// terms times 16.
-template <bool UP>
-__device__ __forceinline__ void split_e4m3x4(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
-  asm("{\n .reg .b16 p, q, r, s;\n .reg .b32 x, y, h, g;\n"
-      " cvt.rn.satfinite.e4m3x2.f32 p, %3, %2;\n cvt.rn.satfinite.e4m3x2.f32 q, %5, %4;\n mov.b32 %0, {p, q};\n"
-      " cvt.rn.f16x2.f32 x, %3, %2;\n cvt.rn.f16x2.f32 y, %5, %4;\n"
-      " cvt.rn.f16x2.e4m3x2 h, p;\n cvt.rn.f16x2.e4m3x2 g, q;\n"
-      " sub.f16x2 x, x, h;\n sub.f16x2 y, y, g;\n mul.f16x2 x, x, %6;\n mul.f16x2 y, y, %6;\n"
-      " cvt.rn.satfinite.e4m3x2.f16x2 r, x;\n cvt.rn.satfinite.e4m3x2.f16x2 s, y;\n mov.b32 %1, {r, s};\n}"
-      : "=r"(hi), "=r"(lo)
-      : "f"(a), "f"(b), "f"(c), "f"(d), "r"(UP ? 0x4c004c00u : 0x3c003c00u));
-}
-
-// The slow part of a wait: polls until the phase completes, or gives up (mbar_wait).
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status) {
-  return mbar_wait(bar, parity, abort_flag, status);
-}
-
 constexpr float kNoKey = -1e30f;  // a row's reference before it has seen a key
 
 // ---------------------------------------------------------------------------------
@@ -210,7 +137,7 @@ constexpr float kNoKey = -1e30f;  // a row's reference before it has seen a key
 // ---------------------------------------------------------------------------------
 template <int D, int HP, int NR>
 __global__ void __launch_bounds__(kThreads, 1)
-    attn_fp8_tc_kernel(const __grid_constant__ CUtensorMap tmap, AttnFp8Params p) {
+    attn_fp8_keys_kernel(const __grid_constant__ CUtensorMap tmap, AttnFp8Params p) {
   using C = Cfg<D, HP, NR>;
   constexpr int NC = C::NC, NST = C::NST, SB = C::SB;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -260,126 +187,23 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   for (int i = threadIdx.x; i < NH * D; i += kThreads) nanv[i] = 0ull;
   if (warp == kSoftWarps + 1) tmem_alloc(smem_u32(misc), C::TMEM_COLS);
-  if (warp == kSoftWarps) {
-    const int per_b = p.hunits * p.row_tiles;
-    int carry = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      const int b = b0 + lane;
-      int v = b < p.batch ? (unit_tiles<TK>(p.kv_len[b], p) + p.unit_overhead) * per_b : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += y;
-      }
-      if (b < p.batch) pb[b + 1] = carry + v;
-      carry += __shfl_sync(0xffffffffu, v, 31);
-    }
-    if (lane == 0) pb[0] = 0;
-  }
+  if (warp == kSoftWarps) prefix_tiles(p, pb);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = misc[0];
-
-  // equal ranges of the tile list, on every SM (a multiple of the units, so that equal units
-  // have no boundary inside a range, measured slower: 135.8 against 123.2 us with 128 ragged
-  // units, 232 against 226 with 64 equal ones)
-  const int64_t total = pb[p.batch];
-  const int ctas = static_cast<int>(total < gridDim.x ? total : gridDim.x);
-  const int cta = blockIdx.x;
-  const int64_t t0 = cta < ctas ? static_cast<int64_t>(cta) * total / ctas : 0;
-  const int64_t t1 = cta < ctas ? static_cast<int64_t>(cta + 1) * total / ctas : 0;
-  const int OVH = p.unit_overhead;
+  const WorkList w = work_list(p, pb);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 3) {
     // ============================ producers ============================
-    const int half = warp == kSoftWarps ? 0 : 1;
-    uint32_t it = 0, seg_no = 0;
-    bool ok = true;
-    const int psh = __ffs(p.page_size) - 1;  // log2
-    const int npg = TK >> psh;               // pages of a tile
-    const uint32_t box_bytes = static_cast<uint32_t>(p.page_size) * D * 2 * HP;
-    for (Seg s = locate<TK>(t0, t1, p, pb, OVH); s.ntile > 0 && ok && !p.starve; ++seg_no) {
-      const bool bad_len = !s.len_ok;
-      bool flag = bad_len;
-      // Pages are taken 32 at a time, a lane each; the next 32 ids and scales are loaded
-      // while these are in use, the ids of the 32 after them too.
-      const int pages = bad_len ? 0 : (s.kv_len + p.page_size - 1) >> psh;
-      const int first = s.tile0 * npg;
-      const int32_t* table = p.page_table + static_cast<int64_t>(s.b) * p.max_pages;
-      auto load_id = [&](int base) { return base + lane < pages ? __ldg(table + base + lane) : 0; };
-      auto load_scale = [&](int id, float2* sc) {
-        const bool in = id >= 0 && id < p.num_pages;
-        const float2* src = reinterpret_cast<const float2*>(p.kv_scale) +
-                            static_cast<int64_t>(in ? id : 0) * p.hkv + s.g * HP;
-#pragma unroll
-        for (int h = 0; h < HP; ++h) sc[h] = __ldg(src + h);
-      };
-      int base = first, id = load_id(first), id1 = load_id(first + 32), id2 = load_id(first + 64);
-      float2 sc[HP], sc1[HP];
-      load_scale(id, sc);
-      load_scale(id1, sc1);
-      for (int k = 0; k < s.ntile && ok; ++k, ++it) {
-        const uint32_t st = it % NST;
-        const int pg0 = first + k * npg;
-        if (pg0 >= base + 32) {
-          base += 32;
-          id = id1;
-          id1 = id2;
-#pragma unroll
-          for (int h = 0; h < HP; ++h) sc[h] = sc1[h];
-          load_scale(id1, sc1);
-          id2 = load_id(base + 64);
-        }
-        if (it >= NST) ok = mbar_wait(empty(st), ((it / NST) - 1) & 1, abort_flag, p.status);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        // lanes [pg0 - base, + npg) hold this tile's pages; this warp copies the half
-        // [q0, q1) of them
-        const int q0 = half * (npg >> 1), q1 = min(q0 + (npg >> 1), pages - pg0);
-        const uint32_t dst = sbase + C::OFF_STAGE + st * C::STAGE;
-        if (lane == 0 && q1 > q0) mbar_expect_tx(full(st), static_cast<uint32_t>(q1 - q0) * box_bytes);
-        for (int q = q0; q < q1; ++q) {
-          const int raw = __shfl_sync(0xffffffffu, id, pg0 - base + q);
-          const bool in_range = raw >= 0 && raw < p.num_pages;
-          flag |= !in_range;
-          if (lane == 0)
-            tma_load_page8(dst + static_cast<uint32_t>(q) * box_bytes, &tmap,
-                           2 * ((in_range ? raw : 0) * p.hkv + s.g * HP), full(st));
-        }
-        const int q = base + lane - pg0;
-        if (q >= q0 && q < q0 + (npg >> 1)) {
-#pragma unroll
-          for (int h = 0; h < HP; ++h) {
-            const float sv = clamp_scale(sc[h].y);
-            scl[(st * 8 + q) * HP + h] = q < q1 ? make_float4(sc[h].x * p.scale_log2, __log2f(sv), __frcp_rn(sv), 0.f)
-                                                : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(full(st));
-        __syncwarp();
-      }
-      if (ok && lane == 0) {
-        seg_flag[half * kFlagRing + seg_no % kFlagRing] = flag ? 1 : 0;
-        mbar_arrive(flag_bar(seg_no % kFlagRing));
-      }
-      if (!has_more(s, t1, OVH)) break;
-      s = locate<TK>(s.vnext, t1, p, pb, OVH);
-    }
-    if (!ok) {  // copies still in flight (bounded)
-      for (uint32_t x = it > static_cast<uint32_t>(NST) ? it - NST : 0; x < it; ++x) {
-        const long long c0 = clock64();
-        while (!mbar_try(full(x % NST), (x / NST) & 1) && clock64() - c0 < kWaitCycles) {
-        }
-      }
-    }
+    produce<D, HP, NST>(p, tmap, w, warp == kSoftWarps ? 0 : 1, sbase + C::OFF_STAGE, full(0), empty(0), flag_bar(0), scl,
+                        seg_flag, abort_flag);
   } else if (warp == kSoftWarps + 1) {
     // ============================ S^T = K Q^T ============================
     constexpr uint32_t kIdesc = idesc_e4m3(128, NR, false, false);
     uint32_t it = 0, seg_no = 0;
     bool ok = true, issued = false;
-    for (Seg s = locate<TK>(t0, t1, p, pb, OVH); s.ntile > 0 && ok; ++seg_no) {
+    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok; ++seg_no) {
       for (int k = 0; k < s.ntile && ok; ++k, ++it) {
         const uint32_t st = it % NST, sb = it % SB;
         ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
@@ -403,8 +227,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
       }
-      if (!has_more(s, t1, OVH)) break;
-      s = locate<TK>(s.vnext, t1, p, pb, OVH);
+      if (!has_more(s, w.t1, w.ovh)) break;
+      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
     }
     if (!ok && __any_sync(0xffffffffu, issued)) {
       if (lane == 0) mma_commit(drain_bar(0));
@@ -418,49 +242,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr uint32_t kIdesc = idesc_e4m3(128, 2 * NR, true, true);
     uint32_t it = 0;
     bool ok = true, issued = false;
-    // V of keys that no row sees must be finite, because their weight of 0 is multiplied:
-    // keys past the end are cleared, and a NaN in a block key's value is cleared and noted,
-    // for the outputs of the rows that see it.
-    auto fix_values = [&](uint32_t st, const Seg& sg, int k) {
-      const int key0 = (sg.tile0 + k) * TK;
-      const int ctx = sg.kv_len - p.gamma;
-      if (!sg.len_ok || key0 + TK <= ctx) return;
-      const int nvalid = min(TK, sg.kv_len - key0);
-      constexpr int kPieces = D / 16;
-      unsigned char* base = smem + C::OFF_STAGE + st * C::STAGE;
-      const int from = max(0, ctx - key0);
-      for (int i = lane; i < (TK - from) * kPieces * HP; i += 32) {
-        const int piece = i % kPieces, h = (i / kPieces) % HP, key = from + i / (kPieces * HP);
-        const int ph = D == 128 ? piece ^ (key & 7) : piece ^ ((key >> 1) & 3);
-        uint4* at = reinterpret_cast<uint4*>(base + (key >> 3) * C::SG + (2 * h + 1) * C::ATOM + (key & 7) * D + ph * 16);
-        if (key >= nvalid) {
-          *at = make_uint4(0, 0, 0, 0);
-          continue;
-        }
-        uint4 v = *at;
-        uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        uint32_t any = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) any |= __vcmpeq4(w[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
-        if (any) {
-          const unsigned long long bit = 1ull << (key0 + key - ctx);
-          for (int e = 0; e < 16; ++e) {
-            const uint32_t sh = (e & 3) * 8;
-            if ((w[e >> 2] >> sh & 0x7fu) == 0x7fu) {
-              atomicOr(nanv + h * D + piece * 16 + e, bit);
-              if (HP == 1) atomicOr(nanv + D + piece * 16 + e, bit);
-              w[e >> 2] &= ~(0xffu << sh);
-            }
-          }
-          nan_flag[h] = 1;
-          if (HP == 1) nan_flag[1] = 1;
-          *at = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
-      fence_async_smem();
-      __syncwarp();
-    };
-    for (Seg s = locate<TK>(t0, t1, p, pb, OVH); s.ntile > 0 && ok;) {
+    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok;) {
       for (int k = 0; k < s.ntile && ok; ++k, ++it) {
         const uint32_t st = it % NST;
         ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
@@ -470,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (k == 0)
           for (int h = 0; h < NH && ok; ++h) ok = mbar_wait(p_full(h), it & 1, abort_flag, p.status);
         if (!ok) break;
-        fix_values(st, s, k);
+        fix_values<D, HP>(p, s, k, smem + C::OFF_STAGE + st * C::STAGE, nanv, nan_flag);
         for (int h = 0; h < NH && ok; ++h) {
           ok = mbar_wait(p_full(h), it & 1, abort_flag, p.status);
           if (!ok) break;
@@ -489,8 +271,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
       }
-      if (!has_more(s, t1, OVH)) break;
-      s = locate<TK>(s.vnext, t1, p, pb, OVH);
+      if (!has_more(s, w.t1, w.ovh)) break;
+      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
     }
     if (!ok && __any_sync(0xffffffffu, issued)) {
       if (lane == 0) mma_commit(drain_bar(1));
@@ -612,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       return __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
     };
 
-    Seg s = locate<TK>(t0, t1, p, pb, OVH);
+    Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh);
     float qf = s.ntile > 0 ? start_segment(s, 0) : 1.f;
     while (s.ntile > 0) {
       const uint32_t par = seg_no & 1;
@@ -744,8 +526,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t xl = it + c.ntile - 1;
       it += c.ntile;
       qf = 1.f;
-      if (has_more(c, t1, OVH)) {
-        s = locate<TK>(c.vnext, t1, p, pb, OVH);
+      if (has_more(c, w.t1, w.ovh)) {
+        s = locate<TK>(c.vnext, w.t1, p, w.pb, w.ovh);
         qf = start_segment(s, par ^ 1);
       } else {
         s.ntile = 0;
@@ -754,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       wait(flag_bar(seg_no % kFlagRing), (seg_no / kFlagRing) & 1);
       const bool bad = (seg_flag[seg_no % kFlagRing] | seg_flag[kFlagRing + seg_no % kFlagRing]) != 0;
       const bool whole = c.tile0 == 0 && c.ntile == c.unit_tiles;
-      const int64_t slot = c.u + cta;
+      const int64_t slot = c.u + w.cta;
       if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
       const int nrows = real_rows(c);
       bar_sync(sbar, nthr);
@@ -803,14 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!whole && h == 0 && stid == 0) {
-        const int c_first = owner_of(c.unit_start, total, ctas);
-        const int c_last = owner_of(c.unit_start + c.unit_tiles - 1, total, ctas);
-        int* e = pend + 8 * (*pend_count);
-        const int row_base = c.rt * tile_rows;
-        e[0] = c.b; e[1] = c.g; e[2] = row_base; e[3] = min(tile_rows, p.rows - row_base);
-        e[4] = static_cast<int>(c.u + c_first); e[5] = c_last - c_first + 1;
-        e[6] = static_cast<int>(c.u); e[7] = 0;
-        *pend_count = *pend_count + 1;
+        note_split_unit(p, c, w, tile_rows, pend, pend_count);
       }
       tc_fence_before();
       bar_sync(sbar, nthr);  // xch, the row state and nanv are read; the next segment may set them
@@ -825,43 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, C::TMEM_COLS);
   }
-  // split units: one ticket each, after a fence; the block that completes a unit merges it
-  if (*abort_flag) return;
-  const int np = *pend_count;
-  if (np == 0) return;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x < np) {
-    int* e = pend + 8 * threadIdx.x;
-    const uint32_t prev = atomicAdd(&p.tickets[e[6]], 1u);
-    e[7] = prev == static_cast<uint32_t>(e[5] - 1);
-    if (e[7]) p.tickets[e[6]] = 0;
-  }
-  __syncthreads();
-  for (int i = 0; i < np; ++i) {
-    const int* e = pend + 8 * i;
-    if (!e[7]) continue;
-    __threadfence();
-    merge_fp8_unit<D>(p, e[0], e[1] * HP, HP, e[2], e[3], e[4], e[5], threadIdx.x, kThreads);
-  }
-}
-
-// The cache as a 4-D tensor of bytes whose box is one page of HP adjacent KV heads: D
-// bytes of a row; 8 rows; K and V of the heads (stride page * D); page / 8 groups of 8 rows.
-// It lands as [8-key group][head, K or V][8 keys][D bytes]: the 8-key groups of one kind
-// and head sit at a uniform stride through a tile, whatever the page size.
-bool encode_fp8_map(CUtensorMap* map, const spec_attn_fp8_args_t& a, int heads_per_box) {
-  EncodeTiledFn enc = encoder();
-  if (!enc) return false;
-  const cuuint64_t D = static_cast<cuuint64_t>(a.head_dim), P = static_cast<cuuint64_t>(a.page_size);
-  const cuuint64_t dims[4] = {D, 8, 2 * static_cast<cuuint64_t>(a.num_pages) * a.num_kv_heads, P / 8};
-  const cuuint64_t strides[3] = {D, P * D, 8 * D};
-  const cuuint32_t box[4] = {static_cast<cuuint32_t>(D), 8, static_cast<cuuint32_t>(2 * heads_per_box),
-                             static_cast<cuuint32_t>(P / 8)};
-  const cuuint32_t estr[4] = {1, 1, 1, 1};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(a.kv_cache), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  if (!*abort_flag) merge_split_units<D, HP, kThreads>(p, pend, *pend_count);
 }
 
 template <int D, int HP, int NR>
@@ -879,7 +618,7 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   // long ones equal (batch 64 / block 16, 0: 166 us, 2: 143, 5: 132, 8: 137).
   p.unit_overhead = 5;
   const size_t smem = C::smem_bytes(a.batch);
-  auto kernel = attn_fp8_tc_kernel<D, HP, NR>;
+  auto kernel = attn_fp8_keys_kernel<D, HP, NR>;
   const cudaError_t e =
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
@@ -904,17 +643,35 @@ size_t smem_of(int sub_rows, int batch) {
 
 }  // namespace
 
-bool attn_fp8_tc_fits(const spec_attn_fp8_args_t& a, int heads, int sub_rows, int row_tiles) {
-  const bool d128 = a.head_dim == 128;
-  const size_t smem = heads == 2 ? (d128 ? smem_of<128, 2>(sub_rows, a.batch) : smem_of<64, 2>(sub_rows, a.batch))
-                                 : (d128 ? smem_of<128, 1>(sub_rows, a.batch) : smem_of<64, 1>(sub_rows, a.batch));
-  const int64_t tiles = (static_cast<int64_t>(a.max_pages_per_seq) * a.page_size + TK - 1) / TK + 2;
-  const int64_t units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / heads) * row_tiles;
-  return smem <= kTcMaxSmem && tiles * units <= INT32_MAX &&
-         2 * static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX;
+namespace fp8tc {
+
+// The cache as a 4-D tensor of bytes whose box is one page of `heads` adjacent KV heads: D
+// bytes of a row; 8 rows; K and V of the heads (stride page * D); page / 8 groups of 8 rows.
+// It lands as [8-key group][head, K or V][8 keys][D bytes]: the 8-key groups of one kind
+// and head sit at a uniform stride through a tile, whatever the page size.
+bool encode_fp8_map(CUtensorMap* map, const spec_attn_fp8_args_t& a, int heads) {
+  tcx::EncodeTiledFn enc = tcx::encoder();
+  if (!enc) return false;
+  const cuuint64_t D = static_cast<cuuint64_t>(a.head_dim), P = static_cast<cuuint64_t>(a.page_size);
+  const cuuint64_t dims[4] = {D, 8, 2 * static_cast<cuuint64_t>(a.num_pages) * a.num_kv_heads, P / 8};
+  const cuuint64_t strides[3] = {D, P * D, 8 * D};
+  const cuuint32_t box[4] = {static_cast<cuuint32_t>(D), 8, static_cast<cuuint32_t>(2 * heads),
+                             static_cast<cuuint32_t>(P / 8)};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(a.kv_cache), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-cudaError_t launch_attn_fp8_tc(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
+}  // namespace fp8tc
+
+size_t attn_fp8_keys_smem(const spec_attn_fp8_args_t& a, int heads, int sub_rows) {
+  const bool d128 = a.head_dim == 128;
+  return heads == 2 ? (d128 ? smem_of<128, 2>(sub_rows, a.batch) : smem_of<64, 2>(sub_rows, a.batch))
+                    : (d128 ? smem_of<128, 1>(sub_rows, a.batch) : smem_of<64, 1>(sub_rows, a.batch));
+}
+
+cudaError_t launch_attn_fp8_keys(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
                                bool starve) {
   if (P.heads == 2)
     return a.head_dim == 128 ? launch_d<128, 2>(a, P, ws, stream, starve) : launch_d<64, 2>(a, P, ws, stream, starve);

@@ -1,0 +1,534 @@
+// Attention of the block queries over the 8-bit KV cache on tcgen05 tensor cores, with the
+// query rows on the MMA's M side (spec_verify_attention_fp8, SPEC_ATTN_TENSOR_CORES, KV groups
+// of many rows).
+//
+//   S[row][key] = Q8[row][:] . K8[key][:]          (M = 128 rows, N = 128 keys, K = D)
+//   O[row][dim] += sum_key P8[row][key] V8[key][dim] (M = 128 rows, N = D, K = 128 keys)
+// The arithmetic is attn_fp8_keys.cu's: e4m3 operands straight from the cache, queries and
+// weights as sums of two e4m3 terms, weights P = 2^(s + log2(sv) - m) against a reference m
+// per row, sum P / sv. Here a thread owns a row: its maximum, its sum and its reference are
+// its own registers, the page constants are the same for all lanes, and no warp waits for
+// another. With few rows the M side would be padding and attn_fp8_keys.cu is faster.
+//
+// A block serves two sub-units of at most 128 query rows: two adjacent KV heads (HP = 2) or
+// two halves of one KV head's rows. Both terms of P live in TMEM over the columns of S that
+// they came from (32 keys of S are 32 columns, of P 8 + 8), so that shared memory holds Q and
+// K/V stages only; S is computed again once the products have read P. While one sub-unit is
+// at its softmax, the tensor core works for the other. m is set so that a row's largest P is
+// 32 and raised when a P would pass 256 (both terms add up in one accumulator, so the second
+// one's smallest step is 2^-9; 2^-14 of a row's largest weight). Warp roles (persistent, one
+// block per SM):
+//   warps 0..7   softmax, four per sub-unit, a thread per row
+//   warps 8, 11  producers (as in attn_fp8_keys.cu)
+//   warp 9       issues S = Q K^T
+//   warp 10      issues O += P V; clears V of keys past the sequence's end
+// Work list, split units, bounded waits: as in attn_fp8_keys.cu.
+#include "attn_fp8_tc.cuh"
+
+namespace specv {
+namespace {
+
+using namespace fp8tc;
+
+constexpr int kSoftWarps = 4 * NH;
+constexpr int kThreads = 32 * (kSoftWarps + 4);
+constexpr int MR = 128;  // rows of a sub-unit's MMA tile
+
+template <int D, int HP>
+struct Cfg {
+  static constexpr uint32_t ATOM = Stage<D, HP>::ATOM, SG = Stage<D, HP>::SG, STAGE = Stage<D, HP>::BYTES;
+  static constexpr int NST = (HP == 2 ? 2 : 4) * (128 / D);  // 128 KB in stages
+  static constexpr uint32_t Q_TERM = MR * D;                 // one term of one sub-unit's Q
+  static constexpr uint32_t OFF_STAGE = 0;
+  static constexpr uint32_t OFF_Q = OFF_STAGE + NST * STAGE;
+  static constexpr uint32_t OFF_SCL = OFF_Q + NH * 2 * Q_TERM;      // float4 [NST][8 pages][HP]
+  static constexpr uint32_t OFF_NAN = OFF_SCL + NST * 8 * HP * 16;  // uint64 [NH][D]: NaN block values
+  static constexpr uint32_t OFF_QS = OFF_NAN + NH * D * 8;          // float [2][NH][MR]: rows' Q scales
+  static constexpr uint32_t OFF_BAR = OFF_QS + 2 * NH * MR * 4;
+  // full[NST], empty[NST], s_full[NH], p_full[NH], pv_done[NH], seg_ready[NH], drain[2],
+  // flag_ready[kFlagRing]
+  static constexpr int NBAR = 2 * NST + 4 * NH + 2 + kFlagRing;
+  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;        // tmem base, abort, pending, -, NaN flags
+  static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;             // int [2][kFlagRing]: segments' bad flags
+  static constexpr uint32_t OFF_PEND = OFF_FLAG + 8 * kFlagRing;  // int [2][8]
+  static constexpr uint32_t OFF_PB = OFF_PEND + 64;               // int [batch + 1]
+  static constexpr uint32_t S_COL = 0;                            // [NH][128]; P over it
+  static constexpr uint32_t O_COL = NH * TK;                      // [NH][D]
+  static constexpr uint32_t TMEM_COLS = 512;
+  static_assert(O_COL + NH * D <= TMEM_COLS, "TMEM holds 512 columns");
+  static size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
+};
+
+// The same with A in tensor memory (M rows on the lanes, four bytes of K per column).
+__device__ __forceinline__ void mma_e4m3_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+template <int D, int HP>
+__global__ void __launch_bounds__(kThreads, 1)
+    attn_fp8_rows_kernel(const __grid_constant__ CUtensorMap tmap, AttnFp8Params p) {
+  using C = Cfg<D, HP>;
+  constexpr int NST = C::NST;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t bar0 = sbase + C::OFF_BAR;
+  auto full = [&](int s) { return bar0 + 8u * s; };
+  auto empty = [&](int s) { return bar0 + 8u * (NST + s); };
+  auto s_full = [&](int h) { return bar0 + 8u * (2 * NST + h); };
+  auto p_full = [&](int h) { return bar0 + 8u * (2 * NST + NH + h); };
+  auto pv_done = [&](int h) { return bar0 + 8u * (2 * NST + 2 * NH + h); };
+  auto seg_ready = [&](int h) { return bar0 + 8u * (2 * NST + 3 * NH + h); };
+  auto drain_bar = [&](int i) { return bar0 + 8u * (2 * NST + 4 * NH + i); };
+  auto flag_bar = [&](int i) { return bar0 + 8u * (2 * NST + 4 * NH + 2 + i); };
+  float4* scl = reinterpret_cast<float4*>(smem + C::OFF_SCL);
+  unsigned long long* nanv = reinterpret_cast<unsigned long long*>(smem + C::OFF_NAN);
+  uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
+  volatile int* pend_count = reinterpret_cast<volatile int*>(misc + 2);
+  volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 4);            // [NH]
+  volatile int* seg_flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);  // [producer][kFlagRing]
+  int* pend = reinterpret_cast<int*>(smem + C::OFF_PEND);
+  int* pb = reinterpret_cast<int*>(smem + C::OFF_PB);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int sub_rows = p.rows_per_cta;
+  const int tile_rows = HP == 2 ? sub_rows : NH * sub_rows;
+  // warps with rows: the sub-unit's first row is on lane 0, or, for the second of two short
+  // ones, on lane 64, so that all four SM sub-partitions work
+  const int nact = (sub_rows + 31) / 32;
+
+  if (warp == 0) {
+    for (int i = lane; i < C::NBAR; i += 32) {
+      constexpr int b_sfull = 2 * NST, b_pfull = b_sfull + NH, b_pv = b_pfull + NH, b_seg = b_pv + NH;
+      constexpr int b_drain = b_seg + NH, b_flag = b_drain + 2;
+      const int n = i < NST || i >= b_flag ? 2  // full, flag_ready
+                    : (i >= b_pfull && i < b_pv) || (i >= b_seg && i < b_drain) ? nact : 1;  // p_full, seg_ready
+      mbar_init(bar0 + 8u * i, n);
+    }
+    if (lane < NH) nan_flag[lane] = 0;
+    if (lane == 0) {
+      *abort_flag = 0;
+      *pend_count = 0;
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = threadIdx.x; i < NH * D; i += kThreads) nanv[i] = 0ull;
+  if (warp == kSoftWarps + 1) tmem_alloc(smem_u32(misc), C::TMEM_COLS);
+  if (warp == kSoftWarps) prefix_tiles(p, pb);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = misc[0];
+  const WorkList w = work_list(p, pb);
+
+  if (warp == kSoftWarps || warp == kSoftWarps + 3) {
+    // ============================ producers ============================
+    produce<D, HP, NST>(p, tmap, w, warp == kSoftWarps ? 0 : 1, sbase + C::OFF_STAGE, full(0), empty(0), flag_bar(0), scl,
+                        seg_flag, abort_flag);
+  } else if (warp == kSoftWarps + 1) {
+    // ============================ S = Q K^T ============================
+    constexpr uint32_t kIdesc = idesc_e4m3(MR, TK, false, false);
+    uint32_t it = 0, seg_no = 0;
+    bool ok = true, issued = false;
+    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok; ++seg_no) {
+      for (int k = 0; k < s.ntile && ok; ++k, ++it) {
+        const uint32_t st = it % NST;
+        ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
+        for (int h = 0; h < NH && ok; ++h) {
+          if (k == 0) ok = mbar_wait(seg_ready(h), seg_no & 1, abort_flag, p.status);
+          // the products of the tile before have read its P, which lies over S
+          if (ok && it > 0) ok = mbar_wait(pv_done(h), (it - 1) & 1, abort_flag, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          if (lane == 0) {
+            const uint32_t kb = sbase + C::OFF_STAGE + st * C::STAGE + (HP == 2 ? h : 0) * 2 * C::ATOM;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int kk = 0; kk < D / 32; ++kk)
+                mma_e4m3(tmem + C::S_COL + h * TK,
+                         desc_rows<D>(sbase + C::OFF_Q + (h * 2 + t) * C::Q_TERM + kk * 32u, 16, C::ATOM),
+                         desc_rows<D>(kb + kk * 32u, 16, C::SG), kIdesc, t > 0 || kk > 0);
+            mma_commit(s_full(h));
+            issued = true;
+          }
+          __syncwarp();
+        }
+      }
+      if (!has_more(s, w.t1, w.ovh)) break;
+      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
+    }
+    if (!ok && __any_sync(0xffffffffu, issued)) {
+      if (lane == 0) mma_commit(drain_bar(0));
+      __syncwarp();
+      const long long c0 = clock64();
+      while (!mbar_try(drain_bar(0), 0) && clock64() - c0 < kWaitCycles) {
+      }
+    }
+  } else if (warp == kSoftWarps + 2) {
+    // ============================ O += P V ============================
+    constexpr uint32_t kIdesc = idesc_e4m3(MR, D, false, true);
+    uint32_t it = 0;
+    bool ok = true, issued = false;
+    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok;) {
+      for (int k = 0; k < s.ntile && ok; ++k, ++it) {
+        const uint32_t st = it % NST;
+        ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
+        if (!ok) break;
+        // a unit's first tile waits for its weights first: they follow the outputs of the unit
+        // before, whose NaN notes are then read
+        if (k == 0)
+          for (int h = 0; h < NH && ok; ++h) ok = mbar_wait(p_full(h), it & 1, abort_flag, p.status);
+        if (!ok) break;
+        fix_values<D, HP>(p, s, k, smem + C::OFF_STAGE + st * C::STAGE, nanv, nan_flag);
+        for (int h = 0; h < NH && ok; ++h) {
+          ok = mbar_wait(p_full(h), it & 1, abort_flag, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          if (lane == 0) {
+            const uint32_t vb = sbase + C::OFF_STAGE + st * C::STAGE + ((HP == 2 ? h : 0) * 2 + 1) * C::ATOM;
+#pragma unroll
+            for (int kk = 0; kk < TK / 32; ++kk)
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+                mma_e4m3_ta(tmem + C::O_COL + h * D, tmem + C::S_COL + h * TK + kk * 32u + t * 8u,
+                            desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG), kIdesc, k > 0 || kk > 0 || t > 0);
+            mma_commit(pv_done(h));
+            if (h == NH - 1) mma_commit(empty(st));
+            issued = true;
+          }
+          __syncwarp();
+        }
+      }
+      if (!has_more(s, w.t1, w.ovh)) break;
+      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
+    }
+    if (!ok && __any_sync(0xffffffffu, issued)) {
+      if (lane == 0) mma_commit(drain_bar(1));
+      __syncwarp();
+      const long long c0 = clock64();
+      while (!mbar_try(drain_bar(1), 0) && clock64() - c0 < kWaitCycles) {
+      }
+    }
+  } else {
+    // ============================ softmax ============================
+    const int h = warp >> 2, q4 = warp & 3, kvh = HP == 2 ? h : 0;
+    const int q0 = h == 1 && sub_rows <= 64 ? 2 : 0;  // first lane quadrant of the sub-unit
+    if (q4 >= q0 && q4 < q0 + nact) {
+      const int sbar = 1 + h, nthr = nact * 32, stid = (q4 - q0) * 32 + lane;  // stid: this thread's row
+      const uint32_t lane_base = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
+      const uint32_t s_col = lane_base + C::S_COL + h * TK, o_col = lane_base + C::O_COL + h * D;
+      const int psh = __ffs(p.page_size) - 1;
+      uint32_t it = 0, seg_no = 0;
+      // After a timeout the warp runs its loops to the end without waiting (nothing else
+      // depends on `dead`), so that it passes every named barrier.
+      bool dead = false;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (!dead && !mbar_try(bar, parity)) dead = !wait_slow(bar, parity, abort_flag, p.status);
+        __syncwarp();
+      };
+      auto unit_row = [&](const Seg& sg, int r) { return sg.rt * tile_rows + (HP == 2 ? 0 : h * sub_rows) + r; };
+      auto real_rows = [&](const Seg& sg) { return min(sub_rows, p.rows - unit_row(sg, 0)); };
+      float* const qscale = reinterpret_cast<float*>(smem + C::OFF_QS) + h * MR;  // [2][NH][MR]
+
+      // Brings a segment's Q into shared memory as two e4m3 terms, each row scaled by the
+      // power of two that takes its largest finite magnitude into (224, 448].
+      auto start_segment = [&](const Seg& sg, uint32_t par) {
+        constexpr int kPieces = D / 16;  // 16 elements per piece: 32 B in, 16 B per term
+        const int nreal = real_rows(sg);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          uint4 x[kPieces / 2][2];
+#pragma unroll
+          for (int i = 0; i < kPieces / 2; ++i) {
+            const int item = (half * (kPieces / 2) + i) * nthr + stid, r = item / kPieces, piece = item % kPieces;
+            x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+            if (r < nreal) {
+              const int ur = unit_row(sg, r), j = ur / p.group;
+              const int head = (sg.g * HP + kvh) * p.group + ur - j * p.group;
+              const uint4* src = reinterpret_cast<const uint4*>(
+                  static_cast<const __nv_bfloat16*>(p.q) +
+                  ((static_cast<int64_t>(sg.b) * p.gamma + j) * p.hq + head) * D + piece * 16);
+              x[i][0] = __ldg(src);
+              x[i][1] = __ldg(src + 1);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kPieces / 2; ++i) {
+            const int item = (half * (kPieces / 2) + i) * nthr + stid, r = item / kPieces, piece = item % kPieces;
+            uint32_t mx = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t v[4] = {x[i][e].x, x[i][e].y, x[i][e].z, x[i][e].w};
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const uint32_t a = v[c] & 0x7fffu, b = (v[c] >> 16) & 0x7fffu;
+                mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+              }
+            }
+#pragma unroll
+            for (int o = 1; o < kPieces; o <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const int ex = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
+            const float inv = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+            if (piece == 0) qscale[par * NH * MR + r] = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
+            uint32_t t1w[4], t2w[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const uint4 u = x[i][c >> 1];
+              const uint32_t v2[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
+              float v[4];
+#pragma unroll
+              for (int d = 0; d < 4; ++d) {
+                v[d] = __uint_as_float((d & 1) ? v2[d >> 1] & 0xffff0000u : v2[d >> 1] << 16) * inv;
+                if (!(fabsf(v[d]) < INFINITY)) v[d] = __int_as_float(0x7fc00000);  // an infinite query is NaN
+              }
+              split_e4m3x4<false>(v[0], v[1], v[2], v[3], t1w[c], t2w[c]);
+            }
+            const int lr = q0 * 32 + r;  // row of the MMA tile
+            const int ph = D == 128 ? piece ^ (lr & 7) : piece ^ ((lr >> 1) & 3);
+            unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + lr * D + ph * 16;
+            *reinterpret_cast<uint4*>(dst) = make_uint4(t1w[0], t1w[1], t1w[2], t1w[3]);
+            *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
+          }
+        }
+        fence_async_smem();
+        bar_sync(sbar, nthr);  // the rows' scales are set
+        if (lane == 0) mbar_arrive(seg_ready(h));
+      };
+
+      Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh);
+      if (s.ntile > 0) start_segment(s, 0);
+      while (s.ntile > 0) {
+        const uint32_t par = seg_no & 1;
+        const int ctx = s.kv_len - p.gamma;
+        const int ur = unit_row(s, stid);
+        const bool real = stid < real_rows(s);
+        const int j = min(ur, p.rows - 1) / p.group;
+        // the block keys this row sees, a bit each
+        const unsigned long long all = p.gamma >= 64 ? ~0ull : (1ull << p.gamma) - 1;
+        const unsigned long long vis =
+            all & (p.tree_mask ? __ldg(p.tree_mask + static_cast<int64_t>(s.b) * p.gamma + j) : (2ull << j) - 1);
+        const float qf = qscale[par * NH * MR + stid];
+        float m = -INFINITY, l = 0.f;  // reference (-inf: no key seen yet) and sum
+
+        for (int k = 0; k < s.ntile; ++k) {
+          const uint32_t x = it + k, st = x % NST;
+          const int rel0 = (s.tile0 + k) * TK - ctx;  // block position of the tile's first key
+          const bool masked = rel0 + TK > 0;
+          // visibility of the 32 keys from key c0 of a masked tile
+          auto seen_of = [&](int c0) -> uint32_t {
+            const int r = rel0 + c0;
+            if (r <= -32) return ~0u;
+            if (r < 0) return static_cast<uint32_t>(vis << -r) | ((1u << -r) - 1u);
+            return r < 64 ? static_cast<uint32_t>(vis >> r) : 0u;
+          };
+          const float4* const sc = scl + st * 8 * HP + kvh;  // page g of the tile: sc[g * HP]
+          wait(s_full(h), x & 1);
+          tc_fence_after();
+          wait(full(st), (x / NST) & 1);  // orders the producer's scales before this
+          // ---- the row's largest weighted exponent ----
+          float top = -INFINITY;
+#pragma unroll
+          for (int c0 = 0; c0 < TK; c0 += 32) {
+            uint32_t raw[32];
+            tmem_ld32(s_col + c0, raw);
+            tmem_wait_ld();
+            if (masked) {
+              const uint32_t seen = seen_of(c0);
+#pragma unroll
+              for (int c = 0; c < 32; ++c) raw[c] = (seen >> c & 1) ? raw[c] : 0xff800000u;
+            }
+#pragma unroll
+            for (int g = 0; g < 32; g += 16) {
+              const float4 q = sc[((c0 + g) >> psh) * HP];
+              float t = __uint_as_float(raw[g]);
+#pragma unroll
+              for (int c = 1; c < 16; ++c) t = fmaxf(t, __uint_as_float(raw[g + c]));
+              if (t != -INFINITY) top = fmaxf(top, fmaf(t, q.x * qf, q.y));
+            }
+          }
+          // ---- raise the reference where a weight would pass 2^8 ----
+          if (__any_sync(0xffffffffu, top > m + 8.f || (m == -INFINITY && top > -INFINITY))) {
+            const float now = top > m + 8.f || m == -INFINITY ? fmaxf(m, top - 5.f) : m;
+            const float alpha = m == -INFINITY ? 0.f : ex2(m - now);
+            if (k > 0) {  // O holds every earlier tile before it is scaled
+              wait(pv_done(h), (x - 1) & 1);
+              tc_fence_after();
+#pragma unroll 1
+              for (int c0 = 0; c0 < D; c0 += 32) {
+                uint32_t raw[32];
+                tmem_ld32(o_col + c0, raw);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 32; ++c) raw[c] = __float_as_uint(__uint_as_float(raw[c]) * alpha);
+                tmem_st32(o_col + c0, raw);
+              }
+              tmem_wait_st();
+              l *= alpha;
+            }
+            m = now;
+          }
+          // ---- weights, their sum, and their two terms over the columns of S ----
+          const float msub = m == -INFINITY ? 0.f : m;
+          // scores so large that log2(sv) - m alone rounds by more than a weight may bear
+          const bool far = __any_sync(0xffffffffu, fabsf(msub) > 1048576.f);
+#pragma unroll
+          for (int c0 = 0; c0 < TK; c0 += 32) {
+            uint32_t raw[32], w1[8], w2[8];
+            tmem_ld32(s_col + c0, raw);
+            tmem_wait_ld();
+            uint32_t seen = ~0u;
+            if (masked) seen = seen_of(c0);
+#pragma unroll
+            for (int g = 0; g < 32; g += 16) {
+              const float4 q = sc[((c0 + g) >> psh) * HP];
+              float a = q.x * qf, b = q.y - msub;
+              if (far) {
+#pragma unroll
+                for (int c = g; c < g + 16; ++c)
+                  raw[c] = __float_as_uint(fmaf(__uint_as_float(raw[c]), a, q.y) - msub);
+                a = 1.f;
+                b = 0.f;
+              }
+              float sum = 0.f;
+#pragma unroll
+              for (int c = g; c < g + 16; c += 4) {
+                float pr[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pr[i] = ex2(fmaf(__uint_as_float(raw[c + i]), a, b));
+                if (masked) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) pr[i] = (seen >> (c + i) & 1) ? pr[i] : 0.f;
+                }
+                sum += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+                split_e4m3x4<false>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
+              }
+              l = fmaf(sum, q.z, l);
+            }
+            tmem_st8(s_col + c0, w1);
+            tmem_st8(s_col + c0 + 8, w2);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full(h));
+        }
+        // The next segment's Q takes the place of this one's: every S of this segment has
+        // been read. Its first scores wait for this segment's last products only.
+        const Seg c = s;
+        const uint32_t xl = it + c.ntile - 1;
+        it += c.ntile;
+        if (has_more(c, w.t1, w.ovh)) {
+          s = locate<TK>(c.vnext, w.t1, p, w.pb, w.ovh);
+          start_segment(s, par ^ 1);
+        } else {
+          s.ntile = 0;
+        }
+        // ---- the unit's (or the part's) output row ----
+        wait(flag_bar(seg_no % kFlagRing), (seg_no / kFlagRing) & 1);
+        const bool bad = (seg_flag[seg_no % kFlagRing] | seg_flag[kFlagRing + seg_no % kFlagRing]) != 0;
+        const bool whole = c.tile0 == 0 && c.ntile == c.unit_tiles;
+        if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
+        const float L = bad ? -1.f : l;
+        const float inv = whole ? fp8_inv(L) : (L <= 0.f ? 0.f : 1.f);
+        const int head = (c.g * HP + kvh) * p.group + ur - j * p.group;
+        const int64_t out_at = (static_cast<int64_t>(c.b) * p.gamma + j) * p.hq + head;
+        const int64_t part_at = (c.u + w.cta) * p.slot_rows + h * sub_rows + stid;
+        if (real) {
+          if (!whole) p.partial_ml[part_at] = make_float2(m, L);
+          else if (p.lse) p.lse[out_at] = fp8_lse(m, L);
+        }
+        wait(pv_done(h), xl & 1);
+        tc_fence_after();
+        const bool has_nan = nan_flag[h] != 0;  // noted before the products just waited for
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          uint32_t raw[32];
+          float o[32];
+          tmem_ld32(o_col + c0, raw);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = inv == 0.f ? 0.f : __uint_as_float(raw[i]) * inv;
+          if (has_nan && inv != 0.f) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (nanv[h * D + c0 + i] & vis) o[i] = __int_as_float(0x7fc00000);
+          }
+          if (!real) continue;
+          if (whole) {
+            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + out_at * D + c0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t v[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 pr = __floats2bfloat162_rn(o[8 * i + 2 * e], o[8 * i + 2 * e + 1]);
+                v[e] = *reinterpret_cast<const uint32_t*>(&pr);
+              }
+              dst[i] = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+          } else {
+            float4* dst = reinterpret_cast<float4*>(p.partial_o + part_at * D + c0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          }
+        }
+        if (!whole && h == 0 && stid == 0) note_split_unit(p, c, w, tile_rows, pend, pend_count);
+        tc_fence_before();
+        bar_sync(sbar, nthr);  // nanv is read; the next segment may set it
+        for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;
+        if (stid == 0) nan_flag[h] = 0;
+        ++seg_no;
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == kSoftWarps + 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, C::TMEM_COLS);
+  }
+  if (!*abort_flag) merge_split_units<D, HP, kThreads>(p, pend, *pend_count);
+}
+
+template <int D, int HP>
+cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
+                         bool starve) {
+  using C = Cfg<D, HP>;
+  CUtensorMap map;
+  if (!encode_fp8_map(&map, a, HP)) return cudaErrorInvalidValue;
+  AttnFp8Params p = make_attn_fp8_params(a, P, ws);
+  p.hunits = a.num_kv_heads / HP;
+  p.rows_per_cta = P.sub_rows;
+  p.starve = starve ? 1 : 0;
+  p.unit_overhead = 3;  // tiles of time that starting a unit costs
+  const size_t smem = C::smem_bytes(a.batch);
+  auto kernel = attn_fp8_rows_kernel<D, HP>;
+  const cudaError_t e =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  kernel<<<P.grid, kThreads, smem, stream>>>(map, p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t attn_fp8_rows_smem(const spec_attn_fp8_args_t& a, int heads) {
+  if (a.head_dim == 128) return heads == 2 ? Cfg<128, 2>::smem_bytes(a.batch) : Cfg<128, 1>::smem_bytes(a.batch);
+  return heads == 2 ? Cfg<64, 2>::smem_bytes(a.batch) : Cfg<64, 1>::smem_bytes(a.batch);
+}
+
+cudaError_t launch_attn_fp8_rows(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
+                                 bool starve) {
+  if (P.heads == 2)
+    return a.head_dim == 128 ? launch_typed<128, 2>(a, P, ws, stream, starve) : launch_typed<64, 2>(a, P, ws, stream, starve);
+  return a.head_dim == 128 ? launch_typed<128, 1>(a, P, ws, stream, starve) : launch_typed<64, 1>(a, P, ws, stream, starve);
+}
+
+}  // namespace specv

@@ -1,0 +1,315 @@
+// What the two tensor-core kernels of the attention over the 8-bit cache share: PTX wrappers
+// for e4m3 products, the staging of keys and values, the work list, and the end of a block.
+#pragma once
+
+#include <cuda.h>  // CUtensorMap
+
+#include "attn_fp8.cuh"
+#include "tc_ptx.cuh"
+
+namespace specv {
+namespace fp8tc {
+
+using namespace tcx;
+
+constexpr int TK = kFp8KeyTile;  // keys per tile
+constexpr int NH = 2;            // sub-units of a block
+constexpr int kFlagRing = 16;    // segments' flags: more than the stages that producers run ahead
+
+// A stage holds a tile of 128 keys: K and V of HP KV heads as [8-key group][head, K or V]
+// [8 keys][D bytes], each atom of 8 rows swizzled by the width of a row.
+template <int D, int HP>
+struct Stage {
+  static constexpr uint32_t ATOM = 8 * D;
+  static constexpr uint32_t SG = 2 * HP * ATOM;  // an 8-key group
+  static constexpr uint32_t BYTES = (TK / 8) * SG;
+};
+
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// One page of HP KV heads, keys and values (encode_fp8_map's box).
+__device__ __forceinline__ void tma_load_page8(uint32_t dst, const CUtensorMap* map, int kind_head, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(0), "r"(kind_head), "r"(0), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Matrix descriptor of a tile whose rows are W bytes (128 or 64) with the W-byte swizzle.
+template <int W>
+__device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>((lbo >> 4) & 0x3FFFu) << 16) |
+         (static_cast<uint64_t>((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46) |
+         (static_cast<uint64_t>(W == 128 ? 2 : 4) << 61);
+}
+// Instruction descriptor, kind::f8f6f4: fp32 accumulator, e4m3 A and B.
+__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn, bool b_mn) {
+  return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+         (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void bar_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// The two e4m3 terms of four values, each packed in order from the low byte; UP: the second
+// terms times 16.
+template <bool UP>
+__device__ __forceinline__ void split_e4m3x4(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
+  asm("{\n .reg .b16 p, q, r, s;\n .reg .b32 x, y, h, g;\n"
+      " cvt.rn.satfinite.e4m3x2.f32 p, %3, %2;\n cvt.rn.satfinite.e4m3x2.f32 q, %5, %4;\n mov.b32 %0, {p, q};\n"
+      " cvt.rn.f16x2.f32 x, %3, %2;\n cvt.rn.f16x2.f32 y, %5, %4;\n"
+      " cvt.rn.f16x2.e4m3x2 h, p;\n cvt.rn.f16x2.e4m3x2 g, q;\n"
+      " sub.f16x2 x, x, h;\n sub.f16x2 y, y, g;\n mul.f16x2 x, x, %6;\n mul.f16x2 y, y, %6;\n"
+      " cvt.rn.satfinite.e4m3x2.f16x2 r, x;\n cvt.rn.satfinite.e4m3x2.f16x2 s, y;\n mov.b32 %1, {r, s};\n}"
+      : "=r"(hi), "=r"(lo)
+      : "f"(a), "f"(b), "f"(c), "f"(d), "r"(UP ? 0x4c004c00u : 0x3c003c00u));
+}
+
+// The slow part of a wait: polls until the phase completes, or gives up (mbar_wait).
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status) {
+  return mbar_wait(bar, parity, abort_flag, status);
+}
+
+#ifdef __CUDACC__
+// ---------------------------------------------------------------------------------
+// The work list: the tiles of all units, cut into equal ranges, one per block
+// ---------------------------------------------------------------------------------
+struct WorkList {
+  int64_t t0, t1, total;  // this block's range, and the list's length
+  const int* pb;          // [batch + 1]: first tile of each sequence
+  int ovh, ctas, cta;
+};
+
+// First tiles of the sequences (one warp).
+__device__ __forceinline__ void prefix_tiles(const AttnParams& p, int* pb) {
+  const int lane = threadIdx.x & 31;
+  const int per_b = p.hunits * p.row_tiles;
+  int carry = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const int b = b0 + lane;
+    int v = b < p.batch ? (unit_tiles<TK>(p.kv_len[b], p) + p.unit_overhead) * per_b : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    if (b < p.batch) pb[b + 1] = carry + v;
+    carry += __shfl_sync(0xffffffffu, v, 31);
+  }
+  if (lane == 0) pb[0] = 0;
+}
+
+// Equal ranges on every SM (a multiple of the units, so that equal units have no boundary
+// inside a range, measured slower: 135.8 against 123.2 us with 128 ragged units, 232 against
+// 226 with 64 equal ones).
+__device__ __forceinline__ WorkList work_list(const AttnParams& p, const int* pb) {
+  WorkList w;
+  w.pb = pb;
+  w.ovh = p.unit_overhead;
+  w.total = pb[p.batch];
+  w.ctas = static_cast<int>(w.total < gridDim.x ? w.total : gridDim.x);
+  w.cta = blockIdx.x;
+  w.t0 = w.cta < w.ctas ? static_cast<int64_t>(w.cta) * w.total / w.ctas : 0;
+  w.t1 = w.cta < w.ctas ? static_cast<int64_t>(w.cta + 1) * w.total / w.ctas : 0;
+  return w;
+}
+
+// Notes a unit that this block has written a partial result of (only a block's first and
+// last segments can be split).
+__device__ __forceinline__ void note_split_unit(const AttnParams& p, const Seg& c, const WorkList& w, int tile_rows,
+                                                int* pend, volatile int* pend_count) {
+  const int c_first = owner_of(c.unit_start, w.total, w.ctas);
+  const int c_last = owner_of(c.unit_start + c.unit_tiles - 1, w.total, w.ctas);
+  int* e = pend + 8 * (*pend_count);
+  const int row_base = c.rt * tile_rows;
+  e[0] = c.b; e[1] = c.g; e[2] = row_base; e[3] = min(tile_rows, p.rows - row_base);
+  e[4] = static_cast<int>(c.u + c_first); e[5] = c_last - c_first + 1;
+  e[6] = static_cast<int>(c.u); e[7] = 0;
+  *pend_count = *pend_count + 1;
+}
+
+// At a block's end: one ticket per split unit, after a fence; the block that completes a unit
+// merges it.
+template <int D, int HP, int kThreads>
+__device__ __forceinline__ void merge_split_units(const AttnParams& p, int* pend, int np) {
+  if (np == 0) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x < np) {
+    int* e = pend + 8 * threadIdx.x;
+    const uint32_t prev = atomicAdd(&p.tickets[e[6]], 1u);
+    e[7] = prev == static_cast<uint32_t>(e[5] - 1);
+    if (e[7]) p.tickets[e[6]] = 0;
+  }
+  __syncthreads();
+  for (int i = 0; i < np; ++i) {
+    const int* e = pend + 8 * i;
+    if (!e[7]) continue;
+    __threadfence();
+    merge_fp8_unit<D>(p, e[0], e[1] * HP, HP, e[2], e[3], e[4], e[5], threadIdx.x, kThreads);
+  }
+}
+
+// ---------------------------------------------------------------------------------
+// Staging
+// ---------------------------------------------------------------------------------
+// A producer warp: the half of each tile's pages, one TMA box each, and their scales as
+// scl[stage][page of the tile][head] = (sk * softmax scale * log2(e), log2(sv), 1 / sv, -).
+// Two of them, because one keeps the copy engine waiting.
+template <int D, int HP, int NST>
+__device__ __forceinline__ void produce(const AttnFp8Params& p, const CUtensorMap& tmap, const WorkList& w, int half,
+                                        uint32_t stages, uint32_t full, uint32_t empty, uint32_t flag_ready,
+                                        float4* scl, volatile int* seg_flag, volatile int* abort_flag) {
+  const int lane = threadIdx.x & 31;
+  uint32_t it = 0, seg_no = 0;
+  bool ok = true;
+  const int psh = __ffs(p.page_size) - 1;  // log2
+  const int npg = TK >> psh;               // pages of a tile
+  const uint32_t box_bytes = static_cast<uint32_t>(p.page_size) * D * 2 * HP;
+  for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok && !p.starve; ++seg_no) {
+    const bool bad_len = !s.len_ok;
+    bool flag = bad_len;
+    // Pages are taken 32 at a time, a lane each; the next 32 ids and scales are loaded
+    // while these are in use, the ids of the 32 after them too.
+    const int pages = bad_len ? 0 : (s.kv_len + p.page_size - 1) >> psh;
+    const int first = s.tile0 * npg;
+    const int32_t* table = p.page_table + static_cast<int64_t>(s.b) * p.max_pages;
+    auto load_id = [&](int base) { return base + lane < pages ? __ldg(table + base + lane) : 0; };
+    auto load_scale = [&](int id, float2* sc) {
+      const bool in = id >= 0 && id < p.num_pages;
+      const float2* src = reinterpret_cast<const float2*>(p.kv_scale) +
+                          static_cast<int64_t>(in ? id : 0) * p.hkv + s.g * HP;
+#pragma unroll
+      for (int h = 0; h < HP; ++h) sc[h] = __ldg(src + h);
+    };
+    int base = first, id = load_id(first), id1 = load_id(first + 32), id2 = load_id(first + 64);
+    float2 sc[HP], sc1[HP];
+    load_scale(id, sc);
+    load_scale(id1, sc1);
+    for (int k = 0; k < s.ntile && ok; ++k, ++it) {
+      const uint32_t st = it % NST;
+      const int pg0 = first + k * npg;
+      if (pg0 >= base + 32) {
+        base += 32;
+        id = id1;
+        id1 = id2;
+#pragma unroll
+        for (int h = 0; h < HP; ++h) sc[h] = sc1[h];
+        load_scale(id1, sc1);
+        id2 = load_id(base + 64);
+      }
+      if (it >= NST) ok = mbar_wait(empty + 8u * st, ((it / NST) - 1) & 1, abort_flag, p.status);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      // lanes [pg0 - base, + npg) hold this tile's pages; this warp copies the half
+      // [q0, q1) of them
+      const int q0 = half * (npg >> 1), q1 = min(q0 + (npg >> 1), pages - pg0);
+      const uint32_t dst = stages + st * Stage<D, HP>::BYTES;
+      if (lane == 0 && q1 > q0) mbar_expect_tx(full + 8u * st, static_cast<uint32_t>(q1 - q0) * box_bytes);
+      for (int q = q0; q < q1; ++q) {
+        const int raw = __shfl_sync(0xffffffffu, id, pg0 - base + q);
+        const bool in_range = raw >= 0 && raw < p.num_pages;
+        flag |= !in_range;
+        if (lane == 0)
+          tma_load_page8(dst + static_cast<uint32_t>(q) * box_bytes, &tmap,
+                         2 * ((in_range ? raw : 0) * p.hkv + s.g * HP), full + 8u * st);
+      }
+      const int q = base + lane - pg0;
+      if (q >= q0 && q < q0 + (npg >> 1)) {
+#pragma unroll
+        for (int h = 0; h < HP; ++h) {
+          const float sv = clamp_scale(sc[h].y);
+          scl[(st * 8 + q) * HP + h] = q < q1 ? make_float4(sc[h].x * p.scale_log2, __log2f(sv), __frcp_rn(sv), 0.f)
+                                              : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full + 8u * st);
+      __syncwarp();
+    }
+    if (ok && lane == 0) {
+      seg_flag[half * kFlagRing + seg_no % kFlagRing] = flag ? 1 : 0;
+      mbar_arrive(flag_ready + 8u * (seg_no % kFlagRing));
+    }
+    if (!has_more(s, w.t1, w.ovh)) break;
+    s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
+  }
+  if (!ok) {  // copies still in flight (bounded)
+    for (uint32_t x = it > static_cast<uint32_t>(NST) ? it - NST : 0; x < it; ++x) {
+      const long long c0 = clock64();
+      while (!mbar_try(full + 8u * (x % NST), (x / NST) & 1) && clock64() - c0 < kWaitCycles) {
+      }
+    }
+  }
+}
+
+// V of keys that no row sees must be finite, because their weight of 0 is multiplied: keys
+// past the end are cleared, and a NaN in a block key's value is cleared and noted in
+// nanv[sub-unit][D] (a bit per block key), for the outputs of the rows that see it.
+template <int D, int HP>
+__device__ __forceinline__ void fix_values(const AttnParams& p, const Seg& sg, int k, unsigned char* base,
+                                           unsigned long long* nanv, volatile int* nan_flag) {
+  const int key0 = (sg.tile0 + k) * TK;
+  const int ctx = sg.kv_len - p.gamma;
+  if (!sg.len_ok || key0 + TK <= ctx) return;
+  const int nvalid = min(TK, sg.kv_len - key0);
+  constexpr int kPieces = D / 16;
+  const int lane = threadIdx.x & 31;
+  const int from = max(0, ctx - key0);
+  for (int i = lane; i < (TK - from) * kPieces * HP; i += 32) {
+    const int piece = i % kPieces, h = (i / kPieces) % HP, key = from + i / (kPieces * HP);
+    const int ph = D == 128 ? piece ^ (key & 7) : piece ^ ((key >> 1) & 3);
+    uint4* at = reinterpret_cast<uint4*>(base + (key >> 3) * Stage<D, HP>::SG + (2 * h + 1) * Stage<D, HP>::ATOM + (key & 7) * D + ph * 16);
+    if (key >= nvalid) {
+      *at = make_uint4(0, 0, 0, 0);
+      continue;
+    }
+    uint4 v = *at;
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) any |= __vcmpeq4(w[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+    if (any) {
+      const unsigned long long bit = 1ull << (key0 + key - ctx);
+      for (int e = 0; e < 16; ++e) {
+        const uint32_t sh = (e & 3) * 8;
+        if ((w[e >> 2] >> sh & 0x7fu) == 0x7fu) {
+          atomicOr(nanv + h * D + piece * 16 + e, bit);
+          if (HP == 1) atomicOr(nanv + D + piece * 16 + e, bit);
+          w[e >> 2] &= ~(0xffu << sh);
+        }
+      }
+      nan_flag[h] = 1;
+      if (HP == 1) nan_flag[1] = 1;
+      *at = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  fence_async_smem();
+  __syncwarp();
+}
+#endif
+
+// The tensor map of the cache: a box is one page of `heads` adjacent KV heads.
+bool encode_fp8_map(CUtensorMap* map, const spec_attn_fp8_args_t& a, int heads);
+
+}  // namespace fp8tc
+}  // namespace specv

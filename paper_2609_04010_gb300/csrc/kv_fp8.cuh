@@ -14,6 +14,7 @@ cudaError_t launch_adjust(const spec_adjust_args_t& a, int sms, cudaStream_t str
 // The launch plan of the attention over the 8-bit cache.
 struct AttnFp8Plan {
   int path;             // SPEC_ATTN_CUDA_CORES or SPEC_ATTN_TENSOR_CORES
+  int rows_on_m;        // tensor cores: attn_fp8_rows.cu, else attn_fp8_keys.cu
   int heads;            // tensor cores: KV heads per block (2: adjacent ones)
   int sub_rows;         // tensor cores: query rows of one of a block's two sub-units
   int grid;             // tensor cores: blocks
@@ -24,13 +25,15 @@ struct AttnFp8Plan {
   size_t tickets, partial_o, partial_ml, end;
 };
 AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path);
-constexpr int kFp8KeyTile = 128;   // keys per tile of the tensor-core kernel
-constexpr int kFp8SubRows = 64;    // query rows of a sub-unit, at most
-// Whether the tensor-core kernel takes the call in this form.
-bool attn_fp8_tc_fits(const spec_attn_fp8_args_t& a, int heads, int sub_rows, int row_tiles);
-// starve (test hook only): the producer issues no copies, so the bounded waits run out.
-cudaError_t launch_attn_fp8_tc(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
-                               cudaStream_t stream, bool starve = false);
+constexpr int kFp8KeyTile = 128;  // keys per tile of the tensor-core kernels
+// Their blocks' shared memory. starve (test hook only): the producers issue no copies, so the
+// bounded waits run out.
+size_t attn_fp8_keys_smem(const spec_attn_fp8_args_t& a, int heads, int sub_rows);
+size_t attn_fp8_rows_smem(const spec_attn_fp8_args_t& a, int heads);
+cudaError_t launch_attn_fp8_keys(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
+                                 cudaStream_t stream, bool starve = false);
+cudaError_t launch_attn_fp8_rows(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
+                                 cudaStream_t stream, bool starve = false);
 cudaError_t launch_attn_fp8_simt(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
                                  cudaStream_t stream);
 
