@@ -46,9 +46,8 @@ spec_status_t check_append(const spec_append_fp8_args_t* a) {
 
 // The tensor-core form of a call. A block serves two sub-units of query rows: two adjacent KV
 // heads where each fits one (a page of both is one copy of twice the size), else two halves
-// of one KV head's rows, in tiles. With the rows on the MMA's M side (up to 128 a sub-unit)
-// a thread owns a row, with the keys there (up to 64) few rows cost little.
-constexpr int kRowsFrom = 33;  // rows of a sub-unit from which they go to the M side
+// of one KV head's rows, in tiles. Up to 128 rows a KV head the keys are on the MMA's M side
+// (up to 64 rows a sub-unit); above, the rows are (up to 128 a sub-unit).
 struct TcForm {
   int rows_on_m, heads, sub_rows, row_tiles;
   bool fits;
@@ -56,10 +55,10 @@ struct TcForm {
 TcForm tc_form(const spec_attn_fp8_args_t& a) {
   const int rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
   TcForm f;
-  f.heads = rows <= 128 && a.num_kv_heads % 2 == 0 ? 2 : 1;
+  f.heads = rows <= 64 && a.num_kv_heads % 2 == 0 ? 2 : 1;
   f.row_tiles = f.heads == 2 ? 1 : (rows + 255) / 256;
   f.sub_rows = f.heads == 2 ? rows : (rows > 256 ? 128 : (rows + 1) / 2);
-  f.rows_on_m = f.sub_rows >= kRowsFrom;
+  f.rows_on_m = f.sub_rows > 64;
   const size_t smem = f.rows_on_m ? attn_fp8_rows_smem(a, f.heads) : attn_fp8_keys_smem(a, f.heads, f.sub_rows);
   const int64_t tiles = (static_cast<int64_t>(a.max_pages_per_seq) * a.page_size + kFp8KeyTile - 1) / kFp8KeyTile + 8;
   const int64_t units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / f.heads) * f.row_tiles;
@@ -146,7 +145,7 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
     P.slots = P.nsplit > 1 ? units * P.nsplit : 0;
   }
   P.tickets = base;
-  P.partial_o = ws_round(P.tickets + sizeof(uint32_t) * units);
+  P.partial_o = ws_round(P.tickets + (P.path == SPEC_ATTN_TENSOR_CORES ? 2 * sizeof(int4) * P.grid : sizeof(uint32_t) * units));
   P.partial_ml = ws_round(P.partial_o + static_cast<size_t>(P.slots) * P.slot_rows * a.head_dim * 4);
   P.end = ws_round(P.partial_ml + static_cast<size_t>(P.slots) * P.slot_rows * sizeof(float2));
   return P;

@@ -11,6 +11,7 @@ namespace specv {
 // AttnParams with k_cache = the 8-bit cache (v_cache unused) and its scales.
 struct AttnFp8Params : AttnParams {
   const float* kv_scale;  // [num_pages][Hkv][2]
+  int4* splits;           // [grid][2]: the split unit that each block ends (tensor-core kernels)
 };
 
 inline AttnFp8Params make_attn_fp8_params(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws) {
@@ -41,6 +42,7 @@ inline AttnFp8Params make_attn_fp8_params(const spec_attn_fp8_args_t& a, const A
   p.lse = a.lse;
   p.status = reinterpret_cast<uint32_t*>(ws);
   p.tickets = reinterpret_cast<uint32_t*>(ws + P.tickets);
+  p.splits = reinterpret_cast<int4*>(ws + P.tickets);
   p.partial_o = reinterpret_cast<float*>(ws + P.partial_o);
   p.partial_ml = reinterpret_cast<float2*>(ws + P.partial_ml);
   p.tree_mask = a.tree_mask;
@@ -63,58 +65,54 @@ __device__ __forceinline__ void write_fp8_lse(const AttnParams& p, int b, int g,
   p.lse[(static_cast<int64_t>(b) * p.gamma + j) * p.hq + h] = fp8_lse(m, l);
 }
 
-// The partials of one unit in slots [slot0, slot0 + nslots): rows [row0, row0 + nrows) of KV
-// heads g .. g + nheads - 1 (a head's rows after another's in a slot) are merged and written.
-// A thread takes a (row, 8 columns) item; the loads of up to four slots are in flight
-// together.
-template <int D>
-__device__ void merge_fp8_unit(const AttnParams& p, int b, int g, int nheads, int row0, int nrows,
-                               int64_t slot0, int nslots, int tid, int nthreads) {
-  constexpr int C8 = D / 8, SB = 4;
-  for (int idx = tid; idx < nheads * nrows * C8; idx += nthreads) {
-    const int hr = idx / C8, c8 = idx % C8;
-    const int head = hr / nrows, r = hr - head * nrows;
-    float M = -INFINITY, L = 0.f, acc[8];
-    bool bad = false;
+// Merges and writes 8 columns (from 8 * c8) of row `row` of KV head g, whose parts are row
+// `hr` of the slots [slot0, slot0 + nslots). A slot's outputs are [row][D], or with BY_COLUMNS
+// [D / 4][row][4]. The loads of up to four slots are in flight together.
+template <int D, bool BY_COLUMNS>
+__device__ __forceinline__ void merge_fp8_item(const AttnParams& p, int b, int g, int row, int64_t slot0, int nslots,
+                                               int hr, int c8) {
+  constexpr int SB = 4;
+  float M = -INFINITY, L = 0.f, acc[8];
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  for (int s0 = 0; s0 < nslots; s0 += SB) {
+    float2 ml[SB];
+    float4 lo[SB], hi[SB];
+#pragma unroll
+    for (int i = 0; i < SB; ++i) {
+      ml[i] = make_float2(-INFINITY, 0.f);
+      lo[i] = hi[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s0 + i < nslots) {
+        const int64_t first = (slot0 + s0 + i) * p.slot_rows;
+        const float4* src = reinterpret_cast<const float4*>(p.partial_o) + first * (D / 4) +
+                            (BY_COLUMNS ? 2 * c8 * p.slot_rows + hr : hr * (D / 4) + 2 * c8);
+        ml[i] = __ldcg(&p.partial_ml[first + hr]);
+        lo[i] = __ldcg(src);
+        hi[i] = __ldcg(src + (BY_COLUMNS ? p.slot_rows : 1));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < SB; ++i) {
+      if (ml[i].y < 0.f) bad = true;
+      if (ml[i].y == 0.f) continue;  // saw no key
+      const float m = fmaxf(M, ml[i].x);
+      const float old = M == -INFINITY ? 0.f : ex2(M - m), w = m == -INFINITY ? 1.f : ex2(ml[i].x - m);
+      L = L * old + ml[i].y * w;
+      const float x[8] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w, hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = acc[e] * old + x[e] * w;
+      M = m;
+    }
+  }
+  if (bad) L = -1.f;
+  const float inv = fp8_inv(L);
+  if (inv == 0.f) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    for (int s0 = 0; s0 < nslots; s0 += SB) {
-      float2 ml[SB];
-      float4 lo[SB], hi[SB];
-#pragma unroll
-      for (int i = 0; i < SB; ++i) {
-        ml[i] = make_float2(-INFINITY, 0.f);
-        lo[i] = hi[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (s0 + i < nslots) {
-          const int64_t row = (slot0 + s0 + i) * p.slot_rows + hr;
-          const float4* src = reinterpret_cast<const float4*>(p.partial_o + row * D) + 2 * c8;
-          ml[i] = __ldcg(&p.partial_ml[row]);
-          lo[i] = __ldcg(src);
-          hi[i] = __ldcg(src + 1);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < SB; ++i) {
-        if (ml[i].y < 0.f) bad = true;
-        if (ml[i].y == 0.f) continue;  // saw no key
-        const float m = fmaxf(M, ml[i].x);
-        const float old = M == -INFINITY ? 0.f : ex2(M - m), w = m == -INFINITY ? 1.f : ex2(ml[i].x - m);
-        L = L * old + ml[i].y * w;
-        const float x[8] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w, hi[i].x, hi[i].y, hi[i].z, hi[i].w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = acc[e] * old + x[e] * w;
-        M = m;
-      }
-    }
-    if (bad) L = -1.f;
-    const float inv = fp8_inv(L);
-    if (inv == 0.f) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    }
-    write_out_row<D>(p, b, g + head, row0 + r, c8 * 8, acc, inv);
-    if (c8 == 0) write_fp8_lse(p, b, g + head, row0 + r, M, L);
   }
+  write_out_row<D>(p, b, g, row, c8 * 8, acc, inv);
+  if (c8 == 0) write_fp8_lse(p, b, g, row, M, L);
 }
 #endif
 

@@ -71,10 +71,9 @@ struct Cfg {
   // full[NST], empty[NST], s_full[NH][SB], s_free[NH][SB], p_full[NH], pv_done[NH],
   // seg_ready[NH], drain[2], flag_ready[kFlagRing]
   static constexpr int NBAR = 2 * NST + 2 * NH * SB + 3 * NH + 2 + kFlagRing;
-  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, pending, -, NaN flags
+  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, -, -, NaN flags
   static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;               // int [2][kFlagRing]: segments' bad flags
-  static constexpr uint32_t OFF_PEND = OFF_FLAG + 8 * kFlagRing;    // int [2][8]
-  static constexpr uint32_t OFF_QMAX = OFF_PEND + 64;       // uint32 [NH][8]
+  static constexpr uint32_t OFF_QMAX = OFF_FLAG + 8 * kFlagRing;       // uint32 [NH][8]
   static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 32;    // int [batch + 1]
   static constexpr uint32_t S_COL = 0;                      // [NH][SB][NR]
   static constexpr uint32_t O_COL = NH * SB * NR;           // [NH][first, second terms][NR]
@@ -157,10 +156,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned long long* nanv = reinterpret_cast<unsigned long long*>(smem + C::OFF_NAN);
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
-  volatile int* pend_count = reinterpret_cast<volatile int*>(misc + 2);
   volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 4);  // [NH]
   volatile int* seg_flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);  // [producer][kFlagRing]
-  int* pend = reinterpret_cast<int*>(smem + C::OFF_PEND);
   int* pb = reinterpret_cast<int*>(smem + C::OFF_PB);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -179,10 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(bar0 + 8u * i, n);
     }
     if (lane < NH) nan_flag[lane] = 0;
-    if (lane == 0) {
-      *abort_flag = 0;
-      *pend_count = 0;
-    }
+    if (lane == 0) *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = threadIdx.x; i < NH * D; i += kThreads) nanv[i] = 0ull;
@@ -193,6 +187,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = misc[0];
   const WorkList w = work_list(p, pb);
+  pdl_launch_dependents();
+  if (threadIdx.x == 32 * (kSoftWarps + 2)) note_split_unit(p, w, tile_rows);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 3) {
     // ============================ producers ============================
@@ -584,9 +580,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           else p.partial_o[row_at[r] + d] = o;
         }
       }
-      if (!whole && h == 0 && stid == 0) {
-        note_split_unit(p, c, w, tile_rows, pend, pend_count);
-      }
       tc_fence_before();
       bar_sync(sbar, nthr);  // xch, the row state and nanv are read; the next segment may set them
       for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;
@@ -600,7 +593,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, C::TMEM_COLS);
   }
-  if (!*abort_flag) merge_split_units<D, HP, kThreads>(p, pend, *pend_count);
 }
 
 template <int D, int HP, int NR>
@@ -623,7 +615,8 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   kernel<<<P.grid, kThreads, smem, stream>>>(map, p);
-  return cudaGetLastError();
+  const cudaError_t k = cudaGetLastError();
+  return k == cudaSuccess ? launch_merge<D, HP, false>(p, P, stream) : k;
 }
 
 template <int D, int HP>

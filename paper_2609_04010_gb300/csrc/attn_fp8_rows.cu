@@ -48,10 +48,9 @@ struct Cfg {
   // full[NST], empty[NST], s_full[NH], p_full[NH], pv_done[NH], seg_ready[NH], drain[2],
   // flag_ready[kFlagRing]
   static constexpr int NBAR = 2 * NST + 4 * NH + 2 + kFlagRing;
-  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;        // tmem base, abort, pending, -, NaN flags
+  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;        // tmem base, abort, -, -, NaN flags
   static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;             // int [2][kFlagRing]: segments' bad flags
-  static constexpr uint32_t OFF_PEND = OFF_FLAG + 8 * kFlagRing;  // int [2][8]
-  static constexpr uint32_t OFF_PB = OFF_PEND + 64;               // int [batch + 1]
+  static constexpr uint32_t OFF_PB = OFF_FLAG + 8 * kFlagRing;               // int [batch + 1]
   static constexpr uint32_t S_COL = 0;                            // [NH][128]; P over it
   static constexpr uint32_t O_COL = NH * TK;                      // [NH][D]
   static constexpr uint32_t TMEM_COLS = 512;
@@ -90,10 +89,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned long long* nanv = reinterpret_cast<unsigned long long*>(smem + C::OFF_NAN);
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
-  volatile int* pend_count = reinterpret_cast<volatile int*>(misc + 2);
   volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 4);            // [NH]
   volatile int* seg_flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);  // [producer][kFlagRing]
-  int* pend = reinterpret_cast<int*>(smem + C::OFF_PEND);
   int* pb = reinterpret_cast<int*>(smem + C::OFF_PB);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -112,10 +109,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(bar0 + 8u * i, n);
     }
     if (lane < NH) nan_flag[lane] = 0;
-    if (lane == 0) {
-      *abort_flag = 0;
-      *pend_count = 0;
-    }
+    if (lane == 0) *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = threadIdx.x; i < NH * D; i += kThreads) nanv[i] = 0ull;
@@ -126,6 +120,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = misc[0];
   const WorkList w = work_list(p, pb);
+  pdl_launch_dependents();
+  if (threadIdx.x == 32 * (kSoftWarps + 2)) note_split_unit(p, w, tile_rows);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 3) {
     // ============================ producers ============================
@@ -328,29 +324,34 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (r < 0) return static_cast<uint32_t>(vis << -r) | ((1u << -r) - 1u);
             return r < 64 ? static_cast<uint32_t>(vis >> r) : 0u;
           };
+          auto hide = [&](uint32_t* r, uint32_t seen) {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) r[c] = (seen >> c & 1) ? r[c] : 0xff800000u;
+            asm volatile("");  // keeps the branch around this
+          };
           const float4* const sc = scl + st * 8 * HP + kvh;  // page g of the tile: sc[g * HP]
           wait(s_full(h), x & 1);
           tc_fence_after();
           wait(full(st), (x / NST) & 1);  // orders the producer's scales before this
           // ---- the row's largest weighted exponent ----
           float top = -INFINITY;
+          {
+            uint32_t raw[2][32];
+            tmem_ld32(s_col, raw[0]);
 #pragma unroll
-          for (int c0 = 0; c0 < TK; c0 += 32) {
-            uint32_t raw[32];
-            tmem_ld32(s_col + c0, raw);
-            tmem_wait_ld();
-            if (masked) {
-              const uint32_t seen = seen_of(c0);
+            for (int c0 = 0; c0 < TK; c0 += 32) {
+              uint32_t* const r = raw[(c0 >> 5) & 1];
+              tmem_wait_ld();
+              if (c0 + 32 < TK) tmem_ld32(s_col + c0 + 32, raw[((c0 >> 5) & 1) ^ 1]);
+              if (masked) hide(r, seen_of(c0));
 #pragma unroll
-              for (int c = 0; c < 32; ++c) raw[c] = (seen >> c & 1) ? raw[c] : 0xff800000u;
-            }
+              for (int g = 0; g < 32; g += 16) {
+                const float4 q = sc[((c0 + g) >> psh) * HP];
+                float t = __uint_as_float(r[g]);
 #pragma unroll
-            for (int g = 0; g < 32; g += 16) {
-              const float4 q = sc[((c0 + g) >> psh) * HP];
-              float t = __uint_as_float(raw[g]);
-#pragma unroll
-              for (int c = 1; c < 16; ++c) t = fmaxf(t, __uint_as_float(raw[g + c]));
-              if (t != -INFINITY) top = fmaxf(top, fmaf(t, q.x * qf, q.y));
+                for (int c = 1; c < 16; ++c) t = fmaxf(t, __uint_as_float(r[g + c]));
+                if (t != -INFINITY) top = fmaxf(top, fmaf(t, q.x * qf, q.y));
+              }
             }
           }
           // ---- raise the reference where a weight would pass 2^8 ----
@@ -377,42 +378,56 @@ __global__ void __launch_bounds__(kThreads, 1)
           // ---- weights, their sum, and their two terms over the columns of S ----
           const float msub = m == -INFINITY ? 0.f : m;
           // scores so large that log2(sv) - m alone rounds by more than a weight may bear
-          const bool far = __any_sync(0xffffffffu, fabsf(msub) > 1048576.f);
+          const bool special = masked || __any_sync(0xffffffffu, fabsf(msub) > 1048576.f);
+          {
+            uint32_t raw[2][32];
+            tmem_ld32(s_col, raw[0]);
+#pragma unroll 1
+            for (int c1 = 0; c1 < TK; c1 += 64) {
 #pragma unroll
-          for (int c0 = 0; c0 < TK; c0 += 32) {
-            uint32_t raw[32], w1[8], w2[8];
-            tmem_ld32(s_col + c0, raw);
-            tmem_wait_ld();
-            uint32_t seen = ~0u;
-            if (masked) seen = seen_of(c0);
+              for (int u = 0; u < 2; ++u) {
+                const int c0 = c1 + 32 * u;
+                uint32_t* const r = raw[u];
+                uint32_t w1[8], w2[8];
+                tmem_wait_ld();
+                if (u == 0 || c1 + 64 < TK) tmem_ld32(s_col + c0 + 32, raw[u ^ 1]);
+                float2 ab[2];  // per 16 keys: e = a * S + b
+                float inv_sv[2];
 #pragma unroll
-            for (int g = 0; g < 32; g += 16) {
-              const float4 q = sc[((c0 + g) >> psh) * HP];
-              float a = q.x * qf, b = q.y - msub;
-              if (far) {
-#pragma unroll
-                for (int c = g; c < g + 16; ++c)
-                  raw[c] = __float_as_uint(fmaf(__uint_as_float(raw[c]), a, q.y) - msub);
-                a = 1.f;
-                b = 0.f;
-              }
-              float sum = 0.f;
-#pragma unroll
-              for (int c = g; c < g + 16; c += 4) {
-                float pr[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) pr[i] = ex2(fmaf(__uint_as_float(raw[c + i]), a, b));
-                if (masked) {
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) pr[i] = (seen >> (c + i) & 1) ? pr[i] : 0.f;
+                for (int g = 0; g < 2; ++g) {
+                  const float4 q = sc[((c0 + 16 * g) >> psh) * HP];
+                  ab[g] = make_float2(q.x * qf, q.y - msub);
+                  inv_sv[g] = q.z;
                 }
-                sum += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-                split_e4m3x4<false>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
+                if (special) {  // hidden keys, or scores too large for the short form
+                  const uint32_t seen = masked ? seen_of(c0) : ~0u;
+#pragma unroll
+                  for (int g = 0; g < 2; ++g) {
+                    const float lv = sc[((c0 + 16 * g) >> psh) * HP].y;
+#pragma unroll
+                    for (int c = 16 * g; c < 16 * g + 16; ++c)
+                      r[c] = __float_as_uint(fmaf(__uint_as_float(r[c]), ab[g].x, lv) - msub);
+                    ab[g] = make_float2(1.f, 0.f);
+                  }
+                  hide(r, seen);
+                }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                  float sum = 0.f;
+#pragma unroll
+                  for (int c = 16 * g; c < 16 * g + 16; c += 4) {
+                    float pr[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pr[i] = ex2(fmaf(__uint_as_float(r[c + i]), ab[g].x, ab[g].y));
+                    sum += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+                    split_e4m3x4<false>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
+                  }
+                  l = fmaf(sum, inv_sv[g], l);
+                }
+                tmem_st8(s_col + c0, w1);
+                tmem_st8(s_col + c0 + 8, w2);
               }
-              l = fmaf(sum, q.z, l);
             }
-            tmem_st8(s_col + c0, w1);
-            tmem_st8(s_col + c0 + 8, w2);
           }
           tmem_wait_st();
           tc_fence_before();
@@ -474,12 +489,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               dst[i] = make_uint4(v[0], v[1], v[2], v[3]);
             }
           } else {
-            float4* dst = reinterpret_cast<float4*>(p.partial_o + part_at * D + c0);
+            float4* dst = reinterpret_cast<float4*>(p.partial_o) + (c.u + w.cta) * p.slot_rows * (D / 4) +
+                          static_cast<int64_t>(c0 / 4) * p.slot_rows + h * sub_rows + stid;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            for (int i = 0; i < 8; ++i) dst[i * p.slot_rows] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
           }
         }
-        if (!whole && h == 0 && stid == 0) note_split_unit(p, c, w, tile_rows, pend, pend_count);
         tc_fence_before();
         bar_sync(sbar, nthr);  // nanv is read; the next segment may set it
         for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;
@@ -494,7 +509,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, C::TMEM_COLS);
   }
-  if (!*abort_flag) merge_split_units<D, HP, kThreads>(p, pend, *pend_count);
 }
 
 template <int D, int HP>
@@ -514,7 +528,8 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   kernel<<<P.grid, kThreads, smem, stream>>>(map, p);
-  return cudaGetLastError();
+  const cudaError_t k = cudaGetLastError();
+  return k == cudaSuccess ? launch_merge<D, HP, true>(p, P, stream) : k;
 }
 
 }  // namespace

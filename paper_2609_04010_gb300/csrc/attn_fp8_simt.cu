@@ -200,7 +200,8 @@ __global__ void __launch_bounds__(NT) attn_fp8_simt_kernel(AttnFp8Params p) {
   __syncthreads();
   if (!sm.last) return;
   __threadfence();
-  merge_fp8_unit<D>(p, b, g, 1, row0, nrows, unit * p.nsplit, p.nsplit, tid, NT);
+  for (int i = tid; i < nrows * (D / 8); i += NT)
+    merge_fp8_item<D, false>(p, b, g, row0 + i / (D / 8), unit * p.nsplit, p.nsplit, i / (D / 8), i % (D / 8));
 }
 
 template <int D>

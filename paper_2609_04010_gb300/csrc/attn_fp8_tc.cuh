@@ -133,40 +133,50 @@ __device__ __forceinline__ WorkList work_list(const AttnParams& p, const int* pb
   return w;
 }
 
-// Notes a unit that this block has written a partial result of (only a block's first and
-// last segments can be split).
-__device__ __forceinline__ void note_split_unit(const AttnParams& p, const Seg& c, const WorkList& w, int tile_rows,
-                                                int* pend, volatile int* pend_count) {
-  const int c_first = owner_of(c.unit_start, w.total, w.ctas);
-  const int c_last = owner_of(c.unit_start + c.unit_tiles - 1, w.total, w.ctas);
-  int* e = pend + 8 * (*pend_count);
-  const int row_base = c.rt * tile_rows;
-  e[0] = c.b; e[1] = c.g; e[2] = row_base; e[3] = min(tile_rows, p.rows - row_base);
-  e[4] = static_cast<int>(c.u + c_first); e[5] = c_last - c_first + 1;
-  e[6] = static_cast<int>(c.u); e[7] = 0;
-  *pend_count = *pend_count + 1;
+// What merge_fp8_kernel is to join: a unit split between blocks, noted by the block with its
+// last tiles (they are that block's first, so a block notes at most one). The note does not
+// depend on the pass over the data; every block writes its own, if only an empty one.
+__device__ __forceinline__ void note_split_unit(const AttnFp8Params& p, const WorkList& w, int tile_rows) {
+  int4 a = make_int4(0, 0, 0, 0), b = a;
+  const Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh);
+  if (w.t0 < w.t1 && s.ntile > 0 && s.tile0 > 0 && s.tile0 + s.ntile == s.unit_tiles) {
+    const int first = owner_of(s.unit_start, w.total, w.ctas), row0 = s.rt * tile_rows;
+    a = make_int4(s.b, s.g, row0, min(tile_rows, p.rows - row0));
+    b = make_int4(static_cast<int>(s.u + first), w.cta - first + 1, 0, 0);
+  }
+  p.splits[2 * blockIdx.x] = a;
+  p.splits[2 * blockIdx.x + 1] = b;
 }
 
-// At a block's end: one ticket per split unit, after a fence; the block that completes a unit
-// merges it.
-template <int D, int HP, int kThreads>
-__device__ __forceinline__ void merge_split_units(const AttnParams& p, int* pend, int np) {
-  if (np == 0) return;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x < np) {
-    int* e = pend + 8 * threadIdx.x;
-    const uint32_t prev = atomicAdd(&p.tickets[e[6]], 1u);
-    e[7] = prev == static_cast<uint32_t>(e[5] - 1);
-    if (e[7]) p.tickets[e[6]] = 0;
-  }
-  __syncthreads();
-  for (int i = 0; i < np; ++i) {
-    const int* e = pend + 8 * i;
-    if (!e[7]) continue;
-    __threadfence();
-    merge_fp8_unit<D>(p, e[0], e[1] * HP, HP, e[2], e[3], e[4], e[5], threadIdx.x, kThreads);
-  }
+// Joins the parts of split units: grid (chunks of a unit's outputs, blocks of the pass). A
+// warp takes 8 rows x 32 columns, a thread 8 columns of a row, with the loads of four parts
+// in flight. It is launched while the pass still runs and waits for its end. (The last block
+// to finish a unit merging it alone took 12 to 15 us at the end of a call where this takes 4
+// to 6: 128 rows in 5 parts are 330 KB, an L2 round trip of one SM at a time.)
+constexpr int kMergeThreads = 256;
+template <int D, int HP, bool BY_COLUMNS>
+__global__ void __launch_bounds__(kMergeThreads) merge_fp8_kernel(AttnFp8Params p) {
+  pdl_wait_prior();
+  const int4 a = __ldcg(p.splits + 2 * blockIdx.y), b = __ldcg(p.splits + 2 * blockIdx.y + 1);
+  const int warp = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int hr = warp / (D / 32) * 8 + (lane & 7), c8 = warp % (D / 32) * 4 + (lane >> 3);
+  if (hr < HP * a.w && b.y > 0)
+    merge_fp8_item<D, BY_COLUMNS>(p, a.x, a.y * HP + hr / a.w, a.z + hr % a.w, b.x, b.y, hr, c8);
+}
+
+template <int D, int HP, bool BY_COLUMNS>
+cudaError_t launch_merge(const AttnFp8Params& p, const AttnFp8Plan& P, cudaStream_t stream) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  const int warps = (P.slot_rows + 7) / 8 * (D / 32);
+  cfg.gridDim = dim3((warps + kMergeThreads / 32 - 1) / (kMergeThreads / 32), P.grid);
+  cfg.blockDim = dim3(kMergeThreads);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, merge_fp8_kernel<D, HP, BY_COLUMNS>, p);
 }
 
 // ---------------------------------------------------------------------------------
