@@ -55,10 +55,10 @@ struct TcForm {
 TcForm tc_form(const spec_attn_fp8_args_t& a) {
   const int rows = (a.num_q_heads / a.num_kv_heads) * a.gamma;
   TcForm f;
-  f.heads = rows <= 64 && a.num_kv_heads % 2 == 0 ? 2 : 1;
+  f.heads = rows <= 128 && a.num_kv_heads % 2 == 0 ? 2 : 1;
   f.row_tiles = f.heads == 2 ? 1 : (rows + 255) / 256;
   f.sub_rows = f.heads == 2 ? rows : (rows > 256 ? 128 : (rows + 1) / 2);
-  f.rows_on_m = f.sub_rows > 64;
+  f.rows_on_m = f.sub_rows > 32;
   const size_t smem = f.rows_on_m ? attn_fp8_rows_smem(a, f.heads) : attn_fp8_keys_smem(a, f.heads, f.sub_rows);
   const int64_t tiles = (static_cast<int64_t>(a.max_pages_per_seq) * a.page_size + kFp8KeyTile - 1) / kFp8KeyTile + 8;
   const int64_t units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / f.heads) * f.row_tiles;

@@ -30,9 +30,10 @@ namespace {
 
 using namespace fp8tc;
 
-constexpr int kSoftWarps = 4 * NH;
+constexpr int kSoftWarps = 8 * NH;
 constexpr int kThreads = 32 * (kSoftWarps + 4);
 constexpr int MR = 128;  // rows of a sub-unit's MMA tile
+constexpr int HK = TK / 2;  // keys of a tile that a thread weighs
 
 template <int D, int HP>
 struct Cfg {
@@ -44,7 +45,8 @@ struct Cfg {
   static constexpr uint32_t OFF_SCL = OFF_Q + NH * 2 * Q_TERM;      // float4 [NST][8 pages][HP]
   static constexpr uint32_t OFF_NAN = OFF_SCL + NST * 8 * HP * 16;  // uint64 [NH][D]: NaN block values
   static constexpr uint32_t OFF_QS = OFF_NAN + NH * D * 8;          // float [2][NH][MR]: rows' Q scales
-  static constexpr uint32_t OFF_BAR = OFF_QS + 2 * NH * MR * 4;
+  static constexpr uint32_t OFF_XCH = OFF_QS + 2 * NH * MR * 4;    // float [NH][2][MR]: between a row's threads
+  static constexpr uint32_t OFF_BAR = OFF_XCH + NH * 2 * MR * 4;
   // full[NST], empty[NST], s_full[NH], p_full[NH], pv_done[NH], seg_ready[NH], drain[2],
   // flag_ready[kFlagRing]
   static constexpr int NBAR = 2 * NST + 4 * NH + 2 + kFlagRing;
@@ -66,6 +68,17 @@ __device__ __forceinline__ void mma_e4m3_ta(uint32_t d_tmem, uint32_t a_tmem, ui
       " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n}" ::"r"(d_tmem),
       "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+
+// Whether any thread of a pair of warps has `any` (named barrier).
+__device__ __forceinline__ bool pair_any(int bar, bool any) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, 64, p;\n selp.u32 %0, 1, 0, q;\n}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(any)), "r"(bar)
+      : "memory");
+  return r != 0;
 }
 
 template <int D, int HP>
@@ -105,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr int b_sfull = 2 * NST, b_pfull = b_sfull + NH, b_pv = b_pfull + NH, b_seg = b_pv + NH;
       constexpr int b_drain = b_seg + NH, b_flag = b_drain + 2;
       const int n = i < NST || i >= b_flag ? 2  // full, flag_ready
-                    : (i >= b_pfull && i < b_pv) || (i >= b_seg && i < b_drain) ? nact : 1;  // p_full, seg_ready
+                    : (i >= b_pfull && i < b_pv) || (i >= b_seg && i < b_drain) ? 2 * nact : 1;  // p_full, seg_ready
       mbar_init(bar0 + 8u * i, n);
     }
     if (lane < NH) nan_flag[lane] = 0;
@@ -214,12 +227,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     // ============================ softmax ============================
-    const int h = warp >> 2, q4 = warp & 3, kvh = HP == 2 ? h : 0;
+    const int h = warp >> 3, ch = warp >> 2 & 1, q4 = warp & 3, kvh = HP == 2 ? h : 0;
     const int q0 = h == 1 && sub_rows <= 64 ? 2 : 0;  // first lane quadrant of the sub-unit
     if (q4 >= q0 && q4 < q0 + nact) {
-      const int sbar = 1 + h, nthr = nact * 32, stid = (q4 - q0) * 32 + lane;  // stid: this thread's row
+      // pbar: the two warps of 32 rows; row: this thread's row of the sub-unit
+      const int sbar = 1 + h, pbar = 1 + NH + h * 4 + q4, nthr = nact * 64, row = (q4 - q0) * 32 + lane;
+      const int stid = ch * nact * 32 + row;
+      float* const xch = reinterpret_cast<float*>(smem + C::OFF_XCH) + h * 2 * MR;
       const uint32_t lane_base = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
-      const uint32_t s_col = lane_base + C::S_COL + h * TK, o_col = lane_base + C::O_COL + h * D;
+      const uint32_t s_col = lane_base + C::S_COL + h * TK, o_col = lane_base + C::O_COL + h * D + ch * (D / 2);
       const int psh = __ffs(p.page_size) - 1;
       uint32_t it = 0, seg_no = 0;
       // After a timeout the warp runs its loops to the end without waiting (nothing else
@@ -238,60 +254,57 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto start_segment = [&](const Seg& sg, uint32_t par) {
         constexpr int kPieces = D / 16;  // 16 elements per piece: 32 B in, 16 B per term
         const int nreal = real_rows(sg);
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          uint4 x[kPieces / 2][2];
+        uint4 x[kPieces / 2][2];
 #pragma unroll
-          for (int i = 0; i < kPieces / 2; ++i) {
-            const int item = (half * (kPieces / 2) + i) * nthr + stid, r = item / kPieces, piece = item % kPieces;
-            x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
-            if (r < nreal) {
-              const int ur = unit_row(sg, r), j = ur / p.group;
-              const int head = (sg.g * HP + kvh) * p.group + ur - j * p.group;
-              const uint4* src = reinterpret_cast<const uint4*>(
-                  static_cast<const __nv_bfloat16*>(p.q) +
-                  ((static_cast<int64_t>(sg.b) * p.gamma + j) * p.hq + head) * D + piece * 16);
-              x[i][0] = __ldg(src);
-              x[i][1] = __ldg(src + 1);
-            }
+        for (int i = 0; i < kPieces / 2; ++i) {
+          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+          x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+          if (r < nreal) {
+            const int ur = unit_row(sg, r), j = ur / p.group;
+            const int head = (sg.g * HP + kvh) * p.group + ur - j * p.group;
+            const uint4* src = reinterpret_cast<const uint4*>(
+                static_cast<const __nv_bfloat16*>(p.q) +
+                ((static_cast<int64_t>(sg.b) * p.gamma + j) * p.hq + head) * D + piece * 16);
+            x[i][0] = __ldg(src);
+            x[i][1] = __ldg(src + 1);
           }
+        }
 #pragma unroll
-          for (int i = 0; i < kPieces / 2; ++i) {
-            const int item = (half * (kPieces / 2) + i) * nthr + stid, r = item / kPieces, piece = item % kPieces;
-            uint32_t mx = 0;
+        for (int i = 0; i < kPieces / 2; ++i) {
+          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+          uint32_t mx = 0;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t v[4] = {x[i][e].x, x[i][e].y, x[i][e].z, x[i][e].w};
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const uint32_t a = v[c] & 0x7fffu, b = (v[c] >> 16) & 0x7fffu;
-                mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
-              }
-            }
-#pragma unroll
-            for (int o = 1; o < kPieces; o <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const int ex = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
-            const float inv = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-            if (piece == 0) qscale[par * NH * MR + r] = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
-            uint32_t t1w[4], t2w[4];
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t v[4] = {x[i][e].x, x[i][e].y, x[i][e].z, x[i][e].w};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const uint4 u = x[i][c >> 1];
-              const uint32_t v2[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
-              float v[4];
-#pragma unroll
-              for (int d = 0; d < 4; ++d) {
-                v[d] = __uint_as_float((d & 1) ? v2[d >> 1] & 0xffff0000u : v2[d >> 1] << 16) * inv;
-                if (!(fabsf(v[d]) < INFINITY)) v[d] = __int_as_float(0x7fc00000);  // an infinite query is NaN
-              }
-              split_e4m3x4<false>(v[0], v[1], v[2], v[3], t1w[c], t2w[c]);
+              const uint32_t a = v[c] & 0x7fffu, b = (v[c] >> 16) & 0x7fffu;
+              mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
             }
-            const int lr = q0 * 32 + r;  // row of the MMA tile
-            const int ph = D == 128 ? piece ^ (lr & 7) : piece ^ ((lr >> 1) & 3);
-            unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + lr * D + ph * 16;
-            *reinterpret_cast<uint4*>(dst) = make_uint4(t1w[0], t1w[1], t1w[2], t1w[3]);
-            *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
           }
+#pragma unroll
+          for (int o = 1; o < kPieces; o <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const int ex = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
+          const float inv = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+          if (piece == 0) qscale[par * NH * MR + r] = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
+          uint32_t t1w[4], t2w[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint4 u = x[i][c >> 1];
+            const uint32_t v2[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
+            float v[4];
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              v[d] = __uint_as_float((d & 1) ? v2[d >> 1] & 0xffff0000u : v2[d >> 1] << 16) * inv;
+              if (!(fabsf(v[d]) < INFINITY)) v[d] = __int_as_float(0x7fc00000);  // an infinite query is NaN
+            }
+            split_e4m3x4<false>(v[0], v[1], v[2], v[3], t1w[c], t2w[c]);
+          }
+          const int lr = q0 * 32 + r;  // row of the MMA tile
+          const int ph = D == 128 ? piece ^ (lr & 7) : piece ^ ((lr >> 1) & 3);
+          unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + lr * D + ph * 16;
+          *reinterpret_cast<uint4*>(dst) = make_uint4(t1w[0], t1w[1], t1w[2], t1w[3]);
+          *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
         }
         fence_async_smem();
         bar_sync(sbar, nthr);  // the rows' scales are set
@@ -303,14 +316,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (s.ntile > 0) {
         const uint32_t par = seg_no & 1;
         const int ctx = s.kv_len - p.gamma;
-        const int ur = unit_row(s, stid);
-        const bool real = stid < real_rows(s);
+        const int ur = unit_row(s, row);
+        const bool real = row < real_rows(s);
         const int j = min(ur, p.rows - 1) / p.group;
         // the block keys this row sees, a bit each
         const unsigned long long all = p.gamma >= 64 ? ~0ull : (1ull << p.gamma) - 1;
         const unsigned long long vis =
             all & (p.tree_mask ? __ldg(p.tree_mask + static_cast<int64_t>(s.b) * p.gamma + j) : (2ull << j) - 1);
-        const float qf = qscale[par * NH * MR + stid];
+        const float qf = qscale[par * NH * MR + row];
         float m = -INFINITY, l = 0.f;  // reference (-inf: no key seen yet) and sum
 
         for (int k = 0; k < s.ntile; ++k) {
@@ -324,45 +337,56 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (r < 0) return static_cast<uint32_t>(vis << -r) | ((1u << -r) - 1u);
             return r < 64 ? static_cast<uint32_t>(vis >> r) : 0u;
           };
-          auto hide = [&](uint32_t* r, uint32_t seen) {
-#pragma unroll
-            for (int c = 0; c < 32; ++c) r[c] = (seen >> c & 1) ? r[c] : 0xff800000u;
-            asm volatile("");  // keeps the branch around this
-          };
           const float4* const sc = scl + st * 8 * HP + kvh;  // page g of the tile: sc[g * HP]
           wait(s_full(h), x & 1);
           tc_fence_after();
           wait(full(st), (x / NST) & 1);  // orders the producer's scales before this
-          // ---- the row's largest weighted exponent ----
-          float top = -INFINITY;
-          {
-            uint32_t raw[2][32];
-            tmem_ld32(s_col, raw[0]);
-#pragma unroll
-            for (int c0 = 0; c0 < TK; c0 += 32) {
-              uint32_t* const r = raw[(c0 >> 5) & 1];
+          if (masked) {  // hidden keys' scores become -inf in place
+#pragma unroll 1
+            for (int c0 = ch * HK; c0 < ch * HK + HK; c0 += 32) {
+              const uint32_t seen = seen_of(c0);
+              uint32_t r[32];
+              tmem_ld32(s_col + c0, r);
               tmem_wait_ld();
-              if (c0 + 32 < TK) tmem_ld32(s_col + c0 + 32, raw[((c0 >> 5) & 1) ^ 1]);
-              if (masked) hide(r, seen_of(c0));
 #pragma unroll
-              for (int g = 0; g < 32; g += 16) {
-                const float4 q = sc[((c0 + g) >> psh) * HP];
-                float t = __uint_as_float(r[g]);
+              for (int c = 0; c < 32; ++c) r[c] = (seen >> c & 1) ? r[c] : 0xff800000u;
+              tmem_st32(s_col + c0, r);
+            }
+            tmem_wait_st();
+          }
+          // e = a * S + b of a page's keys; a is not 0, so that a * -inf stays -inf
+          auto slope = [&](float ks) {
+            const float a = ks * qf;
+            return a == 0.f ? 1.17549435e-38f : a;
+          };
+          // ---- the largest weighted exponent of this thread's half of the row ----
+          float top = -INFINITY;
 #pragma unroll
-                for (int c = 1; c < 16; ++c) t = fmaxf(t, __uint_as_float(r[g + c]));
-                if (t != -INFINITY) top = fmaxf(top, fmaf(t, q.x * qf, q.y));
-              }
+          for (int c0 = ch * HK; c0 < ch * HK + HK; c0 += 32) {
+            uint32_t r[32];
+            tmem_ld32(s_col + c0, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int g = 0; g < 32; g += 16) {
+              const float4 q = sc[((c0 + g) >> psh) * HP];
+              float t = __uint_as_float(r[g]);
+#pragma unroll
+              for (int c = 1; c < 16; ++c) t = fmaxf(t, __uint_as_float(r[g + c]));
+              top = fmaxf(top, fmaf(t, slope(q.x), q.y));
             }
           }
           // ---- raise the reference where a weight would pass 2^8 ----
-          if (__any_sync(0xffffffffu, top > m + 8.f || (m == -INFINITY && top > -INFINITY))) {
-            const float now = top > m + 8.f || m == -INFINITY ? fmaxf(m, top - 5.f) : m;
+          if (pair_any(pbar, top > m + 8.f || (m == -INFINITY && top > -INFINITY))) {
+            xch[ch * MR + row] = top;
+            bar_sync(pbar, 64);
+            top = fmaxf(xch[row], xch[MR + row]);
+            const float now = top > m + 8.f || m == -INFINITY ? fmaxf(m, rintf(top) - 5.f) : m;
             const float alpha = m == -INFINITY ? 0.f : ex2(m - now);
             if (k > 0) {  // O holds every earlier tile before it is scaled
               wait(pv_done(h), (x - 1) & 1);
               tc_fence_after();
 #pragma unroll 1
-              for (int c0 = 0; c0 < D; c0 += 32) {
+              for (int c0 = 0; c0 < D / 2; c0 += 32) {
                 uint32_t raw[32];
                 tmem_ld32(o_col + c0, raw);
                 tmem_wait_ld();
@@ -374,66 +398,45 @@ __global__ void __launch_bounds__(kThreads, 1)
               l *= alpha;
             }
             m = now;
+            bar_sync(pbar, 64);  // xch is read
           }
           // ---- weights, their sum, and their two terms over the columns of S ----
           const float msub = m == -INFINITY ? 0.f : m;
-          // scores so large that log2(sv) - m alone rounds by more than a weight may bear
-          const bool special = masked || __any_sync(0xffffffffu, fabsf(msub) > 1048576.f);
-          {
-            uint32_t raw[2][32];
-            tmem_ld32(s_col, raw[0]);
 #pragma unroll 1
-            for (int c1 = 0; c1 < TK; c1 += 64) {
+          for (int c0 = ch * HK; c0 < ch * HK + HK; c0 += 32) {
+            uint32_t r[32], w1[8], w2[8];
+            tmem_ld32(s_col + c0, r);
+            float2 ab[2];  // of 16 keys each
+            float inv_sv[2];
 #pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                const int c0 = c1 + 32 * u;
-                uint32_t* const r = raw[u];
-                uint32_t w1[8], w2[8];
-                tmem_wait_ld();
-                if (u == 0 || c1 + 64 < TK) tmem_ld32(s_col + c0 + 32, raw[u ^ 1]);
-                float2 ab[2];  // per 16 keys: e = a * S + b
-                float inv_sv[2];
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                  const float4 q = sc[((c0 + 16 * g) >> psh) * HP];
-                  ab[g] = make_float2(q.x * qf, q.y - msub);
-                  inv_sv[g] = q.z;
-                }
-                if (special) {  // hidden keys, or scores too large for the short form
-                  const uint32_t seen = masked ? seen_of(c0) : ~0u;
-#pragma unroll
-                  for (int g = 0; g < 2; ++g) {
-                    const float lv = sc[((c0 + 16 * g) >> psh) * HP].y;
-#pragma unroll
-                    for (int c = 16 * g; c < 16 * g + 16; ++c)
-                      r[c] = __float_as_uint(fmaf(__uint_as_float(r[c]), ab[g].x, lv) - msub);
-                    ab[g] = make_float2(1.f, 0.f);
-                  }
-                  hide(r, seen);
-                }
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                  float sum = 0.f;
-#pragma unroll
-                  for (int c = 16 * g; c < 16 * g + 16; c += 4) {
-                    float pr[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pr[i] = ex2(fmaf(__uint_as_float(r[c + i]), ab[g].x, ab[g].y));
-                    sum += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-                    split_e4m3x4<false>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
-                  }
-                  l = fmaf(sum, inv_sv[g], l);
-                }
-                tmem_st8(s_col + c0, w1);
-                tmem_st8(s_col + c0 + 8, w2);
-              }
+            for (int g = 0; g < 2; ++g) {
+              const float4 q = sc[((c0 + 16 * g) >> psh) * HP];
+              ab[g] = make_float2(slope(q.x), q.y - msub);
+              inv_sv[g] = q.z;
             }
+            tmem_wait_ld();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              float sum = 0.f;
+#pragma unroll
+              for (int c = 16 * g; c < 16 * g + 16; c += 4) {
+                float pr[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pr[i] = ex2(fmaf(__uint_as_float(r[c + i]), ab[g].x, ab[g].y));
+                sum += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+                split_e4m3x4<false>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
+              }
+              l = fmaf(sum, inv_sv[g], l);
+            }
+            tmem_st8(s_col + c0, w1);
+            tmem_st8(s_col + c0 + 8, w2);
           }
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(p_full(h));
         }
+        xch[ch * MR + row] = l;
         // The next segment's Q takes the place of this one's: every S of this segment has
         // been read. Its first scores wait for this segment's last products only.
         const Seg c = s;
@@ -450,12 +453,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool bad = (seg_flag[seg_no % kFlagRing] | seg_flag[kFlagRing + seg_no % kFlagRing]) != 0;
         const bool whole = c.tile0 == 0 && c.ntile == c.unit_tiles;
         if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
-        const float L = bad ? -1.f : l;
+        bar_sync(pbar, 64);
+        const float L = bad ? -1.f : xch[row] + xch[MR + row];
         const float inv = whole ? fp8_inv(L) : (L <= 0.f ? 0.f : 1.f);
         const int head = (c.g * HP + kvh) * p.group + ur - j * p.group;
         const int64_t out_at = (static_cast<int64_t>(c.b) * p.gamma + j) * p.hq + head;
-        const int64_t part_at = (c.u + w.cta) * p.slot_rows + h * sub_rows + stid;
-        if (real) {
+        const int64_t part_at = (c.u + w.cta) * p.slot_rows + h * sub_rows + row;
+        if (real && ch == 0) {
           if (!whole) p.partial_ml[part_at] = make_float2(m, L);
           else if (p.lse) p.lse[out_at] = fp8_lse(m, L);
         }
@@ -463,9 +467,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         const bool has_nan = nan_flag[h] != 0;  // noted before the products just waited for
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
+        for (int c0 = 0; c0 < D / 2; c0 += 32) {
           uint32_t raw[32];
           float o[32];
+          const int d0 = ch * (D / 2) + c0;
           tmem_ld32(o_col + c0, raw);
           tmem_wait_ld();
 #pragma unroll
@@ -473,11 +478,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (has_nan && inv != 0.f) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (nanv[h * D + c0 + i] & vis) o[i] = __int_as_float(0x7fc00000);
+              if (nanv[h * D + d0 + i] & vis) o[i] = __int_as_float(0x7fc00000);
           }
           if (!real) continue;
           if (whole) {
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + out_at * D + c0);
+            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + out_at * D + d0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t v[4];
@@ -490,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           } else {
             float4* dst = reinterpret_cast<float4*>(p.partial_o) + (c.u + w.cta) * p.slot_rows * (D / 4) +
-                          static_cast<int64_t>(c0 / 4) * p.slot_rows + h * sub_rows + stid;
+                          static_cast<int64_t>(d0 / 4) * p.slot_rows + h * sub_rows + row;
 #pragma unroll
             for (int i = 0; i < 8; ++i) dst[i * p.slot_rows] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
           }

@@ -74,14 +74,19 @@ __device__ __forceinline__ void bar_sync(int id, int threads) {
 // terms times 16.
 template <bool UP>
 __device__ __forceinline__ void split_e4m3x4(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
-  asm("{\n .reg .b16 p, q, r, s;\n .reg .b32 x, y, h, g;\n"
-      " cvt.rn.satfinite.e4m3x2.f32 p, %3, %2;\n cvt.rn.satfinite.e4m3x2.f32 q, %5, %4;\n mov.b32 %0, {p, q};\n"
-      " cvt.rn.f16x2.f32 x, %3, %2;\n cvt.rn.f16x2.f32 y, %5, %4;\n"
+  uint32_t x, y;
+  asm("{\n .reg .b16 p, q;\n .reg .b32 h, g;\n"
+      " cvt.rn.satfinite.e4m3x2.f32 p, %4, %3;\n cvt.rn.satfinite.e4m3x2.f32 q, %6, %5;\n mov.b32 %0, {p, q};\n"
+      " cvt.rn.f16x2.f32 %1, %4, %3;\n cvt.rn.f16x2.f32 %2, %6, %5;\n"
       " cvt.rn.f16x2.e4m3x2 h, p;\n cvt.rn.f16x2.e4m3x2 g, q;\n"
-      " sub.f16x2 x, x, h;\n sub.f16x2 y, y, g;\n mul.f16x2 x, x, %6;\n mul.f16x2 y, y, %6;\n"
-      " cvt.rn.satfinite.e4m3x2.f16x2 r, x;\n cvt.rn.satfinite.e4m3x2.f16x2 s, y;\n mov.b32 %1, {r, s};\n}"
-      : "=r"(hi), "=r"(lo)
-      : "f"(a), "f"(b), "f"(c), "f"(d), "r"(UP ? 0x4c004c00u : 0x3c003c00u));
+      " sub.f16x2 %1, %1, h;\n sub.f16x2 %2, %2, g;\n}"
+      : "=&r"(hi), "=&r"(x), "=&r"(y)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  if constexpr (UP) asm("mul.f16x2 %0, %0, %2;\n mul.f16x2 %1, %1, %2;" : "+r"(x), "+r"(y) : "r"(0x4c004c00u));
+  asm("{\n .reg .b16 r, s;\n cvt.rn.satfinite.e4m3x2.f16x2 r, %1;\n cvt.rn.satfinite.e4m3x2.f16x2 s, %2;\n"
+      " mov.b32 %0, {r, s};\n}"
+      : "=r"(lo)
+      : "r"(x), "r"(y));
 }
 
 // The slow part of a wait: polls until the phase completes, or gives up (mbar_wait).
