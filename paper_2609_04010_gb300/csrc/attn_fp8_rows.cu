@@ -31,7 +31,7 @@ namespace {
 using namespace fp8tc;
 
 constexpr int kSoftWarps = 8 * NH;
-constexpr int kThreads = 32 * (kSoftWarps + 4);
+constexpr int kThreads = 32 * (kSoftWarps + 3);
 constexpr int MR = 128;  // rows of a sub-unit's MMA tile
 constexpr int HK = TK / 2;  // keys of a tile that a thread weighs
 
@@ -47,9 +47,9 @@ struct Cfg {
   static constexpr uint32_t OFF_QS = OFF_NAN + NH * D * 8;          // float [2][NH][MR]: rows' Q scales
   static constexpr uint32_t OFF_XCH = OFF_QS + 2 * NH * MR * 4;    // float [NH][2][MR]: between a row's threads
   static constexpr uint32_t OFF_BAR = OFF_XCH + NH * 2 * MR * 4;
-  // full[NST], empty[NST], s_full[NH], p_full[NH], pv_done[NH], seg_ready[NH], drain[2],
+  // full[NST], empty[NST], s_full[NH], p_full[NH], pv_done[NH], seg_ready[NH], drain,
   // flag_ready[kFlagRing]
-  static constexpr int NBAR = 2 * NST + 4 * NH + 2 + kFlagRing;
+  static constexpr int NBAR = 2 * NST + 4 * NH + 1 + kFlagRing;
   static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;        // tmem base, abort, -, -, NaN flags
   static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;             // int [2][kFlagRing]: segments' bad flags
   static constexpr uint32_t OFF_PB = OFF_FLAG + 8 * kFlagRing;               // int [batch + 1]
@@ -96,8 +96,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto p_full = [&](int h) { return bar0 + 8u * (2 * NST + NH + h); };
   auto pv_done = [&](int h) { return bar0 + 8u * (2 * NST + 2 * NH + h); };
   auto seg_ready = [&](int h) { return bar0 + 8u * (2 * NST + 3 * NH + h); };
-  auto drain_bar = [&](int i) { return bar0 + 8u * (2 * NST + 4 * NH + i); };
-  auto flag_bar = [&](int i) { return bar0 + 8u * (2 * NST + 4 * NH + 2 + i); };
+  const uint32_t drain_bar = bar0 + 8u * (2 * NST + 4 * NH);
+  auto flag_bar = [&](int i) { return bar0 + 8u * (2 * NST + 4 * NH + 1 + i); };
   float4* scl = reinterpret_cast<float4*>(smem + C::OFF_SCL);
   unsigned long long* nanv = reinterpret_cast<unsigned long long*>(smem + C::OFF_NAN);
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     for (int i = lane; i < C::NBAR; i += 32) {
       constexpr int b_sfull = 2 * NST, b_pfull = b_sfull + NH, b_pv = b_pfull + NH, b_seg = b_pv + NH;
-      constexpr int b_drain = b_seg + NH, b_flag = b_drain + 2;
+      constexpr int b_drain = b_seg + NH, b_flag = b_drain + 1;
       const int n = i < NST || i >= b_flag ? 2  // full, flag_ready
                     : (i >= b_pfull && i < b_pv) || (i >= b_seg && i < b_drain) ? 2 * nact : 1;  // p_full, seg_ready
       mbar_init(bar0 + 8u * i, n);
@@ -134,62 +134,45 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = misc[0];
   const WorkList w = work_list(p, pb);
   pdl_launch_dependents();
-  if (threadIdx.x == 32 * (kSoftWarps + 2)) note_split_unit(p, w, tile_rows);
+  if (threadIdx.x == 32 * (kSoftWarps + 1)) note_split_unit(p, w, tile_rows);
 
-  if (warp == kSoftWarps || warp == kSoftWarps + 3) {
+  if (warp == kSoftWarps || warp == kSoftWarps + 2) {
     // ============================ producers ============================
     produce<D, HP, NST>(p, tmap, w, warp == kSoftWarps ? 0 : 1, sbase + C::OFF_STAGE, full(0), empty(0), flag_bar(0), scl,
                         seg_flag, abort_flag);
   } else if (warp == kSoftWarps + 1) {
-    // ============================ S = Q K^T ============================
-    constexpr uint32_t kIdesc = idesc_e4m3(MR, TK, false, false);
+    // ============================ products ============================
+    // One thread's products run in the order of their issue: the next tile's S follows at once
+    // on the O += P V that reads its columns.
+    constexpr uint32_t kIdescS = idesc_e4m3(MR, TK, false, false), kIdescO = idesc_e4m3(MR, D, false, true);
     uint32_t it = 0, seg_no = 0;
     bool ok = true, issued = false;
-    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok; ++seg_no) {
-      for (int k = 0; k < s.ntile && ok; ++k, ++it) {
-        const uint32_t st = it % NST;
-        ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
-        for (int h = 0; h < NH && ok; ++h) {
-          if (k == 0) ok = mbar_wait(seg_ready(h), seg_no & 1, abort_flag, p.status);
-          // the products of the tile before have read its P, which lies over S
-          if (ok && it > 0) ok = mbar_wait(pv_done(h), (it - 1) & 1, abort_flag, p.status);
-          if (!ok) break;
-          tc_fence_after();
-          if (lane == 0) {
-            const uint32_t kb = sbase + C::OFF_STAGE + st * C::STAGE + (HP == 2 ? h : 0) * 2 * C::ATOM;
+    auto stage_full = [&](uint32_t x) { return mbar_wait(full(x % NST), (x / NST) & 1, abort_flag, p.status); };
+    auto scores = [&](int h, uint32_t st) {
+      if (lane == 0) {
+        const uint32_t kb = sbase + C::OFF_STAGE + st * C::STAGE + (HP == 2 ? h : 0) * 2 * C::ATOM;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-              for (int kk = 0; kk < D / 32; ++kk)
-                mma_e4m3(tmem + C::S_COL + h * TK,
-                         desc_rows<D>(sbase + C::OFF_Q + (h * 2 + t) * C::Q_TERM + kk * 32u, 16, C::ATOM),
-                         desc_rows<D>(kb + kk * 32u, 16, C::SG), kIdesc, t > 0 || kk > 0);
-            mma_commit(s_full(h));
-            issued = true;
-          }
-          __syncwarp();
-        }
+          for (int kk = 0; kk < D / 32; ++kk)
+            mma_e4m3(tmem + C::S_COL + h * TK,
+                     desc_rows<D>(sbase + C::OFF_Q + (h * 2 + t) * C::Q_TERM + kk * 32u, 16, C::ATOM),
+                     desc_rows<D>(kb + kk * 32u, 16, C::SG), kIdescS, t > 0 || kk > 0);
+        mma_commit(s_full(h));
+        issued = true;
       }
-      if (!has_more(s, w.t1, w.ovh)) break;
-      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
-    }
-    if (!ok && __any_sync(0xffffffffu, issued)) {
-      if (lane == 0) mma_commit(drain_bar(0));
       __syncwarp();
-      const long long c0 = clock64();
-      while (!mbar_try(drain_bar(0), 0) && clock64() - c0 < kWaitCycles) {
+    };
+    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok; ++seg_no) {
+      ok = stage_full(it);
+      for (int h = 0; h < NH && ok; ++h) {
+        ok = mbar_wait(seg_ready(h), seg_no & 1, abort_flag, p.status);
+        if (!ok) break;
+        tc_fence_after();
+        scores(h, it % NST);
       }
-    }
-  } else if (warp == kSoftWarps + 2) {
-    // ============================ O += P V ============================
-    constexpr uint32_t kIdesc = idesc_e4m3(MR, D, false, true);
-    uint32_t it = 0;
-    bool ok = true, issued = false;
-    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok;) {
       for (int k = 0; k < s.ntile && ok; ++k, ++it) {
         const uint32_t st = it % NST;
-        ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
-        if (!ok) break;
         // a unit's first tile waits for its weights first: they follow the outputs of the unit
         // before, whose NaN notes are then read
         if (k == 0)
@@ -207,22 +190,26 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int t = 0; t < 2; ++t)
                 mma_e4m3_ta(tmem + C::O_COL + h * D, tmem + C::S_COL + h * TK + kk * 32u + t * 8u,
-                            desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG), kIdesc, k > 0 || kk > 0 || t > 0);
+                            desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG), kIdescO, k > 0 || kk > 0 || t > 0);
             mma_commit(pv_done(h));
             if (h == NH - 1) mma_commit(empty(st));
             issued = true;
           }
           __syncwarp();
+          if (k + 1 < s.ntile) {
+            if (h == 0) ok = stage_full(it + 1);
+            if (ok) scores(h, (it + 1) % NST);
+          }
         }
       }
       if (!has_more(s, w.t1, w.ovh)) break;
       s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
     }
     if (!ok && __any_sync(0xffffffffu, issued)) {
-      if (lane == 0) mma_commit(drain_bar(1));
+      if (lane == 0) mma_commit(drain_bar);
       __syncwarp();
       const long long c0 = clock64();
-      while (!mbar_try(drain_bar(1), 0) && clock64() - c0 < kWaitCycles) {
+      while (!mbar_try(drain_bar, 0) && clock64() - c0 < kWaitCycles) {
       }
     }
   } else {
