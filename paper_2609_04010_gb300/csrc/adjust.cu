@@ -81,12 +81,6 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
   const int v0 = blockIdx.y * kSlice, nv = min(kSlice, a.vocab - v0);
   const int G = a.gamma;
   const int row0 = blockIdx.z * rows, row1 = min(G, row0 + rows);  // this block's rows
-  Seq q;
-  q.rep = a.repetition ? a.repetition[b] : 1.f;
-  q.freq = a.frequency ? a.frequency[b] : 0.f;
-  q.pres = a.presence ? a.presence[b] : 0.f;
-  q.bias = a.bias_values + static_cast<int64_t>(b) * a.max_bias;
-  const bool penal = q.rep != 1.f || q.freq != 0.f || q.pres != 0.f;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     reinterpret_cast<uint4*>(count)[tid + i * kThreads] = make_uint4(0, 0, 0, 0);
@@ -94,6 +88,14 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
   if (a.bias_tokens)
     for (int i = tid; i < kSlice; i += kThreads) place[i] = 0xffffffffu;
   if (tid == 0) nlist = 0;
+  pdl_launch_dependents();
+  pdl_wait_prior();
+  Seq q;
+  q.rep = a.repetition ? a.repetition[b] : 1.f;
+  q.freq = a.frequency ? a.frequency[b] : 0.f;
+  q.pres = a.presence ? a.presence[b] : 0.f;
+  q.bias = a.bias_values + static_cast<int64_t>(b) * a.max_bias;
+  const bool penal = q.rep != 1.f || q.freq != 0.f || q.pres != 0.f;
   if (tid < 64) btok[tid] = a.block_tokens && tid < G ? a.block_tokens[static_cast<int64_t>(b) * G + tid] : -1;
   __syncthreads();
   const auto index = [&](int token) { return static_cast<uint32_t>(token) - static_cast<uint32_t>(v0); };
@@ -240,15 +242,14 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
 }
 
 template <typename T>
-void launch_typed(const spec_adjust_args_t& a, bool vec, int sms, cudaStream_t stream) {
+cudaError_t launch_typed(const spec_adjust_args_t& a, bool vec, int sms, cudaStream_t stream) {
   // rows are shared out among blocks (each counts the history again) until there are about two
   // rounds of them
   const int64_t blocks = static_cast<int64_t>(a.batch) * ((a.vocab - 1) / kSlice + 1);
   const int64_t splits = std::min<int64_t>(a.gamma, std::max<int64_t>(1, 12 * sms / blocks));
   const int rows = static_cast<int>((a.gamma + splits - 1) / splits);
   const dim3 grid(a.batch, (a.vocab - 1) / kSlice + 1, (a.gamma - 1) / rows + 1);
-  if (vec) adjust_kernel<T, true><<<grid, kThreads, 0, stream>>>(a, rows);
-  else adjust_kernel<T, false><<<grid, kThreads, 0, stream>>>(a, rows);
+  return launch_overlapped(vec ? adjust_kernel<T, true> : adjust_kernel<T, false>, grid, kThreads, 0, stream, a, rows);
 }
 
 }  // namespace
@@ -259,9 +260,7 @@ cudaError_t launch_adjust(const spec_adjust_args_t& a, int sms, cudaStream_t str
   const bool vec = a.vocab % 8 == 0 &&
                    ((reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.out)) & 15u) == 0;
   (void)cudaGetLastError();
-  if (esz == 2) launch_typed<__nv_bfloat16>(a, vec, sms, stream);
-  else launch_typed<float>(a, vec, sms, stream);
-  return cudaGetLastError();
+  return esz == 2 ? launch_typed<__nv_bfloat16>(a, vec, sms, stream) : launch_typed<float>(a, vec, sms, stream);
 }
 
 }  // namespace specv

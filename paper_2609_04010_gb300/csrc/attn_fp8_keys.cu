@@ -181,6 +181,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   for (int i = threadIdx.x; i < NH * D; i += kThreads) nanv[i] = 0ull;
   if (warp == kSoftWarps + 1) tmem_alloc(smem_u32(misc), C::TMEM_COLS);
+  if (threadIdx.x == 32 * kSoftWarps)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap)) : "memory");
+  pdl_wait_prior();
   if (warp == kSoftWarps) prefix_tiles(p, pb);
   tc_fence_before();
   __syncthreads();
@@ -614,8 +617,7 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   const cudaError_t e =
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  kernel<<<P.grid, kThreads, smem, stream>>>(map, p);
-  const cudaError_t k = cudaGetLastError();
+  const cudaError_t k = launch_overlapped(kernel, dim3(P.grid), kThreads, smem, stream, map, p);
   return k == cudaSuccess ? launch_merge<D, HP, false>(p, P, stream) : k;
 }
 

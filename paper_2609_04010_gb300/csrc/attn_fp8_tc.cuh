@@ -171,17 +171,9 @@ __global__ void __launch_bounds__(kMergeThreads) merge_fp8_kernel(AttnFp8Params 
 
 template <int D, int HP, bool BY_COLUMNS>
 cudaError_t launch_merge(const AttnFp8Params& p, const AttnFp8Plan& P, cudaStream_t stream) {
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
   const int warps = (P.slot_rows + 7) / 8 * (D / 32);
-  cfg.gridDim = dim3((warps + kMergeThreads / 32 - 1) / (kMergeThreads / 32), P.grid);
-  cfg.blockDim = dim3(kMergeThreads);
-  cfg.stream = stream;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, merge_fp8_kernel<D, HP, BY_COLUMNS>, p);
+  const dim3 grid((warps + kMergeThreads / 32 - 1) / (kMergeThreads / 32), P.grid);
+  return launch_overlapped(merge_fp8_kernel<D, HP, BY_COLUMNS>, grid, kMergeThreads, 0, stream, p);
 }
 
 // ---------------------------------------------------------------------------------

@@ -76,6 +76,8 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
   const int P = a.page_size, MP = a.max_pages_per_seq;
   const int psh = (P & (P - 1)) == 0 ? __ffs(P) - 1 : -1;  // log2 of a power of two
   const int64_t cap = static_cast<int64_t>(MP) * P;
+  pdl_launch_dependents();
+  pdl_wait_prior();
   const int count0 = min(max(*a.free_count, 0), a.free_capacity);
   if (tid == 0) s_taken = 0;
   Two carry = {0, 0};
@@ -241,6 +243,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams
   const int nheads = min(p.heads, p.hkv - head0);
   const int64_t max_slot = static_cast<int64_t>(p.num_pages) * P;
   if (tid == 0) nlead = 0;
+  pdl_launch_dependents();
+  pdl_wait_prior();
   for (int i = tid; i < kAppendRows + 2 * kWin; i += kAppendThreads) {
     const int64_t r = static_cast<int64_t>(r0) - kWin + i;
     int s = r >= 0 && r < p.rows ? p.slots[r] : -1;
@@ -342,10 +346,10 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams
 template <int D>
 cudaError_t launch_append_d(const AppendParams& p, int page_size, cudaStream_t stream) {
   const dim3 grid((p.rows - 1) / kAppendRows + 1, (p.hkv - 1) / p.heads + 1);
-  if (page_size == 16) append_fp8_kernel<D, 16><<<grid, kAppendThreads, 0, stream>>>(p);
-  else if (page_size == 32) append_fp8_kernel<D, 32><<<grid, kAppendThreads, 0, stream>>>(p);
-  else append_fp8_kernel<D, 64><<<grid, kAppendThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  auto kernel = page_size == 16   ? append_fp8_kernel<D, 16>
+                : page_size == 32 ? append_fp8_kernel<D, 32>
+                                  : append_fp8_kernel<D, 64>;
+  return launch_overlapped(kernel, grid, kAppendThreads, 0, stream, p);
 }
 
 }  // namespace
@@ -362,8 +366,7 @@ cudaError_t launch_map_slots(const spec_slot_args_t& a, char* ws, cudaStream_t s
     if (e != cudaSuccess) return e;
   }
   const int grid = (a.max_rows - 1) / kSlotRowsPerBlock + 1;
-  map_slots_kernel<<<grid, kSlotThreads, smem, stream>>>(p);
-  return cudaGetLastError();
+  return launch_overlapped(map_slots_kernel, dim3(grid), kSlotThreads, smem, stream, p);
 }
 
 cudaError_t launch_append_fp8(const spec_append_fp8_args_t& a, int sms, cudaStream_t stream) {
