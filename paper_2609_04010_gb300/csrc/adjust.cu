@@ -88,7 +88,6 @@ __global__ void __launch_bounds__(kThreads, 6) adjust_kernel(spec_adjust_args_t 
   if (a.bias_tokens)
     for (int i = tid; i < kSlice; i += kThreads) place[i] = 0xffffffffu;
   if (tid == 0) nlist = 0;
-  pdl_launch_dependents();
   pdl_wait_prior();
   Seq q;
   q.rep = a.repetition ? a.repetition[b] : 1.f;

@@ -190,7 +190,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = misc[0];
   const WorkList w = work_list(p, pb);
-  pdl_launch_dependents();
   if (threadIdx.x == 32 * (kSoftWarps + 2)) note_split_unit(p, w, tile_rows);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 3) {

@@ -76,7 +76,6 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
   const int P = a.page_size, MP = a.max_pages_per_seq;
   const int psh = (P & (P - 1)) == 0 ? __ffs(P) - 1 : -1;  // log2 of a power of two
   const int64_t cap = static_cast<int64_t>(MP) * P;
-  pdl_launch_dependents();
   pdl_wait_prior();
   const int count0 = min(max(*a.free_count, 0), a.free_capacity);
   if (tid == 0) s_taken = 0;
@@ -243,7 +242,6 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams
   const int nheads = min(p.heads, p.hkv - head0);
   const int64_t max_slot = static_cast<int64_t>(p.num_pages) * P;
   if (tid == 0) nlead = 0;
-  pdl_launch_dependents();
   pdl_wait_prior();
   for (int i = tid; i < kAppendRows + 2 * kWin; i += kAppendThreads) {
     const int64_t r = static_cast<int64_t>(r0) - kWin + i;
