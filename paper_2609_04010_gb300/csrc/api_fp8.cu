@@ -130,6 +130,7 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
     P.row_tiles = f.row_tiles;
     units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / P.heads) * P.row_tiles;
     P.grid = num_sms;
+    P.splits = static_cast<int>(units < P.grid ? units : P.grid);
     P.nsplit = 1;
     P.slot_rows = 2 * P.sub_rows;
     P.slots = units + P.grid;
@@ -145,9 +146,10 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
     P.slots = P.nsplit > 1 ? units * P.nsplit : 0;
   }
   P.tickets = base;
-  P.partial_o = ws_round(P.tickets + (P.path == SPEC_ATTN_TENSOR_CORES ? 2 * sizeof(int4) * P.grid : sizeof(uint32_t) * units));
+  P.partial_o = ws_round(P.tickets + sizeof(uint32_t) * units);
   P.partial_ml = ws_round(P.partial_o + static_cast<size_t>(P.slots) * P.slot_rows * a.head_dim * 4);
-  P.end = ws_round(P.partial_ml + static_cast<size_t>(P.slots) * P.slot_rows * sizeof(float2));
+  P.split_notes = ws_round(P.partial_ml + static_cast<size_t>(P.slots) * P.slot_rows * sizeof(float2));
+  P.end = ws_round(P.split_notes + 2 * sizeof(int4) * P.splits);
   return P;
 }
 

@@ -11,7 +11,9 @@ namespace specv {
 // AttnParams with k_cache = the 8-bit cache (v_cache unused) and its scales.
 struct AttnFp8Params : AttnParams {
   const float* kv_scale;  // [num_pages][Hkv][2]
-  int4* splits;           // [grid][2]: the split unit that each block ends (tensor-core kernels)
+  int4* splits;           // [P.splits][2]: units to merge (tensor-core kernels)
+  int split_by_unit;      // a place for each unit in it, else for each block
+  int num_slots;          // partial results
 };
 
 inline AttnFp8Params make_attn_fp8_params(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws) {
@@ -42,7 +44,9 @@ inline AttnFp8Params make_attn_fp8_params(const spec_attn_fp8_args_t& a, const A
   p.lse = a.lse;
   p.status = reinterpret_cast<uint32_t*>(ws);
   p.tickets = reinterpret_cast<uint32_t*>(ws + P.tickets);
-  p.splits = reinterpret_cast<int4*>(ws + P.tickets);
+  p.splits = reinterpret_cast<int4*>(ws + P.split_notes);
+  p.split_by_unit = P.splits < P.grid;
+  p.num_slots = static_cast<int>(P.slots);
   p.partial_o = reinterpret_cast<float*>(ws + P.partial_o);
   p.partial_ml = reinterpret_cast<float2*>(ws + P.partial_ml);
   p.tree_mask = a.tree_mask;

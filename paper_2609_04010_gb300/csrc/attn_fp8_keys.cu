@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = misc[0];
   const WorkList w = work_list(p, pb);
-  if (threadIdx.x == 32 * (kSoftWarps + 2)) note_split_unit(p, w, tile_rows);
+  if (threadIdx.x == 0) clear_split(p);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 3) {
     // ============================ producers ============================
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr uint32_t kIdesc = idesc_e4m3(128, NR, false, false);
     uint32_t it = 0, seg_no = 0;
     bool ok = true, issued = false;
-    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok; ++seg_no) {
+    for (Seg s = find(w.t0, w, p); s.ntile > 0 && ok; ++seg_no) {
       for (int k = 0; k < s.ntile && ok; ++k, ++it) {
         const uint32_t st = it % NST, sb = it % SB;
         ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!has_more(s, w.t1, w.ovh)) break;
-      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
+      s = find(s.vnext, w, p);
     }
     if (!ok && __any_sync(0xffffffffu, issued)) {
       if (lane == 0) mma_commit(drain_bar(0));
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr uint32_t kIdesc = idesc_e4m3(128, 2 * NR, true, true);
     uint32_t it = 0;
     bool ok = true, issued = false;
-    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok;) {
+    for (Seg s = find(w.t0, w, p); s.ntile > 0 && ok;) {
       for (int k = 0; k < s.ntile && ok; ++k, ++it) {
         const uint32_t st = it % NST;
         ok = mbar_wait(full(st), (it / NST) & 1, abort_flag, p.status);
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!has_more(s, w.t1, w.ovh)) break;
-      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
+      s = find(s.vnext, w, p);
     }
     if (!ok && __any_sync(0xffffffffu, issued)) {
       if (lane == 0) mma_commit(drain_bar(1));
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       return __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
     };
 
-    Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh);
+    Seg s = find(w.t0, w, p);
     float qf = s.ntile > 0 ? start_segment(s, 0) : 1.f;
     while (s.ntile > 0) {
       const uint32_t par = seg_no & 1;
@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       it += c.ntile;
       qf = 1.f;
       if (has_more(c, w.t1, w.ovh)) {
-        s = locate<TK>(c.vnext, w.t1, p, w.pb, w.ovh);
+        s = find(c.vnext, w, p);
         qf = start_segment(s, par ^ 1);
       } else {
         s.ntile = 0;
@@ -582,6 +582,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           else p.partial_o[row_at[r] + d] = o;
         }
       }
+      if (h == 0 && stid == 0) note_split(p, c, w, tile_rows);
       tc_fence_before();
       bar_sync(sbar, nthr);  // xch, the row state and nanv are read; the next segment may set them
       for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;

@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = misc[0];
   const WorkList w = work_list(p, pb);
-  if (threadIdx.x == 32 * (kSoftWarps + 1)) note_split_unit(p, w, tile_rows);
+  if (threadIdx.x == 0) clear_split(p);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 2) {
     // ============================ producers ============================
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncwarp();
     };
-    for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok; ++seg_no) {
+    for (Seg s = find(w.t0, w, p); s.ntile > 0 && ok; ++seg_no) {
       ok = stage_full(it);
       for (int h = 0; h < NH && ok; ++h) {
         ok = mbar_wait(seg_ready(h), seg_no & 1, abort_flag, p.status);
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!has_more(s, w.t1, w.ovh)) break;
-      s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
+      s = find(s.vnext, w, p);
     }
     if (!ok && __any_sync(0xffffffffu, issued)) {
       if (lane == 0) mma_commit(drain_bar);
@@ -238,15 +238,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto real_rows = [&](const Seg& sg) { return min(sub_rows, p.rows - unit_row(sg, 0)); };
       float* const qscale = reinterpret_cast<float*>(smem + C::OFF_QS) + h * MR;  // [2][NH][MR]
 
-      // Brings a segment's Q into shared memory as two e4m3 terms, each row scaled by the
-      // power of two that takes its largest finite magnitude into (224, 448].
+      // Brings the pair's rows of a segment's Q into shared memory as two e4m3 terms, each row
+      // scaled by the power of two that takes its largest finite magnitude into (224, 448].
       auto start_segment = [&](const Seg& sg, uint32_t par) {
         constexpr int kPieces = D / 16;  // 16 elements per piece: 32 B in, 16 B per term
         const int nreal = real_rows(sg);
         uint4 x[kPieces / 2][2];
 #pragma unroll
         for (int i = 0; i < kPieces / 2; ++i) {
-          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+          const int item = i * 64 + ch * 32 + lane, r = (q4 - q0) * 32 + item / kPieces, piece = item % kPieces;
           x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
           if (r < nreal) {
             const int ur = unit_row(sg, r), j = ur / p.group;
@@ -260,15 +260,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
 #pragma unroll
         for (int i = 0; i < kPieces / 2; ++i) {
-          const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+          const int item = i * 64 + ch * 32 + lane, r = (q4 - q0) * 32 + item / kPieces, piece = item % kPieces;
+          uint32_t v[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
           uint32_t mx = 0;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t v[4] = {x[i][e].x, x[i][e].y, x[i][e].z, x[i][e].w};
+          for (int c = 0; c < 8; ++c) mx = __vmaxu2(mx, v[c] & 0x7fff7fffu);
+          mx = max(mx & 0xffffu, mx >> 16);
+          if (__any_sync(0xffffffffu, mx >= 0x7f80u)) {  // an infinite query is NaN; the scale ignores both
+            mx = 0;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t a = v[c] & 0x7fffu, b = (v[c] >> 16) & 0x7fffu;
-              mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+            for (int c = 0; c < 8; ++c) {
+              const uint32_t lo = v[c] & 0x7fffu, hi = v[c] >> 16 & 0x7fffu;
+              mx = max(mx, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+              v[c] |= (lo < 0x7f80u ? 0u : 0x7fu) | (hi < 0x7f80u ? 0u : 0x7f0000u);
             }
           }
 #pragma unroll
@@ -278,17 +282,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (piece == 0) qscale[par * NH * MR + r] = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
           uint32_t t1w[4], t2w[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const uint4 u = x[i][c >> 1];
-            const uint32_t v2[2] = {(c & 1) ? u.z : u.x, (c & 1) ? u.w : u.y};
-            float v[4];
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-              v[d] = __uint_as_float((d & 1) ? v2[d >> 1] & 0xffff0000u : v2[d >> 1] << 16) * inv;
-              if (!(fabsf(v[d]) < INFINITY)) v[d] = __int_as_float(0x7fc00000);  // an infinite query is NaN
-            }
-            split_e4m3x4<false>(v[0], v[1], v[2], v[3], t1w[c], t2w[c]);
-          }
+          for (int c = 0; c < 4; ++c)
+            split_e4m3x4<false>(__uint_as_float(v[2 * c] << 16) * inv, __uint_as_float(v[2 * c] & 0xffff0000u) * inv,
+                                __uint_as_float(v[2 * c + 1] << 16) * inv,
+                                __uint_as_float(v[2 * c + 1] & 0xffff0000u) * inv, t1w[c], t2w[c]);
           const int lr = q0 * 32 + r;  // row of the MMA tile
           const int ph = D == 128 ? piece ^ (lr & 7) : piece ^ ((lr >> 1) & 3);
           unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + lr * D + ph * 16;
@@ -296,11 +293,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           *reinterpret_cast<uint4*>(dst + C::Q_TERM) = make_uint4(t2w[0], t2w[1], t2w[2], t2w[3]);
         }
         fence_async_smem();
-        bar_sync(sbar, nthr);  // the rows' scales are set
+        bar_sync(pbar, 64);  // the rows' scales are set
         if (lane == 0) mbar_arrive(seg_ready(h));
       };
 
-      Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh);
+      Seg s = find(w.t0, w, p);
       if (s.ntile > 0) start_segment(s, 0);
       while (s.ntile > 0) {
         const uint32_t par = seg_no & 1;
@@ -432,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t xl = it + c.ntile - 1;
         it += c.ntile;
         if (has_more(c, w.t1, w.ovh)) {
-          s = locate<TK>(c.vnext, w.t1, p, w.pb, w.ovh);
+          s = find(c.vnext, w, p);
           start_segment(s, par ^ 1);
         } else {
           s.ntile = 0;
@@ -489,10 +486,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < 8; ++i) dst[i * p.slot_rows] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
           }
         }
+        if (h == 0 && stid == 0) note_split(p, c, w, tile_rows);
         tc_fence_before();
-        bar_sync(sbar, nthr);  // nanv is read; the next segment may set it
-        for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;
-        if (stid == 0) nan_flag[h] = 0;
+        if (has_nan) {  // read by all; the next segment may set them
+          bar_sync(sbar, nthr);
+          for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;
+          if (stid == 0) nan_flag[h] = 0;
+        }
         ++seg_no;
       }
     }

@@ -138,41 +138,70 @@ __device__ __forceinline__ WorkList work_list(const AttnParams& p, const int* pb
   return w;
 }
 
-// What merge_fp8_kernel is to join: a unit split between blocks, noted by the block with its
-// last tiles (they are that block's first, so a block notes at most one). The note does not
-// depend on the pass over the data; every block writes its own, if only an empty one.
-__device__ __forceinline__ void note_split_unit(const AttnFp8Params& p, const WorkList& w, int tile_rows) {
-  int4 a = make_int4(0, 0, 0, 0), b = a;
-  const Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh);
-  if (w.t0 < w.t1 && s.ntile > 0 && s.tile0 > 0 && s.tile0 + s.ntile == s.unit_tiles) {
-    const int first = owner_of(s.unit_start, w.total, w.ctas), row0 = s.rt * tile_rows;
-    a = make_int4(s.b, s.g, row0, min(tile_rows, p.rows - row0));
-    b = make_int4(static_cast<int>(s.u + first), w.cta - first + 1, 0, 0);
+// locate() in 32 bits (a list has at most INT32_MAX tiles).
+__device__ __forceinline__ Seg find(int64_t at, const WorkList& w, const AttnParams& p) {
+  const int v = static_cast<int>(at), v1 = static_cast<int>(w.t1);
+  int lo = 0, hi = p.batch;  // largest b with pb[b] <= v
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (w.pb[mid] <= v) lo = mid; else hi = mid;
   }
-  p.splits[2 * blockIdx.x] = a;
-  p.splits[2 * blockIdx.x + 1] = b;
+  Seg s;
+  s.b = lo;
+  s.kv_len = p.kv_len[lo];
+  s.len_ok = s.kv_len >= p.gamma && s.kv_len <= p.max_keys;
+  s.unit_tiles = unit_tiles<TK>(s.kv_len, p);
+  const uint32_t vlen = s.unit_tiles + w.ovh, rem = v - w.pb[lo], ub = rem / vlen;
+  const int real = v - static_cast<int>(rem - ub * vlen) + w.ovh;  // the unit's first real tile
+  s.g = p.row_tiles == 1 ? ub : ub / p.row_tiles;
+  s.rt = p.row_tiles == 1 ? 0 : ub - s.g * p.row_tiles;
+  s.u = static_cast<int64_t>(lo) * p.hunits * p.row_tiles + ub;
+  s.unit_start = real;
+  const int next = min(real + s.unit_tiles, v1), from = max(v, real);
+  s.vnext = next;
+  s.ntile = max(next - from, 0);
+  s.tile0 = s.ntile > 0 ? from - real : 0;
+  return s;
 }
 
-// Joins the parts of split units: grid (chunks of a unit's outputs, blocks of the pass). A
-// warp takes 8 rows x 32 columns, a thread 8 columns of a row, with the loads of four parts
-// in flight. It is launched while the pass still runs and waits for its end. (The last block
-// to finish a unit merging it alone took 12 to 15 us at the end of a call where this takes 4
-// to 6: 128 rows in 5 parts are 330 KB, an L2 round trip of one SM at a time.)
+// What merge_fp8_kernel is to join: units split between blocks, noted by the block with their
+// last tiles. With at most as many units as blocks each unit has a place; otherwise each
+// block, because only its first segment can end a split unit, and clear_split cleans it first.
+__device__ __forceinline__ void clear_split(const AttnFp8Params& p) {
+  if (!p.split_by_unit) p.splits[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void note_split(const AttnFp8Params& p, const Seg& s, const WorkList& w, int tile_rows) {
+  const bool split = s.tile0 > 0;
+  if (s.tile0 + s.ntile != s.unit_tiles || (!split && !p.split_by_unit)) return;
+  const int first = split ? owner_of(s.unit_start, w.total, w.ctas) : 0, row0 = s.rt * tile_rows;
+  int4* e = p.splits + 2 * (p.split_by_unit ? s.u : blockIdx.x);
+  e[0] = make_int4(s.b, s.g, row0, min(tile_rows, p.rows - row0));
+  e[1] = make_int4(static_cast<int>(s.u + first), split ? w.cta - first + 1 : 0, 0, 0);
+}
+
+// Joins the parts of split units: grid (chunks of a unit's outputs, places of units). A warp
+// takes 8 rows x 32 columns, a thread 8 columns of a row, with the loads of four parts in
+// flight. (The last block to finish a unit merging it alone took 12 to 15 us at the end of a
+// call: 128 rows in 5 parts are 330 KB, an L2 round trip of one SM at a time.)
 constexpr int kMergeThreads = 256;
 template <int D, int HP, bool BY_COLUMNS>
 __global__ void __launch_bounds__(kMergeThreads) merge_fp8_kernel(AttnFp8Params p) {
   pdl_wait_prior();
   const int4 a = __ldcg(p.splits + 2 * blockIdx.y), b = __ldcg(p.splits + 2 * blockIdx.y + 1);
+  // (after a timeout a place may hold anything)
+  if (b.y <= 0 || b.x < 0 || b.y > p.num_slots - b.x || a.x < 0 || a.x >= p.batch || a.y < 0 || a.y >= p.hunits ||
+      a.z < 0 || a.w < 0 || a.w > p.slot_rows / HP || a.w > p.rows - a.z)
+    return;
   const int warp = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int hr = warp / (D / 32) * 8 + (lane & 7), c8 = warp % (D / 32) * 4 + (lane >> 3);
-  if (hr < HP * a.w && b.y > 0)
+  if (hr < HP * a.w)
     merge_fp8_item<D, BY_COLUMNS>(p, a.x, a.y * HP + hr / a.w, a.z + hr % a.w, b.x, b.y, hr, c8);
 }
 
 template <int D, int HP, bool BY_COLUMNS>
 cudaError_t launch_merge(const AttnFp8Params& p, const AttnFp8Plan& P, cudaStream_t stream) {
   const int warps = (P.slot_rows + 7) / 8 * (D / 32);
-  const dim3 grid((warps + kMergeThreads / 32 - 1) / (kMergeThreads / 32), P.grid);
+  const dim3 grid((warps + kMergeThreads / 32 - 1) / (kMergeThreads / 32), P.splits);
   return launch_overlapped(merge_fp8_kernel<D, HP, BY_COLUMNS>, grid, kMergeThreads, 0, stream, p);
 }
 
@@ -192,7 +221,7 @@ __device__ __forceinline__ void produce(const AttnFp8Params& p, const CUtensorMa
   const int psh = __ffs(p.page_size) - 1;  // log2
   const int npg = TK >> psh;               // pages of a tile
   const uint32_t box_bytes = static_cast<uint32_t>(p.page_size) * D * 2 * HP;
-  for (Seg s = locate<TK>(w.t0, w.t1, p, w.pb, w.ovh); s.ntile > 0 && ok && !p.starve; ++seg_no) {
+  for (Seg s = find(w.t0, w, p); s.ntile > 0 && ok && !p.starve; ++seg_no) {
     const bool bad_len = !s.len_ok;
     bool flag = bad_len;
     // Pages are taken 32 at a time, a lane each; the next 32 ids and scales are loaded
@@ -258,7 +287,7 @@ __device__ __forceinline__ void produce(const AttnFp8Params& p, const CUtensorMa
       mbar_arrive(flag_ready + 8u * (seg_no % kFlagRing));
     }
     if (!has_more(s, w.t1, w.ovh)) break;
-    s = locate<TK>(s.vnext, w.t1, p, w.pb, w.ovh);
+    s = find(s.vnext, w, p);
   }
   if (!ok) {  // copies still in flight (bounded)
     for (uint32_t x = it > static_cast<uint32_t>(NST) ? it - NST : 0; x < it; ++x) {

@@ -17,12 +17,12 @@ struct AttnFp8Plan {
   int rows_on_m;        // tensor cores: attn_fp8_rows.cu, else attn_fp8_keys.cu
   int heads;            // tensor cores: KV heads per block (2: adjacent ones)
   int sub_rows;         // tensor cores: query rows of one of a block's two sub-units
-  int grid;             // tensor cores: blocks
+  int grid, splits;     // tensor cores: blocks, and places for units to merge
   int rows, row_tiles;  // (Hq/Hkv) * gamma query rows per KV head, in tiles
   int nsplit, tiles_per_split;  // CUDA cores: KV splits per unit and key tiles of a split
   int64_t slots;        // partial results
   int slot_rows;        // rows of one
-  size_t tickets, partial_o, partial_ml, end;
+  size_t tickets, partial_o, partial_ml, split_notes, end;
 };
 AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path);
 constexpr int kFp8KeyTile = 128;  // keys per tile of the tensor-core kernels
