@@ -45,11 +45,13 @@ spec_status_t check_append(const spec_append_fp8_args_t* a) {
 }
 
 // The tensor-core form of a call. A block serves two sub-units of query rows: two adjacent KV
-// heads where each fits one (a page of both is one copy of twice the size), else two halves
-// of one KV head's rows, in tiles. Up to 128 rows a KV head the keys are on the MMA's M side
-// (up to 64 rows a sub-unit); above, the rows are (up to 128 a sub-unit).
+// heads where each fits one (a page of both is one copy of twice the size; 66 to 128 rows as
+// two halves of one head instead: 174 against 124 us at batch 64 / block 20), else two halves
+// of one KV head's rows, in tiles. Up to 32 rows a sub-unit the keys are on the MMA's M side,
+// from 33 the rows (batch 64 / block 8 of 4 heads, 32 rows: 88 us and 97; block 10: 115 and
+// 102). Sequences are taken kFp8TcBatch at a time, because a block keeps their first tiles.
 struct TcForm {
-  int rows_on_m, heads, sub_rows, row_tiles;
+  int rows_on_m, heads, sub_rows, row_tiles, batch;
   bool fits;
 };
 TcForm tc_form(const spec_attn_fp8_args_t& a) {
@@ -59,11 +61,10 @@ TcForm tc_form(const spec_attn_fp8_args_t& a) {
   f.row_tiles = f.heads == 2 ? 1 : (rows + 255) / 256;
   f.sub_rows = f.heads == 2 ? rows : (rows > 256 ? 128 : (rows + 1) / 2);
   f.rows_on_m = f.sub_rows > 32;
-  const size_t smem = f.rows_on_m ? attn_fp8_rows_smem(a, f.heads) : attn_fp8_keys_smem(a, f.heads, f.sub_rows);
+  f.batch = a.batch < kFp8TcBatch ? a.batch : kFp8TcBatch;
   const int64_t tiles = (static_cast<int64_t>(a.max_pages_per_seq) * a.page_size + kFp8KeyTile - 1) / kFp8KeyTile + 8;
-  const int64_t units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / f.heads) * f.row_tiles;
-  f.fits = smem <= kTcMaxSmem && tiles * units <= INT32_MAX &&
-           2 * static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX;
+  const int64_t units = static_cast<int64_t>(f.batch) * (a.num_kv_heads / f.heads) * f.row_tiles;
+  f.fits = tiles * units <= INT32_MAX && 2 * static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX;
   return f;
 }
 
@@ -128,7 +129,8 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
     P.heads = f.heads;
     P.sub_rows = f.sub_rows;
     P.row_tiles = f.row_tiles;
-    units = static_cast<int64_t>(a.batch) * (a.num_kv_heads / P.heads) * P.row_tiles;
+    P.batch = f.batch;
+    units = static_cast<int64_t>(P.batch) * (a.num_kv_heads / P.heads) * P.row_tiles;
     P.grid = num_sms;
     P.splits = static_cast<int>(units < P.grid ? units : P.grid);
     P.nsplit = 1;
@@ -169,11 +171,23 @@ spec_status_t run_attn_fp8(const spec_attn_fp8_args_t* a, void* ws, size_t ws_by
   const AttnFp8Plan P = attn_fp8_plan(*a, kWsHeader, scope.sms, a->path);
   if (P.end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
   char* w = static_cast<char*>(ws);
-  if (P.path == SPEC_ATTN_TENSOR_CORES)
-    return (P.rows_on_m ? launch_attn_fp8_rows(*a, P, w, s, starve) : launch_attn_fp8_keys(*a, P, w, s, starve)) ==
-                   cudaSuccess
-               ? SPEC_OK
-               : SPEC_ERR_CUDA;
+  if (P.path == SPEC_ATTN_TENSOR_CORES) {
+    for (int b0 = 0; b0 < a->batch; b0 += P.batch) {
+      spec_attn_fp8_args_t part = *a;
+      part.batch = a->batch - b0 < P.batch ? a->batch - b0 : P.batch;
+      const int64_t rows = static_cast<int64_t>(b0) * a->gamma, heads = rows * a->num_q_heads;
+      part.q = static_cast<const char*>(a->q) + heads * a->head_dim * 2;
+      part.out = static_cast<char*>(a->out) + heads * a->head_dim * 2;
+      part.page_table = a->page_table + static_cast<int64_t>(b0) * a->max_pages_per_seq;
+      part.kv_len = a->kv_len + b0;
+      if (a->lse) part.lse = a->lse + heads;
+      if (a->tree_mask) part.tree_mask = a->tree_mask + rows;
+      if ((P.rows_on_m ? launch_attn_fp8_rows(part, P, w, s, starve) : launch_attn_fp8_keys(part, P, w, s, starve)) !=
+          cudaSuccess)
+        return SPEC_ERR_CUDA;
+    }
+    return SPEC_OK;
+  }
   if (starve) return SPEC_ERR_UNSUPPORTED;
   return launch_attn_fp8_simt(*a, P, w, s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }

@@ -45,15 +45,16 @@ using namespace fp8tc;
 constexpr int kSoftWarps = 8 * NH;
 constexpr int kThreads = 32 * (kSoftWarps + 4);
 
-// NR: query rows of a sub-unit (N of the first product), 16, 32 or 64.
+// NR: query rows of a sub-unit (N of the first product), 16 or 32.
 template <int D, int HP, int NR>
 struct Cfg {
   static constexpr int NC = NR / 2;                        // rows per softmax warp
   static constexpr uint32_t ATOM = Stage<D, HP>::ATOM, SG = Stage<D, HP>::SG, STAGE = Stage<D, HP>::BYTES;
-  static constexpr int NST = (HP == 2 ? 2 : 4) * (128 / D);  // 128 KB in stages
   static constexpr int SB = 2;                             // S buffers per sub-unit
   static constexpr uint32_t Q_TERM = NR * D;               // one term of one sub-unit's Q
-  static constexpr uint32_t P_BUF = TK * 128;              // [key][128 B]: first terms, second terms
+  static constexpr uint32_t PW = 2 * NR;                   // a key's weights: first terms, second terms
+  static constexpr uint32_t P_BUF = TK * PW;               // [key][PW], swizzled by its width
+  static constexpr int NST = (208 * 1024 - NH * (P_BUF + 2 * Q_TERM)) / STAGE;  // D = 128, HP = 2: 3 or 2
   static constexpr uint32_t OFF_STAGE = 0;
   static constexpr uint32_t OFF_P = OFF_STAGE + NST * STAGE;
   static constexpr uint32_t OFF_Q = OFF_P + NH * P_BUF;
@@ -79,7 +80,7 @@ struct Cfg {
   static constexpr uint32_t O_COL = NH * SB * NR;           // [NH][first, second terms][NR]
   static constexpr uint32_t TMEM_COLS = NH * (SB + 2) * NR;
   static_assert(TMEM_COLS <= 512, "TMEM holds 512 columns");
-  static size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
+  static constexpr size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
 };
 
 // ---------------------------------------------------------------------------------
@@ -176,6 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(bar0 + 8u * i, n);
     }
     if (lane < NH) nan_flag[lane] = 0;
+    if (lane < 2 * kFlagRing) seg_flag[lane] = 0;
     if (lane == 0) *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int kk = 0; kk < TK / 32; ++kk)
               mma_e4m3(tmem + C::O_COL + h * 2 * NR, desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG),
-                       desc_rows<128>(pa + kk * 4096u, 0, 1024), kIdesc, k > 0 || kk > 0);
+                       desc_rows<C::PW>(pa + kk * 32u * C::PW, 0, 8 * C::PW), kIdesc, k > 0 || kk > 0);
             mma_commit(pv_done(h));
             if (h == NH - 1) mma_commit(empty(st));
             issued = true;
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int pg = (q4 * 32 + lane) / p.page_size;  // this lane's page of a tile
     float* xch = reinterpret_cast<float*>(smem + C::OFF_X) + h * 4 * NR;  // [4][NR]
     uint32_t* qmax = reinterpret_cast<uint32_t*>(smem + C::OFF_QMAX) + h * 8;
-    unsigned char* const pbuf = smem + C::OFF_P + h * C::P_BUF + (q4 * 32 + lane) * 128;
+    unsigned char* const pbuf = smem + C::OFF_P + h * C::P_BUF + (q4 * 32 + lane) * C::PW;
     uint32_t it = 0, seg_no = 0;
     // After a timeout the warp runs its loops to the end without waiting (nothing else
     // depends on `dead`), so that it passes every named barrier.
@@ -499,13 +501,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             split_e4m3x4<true>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
           }
-          const int sw = lane & 7;
-          if constexpr (CB == 16) {
-            const int a = (ch * NC + cb) / 16, b = a + NR / 16;
-            *reinterpret_cast<uint4*>(pbuf + ((a ^ sw) << 4)) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
-            *reinterpret_cast<uint4*>(pbuf + ((b ^ sw) << 4)) = make_uint4(w2[0], w2[1], w2[2], w2[3]);
-          } else {  // NR = 16: eight bytes of a 16-byte chunk
-            *reinterpret_cast<uint2*>(pbuf + ((0 ^ sw) << 4) + ch * 8) = make_uint2(w1[0], w1[1]);
+          if constexpr (NR == 32) {  // this warp's rows are one 16-byte chunk of each term
+            const int sw = lane >> 1 & 3;
+            *reinterpret_cast<uint4*>(pbuf + ((ch ^ sw) << 4)) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+            *reinterpret_cast<uint4*>(pbuf + (((ch + 2) ^ sw) << 4)) = make_uint4(w2[0], w2[1], w2[2], w2[3]);
+          } else {  // half a chunk
+            const int sw = lane >> 2 & 1;
+            *reinterpret_cast<uint2*>(pbuf + (sw << 4) + ch * 8) = make_uint2(w1[0], w1[1]);
             *reinterpret_cast<uint2*>(pbuf + ((1 ^ sw) << 4) + ch * 8) = make_uint2(w2[0], w2[1]);
           }
         }
@@ -610,8 +612,9 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   p.starve = starve ? 1 : 0;
   // Starting a unit inside a block's range costs about this many tiles of time (its Q, the
   // pipeline's refill, its outputs). Charging it keeps blocks of many short units and of few
-  // long ones equal (batch 64 / block 16, 0: 166 us, 2: 143, 5: 132, 8: 137).
-  p.unit_overhead = 5;
+  // long ones equal (batch 64 / block 8, 3: 89.5 us, 4: 87.4, 5: 89.3, 6: 90.4).
+  p.unit_overhead = 4;
+  static_assert(C::smem_bytes(kFp8TcBatch) <= kTcMaxSmem, "a block's shared memory");
   const size_t smem = C::smem_bytes(a.batch);
   auto kernel = attn_fp8_keys_kernel<D, HP, NR>;
   const cudaError_t e =
@@ -625,15 +628,7 @@ template <int D, int HP>
 cudaError_t launch_d(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
                      bool starve) {
   if (P.sub_rows <= 16) return launch_typed<D, HP, 16>(a, P, ws, stream, starve);
-  if (P.sub_rows <= 32) return launch_typed<D, HP, 32>(a, P, ws, stream, starve);
-  return launch_typed<D, HP, 64>(a, P, ws, stream, starve);
-}
-
-template <int D, int HP>
-size_t smem_of(int sub_rows, int batch) {
-  return sub_rows <= 16   ? Cfg<D, HP, 16>::smem_bytes(batch)
-         : sub_rows <= 32 ? Cfg<D, HP, 32>::smem_bytes(batch)
-                          : Cfg<D, HP, 64>::smem_bytes(batch);
+  return launch_typed<D, HP, 32>(a, P, ws, stream, starve);
 }
 
 }  // namespace
@@ -659,12 +654,6 @@ bool encode_fp8_map(CUtensorMap* map, const spec_attn_fp8_args_t& a, int heads) 
 }
 
 }  // namespace fp8tc
-
-size_t attn_fp8_keys_smem(const spec_attn_fp8_args_t& a, int heads, int sub_rows) {
-  const bool d128 = a.head_dim == 128;
-  return heads == 2 ? (d128 ? smem_of<128, 2>(sub_rows, a.batch) : smem_of<64, 2>(sub_rows, a.batch))
-                    : (d128 ? smem_of<128, 1>(sub_rows, a.batch) : smem_of<64, 1>(sub_rows, a.batch));
-}
 
 cudaError_t launch_attn_fp8_keys(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
                                bool starve) {

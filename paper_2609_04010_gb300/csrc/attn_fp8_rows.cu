@@ -57,7 +57,7 @@ struct Cfg {
   static constexpr uint32_t O_COL = NH * TK;                      // [NH][D]
   static constexpr uint32_t TMEM_COLS = 512;
   static_assert(O_COL + NH * D <= TMEM_COLS, "TMEM holds 512 columns");
-  static size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
+  static constexpr size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
 };
 
 // The same with A in tensor memory (M rows on the lanes, four bytes of K per column).
@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(bar0 + 8u * i, n);
     }
     if (lane < NH) nan_flag[lane] = 0;
+    if (lane < 2 * kFlagRing) seg_flag[lane] = 0;
     if (lane == 0) *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -516,6 +517,7 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   p.rows_per_cta = P.sub_rows;
   p.starve = starve ? 1 : 0;
   p.unit_overhead = 3;  // tiles of time that starting a unit costs
+  static_assert(C::smem_bytes(kFp8TcBatch) <= kTcMaxSmem, "a block's shared memory");
   const size_t smem = C::smem_bytes(a.batch);
   auto kernel = attn_fp8_rows_kernel<D, HP>;
   const cudaError_t e =
@@ -526,11 +528,6 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
 }
 
 }  // namespace
-
-size_t attn_fp8_rows_smem(const spec_attn_fp8_args_t& a, int heads) {
-  if (a.head_dim == 128) return heads == 2 ? Cfg<128, 2>::smem_bytes(a.batch) : Cfg<128, 1>::smem_bytes(a.batch);
-  return heads == 2 ? Cfg<64, 2>::smem_bytes(a.batch) : Cfg<64, 1>::smem_bytes(a.batch);
-}
 
 cudaError_t launch_attn_fp8_rows(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws, cudaStream_t stream,
                                  bool starve) {

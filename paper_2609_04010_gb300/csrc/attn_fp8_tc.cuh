@@ -44,12 +44,12 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Matrix descriptor of a tile whose rows are W bytes (128 or 64) with the W-byte swizzle.
+// Matrix descriptor of a tile whose rows are W bytes (128, 64 or 32) with the W-byte swizzle.
 template <int W>
 __device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
   return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>((lbo >> 4) & 0x3FFFu) << 16) |
          (static_cast<uint64_t>((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46) |
-         (static_cast<uint64_t>(W == 128 ? 2 : 4) << 61);
+         (static_cast<uint64_t>(W == 128 ? 2 : W == 64 ? 4 : 6) << 61);
 }
 // Instruction descriptor, kind::f8f6f4: fp32 accumulator, e4m3 A and B.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn, bool b_mn) {

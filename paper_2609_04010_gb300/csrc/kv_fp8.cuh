@@ -16,6 +16,7 @@ struct AttnFp8Plan {
   int path;             // SPEC_ATTN_CUDA_CORES or SPEC_ATTN_TENSOR_CORES
   int rows_on_m;        // tensor cores: attn_fp8_rows.cu, else attn_fp8_keys.cu
   int heads;            // tensor cores: KV heads per block (2: adjacent ones)
+  int batch;            // tensor cores: sequences per launch
   int sub_rows;         // tensor cores: query rows of one of a block's two sub-units
   int grid, splits;     // tensor cores: blocks, and places for units to merge
   int rows, row_tiles;  // (Hq/Hkv) * gamma query rows per KV head, in tiles
@@ -25,11 +26,9 @@ struct AttnFp8Plan {
   size_t tickets, partial_o, partial_ml, split_notes, end;
 };
 AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path);
-constexpr int kFp8KeyTile = 128;  // keys per tile of the tensor-core kernels
-// Their blocks' shared memory. starve (test hook only): the producers issue no copies, so the
-// bounded waits run out.
-size_t attn_fp8_keys_smem(const spec_attn_fp8_args_t& a, int heads, int sub_rows);
-size_t attn_fp8_rows_smem(const spec_attn_fp8_args_t& a, int heads);
+constexpr int kFp8KeyTile = 128;   // keys per tile of the tensor-core kernels
+constexpr int kFp8TcBatch = 2048;  // sequences they take in a launch
+// starve (test hook only): the producers issue no copies, so the bounded waits run out.
 cudaError_t launch_attn_fp8_keys(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
                                  cudaStream_t stream, bool starve = false);
 cudaError_t launch_attn_fp8_rows(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,

@@ -299,6 +299,12 @@ def test_no_lse_and_auto():
     c.check(0)
 
 
+@pytest.mark.parametrize("G,Hq", [(1, 4), (9, 8)])
+def test_more_sequences_than_one_launch_takes(G, Hq):
+    """The tensor-core kernels take 2,048 sequences at a time; the parts meet nowhere."""
+    Case(2051, G, Hq, 2, 64, 16, [40, 3, 0, 129], seed=9, tree=random_tree).check(TENSOR_CORES)
+
+
 def test_wait_timeout_is_reported_and_survived():
     """The kernel with an idle copy producer: its bounded waits run out, it reports, and the
     same workspace serves the next call."""
@@ -312,6 +318,24 @@ def test_wait_timeout_is_reported_and_survived():
     b.test_attention_fp8_wait_timeout_args(a, ws)
     assert b.read_device_status(ws) == (6, b.FLAG_TIMEOUT)
     assert int(ws[256:256 + 64].sum()) == 0
+    b.verify_attention_fp8_args(a, ws)
+    torch.cuda.synchronize()
+    assert b.read_device_status(ws) == (0, 0)
+    assert np.array_equal(out.float().cpu().numpy().astype(np.float64), want[0])
+    assert np.array_equal(lse.cpu().numpy().astype(np.float64), want[1])
+
+
+def test_wait_timeout_with_many_rows_is_reported_and_survived():
+    """The same for the kernel that takes 33 and more query rows."""
+    from paper_2609_04010_gb300 import binding as b
+    c = Case(2, 12, 8, 2, 64, 32, [300, 5], seed=8)
+    want = c.run(TENSOR_CORES)
+    t, _ = c.device()
+    out, lse = torch.zeros_like(t[0]), torch.zeros(t[0].shape[:3], device="cuda")
+    a = b.attn_fp8_args(*t, out, lse, path=TENSOR_CORES)
+    ws = b.new_workspace(b.attn_fp8_workspace_size(a))
+    b.test_attention_fp8_wait_timeout_args(a, ws)
+    assert b.read_device_status(ws) == (6, b.FLAG_TIMEOUT)
     b.verify_attention_fp8_args(a, ws)
     torch.cuda.synchronize()
     assert b.read_device_status(ws) == (0, 0)
