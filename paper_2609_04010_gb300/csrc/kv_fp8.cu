@@ -301,10 +301,21 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(AppendParams
         x[i] = __ldg(reinterpret_cast<const uint4*>(src + row * stride));
       }
     }
+    // Magnitudes of bf16 values compare like their bits, two in a word; Infs and NaNs, which
+    // do not count, are above all others and are sorted out only where there are any.
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i)
-      m = finite_max2(x[i].w, finite_max2(x[i].z, finite_max2(x[i].y, finite_max2(x[i].x, m))));
-    m = __reduce_max_sync(0xffffffffu, m);
+    for (int i = 0; i < STEPS; ++i) {
+      m = __vmaxu2(m, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu));
+      m = __vmaxu2(m, __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
+    }
+    m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+    if (m >= 0x7f80u) {
+      m = 0;
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i)
+        m = finite_max2(x[i].w, finite_max2(x[i].z, finite_max2(x[i].y, finite_max2(x[i].x, m))));
+      m = __reduce_max_sync(0xffffffffu, m);
+    }
     if (GW > 1) {  // over the group's warps; the two halves of amax take turns
       if (lane == 0) amax[group][turn][gwarp] = m;
       asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(GW * 32) : "memory");
