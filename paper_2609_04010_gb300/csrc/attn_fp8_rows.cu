@@ -38,8 +38,8 @@ constexpr int HK = TK / 2;  // keys of a tile that a thread weighs
 template <int D, int HP>
 struct Cfg {
   static constexpr uint32_t ATOM = Stage<D, HP>::ATOM, SG = Stage<D, HP>::SG, STAGE = Stage<D, HP>::BYTES;
-  static constexpr int NST = (HP == 2 ? 2 : 4) * (128 / D);  // 128 KB in stages
-  static constexpr uint32_t Q_TERM = MR * D;                 // one term of one sub-unit's Q
+  static constexpr uint32_t Q_TERM = MR * D;                                // one term of one sub-unit's Q
+  static constexpr int NST = (208 * 1024 - NH * 2 * Q_TERM) / STAGE;  // D = 128: 2 (HP = 2) or 4
   static constexpr uint32_t OFF_STAGE = 0;
   static constexpr uint32_t OFF_Q = OFF_STAGE + NST * STAGE;
   static constexpr uint32_t OFF_SCL = OFF_Q + NH * 2 * Q_TERM;      // float4 [NST][8 pages][HP]
@@ -516,7 +516,8 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   p.hunits = a.num_kv_heads / HP;
   p.rows_per_cta = P.sub_rows;
   p.starve = starve ? 1 : 0;
-  p.unit_overhead = 3;  // tiles of time that starting a unit costs
+  // tiles of time that starting a unit costs (batch 64 / block 20, 2: 126 us, 3: 124, 4: 121)
+  p.unit_overhead = 4;
   static_assert(C::smem_bytes(kFp8TcBatch) <= kTcMaxSmem, "a block's shared memory");
   const size_t smem = C::smem_bytes(a.batch);
   auto kernel = attn_fp8_rows_kernel<D, HP>;
