@@ -8,7 +8,9 @@
 // written without being read), and last rewrites the listed tokens, shared out over all
 // threads: a few in a hundred logits, but so spread that handled in the copy they would hold
 // up most warps (353 us at 64 x 16 x 128,256). The logits are read and written once; memory
-// bounds it.
+// bounds it: 64 x 16 x 128,256 bf16 logits take 91 us, 5.9 TB/s (0.87 of the measured copy
+// rate), 8 x 8 of them 12.8 us, a third of it the launch and a third the history. Fetching the
+// first rows meanwhile into L2 gained nothing (13.3 us; 95.7 with all rows).
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -1,5 +1,6 @@
-// Attention of the block queries over the 8-bit KV cache on tcgen05 tensor cores
-// (spec_verify_attention_fp8, SPEC_ATTN_TENSOR_CORES).
+// Attention of the block queries over the 8-bit KV cache on tcgen05 tensor cores, with the
+// keys on the MMA's M side (spec_verify_attention_fp8, SPEC_ATTN_TENSOR_CORES, KV groups of few
+// rows).
 //
 // Both products run in e4m3 straight from the cache's bytes, which land in shared memory by
 // TMA in the layout that the MMAs read; nothing is decoded on the way. They are transposed,
@@ -20,9 +21,13 @@
 // (e4m3 ends at 448), which after a unit's first tile is rare. The second term of P is kept
 // times 16, which puts its smallest step at 2^-13.
 //
-// A block serves two sub-units of at most 64 query rows: two adjacent KV heads (HP = 2, one
+// A block serves two sub-units of at most 32 query rows: two adjacent KV heads (HP = 2, one
 // box brings K and V of both: 8 KB with 16-token pages and D = 128), or two halves of one KV
-// head's rows (HP = 1). Warp roles (persistent, one block per SM):
+// head's rows (HP = 1). Shared memory beyond Q and P is stages; P's rows are as narrow as its
+// weights (32 or 64 bytes a key), which with 16 rows a sub-unit leaves room for a third stage of
+// two heads (batch 32 decoding: 103 us with two). Keys and values in stages of their own, freed
+// earlier but copied in boxes of half the size, took 99. Warp roles (persistent, one block per
+// SM):
 //   warps 16,19  producers: page ids and scales 32 pages ahead, one TMA box per page, each
 //                the half of a tile's pages
 //   warp 17      issues S^T = K Q^T into two S buffers per sub-unit in TMEM
@@ -31,10 +36,14 @@
 //                share the rows. The sub-units' warps run free of each other, so that the
 //                waits of one are filled by the other's arithmetic. They also convert Q and
 //                write the outputs.
-// The tiles of all units form one list that is cut into equal ranges, one per block; a unit
-// split between blocks is merged from fp32 partials by the last block to finish it (atomic
-// ticket, no waiting). Every mbarrier wait is bounded; after a timeout the softmax warps run
-// their loops to the end without waiting, so that none is missed at a named barrier.
+// The tiles of all units form one list that is cut into equal ranges, one per block; the fp32
+// parts of a unit split between blocks are joined by a second launch. Every mbarrier wait is
+// bounded; after a timeout the softmax warps run their loops to the end without waiting, so
+// that none is missed at a named barrier.
+//
+// Memory bounds it up to 16 rows: batch 32, one token a sequence, contexts 256 to 16,384, 32 / 8
+// heads of 128: 92 us, 5.93 TB/s (0.87 of the measured copy rate). With 32 rows the chain of
+// waits from a tile's scores to its outputs does (batch 64 / block 8: 87 us, floor 46).
 #include "attn_fp8_tc.cuh"
 
 namespace specv {

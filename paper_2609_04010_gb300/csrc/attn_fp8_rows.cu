@@ -6,23 +6,34 @@
 //   O[row][dim] += sum_key P8[row][key] V8[key][dim] (M = 128 rows, N = D, K = 128 keys)
 // The arithmetic is attn_fp8_keys.cu's: e4m3 operands straight from the cache, queries and
 // weights as sums of two e4m3 terms, weights P = 2^(s + log2(sv) - m) against a reference m
-// per row, sum P / sv. Here a thread owns a row: its maximum, its sum and its reference are
-// its own registers, the page constants are the same for all lanes, and no warp waits for
-// another. With few rows the M side would be padding and attn_fp8_keys.cu is faster.
+// per row, sum P / sv. Here two threads share a row, each with half of a tile's keys: maximum,
+// sum and reference are their own registers, the page constants are the same for all lanes,
+// and only the two warps of 32 rows wait for each other (one thread a row: 162 us against 115
+// at batch 64 / block 16, because eight warps cannot hide each other's waits). With few rows the
+// M side would be padding and attn_fp8_keys.cu is faster.
 //
 // A block serves two sub-units of at most 128 query rows: two adjacent KV heads (HP = 2) or
 // two halves of one KV head's rows. Both terms of P live in TMEM over the columns of S that
 // they came from (32 keys of S are 32 columns, of P 8 + 8), so that shared memory holds Q and
 // K/V stages only; S is computed again once the products have read P. While one sub-unit is
 // at its softmax, the tensor core works for the other. m is set so that a row's largest P is
-// 32 and raised when a P would pass 256 (both terms add up in one accumulator, so the second
-// one's smallest step is 2^-9; 2^-14 of a row's largest weight). Warp roles (persistent, one
-// block per SM):
-//   warps 0..7   softmax, four per sub-unit, a thread per row
-//   warps 8, 11  producers (as in attn_fp8_keys.cu)
-//   warp 9       issues S = Q K^T
-//   warp 10      issues O += P V; clears V of keys past the sequence's end
+// 2^4.5 to 2^5.5 and raised when a P would pass 2^8 (both terms add up in one accumulator, so
+// the second one's smallest step is 2^-9; 2^-14 of a row's largest weight). m is a whole number,
+// so that log2(sv) - m is exact with power-of-two scales. Hidden scores are set to -inf in
+// TMEM, before the two passes over a tile (the maximum, the weights), which then know no masks.
+// Warp roles (persistent, one block per SM):
+//   warps 0..15   softmax, eight per sub-unit: a lane quadrant is 32 rows, two warps a quadrant
+//   warps 16, 18  producers (as in attn_fp8_keys.cu)
+//   warp 17       issues S = Q K^T and O += P V; clears V of keys past the sequence's end
 // Work list, split units, bounded waits: as in attn_fp8_keys.cu.
+//
+// What bounds it is the chain S, softmax, P V of a sub-unit: 2.4 us a tile of 128 keys, of which
+// its softmax is 1.3 (the converts to e4m3 and ex2 take 0.5 of it) and the products 0.55; two
+// sub-units, all that TMEM has room for with D = 128, do not cover each other fully. Half tiles
+// with scores in two buffers (231 us), four threads a row (158), and weights taken before the
+// maximum is known (276) were all slower than the 155 us that it takes for batch 4, block 32, 64 /
+// 8 heads, 32,768 keys: 885 TFLOP/s of Q K^T and P V, twice that on the tensor cores. Batch 64,
+// block 16, 32 / 8 heads, contexts 512 to 4,096: 107 us, 3.0 TB/s.
 #include "attn_fp8_tc.cuh"
 
 namespace specv {

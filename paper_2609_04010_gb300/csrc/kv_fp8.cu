@@ -18,7 +18,10 @@ namespace {
 // scan and a dependent expansion. No block waits: the state that may be updated in place
 // (kv_len, free_count) is written by the block that takes the last ticket, after every
 // block has read it. New pages are read from the free list, never from the table entries
-// that other blocks are writing.
+// that other blocks are writing. Up to some 100,000 rows a call is a launch and a chain of three
+// dependent reads (64 requests of 16 tokens: 4.7 us); above, the writes count (512 requests of 1
+// to 4,096 tokens, 1.05 M rows: 8.8 us, 1.5 TB/s; half or twice the rows per block: 10.3 and 16
+// us).
 constexpr int kSlotThreads = 512;
 constexpr int kSlotRowsPerBlock = 8 * kSlotThreads;  // rows the grid is sized for, per block
 
@@ -202,7 +205,10 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
 // page's new keys or values of one head in registers: one pass finds their largest
 // magnitude, from it the page's scale, and the same registers are rounded and stored. Groups
 // run free of each other. HBM traffic is the new rows once and their 8-bit form once (a page
-// whose scale grows is read and written once more); memory bounds it.
+// whose scale grows is read and written once more); memory bounds it: 8 prompts of 4,093 tokens,
+// 8 heads of 128, take 35.3 us, 5.7 TB/s (0.84 of the measured copy rate; 44 us when the
+// magnitudes were compared one by one). 64 blocks of 16 tokens: 4.5 us, the launch and two
+// dependent reads. 16 or 64 rows a block: 38 us both.
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 32;
 constexpr int kWin = SPEC_APPEND_WINDOW;

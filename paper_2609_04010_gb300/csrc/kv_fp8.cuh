@@ -40,6 +40,8 @@ cudaError_t launch_attn_fp8_simt(const spec_attn_fp8_args_t& a, const AttnFp8Pla
 // A launch that may start while the kernel before it on the stream still runs. Every thread of
 // such a kernel calls pdl_wait_prior() before it touches global memory, which waits for that
 // kernel's end; what the launch itself and a block's set-up take is hidden (1.5 to 2 us a call).
+// No kernel lets the next one start before its own blocks end: blocks that wait took the places
+// of working ones (the slots of 512 requests: 12 us against 9).
 template <typename... Params, typename... Args>
 cudaError_t launch_overlapped(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream,
                               Args... args) {
