@@ -95,6 +95,62 @@ def test_decoding(gamma, Hq, H, D, P):
             assert np.all(np.abs(held - x) <= 8 * (2.0 ** -4 * np.abs(x) + 2.0 ** -10 * sc) + 2.0 ** -7 * np.abs(x).max())
 
 
+@pytest.mark.parametrize("gamma,Hq", [(1, 4), (3, 16), (20, 8)])
+def test_calls_that_overlap_see_what_those_before_wrote(gamma, Hq):
+    """Slots, append and attention issued back to back, each launch free to start while the one
+    before ends, directly and as one graph: the same results as with a wait after each call."""
+    from paper_2609_04010_gb300 import binding as b
+    B, H, D, P, V, steps = 5, 2, 128, 16, 1000, 6
+    g = torch.Generator(device="cuda").manual_seed(gamma)
+
+    def rand(*shape):
+        return torch.randn(shape, device="cuda", generator=g)
+
+    k, v = (rand(steps, B * gamma, H, D).bfloat16() for _ in range(2))
+    q, logits = rand(steps, B, gamma, Hq, D).bfloat16(), rand(steps, B, gamma, V)
+    block = torch.randint(0, V, (steps, B, gamma), device="cuda", generator=g, dtype=torch.int32)
+    new = torch.full((B,), gamma, dtype=torch.int32, device="cuda")
+    rep = torch.full((B,), 1.5, device="cuda")
+    got = []
+    for way in ("wait", "issue", "graph"):
+        cache, scale = b.new_kv_cache_fp8(B * 10, H, P, D)
+        table = torch.full((B, 10), -1, dtype=torch.int32, device="cuda")
+        free = torch.arange(B * 10, dtype=torch.int32, device="cuda")
+        count = torch.tensor([B * 10], dtype=torch.int32, device="cuda")
+        kv_len = torch.zeros(B, dtype=torch.int32, device="cuda")
+        rows = [torch.empty(n, dtype=torch.int32, device="cuda") for n in (B + 1, B * gamma)]
+        out, lse, adj = torch.zeros_like(q), torch.zeros(q.shape[:4], device="cuda"), torch.zeros_like(logits)
+        sa = b.slot_args(new, kv_len, kv_len, table, P, B * 10, free, count, count, *rows)
+        sw = b.new_workspace(b.slot_workspace_size(sa))
+        calls, held = [], [sa]
+        for i in range(steps):
+            pa = b.append_fp8_args(k[i], v[i], rows[1], cache, scale)
+            ta = b.attn_fp8_args(q[i], cache, scale, table, kv_len, out[i], lse[i])
+            ja = b.adjust_args(logits[i], adj[i], block[i], repetition=rep)
+            tw = b.new_workspace(b.attn_fp8_workspace_size(ta))
+            held += [pa, ta, ja, tw]
+            calls += [lambda: b.map_slots_args(sa, sw), lambda pa=pa: b.append_kv_fp8_args(pa),
+                      lambda ta=ta, tw=tw: b.verify_attention_fp8_args(ta, tw),
+                      lambda ja=ja: b.adjust_logits_args(ja)]
+        torch.cuda.synchronize()
+        if way == "graph":
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                for c in calls:
+                    c()
+            graph.replay()
+        else:
+            for c in calls:
+                c()
+                if way == "wait":
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        got.append((out, lse, adj, cache.view(torch.uint8), scale, table, kv_len, count))
+    for other in got[1:]:
+        for x, y in zip(got[0], other):
+            assert torch.equal(x, y)
+
+
 def test_the_example_runs(capsys):
     example().main()
     assert "status: 0" in capsys.readouterr().out
