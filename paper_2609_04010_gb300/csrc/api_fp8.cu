@@ -124,7 +124,7 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
   P.path = path != SPEC_ATTN_CUDA_CORES && f.fits ? SPEC_ATTN_TENSOR_CORES : SPEC_ATTN_CUDA_CORES;
   int64_t units;
   if (P.path == SPEC_ATTN_TENSOR_CORES) {
-    // persistent grid; a unit has a slot of its own and one per block that starts inside it
+    // persistent grid; a block's range begins inside one unit at most and ends inside one
     P.rows_on_m = f.rows_on_m;
     P.heads = f.heads;
     P.sub_rows = f.sub_rows;
@@ -135,7 +135,7 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
     P.splits = static_cast<int>(units < P.grid ? units : P.grid);
     P.nsplit = 1;
     P.slot_rows = 2 * P.sub_rows;
-    P.slots = units + P.grid;
+    P.slots = 2 * P.grid;
   } else {
     P.row_tiles = (P.rows + kSimtRowTile - 1) / kSimtRowTile;
     const int max_tiles = (a.max_pages_per_seq * a.page_size + kSimtKeyTile - 1) / kSimtKeyTile;
@@ -147,8 +147,10 @@ AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sm
     P.slot_rows = kSimtRowTile;
     P.slots = P.nsplit > 1 ? units * P.nsplit : 0;
   }
+  // (room for the CUDA cores' tickets on either path: they must stay zero)
   P.tickets = base;
-  P.partial_o = ws_round(P.tickets + sizeof(uint32_t) * units);
+  P.partial_o = ws_round(P.tickets + sizeof(uint32_t) * a.batch * a.num_kv_heads *
+                                            static_cast<size_t>((P.rows + kSimtRowTile - 1) / kSimtRowTile));
   P.partial_ml = ws_round(P.partial_o + static_cast<size_t>(P.slots) * P.slot_rows * a.head_dim * 4);
   P.split_notes = ws_round(P.partial_ml + static_cast<size_t>(P.slots) * P.slot_rows * sizeof(float2));
   P.end = ws_round(P.split_notes + 2 * sizeof(int4) * P.splits);

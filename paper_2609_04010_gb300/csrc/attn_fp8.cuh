@@ -13,7 +13,7 @@ struct AttnFp8Params : AttnParams {
   const float* kv_scale;  // [num_pages][Hkv][2]
   int4* splits;           // [P.splits][2]: units to merge (tensor-core kernels)
   int split_by_unit;      // a place for each unit in it, else for each block
-  int num_slots;          // partial results
+  int blocks;             // of the tensor-core kernels' grid
 };
 
 inline AttnFp8Params make_attn_fp8_params(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws) {
@@ -46,7 +46,7 @@ inline AttnFp8Params make_attn_fp8_params(const spec_attn_fp8_args_t& a, const A
   p.tickets = reinterpret_cast<uint32_t*>(ws + P.tickets);
   p.splits = reinterpret_cast<int4*>(ws + P.split_notes);
   p.split_by_unit = P.splits < P.grid;
-  p.num_slots = static_cast<int>(P.slots);
+  p.blocks = P.grid;
   p.partial_o = reinterpret_cast<float*>(ws + P.partial_o);
   p.partial_ml = reinterpret_cast<float2*>(ws + P.partial_ml);
   p.tree_mask = a.tree_mask;
@@ -69,26 +69,26 @@ __device__ __forceinline__ void write_fp8_lse(const AttnParams& p, int b, int g,
   p.lse[(static_cast<int64_t>(b) * p.gamma + j) * p.hq + h] = fp8_lse(m, l);
 }
 
-// Merges and writes 8 columns (from 8 * c8) of row `row` of KV head g, whose parts are row
-// `hr` of the slots [slot0, slot0 + nslots). A slot's outputs are [row][D], or with BY_COLUMNS
+// Merges and writes 8 columns (from 8 * c8) of row `row` of KV head g, whose n parts are row
+// `hr` of the slots slot_of(0 .. n - 1). A slot's outputs are [row][D], or with BY_COLUMNS
 // [D / 4][row][4]. The loads of up to four slots are in flight together.
-template <int D, bool BY_COLUMNS>
-__device__ __forceinline__ void merge_fp8_item(const AttnParams& p, int b, int g, int row, int64_t slot0, int nslots,
+template <int D, bool BY_COLUMNS, typename SlotOf>
+__device__ __forceinline__ void merge_fp8_item(const AttnParams& p, int b, int g, int row, SlotOf slot_of, int n,
                                                int hr, int c8) {
   constexpr int SB = 4;
   float M = -INFINITY, L = 0.f, acc[8];
   bool bad = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  for (int s0 = 0; s0 < nslots; s0 += SB) {
+  for (int s0 = 0; s0 < n; s0 += SB) {
     float2 ml[SB];
     float4 lo[SB], hi[SB];
 #pragma unroll
     for (int i = 0; i < SB; ++i) {
       ml[i] = make_float2(-INFINITY, 0.f);
       lo[i] = hi[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (s0 + i < nslots) {
-        const int64_t first = (slot0 + s0 + i) * p.slot_rows;
+      if (s0 + i < n) {
+        const int64_t first = static_cast<int64_t>(slot_of(s0 + i)) * p.slot_rows;
         const float4* src = reinterpret_cast<const float4*>(p.partial_o) + first * (D / 4) +
                             (BY_COLUMNS ? 2 * c8 * p.slot_rows + hr : hr * (D / 4) + 2 * c8);
         ml[i] = __ldcg(&p.partial_ml[first + hr]);

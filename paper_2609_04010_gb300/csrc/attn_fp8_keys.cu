@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       wait(flag_bar(seg_no % kFlagRing), (seg_no / kFlagRing) & 1);
       const bool bad = (seg_flag[seg_no % kFlagRing] | seg_flag[kFlagRing + seg_no % kFlagRing]) != 0;
       const bool whole = c.tile0 == 0 && c.ntile == c.unit_tiles;
-      const int64_t slot = c.u + w.cta;
+      const int64_t slot = part_slot(w.cta, c.tile0 == 0);
       if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
       const int nrows = real_rows(c);
       bar_sync(sbar, nthr);

@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float inv = whole ? fp8_inv(L) : (L <= 0.f ? 0.f : 1.f);
         const int head = (c.g * HP + kvh) * p.group + ur - j * p.group;
         const int64_t out_at = (static_cast<int64_t>(c.b) * p.gamma + j) * p.hq + head;
-        const int64_t part_at = (c.u + w.cta) * p.slot_rows + h * sub_rows + row;
+        const int64_t slot = part_slot(w.cta, c.tile0 == 0), part_at = slot * p.slot_rows + h * sub_rows + row;
         if (real && ch == 0) {
           if (!whole) p.partial_ml[part_at] = make_float2(m, L);
           else if (p.lse) p.lse[out_at] = fp8_lse(m, L);
@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               dst[i] = make_uint4(v[0], v[1], v[2], v[3]);
             }
           } else {
-            float4* dst = reinterpret_cast<float4*>(p.partial_o) + (c.u + w.cta) * p.slot_rows * (D / 4) +
+            float4* dst = reinterpret_cast<float4*>(p.partial_o) + slot * p.slot_rows * (D / 4) +
                           static_cast<int64_t>(d0 / 4) * p.slot_rows + h * sub_rows + row;
 #pragma unroll
             for (int i = 0; i < 8; ++i) dst[i * p.slot_rows] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);

@@ -201,7 +201,8 @@ __global__ void __launch_bounds__(NT) attn_fp8_simt_kernel(AttnFp8Params p) {
   if (!sm.last) return;
   __threadfence();
   for (int i = tid; i < nrows * (D / 8); i += NT)
-    merge_fp8_item<D, false>(p, b, g, row0 + i / (D / 8), unit * p.nsplit, p.nsplit, i / (D / 8), i % (D / 8));
+    merge_fp8_item<D, false>(p, b, g, row0 + i / (D / 8), [&](int s) { return unit * p.nsplit + s; }, p.nsplit, i / (D / 8),
+                             i % (D / 8));
 }
 
 template <int D>

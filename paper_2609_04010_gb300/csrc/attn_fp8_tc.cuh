@@ -164,6 +164,10 @@ __device__ __forceinline__ Seg find(int64_t at, const WorkList& w, const AttnPar
   return s;
 }
 
+// Where block `cta` keeps its part of a split unit: the part that starts the unit is its last
+// segment, one that goes on with a unit its first.
+__device__ __forceinline__ int part_slot(int cta, bool starts) { return 2 * cta + (starts ? 1 : 0); }
+
 // What merge_fp8_kernel is to join: units split between blocks, noted by the block with their
 // last tiles. With at most as many units as blocks each unit has a place; otherwise each
 // block, because only its first segment can end a split unit, and clear_split cleans it first.
@@ -176,7 +180,7 @@ __device__ __forceinline__ void note_split(const AttnFp8Params& p, const Seg& s,
   const int first = split ? owner_of(s.unit_start, w.total, w.ctas) : 0, row0 = s.rt * tile_rows;
   int4* e = p.splits + 2 * (p.split_by_unit ? s.u : blockIdx.x);
   e[0] = make_int4(s.b, s.g, row0, min(tile_rows, p.rows - row0));
-  e[1] = make_int4(static_cast<int>(s.u + first), split ? w.cta - first + 1 : 0, 0, 0);
+  e[1] = make_int4(first, split ? w.cta - first + 1 : 0, 0, 0);
 }
 
 // Joins the parts of split units: grid (chunks of a unit's outputs, places of units). A warp
@@ -189,13 +193,14 @@ __global__ void __launch_bounds__(kMergeThreads) merge_fp8_kernel(AttnFp8Params 
   pdl_wait_prior();
   const int4 a = __ldcg(p.splits + 2 * blockIdx.y), b = __ldcg(p.splits + 2 * blockIdx.y + 1);
   // (after a timeout a place may hold anything)
-  if (b.y <= 0 || b.x < 0 || b.y > p.num_slots - b.x || a.x < 0 || a.x >= p.batch || a.y < 0 || a.y >= p.hunits ||
+  if (b.y <= 0 || b.x < 0 || b.y > p.blocks - b.x || a.x < 0 || a.x >= p.batch || a.y < 0 || a.y >= p.hunits ||
       a.z < 0 || a.w < 0 || a.w > p.slot_rows / HP || a.w > p.rows - a.z)
     return;
   const int warp = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int hr = warp / (D / 32) * 8 + (lane & 7), c8 = warp % (D / 32) * 4 + (lane >> 3);
   if (hr < HP * a.w)
-    merge_fp8_item<D, BY_COLUMNS>(p, a.x, a.y * HP + hr / a.w, a.z + hr % a.w, b.x, b.y, hr, c8);
+    merge_fp8_item<D, BY_COLUMNS>(p, a.x, a.y * HP + hr / a.w, a.z + hr % a.w,
+                                  [&](int i) { return part_slot(b.x + i, i == 0); }, b.y, hr, c8);
 }
 
 template <int D, int HP, bool BY_COLUMNS>

@@ -117,6 +117,14 @@ def test_attention_workspace(lib):
     assert lib.spec_verify_attention_fp8(ctypes.byref(a), OK_ADDRESS + 128, 1 << 40, None) == 1
 
 
+def test_attention_workspace_does_not_grow_with_the_batch(lib):
+    """On the tensor cores only units that are split between blocks have partial results: two a
+    block, of 64 rows of two heads here (fp32 outputs and 8 bytes more), on up to 256 SMs."""
+    a = attn(batch=100000, gamma=16, num_q_heads=32, num_kv_heads=8, head_dim=128)
+    counters = 100000 * 8 * 4 * 4  # the other path's
+    assert lib.spec_attn_fp8_workspace_size(ctypes.byref(a)) <= 2 * 256 * 128 * (128 * 4 + 8) + counters + 65536
+
+
 @pytest.mark.parametrize("bad,code", [
     (dict(batch=0), 1), (dict(gamma=0), 1), (dict(vocab=0), 1), (dict(logits_dtype=2), 1),
     (dict(block_shift=2), 1), (dict(max_history=-1), 1), (dict(max_bias=-1), 1), (dict(logits=None), 1),
