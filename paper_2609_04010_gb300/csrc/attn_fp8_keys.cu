@@ -97,8 +97,7 @@ struct Cfg {
 // ---------------------------------------------------------------------------------
 template <int N>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* r) {
-  if constexpr (N == 32) tmem_ld32(taddr, r);
-  else if constexpr (N == 16) tmem_ld16(taddr, r);
+  if constexpr (N == 16) tmem_ld16(taddr, r);
   else tmem_ld8(taddr, r);
 }
 // Named barrier of the four softmax warps that share a set of rows; or-reduces `v`.
@@ -495,18 +494,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(s_free(h, sb));
         if (k > 0) wait(pv_done(h), (x - 1) & 1);  // the last products have read P
-        // weights, their sums, and their two terms into shared memory, 16 (8) rows at a time
-        constexpr int CB = NC >= 16 ? 16 : 8;
+        // weights, their sums, and their two terms into shared memory
+        {
+          uint32_t w1[NC / 4], w2[NC / 4];
 #pragma unroll
-        for (int cb = 0; cb < NC; cb += CB) {
-          uint32_t w1[CB / 4], w2[CB / 4];
-#pragma unroll
-          for (int c = 0; c < CB; c += 4) {
+          for (int c = 0; c < NC; c += 4) {
             float pr[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              pr[i] = ex2(e[cb + c + i]);
-              l[cb + c + i] = fmaf(pr[i], sc.z, l[cb + c + i]);
+              pr[i] = ex2(e[c + i]);
+              l[c + i] = fmaf(pr[i], sc.z, l[c + i]);
             }
             split_e4m3x4<true>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
           }
