@@ -2,30 +2,33 @@
 // keys on the MMA's M side (spec_verify_attention_fp8, SPEC_ATTN_TENSOR_CORES, KV groups of few
 // rows).
 //
-// Both products run in e4m3 straight from the cache's bytes, which land in shared memory by
+// Both products run in 8 bits straight from the cache's bytes, which land in shared memory by
 // TMA in the layout that the MMAs read; nothing is decoded on the way. They are transposed,
 // with the 128 keys (or the D dims) of a tile on the MMA's M side, so that the query rows are
 // its N side and a group of few rows pays for few:
 //   S^T[key][row]  = K8[key][:] . Q8[row][:]          (M = 128 keys, N = rows, K = D)
-//   O^T[dim][row] += sum_key V8[key][dim] P8[key][row] (M = D, N = 2 * rows, K = 128 keys)
-// What is exact in the cache must not be lost on the other side, so the bf16 queries and the
-// fp32 weights enter as sums of two e4m3 terms (x1 = e4m3(x), x2 = e4m3(x - x1)): for a
-// query that is exact to 2^-18 of its group's largest element, for a weight to 2^-8 of
-// itself. Both terms of Q accumulate into the same S; those of P are the first and the
-// second half of N and are added when a unit ends.
+//   O^T[dim][row] += sum_key V8[key][dim] P8[key][row] (M = D, N = 3 * rows, K = 128 keys)
+// What is exact in the cache must not be lost on the other side. A bf16 query enters as the sum
+// of two e4m3 terms (x1 = e4m3(x), x2 = e4m3(x - x1)), exact to 2^-18 of its group's largest
+// element. A weight enters as the sum of three e5m2 terms (split_weights), which is bf16's
+// precision, and for every weight that counts: where one key has most of a row's weight, the
+// rest of the output is the sum of thousands of weights below 2^-15 of the largest. Two e4m3
+// terms, whose smallest step was 2^-13 beside a largest of 2^2, lost all of them (32,768 keys, one
+// with nine tenths of the weight: off by 0.36 of the output's norm, now 0.002). Both terms of Q
+// accumulate into the same S; those of P are thirds of N and are added when a unit ends.
 //
 // With sk, sv the scales of a key's page, m_r the row's reference and the weights
 //   P = 2^(s + log2(sv) - m_r),  s = sk * S^T * softmax_scale * log2(e),
 // O^T accumulates the weighted values with their scales, and sum P / sv is the softmax sum.
-// m_r is chosen so that 4 <= the row's largest P <= 256 and rises only when P would pass 256
-// (e4m3 ends at 448), which after a unit's first tile is rare. The second term of P is kept
-// times 16, which puts its smallest step at 2^-13.
+// m_r is chosen so that 2^9 <= the row's largest P <= 2^15 and rises only when P would pass 2^15
+// (e5m2 ends at 1.75 * 2^15), which after a unit's first tile is rare. The third term of P is kept
+// times 32, which puts its smallest step at 2^-21, 2^-30 of the row's largest P.
 //
 // A block serves two sub-units of at most 32 query rows: two adjacent KV heads (HP = 2, one
 // box brings K and V of both: 8 KB with 16-token pages and D = 128), or two halves of one KV
 // head's rows (HP = 1). Shared memory beyond Q and P is stages; P's rows are as narrow as its
-// weights (32 or 64 bytes a key), which with 16 rows a sub-unit leaves room for a third stage of
-// two heads (batch 32 decoding: 103 us with two). Keys and values in stages of their own, freed
+// weights allow (64 or 128 bytes a key), which with 16 rows a sub-unit leaves room for a third
+// stage of two heads (batch 32 decoding: 103 us with two). Keys and values in stages of their own, freed
 // earlier but copied in boxes of half the size, took 99. Warp roles (persistent, one block per
 // SM):
 //   warps 16,19  producers: page ids and scales 32 pages ahead, one TMA box per page, each
@@ -61,19 +64,19 @@ struct Cfg {
   static constexpr uint32_t ATOM = Stage<D, HP>::ATOM, SG = Stage<D, HP>::SG, STAGE = Stage<D, HP>::BYTES;
   static constexpr int SB = 2;                             // S buffers per sub-unit
   static constexpr uint32_t Q_TERM = NR * D;               // one term of one sub-unit's Q
-  static constexpr uint32_t PW = 2 * NR;                   // a key's weights: first terms, second terms
+  static constexpr uint32_t PW = 4 * NR;                   // a key's weights: first, second, third terms, unused
   static constexpr uint32_t P_BUF = TK * PW;               // [key][PW], swizzled by its width
-  static constexpr int NST = (208 * 1024 - NH * (P_BUF + 2 * Q_TERM)) / STAGE;  // D = 128, HP = 2: 3 or 2
+  static constexpr int NST = ((NR == 16 ? 216 : 208) * 1024 - NH * (P_BUF + 2 * Q_TERM)) / STAGE;  // D = 128, HP = 2: 3 or 2
   static constexpr uint32_t OFF_STAGE = 0;
   static constexpr uint32_t OFF_P = OFF_STAGE + NST * STAGE;
   static constexpr uint32_t OFF_Q = OFF_P + NH * P_BUF;
   static constexpr uint32_t OFF_SCL = OFF_Q + NH * 2 * Q_TERM;      // float4 [NST][8 pages][HP]
   static constexpr uint32_t OFF_NAN = OFF_SCL + NST * 8 * HP * 16;  // uint64 [NH][D]: NaN block values
   // of the current and the next segment: the block keys each row sees, the rows that see
-  // each block key, the rows' references
+  // each block key (a bit each), the rows' references
   static constexpr uint32_t OFF_VIS = OFF_NAN + NH * D * 8;          // uint64 [2][NH][NR]
-  static constexpr uint32_t OFF_SEEN = OFF_VIS + 2 * NH * NR * 8;    // uint32 [2][NH][2][64]
-  static constexpr uint32_t OFF_M = OFF_SEEN + 2 * NH * 2 * 64 * 4;  // float [2][NH][NR]
+  static constexpr uint32_t OFF_SEEN = OFF_VIS + 2 * NH * NR * 8;    // uint32 [2][NH][64]
+  static constexpr uint32_t OFF_M = OFF_SEEN + 2 * NH * 64 * 4;      // float [2][NH][NR]
   static constexpr uint32_t OFF_X = OFF_M + 2 * NH * NR * 4;         // float [NH][4][NR]: cross-quadrant
   static constexpr uint32_t OFF_ROW = OFF_X + NH * 4 * NR * 4;       // int64 [NH][NR]: rows' outputs
   static constexpr uint32_t OFF_INV = OFF_ROW + NH * NR * 8;         // float [NH][NR]: their factors
@@ -86,9 +89,9 @@ struct Cfg {
   static constexpr uint32_t OFF_QMAX = OFF_FLAG + 8 * kFlagRing;       // uint32 [NH][8]
   static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 32;    // int [batch + 1]
   static constexpr uint32_t S_COL = 0;                      // [NH][SB][NR]
-  static constexpr uint32_t O_COL = NH * SB * NR;           // [NH][first, second terms][NR]
-  static constexpr uint32_t TMEM_COLS = NH * (SB + 2) * NR;
-  static_assert(TMEM_COLS <= 512, "TMEM holds 512 columns");
+  static constexpr uint32_t O_COL = NH * SB * NR;           // [NH][first, second, third terms][NR]
+  static constexpr uint32_t TMEM_COLS = NR == 16 ? 256 : 512;
+  static_assert(NH * (SB + 3) * NR <= TMEM_COLS, "a power of two of columns");
   static constexpr size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
 };
 
@@ -208,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         seg_flag, abort_flag);
   } else if (warp == kSoftWarps + 1) {
     // ============================ S^T = K Q^T ============================
-    constexpr uint32_t kIdesc = idesc_e4m3(128, NR, false, false);
+    constexpr uint32_t kIdesc = idesc_f8(128, NR, false, false);
     uint32_t it = 0, seg_no = 0;
     bool ok = true, issued = false;
     for (Seg s = find(w.t0, w, p); s.ntile > 0 && ok; ++seg_no) {
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int t = 0; t < 2; ++t)
 #pragma unroll
               for (int kk = 0; kk < D / 32; ++kk)
-                mma_e4m3(tmem + C::S_COL + (h * SB + sb) * NR, desc_rows<D>(kb + kk * 32u, 16, C::SG),
+                mma_f8(tmem + C::S_COL + (h * SB + sb) * NR, desc_rows<D>(kb + kk * 32u, 16, C::SG),
                          desc_rows<D>(sbase + C::OFF_Q + (h * 2 + t) * C::Q_TERM + kk * 32u, 16, C::ATOM), kIdesc,
                          t > 0 || kk > 0);
             mma_commit(s_full(h, sb));
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == kSoftWarps + 2) {
     // ============================ O^T += V^T P^T ============================
-    constexpr uint32_t kIdesc = idesc_e4m3(128, 2 * NR, true, true);
+    constexpr uint32_t kIdesc = idesc_f8(128, 3 * NR, true, true, false, true);
     uint32_t it = 0;
     bool ok = true, issued = false;
     for (Seg s = find(w.t0, w, p); s.ntile > 0 && ok;) {
@@ -270,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t pa = sbase + C::OFF_P + h * C::P_BUF;
 #pragma unroll
             for (int kk = 0; kk < TK / 32; ++kk)
-              mma_e4m3(tmem + C::O_COL + h * 2 * NR, desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG),
+              mma_f8(tmem + C::O_COL + h * 3 * NR, desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG),
                        desc_rows<C::PW>(pa + kk * 32u * C::PW, 0, 8 * C::PW), kIdesc, k > 0 || kk > 0);
             mma_commit(pv_done(h));
             if (h == NH - 1) mma_commit(empty(st));
@@ -297,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int nthr = nsoft * 32, stid = threadIdx.x & 255;  // threads of the sub-unit
     const int swarp = warp & 7, kvh = HP == 2 ? h : 0;
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
-    const uint32_t o_col = lane_base + C::O_COL + h * 2 * NR + ch * NC;
+    const uint32_t o_col = lane_base + C::O_COL + h * 3 * NR + ch * NC;
     const int pg = (q4 * 32 + lane) / p.page_size;  // this lane's page of a tile
     float* xch = reinterpret_cast<float*>(smem + C::OFF_X) + h * 4 * NR;  // [4][NR]
     uint32_t* qmax = reinterpret_cast<uint32_t*>(smem + C::OFF_QMAX) + h * 8;
@@ -314,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto vis_of = [&](uint32_t par) {
       return reinterpret_cast<unsigned long long*>(smem + C::OFF_VIS) + (par * NH + h) * NR;
     };
-    auto seen_of = [&](uint32_t par) { return reinterpret_cast<uint32_t*>(smem + C::OFF_SEEN) + (par * NH + h) * 128; };
+    auto seen_of = [&](uint32_t par) { return reinterpret_cast<uint32_t*>(smem + C::OFF_SEEN) + (par * NH + h) * 64; };
     auto mref_of = [&](uint32_t par) { return reinterpret_cast<float*>(smem + C::OFF_M) + (par * NH + h) * NR; };
     // the unit row of row r, and how many are real
     auto unit_row = [&](const Seg& sg, int r) { return sg.rt * tile_rows + (HP == 2 ? 0 : h * sub_rows) + r; };
@@ -365,9 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mx = __reduce_max_sync(0xffffffffu, mx);
       if (lane == 0) qmax[swarp] = mx;
       bar_sync(sbar, nthr);
-      for (int i = swarp; i < nsoft / 4 * 64; i += nsoft) {  // lane = row of group i / 64
-        const bool v = lane < NC && (vis[(i >> 6) * NC + (lane & (NC - 1))] >> (i & 63) & 1);
-        const uint32_t m = __ballot_sync(0xffffffffu, v);
+      for (int i = swarp; i < 64; i += nsoft) {  // lane = row
+        const uint32_t m = __ballot_sync(0xffffffffu, lane < NR && (vis[lane % NR] >> i & 1));
         if (lane == 0) seen_of(par)[i] = m;
       }
       mx = 0;
@@ -389,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             v[d] = __uint_as_float((d & 1) ? w[d >> 1] & 0xffff0000u : w[d >> 1] << 16) * inv;
             if (!(fabsf(v[d]) < INFINITY)) v[d] = __int_as_float(0x7fc00000);  // an infinite query is NaN
           }
-          split_e4m3x4<false>(v[0], v[1], v[2], v[3], t1w[c], t2w[c]);
+          split_e4m3x4(v[0], v[1], v[2], v[3], t1w[c], t2w[c]);
         }
         const int ph = D == 128 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3);
         unsigned char* dst = smem + C::OFF_Q + h * 2 * C::Q_TERM + r * D + ph * 16;
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float4 sc = scl[(st * 8 + pg) * HP + kvh];
         const float ks = sc.x * qf;
         uint32_t seen = ~0u;
-        if (masked && rel >= 0) seen = rel < 64 ? seen_of(par)[ch * 64 + rel] : 0u;
+        if (masked && rel >= 0) seen = rel < 64 ? seen_of(par)[rel] >> (ch * NC) : 0u;
         // e = log2 of the key's weight and value scale for each row, over the row's
         // reference; hidden keys have none
         float e[NC];
@@ -443,9 +445,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         float top = -INFINITY;
 #pragma unroll
         for (int c = 0; c < NC; ++c) top = fmaxf(top, e[c]);
-        if (group_any(gbar, top > 8.f)) {
-          // Some weight would pass 2^8: raise the references, so that each row's largest
-          // weight so far becomes 2^2 where it was more.
+        if (group_any(gbar, top > 15.f)) {
+          // Some weight would pass 2^15: raise the references, so that each row's largest
+          // weight so far becomes 2^9 where it was more.
           float mx = -INFINITY;
 #pragma unroll 1
           for (int c8 = 0; c8 < NC; c8 += 8) {
@@ -462,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane < NC) xc[q4 * NR] = mx;
           bar_sync(gbar, 128);
           const float old = mr[lane % NC];
-          const float now = fmaxf(old, fmaxf(fmaxf(xc[0], xc[NR]), fmaxf(xc[2 * NR], xc[3 * NR])) - 2.f);
+          const float now = fmaxf(old, fmaxf(fmaxf(xc[0], xc[NR]), fmaxf(xc[2 * NR], xc[3 * NR])) - 9.f);
           const float alpha = ex2(old - now);
           bar_sync(gbar, 128);
           if (q4 == 0 && lane < NC) mr[lane] = now;
@@ -470,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             wait(pv_done(h), (x - 1) & 1);
             tc_fence_after();
 #pragma unroll 1
-            for (int c8 = 0; c8 < 2 * NC; c8 += 8) {
+            for (int c8 = 0; c8 < 3 * NC; c8 += 8) {
               uint32_t t8[8];
               const uint32_t col = o_col + (c8 / NC) * NR + c8 % NC;
               tmem_ld8(col, t8);
@@ -494,9 +496,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(s_free(h, sb));
         if (k > 0) wait(pv_done(h), (x - 1) & 1);  // the last products have read P
-        // weights, their sums, and their two terms into shared memory
+        // weights, their sums, and their three terms into shared memory
         {
-          uint32_t w1[NC / 4], w2[NC / 4];
+          uint32_t w1[NC / 4], w2[NC / 4], w3[NC / 4];
 #pragma unroll
           for (int c = 0; c < NC; c += 4) {
             float pr[4];
@@ -505,16 +507,18 @@ __global__ void __launch_bounds__(kThreads, 1)
               pr[i] = ex2(e[c + i]);
               l[c + i] = fmaf(pr[i], sc.z, l[c + i]);
             }
-            split_e4m3x4<true>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
+            split_weights<true>(pr, w1[c / 4], w2[c / 4], w3[c / 4]);
           }
           if constexpr (NR == 32) {  // this warp's rows are one 16-byte chunk of each term
-            const int sw = lane >> 1 & 3;
+            const int sw = lane & 7;
             *reinterpret_cast<uint4*>(pbuf + ((ch ^ sw) << 4)) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
             *reinterpret_cast<uint4*>(pbuf + (((ch + 2) ^ sw) << 4)) = make_uint4(w2[0], w2[1], w2[2], w2[3]);
+            *reinterpret_cast<uint4*>(pbuf + (((ch + 4) ^ sw) << 4)) = make_uint4(w3[0], w3[1], w3[2], w3[3]);
           } else {  // half a chunk
-            const int sw = lane >> 2 & 1;
+            const int sw = lane >> 1 & 3;
             *reinterpret_cast<uint2*>(pbuf + (sw << 4) + ch * 8) = make_uint2(w1[0], w1[1]);
             *reinterpret_cast<uint2*>(pbuf + ((1 ^ sw) << 4) + ch * 8) = make_uint2(w2[0], w2[1]);
+            *reinterpret_cast<uint2*>(pbuf + ((2 ^ sw) << 4) + ch * 8) = make_uint2(w3[0], w3[1]);
           }
         }
         fence_async_smem();
@@ -574,16 +578,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int nreal = min(NC, nrows - ch * NC);  // of this warp's rows
 #pragma unroll 1
       for (int c8 = 0; c8 < nreal; c8 += 8) {
-        uint32_t a[8], b[8];
+        uint32_t a[8], b[8], t[8];
         tmem_ld8(o_col + c8, a);
         tmem_ld8(o_col + NR + c8, b);
+        tmem_ld8(o_col + 2 * NR + c8, t);
         tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if (c8 + i >= nreal || d >= D) continue;
           const int r = ch * NC + c8 + i;
           const float inv = row_inv[r];
-          float o = fmaf(__uint_as_float(b[i]), 0.0625f, __uint_as_float(a[i])) * inv;
+          float o = (fmaf(__uint_as_float(t[i]), 0.03125f, __uint_as_float(b[i])) + __uint_as_float(a[i])) * inv;
           if (inv == 0.f) o = 0.f;
           if (has_nan && inv != 0.f && (nanv[h * D + d] & vis_of(par)[r])) o = __int_as_float(0x7fc00000);
           if (whole) static_cast<__nv_bfloat16*>(p.out)[row_at[r] + d] = __float2bfloat16_rn(o);

@@ -4,8 +4,8 @@
 //
 //   S[row][key] = Q8[row][:] . K8[key][:]          (M = 128 rows, N = 128 keys, K = D)
 //   O[row][dim] += sum_key P8[row][key] V8[key][dim] (M = 128 rows, N = D, K = 128 keys)
-// The arithmetic is attn_fp8_keys.cu's: e4m3 operands straight from the cache, queries and
-// weights as sums of two e4m3 terms, weights P = 2^(s + log2(sv) - m) against a reference m
+// The arithmetic is attn_fp8_keys.cu's: e4m3 operands straight from the cache, queries as sums
+// of two e4m3 terms, weights as sums of three e5m2 terms, weights P = 2^(s + log2(sv) - m) against a reference m
 // per row, sum P / sv. Here two threads share a row, each with half of a tile's keys: maximum,
 // sum and reference are their own registers, the page constants are the same for all lanes,
 // and only the two warps of 32 rows wait for each other (one thread a row: 162 us against 115
@@ -13,12 +13,14 @@
 // M side would be padding and attn_fp8_keys.cu is faster.
 //
 // A block serves two sub-units of at most 128 query rows: two adjacent KV heads (HP = 2) or
-// two halves of one KV head's rows. Both terms of P live in TMEM over the columns of S that
-// they came from (32 keys of S are 32 columns, of P 8 + 8), so that shared memory holds Q and
+// two halves of one KV head's rows. The terms of P live in TMEM over the columns of S that
+// they came from (32 keys of S are 32 columns, of P 8 + 8 + 8), so that shared memory holds Q and
 // K/V stages only; S is computed again once the products have read P. While one sub-unit is
 // at its softmax, the tensor core works for the other. m is set so that a row's largest P is
-// 2^4.5 to 2^5.5 and raised when a P would pass 2^8 (both terms add up in one accumulator, so
-// the second one's smallest step is 2^-9; 2^-14 of a row's largest weight). m is a whole number,
+// 2^11.5 to 2^12.5 and raised when a P would pass 2^15 (the terms add up in one accumulator, so
+// the third one's smallest step is 2^-16: a P is off by 2^-28 of the row's largest at most). The
+// third product costs 0.14 us a tile (batch 4, 32,768 keys: 164 us; 153 with two e4m3 terms, which
+// lost the weights below 2^-14 of the largest: up to 0.75 of an output). m is a whole number,
 // so that log2(sv) - m is exact with power-of-two scales. Hidden scores are set to -inf in
 // TMEM, before the two passes over a tile (the maximum, the weights), which then know no masks.
 // Warp roles (persistent, one block per SM):
@@ -72,7 +74,7 @@ struct Cfg {
 };
 
 // The same with A in tensor memory (M rows on the lanes, four bytes of K per column).
-__device__ __forceinline__ void mma_e4m3_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+__device__ __forceinline__ void mma_f8_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                                             uint32_t accumulate) {
   asm volatile(
       "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ============================ products ============================
     // One thread's products run in the order of their issue: the next tile's S follows at once
     // on the O += P V that reads its columns.
-    constexpr uint32_t kIdescS = idesc_e4m3(MR, TK, false, false), kIdescO = idesc_e4m3(MR, D, false, true);
+    constexpr uint32_t kIdescS = idesc_f8(MR, TK, false, false), kIdescO = idesc_f8(MR, D, false, true, true);
     uint32_t it = 0, seg_no = 0;
     bool ok = true, issued = false;
     auto stage_full = [&](uint32_t x) { return mbar_wait(full(x % NST), (x / NST) & 1, abort_flag, p.status); };
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int kk = 0; kk < D / 32; ++kk)
-            mma_e4m3(tmem + C::S_COL + h * TK,
+            mma_f8(tmem + C::S_COL + h * TK,
                      desc_rows<D>(sbase + C::OFF_Q + (h * 2 + t) * C::Q_TERM + kk * 32u, 16, C::ATOM),
                      desc_rows<D>(kb + kk * 32u, 16, C::SG), kIdescS, t > 0 || kk > 0);
         mma_commit(s_full(h));
@@ -202,8 +204,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int kk = 0; kk < TK / 32; ++kk)
 #pragma unroll
-              for (int t = 0; t < 2; ++t)
-                mma_e4m3_ta(tmem + C::O_COL + h * D, tmem + C::S_COL + h * TK + kk * 32u + t * 8u,
+              for (int t = 0; t < 3; ++t)
+                mma_f8_ta(tmem + C::O_COL + h * D, tmem + C::S_COL + h * TK + kk * 32u + t * 8u,
                             desc_rows<D>(vb + kk * 4u * C::SG, 0, C::SG), kIdescO, k > 0 || kk > 0 || t > 0);
             mma_commit(pv_done(h));
             if (h == NH - 1) mma_commit(empty(st));
@@ -295,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t t1w[4], t2w[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c)
-            split_e4m3x4<false>(__uint_as_float(v[2 * c] << 16) * inv, __uint_as_float(v[2 * c] & 0xffff0000u) * inv,
+            split_e4m3x4(__uint_as_float(v[2 * c] << 16) * inv, __uint_as_float(v[2 * c] & 0xffff0000u) * inv,
                                 __uint_as_float(v[2 * c + 1] << 16) * inv,
                                 __uint_as_float(v[2 * c + 1] & 0xffff0000u) * inv, t1w[c], t2w[c]);
           const int lr = q0 * 32 + r;  // row of the MMA tile
@@ -373,12 +375,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               top = fmaxf(top, fmaf(t, slope(q.x), q.y));
             }
           }
-          // ---- raise the reference where a weight would pass 2^8 ----
-          if (pair_any(pbar, top > m + 8.f || (m == -INFINITY && top > -INFINITY))) {
+          // ---- raise the reference where a weight would pass 2^15 ----
+          if (pair_any(pbar, top > m + 15.f || (m == -INFINITY && top > -INFINITY))) {
             xch[ch * MR + row] = top;
             bar_sync(pbar, 64);
             top = fmaxf(xch[row], xch[MR + row]);
-            const float now = top > m + 8.f || m == -INFINITY ? fmaxf(m, rintf(top) - 5.f) : m;
+            const float now = top > m + 15.f || m == -INFINITY ? fmaxf(m, rintf(top) - 12.f) : m;
             const float alpha = m == -INFINITY ? 0.f : ex2(m - now);
             if (k > 0) {  // O holds every earlier tile before it is scaled
               wait(pv_done(h), (x - 1) & 1);
@@ -398,11 +400,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             m = now;
             bar_sync(pbar, 64);  // xch is read
           }
-          // ---- weights, their sum, and their two terms over the columns of S ----
+          // ---- weights, their sum, and their three terms over the columns of S ----
           const float msub = m == -INFINITY ? 0.f : m;
 #pragma unroll 1
           for (int c0 = ch * HK; c0 < ch * HK + HK; c0 += 32) {
-            uint32_t r[32], w1[8], w2[8];
+            uint32_t r[32], w[24];
             tmem_ld32(s_col + c0, r);
             float2 ab[2];  // of 16 keys each
             float inv_sv[2];
@@ -422,12 +424,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pr[i] = ex2(fmaf(__uint_as_float(r[c + i]), ab[g].x, ab[g].y));
                 sum += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-                split_e4m3x4<false>(pr[0], pr[1], pr[2], pr[3], w1[c / 4], w2[c / 4]);
+                split_weights<false>(pr, w[c / 4], w[8 + c / 4], w[16 + c / 4]);
               }
               l = fmaf(sum, inv_sv[g], l);
             }
-            tmem_st8(s_col + c0, w1);
-            tmem_st8(s_col + c0 + 8, w2);
+            tmem_st16(s_col + c0, w);
+            tmem_st8(s_col + c0 + 16, w + 16);
           }
           tmem_wait_st();
           tc_fence_before();

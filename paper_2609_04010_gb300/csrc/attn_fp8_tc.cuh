@@ -1,5 +1,5 @@
 // What the two tensor-core kernels of the attention over the 8-bit cache share: PTX wrappers
-// for e4m3 products, the staging of keys and values, the work list, and the end of a block.
+// for 8-bit products, the staging of keys and values, the work list, and the end of a block.
 #pragma once
 
 #include <cuda.h>  // CUtensorMap
@@ -36,7 +36,7 @@ __device__ __forceinline__ void tma_load_page8(uint32_t dst, const CUtensorMap* 
       "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(0), "r"(kind_head), "r"(0), "r"(bar)
       : "memory");
 }
-__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
                                          uint32_t accumulate) {
   asm volatile(
       "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
@@ -51,10 +51,11 @@ __device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t lbo, uint
          (static_cast<uint64_t>((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46) |
          (static_cast<uint64_t>(W == 128 ? 2 : W == 64 ? 4 : 6) << 61);
 }
-// Instruction descriptor, kind::f8f6f4: fp32 accumulator, e4m3 A and B.
-__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn, bool b_mn) {
-  return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-         (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+// Instruction descriptor, kind::f8f6f4: fp32 accumulator, A and B e4m3 or e5m2.
+__host__ __device__ constexpr uint32_t idesc_f8(int M, int N, bool a_mn, bool b_mn, bool a_e5m2 = false,
+                                                bool b_e5m2 = false) {
+  return (1u << 4) | ((a_e5m2 ? 1u : 0u) << 7) | ((b_e5m2 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) |
+         ((b_mn ? 1u : 0u) << 16) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -70,9 +71,7 @@ __device__ __forceinline__ void bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
-// The two e4m3 terms of four values, each packed in order from the low byte; UP: the second
-// terms times 16.
-template <bool UP>
+// The two e4m3 terms of four values, each packed in order from the low byte.
 __device__ __forceinline__ void split_e4m3x4(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
   uint32_t x, y;
   asm("{\n .reg .b16 p, q;\n .reg .b32 h, g;\n"
@@ -82,10 +81,32 @@ __device__ __forceinline__ void split_e4m3x4(float a, float b, float c, float d,
       " sub.f16x2 %1, %1, h;\n sub.f16x2 %2, %2, g;\n}"
       : "=&r"(hi), "=&r"(x), "=&r"(y)
       : "f"(a), "f"(b), "f"(c), "f"(d));
-  if constexpr (UP) asm("mul.f16x2 %0, %0, %2;\n mul.f16x2 %1, %1, %2;" : "+r"(x), "+r"(y) : "r"(0x4c004c00u));
   asm("{\n .reg .b16 r, s;\n cvt.rn.satfinite.e4m3x2.f16x2 r, %1;\n cvt.rn.satfinite.e4m3x2.f16x2 s, %2;\n"
       " mov.b32 %0, {r, s};\n}"
       : "=r"(lo)
+      : "r"(x), "r"(y));
+}
+
+// The three e5m2 terms of four weights in [0, 2^15], each packed in order from the low byte. A
+// weight is rounded to fp16, whose upper byte is an e5m2 number: that byte, the upper byte of
+// what is left of it, and what is left then, rounded, are the terms: 3 + 3 + 3 bits, off by at most
+// 2^-9 + 2^-11 of the weight. UP: the third terms times 32, so that their smallest step is 2^-21 of 1
+// instead of 2^-16 (they stay below 2^15).
+template <bool UP>
+__device__ __forceinline__ void split_weights(const float* p, uint32_t& w1, uint32_t& w2, uint32_t& w3) {
+  uint32_t x, y, r, s;
+  asm("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(x) : "f"(p[0]), "f"(p[1]));
+  asm("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(y) : "f"(p[2]), "f"(p[3]));
+  w1 = __byte_perm(x, y, 0x7531);
+  asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(x & 0xff00ff00u));
+  asm("sub.f16x2 %0, %1, %2;" : "=r"(s) : "r"(y), "r"(y & 0xff00ff00u));
+  w2 = __byte_perm(r, s, 0x7531);
+  asm("sub.f16x2 %0, %1, %2;" : "=r"(x) : "r"(r), "r"(r & 0xff00ff00u));
+  asm("sub.f16x2 %0, %1, %2;" : "=r"(y) : "r"(s), "r"(s & 0xff00ff00u));
+  if constexpr (UP) asm("mul.f16x2 %0, %0, %2;\n mul.f16x2 %1, %1, %2;" : "+r"(x), "+r"(y) : "r"(0x50005000u));
+  asm("{\n .reg .b16 p, q;\n cvt.rn.satfinite.e5m2x2.f16x2 p, %1;\n cvt.rn.satfinite.e5m2x2.f16x2 q, %2;\n"
+      " mov.b32 %0, {p, q};\n}"
+      : "=r"(w3)
       : "r"(x), "r"(y));
 }
 
