@@ -106,3 +106,33 @@ def test_one_key_dominates_split_units(path, G, Hq, H):
 @pytest.mark.parametrize("share", [0.99, 0.999])
 def test_one_key_has_nearly_all_the_weight(G, Hq, H, share):
     check(dominated(160, G, Hq, H, 128, 8192, share, 0.5, seed=G + 1), TENSOR_CORES, [0, 159])
+
+
+@pytest.mark.parametrize("path", [CUDA_CORES, TENSOR_CORES])
+@pytest.mark.parametrize("G,Hq,H", LAYOUTS)
+@pytest.mark.parametrize("apart", [8, 16, 20, 24])
+def test_value_scales_far_apart(path, G, Hq, H, apart):
+    """Every second page has a value scale 2^apart times the others', and values of 0 in half of
+    the dims, which the other pages alone fill. What enters the product of a key is its weight
+    times its page's value scale, so its error is at most 1.25 * 2^-9 of itself or 2^-28 of the
+    row's largest: |do| <= 1.25 * 2^-9 sum_t p_t |v_t| + 2^-28 * max_t (p_t sv_t) * sum_t |v8_t| +
+    2^-9 |o|, v8 the e4m3 values. All scores are 0."""
+    r = np.random.default_rng(apart)
+    n, P, D = 1500, 32, 128
+    pages = -(-n // P)
+    codes = ref.encode(r.standard_normal((pages, H, 2, P, D)) * 60 + 30)
+    scale = np.ones((pages, H, 2), np.float32)
+    scale[1::2, :, 1] = 2.0 ** -apart
+    codes[::2, :, 1, :, D // 2:] = 0
+    q = torch.zeros(2, G, Hq, D, dtype=torch.bfloat16)
+    from paper_2609_04010_gb300 import binding as b
+    o, _ = b.verify_attention_fp8(q.cuda(), torch.from_numpy(codes).cuda().view(torch.float8_e4m3fn),
+                                  torch.from_numpy(scale).cuda(), i32(np.broadcast_to(np.arange(pages), (2, pages))),
+                                  i32([n, n]), path=path)
+    for s in range(2):
+        ro, _, mass, _, _ = attention(q[s].double().numpy(), codes, scale, n)
+        seen = n - G + 1 + np.arange(G)[:, None, None]
+        v8 = np.abs(ref.decode(codes[:, :, 1])).transpose(1, 0, 2, 3).reshape(H, -1, D)[:, :n].sum(1)
+        tol = 1.25 * 2.0 ** -9 * mass + 2.0 ** -28 / seen * np.repeat(v8, Hq // H, 0)[None] + 2.0 ** -9 * np.abs(ro)
+        err = np.abs(o[s].float().cpu().numpy() - ro)
+        assert (err / tol).max() <= 1, (err / tol).max()
