@@ -33,7 +33,7 @@ struct SlotParams {
 struct SeqSlots {
   int32_t len;     // tokens held; -1: not served
   int32_t first;   // table entry of its first new page
-  int32_t before;  // pages taken by earlier sequences
+  int32_t before;  // pages that earlier sequences need (at most INT32_MAX)
 };
 
 struct Two {  // rows and pages, summed together
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   const spec_slot_args_t& a = p.a;
   int32_t* start = reinterpret_cast<int32_t*>(smem_raw);                // [batch + 1]
-  SeqSlots* seq = reinterpret_cast<SeqSlots*>(start + a.batch + 1);      // [batch]
+  SeqSlots* seq = reinterpret_cast<SeqSlots*>(start + a.batch + 1);      // [batch + 1]
   __shared__ Two sh[kSlotThreads / 32];
   __shared__ int s_last, s_taken;
   const int tid = threadIdx.x;
@@ -107,22 +107,23 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
       start[b] = static_cast<int32_t>(min(carry.rows + before.rows, static_cast<int64_t>(INT32_MAX)));
       const bool served = len >= 0 && (need == 0 || pages + need <= count0);
       if (served && need > 0) atomicMax(&s_taken, static_cast<int>(pages) + need);
-      seq[b] = {served ? len : -1, first, served && need > 0 ? static_cast<int32_t>(pages) : 0};
+      seq[b] = {served ? len : -1, first, static_cast<int32_t>(min(pages, static_cast<int64_t>(INT32_MAX)))};
     }
     carry.rows += all.rows;
     carry.pages += all.pages;
   }
-  if (tid == 0) start[a.batch] = static_cast<int32_t>(min(carry.rows, static_cast<int64_t>(INT32_MAX)));
+  if (tid == 0) {
+    start[a.batch] = static_cast<int32_t>(min(carry.rows, static_cast<int64_t>(INT32_MAX)));
+    seq[a.batch].before = static_cast<int32_t>(min(carry.pages, static_cast<int64_t>(INT32_MAX)));
+  }
   __syncthreads();
   const int total = start[a.batch];
 
-  // Four rows a thread, one search for their sequence; rows past max_rows only put their new
-  // pages into the table.
-  const int64_t rows_end = max(total, a.max_rows);
+  // Four rows a thread, one search for their sequence; a page's first token puts it into the table.
   const int64_t step = static_cast<int64_t>(gridDim.x) * kSlotThreads * 4;
   const bool wide = ((reinterpret_cast<uintptr_t>(a.slots) | reinterpret_cast<uintptr_t>(a.positions) |
                       reinterpret_cast<uintptr_t>(a.row_seq)) & 15u) == 0;
-  for (int64_t r0 = (static_cast<int64_t>(blockIdx.x) * kSlotThreads + tid) * 4; r0 < rows_end; r0 += step) {
+  for (int64_t r0 = (static_cast<int64_t>(blockIdx.x) * kSlotThreads + tid) * 4; r0 < a.max_rows; r0 += step) {
     int lo = 0;
     if (r0 < total) {
       int hi = a.batch;  // largest b with start[b] <= r0
@@ -169,6 +170,24 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
         if (a.positions) a.positions[r0 + e] = pos[e];
         if (a.row_seq) a.row_seq[r0 + e] = sq[e];
       }
+    }
+  }
+
+  // Pages whose first token is a row past max_rows, page by page: there may be many more such rows
+  // than pages, and behind a request of a wrong size their numbers end at INT32_MAX. Page i from
+  // the free list's top is that of the last sequence with before <= i, if it is served.
+  if (total > a.max_rows) {
+    const int pages_end = min(seq[a.batch].before, s_taken);
+    for (int64_t i = blockIdx.x * kSlotThreads + tid; i < pages_end; i += static_cast<int64_t>(gridDim.x) * kSlotThreads) {
+      int lo = 0, hi = a.batch;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (seq[mid].before <= i) lo = mid; else hi = mid;
+      }
+      const SeqSlots s = seq[lo];
+      const int64_t idx = s.first + (i - s.before);
+      if (s.len >= 0 && start[lo] + (idx * P - s.len) >= a.max_rows)
+        a.page_table[static_cast<int64_t>(lo) * MP + idx] = __ldg(a.free_pages + (count0 - 1 - i));
     }
   }
 
@@ -369,7 +388,7 @@ cudaError_t launch_append_d(const AppendParams& p, int page_size, cudaStream_t s
 
 }  // namespace
 
-size_t slot_smem(int batch) { return (batch + 1) * 4 + batch * sizeof(SeqSlots); }
+size_t slot_smem(int batch) { return (batch + 1) * (4 + sizeof(SeqSlots)); }
 
 cudaError_t launch_map_slots(const spec_slot_args_t& a, char* ws, cudaStream_t stream) {
   SlotParams p{a, reinterpret_cast<uint32_t*>(ws + kWsHeader)};
