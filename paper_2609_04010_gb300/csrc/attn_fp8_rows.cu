@@ -502,8 +502,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (h == 0 && stid == 0) note_split(p, c, w, tile_rows);
         tc_fence_before();
-        if (has_nan) {  // read by all; the next segment may set them
-          bar_sync(sbar, nthr);
+        // The notes are read by all; the next segment may set them. Every warp passes this barrier,
+        // because after a timeout nothing orders what they read of nan_flag.
+        bar_sync(sbar, nthr);
+        if (has_nan) {
           for (int i = stid; i < D; i += nthr) nanv[h * D + i] = 0ull;
           if (stid == 0) nan_flag[h] = 0;
         }
