@@ -819,6 +819,8 @@ def append_fp8_args(k, v, slots, kv_cache, kv_scale, status_ws=None) -> AppendFp
         # rows may be strided (a column range of a wider projection), heads are dense
         if R and t[0].stride() != (D, 1) and t[0].numel() != 1:
             raise ValueError(f"{name} must have dense [Hkv][D] rows")
+        if R > 1 and t.stride(0) < Hkv * D:  # broadcast rows; the C call takes 0 for dense ones
+            raise ValueError(f"{name}'s rows overlap")
         strides.append(t.stride(0) if R > 1 else 0)
     return AppendFp8Args(R, Hkv, D, P, num_pages, strides[0], strides[1], k.data_ptr(),
                          v.data_ptr(), slots.data_ptr(), kv_cache.data_ptr(), kv_scale.data_ptr(),
