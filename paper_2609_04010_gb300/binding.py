@@ -822,6 +822,10 @@ def append_fp8_args(k, v, slots, kv_cache, kv_scale, status_ws=None) -> AppendFp
         if R > 1 and t.stride(0) < Hkv * D:  # broadcast rows; the C call takes 0 for dense ones
             raise ValueError(f"{name}'s rows overlap")
         strides.append(t.stride(0) if R > 1 else 0)
+    if status_ws is not None:
+        _check(status_ws, "status_ws", torch.int32 if getattr(status_ws, "dtype", None) == torch.int32 else torch.uint8)
+        if status_ws.numel() * status_ws.element_size() < 4:
+            raise ValueError("status_ws must hold a status word of 4 bytes")
     return AppendFp8Args(R, Hkv, D, P, num_pages, strides[0], strides[1], k.data_ptr(),
                          v.data_ptr(), slots.data_ptr(), kv_cache.data_ptr(), kv_scale.data_ptr(),
                          None if status_ws is None else status_ws.data_ptr())
@@ -833,7 +837,8 @@ def append_kv_fp8_args(a: AppendFp8Args, stream=None):
 
 def append_kv_fp8(k, v, slots, kv_cache, kv_scale, status_ws=None, stream=None):
     """Write rows k, v (bf16 [rows][Hkv][D], row stride free) into the 8-bit cache at slots
-    (spec_append_kv_fp8; kv_cache and kv_scale are updated in place)."""
+    (spec_append_kv_fp8; kv_cache and kv_scale are updated in place). status_ws: a workspace
+    (uint8) or an int32 word, whose first 4 bytes take the status flags."""
     append_kv_fp8_args(append_fp8_args(k, v, slots, kv_cache, kv_scale, status_ws), stream)
 
 

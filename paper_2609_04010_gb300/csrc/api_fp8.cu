@@ -39,7 +39,8 @@ spec_status_t check_append(const spec_append_fp8_args_t* a) {
   const int64_t dense = static_cast<int64_t>(a->num_kv_heads) * a->head_dim;
   for (int64_t s : {a->k_row_stride, a->v_row_stride})
     if (s != 0 && (s < dense || s % 8 != 0)) return SPEC_ERR_INVALID_ARGUMENT;
-  if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->kv_cache, 16) || !aligned(a->kv_scale, 4))
+  if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->kv_cache, 16) || !aligned(a->kv_scale, 4) ||
+      !aligned(a->status, 4))
     return SPEC_ERR_INVALID_ARGUMENT;
   return SPEC_OK;
 }

@@ -46,3 +46,24 @@ def test_append_refuses_broadcast_rows(R):
     half = torch.zeros(R * 64 + 64, dtype=torch.bfloat16).as_strided((R, 2, 64), (64, 64, 1))
     with pytest.raises(ValueError):
         append_args(half)
+
+
+def test_append_checks_the_status_word():
+    k = rows(3, 2, 64)
+    for ok in (torch.zeros(256, dtype=torch.uint8), torch.zeros(1, dtype=torch.int32)):
+        assert append_args(k, status_ws=gpu(ok)).status == ok.data_ptr()
+    for bad, error in ((torch.zeros(256, dtype=torch.uint8), ValueError),             # a host tensor
+                       (gpu(torch.zeros(3, dtype=torch.uint8)), ValueError),          # too short
+                       (gpu(torch.zeros(512, dtype=torch.uint8)[::2]), ValueError),   # not contiguous
+                       (gpu(torch.zeros(4, dtype=torch.float64)), TypeError)):
+        with pytest.raises(error):
+            append_args(k, status_ws=bad)
+
+
+def test_append_call_refuses_an_unaligned_status_word():
+    import ctypes
+    a = append_args(rows(3, 2, 64), status_ws=gpu(torch.zeros(64, dtype=torch.uint8)))
+    for p in ("k", "v", "kv_cache", "kv_scale", "slots"):
+        setattr(a, p, 1 << 20)
+    a.status = (1 << 20) + 2
+    assert binding.lib().spec_append_kv_fp8(ctypes.byref(a), None) == 1
