@@ -816,8 +816,9 @@ def append_fp8_args(k, v, slots, kv_cache, kv_scale, status_ws=None) -> AppendFp
             raise TypeError(f"{name} must be a torch.bfloat16 tensor")
         if not t.is_cuda or tuple(t.shape) != (R, Hkv, D):
             raise ValueError(f"{name} must be a CUDA tensor of shape {(R, Hkv, D)}")
-        # rows may be strided (a column range of a wider projection), heads are dense
-        if R and t[0].stride() != (D, 1) and t[0].numel() != 1:
+        # rows may be strided (a column range of a wider projection), heads are dense; the stride
+        # of a single head or element counts for nothing
+        if R and any(n > 1 and s != want for n, s, want in zip((Hkv, D), t.stride()[1:], (D, 1))):
             raise ValueError(f"{name} must have dense [Hkv][D] rows")
         if R > 1 and t.stride(0) < Hkv * D:  # broadcast rows; the C call takes 0 for dense ones
             raise ValueError(f"{name}'s rows overlap")

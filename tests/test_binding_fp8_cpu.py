@@ -67,3 +67,16 @@ def test_append_call_refuses_an_unaligned_status_word():
         setattr(a, p, 1 << 20)
     a.status = (1 << 20) + 2
     assert binding.lib().spec_append_kv_fp8(ctypes.byref(a), None) == 1
+
+
+def test_append_takes_one_head_whatever_its_stride():
+    """[heads][rows][D] with one head: the head's stride is that of all its rows."""
+    k = torch.zeros(1, 5, 64, dtype=torch.bfloat16).transpose(0, 1)
+    assert k.stride() == (64, 320, 1)
+    assert append_args(k).k_row_stride == 64
+    wide = torch.zeros(3, 5, 256, dtype=torch.bfloat16)[1:2, :, 64:128].transpose(0, 1)
+    assert append_args(wide).k_row_stride == 256
+    with pytest.raises(ValueError):
+        append_args(torch.zeros(2, 5, 64, dtype=torch.bfloat16).transpose(0, 1))
+    with pytest.raises(ValueError):
+        append_args(torch.zeros(5, 1, 128, dtype=torch.bfloat16)[..., ::2])
