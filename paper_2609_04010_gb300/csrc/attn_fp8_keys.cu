@@ -625,13 +625,14 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   // pipeline's refill, its outputs). Charging it keeps blocks of many short units and of few
   // long ones equal (batch 64 / block 8, 3: 89.5 us, 4: 87.4, 5: 89.3, 6: 90.4).
   p.unit_overhead = 4;
-  static_assert(C::smem_bytes(kFp8TcBatch) <= kTcMaxSmem, "a block's shared memory");
-  const size_t smem = C::smem_bytes(a.batch);
+  // the limit is one for all host threads, so every call sets the same
+  constexpr size_t kMost = C::smem_bytes(kFp8TcBatch);
+  static_assert(kMost <= kTcMaxSmem, "a block's shared memory");
   auto kernel = attn_fp8_keys_kernel<D, HP, NR>;
   const cudaError_t e =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMost));
   if (e != cudaSuccess) return e;
-  const cudaError_t k = launch_overlapped(kernel, dim3(P.grid), kThreads, smem, stream, map, p);
+  const cudaError_t k = launch_overlapped(kernel, dim3(P.grid), kThreads, C::smem_bytes(a.batch), stream, map, p);
   return k == cudaSuccess ? launch_merge<D, HP, false>(p, P, stream) : k;
 }
 

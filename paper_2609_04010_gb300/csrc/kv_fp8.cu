@@ -394,9 +394,9 @@ cudaError_t launch_map_slots(const spec_slot_args_t& a, char* ws, cudaStream_t s
   SlotParams p{a, reinterpret_cast<uint32_t*>(ws + kWsHeader)};
   const size_t smem = slot_smem(a.batch);
   (void)cudaGetLastError();
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(
-        map_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (smem > 48 * 1024) {  // the limit is one for all host threads, so every call sets the same
+    const cudaError_t e = cudaFuncSetAttribute(map_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(slot_smem(SPEC_SLOTS_MAX_BATCH)));
     if (e != cudaSuccess) return e;
   }
   const int grid = (a.max_rows - 1) / kSlotRowsPerBlock + 1;
