@@ -16,8 +16,9 @@ namespace {
 // Every block scans the whole batch (its request sizes and page needs) into shared memory
 // and then maps its share of the rows, so that one launch does what would otherwise take a
 // scan and a dependent expansion. No block waits: the state that may be updated in place
-// (kv_len, free_count) is written by the block that takes the last ticket, after every
-// block has read it. New pages are read from the free list, never from the table entries
+// (kv_len, free_count) is read by that scan alone and written by the block that takes the last
+// ticket; tickets are taken right behind the scan, when a block has no writes that the fence
+// before its ticket would wait for. New pages are read from the free list, never from the table entries
 // that other blocks are writing. Up to some 100,000 rows a call is a launch and a chain of three
 // dependent reads (64 requests of 16 tokens: 4.7 us); above, the writes count (512 requests of 1
 // to 4,096 tokens, 1.05 M rows: 8.8 us, 1.5 TB/s; half or twice the rows per block: 10.3 and 16
@@ -32,7 +33,7 @@ struct SlotParams {
 
 struct SeqSlots {
   int32_t len;     // tokens held; -1: not served
-  int32_t first;   // table entry of its first new page
+  int32_t first;   // table entry of its first new page; not served: kv_len
   int32_t before;  // pages that earlier sequences need (at most INT32_MAX)
 };
 
@@ -85,10 +86,10 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
   Two carry = {0, 0};
   for (int b0 = 0; b0 < a.batch; b0 += kSlotThreads) {
     const int b = b0 + tid;
-    int len = -1, n = 0, need = 0, first = 0;
+    int held_len = 0, len = -1, n = 0, need = 0, first = 0;
     if (b < a.batch) {
       n = a.num_new[b];
-      len = a.kv_len[b];
+      len = held_len = a.kv_len[b];
       const bool fits = len >= 0 && n >= 0 && static_cast<int64_t>(len) + n <= cap;
       if (fits) {
         const int64_t held = static_cast<int64_t>(len) + a.reserved + P - 1;
@@ -107,7 +108,7 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
       start[b] = static_cast<int32_t>(min(carry.rows + before.rows, static_cast<int64_t>(INT32_MAX)));
       const bool served = len >= 0 && (need == 0 || pages + need <= count0);
       if (served && need > 0) atomicMax(&s_taken, static_cast<int>(pages) + need);
-      seq[b] = {served ? len : -1, first, static_cast<int32_t>(min(pages, static_cast<int64_t>(INT32_MAX)))};
+      seq[b] = {served ? len : -1, served ? first : held_len, static_cast<int32_t>(min(pages, static_cast<int64_t>(INT32_MAX)))};
     }
     carry.rows += all.rows;
     carry.pages += all.pages;
@@ -117,6 +118,11 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
     seq[a.batch].before = static_cast<int32_t>(min(carry.pages, static_cast<int64_t>(INT32_MAX)));
   }
   __syncthreads();
+  uint32_t ticket = 0;
+  if (gridDim.x > 1 && tid == 0) {
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");  // the block's reads of the state are before its ticket
+    ticket = atomicAdd(p.ticket, 1u);
+  }
   const int total = start[a.batch];
 
   // Four rows a thread, one search for their sequence; a page's first token puts it into the table.
@@ -143,7 +149,7 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
       const SeqSlots s = seq[lo];
       const int i = static_cast<int>(r) - start[lo];
       if (s.len < 0) {
-        pos[e] = a.kv_len[lo] + i;
+        pos[e] = s.first + i;
         continue;
       }
       pos[e] = s.len + i;
@@ -191,22 +197,21 @@ __global__ void __launch_bounds__(kSlotThreads) map_slots_kernel(SlotParams p) {
     }
   }
 
-  // The last block to get here updates the state. What the blocks before it read of it they
-  // have used, and nothing they wrote is read here, so the ticket needs no fence.
+  // The block with the last ticket updates the state, which all have read.
   if (gridDim.x > 1) {
-    __syncthreads();
     if (tid == 0) {
-      s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
-      if (s_last) *p.ticket = 0;
+      s_last = ticket == gridDim.x - 1;
+      if (s_last) {
+        *p.ticket = 0;
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");
+      }
     }
     __syncthreads();
     if (!s_last) return;
-  } else {
-    __syncthreads();  // every row has read kv_len
   }
   for (int b = tid; b < a.batch; b += kSlotThreads) {
     const bool served = seq[b].len >= 0;
-    const int len = a.kv_len[b], n = a.num_new[b];
+    const int len = served ? seq[b].len : seq[b].first, n = a.num_new[b];
     const bool fits = len >= 0 && n >= 0 && static_cast<int64_t>(len) + n <= cap;
     a.new_len[b] = served ? len + n : len;
     if (a.flags) a.flags[b] = served ? 0 : (fits ? 2 : 1);
