@@ -9,7 +9,7 @@
 //   S^T[key][row]  = K8[key][:] . Q8[row][:]          (M = 128 keys, N = rows, K = D)
 //   O^T[dim][row] += sum_key V8[key][dim] P8[key][row] (M = D, N = 3 * rows, K = 128 keys)
 // What is exact in the cache must not be lost on the other side. A bf16 query enters as the sum
-// of two e4m3 terms (x1 = e4m3(x), x2 = e4m3(x - x1)), exact to 2^-18 of its group's largest
+// of two e4m3 terms (x1 = e4m3(x), x2 = e4m3(x - x1)), exact to 2^-18 of its row's largest
 // element. A weight enters as the sum of three e5m2 terms (split_weights), which is bf16's
 // precision, and for every weight that counts: where one key has most of a row's weight, the
 // rest of the output is the sum of thousands of weights below 2^-15 of the largest. Two e4m3
@@ -66,7 +66,7 @@ struct Cfg {
   static constexpr uint32_t Q_TERM = NR * D;               // one term of one sub-unit's Q
   static constexpr uint32_t PW = 4 * NR;                   // a key's weights: first, second, third terms, unused
   static constexpr uint32_t P_BUF = TK * PW;               // [key][PW], swizzled by its width
-  static constexpr int NST = ((NR == 16 ? 216 : 208) * 1024 - NH * (P_BUF + 2 * Q_TERM)) / STAGE;  // D = 128, HP = 2: 3 or 2
+  static constexpr int NST = ((NR == 16 && HP * D >= 128 ? 216 : 208) * 1024 - NH * (P_BUF + 2 * Q_TERM)) / STAGE;  // D = 128, HP = 2: 3 or 2
   static constexpr uint32_t OFF_STAGE = 0;
   static constexpr uint32_t OFF_P = OFF_STAGE + NST * STAGE;
   static constexpr uint32_t OFF_Q = OFF_P + NH * P_BUF;
@@ -77,17 +77,16 @@ struct Cfg {
   static constexpr uint32_t OFF_VIS = OFF_NAN + NH * D * 8;          // uint64 [2][NH][NR]
   static constexpr uint32_t OFF_SEEN = OFF_VIS + 2 * NH * NR * 8;    // uint32 [2][NH][64]
   static constexpr uint32_t OFF_M = OFF_SEEN + 2 * NH * 64 * 4;      // float [2][NH][NR]
-  static constexpr uint32_t OFF_X = OFF_M + 2 * NH * NR * 4;         // float [NH][4][NR]: cross-quadrant
+  static constexpr uint32_t OFF_QS = OFF_M + 2 * NH * NR * 4;        // float [2][NH][NR]: rows' Q scales
+  static constexpr uint32_t OFF_X = OFF_QS + 2 * NH * NR * 4;        // float [NH][4][NR]: cross-quadrant
   static constexpr uint32_t OFF_ROW = OFF_X + NH * 4 * NR * 4;       // int64 [NH][NR]: rows' outputs
-  static constexpr uint32_t OFF_INV = OFF_ROW + NH * NR * 8;         // float [NH][NR]: their factors
-  static constexpr uint32_t OFF_BAR = OFF_INV + NH * NR * 4;
+  static constexpr uint32_t OFF_BAR = OFF_ROW + NH * NR * 8;
   // full[NST], empty[NST], s_full[NH][SB], s_free[NH][SB], p_full[NH], pv_done[NH],
   // seg_ready[NH], drain[2], flag_ready[kFlagRing]
   static constexpr int NBAR = 2 * NST + 2 * NH * SB + 3 * NH + 2 + kFlagRing;
   static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, -, -, NaN flags
   static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;               // int [2][kFlagRing]: segments' bad flags
-  static constexpr uint32_t OFF_QMAX = OFF_FLAG + 8 * kFlagRing;       // uint32 [NH][8]
-  static constexpr uint32_t OFF_PB = OFF_QMAX + NH * 32;    // int [batch + 1]
+  static constexpr uint32_t OFF_PB = OFF_FLAG + 8 * kFlagRing;       // int [batch + 1]
   static constexpr uint32_t S_COL = 0;                      // [NH][SB][NR]
   static constexpr uint32_t O_COL = NH * SB * NR;           // [NH][first, second, third terms][NR]
   static constexpr uint32_t TMEM_COLS = NR == 16 ? 256 : 512;
@@ -303,7 +302,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t o_col = lane_base + C::O_COL + h * 3 * NR + ch * NC;
     const int pg = (q4 * 32 + lane) / p.page_size;  // this lane's page of a tile
     float* xch = reinterpret_cast<float*>(smem + C::OFF_X) + h * 4 * NR;  // [4][NR]
-    uint32_t* qmax = reinterpret_cast<uint32_t*>(smem + C::OFF_QMAX) + h * 8;
     unsigned char* const pbuf = smem + C::OFF_P + h * C::P_BUF + (q4 * 32 + lane) * C::PW;
     uint32_t it = 0, seg_no = 0;
     // After a timeout the warp runs its loops to the end without waiting (nothing else
@@ -319,14 +317,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     auto seen_of = [&](uint32_t par) { return reinterpret_cast<uint32_t*>(smem + C::OFF_SEEN) + (par * NH + h) * 64; };
     auto mref_of = [&](uint32_t par) { return reinterpret_cast<float*>(smem + C::OFF_M) + (par * NH + h) * NR; };
+    auto qs_of = [&](uint32_t par) { return reinterpret_cast<float*>(smem + C::OFF_QS) + (par * NH + h) * NR; };
     // the unit row of row r, and how many are real
     auto unit_row = [&](const Seg& sg, int r) { return sg.rt * tile_rows + (HP == 2 ? 0 : h * sub_rows) + r; };
     auto real_rows = [&](const Seg& sg) { return min(sub_rows, p.rows - unit_row(sg, 0)); };
 
-    // Brings a segment's Q into shared memory as two e4m3 terms, scaled by the power of two
-    // that takes the sub-unit's largest finite magnitude into (224, 448], and sets its
-    // row state. Returns the scale.
-    auto start_segment = [&](const Seg& sg, uint32_t par) -> float {
+    // Brings a segment's Q into shared memory as two e4m3 terms, each row scaled by the power of
+    // two that takes its largest finite magnitude into (224, 448], and sets its row state.
+    auto start_segment = [&](const Seg& sg, uint32_t par) {
       constexpr int kPieces = D / 16;  // 16 elements per piece: 32 B in, 16 B per term
       constexpr int kLoops = NR * kPieces > 256 ? NR * kPieces / 256 : 1;  // NR > 16 has 256 threads
       const int nreal = real_rows(sg);
@@ -353,9 +351,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         vis[r] = all & (p.tree_mask ? __ldg(p.tree_mask + static_cast<int64_t>(sg.b) * p.gamma + j) : (2ull << j) - 1);
         mref_of(par)[r] = kNoKey;
       }
-      uint32_t mx = 0;
+      bar_sync(sbar, nthr);
+      for (int i = swarp; i < 64; i += nsoft) {  // lane = row
+        const uint32_t m = __ballot_sync(0xffffffffu, lane < NR && (vis[lane % NR] >> i & 1));
+        if (lane == 0) seen_of(par)[i] = m;
+      }
 #pragma unroll
-      for (int i = 0; i < kLoops; ++i)
+      for (int i = 0; i < kLoops; ++i) {
+        const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+        uint32_t mx = 0;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const uint32_t w[4] = {x[i][e].x, x[i][e].y, x[i][e].z, x[i][e].w};
@@ -365,21 +369,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             mx = max(mx, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
           }
         }
-      mx = __reduce_max_sync(0xffffffffu, mx);
-      if (lane == 0) qmax[swarp] = mx;
-      bar_sync(sbar, nthr);
-      for (int i = swarp; i < 64; i += nsoft) {  // lane = row
-        const uint32_t m = __ballot_sync(0xffffffffu, lane < NR && (vis[lane % NR] >> i & 1));
-        if (lane == 0) seen_of(par)[i] = m;
-      }
-      mx = 0;
-      for (int w = 0; w < nsoft; ++w) mx = max(mx, qmax[w]);
-      const int ex = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
-      const float inv = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
 #pragma unroll
-      for (int i = 0; i < kLoops; ++i) {
-        const int item = i * nthr + stid, r = item / kPieces, piece = item % kPieces;
+        for (int o = 1; o < kPieces; o <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         if (r >= NR) continue;
+        const int ex = mx == 0 ? 0 : min(118, max(-100, static_cast<int>(mx >> 7) - 135 + ((mx & 0x7fu) > 0x60u ? 1 : 0)));
+        const float inv = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+        if (piece == 0) qs_of(par)[r] = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
         uint32_t t1w[4], t2w[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -401,15 +396,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       fence_async_smem();
       bar_sync(sbar, nthr);  // the row state is set
       if (lane == 0) mbar_arrive(seg_ready(h));
-      return __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
     };
 
     Seg s = find(w.t0, w, p);
-    float qf = s.ntile > 0 ? start_segment(s, 0) : 1.f;
+    if (s.ntile > 0) start_segment(s, 0);
     while (s.ntile > 0) {
       const uint32_t par = seg_no & 1;
       const int ctx = s.kv_len - p.gamma;
       float* const mr = mref_of(par) + ch * NC;
+      const float* const qs = qs_of(par) + ch * NC;
       float l[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
@@ -426,7 +421,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_ld<NC>(s_tmem, raw);
         wait(full(st), (x / NST) & 1);  // orders the producer's scales before this
         const float4 sc = scl[(st * 8 + pg) * HP + kvh];
-        const float ks = sc.x * qf;
         uint32_t seen = ~0u;
         if (masked && rel >= 0) seen = rel < 64 ? seen_of(par)[rel] >> (ch * NC) : 0u;
         // e = log2 of the key's weight and value scale for each row, over the row's
@@ -434,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float e[NC];
         auto exponents = [&](const uint32_t* r) {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(r[c]), ks, sc.y) - mr[c];
+          for (int c = 0; c < NC; ++c) e[c] = fmaf(__uint_as_float(r[c]), sc.x * qs[c], sc.y) - mr[c];
           if (masked) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) e[c] = (seen >> c & 1) ? e[c] : -INFINITY;
@@ -456,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_wait_ld();
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-              const float m = warp_max((seen >> (c8 + c) & 1) ? fmaf(__uint_as_float(t8[c]), ks, sc.y) : -INFINITY);
+              const float m = warp_max((seen >> (c8 + c) & 1) ? fmaf(__uint_as_float(t8[c]), sc.x * qs[c8 + c], sc.y) : -INFINITY);
               if (lane % NC == c8 + c) mx = m;
             }
           }
@@ -535,10 +529,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Seg c = s;
       const uint32_t xl = it + c.ntile - 1;
       it += c.ntile;
-      qf = 1.f;
       if (has_more(c, w.t1, w.ovh)) {
         s = find(c.vnext, w, p);
-        qf = start_segment(s, par ^ 1);
+        start_segment(s, par ^ 1);
       } else {
         s.ntile = 0;
       }
@@ -550,9 +543,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (bad && stid == 0) set_status(p.status, c.len_ok ? SPEC_FLAG_BAD_PAGE : SPEC_FLAG_BAD_KV_LEN);
       const int nrows = real_rows(c);
       bar_sync(sbar, nthr);
-      // a thread per row: its sum, factor and place
+      // a thread per row: its sum, factor (in place of the first part of the sum) and place
       int64_t* row_at = reinterpret_cast<int64_t*>(smem + C::OFF_ROW) + h * NR;
-      float* row_inv = reinterpret_cast<float*>(smem + C::OFF_INV) + h * NR;
+      float* row_inv = xch;
       for (int r = stid; r < nrows; r += nthr) {
         const float L = bad ? -1.f : xch[r] + xch[NR + r] + xch[2 * NR + r] + xch[3 * NR + r];
         const float m = mref_of(par)[r];

@@ -27,7 +27,7 @@ struct AttnFp8Plan {
 };
 AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path);
 constexpr int kFp8KeyTile = 128;   // keys per tile of the tensor-core kernels
-constexpr int kFp8TcBatch = 1024;  // sequences they take in a launch
+constexpr int kFp8TcBatch = 1000;  // sequences they take in a launch
 // starve (test hook only): the producers issue no copies, so the bounded waits run out.
 cudaError_t launch_attn_fp8_keys(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
                                  cudaStream_t stream, bool starve = false);
