@@ -641,8 +641,8 @@ spec_status_t spec_append_kv_fp8(const spec_append_fp8_args_t* append, spec_stre
 typedef struct {
   int32_t batch;              /* >= 1                                                       */
   int32_t gamma;              /* 1 .. 64                                                    */
-  int32_t num_q_heads;        /* a multiple of num_kv_heads                                 */
-  int32_t num_kv_heads;
+  int32_t num_q_heads;        /* a multiple of num_kv_heads; gamma times it / num_kv_heads   */
+  int32_t num_kv_heads;       /*   at most 2^31 - 256                                       */
   int32_t head_dim;           /* 64 or 128                                                  */
   int32_t page_size;          /* 16, 32 or 64                                               */
   int32_t max_pages_per_seq;

@@ -88,6 +88,7 @@ spec_status_t check_attn_fp8(const spec_attn_fp8_args_t* a) {
       static_cast<int64_t>(a->num_pages) * a->page_size > INT32_MAX)
     return SPEC_ERR_UNSUPPORTED;
   const int64_t rows = static_cast<int64_t>(a->num_q_heads / a->num_kv_heads) * a->gamma;
+  if (rows > kFp8MaxRows) return SPEC_ERR_UNSUPPORTED;
   const int64_t z = static_cast<int64_t>(a->batch) * ((rows + kSimtRowTile - 1) / kSimtRowTile);
   const bool tc = tc_form(*a).fits;
   if (a->path == SPEC_ATTN_TENSOR_CORES && !tc) return SPEC_ERR_UNSUPPORTED;
