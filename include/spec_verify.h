@@ -682,7 +682,8 @@ spec_status_t spec_verify_attention_fp8(const spec_attn_fp8_args_t* attn, void* 
  * out may be logits itself. One launch, no workspace.
  */
 typedef struct {
-  int32_t batch, gamma, vocab, logits_dtype;  /* gamma 1 .. 64, batch <= 65535                */
+  int32_t batch, gamma, vocab, logits_dtype;  /* gamma 1 .. 64, batch <= 65535,
+                                   vocab <= 65535 * 2048                                      */
   int32_t block_shift;          /* 0 or 1                                                     */
   int32_t max_history, max_bias;  /* row lengths of history and bias_*; 0: none               */
   const void* logits;           /* [batch][gamma][vocab]                                      */

@@ -22,7 +22,8 @@ namespace specv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSlice = kThreads * 8;  // tokens of a block
+constexpr int kSlice = kAdjustSlice;
+static_assert(kSlice == kThreads * 8, "eight tokens a thread");
 constexpr uint32_t kPrompt = 0x80000000u, kBlock = 0x40000000u, kBias = 0x20000000u;  // beside a count
 constexpr uint32_t kCount = 0x1fffffffu;
 

@@ -107,7 +107,7 @@ spec_status_t check_adjust(const spec_adjust_args_t* a) {
     return SPEC_ERR_INVALID_ARGUMENT;
   const uintptr_t esz = a->logits_dtype == SPEC_BF16 ? 2 : 4;
   if (!aligned(a->logits, esz) || !aligned(a->out, esz)) return SPEC_ERR_INVALID_ARGUMENT;
-  if (a->gamma > 64 || a->batch > 65535) return SPEC_ERR_UNSUPPORTED;
+  if (a->gamma > 64 || a->batch > 65535 || (a->vocab - 1) / kAdjustSlice >= 65535) return SPEC_ERR_UNSUPPORTED;
   return SPEC_OK;
 }
 

@@ -9,6 +9,7 @@ namespace specv {
 cudaError_t launch_map_slots(const spec_slot_args_t& a, char* ws, cudaStream_t stream);
 size_t slot_smem(int batch);  // dynamic shared memory of a block
 cudaError_t launch_append_fp8(const spec_append_fp8_args_t& a, int sms, cudaStream_t stream);
+constexpr int kAdjustSlice = 2048;  // tokens of a block, whose ranges are the grid's second index
 cudaError_t launch_adjust(const spec_adjust_args_t& a, int sms, cudaStream_t stream);
 
 // The launch plan of the attention over the 8-bit cache.
