@@ -6,6 +6,9 @@ are torch's; everything between them is this library's: pages and slots for the 
 (verify_attention_fp8), the constraints on both models' logits (adjust_logits), the drafts
 (sample_block), the acceptance (accept_block) and the cache's roll-back (commit_kv).
 
+With one layer, a prompt's keys and values need no attention, so prefill only writes them. A
+deeper model would run each layer's attention over the prompt, at most 64 tokens a call here.
+
     python examples/decode_fp8.py
 """
 

@@ -631,8 +631,9 @@ spec_status_t spec_append_kv_fp8(const spec_append_fp8_args_t* append, spec_stre
  * mask over an empty prefix) gets out = 0 and lse = -inf. What a row's mask hides (keys past
  * kv_len, or hidden block keys) does not reach it, whatever the bytes there. Scores,
  * softmax statistics and accumulators are fp32. On the tensor cores a query enters
- * as the sum of two e4m3 terms, exact to 2^-18 of its row's largest |q|, and a weight times its page's value scale as the sum of three e5m2 terms, exact to
- * 1.25 * 2^-9 of itself or to 2^-28 of the largest such product of its row.
+ * as the sum of two e4m3 terms, exact to 2^-18 of its row's largest |q|, and a weight times
+ * its page's value scale as the sum of three e5m2 terms, exact to 1.25 * 2^-9 of itself or to
+ * 2^-28 of the largest such product of its row.
  * path: SPEC_ATTN_AUTO takes the tensor cores where the call fits them (32-bit counts of
  * key tiles and cache rows), else CUDA cores; SPEC_ATTN_TENSOR_CORES is
  * SPEC_ERR_UNSUPPORTED where it does not fit. Two launches per 1,000 sequences on the tensor

@@ -47,10 +47,10 @@ spec_status_t check_append(const spec_append_fp8_args_t* a) {
 
 // The tensor-core form of a call. A block serves two sub-units of query rows: two adjacent KV
 // heads where each fits one (a page of both is one copy of twice the size; 66 to 128 rows as
-// two halves of one head instead: 174 against 124 us at batch 64 / block 20), else two halves
+// two halves of one head instead: 189 against 127 us at batch 64 / block 20), else two halves
 // of one KV head's rows, in tiles. Up to 32 rows a sub-unit the keys are on the MMA's M side,
-// from 33 the rows (batch 64 / block 8 of 4 heads, 32 rows: 88 us and 97; block 10: 115 and
-// 102). Sequences are taken kFp8TcBatch at a time, because a block keeps their first tiles.
+// from 33 the rows (batch 64 / block 8, 32 rows a KV head: 90 us, with the rows on M 102; block 10:
+// 108, as two halves with the keys on M 142). Sequences are taken kFp8TcBatch at a time, because a block keeps their first tiles.
 struct TcForm {
   int rows_on_m, heads, sub_rows, row_tiles, batch;
   bool fits;

@@ -14,7 +14,7 @@
 // precision, and for every weight that counts: where one key has most of a row's weight, the
 // rest of the output is the sum of thousands of weights below 2^-15 of the largest. Two e4m3
 // terms, whose smallest step was 2^-13 beside a largest of 2^2, lost all of them (32,768 keys, one
-// with nine tenths of the weight: off by 0.36 of the output's norm, now 0.002). Both terms of Q
+// with nine tenths of the weight: off by 0.63 of the output's norm, now 0.0018). Both terms of Q
 // accumulate into the same S; those of P are thirds of N and are added when a unit ends.
 //
 // With sk, sv the scales of a key's page, m_r the row's reference and the weights
@@ -45,8 +45,11 @@
 // that none is missed at a named barrier.
 //
 // Memory bounds it up to 16 rows: batch 32, one token a sequence, contexts 256 to 16,384, 32 / 8
-// heads of 128: 92 us, 5.93 TB/s (0.87 of the measured copy rate). With 32 rows the chain of
-// waits from a tile's scores to its outputs does (batch 64 / block 8: 87 us, floor 46).
+// heads of 128: 92 us, 5.92 TB/s (0.87 of the measured copy rate). With 32 rows the chain of
+// waits from a tile's scores to its outputs does (batch 64 / block 8: 90 us, floor 46; 87 with two
+// terms a weight). With one or an odd number of KV heads, or heads of 64, a tile brings half or a
+// quarter of the bytes for the same chain (32 sequences as above, 8 / 1 heads: 28 us, floor 10;
+// 32 / 8 heads of 64: 61, floor 40).
 #include "attn_fp8_tc.cuh"
 
 namespace specv {
@@ -616,7 +619,7 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   p.starve = starve ? 1 : 0;
   // Starting a unit inside a block's range costs about this many tiles of time (its Q, the
   // pipeline's refill, its outputs). Charging it keeps blocks of many short units and of few
-  // long ones equal (batch 64 / block 8, 3: 89.5 us, 4: 87.4, 5: 89.3, 6: 90.4).
+  // long ones equal (batch 64 / block 8, 3: 91.0 us, 4: 89.8, 5: 91.8).
   p.unit_overhead = 4;
   // the limit is one for all host threads, so every call sets the same
   constexpr size_t kMost = C::smem_bytes(kFp8TcBatch);

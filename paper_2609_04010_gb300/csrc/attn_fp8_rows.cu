@@ -5,12 +5,12 @@
 //   S[row][key] = Q8[row][:] . K8[key][:]          (M = 128 rows, N = 128 keys, K = D)
 //   O[row][dim] += sum_key P8[row][key] V8[key][dim] (M = 128 rows, N = D, K = 128 keys)
 // The arithmetic is attn_fp8_keys.cu's: e4m3 operands straight from the cache, queries as sums
-// of two e4m3 terms, weights as sums of three e5m2 terms, weights P = 2^(s + log2(sv) - m) against a reference m
-// per row, sum P / sv. Here two threads share a row, each with half of a tile's keys: maximum,
-// sum and reference are their own registers, the page constants are the same for all lanes,
-// and only the two warps of 32 rows wait for each other (one thread a row: 162 us against 115
-// at batch 64 / block 16, because eight warps cannot hide each other's waits). With few rows the
-// M side would be padding and attn_fp8_keys.cu is faster.
+// of two e4m3 terms, weights as sums of three e5m2 terms, weights P = 2^(s + log2(sv) - m) against
+// a reference m per row, sum P / sv. Here two threads share a row, each with half of a tile's
+// keys: maximum, sum and reference are their own registers, the page constants are the same for
+// all lanes, and only the two warps of 32 rows wait for each other (one thread a row, when weights
+// had two terms: 162 us against 115 at batch 64 / block 16, because eight warps cannot hide each
+// other's waits). With few rows the M side would be padding and attn_fp8_keys.cu is faster.
 //
 // A block serves two sub-units of at most 128 query rows: two adjacent KV heads (HP = 2) or
 // two halves of one KV head's rows. The terms of P live in TMEM over the columns of S that
@@ -19,23 +19,24 @@
 // at its softmax, the tensor core works for the other. m is set so that a row's largest P is
 // 2^11.5 to 2^12.5 and raised when a P would pass 2^15 (the terms add up in one accumulator, so
 // the third one's smallest step is 2^-16: a P is off by 2^-28 of the row's largest at most). The
-// third product costs 0.14 us a tile (batch 4, 32,768 keys: 164 us; 153 with two e4m3 terms, which
-// lost the weights below 2^-14 of the largest: up to 0.75 of an output). m is a whole number,
-// so that log2(sv) - m is exact with power-of-two scales. Hidden scores are set to -inf in
-// TMEM, before the two passes over a tile (the maximum, the weights), which then know no masks.
+// third product costs 0.2 us a tile (batch 4, 32,768 keys: 165 us; 153 with two e4m3 terms, which
+// lost the weights below 2^-14 of the largest: 0.77 of an output where attn_fp8_keys.cu lost
+// 0.63). m is a whole number, so that log2(sv) - m is exact with power-of-two scales. Hidden scores
+// are set to -inf in TMEM, before the two passes over a tile (the maximum, the weights), which then
+// know no masks.
 // Warp roles (persistent, one block per SM):
 //   warps 0..15   softmax, eight per sub-unit: a lane quadrant is 32 rows, two warps a quadrant
 //   warps 16, 18  producers (as in attn_fp8_keys.cu)
 //   warp 17       issues S = Q K^T and O += P V; clears V of keys past the sequence's end
 // Work list, split units, bounded waits: as in attn_fp8_keys.cu.
 //
-// What bounds it is the chain S, softmax, P V of a sub-unit: 2.4 us a tile of 128 keys, of which
-// its softmax is 1.3 (the converts to e4m3 and ex2 take 0.5 of it) and the products 0.55; two
-// sub-units, all that TMEM has room for with D = 128, do not cover each other fully. Half tiles
-// with scores in two buffers (231 us), four threads a row (158), and weights taken before the
-// maximum is known (276) were all slower than the 155 us that it takes for batch 4, block 32, 64 /
-// 8 heads, 32,768 keys: 885 TFLOP/s of Q K^T and P V, twice that on the tensor cores. Batch 64,
-// block 16, 32 / 8 heads, contexts 512 to 4,096: 107 us, 3.0 TB/s.
+// What bounds it is the chain S, softmax, P V of a sub-unit: 2.6 us a tile of 128 keys, of which
+// its softmax is about 1.3 (the conversions and ex2 take 0.5 of it) and the products 0.7; two
+// sub-units, all that TMEM has room for with D = 128, do not cover each other fully. Batch 4, block
+// 32, 64 / 8 heads, 32,768 keys take 165 us: 833 TFLOP/s of Q K^T and P V, two and a half times that
+// on the tensor cores. With two terms a weight (155 us) half tiles with scores in two buffers (231),
+// four threads a row (158) and weights taken before the maximum is known (276) were all slower.
+// Batch 64, block 16, 32 / 8 heads, contexts 512 to 4,096: 113 us, 2.8 TB/s.
 #include "attn_fp8_tc.cuh"
 
 namespace specv {
@@ -531,7 +532,7 @@ cudaError_t launch_typed(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, ch
   p.hunits = a.num_kv_heads / HP;
   p.rows_per_cta = P.sub_rows;
   p.starve = starve ? 1 : 0;
-  // tiles of time that starting a unit costs (batch 64 / block 20, 2: 126 us, 3: 124, 4: 121)
+  // tiles of time that starting a unit costs (batch 64 / block 20, 3: 129.5 us, 4: 127.0, 5: 128.3)
   p.unit_overhead = 4;
   // the limit is one for all host threads, so every call sets the same
   constexpr size_t kMost = C::smem_bytes(kFp8TcBatch);

@@ -206,7 +206,7 @@ __device__ __forceinline__ void note_split(const AttnFp8Params& p, const Seg& s,
 
 // Joins the parts of split units: grid (chunks of a unit's outputs, places of units). A warp
 // takes 8 rows x 32 columns, a thread 8 columns of a row. Small blocks start sooner: trees of 31
-// for 8 requests take 42.5 us, 44.6 with 256 threads a block and 45.1 with 512. (The last block
+// for 8 requests take 44.0 us, 44.5 with 256 threads a block. (The last block
 // to finish a unit merging it alone took 12 to 15 us at the end of a call where this takes 4 to
 // 6: 128 rows in 5 parts are 330 KB, an L2 round trip of one SM at a time.)
 constexpr int kMergeThreads = 128;

@@ -21,8 +21,7 @@ namespace {
 // before its ticket would wait for. New pages are read from the free list, never from the table entries
 // that other blocks are writing. Up to some 100,000 rows a call is a launch and a chain of three
 // dependent reads (64 requests of 16 tokens: 4.7 us); above, the writes count (512 requests of 1
-// to 4,096 tokens, 1.05 M rows: 8.8 us, 1.5 TB/s; half or twice the rows per block: 10.3 and 16
-// us).
+// to 4,096 tokens, 1.05 M rows: 8.7 us, 1.5 TB/s; half or twice the rows per block: 10.3 us both).
 constexpr int kSlotThreads = 512;
 constexpr int kSlotRowsPerBlock = 8 * kSlotThreads;  // rows the grid is sized for, per block
 

@@ -35,7 +35,7 @@ def test_append_takes_rows_of_any_stride_that_do_not_overlap():
     assert append_args(rows(1, 2, 64).expand(1, 2, 64)).k_row_stride == 0
 
 
-@pytest.mark.parametrize("R", [2, 700])
+@pytest.mark.parametrize("R", [2, 200])
 def test_append_refuses_broadcast_rows(R):
     """A row stride of 0 would read as dense rows, past the one row that there is."""
     one = rows(1, 2, 64).expand(R, 2, 64)
