@@ -95,6 +95,47 @@ __device__ __forceinline__ bool pair_any(int bar, bool any) {
   return r != 0;
 }
 
+// a of e = a * S + b for a page's keys; a is not 0, so that a * -inf stays -inf.
+__device__ __forceinline__ float slope(float ks, float qf) {
+  const float a = ks * qf;
+  return a == 0.f ? 1.17549435e-38f : a;
+}
+
+// The weights of half a tile for rows whose reference is past kFar, in place of the kernel's own
+// loop: that takes the reference off a product that is not rounded, while the largest exponent
+// was rounded, by up to 0.25 there and by thousands far past it. Here the exponents are rounded like
+// the largest before the reference is taken off, so that none passes it. Returns l plus their sum.
+constexpr float kFar = 4194304.f;  // 2^22
+template <int HP>
+__device__ __forceinline__ float far_weights(uint32_t s_col, int first, const float4* sc, int psh, float qf, float m,
+                                             float l) {
+#pragma unroll 1
+  for (int c0 = first; c0 < first + HK; c0 += 32) {
+    uint32_t w[24];
+#pragma unroll
+    for (int c8 = 0; c8 < 32; c8 += 8) {  // few registers: this is the rare case
+      uint32_t r[8];
+      tmem_ld8(s_col + c0 + c8, r);
+      const float4 q = sc[((c0 + c8) >> psh) * HP];
+      const float a = slope(q.x, qf);
+      tmem_wait_ld();
+#pragma unroll
+      for (int c = 0; c < 8; c += 4) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = ex2(fmaf(__uint_as_float(r[c + i]), a, q.y) - m);
+          l = fmaf(p[i], q.z, l);
+        }
+        split_weights<false>(p, w[(c8 + c) / 4], w[8 + (c8 + c) / 4], w[16 + (c8 + c) / 4]);
+      }
+    }
+    tmem_st16(s_col + c0, w);
+    tmem_st8(s_col + c0 + 16, w + 16);
+  }
+  return l;
+}
+
 template <int D, int HP>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_fp8_rows_kernel(const __grid_constant__ CUtensorMap tmap, AttnFp8Params p) {
@@ -355,11 +396,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tmem_wait_st();
           }
-          // e = a * S + b of a page's keys; a is not 0, so that a * -inf stays -inf
-          auto slope = [&](float ks) {
-            const float a = ks * qf;
-            return a == 0.f ? 1.17549435e-38f : a;
-          };
           // ---- the largest weighted exponent of this thread's half of the row ----
           float top = -INFINITY;
 #pragma unroll
@@ -373,11 +409,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               float t = __uint_as_float(r[g]);
 #pragma unroll
               for (int c = 1; c < 16; ++c) t = fmaxf(t, __uint_as_float(r[g + c]));
-              top = fmaxf(top, fmaf(t, slope(q.x), q.y));
+              top = fmaxf(top, fmaf(t, slope(q.x, qf), q.y));
             }
           }
-          // ---- raise the reference where a weight would pass 2^15 ----
-          if (pair_any(pbar, top > m + 15.f || (m == -INFINITY && top > -INFINITY))) {
+          // ---- raise the reference where a weight would pass 2^15 (and at references past kFar) ----
+          bool weighed = false;
+          if (pair_any(pbar, top > m + 15.f || (fabsf(m) > kFar && top > -INFINITY))) {
             xch[ch * MR + row] = top;
             bar_sync(pbar, 64);
             top = fmaxf(xch[row], xch[MR + row]);
@@ -400,9 +437,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             m = now;
             bar_sync(pbar, 64);  // xch is read
+            if (__any_sync(0xffffffffu, fabsf(m) > kFar && m != -INFINITY)) {
+              l = far_weights<HP>(s_col, ch * HK, sc, psh, qf, m == -INFINITY ? 0.f : m, l);
+              weighed = true;
+            }
           }
           // ---- weights, their sum, and their three terms over the columns of S ----
           const float msub = m == -INFINITY ? 0.f : m;
+          if (!weighed)
 #pragma unroll 1
           for (int c0 = ch * HK; c0 < ch * HK + HK; c0 += 32) {
             uint32_t r[32], w[24];
@@ -412,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
               const float4 q = sc[((c0 + 16 * g) >> psh) * HP];
-              ab[g] = make_float2(slope(q.x), q.y - msub);
+              ab[g] = make_float2(slope(q.x, qf), q.y - msub);
               inv_sv[g] = q.z;
             }
             tmem_wait_ld();

@@ -87,16 +87,17 @@ __device__ __forceinline__ void split_e4m3x4(float a, float b, float c, float d,
       : "r"(x), "r"(y));
 }
 
-// The three e5m2 terms of four weights in [0, 2^15], each packed in order from the low byte. A
+// The three e5m2 terms of four weights in [0, 2^15] (2^16 where scores are so large that their steps
+// are 16, taken as 65504), each packed in order from the low byte. A
 // weight is rounded to fp16, whose upper byte is an e5m2 number: that byte, the upper byte of
 // what is left of it, and what is left then, rounded, are the terms: 3 + 3 + 3 bits, off by at most
 // 2^-9 + 2^-11 of the weight. UP: the third terms times 32, so that their smallest step is 2^-21 of 1
-// instead of 2^-16 (they stay below 2^15).
+// instead of 2^-16 (they stay below 2^16).
 template <bool UP>
 __device__ __forceinline__ void split_weights(const float* p, uint32_t& w1, uint32_t& w2, uint32_t& w3) {
   uint32_t x, y, r, s;
-  asm("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(x) : "f"(p[0]), "f"(p[1]));
-  asm("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(y) : "f"(p[2]), "f"(p[3]));
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %2, %1;" : "=r"(x) : "f"(p[0]), "f"(p[1]));
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %2, %1;" : "=r"(y) : "f"(p[2]), "f"(p[3]));
   w1 = __byte_perm(x, y, 0x7531);
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(x & 0xff00ff00u));
   asm("sub.f16x2 %0, %1, %2;" : "=r"(s) : "r"(y), "r"(y & 0xff00ff00u));
