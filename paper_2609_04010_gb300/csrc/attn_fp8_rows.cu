@@ -19,7 +19,7 @@
 // at its softmax, the tensor core works for the other. m is set so that a row's largest P is
 // 2^11.5 to 2^12.5 and raised when a P would pass 2^15 (the terms add up in one accumulator, so
 // the third one's smallest step is 2^-16: a P is off by 2^-28 of the row's largest at most). The
-// third product costs 0.2 us a tile (batch 4, 32,768 keys: 165 us; 153 with two e4m3 terms, which
+// third product costs 0.2 us a tile (batch 4, 32,768 keys: 165 us against 153 with two e4m3 terms, which
 // lost the weights below 2^-14 of the largest: 0.77 of an output where attn_fp8_keys.cu lost
 // 0.63). m is a whole number, so that log2(sv) - m is exact with power-of-two scales. Hidden scores
 // are set to -inf in TMEM, before the two passes over a tile (the maximum, the weights), which then
@@ -33,7 +33,7 @@
 // What bounds it is the chain S, softmax, P V of a sub-unit: 2.6 us a tile of 128 keys, of which
 // its softmax is about 1.3 (the conversions and ex2 take 0.5 of it) and the products 0.7; two
 // sub-units, all that TMEM has room for with D = 128, do not cover each other fully. Batch 4, block
-// 32, 64 / 8 heads, 32,768 keys take 165 us: 833 TFLOP/s of Q K^T and P V, two and a half times that
+// 32, 64 / 8 heads, 32,768 keys take 166 us: 828 TFLOP/s of Q K^T and P V, two and a half times that
 // on the tensor cores. With two terms a weight (155 us) half tiles with scores in two buffers (231),
 // four threads a row (158) and weights taken before the maximum is known (276) were all slower.
 // Batch 64, block 16, 32 / 8 heads, contexts 512 to 4,096: 113 us, 2.8 TB/s.
@@ -105,6 +105,7 @@ __device__ __forceinline__ float slope(float ks, float qf) {
 // loop: that takes the reference off a product that is not rounded, while the largest exponent
 // was rounded, by up to 0.25 there and by thousands far past it. Here the exponents are rounded like
 // the largest before the reference is taken off, so that none passes it. Returns l plus their sum.
+// (Done for all references it takes 171 us at batch 4 and 32,768 keys; as it is, 166.)
 constexpr float kFar = 4194304.f;  // 2^22
 template <int HP>
 __device__ __forceinline__ float far_weights(uint32_t s_col, int first, const float4* sc, int psh, float qf, float m,
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           // ---- weights, their sum, and their three terms over the columns of S ----
           const float msub = m == -INFINITY ? 0.f : m;
-          if (!weighed)
+          if (!weighed)  // by far_weights
 #pragma unroll 1
           for (int c0 = ch * HK; c0 < ch * HK + HK; c0 += 32) {
             uint32_t r[32], w[24];
