@@ -636,7 +636,7 @@ spec_status_t spec_append_kv_fp8(const spec_append_fp8_args_t* append, spec_stre
  * 2^-28 of the largest such product of its row.
  * path: SPEC_ATTN_AUTO takes the tensor cores where the call fits them (32-bit counts of
  * key tiles and cache rows), else CUDA cores; SPEC_ATTN_TENSOR_CORES is
- * SPEC_ERR_UNSUPPORTED where it does not fit. Two launches per 1,000 sequences on the tensor
+ * SPEC_ERR_UNSUPPORTED where it does not fit. Two launches per 2,048 sequences on the tensor
  * cores, one on CUDA cores. The workspace rules are spec_verify_attention's.
  */
 typedef struct {

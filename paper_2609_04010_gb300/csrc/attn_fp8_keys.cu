@@ -69,7 +69,9 @@ struct Cfg {
   static constexpr uint32_t Q_TERM = NR * D;               // one term of one sub-unit's Q
   static constexpr uint32_t PW = 4 * NR;                   // a key's weights: first, second, third terms, unused
   static constexpr uint32_t P_BUF = TK * PW;               // [key][PW], swizzled by its width
-  static constexpr int NST = ((NR == 16 && HP * D >= 128 ? 216 : 208) * 1024 - NH * (P_BUF + 2 * Q_TERM)) / STAGE;  // D = 128, HP = 2: 3 or 2
+  // where a stage fits for it, the work list's first tiles are those of every second sequence
+  static constexpr int EACH = NR == 16 && HP * D >= 128 ? 2 : 1;
+  static constexpr int NST = ((EACH == 2 ? 216 : 208) * 1024 - NH * (P_BUF + 2 * Q_TERM)) / STAGE;  // D = 128, HP = 2: 3 or 2
   static constexpr uint32_t OFF_STAGE = 0;
   static constexpr uint32_t OFF_P = OFF_STAGE + NST * STAGE;
   static constexpr uint32_t OFF_Q = OFF_P + NH * P_BUF;
@@ -87,14 +89,14 @@ struct Cfg {
   // full[NST], empty[NST], s_full[NH][SB], s_free[NH][SB], p_full[NH], pv_done[NH],
   // seg_ready[NH], drain[2], flag_ready[kFlagRing]
   static constexpr int NBAR = 2 * NST + 2 * NH * SB + 3 * NH + 2 + kFlagRing;
-  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, -, -, NaN flags
-  static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;               // int [2][kFlagRing]: segments' bad flags
-  static constexpr uint32_t OFF_PB = OFF_FLAG + 8 * kFlagRing;       // int [batch + 1]
+  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, NaN flags
+  static constexpr uint32_t OFF_FLAG = OFF_MISC + 16;               // int [2][kFlagRing]: segments' bad flags
+  static constexpr uint32_t OFF_PB = OFF_FLAG + 8 * kFlagRing;       // int [list_entries<EACH>(batch)]
   static constexpr uint32_t S_COL = 0;                      // [NH][SB][NR]
   static constexpr uint32_t O_COL = NH * SB * NR;           // [NH][first, second, third terms][NR]
   static constexpr uint32_t TMEM_COLS = NR == 16 ? 256 : 512;
   static_assert(NH * (SB + 3) * NR <= TMEM_COLS, "a power of two of columns");
-  static constexpr size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
+  static constexpr size_t smem_bytes(int batch) { return OFF_PB + 4u * list_entries<EACH>(batch) + 1024; }
 };
 
 // ---------------------------------------------------------------------------------
@@ -170,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned long long* nanv = reinterpret_cast<unsigned long long*>(smem + C::OFF_NAN);
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
-  volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 4);  // [NH]
+  volatile int* nan_flag = reinterpret_cast<volatile int*>(misc + 2);  // [NH]
   volatile int* seg_flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);  // [producer][kFlagRing]
   int* pb = reinterpret_cast<int*>(smem + C::OFF_PB);
 
@@ -199,17 +201,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 32 * kSoftWarps)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap)) : "memory");
   pdl_wait_prior();
-  if (warp == kSoftWarps) prefix_tiles(p, pb);
+  if (warp == kSoftWarps) prefix_tiles<C::EACH>(p, pb);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = misc[0];
-  const WorkList w = work_list(p, pb);
+  const WorkList<C::EACH> w = work_list<C::EACH>(p, pb);
   if (threadIdx.x == 0) clear_split(p);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 3) {
     // ============================ producers ============================
-    produce<D, HP, NST>(p, tmap, w, warp == kSoftWarps ? 0 : 1, sbase + C::OFF_STAGE, full(0), empty(0), flag_bar(0), scl,
+    produce<D, HP, NST, C::EACH>(p, tmap, w, warp == kSoftWarps ? 0 : 1, sbase + C::OFF_STAGE, full(0), empty(0), flag_bar(0), scl,
                         seg_flag, abort_flag);
   } else if (warp == kSoftWarps + 1) {
     // ============================ S^T = K Q^T ============================

@@ -66,12 +66,12 @@ struct Cfg {
   static constexpr int NBAR = 2 * NST + 4 * NH + 1 + kFlagRing;
   static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;        // tmem base, abort, -, -, NaN flags
   static constexpr uint32_t OFF_FLAG = OFF_MISC + 32;             // int [2][kFlagRing]: segments' bad flags
-  static constexpr uint32_t OFF_PB = OFF_FLAG + 8 * kFlagRing;               // int [batch + 1]
+  static constexpr uint32_t OFF_PB = OFF_FLAG + 8 * kFlagRing;               // int [list_entries<1>(batch)]
   static constexpr uint32_t S_COL = 0;                            // [NH][128]; P over it
   static constexpr uint32_t O_COL = NH * TK;                      // [NH][D]
   static constexpr uint32_t TMEM_COLS = 512;
   static_assert(O_COL + NH * D <= TMEM_COLS, "TMEM holds 512 columns");
-  static constexpr size_t smem_bytes(int batch) { return OFF_PB + 4u * (batch + 1) + 1024; }
+  static constexpr size_t smem_bytes(int batch) { return OFF_PB + 4u * list_entries<1>(batch) + 1024; }
 };
 
 // The same with A in tensor memory (M rows on the lanes, four bytes of K per column).
@@ -187,17 +187,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 32 * kSoftWarps)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap)) : "memory");
   pdl_wait_prior();
-  if (warp == kSoftWarps) prefix_tiles(p, pb);
+  if (warp == kSoftWarps) prefix_tiles<1>(p, pb);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = misc[0];
-  const WorkList w = work_list(p, pb);
+  const WorkList<1> w = work_list<1>(p, pb);
   if (threadIdx.x == 0) clear_split(p);
 
   if (warp == kSoftWarps || warp == kSoftWarps + 2) {
     // ============================ producers ============================
-    produce<D, HP, NST>(p, tmap, w, warp == kSoftWarps ? 0 : 1, sbase + C::OFF_STAGE, full(0), empty(0), flag_bar(0), scl,
+    produce<D, HP, NST, 1>(p, tmap, w, warp == kSoftWarps ? 0 : 1, sbase + C::OFF_STAGE, full(0), empty(0), flag_bar(0), scl,
                         seg_flag, abort_flag);
   } else if (warp == kSoftWarps + 1) {
     // ============================ products ============================

@@ -120,26 +120,35 @@ static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, vol
 // ---------------------------------------------------------------------------------
 // The work list: the tiles of all units, cut into equal ranges, one per block
 // ---------------------------------------------------------------------------------
+// First tiles are kept of each EACH-th sequence, 1 or 2: that of a sequence in between follows from
+// the lengths that find() reads anyway, and half the entries leave shared memory for a stage.
+template <int EACH>
+__host__ __device__ constexpr int list_entries(int batch) { return (batch + EACH - 1) / EACH + 1; }
+
+template <int EACH>
 struct WorkList {
   int64_t t0, t1, total;  // this block's range, and the list's length
-  const int* pb;          // [batch + 1]: first tile of each sequence
+  const int* pb;          // [list_entries<EACH>(batch)]: first tiles, and the total
   int ovh, ctas, cta;
 };
 
+__device__ __forceinline__ int sequence_tiles(int kv_len, const AttnParams& p) {
+  return (unit_tiles<TK>(kv_len, p) + p.unit_overhead) * p.hunits * p.row_tiles;
+}
 // First tiles of the sequences (one warp).
+template <int EACH>
 __device__ __forceinline__ void prefix_tiles(const AttnParams& p, int* pb) {
   const int lane = threadIdx.x & 31;
-  const int per_b = p.hunits * p.row_tiles;
   int carry = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
     const int b = b0 + lane;
-    int v = b < p.batch ? (unit_tiles<TK>(p.kv_len[b], p) + p.unit_overhead) * per_b : 0;
+    int v = b < p.batch ? sequence_tiles(p.kv_len[b], p) : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, v, o);
       if (lane >= o) v += y;
     }
-    if (b < p.batch) pb[b + 1] = carry + v;
+    if (b < p.batch && ((b + 1) % EACH == 0 || b + 1 == p.batch)) pb[b / EACH + 1] = carry + v;
     carry += __shfl_sync(0xffffffffu, v, 31);
   }
   if (lane == 0) pb[0] = 0;
@@ -148,11 +157,12 @@ __device__ __forceinline__ void prefix_tiles(const AttnParams& p, int* pb) {
 // Equal ranges on every SM (a multiple of the units, so that equal units have no boundary
 // inside a range, measured slower before units were joined over all SMs: 135.8 against 123.2 us
 // with 128 ragged units, 232 against 226 with 64 equal ones).
-__device__ __forceinline__ WorkList work_list(const AttnParams& p, const int* pb) {
-  WorkList w;
+template <int EACH>
+__device__ __forceinline__ WorkList<EACH> work_list(const AttnParams& p, const int* pb) {
+  WorkList<EACH> w;
   w.pb = pb;
   w.ovh = p.unit_overhead;
-  w.total = pb[p.batch];
+  w.total = pb[list_entries<EACH>(p.batch) - 1];
   w.ctas = static_cast<int>(w.total < gridDim.x ? w.total : gridDim.x);
   w.cta = blockIdx.x;
   w.t0 = w.cta < w.ctas ? static_cast<int64_t>(w.cta) * w.total / w.ctas : 0;
@@ -161,23 +171,33 @@ __device__ __forceinline__ WorkList work_list(const AttnParams& p, const int* pb
 }
 
 // locate() in 32 bits (a list has at most INT32_MAX tiles).
-__device__ __forceinline__ Seg find(int64_t at, const WorkList& w, const AttnParams& p) {
+template <int EACH>
+__device__ __forceinline__ Seg find(int64_t at, const WorkList<EACH>& w, const AttnParams& p) {
   const int v = static_cast<int>(at), v1 = static_cast<int>(w.t1);
-  int lo = 0, hi = p.batch;  // largest b with pb[b] <= v
+  int lo = 0, hi = list_entries<EACH>(p.batch) - 1;  // largest entry with pb[lo] <= v
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (w.pb[mid] <= v) lo = mid; else hi = mid;
   }
+  int rem = v - w.pb[lo];  // tiles from the sequence's first
   Seg s;
-  s.b = lo;
-  s.kv_len = p.kv_len[lo];
+  s.b = EACH * lo;
+  s.kv_len = p.kv_len[s.b];
+  if constexpr (EACH == 2) {
+    const int next_len = s.b + 1 < p.batch ? p.kv_len[s.b + 1] : 0, tiles = sequence_tiles(s.kv_len, p);
+    if (rem >= tiles) {
+      rem -= tiles;
+      ++s.b;
+      s.kv_len = next_len;
+    }
+  }
   s.len_ok = s.kv_len >= p.gamma && s.kv_len <= p.max_keys;
   s.unit_tiles = unit_tiles<TK>(s.kv_len, p);
-  const uint32_t vlen = s.unit_tiles + w.ovh, rem = v - w.pb[lo], ub = rem / vlen;
+  const uint32_t vlen = s.unit_tiles + w.ovh, ub = static_cast<uint32_t>(rem) / vlen;
   const int real = v - static_cast<int>(rem - ub * vlen) + w.ovh;  // the unit's first real tile
   s.g = p.row_tiles == 1 ? ub : ub / p.row_tiles;
   s.rt = p.row_tiles == 1 ? 0 : ub - s.g * p.row_tiles;
-  s.u = static_cast<int64_t>(lo) * p.hunits * p.row_tiles + ub;
+  s.u = static_cast<int64_t>(s.b) * p.hunits * p.row_tiles + ub;
   s.unit_start = real;
   const int next = min(real + s.unit_tiles, v1), from = max(v, real);
   s.vnext = next;
@@ -196,7 +216,8 @@ __device__ __forceinline__ int part_slot(int cta, bool starts) { return 2 * cta 
 __device__ __forceinline__ void clear_split(const AttnFp8Params& p) {
   if (!p.split_by_unit) p.splits[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
 }
-__device__ __forceinline__ void note_split(const AttnFp8Params& p, const Seg& s, const WorkList& w, int tile_rows) {
+template <int EACH>
+__device__ __forceinline__ void note_split(const AttnFp8Params& p, const Seg& s, const WorkList<EACH>& w, int tile_rows) {
   const bool split = s.tile0 > 0;
   if (s.tile0 + s.ntile != s.unit_tiles || (!split && !p.split_by_unit)) return;
   const int first = split ? owner_of(s.unit_start, w.total, w.ctas) : 0, row0 = s.rt * tile_rows;
@@ -239,8 +260,8 @@ cudaError_t launch_merge(const AttnFp8Params& p, const AttnFp8Plan& P, cudaStrea
 // A producer warp: the half of each tile's pages, one TMA box each, and their scales as
 // scl[stage][page of the tile][head] = (sk * softmax scale * log2(e), log2(sv), 1 / sv, -).
 // Two of them, because one keeps the copy engine waiting.
-template <int D, int HP, int NST>
-__device__ __forceinline__ void produce(const AttnFp8Params& p, const CUtensorMap& tmap, const WorkList& w, int half,
+template <int D, int HP, int NST, int EACH>
+__device__ __forceinline__ void produce(const AttnFp8Params& p, const CUtensorMap& tmap, const WorkList<EACH>& w, int half,
                                         uint32_t stages, uint32_t full, uint32_t empty, uint32_t flag_ready,
                                         float4* scl, volatile int* seg_flag, volatile int* abort_flag) {
   const int lane = threadIdx.x & 31;

@@ -29,7 +29,7 @@ struct AttnFp8Plan {
 AttnFp8Plan attn_fp8_plan(const spec_attn_fp8_args_t& a, size_t base, int num_sms, int path);
 constexpr int kFp8MaxRows = 2147483647 - 255;  // query rows of a KV head: 32-bit counts, in tiles of 256
 constexpr int kFp8KeyTile = 128;   // keys per tile of the tensor-core kernels
-constexpr int kFp8TcBatch = 1000;  // sequences they take in a launch
+constexpr int kFp8TcBatch = 2048;  // sequences they take in a launch
 // starve (test hook only): the producers issue no copies, so the bounded waits run out.
 cudaError_t launch_attn_fp8_keys(const spec_attn_fp8_args_t& a, const AttnFp8Plan& P, char* ws,
                                  cudaStream_t stream, bool starve = false);
