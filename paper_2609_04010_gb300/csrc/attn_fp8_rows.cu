@@ -36,7 +36,7 @@
 // 32, 64 / 8 heads, 32,768 keys take 166 us: 828 TFLOP/s of Q K^T and P V, two and a half times that
 // on the tensor cores. With two terms a weight (155 us) half tiles with scores in two buffers (231),
 // four threads a row (158) and weights taken before the maximum is known (276) were all slower.
-// Batch 64, block 16, 32 / 8 heads, contexts 512 to 4,096: 113 us, 2.8 TB/s.
+// Batch 64, block 16, 32 / 8 heads, contexts 512 to 4,096: 115 us, 2.8 TB/s.
 #include "attn_fp8_tc.cuh"
 
 namespace specv {
