@@ -704,6 +704,176 @@ typedef struct {
 spec_status_t spec_adjust_logits(const spec_adjust_args_t* adjust, spec_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Ragged batches of new tokens: prompts, single tokens and blocks together
+ *
+ * A batch packed by sequence, as spec_map_slots lays it out: rows row_start[b] ..
+ * row_start[b+1] - 1 are sequence b's new tokens, the last of its kv_len[b] tokens.
+ * ------------------------------------------------------------------------------------- */
+
+/*
+ * Rotary positions of queries and keys, and the write of keys and values into the paged bf16
+ * cache. The first rot_dim elements of each head of row r rotate in pairs, (x[i], x[i +
+ * rot_dim/2]) or, with interleaved = 1, (x[2i], x[2i+1]), i < rot_dim/2:
+ *   (x1, x2) -> factor * (x1 cos a - x2 sin a, x2 cos a + x1 sin a),
+ *   a = 2 pi * positions[r] * turns[i] / 2^64,
+ * the other elements stay. turns[i] is a frequency in turns per position, as a fraction of 2^64
+ * (its whole turns dropped), so that angles are exact to 2^-25 of a turn at every position.
+ *   - q -> q_out and k -> k_out (each may be its input); a pair that is not given is left out.
+ *   - With slots, the rotated key and the value of row r go to slot slots[r] of the cache (page
+ *     slots[r] / page_size, place slots[r] % page_size; k_out may then be NULL); negative slots
+ *     are skipped; one at or past num_pages * page_size is skipped and sets SPEC_FLAG_BAD_PAGE in
+ *     *status (if given). No two rows of a call have one slot. For the 8-bit cache the rotated
+ *     keys go to k_out, which spec_append_kv_fp8 takes.
+ *   - A row with a negative position is left out altogether.
+ *   - Sines, products and sums are fp32, results rounded once to bf16.
+ * One launch, no workspace; with rows = 0 nothing is read.
+ */
+typedef struct {
+  int32_t rows, num_q_heads, num_kv_heads, head_dim;  /* head_dim 64 or 128                   */
+  int32_t rot_dim;              /* a multiple of 16, at most head_dim                         */
+  int32_t interleaved;          /* 0: halves; 1: adjacent pairs                               */
+  float factor;                 /* of the rotated elements; 0 => 1                            */
+  int32_t page_size, num_pages; /* of the cache (with slots); page_size 16, 32 or 64          */
+  int64_t q_row_stride, k_row_stride, v_row_stride, q_out_row_stride, k_out_row_stride;
+                                /* elements from one row to the next, multiples of 8; 0: dense */
+  const void* q;                /* bf16 rows of [num_q_heads][head_dim], 16-byte aligned, or NULL */
+  const void* k;                /* bf16 rows of [num_kv_heads][head_dim], or NULL             */
+  const void* v;                /* likewise (with slots), or NULL                             */
+  const int32_t* positions;     /* [rows]                                                     */
+  const uint64_t* turns;        /* [rot_dim / 2]                                              */
+  void* q_out;                  /* with q, written                                            */
+  void* k_out;                  /* written, or NULL                                           */
+  const int32_t* slots;         /* [rows], or NULL: no cache                                  */
+  void* k_cache;                /* bf16 [num_pages][Hkv][page_size][D], updated (with slots)  */
+  void* v_cache;                /* likewise                                                   */
+  uint32_t* status;             /* a status word (e.g. a workspace's first word), or NULL     */
+} spec_rope_args_t;
+
+spec_status_t spec_rope_kv(const spec_rope_args_t* rope, spec_stream_t stream);
+
+/*
+ * Attention of a ragged batch of new tokens over the paged cache, bf16 (k_cache, v_cache) or
+ * 8-bit (kv_cache, kv_scale). Row row_start[b] + j is the token at position kv_len[b] - n_b + j
+ * of sequence b, n_b = row_start[b+1] - row_start[b] >= 0; its own key and value are in the cache
+ * already. With t its position, head h of it sees the keys k of KV head h / (Hq / Hkv) with
+ *   k <= t (causal = 1) or k < kv_len[b] (causal = 0: the new tokens see each other from both
+ *   sides, as in a drafter's pass over its block), and, with window > 0, k > t - window;
+ *   out = sum_k softmax_k(scale * q.k_k) v_k, lse = log sum_k exp(scale * q.k_k) (natural log).
+ *   - What a row's mask hides does not reach it, whatever the bytes there, and page ids that only
+ *     hidden keys use are not looked at. A row whose visible scores are all -inf gets out = NaN
+ *     and lse = -inf.
+ *   - Rows past row_start[batch] are not written. A sequence whose rows do not lie in
+ *     [0, rows) in order is left out; one with rows but kv_len[b] outside [n_b,
+ *     max_pages_per_seq * page_size] gets out = 0 and lse = -inf (both SPEC_FLAG_BAD_KV_LEN), as
+ *     does one with a visible key's page id outside [0, num_pages) (SPEC_FLAG_BAD_PAGE).
+ *   - Scores, softmax statistics and accumulators are fp32; on the tensor cores a weight enters
+ *     its product rounded to bf16, relative to the row's largest of at least 2^-8 of its range.
+ *     Values of the 8-bit cache enter as their bf16 value times scale, exact for the powers of
+ *     two that spec_append_kv_fp8 writes; value scales are clamped to [2^-32, 2^32].
+ *   - path: SPEC_ATTN_AUTO takes the tensor cores where the call fits them (Hq / Hkv at most 128),
+ *     else CUDA cores; SPEC_ATTN_TENSOR_CORES is SPEC_ERR_UNSUPPORTED where it does not fit.
+ *   - Three launches. The workspace rules are spec_verify_attention's.
+ */
+typedef struct {
+  int32_t batch;              /* >= 1                                                       */
+  int32_t rows;               /* >= 0: rows of q, out and lse                               */
+  int32_t num_q_heads;        /* a multiple of num_kv_heads                                 */
+  int32_t num_kv_heads;
+  int32_t head_dim;           /* 64 or 128                                                  */
+  int32_t page_size;          /* 16, 32 or 64                                               */
+  int32_t max_pages_per_seq;
+  int32_t num_pages;
+  int32_t causal;             /* 0 or 1                                                     */
+  int32_t window;             /* keys a token sees up to its own, or 0: all                 */
+  float softmax_scale;        /* 0 => 1/sqrt(head_dim)                                      */
+  int32_t path;               /* spec_attn_path_t, without KEYS_ON_LANES                    */
+  int64_t q_row_stride;       /* elements from one row of q to the next, a multiple of 8; 0: dense */
+  const void* q;              /* bf16 rows of [Hq][D], 16-byte aligned                      */
+  const void* k_cache;        /* bf16 [num_pages][Hkv][page_size][D], 16-byte aligned, or NULL */
+  const void* v_cache;        /* likewise                                                   */
+  const void* kv_cache;       /* the 8-bit cache, 16-byte aligned, or NULL                  */
+  const float* kv_scale;      /* its scales, 8-byte aligned, or NULL                        */
+  const int32_t* page_table;  /* [batch][max_pages_per_seq]; entries past the sequence unread */
+  const int32_t* row_start;   /* [batch + 1]                                                */
+  const int32_t* kv_len;      /* [batch]: keys in the cache, the new ones included          */
+  void* out;                  /* bf16 [rows][Hq][D], 16-byte aligned                        */
+  float* lse;                 /* fp32 [rows][Hq], or NULL                                   */
+} spec_chunk_attn_args_t;
+
+size_t spec_chunk_attn_workspace_size(const spec_chunk_attn_args_t* attn);
+spec_status_t spec_chunk_attention(const spec_chunk_attn_args_t* attn, void* ws, size_t ws_bytes,
+                                   spec_stream_t stream);
+
+/*
+ * Sequences that go on from others, end, or stay: parallel samples of a prompt, beams, and the end
+ * of requests. New sequence b goes on from what sequence parent[b] was before the call; -1: b is
+ * empty afterwards; parent[b] = b: b stays as it is.
+ *   - Of the sequences with one parent, the parent itself, else the lowest, takes over all of its
+ *     pages. Each other one is a fork: it holds the parent's whole pages with it (the first
+ *     kv_len / page_size) and takes new pages from the top of the free list for the rest of the
+ *     kv_len + reserved tokens (reserved as in spec_map_slots). Where the parent's last page is
+ *     partly filled, copies[b] = (that page, the fork's first new page), else (-1, -1):
+ *     spec_copy_pages makes the copies in every layer's cache, before either page is written.
+ *   - shares[page] counts a page's holders past the first (0 for a page that one sequence or none
+ *     holds; spec_map_slots and spec_commit_kv take and release pages that only one holds, so they
+ *     need not know it: a fork's tokens go behind the whole pages, and no rollback goes before it).
+ *   - A sequence that nobody goes on from gives up its pages: those with no holder left go to the
+ *     free list, on top of what the forks left, in the order of (sequence, place), a page that
+ *     several of them held at the last such place. Forks are served from the list as it was
+ *     before, in batch order while their running total fits it; a refused one still counts against
+ *     the later ones and is empty afterwards.
+ *   - flags[b]: 0; 1: parent[b] outside [-1, batch), or kv_len of b or of its parent negative or
+ *     with reserved above max_pages_per_seq * page_size: b stays as it is; 2: refused.
+ *   - Table entries past what a changed sequence holds become -1. Page ids outside [0, num_pages)
+ *     are handed on and counted nowhere.
+ *   - Each new_ array may be the one that is read.
+ * One launch of one thread-block cluster, whose blocks run, and wait for each other, together;
+ * batch <= SPEC_SLOTS_MAX_BATCH.
+ */
+typedef struct {
+  int32_t batch, page_size, max_pages_per_seq, num_pages;
+  int32_t reserved;             /* >= 0: tokens past kv_len whose pages the table holds       */
+  int32_t free_capacity;        /* entries of free_pages, at least num_pages                  */
+  const int32_t* parent;        /* [batch]                                                    */
+  const int32_t* kv_len;        /* [batch]                                                    */
+  int32_t* new_kv_len;          /* [batch], written                                           */
+  const int32_t* page_table;    /* [batch][max_pages_per_seq]                                 */
+  int32_t* new_table;           /* likewise, written                                          */
+  const int32_t* shares;        /* [num_pages]                                                */
+  int32_t* new_shares;          /* [num_pages], written                                       */
+  const int32_t* free_pages;    /* [free_capacity]: the free list, its top at free_count      */
+  int32_t* new_free_pages;      /* [free_capacity], written                                   */
+  const int32_t* free_count;    /* [1], clamped to [0, free_capacity]                         */
+  int32_t* new_free_count;      /* [1], written                                               */
+  int32_t* copies;              /* [batch][2], written                                        */
+  int32_t* flags;               /* [batch], written, or NULL                                  */
+} spec_fork_args_t;
+
+size_t spec_fork_workspace_size(const spec_fork_args_t* fork);
+spec_status_t spec_fork_sequences(const spec_fork_args_t* fork, void* ws, size_t ws_bytes,
+                                  spec_stream_t stream);
+
+/*
+ * Copies whole pages within each of num_buffers caches (K and V of all layers, 8-bit caches,
+ * their scales): for every pair (source, destination), page `source` of each buffer to page
+ * `destination`. Pairs of two negative entries are skipped; one with a page outside
+ * [0, num_pages) is skipped and sets SPEC_FLAG_BAD_PAGE in *status (if given). Sources may
+ * repeat; a destination is neither another pair's destination nor any pair's source (else those
+ * pages hold unspecified values). One launch, no workspace. buffers and page_bytes are host
+ * arrays, read during the call.
+ */
+#define SPEC_COPY_MAX_BUFFERS 128
+typedef struct {
+  int32_t num_pairs, num_pages, num_buffers;
+  const int32_t* pairs;         /* [num_pairs][2]                                             */
+  void* const* buffers;         /* [num_buffers] on the host: device memory, 4-byte aligned, updated */
+  const int64_t* page_bytes;    /* [num_buffers] on the host: bytes of a page, multiples of 4 */
+  uint32_t* status;             /* a status word (e.g. a workspace's first word), or NULL     */
+} spec_copy_args_t;
+
+spec_status_t spec_copy_pages(const spec_copy_args_t* copy, spec_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
  * Test hooks for the timeout path (not part of the verify step)
  *
  * The kernels' internal waits on asynchronous copies and tensor-core operations are

@@ -9,6 +9,7 @@ exist (``python -m paper_2609_04010_gb300.build``); there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import re
 import threading
@@ -31,6 +32,7 @@ FLAG_BAD_TOKEN, FLAG_BAD_LOGITS, FLAG_BAD_PAGE, FLAG_BAD_KV_LEN, FLAG_TIMEOUT = 
 FLAG_BAD_FILTER = 32
 FLAG_BAD_TREE = 64
 FILTER_MAX_TOP_K = 1024
+COPY_MAX_BUFFERS = 128
 
 
 class SpecError(RuntimeError):
@@ -165,6 +167,55 @@ class AdjustArgs(ctypes.Structure):
                 ("bias_values", ctypes.c_void_p), ("allowed", ctypes.c_void_p)]
 
 
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("factor", ctypes.c_float), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("q_row_stride", ctypes.c_int64),
+                ("k_row_stride", ctypes.c_int64), ("v_row_stride", ctypes.c_int64),
+                ("q_out_row_stride", ctypes.c_int64), ("k_out_row_stride", ctypes.c_int64),
+                ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("turns", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p),
+                ("status", ctypes.c_void_p)]
+
+
+class ChunkAttnArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("path", ctypes.c_int32),
+                ("q_row_stride", ctypes.c_int64), ("q", ctypes.c_void_p),
+                ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p),
+                ("kv_cache", ctypes.c_void_p), ("kv_scale", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p)]
+
+
+class ForkArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("free_capacity", ctypes.c_int32),
+                ("parent", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("new_kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("new_table", ctypes.c_void_p), ("shares", ctypes.c_void_p),
+                ("new_shares", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("new_free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+                ("new_free_count", ctypes.c_void_p), ("copies", ctypes.c_void_p),
+                ("flags", ctypes.c_void_p)]
+
+
+class CopyArgs(ctypes.Structure):
+    _fields_ = [("num_pairs", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("num_buffers", ctypes.c_int32), ("pairs", ctypes.c_void_p),
+                ("buffers", ctypes.c_void_p), ("page_bytes", ctypes.c_void_p),
+                ("status", ctypes.c_void_p)]
+
+
 HEADER = os.path.join(_build.ROOT, "include", "spec_verify.h")
 
 
@@ -232,6 +283,15 @@ def lib(build_if_missing: bool = True):
             for f in ("spec_slot_workspace_size", "spec_attn_fp8_workspace_size"):
                 getattr(L, f).argtypes = [P]
                 getattr(L, f).restype = ctypes.c_size_t
+            for f in ("spec_chunk_attn_workspace_size", "spec_fork_workspace_size"):
+                getattr(L, f).argtypes = [P]
+                getattr(L, f).restype = ctypes.c_size_t
+            for f in ("spec_chunk_attention", "spec_fork_sequences"):
+                getattr(L, f).argtypes = [P, P, ctypes.c_size_t, P]
+                getattr(L, f).restype = ctypes.c_int
+            for f in ("spec_rope_kv", "spec_copy_pages"):
+                getattr(L, f).argtypes = [P, P]
+                getattr(L, f).restype = ctypes.c_int
             for f in ("spec_map_slots", "spec_verify_attention_fp8"):
                 getattr(L, f).argtypes = [P, P, ctypes.c_size_t, P]
                 getattr(L, f).restype = ctypes.c_int
@@ -962,6 +1022,319 @@ def adjust_logits(logits, block_tokens=None, history=None, history_len=None, pro
                                    repetition, frequency, presence, bias_tokens, bias_values,
                                    allowed, block_shift), stream)
     return out
+
+
+# ----------------------------------------------------------------------------------
+# Ragged batches: rotary positions, attention of chunks, forked sequences, page copies
+# ----------------------------------------------------------------------------------
+# These argument structures keep their tensors alive (`keep`) and the device they are on
+# (`device`), whose current stream is the default one of a call.
+def _own(a, tensors):
+    tensors = [t for t in tensors if t is not None]
+    devices = {t.device for t in tensors}
+    if len(devices) > 1:
+        raise ValueError(f"the tensors must be on one device, not on {sorted(map(str, devices))}")
+    a.keep, a.device = tensors, tensors[0].device
+    return a
+
+
+def _call(name: str, a, stream, ws=None):
+    f = getattr(lib(), name)
+    if ws is not None:
+        if ws.device != a.device or ws.dtype != torch.uint8 or not ws.is_contiguous():
+            raise ValueError(f"the workspace must be a contiguous uint8 tensor on {a.device}")
+        args = (ctypes.byref(a), _ptr(ws), ws.numel())
+    else:
+        args = (ctypes.byref(a),)
+    if stream is not None and stream.device != a.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {a.device}")
+    if a.device.index == torch.cuda.current_device():
+        _raise(f(*args, _stream(stream)), name)
+    else:
+        with torch.cuda.device(a.device):
+            _raise(f(*args, _stream(stream)), name)
+
+
+def _rows(t, name: str, shape=None):
+    """The row stride of a bf16 tensor [rows][heads][D] with dense rows (0 for one row)."""
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be a torch.bfloat16 tensor")
+    if not t.is_cuda or t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be a CUDA tensor of shape {shape or '[rows][heads][D]'}")
+    R, H, D = t.shape
+    if R and any(n > 1 and s != want for n, s, want in zip((H, D), t.stride()[1:], (D, 1))):
+        raise ValueError(f"{name} must have dense [heads][D] rows")
+    if R > 1 and t.stride(0) < H * D:
+        raise ValueError(f"{name}'s rows overlap")
+    return t.stride(0) if R > 1 else 0
+
+
+def _status(status_ws):
+    if status_ws is None:
+        return None
+    _check(status_ws, "status_ws", torch.int32 if getattr(status_ws, "dtype", None) == torch.int32 else torch.uint8)
+    if status_ws.numel() * status_ws.element_size() < 4:
+        raise ValueError("status_ws must hold a status word of 4 bytes")
+    return status_ws.data_ptr()
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None,
+                     factor: float = 1.0, original_max: int = 0, beta_fast: float = 32.0,
+                     beta_slow: float = 1.0, low: float = 1.0, high: float = 4.0, device=None):
+    """Rotary frequencies base^(-2i / rot_dim), i < rot_dim / 2, in radians per position (float64),
+    and the factor that goes with them. scaling for contexts `factor` times as long as the
+    original_max trained ones:
+
+    * ``"linear"``: every frequency / factor;
+    * ``"ntk"``: base * factor^(rot_dim / (rot_dim - 2)), so that the lowest one is divided;
+    * ``"yarn"``: frequencies that turn less than beta_slow times over original_max positions are
+      divided, those that turn more than beta_fast times stay, with a linear ramp over i between
+      them; the factor is 0.1 ln(factor) + 1;
+    * ``"bands"``: as yarn with `low` and `high` turns, a ramp over the number of turns, and 1.
+    """
+    if scaling not in (None, "linear", "ntk", "yarn", "bands"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if rot_dim < 2 or rot_dim % 2 or not base > 1 or not factor >= 1:
+        raise ValueError("rot_dim must be even, base above 1 and factor at least 1")
+    if scaling in ("yarn", "bands") and original_max < 1:
+        raise ValueError(f"{scaling} needs original_max")
+    if scaling == "ntk":
+        if rot_dim < 4:
+            raise ValueError("ntk needs rot_dim >= 4")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    freq = base ** (-2 * i / rot_dim)
+    mult = 1.0
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "yarn":
+        def place(turns):  # the i whose frequency makes this many turns
+            return rot_dim * math.log(original_max / (turns * 2 * math.pi)) / (2 * math.log(base))
+        first, last = max(0, math.floor(place(beta_fast))), min(rot_dim - 1, math.ceil(place(beta_slow)))
+        divided = ((i - first) / max(last - first, 0.001)).clamp(0, 1)
+        freq = freq / factor * divided + freq * (1 - divided)
+        mult = 0.1 * math.log(factor) + 1.0
+    elif scaling == "bands":
+        if not high > low:
+            raise ValueError("high must be above low")
+        kept = ((original_max * freq / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        freq = freq / factor * (1 - kept) + freq * kept
+    return freq.to(device or "cuda"), mult
+
+
+def rope_turns(frequencies: torch.Tensor) -> torch.Tensor:
+    """Frequencies in radians per position (rope_frequencies, or any float tensor) as the turns
+    of rope_kv: int64 words, a turn = 2^64."""
+    if frequencies.dim() != 1 or not frequencies.is_floating_point():
+        raise ValueError("frequencies must be a float tensor [rot_dim / 2]")
+    turn = frequencies.double() / (2 * math.pi)
+    scaled = (turn - turn.floor()) * 2.0 ** 32
+    high = scaled.floor()
+    low = ((scaled - high) * 2.0 ** 32).floor()
+    return (high.long() << 32) | low.long()
+
+
+def rope_args(q, k, v, positions, turns, q_out=None, k_out=None, slots=None, k_cache=None,
+              v_cache=None, interleaved: bool = False, factor: float = 1.0, status_ws=None) -> RopeArgs:
+    given = [t for t in (q, k) if t is not None]
+    if not given:
+        raise ValueError("rope needs q or k")
+    R, _, D = given[0].shape
+    Hq = q.shape[1] if q is not None else 0
+    Hkv = k.shape[1] if k is not None else 0
+    strides = [0 if t is None else _rows(t, name, (R, H, D)) for t, name, H in (
+        (q, "q", Hq), (k, "k", Hkv), (v, "v", Hkv), (q_out, "q_out", Hq), (k_out, "k_out", Hkv))]
+    _check(positions, "positions", torch.int32, (R,))
+    if turns.dim() != 1:
+        raise ValueError("turns must have shape [rot_dim / 2]")
+    _check(turns, "turns", torch.int64)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if (slots is None) != (k_cache is None) or (slots is None) != (v_cache is None):
+        raise ValueError("slots, k_cache and v_cache go together")
+    if (v is None) != (slots is None):
+        raise ValueError("v goes with a cache")
+    if (k is None) != (k_out is None and slots is None):
+        raise ValueError("k goes with k_out or a cache")
+    pages = P = 0
+    if slots is not None:
+        _check(slots, "slots", torch.int32, (R,))
+        if k_cache.dim() != 4 or k_cache.shape[1] != Hkv or k_cache.shape[3] != D:
+            raise ValueError("k_cache must have shape [num_pages][Hkv][page_size][D]")
+        _check(k_cache, "k_cache", torch.bfloat16)
+        _check(v_cache, "v_cache", torch.bfloat16, k_cache.shape)
+        pages, _, P, _ = k_cache.shape
+    if not factor > 0:
+        raise ValueError("factor must be positive")
+    status = _status(status_ws)
+
+    def ptr(t):
+        return None if t is None else t.data_ptr()
+    a = RopeArgs(R, Hq, Hkv, D, 2 * turns.numel(), int(interleaved), float(factor), P, pages, *strides,
+                 ptr(q), ptr(k), ptr(v), positions.data_ptr(), turns.data_ptr(), ptr(q_out), ptr(k_out),
+                 ptr(slots), ptr(k_cache), ptr(v_cache), status)
+    return _own(a, [q, k, v, positions, turns, q_out, k_out, slots, k_cache, v_cache, status_ws])
+
+
+def rope_kv_args(a: RopeArgs, stream=None):
+    _call("spec_rope_kv", a, stream)
+
+
+def rope_kv(q, k, v, positions, turns, slots=None, k_cache=None, v_cache=None,
+            interleaved: bool = False, factor: float = 1.0, in_place: bool = False, status_ws=None,
+            stream=None):
+    """Rotary positions of q [rows][Hq][D] and k [rows][Hkv][D] (spec_rope_kv; rows may be strided),
+    and, with slots and caches, the write of rotated k and of v into the paged bf16 cache. Returns
+    (q, k) rotated, in place if asked; rows with a negative position are left as they are (in new
+    tensors: zeros)."""
+    def place(t):
+        return t if in_place or t is None else torch.zeros(t.shape, dtype=t.dtype, device=t.device)
+    q_out, k_out = place(q), place(k)
+    rope_kv_args(rope_args(q, k, v, positions, turns, q_out, k_out, slots, k_cache, v_cache,
+                           interleaved, factor, status_ws), stream)
+    return q_out, k_out
+
+
+def chunk_attn_args(q, cache, page_table, row_start, kv_len, out, lse=None, softmax_scale=0.0,
+                    path=ATTN_AUTO, causal: bool = True, window: int = 0) -> ChunkAttnArgs:
+    """cache: (k_cache, v_cache) in bf16, or (kv_cache, kv_scale) of the 8-bit cache."""
+    first, second = cache
+    stride = _rows(q, "q")
+    R, Hq, D = q.shape
+    if first.dtype == torch.float8_e4m3fn:
+        _check_cache_fp8(first, second)
+        num_pages, Hkv, _, P, D2 = first.shape
+        pointers = (None, None, first.data_ptr(), second.data_ptr())
+    else:
+        if first.dim() != 4:
+            raise ValueError("k_cache must have shape [num_pages][Hkv][page_size][D]")
+        _check(first, "k_cache", torch.bfloat16)
+        _check(second, "v_cache", torch.bfloat16, first.shape)
+        num_pages, Hkv, P, D2 = first.shape
+        pointers = (first.data_ptr(), second.data_ptr(), None, None)
+    B = kv_len.numel()
+    _check(kv_len, "kv_len", torch.int32, (B,))
+    _check(row_start, "row_start", torch.int32, (B + 1,))
+    _check(page_table, "page_table", torch.int32)
+    _check(out, "out", torch.bfloat16, (R, Hq, D))
+    if lse is not None:
+        _check(lse, "lse", torch.float32, (R, Hq))
+    if D2 != D or page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError("inconsistent attention shapes")
+    a = ChunkAttnArgs(B, R, Hq, Hkv, D, P, page_table.shape[1], num_pages, int(causal), int(window),
+                      float(softmax_scale), int(path), stride, q.data_ptr(), *pointers,
+                      page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(), out.data_ptr(),
+                      None if lse is None else lse.data_ptr())
+    return _own(a, [q, first, second, page_table, row_start, kv_len, out, lse])
+
+
+def chunk_attn_workspace_size(a: ChunkAttnArgs) -> int:
+    n = lib().spec_chunk_attn_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise SpecError(1, "spec_chunk_attn_workspace_size")
+    return int(n)
+
+
+def chunk_attention_args(a: ChunkAttnArgs, ws: torch.Tensor, stream=None):
+    _call("spec_chunk_attention", a, stream, ws)
+
+
+def chunk_attention(q, cache, page_table, row_start, kv_len, softmax_scale=0.0, path=ATTN_AUTO,
+                    causal: bool = True, window: int = 0, want_lse: bool = True, ws=None, stream=None):
+    """Attention of a packed ragged batch q [rows][Hq][D] over a paged cache (spec_chunk_attention):
+    cache = (k_cache, v_cache) or (kv_cache, kv_scale); row_start and kv_len as map_slots leaves
+    them. Returns (out bf16, lse fp32 or None); rows past row_start[-1] are 0 and -inf."""
+    out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float32, device=q.device) if want_lse else None
+    a = chunk_attn_args(q, cache, page_table, row_start, kv_len, out, lse, softmax_scale, path, causal,
+                        window)
+    if ws is None:
+        ws = new_workspace(chunk_attn_workspace_size(a), q.device)
+    chunk_attention_args(a, ws, stream)
+    return out, lse
+
+
+def fork_args(parent, kv_len, new_kv_len, page_table, new_table, shares, new_shares, free_pages,
+              new_free_pages, free_count, new_free_count, page_size: int, copies, flags=None,
+              reserved: int = 0) -> ForkArgs:
+    B, MP = page_table.shape
+    for t, name, shape in ((parent, "parent", (B,)), (kv_len, "kv_len", (B,)),
+                           (new_kv_len, "new_kv_len", (B,)), (page_table, "page_table", (B, MP)),
+                           (new_table, "new_table", (B, MP)), (shares, "shares", (shares.numel(),)),
+                           (new_shares, "new_shares", shares.shape),
+                           (free_pages, "free_pages", (free_pages.numel(),)),
+                           (new_free_pages, "new_free_pages", free_pages.shape),
+                           (free_count, "free_count", (1,)), (new_free_count, "new_free_count", (1,)),
+                           (copies, "copies", (B, 2))):
+        _check(t, name, torch.int32, shape)
+    if flags is not None:
+        _check(flags, "flags", torch.int32, (B,))
+    a = ForkArgs(B, int(page_size), MP, shares.numel(), int(reserved), free_pages.numel(),
+                 parent.data_ptr(), kv_len.data_ptr(), new_kv_len.data_ptr(), page_table.data_ptr(),
+                 new_table.data_ptr(), shares.data_ptr(), new_shares.data_ptr(), free_pages.data_ptr(),
+                 new_free_pages.data_ptr(), free_count.data_ptr(), new_free_count.data_ptr(),
+                 copies.data_ptr(), None if flags is None else flags.data_ptr())
+    return _own(a, [parent, kv_len, new_kv_len, page_table, new_table, shares, new_shares, free_pages,
+                    new_free_pages, free_count, new_free_count, copies, flags])
+
+
+def fork_workspace_size(a: ForkArgs) -> int:
+    n = lib().spec_fork_workspace_size(ctypes.byref(a))
+    if n == 0:
+        raise SpecError(1, "spec_fork_workspace_size")
+    return int(n)
+
+
+def fork_sequences_args(a: ForkArgs, ws: torch.Tensor, stream=None):
+    _call("spec_fork_sequences", a, stream, ws)
+
+
+def fork_sequences(parent, kv_len, page_table, shares, free_pages, free_count, page_size: int,
+                   reserved: int = 0, ws=None, stream=None) -> Dict[str, torch.Tensor]:
+    """Each sequence goes on from sequence parent[b] (spec_fork_sequences; -1: ends). kv_len,
+    page_table, shares (zeros [num_pages] at first), free_pages and free_count are updated in
+    place. Returns copies, the pairs of pages that copy_pages then copies, and flags."""
+    B = parent.numel()
+    res = dict(copies=torch.empty(B, 2, dtype=torch.int32, device=parent.device),
+               flags=torch.empty(B, dtype=torch.int32, device=parent.device))
+    a = fork_args(parent, kv_len, kv_len, page_table, page_table, shares, shares, free_pages,
+                  free_pages, free_count, free_count, page_size, res["copies"], res["flags"], reserved)
+    if ws is None:
+        ws = new_workspace(fork_workspace_size(a), parent.device)
+    fork_sequences_args(a, ws, stream)
+    return res
+
+
+def copy_args(pairs, buffers, status_ws=None) -> CopyArgs:
+    """buffers: contiguous tensors whose first dimension is the page."""
+    if not buffers:
+        raise ValueError("copy needs a buffer")
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError("pairs must have shape [n][2]")
+    _check(pairs, "pairs", torch.int32)
+    pages = buffers[0].shape[0]
+    for t in buffers:
+        if not isinstance(t, torch.Tensor) or t.dim() < 1 or t.shape[0] != pages or pages < 1:
+            raise ValueError("buffers must be tensors of the same number of pages")
+        _check(t, "a buffer", t.dtype)
+    n = len(buffers)
+    bases = (ctypes.c_void_p * n)(*[t.data_ptr() for t in buffers])
+    sizes = (ctypes.c_int64 * n)(*[t.numel() // pages * t.element_size() for t in buffers])
+    a = CopyArgs(pairs.shape[0], pages, n, pairs.data_ptr(), ctypes.cast(bases, ctypes.c_void_p),
+                 ctypes.cast(sizes, ctypes.c_void_p), _status(status_ws))
+    a.arrays = (bases, sizes)
+    return _own(a, [pairs, *buffers, status_ws])
+
+
+def copy_pages_args(a: CopyArgs, stream=None):
+    _call("spec_copy_pages", a, stream)
+
+
+def copy_pages(pairs, buffers, status_ws=None, stream=None):
+    """Copies page pairs[i][0] of every buffer to page pairs[i][1] (spec_copy_pages): the caches,
+    and scales, of any number of layers, in place."""
+    for i in range(0, len(buffers), COPY_MAX_BUFFERS):
+        copy_pages_args(copy_args(pairs, buffers[i:i + COPY_MAX_BUFFERS], status_ws), stream)
 
 
 def philox_uniforms(seed: int, n: int, offset: int = 0, device=None, stream=None) -> torch.Tensor:

@@ -1,0 +1,311 @@
+// Attention of ragged chunks over the paged caches: what a call prepares and finishes, and the
+// CUDA-core kernel (spec_chunk_attention, SPEC_ATTN_CUDA_CORES).
+//
+//   o = sum_k 2^(s_k - m) v_k / sum_k 2^(s_k - m),  s_k = scale log2(e) q.k, over low <= k < high
+//
+// The CUDA-core kernel takes 16 query rows of one KV head and tiles of 64 keys, gathered through
+// the page table into shared memory in fp32; scores, running maximum and sum, and outputs are
+// fp32. It serves what the tensor-core kernel does not take and is a second implementation to
+// compare it with.
+#include <cuda_bf16.h>
+
+#include <cmath>
+
+#include "chunk.cuh"
+#include "kv_fp8.cuh"
+
+namespace specv {
+namespace {
+
+constexpr int RT = kSimtRowTile;
+constexpr int TK = kSimtKeyTile;
+constexpr int NT = kSimtThreads;
+
+template <int D>
+struct Smem {
+  static constexpr int kStride = D + 4;  // floats per staged row (bank spread)
+  float q[RT][D];
+  float k[TK][kStride];
+  float v[TK][kStride];
+  float s[RT][TK];
+  float alpha[RT], m[RT], l[RT];
+  int bad;
+};
+
+// Lengths of the batch, once per call: which rows a sequence has and whether they can be served.
+constexpr int kSetupThreads = 1024;
+__global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams p) {
+  pdl_wait_prior();
+  for (int b = threadIdx.x; b < p.batch; b += kSetupThreads) {
+    const int r0 = p.row_start[b], r1 = p.row_start[b + 1];
+    const bool rows_ok = chunk_rows_ok(p, r0, r1);
+    ChunkSeq s = {r0, rows_ok ? r1 - r0 : 0, 0, 0};
+    bool bad = !rows_ok;
+    if (s.n > 0) {
+      s.kv_len = p.kv_len[b];
+      if (s.kv_len < s.n || s.kv_len > p.max_keys) {
+        s.n = 0;
+        bad = true;
+      }
+    }
+    p.seqs[b] = s;
+    p.seq_bad[b] = bad ? 1 : 0;
+    if (bad) set_status(p.status, SPEC_FLAG_BAD_KV_LEN);
+  }
+}
+
+// Rows [row0, row0 + nrows) of sequence b and KV head g (row = token * group + head of the group).
+template <int D, bool FP8>
+__device__ void simt_rows(const ChunkParams& p, Smem<D>& sm, int b, const ChunkSeq& seq, int g, int row0, int nrows) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int ctx = seq.kv_len - seq.n;
+  const int at0 = ctx + row0 / p.group, at1 = ctx + (row0 + nrows - 1) / p.group;
+  const int begin = chunk_low(p, at0), end = chunk_high(p, at1, seq.kv_len);
+  const int32_t* table = p.page_table + static_cast<int64_t>(b) * p.max_pages;
+  __syncthreads();  // the rows before are done with the shared memory
+  if (tid == 0) sm.bad = 0;
+  __syncthreads();
+  for (int pg = begin / p.page_size + tid; pg <= (end - 1) / p.page_size; pg += NT) {
+    const int id = table[pg];
+    if (id < 0 || id >= p.num_pages) sm.bad = 1;
+  }
+  const __nv_bfloat16* qg = static_cast<const __nv_bfloat16*>(p.q);
+  for (int i = tid; i < RT * D; i += NT) {
+    const int r = i / D, d = i % D, row = row0 + r;
+    float x = 0.f;
+    if (r < nrows)
+      x = __bfloat162float(qg[(seq.row0 + row / p.group) * p.q_stride + static_cast<int64_t>(g * p.group + row % p.group) * D + d]);
+    sm.q[r][d] = x;
+  }
+  if (tid < RT) {
+    sm.m[tid] = -INFINITY;
+    sm.l[tid] = 0.f;
+  }
+  __syncthreads();
+  if (sm.bad) {  // the whole sequence is cleared at the end
+    if (tid == 0) {
+      p.seq_bad[b] = 1;
+      set_status(p.status, SPEC_FLAG_BAD_PAGE);
+    }
+    return;
+  }
+
+  // P V: a thread owns 8 consecutive dims of rows rg, rg + RG, ...
+  constexpr int DQ = D / 8, RG = NT / DQ, RPT = RT / RG;
+  const int dq = tid % DQ, rg = tid / DQ;
+  float o[RPT][8];
+#pragma unroll
+  for (int i = 0; i < RPT; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[i][e] = 0.f;
+
+  const int kk = tid % TK, hr = tid / TK;  // Q K^T: key kk, rows hr, hr + 2, ...
+  for (int t0 = begin / TK * TK; t0 < end; t0 += TK) {
+    constexpr int kPieces = D / 8;  // 8 elements
+    for (int c = tid; c < 2 * TK * kPieces; c += NT) {
+      const int kind = c / (TK * kPieces), key = (c / kPieces) % TK, piece = c % kPieces, pos = t0 + key;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      if (pos >= begin && pos < end) {
+        const int64_t ph = static_cast<int64_t>(table[pos / p.page_size]) * p.hkv + g;
+        if constexpr (FP8) {
+          const uint2 raw = __ldg(reinterpret_cast<const uint2*>(
+              static_cast<const uint8_t*>(p.k_cache) + ((ph * 2 + kind) * p.page_size + pos % p.page_size) * D + piece * 8));
+          float sc = p.kv_scale[ph * 2 + kind];
+          if (kind) sc = clamp_scale(sc);
+          const uint32_t w[2] = {raw.x, raw.y};
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float2 a = from_e4m3x2(w[e] & 0xffffu), c2 = from_e4m3x2(w[e] >> 16);
+            x[4 * e] = a.x * sc; x[4 * e + 1] = a.y * sc; x[4 * e + 2] = c2.x * sc; x[4 * e + 3] = c2.y * sc;
+          }
+        } else {
+          const uint4 raw = __ldg(reinterpret_cast<const uint4*>(
+              static_cast<const __nv_bfloat16*>(kind ? p.v_cache : p.k_cache) + (ph * p.page_size + pos % p.page_size) * D + piece * 8));
+          const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(w[e] << 16);
+            x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+          }
+        }
+      }
+      float* dst = (kind ? sm.v[key] : sm.k[key]) + piece * 8;
+      *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+      *reinterpret_cast<float4*>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    __syncthreads();
+    {
+      float acc[RT / 2];
+#pragma unroll
+      for (int i = 0; i < RT / 2; ++i) acc[i] = 0.f;
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        const float4 kf = *reinterpret_cast<const float4*>(&sm.k[kk][d]);
+#pragma unroll
+        for (int i = 0; i < RT / 2; ++i) {
+          const float4 q = *reinterpret_cast<const float4*>(&sm.q[hr + 2 * i][d]);
+          acc[i] += q.x * kf.x + q.y * kf.y + q.z * kf.z + q.w * kf.w;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < RT / 2; ++i) {
+        const int r = hr + 2 * i, at = ctx + (row0 + r) / p.group;
+        const bool vis = r < nrows && t0 + kk >= chunk_low(p, at) && t0 + kk < chunk_high(p, at, seq.kv_len);
+        sm.s[r][kk] = vis ? acc[i] * p.scale_log2 : -INFINITY;
+      }
+    }
+    __syncthreads();
+    for (int r = warp; r < RT; r += NT / 32) {
+      const float a0 = sm.s[r][lane], a1 = sm.s[r][lane + 32];
+      float mx = fmaxf(a0, a1);
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+      const float m_old = sm.m[r], m_new = fmaxf(m_old, mx);
+      const float sub = m_new == -INFINITY ? 0.f : m_new;
+      const float p0 = ex2(a0 - sub), p1 = ex2(a1 - sub);
+      const float alpha = m_old == -INFINITY ? 0.f : ex2(m_old - sub);
+      float sum = p0 + p1;
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      __syncwarp();
+      sm.s[r][lane] = p0;
+      sm.s[r][lane + 32] = p1;
+      if (lane == 0) {
+        sm.alpha[r] = alpha;
+        sm.m[r] = m_new;
+        sm.l[r] = sm.l[r] * alpha + sum;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      const float a = sm.alpha[rg + i * RG];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[i][e] *= a;
+    }
+    for (int k = 0; k < TK; ++k) {
+      const float4 v0 = *reinterpret_cast<const float4*>(&sm.v[k][dq * 8]);
+      const float4 v1 = *reinterpret_cast<const float4*>(&sm.v[k][dq * 8 + 4]);
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        const float w = sm.s[rg + i * RG][k];
+        if (w == 0.f) continue;  // a hidden key adds nothing, whatever its value
+        o[i][0] += w * v0.x; o[i][1] += w * v0.y; o[i][2] += w * v0.z; o[i][3] += w * v0.w;
+        o[i][4] += w * v1.x; o[i][5] += w * v1.y; o[i][6] += w * v1.z; o[i][7] += w * v1.w;
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < RPT; ++i) {
+    const int r = rg + i * RG, row = row0 + r;
+    if (r >= nrows) continue;
+    const float inv = 1.f / sm.l[r];  // every row sees a key: a sum of 0 (scores of -inf) is NaN
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __nv_bfloat162 pr = __floats2bfloat162_rn(o[i][2 * e] * inv, o[i][2 * e + 1] * inv);
+      w[e] = *reinterpret_cast<const uint32_t*>(&pr);
+    }
+    const int64_t head = static_cast<int64_t>(seq.row0 + row / p.group) * p.hq + g * p.group + row % p.group;
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + head * D + dq * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (dq == 0 && p.lse) p.lse[head] = (sm.m[r] + log2f(sm.l[r])) * 0.6931471805599453f;
+  }
+}
+
+// Blocks own 16 of the batch's rows * group query rows of a KV head; one that spans sequences
+// takes them in turn.
+template <int D, bool FP8>
+__global__ void __launch_bounds__(NT) chunk_simt_kernel(ChunkParams p) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw);
+  pdl_wait_prior();
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * RT, last = first + RT;
+  const int g = blockIdx.y;
+  int lo = 0, hi = p.batch;  // the first sequence whose rows end past `first`
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (static_cast<int64_t>(p.row_start[mid + 1]) * p.group > first) hi = mid; else lo = mid + 1;
+  }
+  for (int b = lo; b < p.batch && static_cast<int64_t>(p.row_start[b]) * p.group < last; ++b) {
+    const ChunkSeq seq = p.seqs[b];
+    if (seq.n == 0) continue;
+    const int64_t start = static_cast<int64_t>(seq.row0) * p.group, end = start + static_cast<int64_t>(seq.n) * p.group;
+    const int64_t from = max(first, start), to = min(last, end);
+    if (from < to) simt_rows<D, FP8>(p, sm, b, seq, g, static_cast<int>(from - start), static_cast<int>(to - from));
+  }
+}
+
+// Sequences that could not be served get out = 0 and lse = -inf.
+constexpr int kFinishThreads = 128;
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kFinishThreads) chunk_finish_kernel(ChunkParams p) {
+  pdl_wait_prior();
+  for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+    if (p.seq_bad[b] == 0) continue;
+    const int r0 = p.row_start[b], r1 = p.row_start[b + 1];
+    if (!chunk_rows_ok(p, r0, r1)) continue;  // there are none to clear
+    const int64_t heads = static_cast<int64_t>(r1 - r0) * p.hq;
+    uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + static_cast<int64_t>(r0) * p.hq * D);
+    for (int64_t i = threadIdx.x; i < heads * (D / 8); i += kFinishThreads) out[i] = make_uint4(0, 0, 0, 0);
+    if (p.lse)
+      for (int64_t i = threadIdx.x; i < heads; i += kFinishThreads) p.lse[static_cast<int64_t>(r0) * p.hq + i] = -INFINITY;
+  }
+}
+
+template <int D, bool FP8>
+cudaError_t launch_simt_d(const ChunkParams& p, cudaStream_t stream) {
+  const size_t smem = sizeof(Smem<D>);
+  cudaError_t e = cudaFuncSetAttribute(chunk_simt_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = (static_cast<int64_t>(p.rows) * p.group + RT - 1) / RT;
+  e = launch_overlapped(chunk_simt_kernel<D, FP8>, dim3(static_cast<unsigned>(tiles), p.hkv), NT, smem, stream, p);
+  if (e != cudaSuccess) return e;
+  return launch_overlapped(chunk_finish_kernel<D, FP8>, dim3(p.batch < 256 ? p.batch : 256), kFinishThreads, 0, stream, p);
+}
+
+}  // namespace
+
+ChunkParams make_chunk_params(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws) {
+  ChunkParams p{};
+  p.batch = a.batch;
+  p.rows = a.rows;
+  p.hq = a.num_q_heads;
+  p.hkv = a.num_kv_heads;
+  p.group = a.num_q_heads / a.num_kv_heads;
+  p.page_size = a.page_size;
+  p.max_pages = a.max_pages_per_seq;
+  p.num_pages = a.num_pages;
+  p.max_keys = a.max_pages_per_seq * a.page_size;
+  p.causal = a.causal;
+  p.window = a.window;
+  const float scale = a.softmax_scale != 0.f ? a.softmax_scale : 1.f / sqrtf(static_cast<float>(a.head_dim));
+  p.scale_log2 = scale * kLog2e;
+  p.q_stride = a.q_row_stride ? a.q_row_stride : static_cast<int64_t>(a.num_q_heads) * a.head_dim;
+  p.q = a.q;
+  p.k_cache = P.fp8 ? a.kv_cache : a.k_cache;
+  p.v_cache = a.v_cache;
+  p.kv_scale = a.kv_scale;
+  p.page_table = a.page_table;
+  p.row_start = a.row_start;
+  p.kv_len = a.kv_len;
+  p.out = a.out;
+  p.lse = a.lse;
+  p.status = reinterpret_cast<uint32_t*>(ws);
+  p.seqs = reinterpret_cast<ChunkSeq*>(ws + P.seqs);
+  p.seq_bad = reinterpret_cast<int32_t*>(p.seqs + a.batch);
+  return p;
+}
+
+cudaError_t launch_chunk(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws, cudaStream_t stream) {
+  const ChunkParams p = make_chunk_params(a, P, ws);
+  const cudaError_t e = launch_overlapped(chunk_setup_kernel, dim3(1), kSetupThreads, 0, stream, p);
+  if (e != cudaSuccess) return e;
+  if (P.fp8) return a.head_dim == 128 ? launch_simt_d<128, true>(p, stream) : launch_simt_d<64, true>(p, stream);
+  return a.head_dim == 128 ? launch_simt_d<128, false>(p, stream) : launch_simt_d<64, false>(p, stream);
+}
+
+}  // namespace specv
