@@ -888,12 +888,15 @@ spec_status_t spec_copy_pages(const spec_copy_args_t* copy, spec_stream_t stream
  * counters are still zero, so the same workspace serves the next product call.
  * spec_test_attention_wait_timeout returns SPEC_ERR_UNSUPPORTED for shapes the
  * tensor-core row-tile kernel does not take; spec_test_attention_fp8_wait_timeout does the
- * same for spec_verify_attention_fp8 and its tensor-core kernel. Nothing traps, faults or waits without bound.
+ * same for spec_verify_attention_fp8 and its tensor-core kernel, and
+ * spec_test_chunk_attention_wait_timeout for spec_chunk_attention. Nothing traps, faults or waits without bound.
  * ------------------------------------------------------------------------------------- */
 spec_status_t spec_test_attention_wait_timeout(const spec_attn_args_t* attn, void* ws,
                                                size_t ws_bytes, spec_stream_t stream);
 spec_status_t spec_test_attention_fp8_wait_timeout(const spec_attn_fp8_args_t* attn, void* ws,
                                                    size_t ws_bytes, spec_stream_t stream);
+spec_status_t spec_test_chunk_attention_wait_timeout(const spec_chunk_attn_args_t* attn, void* ws,
+                                                     size_t ws_bytes, spec_stream_t stream);
 spec_status_t spec_test_lm_head_wait_timeout(const spec_lm_head_args_t* lm, void* ws,
                                              size_t ws_bytes, spec_stream_t stream);
 

@@ -286,7 +286,8 @@ def lib(build_if_missing: bool = True):
             for f in ("spec_chunk_attn_workspace_size", "spec_fork_workspace_size"):
                 getattr(L, f).argtypes = [P]
                 getattr(L, f).restype = ctypes.c_size_t
-            for f in ("spec_chunk_attention", "spec_fork_sequences"):
+            for f in ("spec_chunk_attention", "spec_fork_sequences",
+                      "spec_test_chunk_attention_wait_timeout"):
                 getattr(L, f).argtypes = [P, P, ctypes.c_size_t, P]
                 getattr(L, f).restype = ctypes.c_int
             for f in ("spec_rope_kv", "spec_copy_pages"):
@@ -1237,6 +1238,12 @@ def chunk_attn_workspace_size(a: ChunkAttnArgs) -> int:
 
 def chunk_attention_args(a: ChunkAttnArgs, ws: torch.Tensor, stream=None):
     _call("spec_chunk_attention", a, stream, ws)
+
+
+def test_chunk_attention_wait_timeout_args(a: ChunkAttnArgs, ws: torch.Tensor, stream=None):
+    """Test hook: spec_chunk_attention's tensor-core kernel with its copy producers idle, so that
+    its bounded waits run out (about 1 s) and it returns with SPEC_FLAG_TIMEOUT set."""
+    _call("spec_test_chunk_attention_wait_timeout", a, stream, ws)
 
 
 def chunk_attention(q, cache, page_table, row_start, kv_len, softmax_scale=0.0, path=ATTN_AUTO,

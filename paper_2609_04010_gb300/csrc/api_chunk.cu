@@ -74,8 +74,36 @@ spec_status_t check_chunk(const spec_chunk_attn_args_t* a) {
     return SPEC_ERR_UNSUPPORTED;
   const int64_t group = a->num_q_heads / a->num_kv_heads;
   if (group * (static_cast<int64_t>(a->rows) + 1) > INT32_MAX - 256) return SPEC_ERR_UNSUPPORTED;
-  if (a->path == SPEC_ATTN_TENSOR_CORES) return SPEC_ERR_UNSUPPORTED;
+  if (a->path == SPEC_ATTN_TENSOR_CORES && !chunk_tc_fits(*a)) return SPEC_ERR_UNSUPPORTED;
   return SPEC_OK;
+}
+
+// The most that a call may need on any device: the grid is one block per SM.
+size_t chunk_bytes(const spec_chunk_attn_args_t& a) {
+  int dev = 0, sms = 160;
+  if (cudaGetDevice(&dev) == cudaSuccess) {
+    const int n = device_sm_count(dev);
+    if (n > sms) sms = n;
+  } else {
+    cudaGetLastError();
+  }
+  return chunk_plan(a, kWsHeader, sms, a.path).end;
+}
+
+spec_status_t run_chunk(const spec_chunk_attn_args_t* a, void* ws, size_t ws_bytes, spec_stream_t stream, bool starve) {
+  const spec_status_t st = check_chunk(a);
+  if (st != SPEC_OK) return st;
+  if (bad_ws(ws)) return SPEC_ERR_INVALID_ARGUMENT;
+  if (starve && (a->path == SPEC_ATTN_CUDA_CORES || !chunk_tc_fits(*a) || a->rows == 0)) return SPEC_ERR_UNSUPPORTED;
+  if (chunk_plan(*a, kWsHeader, 1, a->path).end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+  if (a->rows == 0) return SPEC_OK;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  DeviceScope scope(s);
+  if (!scope.ok) return SPEC_ERR_CUDA;
+  (void)cudaGetLastError();
+  const ChunkPlan P = chunk_plan(*a, kWsHeader, scope.sms, a->path);
+  if (P.end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+  return launch_chunk(*a, P, static_cast<char*>(ws), s, starve) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
 }
 
 spec_status_t check_fork(const spec_fork_args_t* a) {
@@ -119,14 +147,33 @@ spec_status_t check_copy(const spec_copy_args_t* a) {
 
 namespace specv {
 
+bool chunk_tc_fits(const spec_chunk_attn_args_t& a) {
+  const int group = a.num_q_heads / a.num_kv_heads;
+  if (group > kChunkTileRows || a.kv_cache) return false;
+  const int64_t per_unit = 2 * (kChunkTileRows / group);
+  const int64_t units = a.rows / per_unit + a.batch;
+  return units * a.num_kv_heads <= INT32_MAX / 4 && static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX / 2;
+}
+
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path) {
   ChunkPlan P{};
-  (void)num_sms;
-  (void)path;
-  P.path = SPEC_ATTN_CUDA_CORES;
   P.fp8 = a.kv_cache != nullptr;
+  P.path = path != SPEC_ATTN_CUDA_CORES && chunk_tc_fits(a) ? SPEC_ATTN_TENSOR_CORES : SPEC_ATTN_CUDA_CORES;
   P.seqs = base;
-  P.end = ws_round(P.seqs + (sizeof(ChunkSeq) + sizeof(int32_t)) * static_cast<size_t>(a.batch));
+  P.bad = ws_round(P.seqs + sizeof(ChunkSeq) * (static_cast<size_t>(a.batch) + 1));
+  P.end = ws_round(P.bad + sizeof(int32_t) * static_cast<size_t>(a.batch));
+  if (P.path != SPEC_ATTN_TENSOR_CORES) return P;
+  P.tile_tokens = kChunkTileRows / (a.num_q_heads / a.num_kv_heads);
+  P.grid = num_sms;
+  P.max_units = a.rows / (2 * P.tile_tokens) + a.batch;
+  P.redo_cap = P.max_units * a.num_kv_heads + P.grid;
+  const size_t rows = static_cast<size_t>(P.grid) * 2 * 2 * kChunkTileRows;
+  P.cum = P.end;
+  P.work = ws_round(P.cum + sizeof(long long) * (static_cast<size_t>(P.max_units) + 1));
+  P.redo = ws_round(P.work + sizeof(ChunkWork) + sizeof(int4) * static_cast<size_t>(P.grid));
+  P.partial_o = ws_round(P.redo + sizeof(int4) * (static_cast<size_t>(P.redo_cap) + 1));
+  P.partial_ml = ws_round(P.partial_o + rows * a.head_dim * sizeof(float));
+  P.end = ws_round(P.partial_ml + rows * sizeof(float2));
   return P;
 }
 
@@ -145,22 +192,16 @@ spec_status_t spec_rope_kv(const spec_rope_args_t* a, spec_stream_t stream) {
 }
 
 size_t spec_chunk_attn_workspace_size(const spec_chunk_attn_args_t* a) {
-  if (check_chunk(a) != SPEC_OK) return 0;
-  return chunk_plan(*a, kWsHeader, 160, a->path).end;
+  return check_chunk(a) == SPEC_OK ? chunk_bytes(*a) : 0;
 }
 
 spec_status_t spec_chunk_attention(const spec_chunk_attn_args_t* a, void* ws, size_t ws_bytes, spec_stream_t stream) {
-  const spec_status_t st = check_chunk(a);
-  if (st != SPEC_OK) return st;
-  if (bad_ws(ws)) return SPEC_ERR_INVALID_ARGUMENT;
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const ChunkPlan P0 = chunk_plan(*a, kWsHeader, 160, a->path);
-  if (P0.end > ws_bytes) return SPEC_ERR_WORKSPACE_TOO_SMALL;
-  if (a->rows == 0) return SPEC_OK;
-  DeviceScope scope(s);
-  if (!scope.ok) return SPEC_ERR_CUDA;
-  const ChunkPlan P = chunk_plan(*a, kWsHeader, scope.sms, a->path);
-  return launch_chunk(*a, P, static_cast<char*>(ws), s) == cudaSuccess ? SPEC_OK : SPEC_ERR_CUDA;
+  return run_chunk(a, ws, ws_bytes, stream, false);
+}
+
+spec_status_t spec_test_chunk_attention_wait_timeout(const spec_chunk_attn_args_t* a, void* ws, size_t ws_bytes,
+                                                     spec_stream_t stream) {
+  return run_chunk(a, ws, ws_bytes, stream, true);
 }
 
 size_t spec_fork_workspace_size(const spec_fork_args_t* a) { return check_fork(a) == SPEC_OK ? fork_bytes(*a) : 0; }

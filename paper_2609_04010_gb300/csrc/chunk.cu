@@ -18,10 +18,9 @@ namespace specv {
 namespace {
 
 constexpr int RT = kSimtRowTile;
-constexpr int TK = kSimtKeyTile;
 constexpr int NT = kSimtThreads;
 
-template <int D>
+template <int D, int TK>
 struct Smem {
   static constexpr int kStride = D + 4;  // floats per staged row (bank spread)
   float q[RT][D];
@@ -32,31 +31,140 @@ struct Smem {
   int bad;
 };
 
-// Lengths of the batch, once per call: which rows a sequence has and whether they can be served.
+// Lengths of the batch, once per call: which rows a sequence has and whether they can be served;
+// for the tensor cores also the work list, equal numbers of virtual steps per block. One block,
+// because all of it depends on sums over the batch.
 constexpr int kSetupThreads = 1024;
+constexpr int kSetupKept = 2048;  // sequences and units whose sums are kept in shared memory
+
+// The block's exclusive prefix sum of v in thread order, and the total.
+__device__ __forceinline__ long long scan_block(long long v, long long* sh, long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) sh[warp] = x;
+  __syncthreads();
+  long long w = sh[lane];  // kSetupThreads / 32 == 32 warps
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += y;
+  }
+  const long long before = warp ? __shfl_sync(0xffffffffu, w, warp - 1) : 0;
+  *total = __shfl_sync(0xffffffffu, w, 31);
+  __syncthreads();
+  return before + x - v;
+}
+
 __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams p) {
+  __shared__ long long sh[32];
+  __shared__ int first_kept[kSetupKept + 1];
+  __shared__ long long cum_kept[kSetupKept + 1];
   pdl_wait_prior();
-  for (int b = threadIdx.x; b < p.batch; b += kSetupThreads) {
-    const int r0 = p.row_start[b], r1 = p.row_start[b + 1];
-    const bool rows_ok = chunk_rows_ok(p, r0, r1);
-    ChunkSeq s = {r0, rows_ok ? r1 - r0 : 0, 0, 0};
-    bool bad = !rows_ok;
-    if (s.n > 0) {
-      s.kv_len = p.kv_len[b];
-      if (s.kv_len < s.n || s.kv_len > p.max_keys) {
+  const int tid = threadIdx.x;
+  long long carry = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += kSetupThreads) {
+    const int b = b0 + tid;
+    ChunkSeq s = {0, 0, 0, 0};
+    bool bad = false;
+    if (b < p.batch) {
+      const int r0 = p.row_start[b], r1 = p.row_start[b + 1];
+      bad = !chunk_rows_ok(p, r0, r1);
+      s.row0 = r0;
+      s.n = bad ? 0 : r1 - r0;
+      if (s.n > 0) {
+        s.kv_len = p.kv_len[b];
+        if (s.kv_len < s.n || s.kv_len > p.max_keys) {
+          s.n = 0;
+          bad = true;
+        }
+      }
+    }
+    const int units = p.blocks ? chunk_units(p, s.n) : 0;
+    long long all;
+    const long long before = carry + scan_block(units, sh, &all);
+    carry += all;
+    if (b < p.batch) {
+      // (rows that sequences share, out of order, could make more units than there is room for)
+      if (before + units > p.max_units && units > 0) {
         s.n = 0;
         bad = true;
       }
+      s.first_unit = static_cast<int>(min(before, static_cast<long long>(p.max_units)));
+      p.seqs[b] = s;
+      p.seq_bad[b] = bad ? 1 : 0;
+      if (bad) set_status(p.status, SPEC_FLAG_BAD_KV_LEN);
+      if (b < kSetupKept) first_kept[b] = s.first_unit;
     }
-    p.seqs[b] = s;
-    p.seq_bad[b] = bad ? 1 : 0;
-    if (bad) set_status(p.status, SPEC_FLAG_BAD_KV_LEN);
+  }
+  if (!p.blocks) return;
+  const int nunits = static_cast<int>(min(carry, static_cast<long long>(p.max_units)));
+  if (tid == 0) {
+    p.seqs[p.batch] = {0, 0, 0, nunits};
+    if (p.batch < kSetupKept) first_kept[p.batch] = nunits;
+    p.redo[0] = make_int4(0, 0, 0, 0);
+    p.cum[0] = 0;
+    cum_kept[0] = 0;
+  }
+  __syncthreads();
+  auto first = [&](int b) { return p.batch < kSetupKept ? first_kept[b] : p.seqs[b].first_unit; };
+  const long long* cum = nunits <= kSetupKept ? cum_kept : p.cum;
+  carry = 0;
+  for (int u0 = 0; u0 < nunits; u0 += kSetupThreads) {
+    const int u = u0 + tid;
+    int steps = 0;
+    if (u < nunits) {
+      int lo = 0, hi = p.batch;  // the largest b with first(b) <= u
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first(mid) <= u) lo = mid; else hi = mid;
+      }
+      const ChunkSeq s = p.seqs[lo];
+      if (u - s.first_unit < chunk_units(p, s.n)) steps = chunk_unit(p, s, u - s.first_unit).steps + kChunkOverhead;
+    }
+    long long all;
+    const long long before = carry + scan_block(steps, sh, &all);
+    carry += all;
+    if (u < nunits) {
+      p.cum[u + 1] = before + steps;
+      if (u < kSetupKept) cum_kept[u + 1] = before + steps;
+    }
+  }
+  __syncthreads();
+  const long long total = carry * p.hkv;
+  const int active = static_cast<int>(min(total, static_cast<long long>(p.blocks)));
+  if (tid == 0) {
+    p.work->total = total;
+    p.work->active = active;
+  }
+  for (int c = tid; c < active; c += kSetupThreads) {
+    const long long t = c * total / active;
+    int lo = 0, hi = p.batch;  // the largest b whose steps begin at or before t
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (cum[first(mid)] * p.hkv <= t) lo = mid; else hi = mid;
+    }
+    const int b = lo, f = first(b), end = first(b + 1);
+    const long long base = cum[f], each = cum[end] - base;
+    const int g = static_cast<int>((t - base * p.hkv) / each);
+    const long long rem = t - base * p.hkv - g * each;
+    lo = f;
+    hi = end;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (cum[mid] - base <= rem) lo = mid; else hi = mid;
+    }
+    p.work->starts[c] = make_int4(b, g, lo - f, static_cast<int>(rem - (cum[lo] - base)));
   }
 }
 
 // Rows [row0, row0 + nrows) of sequence b and KV head g (row = token * group + head of the group).
-template <int D, bool FP8>
-__device__ void simt_rows(const ChunkParams& p, Smem<D>& sm, int b, const ChunkSeq& seq, int g, int row0, int nrows) {
+template <int D, bool FP8, int TK>
+__device__ void simt_rows(const ChunkParams& p, Smem<D, TK>& sm, int b, const ChunkSeq& seq, int g, int row0, int nrows) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ctx = seq.kv_len - seq.n;
   const int at0 = ctx + row0 / p.group, at1 = ctx + (row0 + nrows - 1) / p.group;
@@ -99,7 +207,8 @@ __device__ void simt_rows(const ChunkParams& p, Smem<D>& sm, int b, const ChunkS
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[i][e] = 0.f;
 
-  const int kk = tid % TK, hr = tid / TK;  // Q K^T: key kk, rows hr, hr + 2, ...
+  constexpr int RS = NT / TK;              // Q K^T: key kk, rows hr, hr + RS, ...
+  const int kk = tid % TK, hr = tid / TK;
   for (int t0 = begin / TK * TK; t0 < end; t0 += TK) {
     constexpr int kPieces = D / 8;  // 8 elements
     for (int c = tid; c < 2 * TK * kPieces; c += NT) {
@@ -137,28 +246,28 @@ __device__ void simt_rows(const ChunkParams& p, Smem<D>& sm, int b, const ChunkS
     }
     __syncthreads();
     {
-      float acc[RT / 2];
+      float acc[RT / RS];
 #pragma unroll
-      for (int i = 0; i < RT / 2; ++i) acc[i] = 0.f;
+      for (int i = 0; i < RT / RS; ++i) acc[i] = 0.f;
 #pragma unroll 4
       for (int d = 0; d < D; d += 4) {
         const float4 kf = *reinterpret_cast<const float4*>(&sm.k[kk][d]);
 #pragma unroll
-        for (int i = 0; i < RT / 2; ++i) {
-          const float4 q = *reinterpret_cast<const float4*>(&sm.q[hr + 2 * i][d]);
+        for (int i = 0; i < RT / RS; ++i) {
+          const float4 q = *reinterpret_cast<const float4*>(&sm.q[hr + RS * i][d]);
           acc[i] += q.x * kf.x + q.y * kf.y + q.z * kf.z + q.w * kf.w;
         }
       }
 #pragma unroll
-      for (int i = 0; i < RT / 2; ++i) {
-        const int r = hr + 2 * i, at = ctx + (row0 + r) / p.group;
+      for (int i = 0; i < RT / RS; ++i) {
+        const int r = hr + RS * i, at = ctx + (row0 + r) / p.group;
         const bool vis = r < nrows && t0 + kk >= chunk_low(p, at) && t0 + kk < chunk_high(p, at, seq.kv_len);
         sm.s[r][kk] = vis ? acc[i] * p.scale_log2 : -INFINITY;
       }
     }
     __syncthreads();
     for (int r = warp; r < RT; r += NT / 32) {
-      const float a0 = sm.s[r][lane], a1 = sm.s[r][lane + 32];
+      const float a0 = lane < TK ? sm.s[r][lane] : -INFINITY, a1 = lane + 32 < TK ? sm.s[r][lane + 32] : -INFINITY;
       float mx = fmaxf(a0, a1);
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
@@ -170,8 +279,8 @@ __device__ void simt_rows(const ChunkParams& p, Smem<D>& sm, int b, const ChunkS
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
       __syncwarp();
-      sm.s[r][lane] = p0;
-      sm.s[r][lane + 32] = p1;
+      if (lane < TK) sm.s[r][lane] = p0;
+      if (lane + 32 < TK) sm.s[r][lane + 32] = p1;
       if (lane == 0) {
         sm.alpha[r] = alpha;
         sm.m[r] = m_new;
@@ -220,7 +329,7 @@ __device__ void simt_rows(const ChunkParams& p, Smem<D>& sm, int b, const ChunkS
 template <int D, bool FP8>
 __global__ void __launch_bounds__(NT) chunk_simt_kernel(ChunkParams p) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw);
+  Smem<D, kSimtKeyTile>& sm = *reinterpret_cast<Smem<D, kSimtKeyTile>*>(smem_raw);
   pdl_wait_prior();
   const int64_t first = static_cast<int64_t>(blockIdx.x) * RT, last = first + RT;
   const int g = blockIdx.y;
@@ -238,12 +347,99 @@ __global__ void __launch_bounds__(NT) chunk_simt_kernel(ChunkParams p) {
   }
 }
 
-// Sequences that could not be served get out = 0 and lse = -inf.
-constexpr int kFinishThreads = 128;
+// The end of a call: joins the parts of units that blocks split, computes again the units in
+// which a hidden value was not finite (on CUDA cores, 16 keys at a time so that the shared memory
+// of a block is small), and clears the rows of sequences that could not be served.
+constexpr int kFinishThreads = NT;
+constexpr int kFinishParts = 8;  // blocks per joined unit
+constexpr int kRedoKeys = 16;
+
+// The block of the work list that owns virtual step t.
+__device__ __forceinline__ int owner_of(long long t, long long total, int blocks) {
+  return static_cast<int>(((t + 1) * blocks - 1) / total);
+}
+
+// A unit that ends in block c's first stop, having begun in an earlier block.
+template <int D>
+__device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part) {
+  ChunkWalk w;
+  if (!w.begin(p, c) || w.starts_unit() || !w.ends_unit() || p.seq_bad[w.b] != 0) return;
+  const long long total = p.work->total;
+  const int active = p.work->active;
+  // the unit's first step, from this block's
+  const long long at = c * total / active - p.work->starts[c].w + kChunkOverhead;
+  const int first = owner_of(at, total, active), subs = w.u.twin ? 2 : 1, n = (c - first + 1) * subs;
+  const int tile_rows = p.tile_tokens * p.group;
+  constexpr int C8 = D / 8;
+  const int rows = w.u.twin ? kChunkTileRows : 2 * kChunkTileRows;
+  for (int i = part * kFinishThreads + threadIdx.x; i < rows * C8; i += kFinishParts * kFinishThreads) {
+    const int r = i / C8, c8 = i % C8, tr = r & (kChunkTileRows - 1);
+    const int token = (r >= kChunkTileRows ? p.tile_tokens : 0) + tr / p.group;
+    if (tr >= tile_rows || token >= w.u.tokens) continue;
+    float M = -INFINITY, L = 0.f, acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    constexpr int SB = 3;  // parts whose loads are in flight together
+    for (int s0 = 0; s0 < n; s0 += SB) {
+      float2 ml[SB];
+      float4 lo[SB], hi[SB];
+#pragma unroll
+      for (int k = 0; k < SB; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        if (s0 + k < n) {
+          const int cta = first + (s0 + k) / subs, sub = (s0 + k) % subs;
+          const int64_t row = static_cast<int64_t>(2 * cta + (cta == first ? 1 : 0)) * (2 * kChunkTileRows) + sub * kChunkTileRows + r;
+          ml[k] = __ldcg(&p.partial_ml[row]);
+          const float4* src = reinterpret_cast<const float4*>(p.partial_o + row * D) + 2 * c8;
+          lo[k] = __ldcg(src);
+          hi[k] = __ldcg(src + 1);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < SB; ++k) {
+        if (s0 + k >= n || ml[k].x == -INFINITY) continue;  // saw no key
+        const float m = fmaxf(M, ml[k].x);
+        const float old = M == -INFINITY ? 0.f : ex2(M - m), x = ex2(ml[k].x - m);
+        const float v[8] = {lo[k].x, lo[k].y, lo[k].z, lo[k].w, hi[k].x, hi[k].y, hi[k].z, hi[k].w};
+        L = L * old + ml[k].y * x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = acc[e] * old + v[e] * x;
+        M = m;
+      }
+    }
+    const float inv = 1.f / L;
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __nv_bfloat162 pr = __floats2bfloat162_rn(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+      o[e] = *reinterpret_cast<const uint32_t*>(&pr);
+    }
+    const int64_t head = static_cast<int64_t>(w.seq.row0 + w.u.token0 + token) * p.hq + w.g * p.group + tr % p.group;
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + head * D + c8 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (c8 == 0 && p.lse) p.lse[head] = (M + log2f(L)) * 0.6931471805599453f;
+  }
+}
+
 template <int D, bool FP8>
 __global__ void __launch_bounds__(kFinishThreads) chunk_finish_kernel(ChunkParams p) {
+  __shared__ Smem<D, kRedoKeys> sm;
   pdl_wait_prior();
-  for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+  if (p.blocks) {
+    if (blockIdx.x > 0 && static_cast<int>(blockIdx.x) < p.blocks) join_unit<D>(p, blockIdx.x, blockIdx.y);
+    const int redo = min(__ldcg(&p.redo[0].x), p.redo_cap);
+    if (redo > 0) {
+      const int tiles = (2 * p.tile_tokens * p.group + RT - 1) / RT;
+      for (int64_t i = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x; i < static_cast<int64_t>(redo) * tiles;
+           i += static_cast<int64_t>(gridDim.x) * gridDim.y) {
+        const int4 e = __ldcg(&p.redo[1 + i / tiles]);
+        const ChunkSeq seq = p.seqs[e.x];
+        const ChunkUnit u = chunk_unit(p, seq, e.z);
+        const int row = static_cast<int>(i % tiles) * RT, nrows = min(RT, u.tokens * p.group - row);
+        if (nrows > 0 && p.seq_bad[e.x] == 0) simt_rows<D, FP8>(p, sm, e.x, seq, e.y, u.token0 * p.group + row, nrows);
+      }
+    }
+  }
+  for (int b = blockIdx.y * gridDim.x + blockIdx.x; b < p.batch; b += gridDim.x * gridDim.y) {
     if (p.seq_bad[b] == 0) continue;
     const int r0 = p.row_start[b], r1 = p.row_start[b + 1];
     if (!chunk_rows_ok(p, r0, r1)) continue;  // there are none to clear
@@ -257,17 +453,19 @@ __global__ void __launch_bounds__(kFinishThreads) chunk_finish_kernel(ChunkParam
 
 template <int D, bool FP8>
 cudaError_t launch_simt_d(const ChunkParams& p, cudaStream_t stream) {
-  const size_t smem = sizeof(Smem<D>);
-  cudaError_t e = cudaFuncSetAttribute(chunk_simt_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  const size_t smem = sizeof(Smem<D, kSimtKeyTile>);
+  const cudaError_t e = cudaFuncSetAttribute(chunk_simt_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   const int64_t tiles = (static_cast<int64_t>(p.rows) * p.group + RT - 1) / RT;
-  e = launch_overlapped(chunk_simt_kernel<D, FP8>, dim3(static_cast<unsigned>(tiles), p.hkv), NT, smem, stream, p);
-  if (e != cudaSuccess) return e;
-  return launch_overlapped(chunk_finish_kernel<D, FP8>, dim3(p.batch < 256 ? p.batch : 256), kFinishThreads, 0, stream, p);
+  return launch_overlapped(chunk_simt_kernel<D, FP8>, dim3(static_cast<unsigned>(tiles), p.hkv), NT, smem, stream, p);
 }
 
-}  // namespace
+template <int D, bool FP8>
+cudaError_t launch_finish_d(const ChunkParams& p, cudaStream_t stream) {
+  const dim3 grid = p.blocks ? dim3(p.blocks, kFinishParts) : dim3(p.batch < 256 ? p.batch : 256);
+  return launch_overlapped(chunk_finish_kernel<D, FP8>, grid, kFinishThreads, 0, stream, p);
+}
 
 ChunkParams make_chunk_params(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws) {
   ChunkParams p{};
@@ -296,16 +494,36 @@ ChunkParams make_chunk_params(const spec_chunk_attn_args_t& a, const ChunkPlan& 
   p.lse = a.lse;
   p.status = reinterpret_cast<uint32_t*>(ws);
   p.seqs = reinterpret_cast<ChunkSeq*>(ws + P.seqs);
-  p.seq_bad = reinterpret_cast<int32_t*>(p.seqs + a.batch);
+  p.seq_bad = reinterpret_cast<int32_t*>(ws + P.bad);
+  if (P.path == SPEC_ATTN_TENSOR_CORES) {
+    p.tile_tokens = P.tile_tokens;
+    p.max_units = P.max_units;
+    p.blocks = P.grid;
+    p.cum = reinterpret_cast<long long*>(ws + P.cum);
+    p.work = reinterpret_cast<ChunkWork*>(ws + P.work);
+    p.redo = reinterpret_cast<int4*>(ws + P.redo);
+    p.redo_cap = P.redo_cap;
+    p.partial_o = reinterpret_cast<float*>(ws + P.partial_o);
+    p.partial_ml = reinterpret_cast<float2*>(ws + P.partial_ml);
+  }
   return p;
 }
 
-cudaError_t launch_chunk(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws, cudaStream_t stream) {
-  const ChunkParams p = make_chunk_params(a, P, ws);
-  const cudaError_t e = launch_overlapped(chunk_setup_kernel, dim3(1), kSetupThreads, 0, stream, p);
+}  // namespace
+
+cudaError_t launch_chunk(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws, cudaStream_t stream,
+                         bool starve) {
+  ChunkParams p = make_chunk_params(a, P, ws);
+  p.starve = starve ? 1 : 0;
+  cudaError_t e = launch_overlapped(chunk_setup_kernel, dim3(1), kSetupThreads, 0, stream, p);
   if (e != cudaSuccess) return e;
-  if (P.fp8) return a.head_dim == 128 ? launch_simt_d<128, true>(p, stream) : launch_simt_d<64, true>(p, stream);
-  return a.head_dim == 128 ? launch_simt_d<128, false>(p, stream) : launch_simt_d<64, false>(p, stream);
+  const bool wide = a.head_dim == 128;
+  if (p.blocks) e = launch_chunk_tc(a, p, stream);
+  else if (P.fp8) e = wide ? launch_simt_d<128, true>(p, stream) : launch_simt_d<64, true>(p, stream);
+  else e = wide ? launch_simt_d<128, false>(p, stream) : launch_simt_d<64, false>(p, stream);
+  if (e != cudaSuccess) return e;
+  if (P.fp8) return wide ? launch_finish_d<128, true>(p, stream) : launch_finish_d<64, true>(p, stream);
+  return wide ? launch_finish_d<128, false>(p, stream) : launch_finish_d<64, false>(p, stream);
 }
 
 }  // namespace specv

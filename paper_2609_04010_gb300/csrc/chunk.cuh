@@ -16,22 +16,32 @@ cudaError_t launch_copy(const spec_copy_args_t& a, cudaStream_t stream);
 
 // --- attention of chunks ---
 struct ChunkPlan {
-  int path;        // SPEC_ATTN_CUDA_CORES or SPEC_ATTN_TENSOR_CORES
-  int fp8;         // the cache is the 8-bit one
-  int tile_tokens; // tensor cores: tokens of an M tile, 128 / group
-  int grid;        // tensor cores: blocks
-  int max_units;   // tensor cores: token tiles of all sequences, at most
-  int64_t slots;   // tensor cores: partial results
-  size_t seqs, cum, starts, redo, partial_o, partial_ml, end;
+  int path;          // SPEC_ATTN_CUDA_CORES or SPEC_ATTN_TENSOR_CORES
+  int fp8;           // the cache is the 8-bit one
+  int tile_tokens;   // tensor cores: tokens of an M tile, 128 / group
+  int grid;          // tensor cores: blocks
+  int max_units;     // tensor cores: units per KV head, at most
+  int redo_cap;      // tensor cores: units that may have to be computed again
+  size_t seqs, bad, cum, work, redo, partial_o, partial_ml, end;
 };
+bool chunk_tc_fits(const spec_chunk_attn_args_t& a);
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path);
-constexpr int kChunkSlotRows = 256;
+constexpr int kChunkKeyTile = 128;     // keys of a tile on the tensor cores
+constexpr int kChunkTileRows = 128;    // query rows of an M tile
+constexpr int kChunkOverhead = 1;      // steps that a unit's start is charged in the work list
 
 // One sequence of the batch, as the setup leaves it.
 struct ChunkSeq {
   int row0, n;     // its rows of q; n = 0: nothing to do
   int kv_len;
-  int first_unit;  // its first token tile among all (tensor cores)
+  int first_unit;  // its first unit among all (tensor cores)
+};
+// The work list of the tensor-core kernel, and where each block starts in it: the sequence, the
+// KV head, the unit of its tokens, and the (virtual) step in it.
+struct ChunkWork {
+  long long total;
+  int active, pad;   // blocks with work
+  int4 starts[1];    // [active]
 };
 
 struct ChunkParams {
@@ -51,22 +61,21 @@ struct ChunkParams {
   float* lse;
   uint32_t* status;
   int32_t* seq_bad;  // [batch]: its rows become out = 0, lse = -inf at the end
-  ChunkSeq* seqs;    // [batch]
-  // tensor cores
-  int tile_tokens, tile_rows, max_units, blocks, overhead;
-  int64_t* cum;      // [max_units + 1]: steps before a token tile, per KV head
-  int4* starts;      // [blocks + 1]
-  int4* redo;        // [0].x: how many; then units whose values have to be taken apart
+  ChunkSeq* seqs;    // [batch + 1]
+  // tensor cores (blocks = 0: not used)
+  int tile_tokens, max_units, blocks;
+  long long* cum;      // [max_units + 1]: virtual steps before a unit, for one KV head
+  ChunkWork* work;
+  int4* redo;          // [0].x: how many; then (sequence, KV head, unit) to compute again
   int redo_cap;
-  float* partial_o;    // [slot][kChunkSlotRows][D]
-  float2* partial_ml;  // [slot][kChunkSlotRows] = (m, l)
+  float* partial_o;    // [2 * blocks][2 * kChunkTileRows][D]
+  float2* partial_ml;  // [2 * blocks][2 * kChunkTileRows] = (m, l)
   int starve;          // test hook: the producers issue no copies, so the waits run out
 };
 
-ChunkParams make_chunk_params(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws);
-cudaError_t launch_chunk(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws, cudaStream_t stream);
-cudaError_t launch_chunk_tc(const spec_chunk_attn_args_t& a, const ChunkPlan& P, const ChunkParams& p,
-                            cudaStream_t stream, bool starve);
+cudaError_t launch_chunk(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws, cudaStream_t stream,
+                         bool starve = false);
+cudaError_t launch_chunk_tc(const spec_chunk_attn_args_t& a, const ChunkParams& p, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // Whether rows [r0, r1) are rows of q.
@@ -78,6 +87,89 @@ __device__ __forceinline__ int chunk_low(const ChunkParams& p, int at) {
   return p.window > 0 ? max(0, at - p.window + 1) : 0;
 }
 __device__ __forceinline__ int chunk_high(const ChunkParams& p, int at, int n) { return p.causal ? at + 1 : n; }
+
+// A unit of the tensor-core kernel: the query rows of up to 2 * tile_tokens tokens of a sequence
+// and one KV head, in two M tiles; with no more than one tile of tokens both M tiles hold the same
+// rows and take every second tile of keys each ("twin"). Its work is counted in steps: a tile of
+// keys for both M tiles, or, twin, one for each.
+struct ChunkUnit {
+  int token0, tokens;  // of the sequence's new tokens
+  int low, high;       // keys that any of them sees
+  int full_low, full_high;  // keys that all of them see
+  int tile0, tiles, steps;
+  bool twin;
+  __device__ __forceinline__ int step_tiles(int i, int h) const { return twin ? 2 * i + h : i; }
+  __device__ __forceinline__ bool has(int i, int h) const { return !twin || 2 * i + h < tiles; }
+};
+__device__ __forceinline__ int chunk_units(const ChunkParams& p, int n) {
+  return (n + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens);
+}
+__device__ __forceinline__ ChunkUnit chunk_unit(const ChunkParams& p, const ChunkSeq& s, int rt) {
+  ChunkUnit u;
+  u.token0 = rt * 2 * p.tile_tokens;
+  u.tokens = min(2 * p.tile_tokens, s.n - u.token0);
+  u.twin = u.tokens <= p.tile_tokens;
+  const int at0 = s.kv_len - s.n + u.token0, at1 = at0 + u.tokens - 1;
+  u.low = chunk_low(p, at0);
+  u.full_low = chunk_low(p, at1);
+  u.full_high = chunk_high(p, at0, s.kv_len);
+  u.high = chunk_high(p, at1, s.kv_len);
+  u.tile0 = u.low / kChunkKeyTile;
+  u.tiles = (u.high + kChunkKeyTile - 1) / kChunkKeyTile - u.tile0;
+  u.steps = u.twin ? (u.tiles + 1) / 2 : u.tiles;
+  return u;
+}
+
+// A walk over a block's part of the work list: each stop is a run of steps of one unit. All roles
+// of a block (and the joining of split units) walk alike. Units follow one another within a KV
+// head, then the heads of a sequence, then the sequences.
+struct ChunkWalk {
+  long long left;    // virtual steps of the range from here on
+  int b, g, rt, off; // off: the virtual step of the unit at which the stop begins
+  int units;         // of the sequence
+  ChunkSeq seq;
+  ChunkUnit u;
+  int s0, ns;        // the stop's first step, and how many
+  __device__ __forceinline__ void stop(const ChunkParams& p) {
+    u = chunk_unit(p, seq, rt);
+    const int all = u.steps + kChunkOverhead;
+    const int take = static_cast<int>(min(static_cast<long long>(all - off), left));
+    s0 = max(off - kChunkOverhead, 0);
+    ns = max(off + take - kChunkOverhead, 0) - s0;
+    off += take;
+    left -= take;
+  }
+  __device__ __forceinline__ bool begin(const ChunkParams& p, int block) {
+    const int active = p.work->active;
+    if (block >= active) return false;
+    const long long total = p.work->total;
+    const long long t0 = block * total / active;
+    left = (block + 1) * total / active - t0;
+    const int4 s = p.work->starts[block];
+    b = s.x; g = s.y; rt = s.z; off = s.w;
+    seq = p.seqs[b];
+    units = chunk_units(p, seq.n);
+    stop(p);
+    return ns > 0;
+  }
+  __device__ __forceinline__ bool next(const ChunkParams& p) {
+    if (left <= kChunkOverhead) return false;  // nothing, or no more than a unit's start
+    off = 0;
+    if (++rt == units) {
+      rt = 0;
+      if (++g == p.hkv) {
+        g = 0;
+        do seq = p.seqs[++b]; while (seq.n == 0 && b < p.batch);
+        units = chunk_units(p, seq.n);
+      }
+    }
+    stop(p);
+    return ns > 0;
+  }
+  __device__ __forceinline__ bool starts_unit() const { return s0 == 0; }
+  __device__ __forceinline__ bool ends_unit() const { return s0 + ns == u.steps; }
+  __device__ __forceinline__ bool whole() const { return ns == u.steps; }
+};
 #endif
 
 }  // namespace specv

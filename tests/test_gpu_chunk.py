@@ -394,3 +394,18 @@ def test_workspace_of_another_device_type_is_refused():
         b.chunk_attention_args(a, torch.zeros(1 << 20, dtype=torch.uint8))
     with pytest.raises(b.SpecError):
         b.chunk_attention_args(a, b.new_workspace(256))
+
+
+def test_waits_run_out():
+    """With idle copy producers every wait ends, the status says so, and the workspace serves on."""
+    from paper_2609_04010_gb300 import binding as b
+    c = make([1, 300, 2], [900, 50, 10], seed=27)
+    out, lse = torch.empty(c["q"].shape, dtype=torch.bfloat16, device="cuda"), torch.empty(c["q"].shape[:2], device="cuda")
+    a = b.chunk_attn_args(c["q"], c["cache"], c["table"], i32(c["starts"]), i32(c["lens"]), out, lse)
+    ws = b.new_workspace(b.chunk_attn_workspace_size(a))
+    b.test_chunk_attention_wait_timeout_args(a, ws)
+    assert b.read_device_status(ws) == (6, b.FLAG_TIMEOUT)
+    b.chunk_attention_args(a, ws)
+    assert b.read_device_status(ws)[0] == 0
+    want = ref.chunk_attention(c["q"], c["cache"], c["table"], c["starts"], c["lens"])
+    ref.check_chunk((out, lse), want, 128, True)
