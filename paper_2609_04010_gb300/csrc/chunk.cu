@@ -363,19 +363,23 @@ __device__ __forceinline__ int owner_of(long long t, long long total, int blocks
 template <int D>
 __device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part) {
   ChunkWalk w;
-  if (!w.begin(p, c) || w.starts_unit() || !w.ends_unit() || p.seq_bad[w.b] != 0) return;
+  if (!w.begin(p, c) || w.starts_unit() || p.seq_bad[w.b] != 0) return;
+  const ChunkUnit u = w.unit(p);
+  if (!w.ends_unit(u)) return;
   const long long total = p.work->total;
   const int active = p.work->active;
   // the unit's first step, from this block's
   const long long at = c * total / active - p.work->starts[c].w + kChunkOverhead;
-  const int first = owner_of(at, total, active), subs = w.u.twin ? 2 : 1, n = (c - first + 1) * subs;
+  const int first = owner_of(at, total, active), subs = u.twin ? 2 : 1, n = (c - first + 1) * subs;
   const int tile_rows = p.tile_tokens * p.group;
   constexpr int C8 = D / 8;
-  const int rows = w.u.twin ? kChunkTileRows : 2 * kChunkTileRows;
-  for (int i = part * kFinishThreads + threadIdx.x; i < rows * C8; i += kFinishParts * kFinishThreads) {
-    const int r = i / C8, c8 = i % C8, tr = r & (kChunkTileRows - 1);
+  const int rows = u.twin ? kChunkTileRows : 2 * kChunkTileRows;
+  // a warp takes 8 rows x 32 columns, a thread 8 columns of a row
+  const int lane = threadIdx.x & 31;
+  for (int x = part * (kFinishThreads / 32) + (threadIdx.x >> 5); x < rows / 8 * (C8 / 4); x += kFinishParts * (kFinishThreads / 32)) {
+    const int r = x / (C8 / 4) * 8 + (lane & 7), c8 = x % (C8 / 4) * 4 + (lane >> 3), tr = r & (kChunkTileRows - 1);
     const int token = (r >= kChunkTileRows ? p.tile_tokens : 0) + tr / p.group;
-    if (tr >= tile_rows || token >= w.u.tokens) continue;
+    if (tr >= tile_rows || token >= u.tokens) continue;
     float M = -INFINITY, L = 0.f, acc[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
@@ -388,11 +392,12 @@ __device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part)
         ml[k] = make_float2(-INFINITY, 0.f);
         if (s0 + k < n) {
           const int cta = first + (s0 + k) / subs, sub = (s0 + k) % subs;
-          const int64_t row = static_cast<int64_t>(2 * cta + (cta == first ? 1 : 0)) * (2 * kChunkTileRows) + sub * kChunkTileRows + r;
-          ml[k] = __ldcg(&p.partial_ml[row]);
-          const float4* src = reinterpret_cast<const float4*>(p.partial_o + row * D) + 2 * c8;
+          const int64_t slot = 2 * static_cast<int64_t>(cta) + (cta == first ? 1 : 0);
+          const int row = sub * kChunkTileRows + r;
+          ml[k] = __ldcg(&p.partial_ml[slot * (2 * kChunkTileRows) + row]);
+          const float4* src = reinterpret_cast<const float4*>(p.partial_o) + (slot * (D / 4) + 2 * c8) * (2 * kChunkTileRows) + row;
           lo[k] = __ldcg(src);
-          hi[k] = __ldcg(src + 1);
+          hi[k] = __ldcg(src + 2 * kChunkTileRows);
         }
       }
 #pragma unroll
@@ -414,7 +419,7 @@ __device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part)
       const __nv_bfloat162 pr = __floats2bfloat162_rn(acc[2 * e] * inv, acc[2 * e + 1] * inv);
       o[e] = *reinterpret_cast<const uint32_t*>(&pr);
     }
-    const int64_t head = static_cast<int64_t>(w.seq.row0 + w.u.token0 + token) * p.hq + w.g * p.group + tr % p.group;
+    const int64_t head = static_cast<int64_t>(w.row0 + u.token0 + token) * p.hq + w.g * p.group + tr % p.group;
     *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + head * D + c8 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
     if (c8 == 0 && p.lse) p.lse[head] = (M + log2f(L)) * 0.6931471805599453f;
   }

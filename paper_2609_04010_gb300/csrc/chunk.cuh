@@ -68,7 +68,7 @@ struct ChunkParams {
   ChunkWork* work;
   int4* redo;          // [0].x: how many; then (sequence, KV head, unit) to compute again
   int redo_cap;
-  float* partial_o;    // [2 * blocks][2 * kChunkTileRows][D]
+  float* partial_o;    // [2 * blocks][D / 4][2 * kChunkTileRows][4]
   float2* partial_ml;  // [2 * blocks][2 * kChunkTileRows] = (m, l)
   int starve;          // test hook: the producers issue no copies, so the waits run out
 };
@@ -122,53 +122,66 @@ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkParams& p, const Chun
 
 // A walk over a block's part of the work list: each stop is a run of steps of one unit. All roles
 // of a block (and the joining of split units) walk alike. Units follow one another within a KV
-// head, then the heads of a sequence, then the sequences.
+// head, then the heads of a sequence, then the sequences. The walk keeps few values, and gives the
+// stop's unit anew where it is asked for, because it lives beside loops that need the registers.
 struct ChunkWalk {
-  long long left;    // virtual steps of the range from here on
-  int b, g, rt, off; // off: the virtual step of the unit at which the stop begins
+  int left;          // virtual steps of the range behind the stop
+  int b, g, rt;
   int units;         // of the sequence
-  ChunkSeq seq;
-  ChunkUnit u;
+  int row0, n, kv_len;
   int s0, ns;        // the stop's first step, and how many
-  __device__ __forceinline__ void stop(const ChunkParams& p) {
-    u = chunk_unit(p, seq, rt);
-    const int all = u.steps + kChunkOverhead;
-    const int take = static_cast<int>(min(static_cast<long long>(all - off), left));
+  __device__ __forceinline__ void enter(const ChunkParams& p) {
+    const ChunkSeq s = p.seqs[b];
+    row0 = s.row0;
+    n = s.n;
+    kv_len = s.kv_len;
+  }
+  __device__ __forceinline__ ChunkUnit unit(const ChunkParams& p) const {
+    int r = rt;
+    asm volatile("" : "+r"(r));  // not kept from before
+    return chunk_unit(p, {row0, n, kv_len, 0}, r);
+  }
+  __device__ __forceinline__ void stop(const ChunkParams& p, int off) {
+    const int all = chunk_unit(p, {row0, n, kv_len, 0}, rt).steps + kChunkOverhead, take = min(all - off, left);
     s0 = max(off - kChunkOverhead, 0);
     ns = max(off + take - kChunkOverhead, 0) - s0;
-    off += take;
     left -= take;
   }
   __device__ __forceinline__ bool begin(const ChunkParams& p, int block) {
     const int active = p.work->active;
     if (block >= active) return false;
-    const long long total = p.work->total;
-    const long long t0 = block * total / active;
-    left = (block + 1) * total / active - t0;
+    const long long total = p.work->total, t0 = block * total / active;
+    left = static_cast<int>((block + 1) * total / active - t0);
     const int4 s = p.work->starts[block];
-    b = s.x; g = s.y; rt = s.z; off = s.w;
-    seq = p.seqs[b];
-    units = chunk_units(p, seq.n);
-    stop(p);
+    b = s.x; g = s.y; rt = s.z;
+    enter(p);
+    units = chunk_units(p, n);
+    stop(p, s.w);
     return ns > 0;
   }
   __device__ __forceinline__ bool next(const ChunkParams& p) {
     if (left <= kChunkOverhead) return false;  // nothing, or no more than a unit's start
-    off = 0;
     if (++rt == units) {
       rt = 0;
       if (++g == p.hkv) {
         g = 0;
-        do seq = p.seqs[++b]; while (seq.n == 0 && b < p.batch);
-        units = chunk_units(p, seq.n);
+        do {
+          ++b;
+          enter(p);
+        } while (n == 0 && b < p.batch);
+        units = chunk_units(p, n);
       }
     }
-    stop(p);
+    stop(p, 0);
     return ns > 0;
   }
   __device__ __forceinline__ bool starts_unit() const { return s0 == 0; }
-  __device__ __forceinline__ bool ends_unit() const { return s0 + ns == u.steps; }
-  __device__ __forceinline__ bool whole() const { return ns == u.steps; }
+  __device__ __forceinline__ bool ends_unit(const ChunkUnit& u) const { return s0 + ns == u.steps; }
+  __device__ __forceinline__ bool whole(const ChunkUnit& u) const { return ns == u.steps; }
+  // tiles of M tile h at this stop
+  __device__ __forceinline__ int tiles(const ChunkUnit& u, int h) const {
+    return u.twin ? max((min(2 * (s0 + ns), u.tiles) - 2 * s0 + 1 - h) / 2, 0) : ns;
+  }
 };
 #endif
 

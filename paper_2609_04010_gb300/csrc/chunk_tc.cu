@@ -11,14 +11,15 @@
 // keys to each, so that single tokens keep two tiles in flight too.
 //
 // Warps:
-//   0..3, 4..7  softmax of M tile 0 and 1, a thread per row: 128 scores from TMEM, maximum,
-//               weights as bf16 over the first half of the scores' columns, from which the second
-//               product reads them; at a unit's end the outputs
-//   8, 9        producers of K (and Q) and of V: a TMA box per page, into two rings of tiles
-//   10          products: S of the next tile follows at once on the O += P V that read its columns
-//   11          passes V on, and makes that of keys that some row does not see finite first (their weight 0 is multiplied):
-//               keys that no row sees are cleared; where one that some rows see is not finite, the
-//               unit is noted and computed again on CUDA cores after all
+//   0..7, 8..15 softmax of M tile 0 and 1, two threads per row, each with half of a tile's keys: 64
+//               scores from TMEM, maximum, weights as bf16 over the first half of their columns, from
+//               which the second product reads them; at a unit's end half of the row's outputs
+//   16, 17      producers of K (and Q) and of V: a TMA box per page, into two rings of tiles
+//   18          products, one thread: S of the next tile follows at once on the O += P V that read
+//               its columns, and the M tiles take turns
+//   19          passes V on, and makes that of keys that some row does not see finite first (their
+//               weight 0 is multiplied): keys that no row sees are cleared; where one that some rows
+//               see is not finite, the unit is noted and computed again on CUDA cores after all
 // The list of units is cut into equal ranges of steps, one per block (chunk.cuh); parts of split
 // units are joined by the finishing launch. Every wait is bounded: one that runs out sets
 // SPEC_FLAG_TIMEOUT, and the block drains its copies and products, frees TMEM and returns.
@@ -36,10 +37,11 @@ using namespace tcx;
 
 constexpr int TK = kChunkKeyTile;
 constexpr int MR = kChunkTileRows;
-constexpr int kSoftWarps = 8;
+constexpr int kSoftWarps = 16;
 constexpr int kThreads = 32 * (kSoftWarps + 4);
-// registers of a softmax and of another thread: 256 * 216 + 128 * 72 = 384 * 168, the launch's
-constexpr int kSoftRegs = 216, kOtherRegs = 72;
+constexpr int HK = TK / 2;  // keys of a tile that a thread weighs
+// registers of a softmax and of another thread: 512 * 104 + 128 * 64 = 640 * 96, the launch's
+constexpr int kSoftRegs = 104, kOtherRegs = 64;
 // Past this the product of a score and the scale loses whole steps of the exponent.
 constexpr float kFar = 4194304.f;  // 2^22
 
@@ -54,8 +56,10 @@ struct Cfg {
   static constexpr uint32_t OFF_Q = 0;              // [2][DH][128 rows][128 B]
   static constexpr uint32_t OFF_K = OFF_Q + 2 * QTILE;
   static constexpr uint32_t OFF_V = OFF_K + KST * TILE;
-  static constexpr uint32_t OFF_ML = OFF_V + VST * TILE;  // float2 [128]: the second half's (m, l)
-  static constexpr uint32_t OFF_BAR = OFF_ML + MR * 8;
+  // float [2][128]: between a row's two threads; or float2 [128]: a twin's (m, l)
+  static constexpr uint32_t OFF_XCH = OFF_V + VST * TILE;
+  static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps]
+  static constexpr uint32_t OFF_BAR = (OFF_WALK + kSoftWarps * sizeof(ChunkWalk) + 7) / 8 * 8;
   // k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], v_ready[VST], s_full[2], p_full[2],
   // o_full[2], q_full, q_free, drain, joined
   static constexpr int NBAR = 2 * KST + 3 * VST + 10;
@@ -80,8 +84,36 @@ __device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map,
       "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(half), "r"(head), "r"(row), "r"(bar)
       : "memory");
 }
+// Whether any thread of the two warps of 32 rows has `any` (named barrier).
+__device__ __forceinline__ bool pair_any(int bar, bool any) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, 64, p;\n selp.u32 %0, 1, 0, q;\n}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(any)), "r"(bar)
+      : "memory");
+  return r != 0;
+}
 __device__ __forceinline__ void bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// Four lanes' 4 x 4 pieces of 16 bytes turned round: afterwards c[j] is piece (lane & 3) of the j-th
+// lane of the four, so that they store 64 bytes of a row together.
+__device__ __forceinline__ void turn_quad(uint4* c, int lane) {
+  const bool odd = lane & 1, high = lane & 2;
+  auto swap = [](uint4& a, uint4& b, bool first, int mask) {
+    uint32_t* x = reinterpret_cast<uint32_t*>(&a);
+    uint32_t* y = reinterpret_cast<uint32_t*>(&b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, first ? x[e] : y[e], mask);
+      if (first) x[e] = got; else y[e] = got;
+    }
+  };
+  swap(c[0], c[1], odd, 1);
+  swap(c[2], c[3], odd, 1);
+  swap(c[0], c[2], high, 2);
+  swap(c[1], c[3], high, 2);
 }
 // (a, b) = (a, b) * s + n, two fp32 lanes at once
 __device__ __forceinline__ void fma2(float& a, float& b, float s, float n) {
@@ -111,8 +143,64 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// Products whose descriptors (desc_sw128) are a low word, which an offset in 16-byte units is added
+// to, and a constant high word: the issuing thread keeps few registers.
+__host__ __device__ constexpr uint32_t desc_high(uint32_t sbo) { return ((sbo >> 4) & 0x3FFFu) | (1u << 14) | (2u << 29); }
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, uint32_t lbo) { return ((saddr & 0x3FFFFu) >> 4) | ((lbo >> 4) << 16); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_low, uint32_t a_high, uint32_t b_low, uint32_t b_high,
+                                       uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %6, 0;\n mov.b64 a, {%1, %2};\n mov.b64 b, {%3, %4};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}" ::"r"(d),
+      "r"(a_low), "r"(a_high), "r"(b_low), "r"(b_high), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_low, uint32_t b_high, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %5, 0;\n mov.b64 b, {%2, %3};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n}" ::"r"(d),
+      "r"(a), "r"(b_low), "r"(b_high), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+      : "memory");
+}
+
 __device__ __forceinline__ void fewer_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+}
+
+// A warp's: clears the values of keys that no row of the unit sees, and tells whether one that some
+// rows do not see is not finite.
+template <int D>
+__device__ __forceinline__ bool finite_values(unsigned char* tile, int key0, const ChunkUnit& u) {
+  constexpr int kPieces = D / 8, kLoads = 4;  // 16-byte pieces of a key; loads in flight
+  // keys before `before` and from `after` on
+  const int before = min(max(u.full_low - key0, 0), TK), after = min(max(u.full_high - key0, before), TK);
+  const int n = (TK - (after - before)) * kPieces;
+  bool odd = false;
+  for (int c0 = threadIdx.x & 31; c0 < n; c0 += 32 * kLoads) {
+    uint4 v[kLoads];
+    uint4* at[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int c = c0 + 32 * k, piece = c % kPieces;
+      int key = c / kPieces;
+      key += key < before ? 0 : after - before;
+      at[k] = nullptr;
+      v[k] = make_uint4(0, 0, 0, 0);
+      if (c < n) {
+        uint4* from = reinterpret_cast<uint4*>(tile + (key >> 3) * Cfg<D>::GROUP + (piece >> 3) * 1024 + (key & 7) * 128 + (piece & 7) * 16);
+        if (key0 + key < u.low || key0 + key >= u.high) at[k] = from; else v[k] = *from;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      if (at[k]) *at[k] = v[k];
+      odd |= (__vcmpeq2(v[k].x & 0x7f807f80u, 0x7f807f80u) | __vcmpeq2(v[k].y & 0x7f807f80u, 0x7f807f80u) |
+              __vcmpeq2(v[k].z & 0x7f807f80u, 0x7f807f80u) | __vcmpeq2(v[k].w & 0x7f807f80u, 0x7f807f80u)) != 0;
+    }
+  }
+  fence_async_smem();
+  __syncwarp();
+  return odd;
 }
 
 template <int D>
@@ -134,7 +222,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto s_full = [&](int h) { return bar0 + 8u * (B0 + h); };
   auto p_full = [&](int h) { return bar0 + 8u * (B0 + 2 + h); };
   auto o_full = [&](int h) { return bar0 + 8u * (B0 + 4 + h); };
-  const uint32_t q_full = bar0 + 8u * (B0 + 6), q_free = bar0 + 8u * (B0 + 7), drain = bar0 + 8u * (B0 + 8);
+  const uint32_t q_full = bar0 + 8u * (B0 + 6), q_free = bar0 + 8u * (B0 + 7);
+  const uint32_t drain = bar0 + 8u * (B0 + 8);
   const uint32_t joined = bar0 + 8u * (B0 + 9);  // twins: the second Q tile's place is free again
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
@@ -142,8 +231,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NBAR; ++i) {
-      // p_full: the four warps of an M tile; joined: the eight of both
-      const int n = i == static_cast<int>(B0) + 2 || i == static_cast<int>(B0) + 3 ? 4 : i == static_cast<int>(B0) + 9 ? 8 : 1;
+      const int at = i - static_cast<int>(B0);
+      // p_full: the warps of an M tile; joined: of both
+      const int n = at == 2 || at == 3 ? kSoftWarps / 2 : at == 9 ? kSoftWarps : 1;
       mbar_init(bar0 + 8u * i, n);
     }
     *abort_flag = 0;
@@ -163,11 +253,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok) ok = mbar_wait(bar, parity, abort_flag, p.status);
     dead = !__all_sync(0xffffffffu, ok);
   };
-  ChunkWalk w;
 
   if (warp == kSoftWarps || warp == kSoftWarps + 1) {
     // ============================ producers ============================
     fewer_registers();
+    ChunkWalk w;
     const bool is_k = warp == kSoftWarps;
     const uint32_t nst = is_k ? KST : VST, ring = sbase + (is_k ? C::OFF_K : C::OFF_V);
     const CUtensorMap* map = is_k ? &map_k : &map_v;
@@ -179,18 +269,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto full = [&](uint32_t s) { return is_k ? k_full(s) : v_full(s); };
     auto empty = [&](uint32_t s) { return is_k ? k_empty(s) : v_empty(s); };
     for (bool more = !p.starve && w.begin(p, blockIdx.x); more && !dead; ++seg) {
+      const ChunkUnit u = w.unit(p);
       const int32_t* table = p.page_table + static_cast<int64_t>(w.b) * p.max_pages;
-      const int pages = (w.u.high - 1 >> psh) + 1;  // of the sequence, as far as the unit sees it
+      const int pages = (u.high - 1 >> psh) + 1;  // of the sequence, as far as the unit sees it
       // page ids, 32 at a time, the next 32 in flight
-      int base = (w.u.tile0 + w.u.step_tiles(w.s0, 0)) * npg;
+      int base = (u.tile0 + u.step_tiles(w.s0, 0)) * npg;
       auto load_id = [&](int at) { return at + lane < pages ? __ldg(table + at + lane) : 0; };
       int id = load_id(base), id_next = load_id(base + 32);
       bool bad = false, first = true;
-      const int per = w.u.twin ? 2 : 1;
+      const int per = u.twin ? 2 : 1;
       for (int x = 0; x < w.ns * per && !dead; ++x) {
         const int i = w.s0 + x / per, h = x % per;
-        if (!w.u.has(i, h)) continue;
-        const int tile = w.u.tile0 + w.u.step_tiles(i, h), key0 = tile * TK, pg0 = tile * npg;
+        if (!u.has(i, h)) continue;
+        const int tile = u.tile0 + u.step_tiles(i, h), key0 = tile * TK, pg0 = tile * npg;
         while (pg0 >= base + 32) {
           base += 32;
           id = id_next;
@@ -200,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (it >= nst) wait(empty(st), (it / nst - 1) & 1);
         if (dead) break;
         // pages with a key that the unit sees
-        const int q0 = max(key0, w.u.low) - key0 >> psh, q1 = (min(key0 + TK, w.u.high) - 1 - key0 >> psh) + 1;
+        const int q0 = max(key0, u.low) - key0 >> psh, q1 = (min(key0 + TK, u.high) - 1 - key0 >> psh) + 1;
         if (lane == 0) mbar_arrive_tx(full(st), static_cast<uint32_t>(q1 - q0) * box);
         for (int q = q0; q < q1; ++q) {
           const int raw = __shfl_sync(0xffffffffu, id, pg0 - base + q);
@@ -217,12 +308,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (was_joined) wait(joined, joins++ & 1);
           if (dead) break;
           if (lane == 0) {
-            const int tiles = w.u.twin ? 1 : 2;
+            const int tiles = u.twin ? 1 : 2;
             mbar_arrive_tx(q_full, static_cast<uint32_t>(tiles * DH) * qbytes);
             for (int m = 0; m < tiles; ++m)
               for (int half = 0; half < DH; ++half)
                 tma_load_q(sbase + C::OFF_Q + m * C::QTILE + half * C::QHALF, &map_q, half, w.g * p.group,
-                           w.seq.row0 + w.u.token0 + m * p.tile_tokens, q_full);
+                           w.row0 + u.token0 + m * p.tile_tokens, q_full);
           }
           __syncwarp();
         }
@@ -232,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         p.seq_bad[w.b] = 1;
         set_status(p.status, SPEC_FLAG_BAD_PAGE);
       }
-      was_joined = w.u.twin && w.whole();
+      was_joined = u.twin && w.whole(u);
       more = w.next(p);
     }
     if (dead) {  // copies still in flight (bounded)
@@ -249,80 +340,69 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == kSoftWarps + 2) {
     // ============================ products ============================
+    // The tensor core keeps about four products in its queue, so that a turn's waits and
+    // book-keeping have to stay within their time: one copy of the code, waits before it, all
+    // products and commits of a turn in one block of one lane.
     fewer_registers();
+    ChunkWalk w;
     constexpr uint32_t kIdescS = idesc_bf16(MR, TK, false), kIdescO = idesc_bf16(MR, D, true);
+    const uint32_t q_low = desc_low(sbase + C::OFF_Q, 16), k_low = desc_low(sbase + C::OFF_K, 16),
+                   v_low = desc_low(sbase + C::OFF_V, 1024);
     uint32_t kc = 0, vc = 0, seg = 0;  // tiles of K and V taken so far
-    uint32_t pc[2] = {0, 0};           // tiles weighed by each M tile
-    bool issued = false;
-    auto scores = [&](int h, int tile_of_q, uint32_t st) {
-      if (lane == 0) {
-        const uint32_t kb = sbase + C::OFF_K + st * C::TILE, qa = sbase + C::OFF_Q + tile_of_q * C::QTILE;
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          mma_bf16(tmem + C::S_COL + h * TK, desc_sw128(qa + (kk / 4) * C::QHALF + (kk % 4) * 32u, 16, 1024),
-                   desc_sw128(kb + (kk / 4) * 1024u + (kk % 4) * 32u, 16, C::GROUP), kIdescS, kk > 0);
-        mma_commit(s_full(h));
-        issued = true;
-      }
-      __syncwarp();
+    uint32_t done = 0;                 // parity of the tiles that each M tile has weighed
+    bool gone = false;                 // of a lane; of all after a turn
+    auto ready = [&](uint32_t bar, uint32_t parity) {
+      if (!mbar_try(bar, parity)) gone = gone || !mbar_wait(bar, parity, abort_flag, p.status);
     };
-    auto release = [&](uint32_t bar) {
-      if (lane == 0) mma_commit(bar);
-      __syncwarp();
-    };
-    for (bool more = w.begin(p, blockIdx.x); more && !dead; ++seg) {
-      const bool twin = w.u.twin;
-      // S of step i for M tile h; the K tile is shared by both unless twin
-      auto next_scores = [&](int i, int h) {
-        const uint32_t st = kc % KST;
-        wait(k_full(st), (kc / KST) & 1);
-        if (dead) return;
-        tc_fence_after();
-        scores(h, twin ? 0 : h, st);
-        if (twin || h == 1) {
-          release(k_empty(st));
-          ++kc;
-        }
-      };
-      wait(q_full, seg & 1);
-      for (int h = 0; h < 2 && !dead; ++h)
-        if (w.u.has(w.s0, h)) next_scores(w.s0, h);
+    for (bool more = w.begin(p, blockIdx.x); more && !gone; ++seg) {
+      const ChunkUnit u = w.unit(p);
+      const bool twin = u.twin;
       const int end = w.s0 + w.ns;
-      for (int i = w.s0; i < end && !dead; ++i) {
-        for (int h = 0; h < 2 && !dead; ++h) {
-          if (!w.u.has(i, h)) continue;
-          const uint32_t st = vc % VST;
-          if (twin || h == 0) {
-            wait(v_full(st), (vc / VST) & 1);
-            wait(v_ready(st), (vc / VST) & 1);
-          }
-          wait(p_full(h), pc[h] & 1);
-          ++pc[h];
-          if (dead) break;
-          tc_fence_after();
-          if (lane == 0) {
-            const uint32_t vb = sbase + C::OFF_V + st * C::TILE;
+      ready(q_full, seg & 1);
+#pragma unroll 1
+      for (int x = -2; x < 2 * w.ns && !gone; ++x) {  // M tile h of step i, and its scores of step i + 1
+        const int i = w.s0 + (x >> 1), h = x & 1;
+        const bool weighed = x >= 0 && u.has(i, h), goes_on = i + 1 < end && u.has(i + 1, h);
+        const bool own = twin || h == 0, frees = twin || h == 1;  // both M tiles use one tile unless twin
+        const uint32_t ks = kc % KST, vs = vc % VST;
+        if (goes_on && own) ready(k_full(ks), (kc / KST) & 1);
+        if (weighed) {
+          if (own) ready(v_ready(vs), (vc / VST) & 1);
+          ready(p_full(h), done >> h & 1);
+          done ^= 1u << h;
+        }
+        gone = __any_sync(0xffffffffu, gone);
+        if (gone) break;
+        tc_fence_after();
+        if (lane == 0) {
+          const uint32_t s_tmem = tmem + C::S_COL + h * TK;
+          if (weighed) {
+            const uint32_t vb = v_low + vs * (C::TILE >> 4);
 #pragma unroll
             for (int kk = 0; kk < TK / 16; ++kk)
-              mma_bf16_ta(tmem + C::O_COL + h * D, tmem + C::S_COL + h * TK + kk * 8u,
-                          desc_sw128(vb + kk * 2u * C::GROUP, 1024, C::GROUP), kIdescO, i > w.s0 || kk > 0);
-            issued = true;
+              mma_ts(tmem + C::O_COL + h * D, s_tmem + (kk / 4) * HK + (kk % 4) * 8u, vb + ((kk * 2u * C::GROUP) >> 4),
+                     desc_high(C::GROUP), kIdescO, kk > 0 || x > 1);
+            if (!goes_on) mma_commit(o_full(h));
+            if (frees) mma_commit(v_empty(vs));
           }
-          __syncwarp();
-          const bool goes_on = i + 1 < end && w.u.has(i + 1, h);
-          if (!goes_on) release(o_full(h));
-          if (twin || h == 1) {
-            release(v_empty(st));
-            ++vc;
+          if (goes_on) {
+            const uint32_t kb = k_low + ks * (C::TILE >> 4), qa = q_low + (twin ? 0 : h) * (C::QTILE >> 4);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_ss(s_tmem, qa + (((kk / 4) * C::QHALF + (kk % 4) * 32u) >> 4), desc_high(1024),
+                     kb + (((kk / 4) * 1024u + (kk % 4) * 32u) >> 4), desc_high(C::GROUP), kIdescS, kk > 0);
+            mma_commit(s_full(h));
+            if (frees) mma_commit(k_empty(ks));
           }
-          if (goes_on) next_scores(i + 1, h);
+          if (x == 2 * w.ns - 3) mma_commit(q_free);  // the stop's last scores are issued
         }
-        // the last scores of the segment are issued: Q is free once they are done
-        if (i == end - 2 || (i == end - 1 && w.ns == 1)) release(q_free);
+        __syncwarp();
+        if (weighed && frees) ++vc;
+        if (goes_on && frees) ++kc;
       }
       more = w.next(p);
     }
-    if (dead && __any_sync(0xffffffffu, issued)) {
+    if (gone) {  // products still in flight (bounded)
       if (lane == 0) mma_commit(drain);
       __syncwarp();
       const long long c0 = clock64();
@@ -332,39 +412,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == kSoftWarps + 3) {
     // ============================ finite values ============================
     fewer_registers();
+    ChunkWalk w;
     uint32_t vc = 0;
     for (bool more = w.begin(p, blockIdx.x); more && !dead;) {
-      const int per = w.u.twin ? 2 : 1;
+      const ChunkUnit u = w.unit(p);
       bool odd = false;
-      for (int x = 0; x < w.ns * per && !dead; ++x) {
-        const int i = w.s0 + x / per, h = x % per;
-        if (!w.u.has(i, h)) continue;
-        const int key0 = (w.u.tile0 + w.u.step_tiles(i, h)) * TK;
+      int key0 = (u.tile0 + u.step_tiles(w.s0, 0)) * TK;
+      for (int n = w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0); n > 0; --n, key0 += TK, ++vc) {
         const uint32_t st = vc % VST;
         wait(v_full(st), (vc / VST) & 1);
         if (dead) break;
-        ++vc;
-        if (key0 >= w.u.full_low && key0 + TK <= w.u.full_high) {
-          if (lane == 0) mbar_arrive(v_ready(st));
-          continue;
-        }
-        unsigned char* tile = smem + C::OFF_V + st * C::TILE;
-        constexpr int kPieces = D / 8;  // 16-byte pieces of a key's values
-        for (int c = lane; c < TK * kPieces; c += 32) {
-          const int key = c / kPieces, piece = c % kPieces, pos = key0 + key;
-          if (pos >= w.u.full_low && pos < w.u.full_high) continue;
-          uint4* at = reinterpret_cast<uint4*>(tile + (key >> 3) * C::GROUP + (piece >> 3) * 1024 + (key & 7) * 128 + (piece & 7) * 16);
-          if (pos < w.u.low || pos >= w.u.high) {
-            *at = make_uint4(0, 0, 0, 0);
-          } else {
-            const uint4 v = *at;
-            const uint32_t e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) odd |= __vcmpeq2(e[k] & 0x7f807f80u, 0x7f807f80u) != 0;
-          }
-        }
-        fence_async_smem();
-        __syncwarp();
+        if (key0 < u.full_low || key0 + TK > u.full_high) odd |= finite_values<D>(smem + C::OFF_V + st * C::TILE, key0, u);
         if (lane == 0) mbar_arrive(v_ready(st));
       }
       if (__any_sync(0xffffffffu, odd) && lane == 0) {
@@ -376,69 +434,102 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     // ============================ softmax ============================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    const int h = warp >> 2, row = (warp & 3) * 32 + lane;  // row of the M tile
-    const int tok = row / p.group, head = row - tok * p.group;
-    const bool in_tile = row < p.tile_tokens * p.group;
+    // A thread's registers are the scarce thing here (spilled ones miss the little L1 that is left
+    // beside the shared memory): the walk is kept in shared memory, by a warp's first lane, and
+    // what a stop's ends need is worked out there anew.
+    ChunkWalk& w = reinterpret_cast<ChunkWalk*>(smem + C::OFF_WALK)[warp];
+    // M tile, half of a tile's keys (and of the outputs' columns), row of the M tile
+    const int h = warp >> 3, ch = warp >> 2 & 1, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_col = tmem + lanes + C::S_COL + h * TK, o_col = tmem + lanes + C::O_COL + h * D;
-    float2* const other = reinterpret_cast<float2*>(smem + C::OFF_ML);
+    const uint32_t s_col = tmem + lanes + C::S_COL + h * TK + ch * HK, o_col = tmem + lanes + C::O_COL + h * D + ch * (D / 2);
+    float* const xch = reinterpret_cast<float*>(smem + C::OFF_XCH) + h * MR + row;
+    const int pbar = 1 + h * 4 + (warp & 3), allbar = 9;
     const float c = p.scale_log2;
-    uint32_t sc = 0, oc = 0;
+    uint32_t sc = 0, oc = 0;  // tiles weighed, units ended
+    // f(own, the other thread's) of a row, in both of its threads
+    auto joint = [&](float own, auto f) {
+      if (ch == 1) *xch = own;
+      bar_sync(pbar, 64);
+      if (ch == 0) *xch = own = f(own, *xch);
+      bar_sync(pbar, 64);
+      return ch == 0 ? own : *xch;
+    };
     auto settle = [&](uint32_t bar, uint32_t parity) {
       wait(bar, parity);
       tc_fence_after();
     };
-    for (bool more = w.begin(p, blockIdx.x); more;) {
-      const int token = (w.u.twin ? 0 : h * p.tile_tokens) + tok;
-      const bool real = in_tile && token < w.u.tokens;
-      const bool any = __any_sync(0xffffffffu, real);
-      // (rows of no token see what the last one sees, nothing stale)
-      const int at = w.seq.kv_len - w.seq.n + w.u.token0 + min(token, w.u.tokens - 1);
-      const int low = chunk_low(p, at), high = chunk_high(p, at, w.seq.kv_len);
-      float m = -INFINITY, l = 0.f;  // the reference, a score; the sum
-      bool none = true;              // this M tile has had no tile of keys
-      for (int i = w.s0; i < w.s0 + w.ns; ++i) {
-        if (!w.u.has(i, h)) continue;
-        const int key0 = (w.u.tile0 + w.u.step_tiles(i, h)) * TK;
+    // this row's token among the unit's, or -1
+    auto token_of = [&](const ChunkUnit& u) {
+      int r = row;
+      asm volatile("" : "+r"(r));  // not kept from before
+      const int token = (u.twin ? 0 : h * p.tile_tokens) + r / p.group;
+      return r < p.tile_tokens * p.group && token < u.tokens ? token : -1;
+    };
+    bool more = false;
+    if (lane == 0) more = w.begin(p, blockIdx.x);
+    for (more = __any_sync(0xffffffffu, more); more;) {
+      __syncwarp();
+      int n, whole_from, whole_to;  // this M tile's tiles at the stop; those that all rows see fully
+      uint32_t reals;               // rows of a token
+      {
+        const ChunkUnit u = w.unit(p);
+        const int key0 = (u.tile0 + u.step_tiles(w.s0, h)) * TK, step = u.twin ? 2 * TK : TK;
+        n = w.tiles(u, h);
+        whole_from = (max(u.full_low - key0, 0) + step - 1) / step;
+        whole_to = u.full_high - key0 >= TK ? (u.full_high - key0 - TK) / step + 1 : 0;
+        reals = __ballot_sync(0xffffffffu, token_of(u) >= 0);
+      }
+      float m = -INFINITY, l = 0.f;  // the row's reference, a score; the sum of this thread's weights
+      for (int k = 0; k < n; ++k) {
         settle(s_full(h), sc & 1);
         ++sc;
-        if (any) {
-          uint32_t raw[TK];
-          float* s = reinterpret_cast<float*>(raw);
-#pragma unroll
-          for (int c0 = 0; c0 < TK; c0 += 32) tmem_ld32(s_col + c0, raw + c0);
-          tmem_wait_ld();
-          if (key0 < w.u.full_low || key0 + TK > w.u.full_high) {
-            const int from = low - key0, to = high - key0;  // the columns this row sees
-#pragma unroll
-            for (int g = 0; g < TK; g += 32) {
+        if (reals) {
+          const bool partial = k < whole_from || k >= whole_to;  // some row does not see all
+          if (partial) {  // hidden keys' scores become -inf in place
+            const ChunkUnit u = w.unit(p);
+            // (rows of no token see what the last one sees, nothing stale)
+            const int token = token_of(u), at = w.kv_len - w.n + u.token0 + (token < 0 ? u.tokens - 1 : token);
+            const int key0 = (u.tile0 + u.step_tiles(w.s0, h) + (u.twin ? 2 * k : k)) * TK + ch * HK;
+            const int from = chunk_low(p, at) - key0, to = chunk_high(p, at, w.kv_len) - key0;  // columns that this row sees
+#pragma unroll 1
+            for (int g = 0; g < HK; g += 32) {
               const uint32_t above = to - g >= 32 ? ~0u : to - g <= 0 ? 0u : (1u << (to - g)) - 1u;
               const uint32_t below = from - g >= 32 ? ~0u : from - g <= 0 ? 0u : (1u << (from - g)) - 1u;
               const uint32_t seen = above & ~below;
+              uint32_t r[32];
+              tmem_ld32(s_col + g, r);
+              tmem_wait_ld();
 #pragma unroll
-              for (int k = 0; k < 32; ++k) s[g + k] = (seen >> k & 1) ? s[g + k] : -INFINITY;
+              for (int j = 0; j < 32; ++j) r[j] = (seen >> j & 1) ? r[j] : 0xff800000u;
+              tmem_st32(s_col + g, r);
             }
+            tmem_wait_st();
           }
-          float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+          // scores are loaded twice, 32 at a time, which leaves registers for four warps a scheduler
+          float top = -INFINITY;
 #pragma unroll
-          for (int k = 4; k < TK - 4; k += 8) {
-            t0 = max3(t0, s[k], s[k + 1]);
-            t1 = max3(t1, s[k + 2], s[k + 3]);
-            t2 = max3(t2, s[k + 4], s[k + 5]);
-            t3 = max3(t3, s[k + 6], s[k + 7]);
+          for (int g = 0; g < HK; g += 32) {
+            float s[32];
+            tmem_ld32(s_col + g, reinterpret_cast<uint32_t*>(s));
+            tmem_wait_ld();
+            float t0 = fmaxf(s[0], s[1]), t1 = fmaxf(s[2], s[3]);
+#pragma unroll
+            for (int k = 4; k < 32; k += 4) {
+              t0 = max3(t0, s[k], s[k + 1]);
+              t1 = max3(t1, s[k + 2], s[k + 3]);
+            }
+            top = max3(top, t0, t1);
           }
-          t0 = max3(t0, s[TK - 4], s[TK - 3]);
-          t1 = max3(t1, s[TK - 2], s[TK - 1]);
-          const float top = max3(fmaxf(t0, t1), t2, t3);
-          // raise the reference where a weight would pass 2^8 (and at first)
-          const bool raise = top > m && (m == -INFINITY || (top - m) * c > 8.f);
-          if (__any_sync(0xffffffffu, raise)) {
-            const float now = raise ? top : m;
+          // raise the row's reference where a weight would pass 2^8 (and at first)
+          auto raises = [&](float x) { return x > m && (m == -INFINITY || (x - m) * c > 8.f); };
+          if (pair_any(pbar, raises(top))) {
+            const float both = joint(top, [](float x, float y) { return fmaxf(x, y); });
+            const float now = raises(both) ? both : m;
             const float alpha = m == -INFINITY ? 0.f : ex2((m - now) * c);
-            if (!none && __any_sync(0xffffffffu, raise && m != -INFINITY)) {
+            if (k > 0 && __any_sync(0xffffffffu, now != m && m != -INFINITY)) {
               // (the scores are done, so the products before them, which O holds, are too)
 #pragma unroll 1
-              for (int c0 = 0; c0 < D; c0 += 16) {
+              for (int c0 = 0; c0 < D / 2; c0 += 16) {
                 uint32_t o[16];
                 tmem_ld16(o_col + c0, o);
                 tmem_wait_ld();
@@ -451,22 +542,33 @@ __global__ void __launch_bounds__(kThreads, 1)
             m = now;
           }
           // weights; m c is rounded up, so that no exponent passes what the reference allows
-          const float neg = m == -INFINITY ? 0.f : -__fmul_ru(m, c);
+          float neg = m == -INFINITY ? 0.f : -__fmul_ru(m, c);
           const bool far = fabsf(neg) > kFar;
-          if (__any_sync(0xffffffffu, far)) {
+          if (__any_sync(0xffffffffu, far)) {  // the reference is taken off the scores themselves
+#pragma unroll 1
+            for (int g = 0; g < HK; g += 16) {
+              uint32_t r[16];
+              tmem_ld16(s_col + g, r);
+              tmem_wait_ld();
 #pragma unroll
-            for (int k = 0; k < TK; ++k) s[k] = far ? (s[k] - m) * c : fmaf(s[k], c, neg);
-          } else {
-#pragma unroll
-            for (int k = 0; k < TK; k += 2) fma2(s[k], s[k + 1], c, neg);
+              for (int j = 0; j < 16; ++j) r[j] = far ? __float_as_uint(__uint_as_float(r[j]) - m) : r[j];
+              tmem_st16(s_col + g, r);
+            }
+            tmem_wait_st();
+            neg = far ? 0.f : neg;
           }
           float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
 #pragma unroll
-          for (int g = 0; g < TK; g += 32) {
+          for (int g = 0; g < HK; g += 32) {
+            float s[32];
+            tmem_ld32(s_col + g, reinterpret_cast<uint32_t*>(s));
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) fma2(s[k], s[k + 1], c, neg);
             uint32_t pk[16];
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
-              const float x = ex2(s[g + k]), y = ex2(s[g + k + 1]);
+              const float x = ex2(s[k]), y = ex2(s[k + 1]);
               if (k & 2) add2(a2, a3, x, y); else add2(a0, a1, x, y);
               pk[k / 2] = pack_bf16(x, y);
             }
@@ -475,111 +577,130 @@ __global__ void __launch_bounds__(kThreads, 1)
           l += (a0 + a1) + (a2 + a3);
           tmem_wait_st();
         }
-        none = false;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full(h));
       }
       // ---- the unit's outputs ----
-      const bool had = !none;
+      if (reals) l = joint(l, [](float x, float y) { return x + y; });
+      const bool had = n > 0;
       if (had) {
         settle(o_full(h), oc & 1);
         ++oc;
       }
+      const ChunkUnit u = w.unit(p);
+      const int token = token_of(u);
+      const bool real = token >= 0;
       const float mc = m == -INFINITY ? -INFINITY : fabsf(m * c) > kFar ? m * c : __fmul_ru(m, c);
-      const int64_t out_row = (static_cast<int64_t>(w.seq.row0) + w.u.token0 + token) * p.hq + w.g * p.group + head;
-      __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out) + out_row * D;
-      if (w.whole() && w.u.twin) {
-        // the two M tiles hold the same rows: the second hands its part over in shared memory
-        // (the second Q tile's, unused here), 32 columns at a time
-        float* const place = reinterpret_cast<float*>(smem + C::OFF_Q + C::QTILE);
-        if (h == 1) other[row] = make_float2(had ? mc : -INFINITY, had ? l : 0.f);
-        float w0 = 1.f, w1 = 0.f;
+      const int64_t out_row = (static_cast<int64_t>(w.row0) + u.token0 + token) * p.hq + w.g * p.group + row % p.group;
+      __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out);
+      // stores 32 columns of the warp's rows, from column c0 of this thread's half
+      auto store = [&](const uint32_t* pk, int c0) {
+        uint4 q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
+        turn_quad(q, lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int from = (lane & ~3) + k;
+          const int64_t r = __shfl_sync(0xffffffffu, out_row, from);
+          if (reals >> from & 1) *reinterpret_cast<uint4*>(out + r * D + ch * (D / 2) + c0 + (lane & 3) * 8) = q[k];
+        }
+      };
+      if (w.whole(u) && u.twin) {
+        // the two M tiles hold the same rows: the second hands its part over in shared memory (the
+        // second Q tile's, unused here), a quarter of the columns of each half at a time
+        constexpr int CP = D / 4;
+        float* const place = reinterpret_cast<float*>(smem + C::OFF_Q + C::QTILE) + ch * CP * MR;
+        float2* const other = reinterpret_cast<float2*>(smem + C::OFF_XCH);
         float2 ml = make_float2(-INFINITY, 0.f);
+        float w0 = 1.f, w1 = 0.f;
+        bar_sync(allbar, 32 * kSoftWarps);  // both M tiles have their sums
+        if (h == 1 && ch == 0) other[row] = make_float2(had ? mc : -INFINITY, had ? l : 0.f);
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-          float* const buf = place + (C::QTILE >= 32768 ? (c0 & 32) * MR : 0);
-          uint32_t o[32];
+        for (int c0 = 0; c0 < D / 2; c0 += CP) {
+          uint32_t o[CP];
           if (had) {
-            tmem_ld32(o_col + c0, o);
+            if constexpr (CP == 32) tmem_ld32(o_col + c0, o); else tmem_ld16(o_col + c0, o);
             tmem_wait_ld();
           }
-          if (h == 1 && had && any) {
+          if (h == 1 && had && reals) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) buf[k * MR + row] = __uint_as_float(o[k]);
+            for (int k = 0; k < CP; ++k) place[k * MR + row] = __uint_as_float(o[k]);
           }
-          bar_sync(1, 256);
-          if (h == 0 && any) {
+          bar_sync(allbar, 32 * kSoftWarps);
+          if (h == 0 && reals) {
             if (c0 == 0) {
               ml = other[row];
               const float top = fmaxf(mc, ml.x);
               w0 = mc == -INFINITY ? 0.f : ex2(mc - top);
               w1 = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
               const float total = l * w0 + ml.y * w1;
-              if (real && p.lse) p.lse[out_row] = (top + log2f(total)) * 0.6931471805599453f;
+              if (real && p.lse && ch == 0) p.lse[out_row] = (top + log2f(total)) * 0.6931471805599453f;
               const float inv = 1.f / total;
               w0 *= inv;
               w1 *= inv;
             }
-            uint32_t pk[16];
+            uint32_t pk[CP / 2];
 #pragma unroll
-            for (int k = 0; k < 32; k += 2) {
+            for (int k = 0; k < CP; k += 2) {
               float x = __uint_as_float(o[k]) * w0, y = __uint_as_float(o[k + 1]) * w0;
               if (ml.x != -INFINITY) {
-                x = fmaf(buf[k * MR + row], w1, x);
-                y = fmaf(buf[(k + 1) * MR + row], w1, y);
+                x = fmaf(place[k * MR + row], w1, x);
+                y = fmaf(place[(k + 1) * MR + row], w1, y);
               }
               pk[k / 2] = pack_bf16(x, y);
             }
             if (real) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                reinterpret_cast<uint4*>(out + c0)[k] = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
+              for (int k = 0; k < CP / 8; ++k)
+                reinterpret_cast<uint4*>(out + out_row * D + ch * (D / 2) + c0)[k] =
+                    make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
             }
           }
-          if (C::QTILE < 32768) bar_sync(1, 256);  // one buffer only
+          bar_sync(allbar, 32 * kSoftWarps);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(joined);
-      } else if (w.whole()) {
+      } else if (w.whole(u)) {
         const float inv = 1.f / l;  // every row sees a key: a sum of 0 (scores of -inf) is NaN
-        if (any) {
+        if (reals) {
 #pragma unroll 1
-          for (int c0 = 0; c0 < D; c0 += 32) {
+          for (int c0 = 0; c0 < D / 2; c0 += 32) {
             uint32_t o[32], pk[16];
             tmem_ld32(o_col + c0, o);
             tmem_wait_ld();
 #pragma unroll
             for (int k = 0; k < 32; k += 2) pk[k / 2] = pack_bf16(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
-            if (real) {
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                reinterpret_cast<uint4*>(out + c0)[k] = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
-            }
+            store(pk, c0);
           }
-          if (real && p.lse) p.lse[out_row] = (mc + log2f(l)) * 0.6931471805599453f;
+          if (real && p.lse && ch == 0) p.lse[out_row] = (mc + log2f(l)) * 0.6931471805599453f;
         }
-      } else if (any) {
+      } else if (reals) {
         // a part: its place is the block's second where it starts the unit, else its first
-        const int64_t slot = static_cast<int64_t>(2 * blockIdx.x + (w.starts_unit() ? 1 : 0)) * (2 * MR) + h * MR + row;
+        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (w.starts_unit() ? 1 : 0);
         if (had) {
 #pragma unroll 1
-          for (int c0 = 0; c0 < D; c0 += 32) {
+          for (int c0 = 0; c0 < D / 2; c0 += 32) {
             uint32_t o[32];
             tmem_ld32(o_col + c0, o);
             tmem_wait_ld();
+            float4* const part = reinterpret_cast<float4*>(p.partial_o) + (slot * (D / 4) + (ch * (D / 2) + c0) / 4) * (2 * MR) + h * MR + row;
             if (real) {
 #pragma unroll
               for (int k = 0; k < 8; ++k)
-                reinterpret_cast<uint4*>(p.partial_o + slot * D + c0)[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                part[k * 2 * MR] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
+                                               __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
             }
           }
         }
-        if (real) p.partial_ml[slot] = make_float2(had ? mc : -INFINITY, had ? l : 0.f);
+        if (real && ch == 0) p.partial_ml[slot * (2 * MR) + h * MR + row] = make_float2(had ? mc : -INFINITY, had ? l : 0.f);
       }
       tc_fence_before();
       __syncwarp();
-      more = w.next(p);
+      more = false;
+      if (lane == 0) more = w.next(p);
+      more = __any_sync(0xffffffffu, more);
     }
   }
   tc_fence_before();
