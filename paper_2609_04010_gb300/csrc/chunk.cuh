@@ -28,7 +28,7 @@ bool chunk_tc_fits(const spec_chunk_attn_args_t& a);
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path);
 constexpr int kChunkKeyTile = 128;     // keys of a tile on the tensor cores
 constexpr int kChunkTileRows = 128;    // query rows of an M tile
-constexpr int kChunkOverhead = 1;      // steps that a unit's start is charged in the work list
+constexpr int kChunkOverhead = 3;      // steps that a unit's start is charged in the work list
 
 // One sequence of the batch, as the setup leaves it.
 struct ChunkSeq {
@@ -127,7 +127,6 @@ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkParams& p, const Chun
 struct ChunkWalk {
   int left;          // virtual steps of the range behind the stop
   int b, g, rt;
-  int units;         // of the sequence
   int row0, n, kv_len;
   int s0, ns;        // the stop's first step, and how many
   __device__ __forceinline__ void enter(const ChunkParams& p) {
@@ -155,13 +154,12 @@ struct ChunkWalk {
     const int4 s = p.work->starts[block];
     b = s.x; g = s.y; rt = s.z;
     enter(p);
-    units = chunk_units(p, n);
     stop(p, s.w);
     return ns > 0;
   }
   __device__ __forceinline__ bool next(const ChunkParams& p) {
     if (left <= kChunkOverhead) return false;  // nothing, or no more than a unit's start
-    if (++rt == units) {
+    if (++rt == chunk_units(p, n)) {
       rt = 0;
       if (++g == p.hkv) {
         g = 0;
@@ -169,7 +167,6 @@ struct ChunkWalk {
           ++b;
           enter(p);
         } while (n == 0 && b < p.batch);
-        units = chunk_units(p, n);
       }
     }
     stop(p, 0);

@@ -45,6 +45,14 @@ constexpr int kSoftRegs = 104, kOtherRegs = 64;
 // Past this the product of a score and the scale loses whole steps of the exponent.
 constexpr float kFar = 4194304.f;  // 2^22
 
+// A stop whose outputs are being written, while the walk is at the next one.
+struct Ended {
+  int row;   // of its first token
+  int what;  // its tokens, and what follows
+  int g;
+};
+constexpr int kTwin = 1 << 16, kWhole = 1 << 17, kStarts = 1 << 18;
+
 template <int D>
 struct Cfg {
   static constexpr int DH = D / 64;                 // 128-byte column halves of a row
@@ -52,20 +60,21 @@ struct Cfg {
   static constexpr uint32_t TILE = (TK / 8) * GROUP;
   static constexpr uint32_t QHALF = MR * 128;
   static constexpr uint32_t QTILE = DH * QHALF;
-  static constexpr int KST = D == 128 ? 3 : 5, VST = D == 128 ? 2 : 5;
+  static constexpr int KST = D == 128 ? 2 : 5, VST = D == 128 ? 3 : 5;
   static constexpr uint32_t OFF_Q = 0;              // [2][DH][128 rows][128 B]
   static constexpr uint32_t OFF_K = OFF_Q + 2 * QTILE;
   static constexpr uint32_t OFF_V = OFF_K + KST * TILE;
   // float [2][128]: between a row's two threads; or float2 [128]: a twin's (m, l)
   static constexpr uint32_t OFF_XCH = OFF_V + VST * TILE;
   static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps]
-  static constexpr uint32_t OFF_BAR = (OFF_WALK + kSoftWarps * sizeof(ChunkWalk) + 7) / 8 * 8;
+  static constexpr uint32_t OFF_LAST = OFF_WALK + kSoftWarps * sizeof(ChunkWalk);  // Ended [kSoftWarps]
+  static constexpr uint32_t OFF_BAR = (OFF_LAST + kSoftWarps * sizeof(Ended) + 7) / 8 * 8;
   // k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], v_ready[VST], s_full[2], p_full[2],
   // o_full[2], q_full, q_free, drain, joined
   static constexpr int NBAR = 2 * KST + 3 * VST + 10;
   static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort
   static constexpr uint32_t BYTES = OFF_MISC + 16;
-  static constexpr size_t SMEM = BYTES + 1024;
+  static constexpr size_t SMEM = BYTES;
   static_assert(SMEM <= kTcMaxSmem, "a block's shared memory");
   static constexpr uint32_t S_COL = 0, O_COL = 2 * TK, TMEM_COLS = 512;
 };
@@ -209,9 +218,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const __grid_constant__ CUtensorMap map_q, const __grid_constant__ ChunkParams p) {
   using C = Cfg<D>;
   constexpr int KST = C::KST, VST = C::VST, DH = C::DH;
-  extern __shared__ __align__(1024) unsigned char smem_raw[];
-  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  extern __shared__ __align__(1024) unsigned char smem[];  // at a fixed address: offsets cost no registers
   const uint32_t sbase = smem_u32(smem);
+  if ((sbase & 1023u) != 0) {  // (the swizzle needs it; dynamic shared memory starts there)
+    if (threadIdx.x == 0) set_status(p.status, SPEC_FLAG_TIMEOUT);
+    return;
+  }
   const uint32_t bar0 = sbase + C::OFF_BAR;
   auto k_full = [&](uint32_t s) { return bar0 + 8u * s; };
   auto k_empty = [&](uint32_t s) { return bar0 + 8u * (KST + s); };
@@ -459,12 +471,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_after();
     };
     // this row's token among the unit's, or -1
-    auto token_of = [&](const ChunkUnit& u) {
+    auto token_of = [&](bool twin, int tokens) {
       int r = row;
       asm volatile("" : "+r"(r));  // not kept from before
-      const int token = (u.twin ? 0 : h * p.tile_tokens) + r / p.group;
-      return r < p.tile_tokens * p.group && token < u.tokens ? token : -1;
+      const int token = (twin ? 0 : h * p.tile_tokens) + r / p.group;
+      return r < p.tile_tokens * p.group && token < tokens ? token : -1;
     };
+    Ended& ended = reinterpret_cast<Ended*>(smem + C::OFF_LAST)[warp];
     bool more = false;
     if (lane == 0) more = w.begin(p, blockIdx.x);
     for (more = __any_sync(0xffffffffu, more); more;) {
@@ -477,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         n = w.tiles(u, h);
         whole_from = (max(u.full_low - key0, 0) + step - 1) / step;
         whole_to = u.full_high - key0 >= TK ? (u.full_high - key0 - TK) / step + 1 : 0;
-        reals = __ballot_sync(0xffffffffu, token_of(u) >= 0);
+        reals = __ballot_sync(0xffffffffu, token_of(u.twin, u.tokens) >= 0);
       }
       float m = -INFINITY, l = 0.f;  // the row's reference, a score; the sum of this thread's weights
       for (int k = 0; k < n; ++k) {
@@ -488,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (partial) {  // hidden keys' scores become -inf in place
             const ChunkUnit u = w.unit(p);
             // (rows of no token see what the last one sees, nothing stale)
-            const int token = token_of(u), at = w.kv_len - w.n + u.token0 + (token < 0 ? u.tokens - 1 : token);
+            const int token = token_of(u.twin, u.tokens), at = w.kv_len - w.n + u.token0 + (token < 0 ? u.tokens - 1 : token);
             const int key0 = (u.tile0 + u.step_tiles(w.s0, h) + (u.twin ? 2 * k : k)) * TK + ch * HK;
             const int from = chunk_low(p, at) - key0, to = chunk_high(p, at, w.kv_len) - key0;  // columns that this row sees
 #pragma unroll 1
@@ -584,15 +597,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       // ---- the unit's outputs ----
       if (reals) l = joint(l, [](float x, float y) { return x + y; });
       const bool had = n > 0;
+      more = false;
+      if (lane == 0) {  // the walk goes on while the last products run
+        const ChunkUnit u = w.unit(p);
+        ended.row = w.row0 + u.token0;
+        ended.what = u.tokens | (u.twin ? kTwin : 0) | (w.whole(u) ? kWhole : 0) | (w.starts_unit() ? kStarts : 0);
+        ended.g = w.g;
+        more = w.next(p);
+      }
+      more = __any_sync(0xffffffffu, more);
       if (had) {
         settle(o_full(h), oc & 1);
         ++oc;
       }
-      const ChunkUnit u = w.unit(p);
-      const int token = token_of(u);
+      const int what = ended.what;
+      const bool twin = what & kTwin, whole = what & kWhole;
+      const int token = token_of(twin, what & 0xffff);
       const bool real = token >= 0;
       const float mc = m == -INFINITY ? -INFINITY : fabsf(m * c) > kFar ? m * c : __fmul_ru(m, c);
-      const int64_t out_row = (static_cast<int64_t>(w.row0) + u.token0 + token) * p.hq + w.g * p.group + row % p.group;
+      const int64_t out_row = (static_cast<int64_t>(ended.row) + token) * p.hq + ended.g * p.group + row % p.group;
       __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out);
       // stores 32 columns of the warp's rows, from column c0 of this thread's half
       auto store = [&](const uint32_t* pk, int c0) {
@@ -607,21 +630,20 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (reals >> from & 1) *reinterpret_cast<uint4*>(out + r * D + ch * (D / 2) + c0 + (lane & 3) * 8) = q[k];
         }
       };
-      if (w.whole(u) && u.twin) {
+      if (whole && twin) {
         // the two M tiles hold the same rows: the second hands its part over in shared memory (the
-        // second Q tile's, unused here), a quarter of the columns of each half at a time
-        constexpr int CP = D / 4;
+        // second Q tile's, unused here), 16 columns of each half at a time
+        constexpr int CP = 16;
         float* const place = reinterpret_cast<float*>(smem + C::OFF_Q + C::QTILE) + ch * CP * MR;
         float2* const other = reinterpret_cast<float2*>(smem + C::OFF_XCH);
-        float2 ml = make_float2(-INFINITY, 0.f);
-        float w0 = 1.f, w1 = 0.f;
+        float w0 = 1.f, w1 = 0.f;  // what each part counts for
         bar_sync(allbar, 32 * kSoftWarps);  // both M tiles have their sums
         if (h == 1 && ch == 0) other[row] = make_float2(had ? mc : -INFINITY, had ? l : 0.f);
 #pragma unroll 1
         for (int c0 = 0; c0 < D / 2; c0 += CP) {
           uint32_t o[CP];
           if (had) {
-            if constexpr (CP == 32) tmem_ld32(o_col + c0, o); else tmem_ld16(o_col + c0, o);
+            tmem_ld16(o_col + c0, o);
             tmem_wait_ld();
           }
           if (h == 1 && had && reals) {
@@ -631,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           bar_sync(allbar, 32 * kSoftWarps);
           if (h == 0 && reals) {
             if (c0 == 0) {
-              ml = other[row];
+              const float2 ml = other[row];
               const float top = fmaxf(mc, ml.x);
               w0 = mc == -INFINITY ? 0.f : ex2(mc - top);
               w1 = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
@@ -645,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int k = 0; k < CP; k += 2) {
               float x = __uint_as_float(o[k]) * w0, y = __uint_as_float(o[k + 1]) * w0;
-              if (ml.x != -INFINITY) {
+              if (w1 != 0.f) {
                 x = fmaf(place[k * MR + row], w1, x);
                 y = fmaf(place[(k + 1) * MR + row], w1, y);
               }
@@ -662,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(joined);
-      } else if (w.whole(u)) {
+      } else if (whole) {
         const float inv = 1.f / l;  // every row sees a key: a sum of 0 (scores of -inf) is NaN
         if (reals) {
 #pragma unroll 1
@@ -678,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       } else if (reals) {
         // a part: its place is the block's second where it starts the unit, else its first
-        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (w.starts_unit() ? 1 : 0);
+        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (what & kStarts ? 1 : 0);
         if (had) {
 #pragma unroll 1
           for (int c0 = 0; c0 < D / 2; c0 += 32) {
@@ -697,10 +719,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (real && ch == 0) p.partial_ml[slot * (2 * MR) + h * MR + row] = make_float2(had ? mc : -INFINITY, had ? l : 0.f);
       }
       tc_fence_before();
-      __syncwarp();
-      more = false;
-      if (lane == 0) more = w.next(p);
-      more = __any_sync(0xffffffffu, more);
     }
   }
   tc_fence_before();
