@@ -360,45 +360,51 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr uint32_t kIdescS = idesc_bf16(MR, TK, false), kIdescO = idesc_bf16(MR, D, true);
     const uint32_t q_low = desc_low(sbase + C::OFF_Q, 16), k_low = desc_low(sbase + C::OFF_K, 16),
                    v_low = desc_low(sbase + C::OFF_V, 1024);
-    uint32_t kc = 0, vc = 0, seg = 0;  // tiles of K and V taken so far
-    uint32_t done = 0;                 // parity of the tiles that each M tile has weighed
-    bool gone = false;                 // of a lane; of all after a turn
+    uint32_t ks = 0, vs = 0;       // stages of the next tiles of K and V
+    uint32_t k_par = 0, v_par = 0; // and the parities of their barriers
+    uint32_t q_par = 0, p_par = 0; // of Q, and a bit per M tile of its weights
+    bool gone = false;             // of a lane; of all after a turn
     auto ready = [&](uint32_t bar, uint32_t parity) {
       if (!mbar_try(bar, parity)) gone = gone || !mbar_wait(bar, parity, abort_flag, p.status);
     };
-    for (bool more = w.begin(p, blockIdx.x); more && !gone; ++seg) {
-      const ChunkUnit u = w.unit(p);
-      const bool twin = u.twin;
-      const int end = w.s0 + w.ns;
-      ready(q_full, seg & 1);
+    for (bool more = w.begin(p, blockIdx.x); more && !gone;) {
+      int turns, first_last;  // of both M tiles together; M tile 1 of a twin may have a tile less
+      bool twin;
+      {
+        const ChunkUnit u = w.unit(p);
+        twin = u.twin;
+        turns = 2 * w.ns;
+        first_last = turns - (w.tiles(u, 1) < w.tiles(u, 0) ? 1 : 0);  // turns from here on have no tile
+      }
+      ready(q_full, q_par);
+      q_par ^= 1;
 #pragma unroll 1
-      for (int x = -2; x < 2 * w.ns && !gone; ++x) {  // M tile h of step i, and its scores of step i + 1
-        const int i = w.s0 + (x >> 1), h = x & 1;
-        const bool weighed = x >= 0 && u.has(i, h), goes_on = i + 1 < end && u.has(i + 1, h);
+      for (int x = -2; x < turns && !gone; ++x) {  // M tile x & 1: a step's products, the next step's scores
+        const int h = x & 1;
+        const bool weighed = x >= 0 && x < first_last, goes_on = x + 2 < first_last;
         const bool own = twin || h == 0, frees = twin || h == 1;  // both M tiles use one tile unless twin
-        const uint32_t ks = kc % KST, vs = vc % VST;
-        if (goes_on && own) ready(k_full(ks), (kc / KST) & 1);
+        const uint32_t s_tmem = tmem + C::S_COL + h * TK, o_tmem = tmem + C::O_COL + h * D;
+        const uint32_t vb = v_low + vs * (C::TILE >> 4), kb = k_low + ks * (C::TILE >> 4);
+        const uint32_t qa = q_low + (twin ? 0 : h) * (C::QTILE >> 4);
+        if (goes_on && own) ready(k_full(ks), k_par);
         if (weighed) {
-          if (own) ready(v_ready(vs), (vc / VST) & 1);
-          ready(p_full(h), done >> h & 1);
-          done ^= 1u << h;
+          if (own) ready(v_ready(vs), v_par);
+          ready(p_full(h), p_par >> h & 1);
+          p_par ^= 1u << h;
         }
         gone = __any_sync(0xffffffffu, gone);
         if (gone) break;
         tc_fence_after();
         if (lane == 0) {
-          const uint32_t s_tmem = tmem + C::S_COL + h * TK;
           if (weighed) {
-            const uint32_t vb = v_low + vs * (C::TILE >> 4);
 #pragma unroll
             for (int kk = 0; kk < TK / 16; ++kk)
-              mma_ts(tmem + C::O_COL + h * D, s_tmem + (kk / 4) * HK + (kk % 4) * 8u, vb + ((kk * 2u * C::GROUP) >> 4),
-                     desc_high(C::GROUP), kIdescO, kk > 0 || x > 1);
+              mma_ts(o_tmem, s_tmem + (kk / 4) * HK + (kk % 4) * 8u, vb + ((kk * 2u * C::GROUP) >> 4), desc_high(C::GROUP),
+                     kIdescO, kk > 0 || x > 1);
             if (!goes_on) mma_commit(o_full(h));
             if (frees) mma_commit(v_empty(vs));
           }
           if (goes_on) {
-            const uint32_t kb = k_low + ks * (C::TILE >> 4), qa = q_low + (twin ? 0 : h) * (C::QTILE >> 4);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
               mma_ss(s_tmem, qa + (((kk / 4) * C::QHALF + (kk % 4) * 32u) >> 4), desc_high(1024),
@@ -406,11 +412,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_commit(s_full(h));
             if (frees) mma_commit(k_empty(ks));
           }
-          if (x == 2 * w.ns - 3) mma_commit(q_free);  // the stop's last scores are issued
+          if (x == turns - 3) mma_commit(q_free);  // the stop's last scores are issued
         }
         __syncwarp();
-        if (weighed && frees) ++vc;
-        if (goes_on && frees) ++kc;
+        if (weighed && frees && ++vs == VST) {
+          vs = 0;
+          v_par ^= 1;
+        }
+        if (goes_on && frees && ++ks == KST) {
+          ks = 0;
+          k_par ^= 1;
+        }
       }
       more = w.next(p);
     }
