@@ -172,6 +172,14 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_low, u
       : "memory");
 }
 
+// One lane of a converged warp. (The compiler knows that it is one; with lane == 0 in its place the
+// products' operands cost more than the products hide: a long prompt took 1,404 us instead of 1,304.)
+__device__ __forceinline__ bool elected() {
+  uint32_t one;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0;
+}
+
 __device__ __forceinline__ void fewer_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
 }
@@ -385,24 +393,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool own = twin || h == 0, frees = twin || h == 1;  // both M tiles use one tile unless twin
         const uint32_t s_tmem = tmem + C::S_COL + h * TK, o_tmem = tmem + C::O_COL + h * D;
         const uint32_t vb = v_low + vs * (C::TILE >> 4), kb = k_low + ks * (C::TILE >> 4);
-        const uint32_t qa = q_low + (twin ? 0 : h) * (C::QTILE >> 4);
+        const uint32_t qa = q_low + (twin ? 0 : h) * (C::QTILE >> 4), v_now = vs;
         if (goes_on && own) ready(k_full(ks), k_par);
         if (weighed) {
           if (own) ready(v_ready(vs), v_par);
           ready(p_full(h), p_par >> h & 1);
-          p_par ^= 1u << h;
         }
         gone = __any_sync(0xffffffffu, gone);
         if (gone) break;
         tc_fence_after();
-        if (lane == 0) {
+        if (weighed) {
+          p_par ^= 1u << h;
+          if (frees && ++vs == VST) {
+            vs = 0;
+            v_par ^= 1;
+          }
+        }
+        if (elected()) {
           if (weighed) {
 #pragma unroll
             for (int kk = 0; kk < TK / 16; ++kk)
               mma_ts(o_tmem, s_tmem + (kk / 4) * HK + (kk % 4) * 8u, vb + ((kk * 2u * C::GROUP) >> 4), desc_high(C::GROUP),
                      kIdescO, kk > 0 || x > 1);
             if (!goes_on) mma_commit(o_full(h));
-            if (frees) mma_commit(v_empty(vs));
+            if (frees) mma_commit(v_empty(v_now));
           }
           if (goes_on) {
 #pragma unroll
@@ -415,10 +429,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (x == turns - 3) mma_commit(q_free);  // the stop's last scores are issued
         }
         __syncwarp();
-        if (weighed && frees && ++vs == VST) {
-          vs = 0;
-          v_par ^= 1;
-        }
         if (goes_on && frees && ++ks == KST) {
           ks = 0;
           k_par ^= 1;
