@@ -149,12 +149,12 @@ namespace specv {
 
 bool chunk_tc_fits(const spec_chunk_attn_args_t& a) {
   const int group = a.num_q_heads / a.num_kv_heads;
-  if (group > kChunkTileRows || a.kv_cache) return false;
+  if (group > kChunkTileRows) return false;
   const int64_t per_unit = 2 * (kChunkTileRows / group);
   const int64_t units = a.rows / per_unit + a.batch;
   // 32-bit counts: units, and the steps of a block (of at least 64)
-  const int64_t tiles = static_cast<int64_t>(a.max_pages_per_seq) * a.page_size / kChunkKeyTile + 1 + kChunkOverhead;
-  return units * a.num_kv_heads <= INT32_MAX / 4 && units * a.num_kv_heads <= (static_cast<int64_t>(INT32_MAX) * 32) / tiles && static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX / 2;
+  const int64_t tiles = static_cast<int64_t>(a.max_pages_per_seq) * a.page_size / kChunkKeyTile * kChunkTwinCost + 32;
+  return units * a.num_kv_heads <= INT32_MAX / 4 && units * a.num_kv_heads <= (static_cast<int64_t>(INT32_MAX) * 32) / tiles && static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX / 4;
 }
 
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path) {

@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
         if (first(mid) <= u) lo = mid; else hi = mid;
       }
       const ChunkSeq s = p.seqs[lo];
-      if (u - s.first_unit < chunk_units(p, s.n)) steps = chunk_unit(p, s, u - s.first_unit).steps + kChunkOverhead;
+      if (u - s.first_unit < chunk_units(p, s.n)) steps = chunk_unit(p, s, u - s.first_unit).length();
     }
     long long all;
     const long long before = carry + scan_block(steps, sh, &all);
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
   }
   __syncthreads();
   const long long total = carry * p.hkv;
-  const int active = static_cast<int>(min(total, static_cast<long long>(p.blocks)));
+  const int active = static_cast<int>(min(total / kChunkTwinCost, static_cast<long long>(p.blocks)));
   if (tid == 0) {
     p.work->total = total;
     p.work->active = active;
@@ -368,8 +368,8 @@ __device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part)
   if (!w.ends_unit(u)) return;
   const long long total = p.work->total;
   const int active = p.work->active;
-  // the unit's first step, from this block's
-  const long long at = c * total / active - p.work->starts[c].w + kChunkOverhead;
+  // the unit's first step, from this block's first virtual one
+  const long long at = c * total / active - p.work->starts[c].w + u.start();
   const int first = owner_of(at, total, active), subs = u.twin ? 2 : 1, n = (c - first + 1) * subs;
   const int tile_rows = p.tile_tokens * p.group;
   constexpr int C8 = D / 8;

@@ -28,7 +28,13 @@ bool chunk_tc_fits(const spec_chunk_attn_args_t& a);
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path);
 constexpr int kChunkKeyTile = 128;     // keys of a tile on the tensor cores
 constexpr int kChunkTileRows = 128;    // query rows of an M tile
-constexpr int kChunkOverhead = 3;      // steps that a unit's start is charged in the work list
+// The work list counts in virtual steps: what a step costs (a twin's reads twice the bytes for the same
+// products), and what a unit's start costs (its queries, the pipeline's refill, the outputs before).
+// 60 requests decoding beside four chunks take 668 us; with a step of either kind at 1 and a start at
+// 3 they take 778, with a twin's step at 2 and a start at 4, 745.
+constexpr int kChunkCost = 3, kChunkTwinCost = 4;
+constexpr int kChunkStart = 12, kChunkTwinStart = 10;
+constexpr int kChunkShortest = kChunkStart < kChunkTwinStart ? kChunkStart : kChunkTwinStart;
 
 // One sequence of the batch, as the setup leaves it.
 struct ChunkSeq {
@@ -98,6 +104,11 @@ struct ChunkUnit {
   int full_low, full_high;  // keys that all of them see
   int tile0, tiles, steps;
   bool twin;
+  __device__ __forceinline__ int start() const { return twin ? kChunkTwinStart : kChunkStart; }
+  __device__ __forceinline__ int cost() const { return twin ? kChunkTwinCost : kChunkCost; }
+  __device__ __forceinline__ int length() const { return start() + steps * cost(); }
+  // the first step that begins at or after virtual step v of the unit
+  __device__ __forceinline__ int step_at(int v) const { return (max(v - start(), 0) + cost() - 1) / cost(); }
   __device__ __forceinline__ int step_tiles(int i, int h) const { return twin ? 2 * i + h : i; }
   __device__ __forceinline__ bool has(int i, int h) const { return !twin || 2 * i + h < tiles; }
 };
@@ -141,11 +152,14 @@ struct ChunkWalk {
     return chunk_unit(p, {row0, n, kv_len, 0}, r);
   }
   __device__ __forceinline__ void stop(const ChunkParams& p, int off) {
-    const int all = chunk_unit(p, {row0, n, kv_len, 0}, rt).steps + kChunkOverhead, take = min(all - off, left);
-    s0 = max(off - kChunkOverhead, 0);
-    ns = max(off + take - kChunkOverhead, 0) - s0;
+    const ChunkUnit u = chunk_unit(p, {row0, n, kv_len, 0}, rt);
+    const int take = min(u.length() - off, left);
+    s0 = u.step_at(off);
+    ns = u.step_at(off + take) - s0;
     left -= take;
   }
+  // A range has at least kChunkTwinCost virtual steps, so that it has a step of a unit that it lies
+  // within; the first stop of one that begins at the very end of a unit has none, and is passed.
   __device__ __forceinline__ bool begin(const ChunkParams& p, int block) {
     const int active = p.work->active;
     if (block >= active) return false;
@@ -155,10 +169,10 @@ struct ChunkWalk {
     b = s.x; g = s.y; rt = s.z;
     enter(p);
     stop(p, s.w);
-    return ns > 0;
+    return ns > 0 || next(p);
   }
   __device__ __forceinline__ bool next(const ChunkParams& p) {
-    if (left <= kChunkOverhead) return false;  // nothing, or no more than a unit's start
+    if (left <= kChunkShortest) return false;  // nothing, or no more than a unit's start
     if (++rt == chunk_units(p, n)) {
       rt = 0;
       if (++g == p.hkv) {

@@ -53,25 +53,28 @@ struct Ended {
 };
 constexpr int kTwin = 1 << 16, kWhole = 1 << 17, kStarts = 1 << 18;
 
-template <int D>
+template <int D, bool FP8>
 struct Cfg {
   static constexpr int DH = D / 64;                 // 128-byte column halves of a row
   static constexpr uint32_t GROUP = DH * 1024;      // 8 keys of a tile: [half][8 keys][128 B]
   static constexpr uint32_t TILE = (TK / 8) * GROUP;
   static constexpr uint32_t QHALF = MR * 128;
   static constexpr uint32_t QTILE = DH * QHALF;
-  static constexpr int KST = D == 128 ? 2 : 5, VST = D == 128 ? 3 : 5;
+  static constexpr int KST = FP8 ? (D == 128 ? 2 : 4) : (D == 128 ? 2 : 5);
+  static constexpr int VST = FP8 ? KST : (D == 128 ? 3 : 5);
+  static constexpr uint32_t RAW = FP8 ? TK * D : 0;  // a tile of the 8-bit cache as it is: [key][D bytes]
   static constexpr uint32_t OFF_Q = 0;              // [2][DH][128 rows][128 B]
   static constexpr uint32_t OFF_K = OFF_Q + 2 * QTILE;
   static constexpr uint32_t OFF_V = OFF_K + KST * TILE;
   // float [2][128]: between a row's two threads; or float2 [128]: a twin's (m, l)
-  static constexpr uint32_t OFF_XCH = OFF_V + VST * TILE;
+  static constexpr uint32_t OFF_RAW = OFF_V + VST * TILE;  // [K, V]
+  static constexpr uint32_t OFF_XCH = OFF_RAW + 2 * RAW;
   static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps]
   static constexpr uint32_t OFF_LAST = OFF_WALK + kSoftWarps * sizeof(ChunkWalk);  // Ended [kSoftWarps]
   static constexpr uint32_t OFF_BAR = (OFF_LAST + kSoftWarps * sizeof(Ended) + 7) / 8 * 8;
   // k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], v_ready[VST], s_full[2], p_full[2],
-  // o_full[2], q_full, q_free, drain, joined
-  static constexpr int NBAR = 2 * KST + 3 * VST + 10;
+  // o_full[2], q_full, q_free, drain, joined[2], raw_full[2], raw_empty[2]
+  static constexpr int NBAR = 2 * KST + 3 * VST + 15;
   static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort
   static constexpr uint32_t BYTES = OFF_MISC + 16;
   static constexpr size_t SMEM = BYTES;
@@ -84,6 +87,13 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* m
       "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(0), "r"(0), "r"(0), "r"(page_head), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_raw(uint32_t dst, const CUtensorMap* map, int page_head_kind, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(0), "r"(page_head_kind), "r"(bar)
       : "memory");
 }
 __device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map, int half, int head, int row, uint32_t bar) {
@@ -204,7 +214,7 @@ __device__ __forceinline__ bool finite_values(unsigned char* tile, int key0, con
       at[k] = nullptr;
       v[k] = make_uint4(0, 0, 0, 0);
       if (c < n) {
-        uint4* from = reinterpret_cast<uint4*>(tile + (key >> 3) * Cfg<D>::GROUP + (piece >> 3) * 1024 + (key & 7) * 128 + (piece & 7) * 16);
+        uint4* from = reinterpret_cast<uint4*>(tile + (key >> 3) * Cfg<D, false>::GROUP + (piece >> 3) * 1024 + (key & 7) * 128 + (piece & 7) * 16);
         if (key0 + key < u.low || key0 + key >= u.high) at[k] = from; else v[k] = *from;
       }
     }
@@ -220,11 +230,54 @@ __device__ __forceinline__ bool finite_values(unsigned char* tile, int key0, con
   return odd;
 }
 
-template <int D>
+// Part `part` of kConverters warps: a tile of the 8-bit cache as bf16 in the products' layout, each
+// value the rounded product of its e4m3 value and its page's scale (lane i holds that of the tile's
+// page i). With VALUES, keys outside [low, high) are cleared and the result tells whether one that
+// some rows do not see is NaN.
+constexpr int kConverters = 3;
+template <int D, bool VALUES>
+__device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned char* tile, float scale, int psh, int key0,
+                                             const ChunkUnit& u, int part) {
+  constexpr int kPieces = D / 16, kItems = TK * kPieces;  // 16 values each
+  const int lane = threadIdx.x & 31;
+  bool odd = false;
+#pragma unroll 2
+  for (int i0 = part * 32; i0 < kItems; i0 += 32 * kConverters) {
+    const int item = i0 + lane, key = item / kPieces, j = item % kPieces;
+    const float sc = __shfl_sync(0xffffffffu, scale, key >> psh);
+    uint4 v = *reinterpret_cast<const uint4*>(raw + item * 16);
+    if constexpr (VALUES) {
+      const int pos = key0 + key;
+      if (pos < u.low || pos >= u.high) v = make_uint4(0, 0, 0, 0);
+      if (pos < u.full_low || pos >= u.full_high)
+        odd |= (__vcmpeq4(v.x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v.y & 0x7f7f7f7fu, 0x7f7f7f7fu) |
+                __vcmpeq4(v.z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v.w & 0x7f7f7f7fu, 0x7f7f7f7fu)) != 0;
+    }
+    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+    uint32_t o[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float2 a = from_e4m3x2(in[e] & 0xffffu), b = from_e4m3x2(in[e] >> 16);
+      mul2(a.x, a.y, sc);
+      mul2(b.x, b.y, sc);
+      o[2 * e] = pack_bf16(a.x, a.y);
+      o[2 * e + 1] = pack_bf16(b.x, b.y);
+    }
+    unsigned char* row = tile + (key >> 3) * Cfg<D, true>::GROUP + (j >> 2) * 1024 + (key & 7) * 128;
+    const int p0 = 2 * (j & 3), x = key & 7;
+    *reinterpret_cast<uint4*>(row + ((p0 ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<uint4*>(row + (((p0 + 1) ^ x) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+  }
+  fence_async_smem();
+  __syncwarp();
+  return odd;
+}
+
+template <int D, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1)
     chunk_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                     const __grid_constant__ CUtensorMap map_q, const __grid_constant__ ChunkParams p) {
-  using C = Cfg<D>;
+  using C = Cfg<D, FP8>;
   constexpr int KST = C::KST, VST = C::VST, DH = C::DH;
   extern __shared__ __align__(1024) unsigned char smem[];  // at a fixed address: offsets cost no registers
   const uint32_t sbase = smem_u32(smem);
@@ -244,7 +297,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto o_full = [&](int h) { return bar0 + 8u * (B0 + 4 + h); };
   const uint32_t q_full = bar0 + 8u * (B0 + 6), q_free = bar0 + 8u * (B0 + 7);
   const uint32_t drain = bar0 + 8u * (B0 + 8);
-  const uint32_t joined = bar0 + 8u * (B0 + 9);  // twins: the second Q tile's place is free again
+  auto joined = [&](uint32_t j) { return bar0 + 8u * (B0 + 9 + (j & 1)); };  // twin j has joined its halves
+  auto raw_full = [&](int kind) { return bar0 + 8u * (B0 + 11 + kind); };
+  auto raw_empty = [&](int kind) { return bar0 + 8u * (B0 + 13 + kind); };
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
 
@@ -252,8 +307,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NBAR; ++i) {
       const int at = i - static_cast<int>(B0);
-      // p_full: the warps of an M tile; joined: of both
-      const int n = at == 2 || at == 3 ? kSoftWarps / 2 : at == 9 ? kSoftWarps : 1;
+      const bool made = FP8 && (i < KST || (i >= 2 * KST + 2 * VST && at < 0) || at >= 13);
+      // k_full, v_ready, raw_empty of the 8-bit cache: the converters; p_full: the warps of an M tile;
+      // joined: of both
+      const int n = made ? kConverters : at == 2 || at == 3 ? kSoftWarps / 2 : at == 9 || at == 10 ? kSoftWarps : 1;
       mbar_init(bar0 + 8u * i, n);
     }
     *abort_flag = 0;
@@ -274,7 +331,122 @@ __global__ void __launch_bounds__(kThreads, 1)
     dead = !__all_sync(0xffffffffu, ok);
   };
 
-  if (warp == kSoftWarps || warp == kSoftWarps + 1) {
+  if (FP8 && (warp == kSoftWarps || warp == kSoftWarps + 1 || warp == kSoftWarps + 3)) {
+    // ============================ producer and converters of the 8-bit cache ============================
+    // A tile of K, then of V. The first of the three warps also brings the tiles: the next one as
+    // soon as all three have read the one before. Its walk is a tile ahead of its conversions.
+    fewer_registers();
+    ChunkWalk w;
+    const bool brings = warp == kSoftWarps;
+    const int part = brings ? 0 : warp == kSoftWarps + 1 ? 1 : 2;
+    const int psh = __ffs(p.page_size) - 1, npg = TK >> psh;
+    const uint32_t box = static_cast<uint32_t>(p.page_size) * D;
+    const uint32_t qbytes = static_cast<uint32_t>(p.tile_tokens * p.group) * 128u;
+    uint32_t it = 0, made = 0, seg = 0, joins = 0, twins = 0;
+    uint32_t noted = 0;  // stops + 1 of the last note
+    bool was_twin = false;
+    // the tile to convert next
+    struct { ChunkUnit u; int key0, b, g, rt; uint32_t stop; float2 scale; } t;
+    auto convert = [&](int kind) {
+      const uint32_t st = made % (kind ? VST : KST), use = made / (kind ? VST : KST);
+      wait(raw_full(kind), made & 1);
+      if (use > 0) wait(kind ? v_empty(st) : k_empty(st), (use - 1) & 1);
+      if (dead) return;
+      const unsigned char* raw = smem + C::OFF_RAW + kind * C::RAW;
+      if (kind) {
+        const bool odd = convert_tile<D, true>(raw, smem + C::OFF_V + st * C::TILE, t.scale.y, psh, t.key0, t.u, part);
+        if (__any_sync(0xffffffffu, odd) && noted != t.stop + 1) {
+          noted = t.stop + 1;
+          if (lane == 0) {
+            const int n = atomicAdd(&p.redo[0].x, 1);
+            if (n < p.redo_cap) p.redo[1 + n] = make_int4(t.b, t.g, t.rt, 0);
+          }
+        }
+      } else {
+        convert_tile<D, false>(raw, smem + C::OFF_K + st * C::TILE, t.scale.x, psh, t.key0, t.u, part);
+      }
+      if (lane == 0) {
+        mbar_arrive(raw_empty(kind));
+        mbar_arrive(kind ? v_ready(st) : k_full(st));
+      }
+      __syncwarp();
+    };
+    for (bool more = !p.starve && w.begin(p, blockIdx.x); more && !dead; ++seg) {
+      const ChunkUnit u = w.unit(p);
+      const int32_t* table = p.page_table + static_cast<int64_t>(w.b) * p.max_pages;
+      bool bad = false;
+      int key0 = (u.tile0 + u.step_tiles(w.s0, 0)) * TK;
+      const int tiles = w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0);
+      for (int x = 0; x < tiles && !dead; ++x, key0 += TK) {
+        // pages with a key that the unit sees, a lane each
+        const int q0 = max(key0, u.low) - key0 >> psh, q1 = (min(key0 + TK, u.high) - 1 - key0 >> psh) + 1;
+        int id = 0;
+        if (lane >= q0 && lane < q1) {
+          id = __ldg(table + (key0 >> psh) + lane);
+          if (id < 0 || id >= p.num_pages) {
+            bad = true;
+            id = 0;
+          }
+        }
+        const int64_t page = static_cast<int64_t>(id) * p.hkv + w.g;
+        const float2 scale = __ldg(reinterpret_cast<const float2*>(p.kv_scale) + page);
+        for (int kind = 0; kind < 2 && !dead; ++kind) {
+          if (it > 0) convert(kind);
+          if (brings && !dead) {
+            if (it > 0) wait(raw_empty(kind), (it - 1) & 1);
+            if (!dead) {
+              if (elected()) mbar_arrive_tx(raw_full(kind), static_cast<uint32_t>(q1 - q0) * box);
+              __syncwarp();
+              if (lane >= q0 && lane < q1)
+                tma_load_raw(sbase + C::OFF_RAW + kind * C::RAW + static_cast<uint32_t>(lane) * box, &map_k,
+                             static_cast<int>(2 * page + kind), raw_full(kind));
+            }
+          }
+        }
+        if (dead) break;
+        if (it > 0) ++made;
+        ++it;
+        t.u = u;
+        t.key0 = key0;
+        t.b = w.b;
+        t.g = w.g;
+        t.rt = w.rt;
+        t.stop = seg;
+        t.scale = make_float2(scale.x, clamp_scale(scale.y));
+        if (brings && x == 0) {
+          // Q follows the first tile of keys, once the stop before is done with its own
+          if (seg > 0) wait(q_free, (seg - 1) & 1);
+          for (; joins < twins - (was_twin && u.twin ? 1 : 0) && !dead; ++joins) wait(joined(joins), joins >> 1 & 1);
+          if (dead) break;
+          if (lane == 0) {
+            const int m_tiles = u.twin ? 1 : 2;
+            mbar_arrive_tx(q_full, static_cast<uint32_t>(m_tiles * DH) * qbytes);
+            for (int m = 0; m < m_tiles; ++m)
+              for (int half = 0; half < DH; ++half)
+                tma_load_q(sbase + C::OFF_Q + m * C::QTILE + half * C::QHALF, &map_q, half, w.g * p.group,
+                           w.row0 + u.token0 + m * p.tile_tokens, q_full);
+          }
+          __syncwarp();
+        }
+      }
+      if (brings && __any_sync(0xffffffffu, bad) && lane == 0) {  // the sequence is cleared at the end
+        p.seq_bad[w.b] = 1;
+        set_status(p.status, SPEC_FLAG_BAD_PAGE);
+      }
+      was_twin = u.twin && w.whole(u);
+      twins += was_twin ? 1 : 0;
+      more = w.next(p);
+    }
+    for (int kind = 0; kind < 2 && it > 0 && !dead; ++kind) convert(kind);
+    if (dead && brings && it > 0) {  // copies still in flight (bounded)
+      const long long c0 = clock64();
+      for (int kind = 0; kind < 2; ++kind)
+        while (!mbar_try(raw_full(kind), (it - 1) & 1) && clock64() - c0 < kWaitCycles) {
+        }
+      while (seg > 0 && !mbar_try(q_full, (seg - 1) & 1) && clock64() - c0 < kWaitCycles) {
+      }
+    }
+  } else if (warp == kSoftWarps || warp == kSoftWarps + 1) {
     // ============================ producers ============================
     fewer_registers();
     ChunkWalk w;
@@ -284,8 +456,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int psh = __ffs(p.page_size) - 1, npg = TK >> psh;
     const uint32_t box = static_cast<uint32_t>(p.page_size) * D * 2;
     const uint32_t qbytes = static_cast<uint32_t>(p.tile_tokens * p.group) * 128u;
-    uint32_t it = 0, seg = 0, joins = 0;
-    bool was_joined = false;
+    uint32_t it = 0, seg = 0, joins = 0, twins = 0;  // twins joined, of all whole ones so far
+    bool was_twin = false;
     auto full = [&](uint32_t s) { return is_k ? k_full(s) : v_full(s); };
     auto empty = [&](uint32_t s) { return is_k ? k_empty(s) : v_empty(s); };
     for (bool more = !p.starve && w.begin(p, blockIdx.x); more && !dead; ++seg) {
@@ -312,20 +484,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (dead) break;
         // pages with a key that the unit sees
         const int q0 = max(key0, u.low) - key0 >> psh, q1 = (min(key0 + TK, u.high) - 1 - key0 >> psh) + 1;
-        if (lane == 0) mbar_arrive_tx(full(st), static_cast<uint32_t>(q1 - q0) * box);
-        for (int q = q0; q < q1; ++q) {
-          const int raw = __shfl_sync(0xffffffffu, id, pg0 - base + q);
-          const bool in_range = raw >= 0 && raw < p.num_pages;
+        if (elected()) mbar_arrive_tx(full(st), static_cast<uint32_t>(q1 - q0) * box);
+        __syncwarp();
+        const int q = base + lane - pg0;
+        if (q >= q0 && q < q1) {
+          const bool in_range = id >= 0 && id < p.num_pages;
           bad |= !in_range;
-          if (lane == 0)
-            tma_load_page(ring + st * C::TILE + static_cast<uint32_t>(q) * box, map, (in_range ? raw : 0) * p.hkv + w.g, full(st));
+          tma_load_page(ring + st * C::TILE + static_cast<uint32_t>(q) * box, map, (in_range ? id : 0) * p.hkv + w.g, full(st));
         }
         __syncwarp();
         ++it;
         if (is_k && first) {
           // Q follows the first tile of keys, once the segment before is done with its own
           if (seg > 0) wait(q_free, (seg - 1) & 1);
-          if (was_joined) wait(joined, joins++ & 1);
+          // (the last twin joins in the second Q tile's place; its join is awaited a stop later
+          // where that place is not needed)
+          for (; joins < twins - (was_twin && u.twin ? 1 : 0) && !dead; ++joins) wait(joined(joins), joins >> 1 & 1);
           if (dead) break;
           if (lane == 0) {
             const int tiles = u.twin ? 1 : 2;
@@ -339,11 +513,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         first = false;
       }
-      if (bad && lane == 0) {  // the sequence is cleared at the end
+      if (__any_sync(0xffffffffu, bad) && lane == 0) {  // the sequence is cleared at the end
         p.seq_bad[w.b] = 1;
         set_status(p.status, SPEC_FLAG_BAD_PAGE);
       }
-      was_joined = u.twin && w.whole(u);
+      was_twin = u.twin && w.whole(u);
+      twins += was_twin ? 1 : 0;
       more = w.next(p);
     }
     if (dead) {  // copies still in flight (bounded)
@@ -443,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (!mbar_try(drain, 0) && clock64() - c0 < kWaitCycles) {
       }
     }
-  } else if (warp == kSoftWarps + 3) {
+  } else if (!FP8 && warp == kSoftWarps + 3) {
     // ============================ finite values ============================
     fewer_registers();
     ChunkWalk w;
@@ -479,7 +654,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     float* const xch = reinterpret_cast<float*>(smem + C::OFF_XCH) + h * MR + row;
     const int pbar = 1 + h * 4 + (warp & 3), allbar = 9;
     const float c = p.scale_log2;
-    uint32_t sc = 0, oc = 0;  // tiles weighed, units ended
+    uint32_t sc = 0, oc = 0, joins = 0;  // tiles weighed, units ended, twins joined
     // f(own, the other thread's) of a row, in both of its threads
     auto joint = [&](float own, auto f) {
       if (ch == 1) *xch = own;
@@ -705,7 +880,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           bar_sync(allbar, 32 * kSoftWarps);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(joined);
+        if (lane == 0) mbar_arrive(joined(joins));
+        ++joins;
       } else if (whole) {
         const float inv = 1.f / l;  // every row sees a key: a sum of 0 (scores of -inf) is NaN
         if (reals) {
@@ -765,6 +941,21 @@ bool encode_cache(CUtensorMap* map, const void* base, const spec_chunk_attn_args
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The 8-bit cache viewed as (bytes of a key; keys of a page; page, head and kind), the box the keys or
+// the values of one page and KV head, as they are.
+bool encode_raw(CUtensorMap* map, const spec_chunk_attn_args_t& a) {
+  EncodeTiledFn enc = encoder();
+  if (!enc) return false;
+  const cuuint64_t D = a.head_dim, P = a.page_size;
+  const cuuint64_t dims[3] = {D, P, 2 * static_cast<cuuint64_t>(a.num_pages) * a.num_kv_heads};
+  const cuuint64_t strides[2] = {D, D * P};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(D), static_cast<cuuint32_t>(P), 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(a.kv_cache), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Q viewed as (64 columns; column halves; heads; rows), the box one column half of an M tile: the
 // group's heads of tile_tokens rows. Rows past the last read zeros.
 bool encode_q(CUtensorMap* map, const spec_chunk_attn_args_t& a, const ChunkParams& p) {
@@ -780,20 +971,28 @@ bool encode_q(CUtensorMap* map, const spec_chunk_attn_args_t& a, const ChunkPara
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, bool FP8>
 cudaError_t launch_d(const spec_chunk_attn_args_t& a, const ChunkParams& p, cudaStream_t stream) {
   CUtensorMap mk, mv, mq;
-  if (!encode_cache(&mk, a.k_cache, a) || !encode_cache(&mv, a.v_cache, a) || !encode_q(&mq, a, p)) return cudaErrorInvalidValue;
-  const cudaError_t e = cudaFuncSetAttribute(chunk_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             static_cast<int>(Cfg<D>::SMEM));
+  if (!encode_q(&mq, a, p)) return cudaErrorInvalidValue;
+  if (FP8) {
+    if (!encode_raw(&mk, a)) return cudaErrorInvalidValue;
+    mv = mk;
+  } else if (!encode_cache(&mk, a.k_cache, a) || !encode_cache(&mv, a.v_cache, a)) {
+    return cudaErrorInvalidValue;
+  }
+  constexpr size_t smem = Cfg<D, FP8>::SMEM;
+  const cudaError_t e = cudaFuncSetAttribute(chunk_tc_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  return launch_overlapped(chunk_tc_kernel<D>, dim3(p.blocks), kThreads, Cfg<D>::SMEM, stream, mk, mv, mq, p);
+  return launch_overlapped(chunk_tc_kernel<D, FP8>, dim3(p.blocks), kThreads, smem, stream, mk, mv, mq, p);
 }
 
 }  // namespace
 
 cudaError_t launch_chunk_tc(const spec_chunk_attn_args_t& a, const ChunkParams& p, cudaStream_t stream) {
-  return a.head_dim == 128 ? launch_d<128>(a, p, stream) : launch_d<64>(a, p, stream);
+  if (a.kv_cache) return a.head_dim == 128 ? launch_d<128, true>(a, p, stream) : launch_d<64, true>(a, p, stream);
+  return a.head_dim == 128 ? launch_d<128, false>(a, p, stream) : launch_d<64, false>(a, p, stream);
 }
 
 }  // namespace specv
