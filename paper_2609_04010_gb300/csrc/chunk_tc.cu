@@ -40,8 +40,12 @@ constexpr int MR = kChunkTileRows;
 constexpr int kSoftWarps = 16;
 constexpr int kThreads = 32 * (kSoftWarps + 4);
 constexpr int HK = TK / 2;  // keys of a tile that a thread weighs
-// registers of a softmax and of another thread: 512 * 104 + 128 * 64 = 640 * 96, the launch's
-constexpr int kSoftRegs = 104, kOtherRegs = 64;
+// registers of a softmax and of another thread: 512 * 104 + 128 * 64 = 640 * 96, the launch's; the
+// converters of the 8-bit cache need as many
+template <bool FP8>
+constexpr int kSoftRegs = FP8 ? 96 : 104;
+template <bool FP8>
+constexpr int kOtherRegs = FP8 ? 96 : 64;
 // Past this the product of a score and the scale loses whole steps of the exponent.
 constexpr float kFar = 4194304.f;  // 2^22
 
@@ -52,6 +56,14 @@ struct Ended {
   int g;
 };
 constexpr int kTwin = 1 << 16, kWhole = 1 << 17, kStarts = 1 << 18;
+
+// A tile of the 8-bit cache that a converter has before it.
+struct RawTile {
+  int low, high, full_low, full_high;  // of its unit
+  int key0, b, g, rt;
+  uint32_t stop;
+};
+constexpr int kConverters = 3;
 
 template <int D, bool FP8>
 struct Cfg {
@@ -71,7 +83,8 @@ struct Cfg {
   static constexpr uint32_t OFF_XCH = OFF_RAW + 2 * RAW;
   static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps]
   static constexpr uint32_t OFF_LAST = OFF_WALK + kSoftWarps * sizeof(ChunkWalk);  // Ended [kSoftWarps]
-  static constexpr uint32_t OFF_BAR = (OFF_LAST + kSoftWarps * sizeof(Ended) + 7) / 8 * 8;
+  static constexpr uint32_t OFF_RAWS = OFF_LAST + kSoftWarps * sizeof(Ended);  // RawTile [kConverters]
+  static constexpr uint32_t OFF_BAR = (OFF_RAWS + (FP8 ? kConverters * sizeof(RawTile) : 0) + 7) / 8 * 8;
   // k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], v_ready[VST], s_full[2], p_full[2],
   // o_full[2], q_full, q_free, drain, joined[2], raw_full[2], raw_empty[2]
   static constexpr int NBAR = 2 * KST + 3 * VST + 15;
@@ -190,8 +203,9 @@ __device__ __forceinline__ bool elected() {
   return one != 0;
 }
 
+template <bool FP8>
 __device__ __forceinline__ void fewer_registers() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<FP8>));
 }
 
 // A warp's: clears the values of keys that no row of the unit sees, and tells whether one that some
@@ -234,39 +248,56 @@ __device__ __forceinline__ bool finite_values(unsigned char* tile, int key0, con
 // value the rounded product of its e4m3 value and its page's scale (lane i holds that of the tile's
 // page i). With VALUES, keys outside [low, high) are cleared and the result tells whether one that
 // some rows do not see is NaN.
-constexpr int kConverters = 3;
 template <int D, bool VALUES>
-__device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned char* tile, float scale, int psh, int key0,
-                                             const ChunkUnit& u, int part) {
-  constexpr int kPieces = D / 16, kItems = TK * kPieces;  // 16 values each
+__device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned char* tile, float scale, int psh,
+                                             const RawTile& t, int part) {
+  constexpr int kPieces = D / 16, kItems = TK * kPieces, kLoads = D == 128 ? 4 : 2;  // 16 values each
   const int lane = threadIdx.x & 31;
   bool odd = false;
-#pragma unroll 2
-  for (int i0 = part * 32; i0 < kItems; i0 += 32 * kConverters) {
-    const int item = i0 + lane, key = item / kPieces, j = item % kPieces;
-    const float sc = __shfl_sync(0xffffffffu, scale, key >> psh);
-    uint4 v = *reinterpret_cast<const uint4*>(raw + item * 16);
-    if constexpr (VALUES) {
-      const int pos = key0 + key;
-      if (pos < u.low || pos >= u.high) v = make_uint4(0, 0, 0, 0);
-      if (pos < u.full_low || pos >= u.full_high)
-        odd |= (__vcmpeq4(v.x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v.y & 0x7f7f7f7fu, 0x7f7f7f7fu) |
-                __vcmpeq4(v.z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v.w & 0x7f7f7f7fu, 0x7f7f7f7fu)) != 0;
-    }
-    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-    uint32_t o[8];
+  int low = 0, high = TK, full_low = 0, full_high = TK;  // keys of the tile that any and that all rows see
+  if constexpr (VALUES) {
+    low = t.low - t.key0;
+    high = t.high - t.key0;
+    full_low = t.full_low - t.key0;
+    full_high = t.full_high - t.key0;
+  }
+  // 32 items a round; the warp that also brings the tiles takes fewer
+  constexpr int kRounds = kItems / 32, kFirst = D == 128 ? 8 : 4, kSecond = (kRounds - kFirst) / 2;
+  const int from = part == 0 ? 0 : part == 1 ? kFirst : kFirst + kSecond, to = part == 0 ? kFirst : from + kSecond;
+#pragma unroll 1
+  for (int r = from; r < to; r += kLoads) {
+    uint4 v[kLoads];
+    float sc[kLoads];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float2 a = from_e4m3x2(in[e] & 0xffffu), b = from_e4m3x2(in[e] >> 16);
-      mul2(a.x, a.y, sc);
-      mul2(b.x, b.y, sc);
-      o[2 * e] = pack_bf16(a.x, a.y);
-      o[2 * e + 1] = pack_bf16(b.x, b.y);
+    for (int k = 0; k < kLoads; ++k) {
+      const int item = (r + k) * 32 + lane, key = item / kPieces;
+      sc[k] = __shfl_sync(0xffffffffu, scale, key >> psh);
+      v[k] = *reinterpret_cast<const uint4*>(raw + item * 16);
+      if constexpr (VALUES) {
+        if (key < low || key >= high) v[k] = make_uint4(0, 0, 0, 0);
+        if (key < full_low || key >= full_high)
+          odd |= (__vcmpeq4(v[k].x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v[k].y & 0x7f7f7f7fu, 0x7f7f7f7fu) |
+                  __vcmpeq4(v[k].z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v[k].w & 0x7f7f7f7fu, 0x7f7f7f7fu)) != 0;
+      }
     }
-    unsigned char* row = tile + (key >> 3) * Cfg<D, true>::GROUP + (j >> 2) * 1024 + (key & 7) * 128;
-    const int p0 = 2 * (j & 3), x = key & 7;
-    *reinterpret_cast<uint4*>(row + ((p0 ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-    *reinterpret_cast<uint4*>(row + (((p0 + 1) ^ x) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int item = (r + k) * 32 + lane, key = item / kPieces, j = item % kPieces;
+      const uint32_t in[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+      uint32_t o[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float2 a = from_e4m3x2(in[e] & 0xffffu), b = from_e4m3x2(in[e] >> 16);
+        mul2(a.x, a.y, sc[k]);
+        mul2(b.x, b.y, sc[k]);
+        o[2 * e] = pack_bf16(a.x, a.y);
+        o[2 * e + 1] = pack_bf16(b.x, b.y);
+      }
+      unsigned char* row = tile + (key >> 3) * Cfg<D, true>::GROUP + (j >> 2) * 1024 + (key & 7) * 128;
+      const int p0 = 2 * (j & 3), x = key & 7;
+      *reinterpret_cast<uint4*>(row + ((p0 ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<uint4*>(row + (((p0 + 1) ^ x) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+    }
   }
   fence_async_smem();
   __syncwarp();
@@ -335,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ============================ producer and converters of the 8-bit cache ============================
     // A tile of K, then of V. The first of the three warps also brings the tiles: the next one as
     // soon as all three have read the one before. Its walk is a tile ahead of its conversions.
-    fewer_registers();
+    fewer_registers<FP8>();
     ChunkWalk w;
     const bool brings = warp == kSoftWarps;
     const int part = brings ? 0 : warp == kSoftWarps + 1 ? 1 : 2;
@@ -346,7 +377,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t noted = 0;  // stops + 1 of the last note
     bool was_twin = false;
     // the tile to convert next
-    struct { ChunkUnit u; int key0, b, g, rt; uint32_t stop; float2 scale; } t;
+    RawTile& t = reinterpret_cast<RawTile*>(smem + C::OFF_RAWS)[part];
+    float scale_k = 0.f, scale_v = 0.f;  // lane i: of the tile's page i
     auto convert = [&](int kind) {
       const uint32_t st = made % (kind ? VST : KST), use = made / (kind ? VST : KST);
       wait(raw_full(kind), made & 1);
@@ -354,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (dead) return;
       const unsigned char* raw = smem + C::OFF_RAW + kind * C::RAW;
       if (kind) {
-        const bool odd = convert_tile<D, true>(raw, smem + C::OFF_V + st * C::TILE, t.scale.y, psh, t.key0, t.u, part);
+        const bool odd = convert_tile<D, true>(raw, smem + C::OFF_V + st * C::TILE, scale_v, psh, t, part);
         if (__any_sync(0xffffffffu, odd) && noted != t.stop + 1) {
           noted = t.stop + 1;
           if (lane == 0) {
@@ -363,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       } else {
-        convert_tile<D, false>(raw, smem + C::OFF_K + st * C::TILE, t.scale.x, psh, t.key0, t.u, part);
+        convert_tile<D, false>(raw, smem + C::OFF_K + st * C::TILE, scale_k, psh, t, part);
       }
       if (lane == 0) {
         mbar_arrive(raw_empty(kind));
@@ -377,19 +409,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool bad = false;
       int key0 = (u.tile0 + u.step_tiles(w.s0, 0)) * TK;
       const int tiles = w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0);
+      // pages of the tile at key k with a key that the unit sees, a lane each: the ids of the tile after
+      // the next one and the scales of the next one are in flight
+      auto in_tile = [&](int k) { return lane >= (max(k, u.low) - k >> psh) && lane <= (min(k + TK, u.high) - 1 - k >> psh); };
+      auto load_id = [&](int k, bool in) { return in && in_tile(k) ? __ldg(table + (k >> psh) + lane) : 0; };
+      auto load_scale = [&](int i) {
+        const int64_t at = static_cast<int64_t>(i >= 0 && i < p.num_pages ? i : 0) * p.hkv + w.g;
+        return __ldg(reinterpret_cast<const float2*>(p.kv_scale) + at);
+      };
+      int id = load_id(key0, true), id_next = load_id(key0 + TK, tiles > 1);
+      float2 scale = load_scale(id);
       for (int x = 0; x < tiles && !dead; ++x, key0 += TK) {
-        // pages with a key that the unit sees, a lane each
         const int q0 = max(key0, u.low) - key0 >> psh, q1 = (min(key0 + TK, u.high) - 1 - key0 >> psh) + 1;
-        int id = 0;
-        if (lane >= q0 && lane < q1) {
-          id = __ldg(table + (key0 >> psh) + lane);
-          if (id < 0 || id >= p.num_pages) {
-            bad = true;
-            id = 0;
-          }
-        }
-        const int64_t page = static_cast<int64_t>(id) * p.hkv + w.g;
-        const float2 scale = __ldg(reinterpret_cast<const float2*>(p.kv_scale) + page);
+        bad |= id < 0 || id >= p.num_pages;
+        const int64_t page = static_cast<int64_t>(id >= 0 && id < p.num_pages ? id : 0) * p.hkv + w.g;
+        const float2 scale_next = load_scale(id_next);
+        const int id_last = load_id(key0 + 2 * TK, x + 2 < tiles);
         for (int kind = 0; kind < 2 && !dead; ++kind) {
           if (it > 0) convert(kind);
           if (brings && !dead) {
@@ -406,13 +441,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (dead) break;
         if (it > 0) ++made;
         ++it;
-        t.u = u;
-        t.key0 = key0;
-        t.b = w.b;
-        t.g = w.g;
-        t.rt = w.rt;
-        t.stop = seg;
-        t.scale = make_float2(scale.x, clamp_scale(scale.y));
+        __syncwarp();
+        if (lane == 0) t = {u.low, u.high, u.full_low, u.full_high, key0, w.b, w.g, w.rt, seg};
+        __syncwarp();
+        scale_k = scale.x;
+        scale_v = clamp_scale(scale.y);
+        id = id_next;
+        id_next = id_last;
+        scale = scale_next;
         if (brings && x == 0) {
           // Q follows the first tile of keys, once the stop before is done with its own
           if (seg > 0) wait(q_free, (seg - 1) & 1);
@@ -448,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == kSoftWarps || warp == kSoftWarps + 1) {
     // ============================ producers ============================
-    fewer_registers();
+    fewer_registers<FP8>();
     ChunkWalk w;
     const bool is_k = warp == kSoftWarps;
     const uint32_t nst = is_k ? KST : VST, ring = sbase + (is_k ? C::OFF_K : C::OFF_V);
@@ -538,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // The tensor core keeps about four products in its queue, so that a turn's waits and
     // book-keeping have to stay within their time: one copy of the code, waits before it, all
     // products and commits of a turn in one block of one lane.
-    fewer_registers();
+    fewer_registers<FP8>();
     ChunkWalk w;
     constexpr uint32_t kIdescS = idesc_bf16(MR, TK, false), kIdescO = idesc_bf16(MR, D, true);
     const uint32_t q_low = desc_low(sbase + C::OFF_Q, 16), k_low = desc_low(sbase + C::OFF_K, 16),
@@ -620,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (!FP8 && warp == kSoftWarps + 3) {
     // ============================ finite values ============================
-    fewer_registers();
+    fewer_registers<FP8>();
     ChunkWalk w;
     uint32_t vc = 0;
     for (bool more = w.begin(p, blockIdx.x); more && !dead;) {
@@ -642,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     // ============================ softmax ============================
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs<FP8>));
     // A thread's registers are the scarce thing here (spilled ones miss the little L1 that is left
     // beside the shared memory): the walk is kept in shared memory, by a warp's first lane, and
     // what a stop's ends need is worked out there anew.
