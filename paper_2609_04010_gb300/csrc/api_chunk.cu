@@ -175,7 +175,10 @@ ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, 
   P.redo = ws_round(P.work + sizeof(ChunkWork) + sizeof(int4) * static_cast<size_t>(P.grid));
   P.partial_o = ws_round(P.redo + sizeof(int4) * (static_cast<size_t>(P.redo_cap) + 1));
   P.partial_ml = ws_round(P.partial_o + rows * a.head_dim * sizeof(float));
-  P.end = ws_round(P.partial_ml + rows * sizeof(float2));
+  P.q_half = ws_round(P.partial_ml + rows * sizeof(float2));
+  const size_t heads = P.fp8 ? static_cast<size_t>(a.rows) * a.num_q_heads : 0;
+  P.q_scale = ws_round(P.q_half + heads * a.head_dim * 2);
+  P.end = ws_round(P.q_scale + heads * sizeof(float));
   return P;
 }
 

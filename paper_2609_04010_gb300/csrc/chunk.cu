@@ -8,6 +8,7 @@
 // fp32. It serves what the tensor-core kernel does not take and is a second implementation to
 // compare it with.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include <cmath>
 
@@ -60,7 +61,55 @@ __device__ __forceinline__ long long scan_block(long long v, long long* sh, long
   return before + x - v;
 }
 
+// Query rows as fp16 for the products with the 8-bit cache, each scaled by the power of two that takes
+// its largest finite magnitude into [2^14, 2^15): bf16 values down to 2^-28 of that are exact, smaller
+// ones to 2^-39 of it.
+template <int D>
+__device__ __forceinline__ void halve_queries(const ChunkParams& p, int64_t warp, int64_t warps) {
+  constexpr int kLanes = D / 8, kEach = 32 / kLanes;  // lanes of a row, rows of a warp
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, piece = lane % kLanes;
+  const int64_t heads = static_cast<int64_t>(p.rows) * p.hq;
+  for (int64_t r0 = warp * kEach; r0 < heads; r0 += warps * kEach) {
+    const int64_t r = r0 + sub;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < heads)
+      v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + r / p.hq * p.q_stride + r % p.hq * D) + piece);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t lo = w[e] & 0x7fffu, hi = w[e] >> 16 & 0x7fffu;
+      top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+    }
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    // top = f * 2^(e - 127): times 2^(141 - e); both factors stay normal numbers
+    const int up = top == 0 ? 0 : min(126, max(-113, 141 - static_cast<int>(top >> 7)));
+    const float f = __uint_as_float(static_cast<uint32_t>(up + 127) << 23);
+    uint32_t h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __half2 x = __floats2half2_rn(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
+      h[e] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    if (r < heads) {
+      reinterpret_cast<uint4*>(p.q_half)[r * kLanes + piece] = make_uint4(h[0], h[1], h[2], h[3]);
+      if (piece == 0) p.q_scale[r] = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+    }
+  }
+}
+
+// D: 0, or the head dimension where query rows are to be made fp16, by all blocks but the first.
+template <int D>
 __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams p) {
+  if constexpr (D > 0) {
+    if (blockIdx.x > 0) {
+      pdl_wait_prior();
+      halve_queries<D>(p, (blockIdx.x - 1) * (kSetupThreads / 32) + (threadIdx.x >> 5),
+                       static_cast<int64_t>(gridDim.x - 1) * (kSetupThreads / 32));
+      return;
+    }
+  }
   __shared__ long long sh[32];
   __shared__ int first_kept[kSetupKept + 1];
   __shared__ long long cum_kept[kSetupKept + 1];
@@ -510,6 +559,8 @@ ChunkParams make_chunk_params(const spec_chunk_attn_args_t& a, const ChunkPlan& 
     p.redo_cap = P.redo_cap;
     p.partial_o = reinterpret_cast<float*>(ws + P.partial_o);
     p.partial_ml = reinterpret_cast<float2*>(ws + P.partial_ml);
+    p.q_half = ws + P.q_half;
+    p.q_scale = reinterpret_cast<float*>(ws + P.q_scale);
   }
   return p;
 }
@@ -520,9 +571,17 @@ cudaError_t launch_chunk(const spec_chunk_attn_args_t& a, const ChunkPlan& P, ch
                          bool starve) {
   ChunkParams p = make_chunk_params(a, P, ws);
   p.starve = starve ? 1 : 0;
-  cudaError_t e = launch_overlapped(chunk_setup_kernel, dim3(1), kSetupThreads, 0, stream, p);
-  if (e != cudaSuccess) return e;
   const bool wide = a.head_dim == 128;
+  cudaError_t e;
+  if (p.blocks && P.fp8) {
+    const int64_t heads = static_cast<int64_t>(a.rows) * a.num_q_heads;
+    const int each = kSetupThreads / (a.head_dim / 8), most = 2 * P.grid;  // two such blocks fit an SM
+    const int extra = static_cast<int>(heads / each < most ? (heads + each - 1) / each : most);
+    e = launch_overlapped(wide ? chunk_setup_kernel<128> : chunk_setup_kernel<64>, dim3(1 + extra), kSetupThreads, 0, stream, p);
+  } else {
+    e = launch_overlapped(chunk_setup_kernel<0>, dim3(1), kSetupThreads, 0, stream, p);
+  }
+  if (e != cudaSuccess) return e;
   if (p.blocks) e = launch_chunk_tc(a, p, stream);
   else if (P.fp8) e = wide ? launch_simt_d<128, true>(p, stream) : launch_simt_d<64, true>(p, stream);
   else e = wide ? launch_simt_d<128, false>(p, stream) : launch_simt_d<64, false>(p, stream);

@@ -22,7 +22,7 @@ struct ChunkPlan {
   int grid;          // tensor cores: blocks
   int max_units;     // tensor cores: units per KV head, at most
   int redo_cap;      // tensor cores: units that may have to be computed again
-  size_t seqs, bad, cum, work, redo, partial_o, partial_ml, end;
+  size_t seqs, bad, cum, work, redo, partial_o, partial_ml, q_half, q_scale, end;
 };
 bool chunk_tc_fits(const spec_chunk_attn_args_t& a);
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path);
@@ -76,6 +76,8 @@ struct ChunkParams {
   int redo_cap;
   float* partial_o;    // [2 * blocks][D / 4][2 * kChunkTileRows][4]
   float2* partial_ml;  // [2 * blocks][2 * kChunkTileRows] = (m, l)
+  void* q_half;        // 8-bit cache: [rows][Hq][D] fp16, each row scaled by a power of two
+  float* q_scale;      // 8-bit cache: [rows][Hq], what its scores are to be multiplied by
   int starve;          // test hook: the producers issue no copies, so the waits run out
 };
 

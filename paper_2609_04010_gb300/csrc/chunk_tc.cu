@@ -41,7 +41,7 @@ constexpr int kSoftWarps = 16;
 constexpr int kThreads = 32 * (kSoftWarps + 4);
 constexpr int HK = TK / 2;  // keys of a tile that a thread weighs
 // registers of a softmax and of another thread: 512 * 104 + 128 * 64 = 640 * 96, the launch's; the
-// converters of the 8-bit cache need as many
+// 8-bit cache's producer and converters need as many as the softmax
 template <bool FP8>
 constexpr int kSoftRegs = FP8 ? 96 : 104;
 template <bool FP8>
@@ -57,11 +57,12 @@ struct Ended {
 };
 constexpr int kTwin = 1 << 16, kWhole = 1 << 17, kStarts = 1 << 18;
 
-// A tile of the 8-bit cache that a converter has before it.
+// Notes of a tile of the 8-bit cache for its converters.
 struct RawTile {
   int low, high, full_low, full_high;  // of its unit
   int key0, b, g, rt;
   uint32_t stop;
+  int more;  // another tile follows
 };
 constexpr int kConverters = 3;
 
@@ -81,10 +82,11 @@ struct Cfg {
   // float [2][128]: between a row's two threads; or float2 [128]: a twin's (m, l)
   static constexpr uint32_t OFF_RAW = OFF_V + VST * TILE;  // [K, V]
   static constexpr uint32_t OFF_XCH = OFF_RAW + 2 * RAW;
-  static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps]
-  static constexpr uint32_t OFF_LAST = OFF_WALK + kSoftWarps * sizeof(ChunkWalk);  // Ended [kSoftWarps]
-  static constexpr uint32_t OFF_RAWS = OFF_LAST + kSoftWarps * sizeof(Ended);  // RawTile [kConverters]
-  static constexpr uint32_t OFF_BAR = (OFF_RAWS + (FP8 ? kConverters * sizeof(RawTile) : 0) + 7) / 8 * 8;
+  static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps, then kConverters]
+  static constexpr uint32_t OFF_LAST = OFF_WALK + (kSoftWarps + (FP8 ? kConverters : 0)) * sizeof(ChunkWalk);  // Ended [kSoftWarps]
+  static constexpr uint32_t OFF_PAGES = (OFF_LAST + kSoftWarps * sizeof(Ended) + 15) / 16 * 16;  // float4 [4 tiles][8 pages]
+  static constexpr uint32_t OFF_RAWS = OFF_PAGES + (FP8 ? 4 * 8 * 16 : 0);  // RawTile [4 tiles]
+  static constexpr uint32_t OFF_BAR = (OFF_RAWS + (FP8 ? 4 * sizeof(RawTile) : 0) + 7) / 8 * 8;
   // k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], v_ready[VST], s_full[2], p_full[2],
   // o_full[2], q_full, q_free, drain, joined[2], raw_full[2], raw_empty[2]
   static constexpr int NBAR = 2 * KST + 3 * VST + 15;
@@ -115,6 +117,11 @@ __device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map,
       " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(half), "r"(head), "r"(row), "r"(bar)
       : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 // Whether any thread of the two warps of 32 rows has `any` (named barrier).
 __device__ __forceinline__ bool pair_any(int bar, bool any) {
@@ -167,6 +174,18 @@ __device__ __forceinline__ void mul2(float& a, float& b, float s) {
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+// (a, b) += (x, y) * s
+__device__ __forceinline__ void addmul2(float& a, float& b, float x, float y, float s) {
+  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n mov.b64 z, {%4, %4};\n"
+      " fma.rn.f32x2 x, y, z, x;\n mov.b64 {%0, %1}, x;\n}"
+      : "+f"(a), "+f"(b)
+      : "f"(x), "f"(y), "f"(s));
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -244,14 +263,12 @@ __device__ __forceinline__ bool finite_values(unsigned char* tile, int key0, con
   return odd;
 }
 
-// Part `part` of kConverters warps: a tile of the 8-bit cache as bf16 in the products' layout, each
-// value the rounded product of its e4m3 value and its page's scale (lane i holds that of the tile's
-// page i). With VALUES, keys outside [low, high) are cleared and the result tells whether one that
-// some rows do not see is NaN.
+// Part `part` of kConverters warps: a tile of the 8-bit cache as fp16, exactly, in the products'
+// layout. With VALUES, keys outside [low, high) are cleared and the result tells whether one that some
+// rows do not see is NaN.
 template <int D, bool VALUES>
-__device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned char* tile, float scale, int psh,
-                                             const RawTile& t, int part) {
-  constexpr int kPieces = D / 16, kItems = TK * kPieces, kLoads = D == 128 ? 4 : 2;  // 16 values each
+__device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned char* tile, const RawTile& t, int part) {
+  constexpr int kPieces = D / 16, kItems = TK * kPieces, kLoads = 2;  // 16 values each
   const int lane = threadIdx.x & 31;
   bool odd = false;
   int low = 0, high = TK, full_low = 0, full_high = TK;  // keys of the tile that any and that all rows see
@@ -261,19 +278,19 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned 
     full_low = t.full_low - t.key0;
     full_high = t.full_high - t.key0;
   }
+  const bool partial = full_low > 0 || full_high < TK;
   // 32 items a round; the warp that also brings the tiles takes fewer
   constexpr int kRounds = kItems / 32, kFirst = D == 128 ? 8 : 4, kSecond = (kRounds - kFirst) / 2;
   const int from = part == 0 ? 0 : part == 1 ? kFirst : kFirst + kSecond, to = part == 0 ? kFirst : from + kSecond;
 #pragma unroll 1
   for (int r = from; r < to; r += kLoads) {
     uint4 v[kLoads];
-    float sc[kLoads];
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      const int item = (r + k) * 32 + lane, key = item / kPieces;
-      sc[k] = __shfl_sync(0xffffffffu, scale, key >> psh);
-      v[k] = *reinterpret_cast<const uint4*>(raw + item * 16);
-      if constexpr (VALUES) {
+    for (int k = 0; k < kLoads; ++k) v[k] = *reinterpret_cast<const uint4*>(raw + ((r + k) * 32 + lane) * 16);
+    if (VALUES && partial) {
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) {
+        const int key = ((r + k) * 32 + lane) / kPieces;
         if (key < low || key >= high) v[k] = make_uint4(0, 0, 0, 0);
         if (key < full_low || key >= full_high)
           odd |= (__vcmpeq4(v[k].x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v[k].y & 0x7f7f7f7fu, 0x7f7f7f7fu) |
@@ -287,11 +304,8 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned 
       uint32_t o[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float2 a = from_e4m3x2(in[e] & 0xffffu), b = from_e4m3x2(in[e] >> 16);
-        mul2(a.x, a.y, sc[k]);
-        mul2(b.x, b.y, sc[k]);
-        o[2 * e] = pack_bf16(a.x, a.y);
-        o[2 * e + 1] = pack_bf16(b.x, b.y);
+        o[2 * e] = e4m3x2_to_f16x2(in[e] & 0xffffu);
+        o[2 * e + 1] = e4m3x2_to_f16x2(in[e] >> 16);
       }
       unsigned char* row = tile + (key >> 3) * Cfg<D, true>::GROUP + (j >> 2) * 1024 + (key & 7) * 128;
       const int p0 = 2 * (j & 3), x = key & 7;
@@ -364,29 +378,21 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (FP8 && (warp == kSoftWarps || warp == kSoftWarps + 1 || warp == kSoftWarps + 3)) {
     // ============================ producer and converters of the 8-bit cache ============================
-    // A tile of K, then of V. The first of the three warps also brings the tiles: the next one as
-    // soon as all three have read the one before. Its walk is a tile ahead of its conversions.
+    // A tile of K, then of V. The first of the three warps also brings the tiles, each as soon as all
+    // three have read the one before, and leaves notes of it, so that the others need no walk.
     fewer_registers<FP8>();
-    ChunkWalk w;
-    const bool brings = warp == kSoftWarps;
-    const int part = brings ? 0 : warp == kSoftWarps + 1 ? 1 : 2;
-    const int psh = __ffs(p.page_size) - 1, npg = TK >> psh;
-    const uint32_t box = static_cast<uint32_t>(p.page_size) * D;
-    const uint32_t qbytes = static_cast<uint32_t>(p.tile_tokens * p.group) * 128u;
-    uint32_t it = 0, made = 0, seg = 0, joins = 0, twins = 0;
-    uint32_t noted = 0;  // stops + 1 of the last note
-    bool was_twin = false;
-    // the tile to convert next
-    RawTile& t = reinterpret_cast<RawTile*>(smem + C::OFF_RAWS)[part];
-    float scale_k = 0.f, scale_v = 0.f;  // lane i: of the tile's page i
+    const int part = warp == kSoftWarps ? 0 : warp == kSoftWarps + 1 ? 1 : 2;
+    RawTile* const notes = reinterpret_cast<RawTile*>(smem + C::OFF_RAWS);
+    uint32_t made = 0, noted = 0;  // tiles converted; stops + 1 of the last unit noted for redoing
     auto convert = [&](int kind) {
       const uint32_t st = made % (kind ? VST : KST), use = made / (kind ? VST : KST);
       wait(raw_full(kind), made & 1);
       if (use > 0) wait(kind ? v_empty(st) : k_empty(st), (use - 1) & 1);
       if (dead) return;
+      const RawTile& t = notes[made & 3];
       const unsigned char* raw = smem + C::OFF_RAW + kind * C::RAW;
       if (kind) {
-        const bool odd = convert_tile<D, true>(raw, smem + C::OFF_V + st * C::TILE, scale_v, psh, t, part);
+        const bool odd = convert_tile<D, true>(raw, smem + C::OFF_V + st * C::TILE, t, part);
         if (__any_sync(0xffffffffu, odd) && noted != t.stop + 1) {
           noted = t.stop + 1;
           if (lane == 0) {
@@ -395,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       } else {
-        convert_tile<D, false>(raw, smem + C::OFF_K + st * C::TILE, scale_k, psh, t, part);
+        convert_tile<D, false>(raw, smem + C::OFF_K + st * C::TILE, t, part);
       }
       if (lane == 0) {
         mbar_arrive(raw_empty(kind));
@@ -403,83 +409,114 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncwarp();
     };
-    for (bool more = !p.starve && w.begin(p, blockIdx.x); more && !dead; ++seg) {
-      const ChunkUnit u = w.unit(p);
-      const int32_t* table = p.page_table + static_cast<int64_t>(w.b) * p.max_pages;
-      bool bad = false;
-      int key0 = (u.tile0 + u.step_tiles(w.s0, 0)) * TK;
-      const int tiles = w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0);
-      // pages of the tile at key k with a key that the unit sees, a lane each: the ids of the tile after
-      // the next one and the scales of the next one are in flight
-      auto in_tile = [&](int k) { return lane >= (max(k, u.low) - k >> psh) && lane <= (min(k + TK, u.high) - 1 - k >> psh); };
-      auto load_id = [&](int k, bool in) { return in && in_tile(k) ? __ldg(table + (k >> psh) + lane) : 0; };
-      auto load_scale = [&](int i) {
-        const int64_t at = static_cast<int64_t>(i >= 0 && i < p.num_pages ? i : 0) * p.hkv + w.g;
-        return __ldg(reinterpret_cast<const float2*>(p.kv_scale) + at);
-      };
-      int id = load_id(key0, true), id_next = load_id(key0 + TK, tiles > 1);
-      float2 scale = load_scale(id);
-      for (int x = 0; x < tiles && !dead; ++x, key0 += TK) {
-        const int q0 = max(key0, u.low) - key0 >> psh, q1 = (min(key0 + TK, u.high) - 1 - key0 >> psh) + 1;
-        bad |= id < 0 || id >= p.num_pages;
-        const int64_t page = static_cast<int64_t>(id >= 0 && id < p.num_pages ? id : 0) * p.hkv + w.g;
-        const float2 scale_next = load_scale(id_next);
-        const int id_last = load_id(key0 + 2 * TK, x + 2 < tiles);
-        for (int kind = 0; kind < 2 && !dead; ++kind) {
-          if (it > 0) convert(kind);
-          if (brings && !dead) {
-            if (it > 0) wait(raw_empty(kind), (it - 1) & 1);
-            if (!dead) {
-              if (elected()) mbar_arrive_tx(raw_full(kind), static_cast<uint32_t>(q1 - q0) * box);
-              __syncwarp();
-              if (lane >= q0 && lane < q1)
-                tma_load_raw(sbase + C::OFF_RAW + kind * C::RAW + static_cast<uint32_t>(lane) * box, &map_k,
-                             static_cast<int>(2 * page + kind), raw_full(kind));
+    ChunkWalk& w = reinterpret_cast<ChunkWalk*>(smem + C::OFF_WALK)[kSoftWarps + part];  // (saves registers)
+    bool more = false;
+    if (lane == 0) more = !p.starve && w.begin(p, blockIdx.x);
+    more = __any_sync(0xffffffffu, more);
+    if (part > 0) {
+      while (more && !dead) {
+#pragma unroll 1
+        for (int kind = 0; kind < 2 && !dead; ++kind) convert(kind);
+        if (!dead) more = notes[made & 3].more != 0;
+        ++made;
+      }
+    } else {
+      const int psh = __ffs(p.page_size) - 1;
+      const uint32_t box = static_cast<uint32_t>(p.page_size) * D;
+      const uint32_t qbytes = static_cast<uint32_t>(p.tile_tokens * p.group) * 128u;
+      float4* const pages = reinterpret_cast<float4*>(smem + C::OFF_PAGES);
+      uint32_t it = 0, seg = 0, joins = 0, twins = 0;  // tiles brought, stops; twins joined, of all whole ones so far
+      bool was_twin = false;
+      while (more && !dead) {
+        __syncwarp();
+        const ChunkUnit u = w.unit(p);
+        const int b = w.b, g = w.g, rt = w.rt, row = w.row0 + u.token0;
+        const int32_t* table = p.page_table + static_cast<int64_t>(b) * p.max_pages;
+        const int tiles = w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0);
+        int key0 = (u.tile0 + u.step_tiles(w.s0, 0)) * TK;
+        const bool whole_twin = u.twin && w.whole(u);
+        bool bad = false;
+        // the walk goes ahead, so that the last tile can say that it is the last
+        __syncwarp();
+        more = false;
+        if (lane == 0) more = w.next(p);
+        more = __any_sync(0xffffffffu, more);
+        // pages of the tile at key k with a key that the unit sees, a lane each: the ids of the tile
+        // after the next one and the scales of the next one are in flight
+        auto load_id = [&](int k) {
+          const bool in = lane >= (max(k, u.low) - k >> psh) && lane <= (min(k + TK, u.high) - 1 - k >> psh);
+          return in && k < u.high ? __ldg(table + (k >> psh) + lane) : 0;
+        };
+        auto load_scale = [&](int i) {
+          return __ldg(reinterpret_cast<const float2*>(p.kv_scale) + static_cast<int64_t>(i >= 0 && i < p.num_pages ? i : 0) * p.hkv + g);
+        };
+        int id = load_id(key0), id_next = load_id(key0 + TK);
+        float2 scale = load_scale(id);
+        for (int x = 0; x < tiles && !dead; ++x, key0 += TK) {
+          const int q0 = max(key0, u.low) - key0 >> psh, q1 = (min(key0 + TK, u.high) - 1 - key0 >> psh) + 1;
+          const bool in_range = id >= 0 && id < p.num_pages;
+          bad |= !in_range;
+          const int at = 2 * ((in_range ? id : 0) * p.hkv + g);
+          const float2 scale_next = load_scale(id_next);
+          const int id_last = load_id(key0 + 2 * TK);
+#pragma unroll 1
+          for (int kind = 0; kind < 2; ++kind) {
+            if (it > 0) {
+              convert(kind);
+              wait(raw_empty(kind), (it - 1) & 1);
             }
+            if (dead) break;
+            if (kind == 0) {
+              if (lane == 0) notes[it & 3] = {u.low, u.high, u.full_low, u.full_high, key0, b, g, rt, seg, more || x + 1 < tiles};
+              const float sv = clamp_scale(scale.y);
+              // what the tile's scores and weights are to be scaled by
+              if (lane < 8) pages[(it & 3) * 8 + lane] = make_float4(scale.x, log2f(sv), 1.f / sv, 0.f);
+              __syncwarp();
+            }
+            if (elected()) mbar_arrive_tx(raw_full(kind), static_cast<uint32_t>(q1 - q0) * box);
+            __syncwarp();
+            if (lane >= q0 && lane < q1)
+              tma_load_raw(sbase + C::OFF_RAW + kind * C::RAW + static_cast<uint32_t>(lane) * box, &map_k, at + kind, raw_full(kind));
           }
-        }
-        if (dead) break;
-        if (it > 0) ++made;
-        ++it;
-        __syncwarp();
-        if (lane == 0) t = {u.low, u.high, u.full_low, u.full_high, key0, w.b, w.g, w.rt, seg};
-        __syncwarp();
-        scale_k = scale.x;
-        scale_v = clamp_scale(scale.y);
-        id = id_next;
-        id_next = id_last;
-        scale = scale_next;
-        if (brings && x == 0) {
-          // Q follows the first tile of keys, once the stop before is done with its own
-          if (seg > 0) wait(q_free, (seg - 1) & 1);
-          for (; joins < twins - (was_twin && u.twin ? 1 : 0) && !dead; ++joins) wait(joined(joins), joins >> 1 & 1);
           if (dead) break;
-          if (lane == 0) {
-            const int m_tiles = u.twin ? 1 : 2;
-            mbar_arrive_tx(q_full, static_cast<uint32_t>(m_tiles * DH) * qbytes);
-            for (int m = 0; m < m_tiles; ++m)
-              for (int half = 0; half < DH; ++half)
-                tma_load_q(sbase + C::OFF_Q + m * C::QTILE + half * C::QHALF, &map_q, half, w.g * p.group,
-                           w.row0 + u.token0 + m * p.tile_tokens, q_full);
+          if (it > 0) ++made;
+          ++it;
+          id = id_next;
+          id_next = id_last;
+          scale = scale_next;
+          if (x == 0) {
+            // Q follows the first tile of keys, once the stop before is done with its own
+            if (seg > 0) wait(q_free, (seg - 1) & 1);
+            for (; joins < twins - (was_twin && u.twin ? 1 : 0) && !dead; ++joins) wait(joined(joins), joins >> 1 & 1);
+            if (dead) break;
+            if (lane == 0) {
+              const int m_tiles = u.twin ? 1 : 2;
+              mbar_arrive_tx(q_full, static_cast<uint32_t>(m_tiles * DH) * qbytes);
+              for (int m = 0; m < m_tiles; ++m)
+                for (int half = 0; half < DH; ++half)
+                  tma_load_q(sbase + C::OFF_Q + m * C::QTILE + half * C::QHALF, &map_q, half, g * p.group,
+                             row + m * p.tile_tokens, q_full);
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
-      }
-      if (brings && __any_sync(0xffffffffu, bad) && lane == 0) {  // the sequence is cleared at the end
-        p.seq_bad[w.b] = 1;
-        set_status(p.status, SPEC_FLAG_BAD_PAGE);
-      }
-      was_twin = u.twin && w.whole(u);
-      twins += was_twin ? 1 : 0;
-      more = w.next(p);
-    }
-    for (int kind = 0; kind < 2 && it > 0 && !dead; ++kind) convert(kind);
-    if (dead && brings && it > 0) {  // copies still in flight (bounded)
-      const long long c0 = clock64();
-      for (int kind = 0; kind < 2; ++kind)
-        while (!mbar_try(raw_full(kind), (it - 1) & 1) && clock64() - c0 < kWaitCycles) {
+        if (__any_sync(0xffffffffu, bad) && lane == 0) {  // the sequence is cleared at the end
+          p.seq_bad[b] = 1;
+          set_status(p.status, SPEC_FLAG_BAD_PAGE);
         }
-      while (seg > 0 && !mbar_try(q_full, (seg - 1) & 1) && clock64() - c0 < kWaitCycles) {
+        was_twin = whole_twin;
+        twins += whole_twin ? 1 : 0;
+        ++seg;
+      }
+#pragma unroll 1
+      for (int kind = 0; kind < 2 && it > 0 && !dead; ++kind) convert(kind);
+      if (dead && it > 0) {  // copies still in flight (bounded)
+        const long long c0 = clock64();
+        for (int kind = 0; kind < 2; ++kind)
+          while (!mbar_try(raw_full(kind), (it - 1) & 1) && clock64() - c0 < kWaitCycles) {
+          }
+        while (seg > 0 && !mbar_try(q_full, (seg - 1) & 1) && clock64() - c0 < kWaitCycles) {
+        }
       }
     }
   } else if (warp == kSoftWarps || warp == kSoftWarps + 1) {
@@ -576,7 +613,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     // products and commits of a turn in one block of one lane.
     fewer_registers<FP8>();
     ChunkWalk w;
-    constexpr uint32_t kIdescS = idesc_bf16(MR, TK, false), kIdescO = idesc_bf16(MR, D, true);
+    // (fp16 operands: both type fields 0)
+    constexpr uint32_t kHalf = FP8 ? ~((1u << 7) | (1u << 10)) : ~0u;
+    constexpr uint32_t kIdescS = idesc_bf16(MR, TK, false) & kHalf, kIdescO = idesc_bf16(MR, D, true) & kHalf;
     const uint32_t q_low = desc_low(sbase + C::OFF_Q, 16), k_low = desc_low(sbase + C::OFF_K, 16),
                    v_low = desc_low(sbase + C::OFF_V, 1024);
     uint32_t ks = 0, vs = 0;       // stages of the next tiles of K and V
@@ -689,7 +728,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t s_col = tmem + lanes + C::S_COL + h * TK + ch * HK, o_col = tmem + lanes + C::O_COL + h * D + ch * (D / 2);
     float* const xch = reinterpret_cast<float*>(smem + C::OFF_XCH) + h * MR + row;
     const int pbar = 1 + h * 4 + (warp & 3), allbar = 9;
-    const float c = p.scale_log2;
+    float c = p.scale_log2;  // what a score is multiplied by (8-bit cache: of this row, before its key's scale)
+    const float4* const pages = reinterpret_cast<const float4*>(smem + C::OFF_PAGES);
+    const int psh = __ffs(p.page_size) - 1;
+    uint32_t tiles = 0;  // of the block before the stop
     uint32_t sc = 0, oc = 0, joins = 0;  // tiles weighed, units ended, twins joined
     // f(own, the other thread's) of a row, in both of its threads
     auto joint = [&](float own, auto f) {
@@ -716,14 +758,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (more = __any_sync(0xffffffffu, more); more;) {
       __syncwarp();
       int n, whole_from, whole_to;  // this M tile's tiles at the stop; those that all rows see fully
+      int step, stop_tiles;         // keys from one to the next; of both M tiles
       uint32_t reals;               // rows of a token
       {
         const ChunkUnit u = w.unit(p);
-        const int key0 = (u.tile0 + u.step_tiles(w.s0, h)) * TK, step = u.twin ? 2 * TK : TK;
+        const int key0 = (u.tile0 + u.step_tiles(w.s0, h)) * TK;
+        step = u.twin ? 2 * TK : TK;
+        stop_tiles = w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0);
         n = w.tiles(u, h);
         whole_from = (max(u.full_low - key0, 0) + step - 1) / step;
         whole_to = u.full_high - key0 >= TK ? (u.full_high - key0 - TK) / step + 1 : 0;
-        reals = __ballot_sync(0xffffffffu, token_of(u.twin, u.tokens) >= 0);
+        const int token = token_of(u.twin, u.tokens);
+        reals = __ballot_sync(0xffffffffu, token >= 0);
+        if constexpr (FP8) {
+          if (token >= 0)
+            c = p.scale_log2 * __ldg(p.q_scale + (static_cast<int64_t>(w.row0) + u.token0 + token) * p.hq + w.g * p.group + row % p.group);
+        }
       }
       float m = -INFINITY, l = 0.f;  // the row's reference, a score; the sum of this thread's weights
       for (int k = 0; k < n; ++k) {
@@ -751,6 +801,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tmem_wait_st();
           }
+          // 8-bit cache: exponents are s a + b, with a and b of the key's page: a the scales of the row, of
+          // the keys and of the softmax, b the logarithm of the values' scale, so that the products
+          // take the values as they are; a is not 0, so that a * -inf stays -inf
+          const float4* const page = pages + ((tiles + (step == 2 * TK ? 2 * k + h : k)) & 3) * 8;
+          auto page_of = [&](int g) { return page[(ch * HK + g) >> psh]; };
+          auto slope = [&](const float4& q) { return fmaxf(q.x * c, 1.17549435e-38f); };
           // scores are loaded twice, 32 at a time, which leaves registers for four warps a scheduler
           float top = -INFINITY;
 #pragma unroll
@@ -758,20 +814,37 @@ __global__ void __launch_bounds__(kThreads, 1)
             float s[32];
             tmem_ld32(s_col + g, reinterpret_cast<uint32_t*>(s));
             tmem_wait_ld();
-            float t0 = fmaxf(s[0], s[1]), t1 = fmaxf(s[2], s[3]);
+            if constexpr (FP8) {
 #pragma unroll
-            for (int k = 4; k < 32; k += 4) {
-              t0 = max3(t0, s[k], s[k + 1]);
-              t1 = max3(t1, s[k + 2], s[k + 3]);
+              for (int e = 0; e < 32; e += 16) {
+                float t0 = fmaxf(s[e], s[e + 1]), t1 = fmaxf(s[e + 2], s[e + 3]);
+#pragma unroll
+                for (int j = 4; j < 16; j += 4) {
+                  t0 = max3(t0, s[e + j], s[e + j + 1]);
+                  t1 = max3(t1, s[e + j + 2], s[e + j + 3]);
+                }
+                const float4 q = page_of(g + e);
+                top = fmaxf(top, fmaf(fmaxf(t0, t1), slope(q), q.y));
+              }
+            } else {
+              float t0 = fmaxf(s[0], s[1]), t1 = fmaxf(s[2], s[3]);
+#pragma unroll
+              for (int j = 4; j < 32; j += 4) {
+                t0 = max3(t0, s[j], s[j + 1]);
+                t1 = max3(t1, s[j + 2], s[j + 3]);
+              }
+              top = max3(top, t0, t1);
             }
-            top = max3(top, t0, t1);
           }
-          // raise the row's reference where a weight would pass 2^8 (and at first)
-          auto raises = [&](float x) { return x > m && (m == -INFINITY || (x - m) * c > 8.f); };
+          // raise the row's reference where a weight would pass 2^8 (and at first); 8-bit cache: 2^15, to
+          // where the largest is 2^8, because fp16 weights have steps of 2^-24 below 2^-14
+          auto raises = [&](float x) {
+            return x > m && (m == -INFINITY || (FP8 ? x - m > 15.f : (x - m) * c > 8.f));
+          };
           if (pair_any(pbar, raises(top))) {
             const float both = joint(top, [](float x, float y) { return fmaxf(x, y); });
-            const float now = raises(both) ? both : m;
-            const float alpha = m == -INFINITY ? 0.f : ex2((m - now) * c);
+            const float now = raises(both) ? (FP8 ? both - 8.f : both) : m;
+            const float alpha = m == -INFINITY ? 0.f : ex2(FP8 ? m - now : (m - now) * c);
             if (k > 0 && __any_sync(0xffffffffu, now != m && m != -INFINITY)) {
               // (the scores are done, so the products before them, which O holds, are too)
 #pragma unroll 1
@@ -788,37 +861,62 @@ __global__ void __launch_bounds__(kThreads, 1)
             m = now;
           }
           // weights; m c is rounded up, so that no exponent passes what the reference allows
-          float neg = m == -INFINITY ? 0.f : -__fmul_ru(m, c);
+          float neg = m == -INFINITY ? 0.f : FP8 ? -m : -__fmul_ru(m, c);
           const bool far = fabsf(neg) > kFar;
-          if (__any_sync(0xffffffffu, far)) {  // the reference is taken off the scores themselves
+          if (__any_sync(0xffffffffu, far)) {  // the reference is taken off the scores (exponents) themselves
 #pragma unroll 1
             for (int g = 0; g < HK; g += 16) {
               uint32_t r[16];
               tmem_ld16(s_col + g, r);
+              const float4 q = FP8 ? page_of(g) : make_float4(0.f, 0.f, 0.f, 0.f);
+              const float slope_g = FP8 ? slope(q) : 1.f;
               tmem_wait_ld();
 #pragma unroll
-              for (int j = 0; j < 16; ++j) r[j] = far ? __float_as_uint(__uint_as_float(r[j]) - m) : r[j];
+              for (int j = 0; j < 16; ++j) {
+                const float x = __uint_as_float(r[j]), e = FP8 ? fmaf(x, slope_g, q.y) : x;
+                r[j] = far ? __float_as_uint(e - m) : r[j];
+              }
               tmem_st16(s_col + g, r);
             }
             tmem_wait_st();
             neg = far ? 0.f : neg;
           }
           float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+          if constexpr (FP8) {
 #pragma unroll
-          for (int g = 0; g < HK; g += 32) {
-            float s[32];
-            tmem_ld32(s_col + g, reinterpret_cast<uint32_t*>(s));
-            tmem_wait_ld();
+            for (int g = 0; g < HK; g += 16) {
+              float s[16];
+              tmem_ld16(s_col + g, reinterpret_cast<uint32_t*>(s));
+              const float4 q = page_of(g);
+              const float a = far ? 1.f : slope(q), b = far ? 0.f : q.y + neg;
+              tmem_wait_ld();
+              uint32_t pk[8];
 #pragma unroll
-            for (int k = 0; k < 32; k += 2) fma2(s[k], s[k + 1], c, neg);
-            uint32_t pk[16];
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              const float x = ex2(s[k]), y = ex2(s[k + 1]);
-              if (k & 2) add2(a2, a3, x, y); else add2(a0, a1, x, y);
-              pk[k / 2] = pack_bf16(x, y);
+              for (int j = 0; j < 16; j += 2) {
+                fma2(s[j], s[j + 1], a, b);
+                const float x = ex2(s[j]), y = ex2(s[j + 1]);
+                if (j & 2) addmul2(a2, a3, x, y, q.z); else addmul2(a0, a1, x, y, q.z);
+                pk[j / 2] = pack_f16(x, y);
+              }
+              tmem_st8(s_col + g / 2, pk);
             }
-            tmem_st16(s_col + g / 2, pk);
+          } else {
+#pragma unroll
+            for (int g = 0; g < HK; g += 32) {
+              float s[32];
+              tmem_ld32(s_col + g, reinterpret_cast<uint32_t*>(s));
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) fma2(s[j], s[j + 1], c, neg);
+              uint32_t pk[16];
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                const float x = ex2(s[j]), y = ex2(s[j + 1]);
+                if (j & 2) add2(a2, a3, x, y); else add2(a0, a1, x, y);
+                pk[j / 2] = pack_bf16(x, y);
+              }
+              tmem_st16(s_col + g / 2, pk);
+            }
           }
           l += (a0 + a1) + (a2 + a3);
           tmem_wait_st();
@@ -827,6 +925,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full(h));
       }
+      tiles += stop_tiles;
       // ---- the unit's outputs ----
       if (reals) l = joint(l, [](float x, float y) { return x + y; });
       const bool had = n > 0;
@@ -847,7 +946,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool twin = what & kTwin, whole = what & kWhole;
       const int token = token_of(twin, what & 0xffff);
       const bool real = token >= 0;
-      const float mc = m == -INFINITY ? -INFINITY : fabsf(m * c) > kFar ? m * c : __fmul_ru(m, c);
+      const float mc = m == -INFINITY ? -INFINITY : FP8 ? m : fabsf(m * c) > kFar ? m * c : __fmul_ru(m, c);
       const int64_t out_row = (static_cast<int64_t>(ended.row) + token) * p.hq + ended.g * p.group + row % p.group;
       __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(p.out);
       // stores 32 columns of the warp's rows, from column c0 of this thread's half
@@ -999,10 +1098,13 @@ bool encode_q(CUtensorMap* map, const spec_chunk_attn_args_t& a, const ChunkPara
   if (!enc) return false;
   const cuuint64_t D = a.head_dim;
   const cuuint64_t dims[4] = {64, D / 64, static_cast<cuuint64_t>(a.num_q_heads), static_cast<cuuint64_t>(a.rows)};
-  const cuuint64_t strides[3] = {128, D * 2, static_cast<cuuint64_t>(p.q_stride) * 2};
+  // the 8-bit cache's queries are the dense fp16 ones
+  const int64_t stride = a.kv_cache ? static_cast<int64_t>(a.num_q_heads) * a.head_dim : p.q_stride;
+  const cuuint64_t strides[3] = {128, D * 2, static_cast<cuuint64_t>(stride) * 2};
   const cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(p.group), static_cast<cuuint32_t>(p.tile_tokens)};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(a.q), dims, strides, box, estr,
+  return enc(map, a.kv_cache ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+             a.kv_cache ? p.q_half : const_cast<void*>(a.q), dims, strides, box, estr,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
