@@ -64,7 +64,7 @@ struct RawTile {
   uint32_t stop;
   int more;  // another tile follows
 };
-constexpr int kConverters = 3;
+constexpr int kConverters = 2;
 
 template <int D, bool FP8>
 struct Cfg {
@@ -83,7 +83,7 @@ struct Cfg {
   static constexpr uint32_t OFF_RAW = OFF_V + VST * TILE;  // [K, V]
   static constexpr uint32_t OFF_XCH = OFF_RAW + 2 * RAW;
   static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps, then kConverters]
-  static constexpr uint32_t OFF_LAST = OFF_WALK + (kSoftWarps + (FP8 ? kConverters : 0)) * sizeof(ChunkWalk);  // Ended [kSoftWarps]
+  static constexpr uint32_t OFF_LAST = OFF_WALK + (kSoftWarps + (FP8 ? 3 : 0)) * sizeof(ChunkWalk);  // Ended [kSoftWarps]
   static constexpr uint32_t OFF_PAGES = (OFF_LAST + kSoftWarps * sizeof(Ended) + 15) / 16 * 16;  // float4 [4 tiles][8 pages]
   static constexpr uint32_t OFF_RAWS = OFF_PAGES + (FP8 ? 4 * 8 * 16 : 0);  // RawTile [4 tiles]
   static constexpr uint32_t OFF_BAR = (OFF_RAWS + (FP8 ? 4 * sizeof(RawTile) : 0) + 7) / 8 * 8;
@@ -268,7 +268,7 @@ __device__ __forceinline__ bool finite_values(unsigned char* tile, int key0, con
 // rows do not see is NaN.
 template <int D, bool VALUES>
 __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned char* tile, const RawTile& t, int part) {
-  constexpr int kPieces = D / 16, kItems = TK * kPieces, kLoads = 2;  // 16 values each
+  constexpr int kPieces = D / 16, kItems = TK * kPieces, kLoads = 4;  // 16 values each
   const int lane = threadIdx.x & 31;
   bool odd = false;
   int low = 0, high = TK, full_low = 0, full_high = TK;  // keys of the tile that any and that all rows see
@@ -279,9 +279,8 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned 
     full_high = t.full_high - t.key0;
   }
   const bool partial = full_low > 0 || full_high < TK;
-  // 32 items a round; the warp that also brings the tiles takes fewer
-  constexpr int kRounds = kItems / 32, kFirst = D == 128 ? 8 : 4, kSecond = (kRounds - kFirst) / 2;
-  const int from = part == 0 ? 0 : part == 1 ? kFirst : kFirst + kSecond, to = part == 0 ? kFirst : from + kSecond;
+  constexpr int kRounds = kItems / 32;  // 32 items a round
+  const int from = part * (kRounds / 2), to = from + kRounds / 2;
 #pragma unroll 1
   for (int r = from; r < to; r += kLoads) {
     uint4 v[kLoads];
@@ -381,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // A tile of K, then of V. The first of the three warps also brings the tiles, each as soon as all
     // three have read the one before, and leaves notes of it, so that the others need no walk.
     fewer_registers<FP8>();
-    const int part = warp == kSoftWarps ? 0 : warp == kSoftWarps + 1 ? 1 : 2;
+    const int part = warp == kSoftWarps ? -1 : warp == kSoftWarps + 1 ? 0 : 1;  // -1: the producer
     RawTile* const notes = reinterpret_cast<RawTile*>(smem + C::OFF_RAWS);
     uint32_t made = 0, noted = 0;  // tiles converted; stops + 1 of the last unit noted for redoing
     auto convert = [&](int kind) {
@@ -409,11 +408,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncwarp();
     };
-    ChunkWalk& w = reinterpret_cast<ChunkWalk*>(smem + C::OFF_WALK)[kSoftWarps + part];  // (saves registers)
+    ChunkWalk& w = reinterpret_cast<ChunkWalk*>(smem + C::OFF_WALK)[kSoftWarps + 1 + part];  // (saves registers)
     bool more = false;
     if (lane == 0) more = !p.starve && w.begin(p, blockIdx.x);
     more = __any_sync(0xffffffffu, more);
-    if (part > 0) {
+    if (part >= 0) {
       while (more && !dead) {
 #pragma unroll 1
         for (int kind = 0; kind < 2 && !dead; ++kind) convert(kind);
@@ -461,10 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int id_last = load_id(key0 + 2 * TK);
 #pragma unroll 1
           for (int kind = 0; kind < 2; ++kind) {
-            if (it > 0) {
-              convert(kind);
-              wait(raw_empty(kind), (it - 1) & 1);
-            }
+            if (it > 0) wait(raw_empty(kind), (it - 1) & 1);
             if (dead) break;
             if (kind == 0) {
               if (lane == 0) notes[it & 3] = {u.low, u.high, u.full_low, u.full_high, key0, b, g, rt, seg, more || x + 1 < tiles};
@@ -479,7 +475,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               tma_load_raw(sbase + C::OFF_RAW + kind * C::RAW + static_cast<uint32_t>(lane) * box, &map_k, at + kind, raw_full(kind));
           }
           if (dead) break;
-          if (it > 0) ++made;
           ++it;
           id = id_next;
           id_next = id_last;
@@ -508,8 +503,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         twins += whole_twin ? 1 : 0;
         ++seg;
       }
-#pragma unroll 1
-      for (int kind = 0; kind < 2 && it > 0 && !dead; ++kind) convert(kind);
       if (dead && it > 0) {  // copies still in flight (bounded)
         const long long c0 = clock64();
         for (int kind = 0; kind < 2; ++kind)
@@ -758,13 +751,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (more = __any_sync(0xffffffffu, more); more;) {
       __syncwarp();
       int n, whole_from, whole_to;  // this M tile's tiles at the stop; those that all rows see fully
-      int step, stop_tiles;         // keys from one to the next; of both M tiles
+      bool twin_stop;
       uint32_t reals;               // rows of a token
       {
         const ChunkUnit u = w.unit(p);
         const int key0 = (u.tile0 + u.step_tiles(w.s0, h)) * TK;
-        step = u.twin ? 2 * TK : TK;
-        stop_tiles = w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0);
+        const int step = u.twin ? 2 * TK : TK;
+        twin_stop = u.twin;
         n = w.tiles(u, h);
         whole_from = (max(u.full_low - key0, 0) + step - 1) / step;
         whole_to = u.full_high - key0 >= TK ? (u.full_high - key0 - TK) / step + 1 : 0;
@@ -804,7 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // 8-bit cache: exponents are s a + b, with a and b of the key's page: a the scales of the row, of
           // the keys and of the softmax, b the logarithm of the values' scale, so that the products
           // take the values as they are; a is not 0, so that a * -inf stays -inf
-          const float4* const page = pages + ((tiles + (step == 2 * TK ? 2 * k + h : k)) & 3) * 8;
+          const float4* const page = pages + ((tiles + (twin_stop ? 2 * k + h : k)) & 3) * 8;
           auto page_of = [&](int g) { return page[(ch * HK + g) >> psh]; };
           auto slope = [&](const float4& q) { return fmaxf(q.x * c, 1.17549435e-38f); };
           // scores are loaded twice, 32 at a time, which leaves registers for four warps a scheduler
@@ -925,7 +918,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full(h));
       }
-      tiles += stop_tiles;
+      if constexpr (FP8) {
+        const ChunkUnit u = w.unit(p);
+        tiles += w.tiles(u, 0) + (u.twin ? w.tiles(u, 1) : 0);
+      }
       // ---- the unit's outputs ----
       if (reals) l = joint(l, [](float x, float y) { return x + y; });
       const bool had = n > 0;
