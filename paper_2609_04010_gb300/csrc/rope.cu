@@ -54,12 +54,24 @@ __device__ __forceinline__ void rotate_pairs(uint4& x, const float* c, const flo
 
 // A block takes rows_per_block rows: their sines first, in shared memory, then items of two
 // 16-byte vectors (the two halves' vectors of 8 pairs, or 16 adjacent elements).
+constexpr int kRopeRows = 8;
+template <int D>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeParams p) {
   extern __shared__ __align__(16) float table[];  // [rows][2][rot / 2]: cosines, sines
   const spec_rope_args_t& a = p.a;
-  const int half = a.rot_dim / 2, items = a.head_dim / 16;
+  __shared__ int pos_of[kRopeRows], slot_of[kRopeRows];
+  constexpr int kItems = D / 16;
+  const int half = a.rot_dim / 2;
   pdl_wait_prior();
   const int row0 = blockIdx.x * p.rows_per_block, nrows = min(p.rows_per_block, a.rows - row0);
+  if (threadIdx.x < nrows) {
+    const int slot = a.slots != nullptr ? a.slots[row0 + threadIdx.x] : -1;
+    const int pos = a.positions[row0 + threadIdx.x];
+    const bool past = slot >= 0 && slot / a.page_size >= a.num_pages;
+    pos_of[threadIdx.x] = pos;
+    slot_of[threadIdx.x] = past ? -1 : slot;
+    if (past && pos >= 0 && a.status != nullptr) set_status(a.status, SPEC_FLAG_BAD_PAGE);
+  }
   for (int i = threadIdx.x; i < nrows * half; i += kRopeThreads) {
     const int r = i / half, f = i - r * half;
     const int pos = a.positions[row0 + r];
@@ -70,55 +82,76 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     table[(2 * r + 1) * half + f] = s * p.factor;
   }
   __syncthreads();
-  const int per_row = p.heads * items;
-  for (int i = threadIdx.x; i < nrows * per_row; i += kRopeThreads) {
-    const int r = i / per_row, rest = i - r * per_row, head = rest / items, it = rest - head * items;
-    const int64_t row = row0 + r;
-    if (a.positions[row] < 0) continue;
-    const bool is_q = head < a.num_q_heads, is_v = head >= a.num_q_heads + a.num_kv_heads;
-    const int h = is_q ? head : (is_v ? head - a.num_q_heads - a.num_kv_heads : head - a.num_q_heads);
-    // where the two vectors are within the head
-    const bool turned = !is_v && it * 16 < a.rot_dim;
-    const bool apart = turned && !a.interleaved;
-    const int d0 = apart ? it * 8 : it * 16, d1 = apart ? half + it * 8 : it * 16 + 8;
-    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_q ? a.q : (is_v ? a.v : a.k));
-    if (src == nullptr) continue;
-    src += row * (is_q ? p.q_stride : (is_v ? p.v_stride : p.k_stride)) + static_cast<int64_t>(h) * a.head_dim;
-    __nv_bfloat16* cached = nullptr;
-    if (!is_q && a.slots != nullptr) {
-      const int slot = a.slots[row];
-      if (slot >= 0) {
-        const int page = slot / a.page_size;
-        if (page < a.num_pages) {
-          cached = static_cast<__nv_bfloat16*>(is_v ? a.v_cache : a.k_cache) +
-                   ((static_cast<int64_t>(page) * a.num_kv_heads + h) * a.page_size + slot % a.page_size) * a.head_dim;
-        } else if (a.status != nullptr && it == 0 && h == 0 && is_v) {
-          set_status(a.status, SPEC_FLAG_BAD_PAGE);
+  // Thread: item `it` of heads (head, row) hr, hr + step, ..; two are in flight together.
+  const int it = threadIdx.x % kItems, step = kRopeThreads / kItems;
+  const bool turned_item = it * 16 < a.rot_dim;
+  int head = threadIdx.x / kItems, r = 0;
+  auto settle = [&]() {
+    while (head >= p.heads) {
+      head -= p.heads;
+      ++r;
+    }
+  };
+  settle();
+  while (r < nrows) {
+    uint4 x0[2], x1[2];
+    __nv_bfloat16 *out[2], *cached[2];
+    int d0[2], d1[2], row_of[2];
+    bool turned[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      out[k] = cached[k] = nullptr;
+      if (r < nrows) {
+        const int64_t row = row0 + r;
+        const bool is_q = head < a.num_q_heads, is_v = head >= a.num_q_heads + a.num_kv_heads;
+        const int h = is_q ? head : (is_v ? head - a.num_q_heads - a.num_kv_heads : head - a.num_q_heads);
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_q ? a.q : (is_v ? a.v : a.k));
+        if (src != nullptr && pos_of[r] >= 0) {
+          // where the two vectors are within the head
+          turned[k] = !is_v && turned_item;
+          const bool apart = turned[k] && !a.interleaved;
+          d0[k] = apart ? it * 8 : it * 16;
+          d1[k] = apart ? half + it * 8 : it * 16 + 8;
+          row_of[k] = r;
+          src += row * (is_q ? p.q_stride : (is_v ? p.v_stride : p.k_stride)) + static_cast<int64_t>(h) * D;
+          const int slot = slot_of[r];
+          if (!is_q && slot >= 0) {
+            const int page = slot / a.page_size;
+            cached[k] = static_cast<__nv_bfloat16*>(is_v ? a.v_cache : a.k_cache) +
+                        ((static_cast<int64_t>(page) * a.num_kv_heads + h) * a.page_size + slot % a.page_size) * D;
+          }
+          if (is_q) out[k] = static_cast<__nv_bfloat16*>(a.q_out);
+          else if (!is_v) out[k] = static_cast<__nv_bfloat16*>(a.k_out);
+          if (out[k]) out[k] += row * (is_q ? p.q_out_stride : p.k_out_stride) + static_cast<int64_t>(h) * D;
+          if (out[k] || cached[k]) {
+            x0[k] = *reinterpret_cast<const uint4*>(src + d0[k]);
+            x1[k] = *reinterpret_cast<const uint4*>(src + d1[k]);
+          }
         }
       }
+      head += step;
+      settle();
     }
-    __nv_bfloat16* out = nullptr;
-    if (is_q) out = static_cast<__nv_bfloat16*>(a.q_out);
-    else if (!is_v) out = static_cast<__nv_bfloat16*>(a.k_out);
-    if (out) out += row * (is_q ? p.q_out_stride : p.k_out_stride) + static_cast<int64_t>(h) * a.head_dim;
-    if (out == nullptr && cached == nullptr) continue;
-    uint4 x0 = *reinterpret_cast<const uint4*>(src + d0), x1 = *reinterpret_cast<const uint4*>(src + d1);
-    if (turned) {
-      const float* c = table + 2 * r * half + 8 * it;
-      if (a.interleaved) {
-        rotate_pairs(x0, c, c + half);
-        rotate_pairs(x1, c + 4, c + half + 4);
-      } else {
-        rotate_halves(x0, x1, c, c + half);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (!out[k] && !cached[k]) continue;
+      if (turned[k]) {
+        const float* c = table + 2 * row_of[k] * half + 8 * it;
+        if (a.interleaved) {
+          rotate_pairs(x0[k], c, c + half);
+          rotate_pairs(x1[k], c + 4, c + half + 4);
+        } else {
+          rotate_halves(x0[k], x1[k], c, c + half);
+        }
       }
-    }
-    if (out) {
-      *reinterpret_cast<uint4*>(out + d0) = x0;
-      *reinterpret_cast<uint4*>(out + d1) = x1;
-    }
-    if (cached) {
-      *reinterpret_cast<uint4*>(cached + d0) = x0;
-      *reinterpret_cast<uint4*>(cached + d1) = x1;
+      if (out[k]) {
+        *reinterpret_cast<uint4*>(out[k] + d0[k]) = x0[k];
+        *reinterpret_cast<uint4*>(out[k] + d1[k]) = x1[k];
+      }
+      if (cached[k]) {
+        *reinterpret_cast<uint4*>(cached[k] + d0[k]) = x0[k];
+        *reinterpret_cast<uint4*>(cached[k] + d1[k]) = x1[k];
+      }
     }
   }
 }
@@ -136,11 +169,11 @@ cudaError_t launch_rope(const spec_rope_args_t& a, int sms, cudaStream_t stream)
   p.q_out_stride = a.q_out_row_stride ? a.q_out_row_stride : dq;
   p.k_out_stride = a.k_out_row_stride ? a.k_out_row_stride : dk;
   p.factor = a.factor == 0.f ? 1.f : a.factor;
-  p.rows_per_block = 1;
-  (void)sms;
+  // several rows a block once there are blocks for all SMs, so that threads have few idle turns
+  p.rows_per_block = a.rows >= kRopeRows * 8 * sms ? kRopeRows : 1;
   const size_t smem = static_cast<size_t>(p.rows_per_block) * a.rot_dim * sizeof(float);
   const dim3 grid((a.rows + p.rows_per_block - 1) / p.rows_per_block);
-  return launch_overlapped(rope_kernel, grid, kRopeThreads, smem, stream, p);
+  return launch_overlapped(a.head_dim == 128 ? rope_kernel<128> : rope_kernel<64>, grid, kRopeThreads, smem, stream, p);
 }
 
 }  // namespace specv
