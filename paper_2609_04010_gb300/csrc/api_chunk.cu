@@ -172,7 +172,7 @@ ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, 
   const size_t rows = static_cast<size_t>(P.grid) * 2 * 2 * kChunkTileRows;
   P.cum = P.end;
   P.work = ws_round(P.cum + sizeof(long long) * (static_cast<size_t>(P.max_units) + 1));
-  P.redo = ws_round(P.work + sizeof(ChunkWork) + sizeof(int4) * static_cast<size_t>(P.grid));
+  P.redo = ws_round(P.work + sizeof(ChunkWork) + sizeof(ChunkStart) * static_cast<size_t>(P.grid));
   P.partial_o = ws_round(P.redo + sizeof(int4) * (static_cast<size_t>(P.redo_cap) + 1));
   P.partial_ml = ws_round(P.partial_o + rows * a.head_dim * sizeof(float));
   P.q_half = ws_round(P.partial_ml + rows * sizeof(float2));

@@ -190,7 +190,11 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
     p.work->total = total;
     p.work->active = active;
   }
-  for (int c = tid; c < active; c += kSetupThreads) {
+  for (int c = tid; c < p.blocks; c += kSetupThreads) {
+    if (c >= active) {
+      p.work->starts[c] = {0, 0, 0, 0, 0, 0, 0, 0};
+      continue;
+    }
     const long long t = c * total / active;
     int lo = 0, hi = p.batch;  // the largest b whose steps begin at or before t
     while (hi - lo > 1) {
@@ -207,7 +211,9 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
       const int mid = (lo + hi) >> 1;
       if (cum[mid] - base <= rem) lo = mid; else hi = mid;
     }
-    p.work->starts[c] = make_int4(b, g, lo - f, static_cast<int>(rem - (cum[lo] - base)));
+    const ChunkSeq s = p.seqs[b];
+    p.work->starts[c] = {b,      g,   lo - f,   static_cast<int>(rem - (cum[lo] - base)),
+                         s.row0, s.n, s.kv_len, static_cast<int>((c + 1) * total / active - t)};
   }
 }
 
@@ -418,7 +424,7 @@ __device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part)
   const long long total = p.work->total;
   const int active = p.work->active;
   // the unit's first step, from this block's first virtual one
-  const long long at = c * total / active - p.work->starts[c].w + u.start();
+  const long long at = c * total / active - p.work->starts[c].off + u.start();
   const int first = owner_of(at, total, active), subs = u.twin ? 2 : 1, n = (c - first + 1) * subs;
   const int tile_rows = p.tile_tokens * p.group;
   constexpr int C8 = D / 8;

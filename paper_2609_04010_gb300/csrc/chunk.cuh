@@ -42,12 +42,16 @@ struct ChunkSeq {
   int kv_len;
   int first_unit;  // its first unit among all (tensor cores)
 };
-// The work list of the tensor-core kernel, and where each block starts in it: the sequence, the
-// KV head, the unit of its tokens, and the (virtual) step in it.
+// The work list of the tensor-core kernel, and where each block starts in it: the sequence and what is
+// known of it, the KV head, the unit of its tokens, the virtual step in it, and the steps to take.
+struct alignas(16) ChunkStart {
+  int b, g, rt, off;
+  int row0, n, kv_len, left;
+};
 struct ChunkWork {
   long long total;
-  int active, pad;   // blocks with work
-  int4 starts[1];    // [active]
+  int active, pad;       // blocks with work
+  ChunkStart starts[1];  // [blocks], left = 0 without work
 };
 
 struct ChunkParams {
@@ -163,14 +167,12 @@ struct ChunkWalk {
   // A range has at least kChunkTwinCost virtual steps, so that it has a step of a unit that it lies
   // within; the first stop of one that begins at the very end of a unit has none, and is passed.
   __device__ __forceinline__ bool begin(const ChunkParams& p, int block) {
-    const int active = p.work->active;
-    if (block >= active) return false;
-    const long long total = p.work->total, t0 = block * total / active;
-    left = static_cast<int>((block + 1) * total / active - t0);
-    const int4 s = p.work->starts[block];
-    b = s.x; g = s.y; rt = s.z;
-    enter(p);
-    stop(p, s.w);
+    const int4* at = reinterpret_cast<const int4*>(&p.work->starts[block]);
+    const int4 x = at[0], y = at[1];
+    b = x.x; g = x.y; rt = x.z;
+    row0 = y.x; n = y.y; kv_len = y.z; left = y.w;
+    if (left == 0) return false;
+    stop(p, x.w);
     return ns > 0 || next(p);
   }
   __device__ __forceinline__ bool next(const ChunkParams& p) {

@@ -10,7 +10,8 @@ namespace {
 // Forks
 // ---------------------------------------------------------------------------------
 constexpr int kForkThreads = 1024;
-constexpr int kForkBlocks = 8;     // one cluster
+constexpr int kForkBlocks = 16;    // of a cluster, at most
+constexpr int kForkEntries = 4096; // table entries that a block takes before there are more blocks
 constexpr int kNobody = INT32_MAX;
 constexpr int kClaim = 1 << 30;    // claims of freed pages are stored as -kClaim - place
 
@@ -48,17 +49,36 @@ __device__ __forceinline__ int scan_block(int v, int* sh, int* total) {
   return before + x - v;
 }
 
+// The ids of up to 32 * kAhead entries of a table row, a lane's in a register each.
+constexpr int kAhead = 8;
+template <typename F>
+__device__ __forceinline__ void for_entries(const int32_t* row, int n, F f) {
+  const int lane = threadIdx.x & 31;
+  for (int i0 = 0; i0 < n; i0 += 32 * kAhead) {
+    int id[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) id[k] = i0 + 32 * k + lane < n ? row[i0 + 32 * k + lane] : -1;
+    f(i0, id);
+  }
+}
+
 // One cluster. Each block works out for itself who goes on from whom and which pages the forks
 // get (the same in all of them); rows of the table and pages are shared out by warps. Freed
 // pages keep one order whatever the order of the blocks: a page goes to the last place that
 // held it, by a minimum over the places, and places are counted in order.
+//
+// What bounds it is latency: seven passes (who goes on, the scan, the rows, claims, counts, the list, the
+// lengths), each a round trip or two to L2 and a barrier of the blocks. 512 sequences of up to 8,192
+// tokens, a quarter of which fork or end: 29 us with up to 16 blocks, 41 with 8, 78 with a load at a time.
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constant__ ForkParams p) {
   extern __shared__ int32_t smem[];
   const spec_fork_args_t& a = p.a;
-  const int B = a.batch, P = a.page_size, MP = a.max_pages_per_seq;
-  int32_t* keeper = smem;        // [B]: who goes on with a sequence's pages
-  int32_t* fresh = smem + B;     // [B]: new pages before a fork's, -1: not a fork, -2: refused
-  int32_t* length = smem + 2 * B;  // [B]: new lengths
+  const int B = a.batch, P = a.page_size, MP = a.max_pages_per_seq, N = a.num_pages;
+  int32_t* keeper = smem;          // [B]: who goes on with a sequence's pages
+  int32_t* fresh = smem + B;       // [B]: new pages before a fork's, -1: not a fork, -2: refused
+  int32_t* source = smem + 2 * B;  // [B]: whom it goes on from (-1: nobody; itself where it stays)
+  int32_t* length = smem + 3 * B;  // [B]: tokens it holds so far (-1: out of range)
+  uint8_t* refused = reinterpret_cast<uint8_t*>(smem + 4 * B);  // [B]
   __shared__ int sh[32];
   __shared__ int s_taken;
   const int tid = threadIdx.x, lane = tid & 31;
@@ -66,130 +86,136 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
   const int gwarp = (tid >> 5) * blocks + rank, warps = blocks * (kForkThreads / 32);
   pdl_wait_prior();
   const int count0 = min(max(*a.free_count, 0), a.free_capacity);
-
-  auto len_ok = [&](int b) {
-    const int n = a.kv_len[b];
-    return n >= 0 && static_cast<int64_t>(n) + a.reserved <= static_cast<int64_t>(MP) * P;
-  };
-  // whom b goes on from (-1: nobody), b itself where the request or a length is out of range
-  auto source = [&](int b, bool* bad) {
-    const int q = a.parent[b];
-    const bool ok = q >= -1 && q < B && len_ok(b) && (q < 0 || len_ok(q));
-    *bad = !ok;
-    return ok ? q : b;
-  };
   auto held = [&](int n) { return static_cast<int>((static_cast<int64_t>(n) + a.reserved + P - 1) / P); };
+  auto row_of = [&](int b) { return a.page_table + static_cast<int64_t>(b) * MP; };
 
-  if (a.new_shares != a.shares)
-    for (int i = rank * kForkThreads + tid; i < a.num_pages; i += blocks * kForkThreads) a.new_shares[i] = a.shares[i];
-  if (a.new_free_pages != a.free_pages)
-    for (int i = rank * kForkThreads + tid; i < a.free_capacity; i += blocks * kForkThreads)
-      a.new_free_pages[i] = a.free_pages[i];
-  for (int b = tid; b < B; b += kForkThreads) keeper[b] = kNobody;
+  for (int b = tid; b < B; b += kForkThreads) {
+    const int n = a.kv_len[b];
+    keeper[b] = kNobody;
+    source[b] = a.parent[b];
+    length[b] = n >= 0 && static_cast<int64_t>(n) + a.reserved <= static_cast<int64_t>(MP) * P ? n : -1;
+  }
+  // (holders and the free list, while that is on its way)
+  auto copy = [&](int32_t* to, const int32_t* from, int n) {
+    const int64_t step = static_cast<int64_t>(blocks) * kForkThreads;
+    for (int64_t i0 = rank * kForkThreads + tid; to != from && i0 < n; i0 += kAhead * step) {
+      int x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + k * step < n) x[k] = from[i0 + k * step];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + k * step < n) to[i0 + k * step] = x[k];
+    }
+  };
+  copy(a.new_shares, a.shares, N);
+  copy(a.new_free_pages, a.free_pages, a.free_capacity);
   if (tid == 0) s_taken = 0;
   __syncthreads();
+  // requests and lengths out of range: the sequence stays as it is (flag 1)
   for (int b = tid; b < B; b += kForkThreads) {
-    bool bad;
-    const int q = source(b, &bad);
+    const int q = source[b];
+    const bool ok = q >= -1 && q < B && length[b] >= 0 && (q < 0 || length[q] >= 0);
+    fresh[b] = ok ? -1 : -3;
+  }
+  __syncthreads();
+  for (int b = tid; b < B; b += kForkThreads) {
+    if (fresh[b] == -3) source[b] = b;
+    const int q = source[b];
     if (q >= 0) atomicMin(&keeper[q], q == b ? -1 : b);
   }
   __syncthreads();
   int64_t carry = 0;
   for (int b0 = 0; b0 < B; b0 += kForkThreads) {
     const int b = b0 + tid;
-    int need = 0, n = 0, q = -1;
+    int need = 0, q = -1;
     bool bad = false, fork = false;
     if (b < B) {
-      q = source(b, &bad);
-      if (q >= 0) {
-        n = a.kv_len[q];
-        fork = q != b && keeper[q] != b;
-        if (fork) need = held(n) - n / P;
-      }
+      q = source[b];
+      bad = fresh[b] == -3;
+      fork = q >= 0 && q != b && keeper[q] != b;
+      if (fork) need = held(length[q]) - length[q] / P;
     }
     int all;
     const int64_t before = carry + scan_block(need, sh, &all);
     if (b < B) {
-      const bool refused = fork && need > 0 && before + need > count0;
-      if (fork && need > 0 && !refused) atomicMax(&s_taken, static_cast<int>(before) + need);
-      fresh[b] = !fork ? -1 : (refused ? -2 : static_cast<int>(min(before, static_cast<int64_t>(kNobody))));
-      length[b] = q < 0 || refused ? 0 : n;
-      if (rank == 0 && a.flags) a.flags[b] = bad ? 1 : (refused ? 2 : 0);
+      const bool none_left = fork && need > 0 && before + need > count0;
+      if (fork && need > 0 && !none_left) atomicMax(&s_taken, static_cast<int>(before) + need);
+      refused[b] = none_left;
+      fresh[b] = !fork ? -1 : (none_left ? -2 : static_cast<int>(min(before, static_cast<int64_t>(kNobody))));
+      if (rank == 0 && a.flags) a.flags[b] = bad ? 1 : (none_left ? 2 : 0);
     }
     carry += all;
   }
   __syncthreads();
   const int taken = s_taken;
-  cluster_sync();  // holders are copied, lengths and the free count read by all
+  cluster_sync();  // holders are copied, the free count is read by all
 
   // ---- tables, copies, holders ----
-  auto ended = [&](int b) {  // nobody goes on with b's pages
-    return keeper[b] == kNobody && len_ok(b);
-  };
+  auto ended = [&](int b) { return keeper[b] == kNobody && length[b] >= 0; };  // nobody goes on with b's pages
   int32_t* rows_out = p.stage ? p.stage : a.new_table;
   for (int b = gwarp; b < B; b += warps) {
-    bool bad;
-    const int q = source(b, &bad);
-    const int32_t* own = a.page_table + static_cast<int64_t>(b) * MP;
+    const int q = source[b];
     int32_t* out = rows_out + static_cast<int64_t>(b) * MP;
     if (q == b) {
       if (!p.stage)
-        for (int i = lane; i < MP; i += 32) out[i] = own[i];
+        for_entries(row_of(b), MP, [&](int i0, const int* id) {
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k)
+            if (i0 + 32 * k + lane < MP) out[i0 + 32 * k + lane] = id[k];
+        });
       if (lane == 0) a.copies[2 * b] = a.copies[2 * b + 1] = -1;
-      continue;
-    }
-    const int32_t* from = a.page_table + static_cast<int64_t>(q < 0 ? 0 : q) * MP;
-    const bool none = q < 0 || fresh[b] == -2;
-    const int n = none ? 0 : a.kv_len[q], hold = none ? 0 : held(n);
-    const int whole = fresh[b] >= 0 ? n / P : hold;  // pages held together with others, or taken over
-    for (int i = lane; i < MP; i += 32) {
-      int page = -1;
-      if (i < whole) {
-        page = from[i];
-        if (fresh[b] >= 0 && page >= 0 && page < a.num_pages) atomicAdd(&a.new_shares[page], 1);
-      } else if (i < hold) {
-        page = a.free_pages[count0 - 1 - fresh[b] - (i - whole)];
+    } else {
+      const bool none = q < 0 || fresh[b] == -2, fork = fresh[b] >= 0;
+      const int n = none ? 0 : length[q], hold = none ? 0 : held(n);
+      const int whole = fork ? n / P : hold;  // pages held together with others, or taken over
+      for_entries(row_of(q < 0 ? 0 : q), none ? 0 : whole, [&](int i0, const int* id) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (i0 + 32 * k + lane < whole) {
+            out[i0 + 32 * k + lane] = id[k];
+            if (fork && id[k] >= 0 && id[k] < N) atomicAdd(&a.new_shares[id[k]], 1);
+          }
+      });
+      for (int i = whole + lane; i < MP; i += 32)
+        out[i] = i < hold ? a.free_pages[count0 - 1 - fresh[b] - (i - whole)] : -1;
+      if (lane == 0) {
+        const bool copy = !none && fork && n % P != 0;
+        a.copies[2 * b] = copy ? row_of(q)[whole] : -1;
+        a.copies[2 * b + 1] = copy ? a.free_pages[count0 - 1 - fresh[b]] : -1;
       }
-      out[i] = page;
     }
-    if (lane == 0) {
-      const bool copy = !none && fresh[b] >= 0 && n % P != 0;
-      a.copies[2 * b] = copy ? from[whole] : -1;
-      a.copies[2 * b + 1] = copy ? a.free_pages[count0 - 1 - fresh[b]] : -1;
-    }
-  }
-  for (int b = gwarp; b < B; b += warps) {
-    if (!ended(b)) continue;
-    const int hold = held(a.kv_len[b]);
-    const int32_t* own = a.page_table + static_cast<int64_t>(b) * MP;
-    for (int i = lane; i < hold; i += 32)
-      if (own[i] >= 0 && own[i] < a.num_pages) atomicSub(&a.new_shares[own[i]], 1);
+    if (ended(b))
+      for_entries(row_of(b), held(length[b]), [&](int, const int* id) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (id[k] >= 0 && id[k] < N) atomicSub(&a.new_shares[id[k]], 1);
+      });
   }
   cluster_sync();
   // ---- pages that nobody holds any more: the last place claims each ----
-  for (int b = gwarp; b < B; b += warps) {
-    if (!ended(b)) continue;
-    const int hold = held(a.kv_len[b]);
-    const int32_t* own = a.page_table + static_cast<int64_t>(b) * MP;
-    for (int i = lane; i < hold; i += 32) {
-      const int page = own[i];
-      if (page >= 0 && page < a.num_pages && a.new_shares[page] < 0)
-        atomicMin(&a.new_shares[page], -kClaim - (b * MP + i));
-    }
-  }
+  for (int b = gwarp; b < B; b += warps)
+    if (ended(b))
+      for_entries(row_of(b), held(length[b]), [&](int i0, const int* id) {
+        int left[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) left[k] = id[k] >= 0 && id[k] < N ? __ldcg(&a.new_shares[id[k]]) : 0;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (left[k] < 0) atomicMin(&a.new_shares[id[k]], -kClaim - (b * MP + i0 + 32 * k + lane));
+      });
   cluster_sync();
-  auto claimed = [&](const int32_t* own, int b, int i, int hold) {
-    if (i >= hold) return false;
-    const int page = own[i];
-    return page >= 0 && page < a.num_pages && __ldcg(&a.new_shares[page]) == -kClaim - (b * MP + i);
-  };
   for (int b = gwarp; b < B; b += warps) {
     int n = 0;
-    if (ended(b)) {
-      const int hold = held(a.kv_len[b]);
-      const int32_t* own = a.page_table + static_cast<int64_t>(b) * MP;
-      for (int i0 = 0; i0 < hold; i0 += 32) n += __popc(__ballot_sync(0xffffffffu, claimed(own, b, i0 + lane, hold)));
-    }
+    if (ended(b))
+      for_entries(row_of(b), held(length[b]), [&](int i0, const int* id) {
+        int claim[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) claim[k] = id[k] >= 0 && id[k] < N ? __ldcg(&a.new_shares[id[k]]) : 0;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          n += __popc(__ballot_sync(0xffffffffu, claim[k] == -kClaim - (b * MP + i0 + 32 * k + lane)));
+      });
     if (lane == 0) p.freed[b] = n;
   }
   cluster_sync();
@@ -205,37 +231,41 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
   __syncthreads();
   for (int b = gwarp; b < B; b += warps) {
     if (!ended(b)) continue;
-    const int hold = held(a.kv_len[b]);
-    const int32_t* own = a.page_table + static_cast<int64_t>(b) * MP;
     int at = fresh[b];
-    for (int i0 = 0; i0 < hold; i0 += 32) {
-      const bool mine = claimed(own, b, i0 + lane, hold);
-      const uint32_t who = __ballot_sync(0xffffffffu, mine);
-      if (mine) {
-        const int page = own[i0 + lane], to = at + __popc(who & ((1u << lane) - 1));
-        if (to < a.free_capacity) a.new_free_pages[to] = page;
-        a.new_shares[page] = 0;
+    for_entries(row_of(b), held(length[b]), [&](int i0, const int* id) {
+      int claim[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) claim[k] = id[k] >= 0 && id[k] < N ? __ldcg(&a.new_shares[id[k]]) : 0;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const bool mine = claim[k] == -kClaim - (b * MP + i0 + 32 * k + lane);
+        const uint32_t who = __ballot_sync(0xffffffffu, mine);
+        if (mine) {
+          const int to = at + __popc(who & ((1u << lane) - 1));
+          if (to < a.free_capacity) a.new_free_pages[to] = id[k];
+          a.new_shares[id[k]] = 0;
+        }
+        at += __popc(who);
       }
-      at += __popc(who);
-    }
+    });
   }
-  cluster_sync();
-  // ---- what may have been read until here ----
+  if (p.stage) cluster_sync();  // the rows have been read
+  // ---- what has been read until here ----
   if (p.stage)
-    for (int b = gwarp; b < B; b += warps) {
-      bool bad;
-      if (source(b, &bad) == b) continue;
-      for (int i = lane; i < MP; i += 32) a.new_table[static_cast<int64_t>(b) * MP + i] = p.stage[static_cast<int64_t>(b) * MP + i];
-    }
-  cluster_sync();
+    for (int b = gwarp; b < B; b += warps)
+      if (source[b] != b)
+        for_entries(p.stage + static_cast<int64_t>(b) * MP, MP, [&](int i0, const int* id) {
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k)
+            if (i0 + 32 * k + lane < MP) a.new_table[static_cast<int64_t>(b) * MP + i0 + 32 * k + lane] = id[k];
+        });
   if (rank == 0) {
+    // (every block has read the lengths and the count before its first barrier)
     for (int b = tid; b < B; b += kForkThreads) {
-      bool bad;
-      const bool stays = source(b, &bad) == b;
-      length[b] = stays ? a.kv_len[b] : length[b];
+      const int q = source[b];
+      if (q != b) a.new_kv_len[b] = q < 0 || refused[b] ? 0 : length[q];
+      else if (a.new_kv_len != a.kv_len) a.new_kv_len[b] = a.kv_len[b];
     }
-    __syncthreads();
-    for (int b = tid; b < B; b += kForkThreads) a.new_kv_len[b] = length[b];
     if (tid == 0) *a.new_free_count = min(base, a.free_capacity);
   }
 }
@@ -292,7 +322,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
 
 }  // namespace
 
-size_t fork_smem(int batch) { return static_cast<size_t>(batch) * 3 * sizeof(int32_t); }
+size_t fork_smem(int batch) { return static_cast<size_t>(batch) * (4 * sizeof(int32_t) + 1); }
 
 cudaError_t launch_fork(const spec_fork_args_t& a, char* ws, cudaStream_t stream) {
   ForkParams p;
@@ -306,14 +336,18 @@ cudaError_t launch_fork(const spec_fork_args_t& a, char* ws, cudaStream_t stream
   const cudaError_t e = cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(fork_smem(SPEC_SLOTS_MAX_BATCH)));
   if (e != cudaSuccess) return e;
+  const cudaError_t wide = cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);  // 16 blocks
+  if (wide != cudaSuccess) return wide;
+  const int64_t entries = static_cast<int64_t>(a.batch) * a.max_pages_per_seq;
+  const int blocks = static_cast<int>(entries / kForkEntries < 1 ? 1 : entries / kForkEntries > kForkBlocks ? kForkBlocks : entries / kForkEntries);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kForkBlocks;
+  attr[1].val.clusterDim.x = blocks;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kForkBlocks);
+  cfg.gridDim = dim3(blocks);
   cfg.blockDim = dim3(kForkThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
