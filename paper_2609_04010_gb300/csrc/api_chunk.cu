@@ -147,14 +147,18 @@ spec_status_t check_copy(const spec_copy_args_t* a) {
 
 namespace specv {
 
+// Virtual steps of a unit that sees all the keys that a table row holds, at most.
+static int64_t chunk_longest(const spec_chunk_attn_args_t& a) {
+  return static_cast<int64_t>(a.max_pages_per_seq) * a.page_size / kChunkKeyTile * kChunkTwinCost + 32;
+}
+
 bool chunk_tc_fits(const spec_chunk_attn_args_t& a) {
   const int group = a.num_q_heads / a.num_kv_heads;
   if (group > kChunkTileRows) return false;
   const int64_t per_unit = 2 * (kChunkTileRows / group);
   const int64_t units = a.rows / per_unit + a.batch;
   // 32-bit counts: units, and the steps of a block (of at least 64)
-  const int64_t tiles = static_cast<int64_t>(a.max_pages_per_seq) * a.page_size / kChunkKeyTile * kChunkTwinCost + 32;
-  return units * a.num_kv_heads <= INT32_MAX / 4 && units * a.num_kv_heads <= (static_cast<int64_t>(INT32_MAX) * 32) / tiles && static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX / 4;
+  return units * a.num_kv_heads <= INT32_MAX / 4 && units * a.num_kv_heads <= (static_cast<int64_t>(INT32_MAX) * 32) / chunk_longest(a) && static_cast<int64_t>(a.num_pages) * a.num_kv_heads <= INT32_MAX / 4;
 }
 
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path) {
@@ -166,8 +170,10 @@ ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, 
   P.end = ws_round(P.bad + sizeof(int32_t) * static_cast<size_t>(a.batch));
   if (P.path != SPEC_ATTN_TENSOR_CORES) return P;
   P.tile_tokens = kChunkTileRows / (a.num_q_heads / a.num_kv_heads);
-  P.grid = num_sms;
   P.max_units = a.rows / (2 * P.tile_tokens) + a.batch;
+  // a block per SM, or as many as the longest sequences could give work
+  const int64_t work = static_cast<int64_t>(P.max_units) * a.num_kv_heads * chunk_longest(a) / kChunkTwinCost;
+  P.grid = static_cast<int>(work < num_sms ? (work < 1 ? 1 : work) : num_sms);
   P.redo_cap = P.max_units * a.num_kv_heads + P.grid;
   const size_t rows = static_cast<size_t>(P.grid) * 2 * 2 * kChunkTileRows;
   P.cum = P.end;

@@ -36,7 +36,7 @@ struct Smem {
 // for the tensor cores also the work list, equal numbers of virtual steps per block. One block,
 // because all of it depends on sums over the batch.
 constexpr int kSetupThreads = 1024;
-constexpr int kSetupKept = 2048;  // sequences and units whose sums are kept in shared memory
+constexpr int kSetupKept = 1024;  // sequences and units that are kept in shared memory too
 
 // The block's exclusive prefix sum of v in thread order, and the total.
 __device__ __forceinline__ long long scan_block(long long v, long long* sh, long long* total) {
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
     }
   }
   __shared__ long long sh[32];
-  __shared__ int first_kept[kSetupKept + 1];
+  __shared__ ChunkSeq seq_kept[kSetupKept + 1];
   __shared__ long long cum_kept[kSetupKept + 1];
   pdl_wait_prior();
   const int tid = threadIdx.x;
@@ -147,20 +147,21 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
       p.seqs[b] = s;
       p.seq_bad[b] = bad ? 1 : 0;
       if (bad) set_status(p.status, SPEC_FLAG_BAD_KV_LEN);
-      if (b < kSetupKept) first_kept[b] = s.first_unit;
+      if (b < kSetupKept) seq_kept[b] = s;
     }
   }
   if (!p.blocks) return;
   const int nunits = static_cast<int>(min(carry, static_cast<long long>(p.max_units)));
   if (tid == 0) {
     p.seqs[p.batch] = {0, 0, 0, nunits};
-    if (p.batch < kSetupKept) first_kept[p.batch] = nunits;
+    if (p.batch <= kSetupKept) seq_kept[p.batch] = {0, 0, 0, nunits};
     p.redo[0] = make_int4(0, 0, 0, 0);
     p.cum[0] = 0;
     cum_kept[0] = 0;
   }
   __syncthreads();
-  auto first = [&](int b) { return p.batch < kSetupKept ? first_kept[b] : p.seqs[b].first_unit; };
+  const ChunkSeq* seqs = p.batch <= kSetupKept ? seq_kept : p.seqs;
+  auto first = [&](int b) { return seqs[b].first_unit; };
   const long long* cum = nunits <= kSetupKept ? cum_kept : p.cum;
   carry = 0;
   for (int u0 = 0; u0 < nunits; u0 += kSetupThreads) {
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
         const int mid = (lo + hi) >> 1;
         if (first(mid) <= u) lo = mid; else hi = mid;
       }
-      const ChunkSeq s = p.seqs[lo];
+      const ChunkSeq s = seqs[lo];
       if (u - s.first_unit < chunk_units(p, s.n)) steps = chunk_unit(p, s, u - s.first_unit).length();
     }
     long long all;
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
       const int mid = (lo + hi) >> 1;
       if (cum[mid] - base <= rem) lo = mid; else hi = mid;
     }
-    const ChunkSeq s = p.seqs[b];
+    const ChunkSeq s = seqs[b];
     p.work->starts[c] = {b,      g,   lo - f,   static_cast<int>(rem - (cum[lo] - base)),
                          s.row0, s.n, s.kv_len, static_cast<int>((c + 1) * total / active - t)};
   }
