@@ -45,9 +45,9 @@
  *     +inf logits) never traps: the kernels set a bit in the workspace status word
  *     (SPEC_FLAG_*), write the documented sentinel outputs for the affected
  *     sequence, and carry on. spec_read_device_status reads and clears the word.
- *   - Kernels never wait on other thread blocks; every internal wait on an
- *     asynchronous copy or tensor-core operation is bounded, and a timeout sets
- *     SPEC_FLAG_TIMEOUT instead of hanging.
+ *   - Kernels never wait on other thread blocks, those of one cluster excepted (they run
+ *     together); every internal wait on an asynchronous copy or tensor-core operation
+ *     is bounded, and a timeout sets SPEC_FLAG_TIMEOUT instead of hanging.
  */
 #ifndef SPEC_VERIFY_H
 #define SPEC_VERIFY_H
@@ -766,13 +766,16 @@ spec_status_t spec_rope_kv(const spec_rope_args_t* rope, spec_stream_t stream);
  *     [0, rows) in order is left out; one with rows but kv_len[b] outside [n_b,
  *     max_pages_per_seq * page_size] gets out = 0 and lse = -inf (both SPEC_FLAG_BAD_KV_LEN), as
  *     does one with a visible key's page id outside [0, num_pages) (SPEC_FLAG_BAD_PAGE).
- *   - Scores, softmax statistics and accumulators are fp32; on the tensor cores a weight enters
- *     its product rounded to bf16, relative to the row's largest of at least 2^-8 of its range.
- *     Values of the 8-bit cache enter as their bf16 value times scale, exact for the powers of
- *     two that spec_append_kv_fp8 writes; value scales are clamped to [2^-32, 2^32].
+ *   - Scores, softmax statistics and accumulators are fp32. On the tensor cores the weights enter
+ *     their product rounded to bf16, off by at most 2^-8 of themselves. With the 8-bit cache they
+ *     enter as fp16 times their page's value scale, off by 2^-11 of that product or 2^-33 of the
+ *     row's largest; its values enter exactly, and queries as fp16 times a power of two of their
+ *     row: elements below 2^-31 of its largest are off by at most 2^-39 of that. Scales
+ *     need not be powers of two; value scales are clamped to [2^-32, 2^32].
  *   - path: SPEC_ATTN_AUTO takes the tensor cores where the call fits them (Hq / Hkv at most 128),
  *     else CUDA cores; SPEC_ATTN_TENSOR_CORES is SPEC_ERR_UNSUPPORTED where it does not fit.
- *   - Three launches. The workspace rules are spec_verify_attention's.
+ *   - Three launches. The workspace rules are spec_verify_attention's; it holds the parts of
+ *     sequences that several blocks share and, with the 8-bit cache, the queries in fp16.
  */
 typedef struct {
   int32_t batch;              /* >= 1                                                       */
@@ -889,7 +892,8 @@ spec_status_t spec_copy_pages(const spec_copy_args_t* copy, spec_stream_t stream
  * spec_test_attention_wait_timeout returns SPEC_ERR_UNSUPPORTED for shapes the
  * tensor-core row-tile kernel does not take; spec_test_attention_fp8_wait_timeout does the
  * same for spec_verify_attention_fp8 and its tensor-core kernel, and
- * spec_test_chunk_attention_wait_timeout for spec_chunk_attention. Nothing traps, faults or waits without bound.
+ * spec_test_chunk_attention_wait_timeout for spec_chunk_attention. Nothing traps, faults or
+ * waits without bound.
  * ------------------------------------------------------------------------------------- */
 spec_status_t spec_test_attention_wait_timeout(const spec_attn_args_t* attn, void* ws,
                                                size_t ws_bytes, spec_stream_t stream);

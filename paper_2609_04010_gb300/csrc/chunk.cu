@@ -62,7 +62,7 @@ __device__ __forceinline__ long long scan_block(long long v, long long* sh, long
 }
 
 // Query rows as fp16 for the products with the 8-bit cache, each scaled by the power of two that takes
-// its largest finite magnitude into [2^14, 2^15): bf16 values down to 2^-28 of that are exact, smaller
+// its largest finite magnitude into [2^14, 2^15): bf16 values down to 2^-31 of that are exact, smaller
 // ones to 2^-39 of it.
 template <int D>
 __device__ __forceinline__ void halve_queries(const ChunkParams& p, int64_t warp, int64_t warps) {

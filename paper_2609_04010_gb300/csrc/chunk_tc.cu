@@ -1,4 +1,4 @@
-// Attention of ragged chunks over the paged bf16 cache on tcgen05 tensor cores
+// Attention of ragged chunks over the paged caches on tcgen05 tensor cores
 // (spec_chunk_attention, SPEC_ATTN_TENSOR_CORES).
 //
 //   S[row][key] = Q[row][:] . K[key][:]              (M = 128 rows, N = 128 keys, K = D)
@@ -8,21 +8,39 @@
 // query rows (token, head of the group) of consecutive tokens and one KV head. Each tile of 128
 // keys is read once for both; while one M tile is at its softmax the tensor core works for the
 // other. A unit with no more rows than one M tile holds them twice and gives every second tile of
-// keys to each, so that single tokens keep two tiles in flight too.
+// keys to each ("twin"), so that single tokens keep two tiles in flight too.
+//
+// The 8-bit cache's values are made fp16 on the way, exactly; queries are fp16 times a power of two
+// per row (made beside the set-up). Its scales stay out of the products: with the key's scale sk and
+// the value's sv, P = 2^(c sq sk S + log2(sv) - m) and the sum is of P / sv. P is fp16, at most 2^15.
 //
 // Warps:
 //   0..7, 8..15 softmax of M tile 0 and 1, two threads per row, each with half of a tile's keys: 64
-//               scores from TMEM, maximum, weights as bf16 over the first half of their columns, from
+//               scores from TMEM, maximum, weights in 16 bits over the first half of their columns, from
 //               which the second product reads them; at a unit's end half of the row's outputs
 //   16, 17      producers of K (and Q) and of V: a TMA box per page, into two rings of tiles
-//   18          products, one thread: S of the next tile follows at once on the O += P V that read
-//               its columns, and the M tiles take turns
+//   18          products: S of the next tile follows at once on the O += P V that read its columns, and
+//               the M tiles take turns
 //   19          passes V on, and makes that of keys that some row does not see finite first (their
 //               weight 0 is multiplied): keys that no row sees are cleared; where one that some rows
 //               see is not finite, the unit is noted and computed again on CUDA cores after all
+//   (8-bit cache: 16 brings tiles and Q, 17 and 19 convert, and do to V what 19 does)
 // The list of units is cut into equal ranges of steps, one per block (chunk.cuh); parts of split
 // units are joined by the finishing launch. Every wait is bounded: one that runs out sets
 // SPEC_FLAG_TIMEOUT, and the block drains its copies and products, frees TMEM and returns.
+//
+// What bounds it. Long chunks (4,096 tokens behind 28,672, 32 / 8 heads): 1,306 us, 1,578 TFLOP/s of
+// Q K^T and P V (1,893 measured peak); without the softmax's work the same code takes 1,150, the
+// products' own time and the turns between them. Whole prompts (4 x 4,093): 458 us, 1,200 TFLOP/s: a unit
+// of 64 tokens has 17 steps on average, and its outputs and first weights, about 4 steps of time, are
+// not hidden. Single tokens (32 requests to 16,384 tokens): 200 us, 5.5 TB/s, 0.81 of the copy rate: a
+// step's five tiles in flight. 8-bit, two chunks of 2,048 tokens: 610 us, 1,000 TFLOP/s:
+// two warps make 32,768 values fp16 a step.
+// What was measured on the way (long chunk): one softmax thread per row 1,697 us (eight warps cannot
+// hide each other's waits); two product warps in turns 1,446; products issued by "lane == 0" instead of
+// an elected lane 1,404; registers spilled in any role's loop 1,800 to 2,900, because next to 226 KB of
+// shared memory there is hardly any L1; outputs written after the next unit's first weights 1,626.
+
 #include <cuda.h>  // CUtensorMap
 #include <cuda_bf16.h>
 
@@ -79,13 +97,18 @@ struct Cfg {
   static constexpr uint32_t OFF_Q = 0;              // [2][DH][128 rows][128 B]
   static constexpr uint32_t OFF_K = OFF_Q + 2 * QTILE;
   static constexpr uint32_t OFF_V = OFF_K + KST * TILE;
-  // float [2][128]: between a row's two threads; or float2 [128]: a twin's (m, l)
   static constexpr uint32_t OFF_RAW = OFF_V + VST * TILE;  // [K, V]
+  // float [2][128]: between a row's two threads; or float2 [128]: a twin's (m, l)
   static constexpr uint32_t OFF_XCH = OFF_RAW + 2 * RAW;
-  static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps, then kConverters]
-  static constexpr uint32_t OFF_LAST = OFF_WALK + (kSoftWarps + (FP8 ? 3 : 0)) * sizeof(ChunkWalk);  // Ended [kSoftWarps]
-  static constexpr uint32_t OFF_PAGES = (OFF_LAST + kSoftWarps * sizeof(Ended) + 15) / 16 * 16;  // float4 [4 tiles][8 pages]
-  static constexpr uint32_t OFF_RAWS = OFF_PAGES + (FP8 ? 4 * 8 * 16 : 0);  // RawTile [4 tiles]
+  static constexpr uint32_t OFF_WALK = OFF_XCH + 2 * MR * 4;  // ChunkWalk [kSoftWarps, then the 8-bit producer's]
+  static constexpr uint32_t OFF_LAST = OFF_WALK + (kSoftWarps + (FP8 ? 1 : 0)) * sizeof(ChunkWalk);  // Ended [kSoftWarps]
+  // The scales of a tile's pages, float4 [PT tiles][8 pages]. They are written when tile t is brought; by
+  // then K of tile t - 1 is converted, so S of tile e = t - 1 - KST is done, and with it the weights of
+  // its M tile's tile before it. Tile e's weights may be in work, in a twin e - 1's of the other M tile,
+  // and where a twin of one tile follows e - 2's (the join holds its successor): e - 2..t are in use.
+  static constexpr int PT = KST + 4;
+  static constexpr uint32_t OFF_PAGES = (OFF_LAST + kSoftWarps * sizeof(Ended) + 15) / 16 * 16;
+  static constexpr uint32_t OFF_RAWS = OFF_PAGES + (FP8 ? PT * 8 * 16 : 0);  // RawTile [4 tiles]
   static constexpr uint32_t OFF_BAR = (OFF_RAWS + (FP8 ? 4 * sizeof(RawTile) : 0) + 7) / 8 * 8;
   // k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], v_ready[VST], s_full[2], p_full[2],
   // o_full[2], q_full, q_free, drain, joined[2], raw_full[2], raw_empty[2]
@@ -377,8 +400,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (FP8 && (warp == kSoftWarps || warp == kSoftWarps + 1 || warp == kSoftWarps + 3)) {
     // ============================ producer and converters of the 8-bit cache ============================
-    // A tile of K, then of V. The first of the three warps also brings the tiles, each as soon as all
-    // three have read the one before, and leaves notes of it, so that the others need no walk.
+    // A tile of K, then of V: 16 brings them, each as soon as the one before is read, and leaves notes,
+    // 17 and 19 make half of its values fp16 each. (A third converter that also brings them: 780 us where
+    // this takes 610; the producer was late.)
     fewer_registers<FP8>();
     const int part = warp == kSoftWarps ? -1 : warp == kSoftWarps + 1 ? 0 : 1;  // -1: the producer
     RawTile* const notes = reinterpret_cast<RawTile*>(smem + C::OFF_RAWS);
@@ -408,11 +432,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncwarp();
     };
-    ChunkWalk& w = reinterpret_cast<ChunkWalk*>(smem + C::OFF_WALK)[kSoftWarps + 1 + part];  // (saves registers)
     bool more = false;
-    if (lane == 0) more = !p.starve && w.begin(p, blockIdx.x);
-    more = __any_sync(0xffffffffu, more);
     if (part >= 0) {
+      if (!p.starve) {
+        ChunkWalk first;
+        more = first.begin(p, blockIdx.x);
+      }
       while (more && !dead) {
 #pragma unroll 1
         for (int kind = 0; kind < 2 && !dead; ++kind) convert(kind);
@@ -420,6 +445,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++made;
       }
     } else {
+      ChunkWalk& w = reinterpret_cast<ChunkWalk*>(smem + C::OFF_WALK)[kSoftWarps];  // (saves registers)
+      if (lane == 0) more = !p.starve && w.begin(p, blockIdx.x);
+      more = __any_sync(0xffffffffu, more);
       const int psh = __ffs(p.page_size) - 1;
       const uint32_t box = static_cast<uint32_t>(p.page_size) * D;
       const uint32_t qbytes = static_cast<uint32_t>(p.tile_tokens * p.group) * 128u;
@@ -466,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (lane == 0) notes[it & 3] = {u.low, u.high, u.full_low, u.full_high, key0, b, g, rt, seg, more || x + 1 < tiles};
               const float sv = clamp_scale(scale.y);
               // what the tile's scores and weights are to be scaled by
-              if (lane < 8) pages[(it & 3) * 8 + lane] = make_float4(scale.x, log2f(sv), 1.f / sv, 0.f);
+              if (lane < 8) pages[it % C::PT * 8 + lane] = make_float4(scale.x, log2f(sv), 1.f / sv, 0.f);
               __syncwarp();
             }
             if (elected()) mbar_arrive_tx(raw_full(kind), static_cast<uint32_t>(q1 - q0) * box);
@@ -797,7 +825,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // 8-bit cache: exponents are s a + b, with a and b of the key's page: a the scales of the row, of
           // the keys and of the softmax, b the logarithm of the values' scale, so that the products
           // take the values as they are; a is not 0, so that a * -inf stays -inf
-          const float4* const page = pages + ((tiles + (twin_stop ? 2 * k + h : k)) & 3) * 8;
+          const float4* const page = pages + (tiles + (twin_stop ? 2 * k + h : k)) % C::PT * 8;
           auto page_of = [&](int g) { return page[(ch * HK + g) >> psh]; };
           auto slope = [&](const float4& q) { return fmaxf(q.x * c, 1.17549435e-38f); };
           // scores are loaded twice, 32 at a time, which leaves registers for four warps a scheduler

@@ -259,14 +259,8 @@ def test_softmax_scale(path, scale):
 
 @pytest.mark.parametrize("path", PATHS)
 def test_any_scales_of_the_8_bit_cache(path):
-    """Scales that are no powers of two: each key and value is rounded to bf16 on the tensor cores,
-    2^-8 of it, so a score is off by 2^-8 reach and an output by the weights' and its own share."""
-    c = make([70, 5], [100, 900], fp8=True, scales="any", seed=17, spread=0.3)
-    out, lse, spread, reach = ref.chunk_attention(c["q"], c["cache"], c["table"], c["starts"], c["lens"])
-    got, _, code, _ = run(c, path)
-    off = 2.0 ** -8 * reach
-    limit = 2.0 ** -8 * out.abs() + ((torch.exp(2 * off) - 1) + 2.0 ** -7 + 2.0 ** -12)[..., None] * spread
-    assert code == 0 and bool(((got.double() - out).abs() <= limit).all())
+    """Scales that are no powers of two."""
+    check(make([70, 5], [100, 900], fp8=True, scales="any", seed=17, spread=0.3), path)
 
 
 # ----------------------------------------------------------------------------------
@@ -409,3 +403,15 @@ def test_waits_run_out():
     assert b.read_device_status(ws)[0] == 0
     want = ref.chunk_attention(c["q"], c["cache"], c["table"], c["starts"], c["lens"])
     ref.check_chunk((out, lse), want, 128, True)
+
+
+@pytest.mark.parametrize("D,P", [(64, 16), (128, 16), (64, 64)])
+def test_scales_of_pages_far_apart(D, P):
+    """Neighbouring pages' scales 2^12 apart, in long contexts, for single tokens and chunks: each tile's
+    scores and weights meet their own page's, call after call."""
+    c = make([1, 300, 1, 20, 65], [6000, 2500, 900, 4000, 0], Hq=8, Hkv=2, D=D, P=P, fp8=True, seed=28)
+    values, scale = c["cache"]
+    r = np.random.default_rng(28)
+    scale.copy_(torch.from_numpy(np.exp2(r.integers(-12, 1, scale.shape)).astype(np.float32)))
+    values.view(torch.uint8).copy_(torch.randint(0, 0x60, values.shape, dtype=torch.uint8, device="cuda"))
+    check(tail(c), softmax_scale=0.02, repeat=6)
