@@ -415,13 +415,22 @@ __device__ __forceinline__ int owner_of(long long t, long long total, int blocks
   return static_cast<int>(((t + 1) * blocks - 1) / total);
 }
 
-// A unit that ends in block c's first stop, having begun in an earlier block.
+// A unit that ends in block c's first stop, having begun in an earlier block. One that is computed again
+// is not joined: other blocks write its rows meanwhile.
 template <int D>
-__device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part) {
+__device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part, int redo) {
   ChunkWalk w;
   if (!w.begin(p, c) || w.starts_unit() || p.seq_bad[w.b] != 0) return;
   const ChunkUnit u = w.unit(p);
   if (!w.ends_unit(u)) return;
+  if (redo > 0) {
+    bool again = false;
+    for (int i = threadIdx.x; i < redo; i += kFinishThreads) {
+      const int4 e = __ldcg(&p.redo[1 + i]);
+      again |= e.x == w.b && e.y == w.g && e.z == w.rt;
+    }
+    if (__syncthreads_or(again)) return;
+  }
   const long long total = p.work->total;
   const int active = p.work->active;
   // the unit's first step, from this block's first virtual one
@@ -486,8 +495,8 @@ __global__ void __launch_bounds__(kFinishThreads) chunk_finish_kernel(ChunkParam
   __shared__ Smem<D, kRedoKeys> sm;
   pdl_wait_prior();
   if (p.blocks) {
-    if (blockIdx.x > 0 && static_cast<int>(blockIdx.x) < p.blocks) join_unit<D>(p, blockIdx.x, blockIdx.y);
     const int redo = min(__ldcg(&p.redo[0].x), p.redo_cap);
+    if (blockIdx.x > 0 && static_cast<int>(blockIdx.x) < p.blocks) join_unit<D>(p, blockIdx.x, blockIdx.y, redo);
     if (redo > 0) {
       const int tiles = (2 * p.tile_tokens * p.group + RT - 1) / RT;
       for (int64_t i = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x; i < static_cast<int64_t>(redo) * tiles;

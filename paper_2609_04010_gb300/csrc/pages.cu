@@ -287,7 +287,6 @@ struct CopyParams {
 
 template <typename T>
 __device__ __forceinline__ void copy_piece(char* base, int64_t src, int64_t dst, int64_t from, int64_t bytes) {
-  constexpr int N = 16 / sizeof(T) * kCopyLoads;
   const T* s = reinterpret_cast<const T*>(base + src + from);
   T* d = reinterpret_cast<T*>(base + dst + from);
   const int n = static_cast<int>(min(bytes - from, static_cast<int64_t>(kCopyChunk)) / static_cast<int64_t>(sizeof(T)));
@@ -300,7 +299,6 @@ __device__ __forceinline__ void copy_piece(char* base, int64_t src, int64_t dst,
     for (int i = 0; i < kCopyLoads; ++i)
       if (i0 + i * kCopyThreads < n) d[i0 + i * kCopyThreads] = x[i];
   }
-  (void)N;
 }
 
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyParams p) {

@@ -415,3 +415,19 @@ def test_scales_of_pages_far_apart(D, P):
     scale.copy_(torch.from_numpy(np.exp2(r.integers(-12, 1, scale.shape)).astype(np.float32)))
     values.view(torch.uint8).copy_(torch.randint(0, 0x60, values.shape, dtype=torch.uint8, device="cuda"))
     check(tail(c), softmax_scale=0.02, repeat=6)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new", [3, 64, 200])
+def test_hidden_values_in_units_that_blocks_share(fp8, new):
+    """A value that is not finite, seen by later tokens only, behind a context that many blocks share: the
+    unit is computed again, and its joined parts must not come over that."""
+    c = make([new], [30000], Hq=8, Hkv=2, D=128, P=16, fp8=fp8, seed=29, spread=0.3)
+    for at, h in ((30000 + new - 1, 0), (30000 + new // 2, 1)):
+        page, slot = int(c["table"][0, at // 16]), at % 16
+        if fp8:
+            c["cache"][0].view(torch.uint8)[page, h, 1, slot, 3] = 0x7f
+        else:
+            c["cache"][1][page, h, slot, 3] = float("nan")
+    for _ in range(6):
+        check(c, repeat=1)
