@@ -6,7 +6,7 @@
 // The CUDA-core kernel takes 16 query rows of one KV head and tiles of 64 keys, gathered through
 // the page table into shared memory in fp32; scores, running maximum and sum, and outputs are
 // fp32. It serves what the tensor-core kernel does not take and is a second implementation to
-// compare it with.
+// compare it with; long prompts, which take the tensor cores 458 us, take it 53 ms.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -34,11 +34,15 @@ struct Smem {
 
 // Lengths of the batch, once per call: which rows a sequence has and whether they can be served;
 // for the tensor cores also the work list, equal numbers of virtual steps per block. One block,
-// because all of it depends on sums over the batch.
+// because all of it depends on sums over the batch. What bounds it is latency: a chain of loads, two
+// scans and searches, 2 to 5 us that a short call sees in full. Of 14.7 us for one token behind 512 keys
+// the block of 1,024 threads took .5 more than the one of 128 that small calls get.
 constexpr int kSetupThreads = 1024;
+constexpr int kSetupFew = 128;    // threads for at most as many sequences and units
 constexpr int kSetupKept = 1024;  // sequences and units that are kept in shared memory too
 
-// The block's exclusive prefix sum of v in thread order, and the total.
+// The exclusive prefix sum of v in thread order over a block of THREADS threads, and the total.
+template <int THREADS>
 __device__ __forceinline__ long long scan_block(long long v, long long* sh, long long* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long x = v;
@@ -49,7 +53,7 @@ __device__ __forceinline__ long long scan_block(long long v, long long* sh, long
   }
   if (lane == 31) sh[warp] = x;
   __syncthreads();
-  long long w = sh[lane];  // kSetupThreads / 32 == 32 warps
+  long long w = lane < THREADS / 32 ? sh[lane] : 0;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long y = __shfl_up_sync(0xffffffffu, w, o);
@@ -100,13 +104,12 @@ __device__ __forceinline__ void halve_queries(const ChunkParams& p, int64_t warp
 }
 
 // D: 0, or the head dimension where query rows are to be made fp16, by all blocks but the first.
-template <int D>
-__global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams p) {
+template <int D, int THREADS>
+__global__ void __launch_bounds__(THREADS) chunk_setup_kernel(ChunkParams p) {
   if constexpr (D > 0) {
     if (blockIdx.x > 0) {
       pdl_wait_prior();
-      halve_queries<D>(p, (blockIdx.x - 1) * (kSetupThreads / 32) + (threadIdx.x >> 5),
-                       static_cast<int64_t>(gridDim.x - 1) * (kSetupThreads / 32));
+      halve_queries<D>(p, (blockIdx.x - 1) * (THREADS / 32) + (threadIdx.x >> 5), static_cast<int64_t>(gridDim.x - 1) * (THREADS / 32));
       return;
     }
   }
@@ -116,7 +119,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
   pdl_wait_prior();
   const int tid = threadIdx.x;
   long long carry = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kSetupThreads) {
+  for (int b0 = 0; b0 < p.batch; b0 += THREADS) {
     const int b = b0 + tid;
     ChunkSeq s = {0, 0, 0, 0};
     bool bad = false;
@@ -135,7 +138,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
     }
     const int units = p.blocks ? chunk_units(p, s.n) : 0;
     long long all;
-    const long long before = carry + scan_block(units, sh, &all);
+    const long long before = carry + scan_block<THREADS>(units, sh, &all);
     carry += all;
     if (b < p.batch) {
       // (rows that sequences share, out of order, could make more units than there is room for)
@@ -164,7 +167,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
   auto first = [&](int b) { return seqs[b].first_unit; };
   const long long* cum = nunits <= kSetupKept ? cum_kept : p.cum;
   carry = 0;
-  for (int u0 = 0; u0 < nunits; u0 += kSetupThreads) {
+  for (int u0 = 0; u0 < nunits; u0 += THREADS) {
     const int u = u0 + tid;
     int steps = 0;
     if (u < nunits) {
@@ -177,7 +180,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
       if (u - s.first_unit < chunk_units(p, s.n)) steps = chunk_unit(p, s, u - s.first_unit).length();
     }
     long long all;
-    const long long before = carry + scan_block(steps, sh, &all);
+    const long long before = carry + scan_block<THREADS>(steps, sh, &all);
     carry += all;
     if (u < nunits) {
       p.cum[u + 1] = before + steps;
@@ -191,7 +194,7 @@ __global__ void __launch_bounds__(kSetupThreads) chunk_setup_kernel(ChunkParams 
     p.work->total = total;
     p.work->active = active;
   }
-  for (int c = tid; c < p.blocks; c += kSetupThreads) {
+  for (int c = tid; c < p.blocks; c += THREADS) {
     if (c >= active) {
       p.work->starts[c] = {0, 0, 0, 0, 0, 0, 0, 0};
       continue;
@@ -405,7 +408,9 @@ __global__ void __launch_bounds__(NT) chunk_simt_kernel(ChunkParams p) {
 
 // The end of a call: joins the parts of units that blocks split, computes again the units in
 // which a hidden value was not finite (on CUDA cores, 16 keys at a time so that the shared memory
-// of a block is small), and clears the rows of sequences that could not be served.
+// of a block is small), and clears the rows of sequences that could not be served. A block splits
+// two units at most, so the parts, twice 128 KB of fp32 per block, are a few us of L2 traffic, spread
+// over eight blocks for each joined unit.
 constexpr int kFinishThreads = NT;
 constexpr int kFinishParts = 8;  // blocks per joined unit
 constexpr int kRedoKeys = 16;
@@ -537,6 +542,16 @@ cudaError_t launch_finish_d(const ChunkParams& p, cudaStream_t stream) {
   return launch_overlapped(chunk_finish_kernel<D, FP8>, grid, kFinishThreads, 0, stream, p);
 }
 
+template <int THREADS>
+cudaError_t launch_setup(const spec_chunk_attn_args_t& a, const ChunkPlan& P, const ChunkParams& p, cudaStream_t stream) {
+  if (!p.blocks || !P.fp8) return launch_overlapped(chunk_setup_kernel<0, THREADS>, dim3(1), THREADS, 0, stream, p);
+  const int64_t heads = static_cast<int64_t>(a.rows) * a.num_q_heads;
+  const int each = THREADS / (a.head_dim / 8), most = 2 * P.grid * (kSetupThreads / THREADS);  // as many fit the SMs
+  const int extra = static_cast<int>(heads / each < most ? (heads + each - 1) / each : most);
+  return launch_overlapped(a.head_dim == 128 ? chunk_setup_kernel<128, THREADS> : chunk_setup_kernel<64, THREADS>,
+                           dim3(1 + extra), THREADS, 0, stream, p);
+}
+
 ChunkParams make_chunk_params(const spec_chunk_attn_args_t& a, const ChunkPlan& P, char* ws) {
   ChunkParams p{};
   p.batch = a.batch;
@@ -588,15 +603,8 @@ cudaError_t launch_chunk(const spec_chunk_attn_args_t& a, const ChunkPlan& P, ch
   ChunkParams p = make_chunk_params(a, P, ws);
   p.starve = starve ? 1 : 0;
   const bool wide = a.head_dim == 128;
-  cudaError_t e;
-  if (p.blocks && P.fp8) {
-    const int64_t heads = static_cast<int64_t>(a.rows) * a.num_q_heads;
-    const int each = kSetupThreads / (a.head_dim / 8), most = 2 * P.grid;  // two such blocks fit an SM
-    const int extra = static_cast<int>(heads / each < most ? (heads + each - 1) / each : most);
-    e = launch_overlapped(wide ? chunk_setup_kernel<128> : chunk_setup_kernel<64>, dim3(1 + extra), kSetupThreads, 0, stream, p);
-  } else {
-    e = launch_overlapped(chunk_setup_kernel<0>, dim3(1), kSetupThreads, 0, stream, p);
-  }
+  cudaError_t e = a.batch <= kSetupFew && (!p.blocks || p.max_units <= kSetupFew) ? launch_setup<kSetupFew>(a, P, p, stream)
+                                                                                : launch_setup<kSetupThreads>(a, P, p, stream);
   if (e != cudaSuccess) return e;
   if (p.blocks) e = launch_chunk_tc(a, p, stream);
   else if (P.fp8) e = wide ? launch_simt_d<128, true>(p, stream) : launch_simt_d<64, true>(p, stream);

@@ -273,6 +273,9 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
 // ---------------------------------------------------------------------------------
 // Copies
 // ---------------------------------------------------------------------------------
+// Blocks: (pair, buffer, piece of 16 KB), four loads in flight per thread before the stores. Bound by
+// memory: 64 pairs in 64 buffers of 32 KB pages, 268 MB, take 37 us, 7.2 TB/s, because sources of several
+// pairs are read from L2; eight pages of one layer take 1.6 us in a graph, a launch.
 constexpr int kCopyThreads = 256;
 constexpr int kCopyLoads = 4;  // 16-byte loads in flight per thread
 constexpr int kCopyChunk = kCopyThreads * kCopyLoads * 16;
