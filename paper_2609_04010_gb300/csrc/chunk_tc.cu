@@ -302,17 +302,20 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned 
     full_high = t.full_high - t.key0;
   }
   const bool partial = full_low > 0 || full_high < TK;
-  constexpr int kRounds = kItems / 32;  // 32 items a round
+  // Lane l of a round takes piece l % kPieces of key l / kPieces, the upper half of a row's pieces of the
+  // neighbour key: the 16-byte places of 8 lanes then lie in different banks in both stores.
+  const int piece = lane % kPieces, key_of = (lane / kPieces) ^ (piece >> 2);
+  constexpr int kRounds = kItems / 32, kKeys = 32 / kPieces;  // 32 items a round
   const int from = part * (kRounds / 2), to = from + kRounds / 2;
 #pragma unroll 1
   for (int r = from; r < to; r += kLoads) {
     uint4 v[kLoads];
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) v[k] = *reinterpret_cast<const uint4*>(raw + ((r + k) * 32 + lane) * 16);
+    for (int k = 0; k < kLoads; ++k) v[k] = *reinterpret_cast<const uint4*>(raw + ((r + k) * kKeys + key_of) * D + piece * 16);
     if (VALUES && partial) {
 #pragma unroll
       for (int k = 0; k < kLoads; ++k) {
-        const int key = ((r + k) * 32 + lane) / kPieces;
+        const int key = (r + k) * kKeys + key_of;
         if (key < low || key >= high) v[k] = make_uint4(0, 0, 0, 0);
         if (key < full_low || key >= full_high)
           odd |= (__vcmpeq4(v[k].x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v[k].y & 0x7f7f7f7fu, 0x7f7f7f7fu) |
@@ -321,7 +324,7 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned 
     }
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
-      const int item = (r + k) * 32 + lane, key = item / kPieces, j = item % kPieces;
+      const int key = (r + k) * kKeys + key_of;
       const uint32_t in[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
       uint32_t o[8];
 #pragma unroll
@@ -329,8 +332,8 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned 
         o[2 * e] = e4m3x2_to_f16x2(in[e] & 0xffffu);
         o[2 * e + 1] = e4m3x2_to_f16x2(in[e] >> 16);
       }
-      unsigned char* row = tile + (key >> 3) * Cfg<D, true>::GROUP + (j >> 2) * 1024 + (key & 7) * 128;
-      const int p0 = 2 * (j & 3), x = key & 7;
+      unsigned char* row = tile + (key >> 3) * Cfg<D, true>::GROUP + (piece >> 2) * 1024 + (key & 7) * 128;
+      const int p0 = 2 * (piece & 3), x = key & 7;
       *reinterpret_cast<uint4*>(row + ((p0 ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<uint4*>(row + (((p0 + 1) ^ x) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
     }
