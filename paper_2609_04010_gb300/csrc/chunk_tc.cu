@@ -34,8 +34,8 @@
 // products' own time and the turns between them. Whole prompts (4 x 4,093): 458 us, 1,200 TFLOP/s: a unit
 // of 64 tokens has 17 steps on average, and its outputs and first weights, about 4 steps of time, are
 // not hidden. Single tokens (32 requests to 16,384 tokens): 200 us, 5.5 TB/s, 0.81 of the copy rate: a
-// step's five tiles in flight. 8-bit, two chunks of 2,048 tokens: 610 us, 1,000 TFLOP/s:
-// two warps make 32,768 values fp16 a step.
+// step's five tiles in flight. 8-bit, two chunks of 2,048 tokens: 522 us, 1,180 TFLOP/s:
+// two warps make 32,768 values fp16 a step, in shared memory that the products read most of the time.
 // What was measured on the way (long chunk): one softmax thread per row 1,697 us (eight warps cannot
 // hide each other's waits); two product warps in turns 1,446; products issued by "lane == 0" instead of
 // an elected lane 1,404; registers spilled in any role's loop 1,800 to 2,900, because next to 226 KB of
@@ -303,7 +303,7 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, unsigned 
   }
   const bool partial = full_low > 0 || full_high < TK;
   // Lane l of a round takes piece l % kPieces of key l / kPieces, the upper half of a row's pieces of the
-  // neighbour key: the 16-byte places of 8 lanes then lie in different banks in both stores.
+  // neighbour key: the 16-byte places of 8 lanes then lie in different banks in both stores (522 us; 610 without).
   const int piece = lane % kPieces, key_of = (lane / kPieces) ^ (piece >> 2);
   constexpr int kRounds = kItems / 32, kKeys = 32 / kPieces;  // 32 items a round
   const int from = part * (kRounds / 2), to = from + kRounds / 2;
@@ -404,8 +404,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (FP8 && (warp == kSoftWarps || warp == kSoftWarps + 1 || warp == kSoftWarps + 3)) {
     // ============================ producer and converters of the 8-bit cache ============================
     // A tile of K, then of V: 16 brings them, each as soon as the one before is read, and leaves notes,
-    // 17 and 19 make half of its values fp16 each. (A third converter that also brings them: 780 us where
-    // this takes 610; the producer was late.)
+    // 17 and 19 make half of its values fp16 each: 522 us for two chunks of 2,048 tokens. A third converter
+    // leaves the softmax 80 registers (536); one that also brings the tiles is late with them (780 where two
+    // took 610).
     fewer_registers<FP8>();
     const int part = warp == kSoftWarps ? -1 : warp == kSoftWarps + 1 ? 0 : 1;  // -1: the producer
     RawTile* const notes = reinterpret_cast<RawTile*>(smem + C::OFF_RAWS);
