@@ -770,8 +770,8 @@ spec_status_t spec_rope_kv(const spec_rope_args_t* rope, spec_stream_t stream);
  *     their product rounded to bf16, off by at most 2^-8 of themselves. With the 8-bit cache they
  *     enter as fp16 times their page's value scale, off by 2^-11 of that product or 2^-33 of the
  *     row's largest; its values enter exactly, and queries as fp16 times a power of two of their
- *     row: elements below 2^-31 of its largest are off by at most 2^-39 of that. Scales
- *     need not be powers of two; value scales are clamped to [2^-32, 2^32].
+ *     row: elements below 2^-31 of its largest are off by at most 2^-39 of that. Scales are finite and
+ *     not negative, of any fraction; value scales are clamped to [2^-32, 2^32].
  *   - path: SPEC_ATTN_AUTO takes the tensor cores where the call fits them (Hq / Hkv at most 128),
  *     else CUDA cores; SPEC_ATTN_TENSOR_CORES is SPEC_ERR_UNSUPPORTED where it does not fit.
  *   - Three launches. The workspace rules are spec_verify_attention's; it holds the parts of

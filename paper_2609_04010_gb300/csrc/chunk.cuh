@@ -34,7 +34,10 @@ constexpr int kChunkTileRows = 128;    // query rows of an M tile
 // 3 they take 778, with a twin's step at 2 and a start at 4, 745.
 constexpr int kChunkCost = 3, kChunkTwinCost = 4;
 constexpr int kChunkStart = 12, kChunkTwinStart = 10;
-constexpr int kChunkShortest = kChunkStart < kChunkTwinStart ? kChunkStart : kChunkTwinStart;
+// 8-bit cache: a tile takes its conversion's time whichever unit it is for, so a twin's step takes twice
+// another's, and starts weigh half as much.
+constexpr int kChunkCost8 = 2;
+constexpr int kChunkStart8 = 6, kChunkTwinStart8 = 5;
 
 // One sequence of the batch, as the setup leaves it.
 struct ChunkSeq {
@@ -109,12 +112,17 @@ struct ChunkUnit {
   int low, high;       // keys that any of them sees
   int full_low, full_high;  // keys that all of them see
   int tile0, tiles, steps;
-  bool twin;
-  __device__ __forceinline__ int start() const { return twin ? kChunkTwinStart : kChunkStart; }
-  __device__ __forceinline__ int cost() const { return twin ? kChunkTwinCost : kChunkCost; }
-  __device__ __forceinline__ int length() const { return start() + steps * cost(); }
+  bool twin, eight;  // of the 8-bit cache
+  __device__ __forceinline__ int start() const {
+    return eight ? (twin ? kChunkTwinStart8 : kChunkStart8) : (twin ? kChunkTwinStart : kChunkStart);
+  }
+  __device__ __forceinline__ int length() const { return start() + steps * (twin ? kChunkTwinCost : eight ? kChunkCost8 : kChunkCost); }
   // the first step that begins at or after virtual step v of the unit
-  __device__ __forceinline__ int step_at(int v) const { return (max(v - start(), 0) + cost() - 1) / cost(); }
+  __device__ __forceinline__ int step_at(int v) const {
+    const int x = max(v - start(), 0);
+    return twin ? (x + kChunkTwinCost - 1) / kChunkTwinCost
+                : eight ? (x + kChunkCost8 - 1) / kChunkCost8 : (x + kChunkCost - 1) / kChunkCost;
+  }
   __device__ __forceinline__ int step_tiles(int i, int h) const { return twin ? 2 * i + h : i; }
   __device__ __forceinline__ bool has(int i, int h) const { return !twin || 2 * i + h < tiles; }
 };
@@ -126,6 +134,7 @@ __device__ __forceinline__ ChunkUnit chunk_unit(const ChunkParams& p, const Chun
   u.token0 = rt * 2 * p.tile_tokens;
   u.tokens = min(2 * p.tile_tokens, s.n - u.token0);
   u.twin = u.tokens <= p.tile_tokens;
+  u.eight = p.kv_scale != nullptr;
   const int at0 = s.kv_len - s.n + u.token0, at1 = at0 + u.tokens - 1;
   u.low = chunk_low(p, at0);
   u.full_low = chunk_low(p, at1);
@@ -176,7 +185,8 @@ struct ChunkWalk {
     return ns > 0 || next(p);
   }
   __device__ __forceinline__ bool next(const ChunkParams& p) {
-    if (left <= kChunkShortest) return false;  // nothing, or no more than a unit's start
+    // nothing, or no more than a unit's start
+    if (left <= (p.kv_scale ? min(kChunkStart8, kChunkTwinStart8) : min(kChunkStart, kChunkTwinStart))) return false;
     if (++rt == chunk_units(p, n)) {
       rt = 0;
       if (++g == p.hkv) {
