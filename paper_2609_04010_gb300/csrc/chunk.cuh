@@ -35,7 +35,7 @@ constexpr int kChunkTileRows = 128;    // query rows of an M tile
 constexpr int kChunkCost = 3, kChunkTwinCost = 4;
 constexpr int kChunkStart = 12, kChunkTwinStart = 10;
 // 8-bit cache: a tile takes its conversion's time whichever unit it is for, so a twin's step takes twice
-// another's, and starts weigh half as much.
+// another's, and starts weigh half as much: that batch 967 us, with the weights above 987.
 constexpr int kChunkCost8 = 2;
 constexpr int kChunkStart8 = 6, kChunkTwinStart8 = 5;
 

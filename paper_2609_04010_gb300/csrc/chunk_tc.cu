@@ -35,7 +35,8 @@
 // of 64 tokens has 17 steps on average, and its outputs and first weights, about 4 steps of time, are
 // not hidden. Single tokens (32 requests to 16,384 tokens): 200 us, 5.5 TB/s, 0.81 of the copy rate: a
 // step's five tiles in flight. 8-bit, two chunks of 2,048 tokens: 522 us, 1,180 TFLOP/s:
-// two warps make 32,768 values fp16 a step, in shared memory that the products read most of the time.
+// two warps make 32,768 values fp16 a step, 2,570 of its 3,860 cycles, in shared memory that the products
+// read most of the time.
 // What was measured on the way (long chunk): one softmax thread per row 1,697 us (eight warps cannot
 // hide each other's waits); two product warps in turns 1,446; products issued by "lane == 0" instead of
 // an elected lane 1,404; registers spilled in any role's loop 1,800 to 2,900, because next to 226 KB of
@@ -456,7 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t box = static_cast<uint32_t>(p.page_size) * D;
       const uint32_t qbytes = static_cast<uint32_t>(p.tile_tokens * p.group) * 128u;
       float4* const pages = reinterpret_cast<float4*>(smem + C::OFF_PAGES);
-      uint32_t it = 0, seg = 0, joins = 0, twins = 0;  // tiles brought, stops; twins joined, of all whole ones so far
+      uint32_t it = 0, copies = 0, seg = 0;  // tiles, and K or V of a tile, brought; stops
+      uint32_t joins = 0, twins = 0;         // twins joined, of all whole ones so far
       bool was_twin = false;
       while (more && !dead) {
         __syncwarp();
@@ -505,6 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             if (lane >= q0 && lane < q1)
               tma_load_raw(sbase + C::OFF_RAW + kind * C::RAW + static_cast<uint32_t>(lane) * box, &map_k, at + kind, raw_full(kind));
+            ++copies;
           }
           if (dead) break;
           ++it;
@@ -535,11 +538,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         twins += whole_twin ? 1 : 0;
         ++seg;
       }
-      if (dead && it > 0) {  // copies still in flight (bounded)
+      if (dead && copies > 0) {  // copies still in flight (bounded)
         const long long c0 = clock64();
-        for (int kind = 0; kind < 2; ++kind)
-          while (!mbar_try(raw_full(kind), (it - 1) & 1) && clock64() - c0 < kWaitCycles) {
+        for (uint32_t kind = 0; kind < 2; ++kind) {
+          const uint32_t n = (copies + 1 - kind) / 2;
+          while (n > 0 && !mbar_try(raw_full(kind), (n - 1) & 1) && clock64() - c0 < kWaitCycles) {
           }
+        }
         while (seg > 0 && !mbar_try(q_full, (seg - 1) & 1) && clock64() - c0 < kWaitCycles) {
         }
       }
