@@ -35,9 +35,10 @@ constexpr int kChunkTileRows = 128;    // query rows of an M tile
 constexpr int kChunkCost = 3, kChunkTwinCost = 4;
 constexpr int kChunkStart = 12, kChunkTwinStart = 10;
 // 8-bit cache: a tile takes its conversion's time whichever unit it is for, so a twin's step takes twice
-// another's, and starts weigh half as much: that batch 967 us, with the weights above 987.
+// another's, and starts weigh a third as much: that batch 964 us, with the weights above 987; four whole
+// prompts 586, with starts of 6 and 5 595, of 12 and 8 615.
 constexpr int kChunkCost8 = 2;
-constexpr int kChunkStart8 = 6, kChunkTwinStart8 = 5;
+constexpr int kChunkStart8 = 4, kChunkTwinStart8 = 3;
 
 // One sequence of the batch, as the setup leaves it.
 struct ChunkSeq {
