@@ -9,6 +9,8 @@ exist (``python -m paper_2609_04010_gb300.build``); there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import math
 import os
 import re
@@ -324,6 +326,29 @@ def _stream(stream=None):
         return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
+
+
+def _on_its_stream(f):
+    """A call that is given a `stream` makes its outputs and its workspace there: they are filled
+    before the launch, and a workspace that the call drops is given out again only behind it. What
+    it returns is kept for the work that the caller's current stream has queued on it."""
+    at = list(inspect.signature(f).parameters).index("stream")
+
+    @functools.wraps(f)
+    def call(*args, **kwargs):
+        stream = args[at] if len(args) > at else kwargs.get("stream")
+        if stream is None:
+            return f(*args, **kwargs)
+        here = torch.cuda.current_stream(stream.device)
+        with torch.cuda.stream(stream):
+            made = f(*args, **kwargs)
+        if here != stream:
+            tensors = made.values() if isinstance(made, dict) else made if isinstance(made, tuple) else (made,)
+            for t in tensors:
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(here)
+        return made
+    return call
 
 
 def _check(t: torch.Tensor, name: str, dtype, shape=None):
@@ -1029,7 +1054,8 @@ def adjust_logits(logits, block_tokens=None, history=None, history_len=None, pro
 # Ragged batches: rotary positions, attention of chunks, forked sequences, page copies
 # ----------------------------------------------------------------------------------
 # These argument structures keep their tensors alive (`keep`) and the device they are on
-# (`device`), whose current stream is the default one of a call.
+# (`device`), whose current stream is the default one of a call. On another stream a call uses what
+# the caller has made ready there.
 def _own(a, tensors):
     tensors = [t for t in tensors if t is not None]
     devices = {t.device for t in tensors}
@@ -1047,8 +1073,11 @@ def _call(name: str, a, stream, ws=None):
         args = (ctypes.byref(a), _ptr(ws), ws.numel())
     else:
         args = (ctypes.byref(a),)
-    if stream is not None and stream.device != a.device:
-        raise ValueError(f"the stream is on {stream.device}, the tensors on {a.device}")
+    if stream is not None:
+        if stream.device != a.device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {a.device}")
+        for t in a.keep if ws is None else (*a.keep, ws):
+            t.record_stream(stream)  # the caller may drop it before the work there is done
     if a.device.index == torch.cuda.current_device():
         _raise(f(*args, _stream(stream)), name)
     else:
@@ -1181,6 +1210,7 @@ def rope_kv_args(a: RopeArgs, stream=None):
     _call("spec_rope_kv", a, stream)
 
 
+@_on_its_stream
 def rope_kv(q, k, v, positions, turns, slots=None, k_cache=None, v_cache=None,
             interleaved: bool = False, factor: float = 1.0, in_place: bool = False, status_ws=None,
             stream=None):
@@ -1246,6 +1276,7 @@ def test_chunk_attention_wait_timeout_args(a: ChunkAttnArgs, ws: torch.Tensor, s
     _call("spec_test_chunk_attention_wait_timeout", a, stream, ws)
 
 
+@_on_its_stream
 def chunk_attention(q, cache, page_table, row_start, kv_len, softmax_scale=0.0, path=ATTN_AUTO,
                     causal: bool = True, window: int = 0, want_lse: bool = True, ws=None, stream=None):
     """Attention of a packed ragged batch q [rows][Hq][D] over a paged cache (spec_chunk_attention):
@@ -1296,6 +1327,7 @@ def fork_sequences_args(a: ForkArgs, ws: torch.Tensor, stream=None):
     _call("spec_fork_sequences", a, stream, ws)
 
 
+@_on_its_stream
 def fork_sequences(parent, kv_len, page_table, shares, free_pages, free_count, page_size: int,
                    reserved: int = 0, ws=None, stream=None) -> Dict[str, torch.Tensor]:
     """Each sequence goes on from sequence parent[b] (spec_fork_sequences; -1: ends). kv_len,
