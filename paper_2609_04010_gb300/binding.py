@@ -453,6 +453,7 @@ def verify_step_args(attn: Optional[AttnArgs], acc: Optional[AcceptArgs], ws: to
                                   ws.numel(), _stream(stream)), "spec_verify_step")
 
 
+@_on_its_stream
 def verify_attention(q, k_cache, v_cache, page_table, kv_len, softmax_scale=0.0, path=ATTN_AUTO,
                      want_lse=True, ws=None, stream=None, tree_mask=None):
     """Block-causal (or, with tree_mask, tree) paged GQA verify attention. Returns
@@ -466,6 +467,7 @@ def verify_attention(q, k_cache, v_cache, page_table, kv_len, softmax_scale=0.0,
     return out, lse
 
 
+@_on_its_stream
 def accept_block(target_logits, drafter_logits, block_tokens, temperature, uniforms,
                  want_diag=True, ws=None, stream=None) -> Dict[str, torch.Tensor]:
     """Lossless acceptance over a batch. Returns num_accepted, out_tokens, num_emitted, diag."""
@@ -527,6 +529,7 @@ def accept_block_filtered_args(acc: AcceptArgs, filt: FilterArgs, ws: torch.Tens
            "spec_accept_block_filtered")
 
 
+@_on_its_stream
 def accept_block_filtered(target_logits, drafter_logits, block_tokens, temperature, top_k, top_p,
                           uniforms, max_top_k: Optional[int] = None, want_diag=True, ws=None,
                           stream=None) -> Dict[str, torch.Tensor]:
@@ -580,6 +583,7 @@ def sample_block_args(d: DraftArgs, filt: Optional[FilterArgs], ws: torch.Tensor
                                    _ptr(ws), ws.numel(), _stream(stream)), "spec_sample_block")
 
 
+@_on_its_stream
 def sample_block(drafter_logits, temperature, uniforms, top_k=None, top_p=None, max_top_k=None,
                  ws=None, stream=None) -> Dict[str, torch.Tensor]:
     """Draft-side sampling of every block token from its drafter row (x^{L+1} ~ q_0,
@@ -596,6 +600,7 @@ def sample_block(drafter_logits, temperature, uniforms, top_k=None, top_p=None, 
     return res
 
 
+@_on_its_stream
 def noise_tokens(seed: int, n: int, vocab: int, offset: int = 0, device=None,
                  stream=None) -> torch.Tensor:
     """The uniform noise tokens z ~ U[V] that start a draft pass (Alg. line 1)."""
@@ -662,6 +667,7 @@ def accept_tree_args(t: TreeAcceptArgs, ws: torch.Tensor, stream=None):
            "spec_accept_tree")
 
 
+@_on_its_stream
 def accept_tree(target_logits, tokens, parents, ws=None, stream=None, temperature=None,
                 uniforms=None) -> Dict[str, torch.Tensor]:
     """Verification of a candidate tree (spec_accept_tree): greedy, or sampled for the
@@ -737,6 +743,7 @@ def build_tree_args(t: TreeBuildArgs, ws: torch.Tensor, stream=None):
            "spec_build_tree")
 
 
+@_on_its_stream
 def build_tree(drafter_logits, temperature, root_tokens, top_k: int, num_nodes: int, ws=None,
                stream=None) -> Dict[str, torch.Tensor]:
     """The tree sampler (spec_build_tree). Returns tokens, parents, depth and mask
@@ -797,6 +804,7 @@ def test_lm_head_wait_timeout_args(a: LmHeadArgs, ws: torch.Tensor, stream=None)
                                                 _stream(stream)), "spec_test_lm_head_wait_timeout")
 
 
+@_on_its_stream
 def lm_head_stats(hidden_states, weight, temperature, rows_per_seq: int, tokens=None,
                   want_logits: bool = False, ws=None, stream=None) -> Dict[str, torch.Tensor]:
     """spec_lm_head_stats: the LM head's logits reduced per row (max, sum of
@@ -865,6 +873,7 @@ def map_slots_args(a: SlotArgs, ws: torch.Tensor, stream=None):
            "spec_map_slots")
 
 
+@_on_its_stream
 def map_slots(num_new, kv_len, page_table, page_size: int, num_pages: int, free_pages, free_count,
               max_rows: int, reserved: int = 0, ws=None, stream=None) -> Dict[str, torch.Tensor]:
     """Pages and cache slots for num_new[b] more tokens of each sequence (spec_map_slots).
@@ -971,6 +980,7 @@ def test_attention_fp8_wait_timeout_args(a: AttnFp8Args, ws: torch.Tensor, strea
            "spec_test_attention_fp8_wait_timeout")
 
 
+@_on_its_stream
 def verify_attention_fp8(q, kv_cache, kv_scale, page_table, kv_len, softmax_scale=0.0,
                          path=ATTN_AUTO, want_lse=True, ws=None, stream=None, tree_mask=None):
     """verify_attention over the 8-bit cache (spec_verify_attention_fp8). Returns
@@ -1035,6 +1045,7 @@ def adjust_logits_args(a: AdjustArgs, stream=None):
     _raise(lib().spec_adjust_logits(ctypes.byref(a), _stream(stream)), "spec_adjust_logits")
 
 
+@_on_its_stream
 def adjust_logits(logits, block_tokens=None, history=None, history_len=None, prompt_len=None,
                   repetition=None, frequency=None, presence=None, bias_tokens=None,
                   bias_values=None, allowed=None, block_shift: int = 0, out=None,
@@ -1376,6 +1387,7 @@ def copy_pages(pairs, buffers, status_ws=None, stream=None):
         copy_pages_args(copy_args(pairs, buffers[i:i + COPY_MAX_BUFFERS], status_ws), stream)
 
 
+@_on_its_stream
 def philox_uniforms(seed: int, n: int, offset: int = 0, device=None, stream=None) -> torch.Tensor:
     out = torch.empty(n, dtype=torch.float32, device=device or "cuda")
     _raise(lib().spec_philox_uniforms(ctypes.c_uint64(seed), ctypes.c_uint64(offset), n,

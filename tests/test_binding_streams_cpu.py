@@ -105,3 +105,46 @@ def test_what_a_call_is_given_is_kept_for_its_stream(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: None)
     b.chunk_attention_args(a, ws, other)
     assert all(t.used_on == (other,) for t in (*a.keep, ws))
+
+
+def f32(*shape):
+    return torch.zeros(shape).as_subclass(OnGpu)
+
+
+def e4m3(*shape):
+    return torch.zeros(shape, dtype=torch.uint8).view(torch.float8_e4m3fn).as_subclass(OnGpu)
+
+
+EARLIER = {
+    "verify_attention": lambda: (bf16(2, 3, 4, 64), bf16(7, 2, 16, 64), bf16(7, 2, 16, 64), i32(2, 3), i32(2)),
+    "verify_attention_fp8": lambda: (bf16(2, 3, 4, 64), e4m3(7, 2, 2, 16, 64), f32(7, 2, 2), i32(2, 3), i32(2)),
+    "accept_block": lambda: (f32(2, 3, 50), f32(2, 3, 50), i32(2, 3), f32(2), f32(2, 3)),
+    "accept_block_filtered": lambda: (f32(2, 3, 50), f32(2, 3, 50), i32(2, 3), f32(2), i32(2), f32(2), f32(2, 3), 8),
+    "sample_block": lambda: (f32(2, 3, 50), f32(2), f32(2, 3)),
+    "accept_tree": lambda: (f32(2, 3, 50), i32(2, 3), i32(2, 3)),
+    "build_tree": lambda: (f32(2, 3, 50), f32(2), i32(2), 2, 5),
+    "lm_head_stats": lambda: (bf16(6, 64), bf16(256, 64), f32(2), 3),
+    "map_slots": lambda: (i32(2), i32(2), i32(2, 3), 16, 7, i32(7), i32(1), 6),
+    "adjust_logits": lambda: (f32(2, 3, 50),),
+    "noise_tokens": lambda: (0, 5, 50),
+    "philox_uniforms": lambda: (0, 5),
+}
+
+
+@pytest.mark.parametrize("name", sorted(EARLIER))
+def test_the_other_calls_too(watched, name):
+    caller, other, made, launched = watched
+    given = EARLIER[name]()
+    made.clear()
+    launched.clear()
+    getattr(b, name)(*given, stream=other)
+    assert launched and made and all(s is other for _, s in made)
+
+
+def test_every_call_that_allocates_is_covered():
+    import inspect
+    with_stream = {n for n, f in inspect.getmembers(b, inspect.isfunction)
+                   if f.__module__ == b.__name__ and "stream" in inspect.signature(f).parameters
+                   and not n.startswith("_") and not n.endswith("_args")}
+    made_nothing = {"accept_block_noalloc", "append_kv_fp8", "commit_kv", "commit_tree_kv", "copy_pages", "read_device_status"}
+    assert with_stream - made_nothing == set(EARLIER) | {"rope_kv", "chunk_attention", "fork_sequences"}

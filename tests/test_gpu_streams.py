@@ -73,3 +73,26 @@ def test_fork():
                                stream=stream)
         return [*t.values(), res["copies"], res["flags"]]
     check(call)
+
+
+def test_verify_attention():
+    """Its workspace holds counters, which are zeros when the launch begins."""
+    from paper_2609_04010_gb300 import binding as b
+    c = make([16, 16], [5000, 900], Hq=8, Hkv=2, seed=34)
+    q = c["q"].reshape(2, 16, 8, 128).contiguous()
+    lens = i32(c["lens"])
+    check(lambda stream: list(b.verify_attention(q, *c["cache"], c["table"].clamp_min(0), lens, stream=stream)))
+
+
+def test_map_slots():
+    from paper_2609_04010_gb300 import binding as b
+    n = 200
+    new = i32(np.arange(n) % 7)
+    first = dict(kv_len=i32(np.arange(n) * 3), table=i32(np.full((n, 60), -1)), free=i32(np.arange(5000)), count=i32([5000]))
+
+    def call(stream):
+        with torch.cuda.stream(stream):
+            t = {k: v.clone() for k, v in first.items()}
+        res = b.map_slots(new, t["kv_len"], t["table"], 16, 5000, t["free"], t["count"], 700, stream=stream)
+        return [*t.values(), *res.values()]
+    check(call)
