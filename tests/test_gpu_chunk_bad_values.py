@@ -1,0 +1,59 @@
+"""NaN among keys, values and queries of attention of chunks: what a row's mask hides does not reach it,
+however many units hold such values; what a row sees does, however small its weight is and wherever
+the work is cut."""
+
+import pytest
+import torch
+
+import chunk_reference as ref
+from test_gpu_chunk import make, run
+
+pytestmark = pytest.mark.gpu
+AUTO, CUDA_CORES = 0, 1
+
+
+def spoil(c, kind, b, at, heads=slice(None), dims=slice(None)):
+    """Keys (0) or values (1) of sequence b at token `at` become NaN."""
+    P = c["cache"][0].shape[3 if c["fp8"] else 2]
+    page = int(c["table"][b, at // P])
+    if c["fp8"]:
+        c["cache"][0].view(torch.uint8)[page, heads, kind, at % P, dims] = 0x7f
+    else:
+        c["cache"][kind][page, heads, at % P, dims] = float("nan")
+
+
+def check(c, path=AUTO, repeat=2, **kw):
+    want = ref.attend(c, **kw)
+    for _ in range(repeat):
+        out, lse, code, flags = run(c, path, **kw)
+        assert code == 0, flags
+        ref.check((out, lse), want, c, path == CUDA_CORES)
+    return want
+
+
+# ----------------------------------------------------------------------------------
+# Hidden values, in more units than a list of one note per unit and warp would hold
+# ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+def test_hidden_values_in_every_unit(fp8, D):
+    """64 sequences of 16 new tokens, 8 KV heads: in each unit a value of the tile's first half and one of
+    its second that only later tokens see."""
+    c = make([16] * 64, [56 + 128 * (i % 3) for i in range(64)], Hq=32, Hkv=8, D=D, fp8=fp8, seed=41)
+    for b in range(64):
+        base = c["lens"][b] - 16 - 56
+        spoil(c, 1, b, base + 60, dims=slice(0, 1))
+        spoil(c, 1, b, base + 66, dims=slice(1, 2))
+    want = check(c, repeat=4)
+    assert bool(torch.isfinite(want[0][:, :, 2:]).all()) and not bool(torch.isfinite(want[0]).all())
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_hidden_values_under_a_window(fp8):
+    """Every 32nd value of a long chunk NaN, a window of 8 tokens."""
+    c = make([1500, 900], [1000, 77], Hq=8, Hkv=8, D=64, fp8=fp8, seed=42)
+    for b, n in enumerate(c["lens"]):
+        for at in range(5, n, 32):
+            spoil(c, 1, b, at, dims=slice(0, 1))
+    want = check(c, repeat=4, window=8)
+    assert 0.5 < float(torch.isfinite(want[0][:, :, 0]).float().mean()) < 0.9
