@@ -472,7 +472,8 @@ __device__ __forceinline__ void join_unit(const ChunkParams& p, int c, int part,
       }
 #pragma unroll
       for (int k = 0; k < SB; ++k) {
-        if (s0 + k >= n || ml[k].x == -INFINITY) continue;  // saw no key
+        // saw no key (one whose scores are all NaN has no maximum either, but a sum)
+        if (s0 + k >= n || (ml[k].x == -INFINITY && ml[k].y == 0.f)) continue;
         const float m = fmaxf(M, ml[k].x);
         const float old = M == -INFINITY ? 0.f : ex2(M - m), x = ex2(ml[k].x - m);
         const float v[8] = {lo[k].x, lo[k].y, lo[k].z, lo[k].w, hi[k].x, hi[k].y, hi[k].z, hi[k].w};

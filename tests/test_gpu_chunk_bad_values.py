@@ -57,3 +57,45 @@ def test_hidden_values_under_a_window(fp8):
             spoil(c, 1, b, at, dims=slice(0, 1))
     want = check(c, repeat=4, window=8)
     assert 0.5 < float(torch.isfinite(want[0][:, :, 0]).float().mean()) < 0.9
+
+
+# ----------------------------------------------------------------------------------
+# What a row sees, in units that several blocks share
+# ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new", [1, 40, 200])
+def test_bad_keys_fill_a_part(fp8, new):
+    """Keys NaN over whole tiles, so that all scores of some block's part are: not a part without keys."""
+    c = make([new], [30000], Hq=4, Hkv=2, D=128, fp8=fp8, seed=43)
+    P = 16
+    for page in range(7168 // P, 9728 // P):  # 20 tiles
+        at = int(c["table"][0, page])
+        if fp8:
+            c["cache"][0].view(torch.uint8)[at, 0, 0] = 0x7f
+        else:
+            c["cache"][0][at, 0] = float("nan")
+    want = check(c)
+    assert bool(torch.isnan(want[0][:, :2]).all()) and bool(torch.isfinite(want[0][:, 2:]).all())
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new", [1, 200])
+def test_a_last_key_alone_in_its_tile(fp8, new):
+    """The last part's tile holds one key that the row sees, and it is NaN."""
+    for ctx in (30080 - new + 1, 12800 - new + 1):  # the last token begins a tile
+        c = make([new], [ctx], Hq=4, Hkv=2, D=64, fp8=fp8, seed=44)
+        assert c["lens"][0] % 128 == 1
+        spoil(c, 0, 0, c["lens"][0] - 1, heads=1)
+        want = check(c)
+        assert bool(torch.isnan(want[0][-1, 2:]).all()) and bool(torch.isfinite(want[0][-1, :2]).all())
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new,ctx", [(1, 30000), (1, 100), (3, 9000), (200, 9000), (70, 0)])
+def test_a_bad_query(fp8, new, ctx):
+    """A NaN query row: NaN and NaN, and no other row is touched."""
+    c = make([new, 2], [ctx, 300], Hq=4, Hkv=2, D=128, fp8=fp8, seed=45)
+    c["q"][new // 2, 1, 77] = float("nan")
+    want = check(c)
+    assert bool(torch.isnan(want[0][new // 2, 1]).all()) and bool(torch.isnan(want[1][new // 2, 1]))
+    assert int(torch.isnan(want[0]).sum()) == 128
