@@ -337,9 +337,12 @@ __device__ void simt_rows(const ChunkParams& p, Smem<D, TK>& sm, int b, const Ch
       float sum = p0 + p1;
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      // weights of keys that the row does not see are marked: what it sees adds 0 * value where a weight underflows
+      const int at = ctx + (row0 + r) / p.group;
+      const int from = r < nrows ? chunk_low(p, at) - t0 : TK, to = chunk_high(p, at, seq.kv_len) - t0;
       __syncwarp();
-      if (lane < TK) sm.s[r][lane] = p0;
-      if (lane + 32 < TK) sm.s[r][lane + 32] = p1;
+      if (lane < TK) sm.s[r][lane] = lane >= from && lane < to ? p0 : -1.f;
+      if (lane + 32 < TK) sm.s[r][lane + 32] = lane + 32 >= from && lane + 32 < to ? p1 : -1.f;
       if (lane == 0) {
         sm.alpha[r] = alpha;
         sm.m[r] = m_new;
@@ -359,7 +362,7 @@ __device__ void simt_rows(const ChunkParams& p, Smem<D, TK>& sm, int b, const Ch
 #pragma unroll
       for (int i = 0; i < RPT; ++i) {
         const float w = sm.s[rg + i * RG][k];
-        if (w == 0.f) continue;  // a hidden key adds nothing, whatever its value
+        if (w < 0.f) continue;  // a hidden key adds nothing, whatever its value
         o[i][0] += w * v0.x; o[i][1] += w * v0.y; o[i][2] += w * v0.z; o[i][3] += w * v0.w;
         o[i][4] += w * v1.x; o[i][5] += w * v1.y; o[i][6] += w * v1.z; o[i][7] += w * v1.w;
       }

@@ -1002,7 +1002,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         constexpr int CP = 16;
         float* const place = reinterpret_cast<float*>(smem + C::OFF_Q + C::QTILE) + ch * CP * MR;
         float2* const other = reinterpret_cast<float2*>(smem + C::OFF_XCH);
-        float w0 = 1.f, w1 = 0.f;  // what each part counts for
+        float w0 = 1.f, w1 = 0.f;  // what each part counts for; w1 < 0: it saw no key, and may have left nothing
         bar_sync(allbar, 32 * kSoftWarps);  // both M tiles have their sums
         if (h == 1 && ch == 0) other[row] = make_float2(had ? mc : -INFINITY, had ? l : 0.f);
 #pragma unroll 1
@@ -1027,13 +1027,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (real && p.lse && ch == 0) p.lse[out_row] = (top + log2f(total)) * 0.6931471805599453f;
               const float inv = 1.f / total;
               w0 *= inv;
-              w1 *= inv;
+              w1 = ml.x == -INFINITY && ml.y == 0.f ? -1.f : w1 * inv;
             }
             uint32_t pk[CP / 2];
 #pragma unroll
             for (int k = 0; k < CP; k += 2) {
               float x = __uint_as_float(o[k]) * w0, y = __uint_as_float(o[k + 1]) * w0;
-              if (w1 != 0.f) {
+              if (!(w1 < 0.f)) {
                 x = fmaf(place[k * MR + row], w1, x);
                 y = fmaf(place[(k + 1) * MR + row], w1, y);
               }

@@ -99,3 +99,44 @@ def test_a_bad_query(fp8, new, ctx):
     want = check(c)
     assert bool(torch.isnan(want[0][new // 2, 1]).all()) and bool(torch.isnan(want[1][new // 2, 1]))
     assert int(torch.isnan(want[0]).sum()) == 128
+
+
+# ----------------------------------------------------------------------------------
+# What a row sees with a weight that underflows
+# ----------------------------------------------------------------------------------
+def sink(c, b, tokens):
+    """Queries of ones, and keys of these tokens far below: weights below 2^-150."""
+    c["q"][:] = 1
+    for at in tokens:
+        page = int(c["table"][b, at // 16])
+        if c["fp8"]:
+            c["cache"][0].view(torch.uint8)[page, :, 0, at % 16] = 0xfe  # -448
+            c["cache"][1][page, :, 0] = 0.125
+        else:
+            c["cache"][0][page, :, at % 16] = -32
+
+
+@pytest.mark.parametrize("path", [CUDA_CORES, AUTO])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("new,ctx,low,bad", [
+    (1, 200, range(128, 201), 140), (1, 200, range(0, 128), 5), (1, 30000, range(20000, 20100), 20050), (200, 300, [50], 50),
+    (64, 200, [130], 130)])
+def test_bad_values_of_no_weight(path, fp8, new, ctx, low, bad):
+    c = make([new, 3], [ctx, 40], Hq=4, Hkv=2, D=64, fp8=fp8, seed=46, spread=0.25)
+    sink(c, 0, low)
+    spoil(c, 1, 0, bad, heads=1, dims=slice(7, 8))
+    want = check(c, path)
+    assert bool(torch.isnan(want[0][:new, 2:, 7]).all()) and int(torch.isnan(want[0]).sum()) == 2 * new
+
+
+@pytest.mark.parametrize("path", [CUDA_CORES, AUTO])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_bad_values_of_no_weight_beside_hidden_ones(path, fp8):
+    """A unit that is computed again because of the one keeps the other."""
+    c = make([70], [300], Hq=4, Hkv=2, D=64, fp8=fp8, seed=47, spread=0.25)
+    sink(c, 0, [33])
+    spoil(c, 1, 0, 33, heads=0, dims=slice(7, 8))
+    spoil(c, 1, 0, 350, heads=0, dims=slice(9, 10))
+    want = check(c, path)
+    assert bool(torch.isnan(want[0][:, :2, 7]).all()) and bool(torch.isfinite(want[0][:50, :, 9]).all())
+    assert bool(torch.isnan(want[0][50:, :2, 9]).all())
