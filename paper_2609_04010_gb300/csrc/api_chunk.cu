@@ -1,6 +1,7 @@
 // The C ABI of the operators that serve ragged batches (include/spec_verify.h): host-side
 // argument checks, workspace layout and launches.
 #include <climits>
+#include <initializer_list>
 
 #include "chunk.cuh"
 
@@ -113,10 +114,9 @@ spec_status_t check_fork(const spec_fork_args_t* a) {
   if (!a->parent || !a->kv_len || !a->new_kv_len || !a->page_table || !a->new_table || !a->shares || !a->new_shares ||
       !a->free_pages || !a->new_free_pages || !a->free_count || !a->new_free_count || !a->copies)
     return SPEC_ERR_INVALID_ARGUMENT;
-  for (const void* p : {static_cast<const void*>(a->parent), static_cast<const void*>(a->kv_len),
-                        static_cast<const void*>(a->page_table), static_cast<const void*>(a->new_table),
-                        static_cast<const void*>(a->shares), static_cast<const void*>(a->free_pages),
-                        static_cast<const void*>(a->copies)})
+  for (const void* p : std::initializer_list<const void*>{
+           a->parent, a->kv_len, a->new_kv_len, a->page_table, a->new_table, a->shares, a->new_shares, a->free_pages,
+           a->new_free_pages, a->free_count, a->new_free_count, a->copies, a->flags})
     if (!aligned(p, 4)) return SPEC_ERR_INVALID_ARGUMENT;
   if (a->batch > SPEC_SLOTS_MAX_BATCH || a->reserved > (1 << 30) ||
       static_cast<int64_t>(a->max_pages_per_seq) * a->page_size > (1 << 30) ||
