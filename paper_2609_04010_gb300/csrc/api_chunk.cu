@@ -74,7 +74,9 @@ spec_status_t check_chunk(const spec_chunk_attn_args_t* a) {
       static_cast<int64_t>(a->num_pages) * a->page_size > INT32_MAX || a->num_kv_heads > 65535)
     return SPEC_ERR_UNSUPPORTED;
   const int64_t group = a->num_q_heads / a->num_kv_heads;
-  if (group * (static_cast<int64_t>(a->rows) + 1) > INT32_MAX - 256) return SPEC_ERR_UNSUPPORTED;
+  if (group * (static_cast<int64_t>(a->rows) + 1) > INT32_MAX - 256 ||
+      group * a->rows / kSimtRowTile + a->batch > INT32_MAX)
+    return SPEC_ERR_UNSUPPORTED;
   if (a->path == SPEC_ATTN_TENSOR_CORES && !chunk_tc_fits(*a)) return SPEC_ERR_UNSUPPORTED;
   return SPEC_OK;
 }
@@ -168,7 +170,10 @@ ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, 
   P.seqs = base;
   P.bad = ws_round(P.seqs + sizeof(ChunkSeq) * (static_cast<size_t>(a.batch) + 1));
   P.end = ws_round(P.bad + sizeof(int32_t) * static_cast<size_t>(a.batch));
-  if (P.path != SPEC_ATTN_TENSOR_CORES) return P;
+  if (P.path != SPEC_ATTN_TENSOR_CORES) {
+    P.max_units = a.rows * (a.num_q_heads / a.num_kv_heads) / kSimtRowTile + a.batch;
+    return P;
+  }
   P.tile_tokens = kChunkTileRows / (a.num_q_heads / a.num_kv_heads);
   P.max_units = a.rows / (2 * P.tile_tokens) + a.batch;
   // a block per SM, or as many as the longest sequences could give work

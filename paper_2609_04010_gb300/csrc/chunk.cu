@@ -41,6 +41,9 @@ constexpr int kSetupThreads = 1024;
 constexpr int kSetupFew = 128;    // threads for at most as many sequences and units
 constexpr int kSetupKept = 1024;  // sequences and units that are kept in shared memory too
 
+// Blocks of RT query rows (token, head of the group) of a sequence with n new tokens, for one KV head.
+__device__ __forceinline__ int simt_units(const ChunkParams& p, int n) { return (n * p.group + RT - 1) / RT; }
+
 // The exclusive prefix sum of v in thread order over a block of THREADS threads, and the total.
 template <int THREADS>
 __device__ __forceinline__ long long scan_block(long long v, long long* sh, long long* total) {
@@ -136,7 +139,7 @@ __global__ void __launch_bounds__(THREADS) chunk_setup_kernel(ChunkParams p) {
         }
       }
     }
-    const int units = p.blocks ? chunk_units(p, s.n) : 0;
+    const int units = p.blocks ? chunk_units(p, s.n) : simt_units(p, s.n);
     long long all;
     const long long before = carry + scan_block<THREADS>(units, sh, &all);
     carry += all;
@@ -153,10 +156,10 @@ __global__ void __launch_bounds__(THREADS) chunk_setup_kernel(ChunkParams p) {
       if (b < kSetupKept) seq_kept[b] = s;
     }
   }
-  if (!p.blocks) return;
   const int nunits = static_cast<int>(min(carry, static_cast<long long>(p.max_units)));
+  if (tid == 0) p.seqs[p.batch] = {0, 0, 0, nunits};
+  if (!p.blocks) return;
   if (tid == 0) {
-    p.seqs[p.batch] = {0, 0, 0, nunits};
     if (p.batch <= kSetupKept) seq_kept[p.batch] = {0, 0, 0, nunits};
     p.redo[0] = make_int4(0, 0, 0, 0);
     p.cum[0] = 0;
@@ -386,27 +389,23 @@ __device__ void simt_rows(const ChunkParams& p, Smem<D, TK>& sm, int b, const Ch
   }
 }
 
-// Blocks own 16 of the batch's rows * group query rows of a KV head; one that spans sequences
-// takes them in turn.
+// A block owns 16 query rows of a sequence and KV head, found by its place in the prefix sums of the
+// set-up (row_start itself need not rise where sequences are left out).
 template <int D, bool FP8>
 __global__ void __launch_bounds__(NT) chunk_simt_kernel(ChunkParams p) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   Smem<D, kSimtKeyTile>& sm = *reinterpret_cast<Smem<D, kSimtKeyTile>*>(smem_raw);
   pdl_wait_prior();
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * RT, last = first + RT;
-  const int g = blockIdx.y;
-  int lo = 0, hi = p.batch;  // the first sequence whose rows end past `first`
-  while (lo < hi) {
+  const int unit = blockIdx.x;
+  if (unit >= p.seqs[p.batch].first_unit) return;
+  int lo = 0, hi = p.batch;  // the largest b with first_unit <= unit
+  while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (static_cast<int64_t>(p.row_start[mid + 1]) * p.group > first) hi = mid; else lo = mid + 1;
+    if (p.seqs[mid].first_unit <= unit) lo = mid; else hi = mid;
   }
-  for (int b = lo; b < p.batch && static_cast<int64_t>(p.row_start[b]) * p.group < last; ++b) {
-    const ChunkSeq seq = p.seqs[b];
-    if (seq.n == 0) continue;
-    const int64_t start = static_cast<int64_t>(seq.row0) * p.group, end = start + static_cast<int64_t>(seq.n) * p.group;
-    const int64_t from = max(first, start), to = min(last, end);
-    if (from < to) simt_rows<D, FP8>(p, sm, b, seq, g, static_cast<int>(from - start), static_cast<int>(to - from));
-  }
+  const ChunkSeq seq = p.seqs[lo];
+  const int row0 = (unit - seq.first_unit) * RT, nrows = min(RT, seq.n * p.group - row0);
+  if (nrows > 0) simt_rows<D, FP8>(p, sm, lo, seq, blockIdx.y, row0, nrows);
 }
 
 // The end of a call: joins the parts of units that blocks split, computes again the units in
@@ -536,8 +535,7 @@ cudaError_t launch_simt_d(const ChunkParams& p, cudaStream_t stream) {
   const cudaError_t e = cudaFuncSetAttribute(chunk_simt_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  const int64_t tiles = (static_cast<int64_t>(p.rows) * p.group + RT - 1) / RT;
-  return launch_overlapped(chunk_simt_kernel<D, FP8>, dim3(static_cast<unsigned>(tiles), p.hkv), NT, smem, stream, p);
+  return launch_overlapped(chunk_simt_kernel<D, FP8>, dim3(p.max_units, p.hkv), NT, smem, stream, p);
 }
 
 template <int D, bool FP8>
@@ -584,9 +582,9 @@ ChunkParams make_chunk_params(const spec_chunk_attn_args_t& a, const ChunkPlan& 
   p.status = reinterpret_cast<uint32_t*>(ws);
   p.seqs = reinterpret_cast<ChunkSeq*>(ws + P.seqs);
   p.seq_bad = reinterpret_cast<int32_t*>(ws + P.bad);
+  p.max_units = P.max_units;
   if (P.path == SPEC_ATTN_TENSOR_CORES) {
     p.tile_tokens = P.tile_tokens;
-    p.max_units = P.max_units;
     p.blocks = P.grid;
     p.cum = reinterpret_cast<long long*>(ws + P.cum);
     p.work = reinterpret_cast<ChunkWork*>(ws + P.work);

@@ -20,7 +20,7 @@ struct ChunkPlan {
   int fp8;           // the cache is the 8-bit one
   int tile_tokens;   // tensor cores: tokens of an M tile, 128 / group
   int grid;          // tensor cores: blocks
-  int max_units;     // tensor cores: units per KV head, at most
+  int max_units;     // units per KV head, at most
   int redo_cap;      // tensor cores: units that may have to be computed again
   size_t seqs, bad, cum, work, redo, partial_o, partial_ml, q_half, q_scale, end;
 };
@@ -44,7 +44,7 @@ constexpr int kChunkStart8 = 4, kChunkTwinStart8 = 3;
 struct ChunkSeq {
   int row0, n;     // its rows of q; n = 0: nothing to do
   int kv_len;
-  int first_unit;  // its first unit among all (tensor cores)
+  int first_unit;  // its first unit among all
 };
 // The work list of the tensor-core kernel, and where each block starts in it: the sequence and what is
 // known of it, the KV head, the unit of its tokens, the virtual step in it, and the steps to take.
@@ -76,8 +76,9 @@ struct ChunkParams {
   uint32_t* status;
   int32_t* seq_bad;  // [batch]: its rows become out = 0, lse = -inf at the end
   ChunkSeq* seqs;    // [batch + 1]
+  int max_units;     // there is room for: tensor cores, a ChunkUnit each; CUDA cores, blocks of kSimtRowTile query rows
   // tensor cores (blocks = 0: not used)
-  int tile_tokens, max_units, blocks;
+  int tile_tokens, blocks;
   long long* cum;      // [max_units + 1]: virtual steps before a unit, for one KV head
   ChunkWork* work;
   int4* redo;          // [0].x: how many; then (sequence, KV head, unit) to compute again
