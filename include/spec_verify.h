@@ -774,8 +774,9 @@ spec_status_t spec_rope_kv(const spec_rope_args_t* rope, spec_stream_t stream);
  *     not negative, of any fraction; value scales are clamped to [2^-32, 2^32].
  *   - path: SPEC_ATTN_AUTO takes the tensor cores where the call fits them (Hq / Hkv at most 128),
  *     else CUDA cores; SPEC_ATTN_TENSOR_CORES is SPEC_ERR_UNSUPPORTED where it does not fit.
- *   - Three launches. The workspace rules are spec_verify_attention's; it holds the parts of
- *     sequences that several blocks share and, with the 8-bit cache, the queries in fp16.
+ *   - Three launches. The workspace rules are spec_verify_attention's, but of a new one only the
+ *     first 256 bytes need be zero; it holds the parts of sequences that several blocks share and,
+ *     with the 8-bit cache, the queries in fp16.
  */
 typedef struct {
   int32_t batch;              /* >= 1                                                       */

@@ -35,6 +35,7 @@ FLAG_BAD_FILTER = 32
 FLAG_BAD_TREE = 64
 FILTER_MAX_TOP_K = 1024
 COPY_MAX_BUFFERS = 128
+WS_HEADER = 256  # bytes of a workspace that hold its status word
 
 
 class SpecError(RuntimeError):
@@ -1277,6 +1278,14 @@ def chunk_attn_workspace_size(a: ChunkAttnArgs) -> int:
     return int(n)
 
 
+def new_chunk_attn_workspace(a: ChunkAttnArgs) -> torch.Tensor:
+    """A workspace for this call: only its header (the status word) is zero-filled, each call writes
+    the rest, tens of MB, before it reads it."""
+    ws = torch.empty(chunk_attn_workspace_size(a), dtype=torch.uint8, device=a.device)
+    ws[:WS_HEADER].zero_()
+    return ws
+
+
 def chunk_attention_args(a: ChunkAttnArgs, ws: torch.Tensor, stream=None):
     _call("spec_chunk_attention", a, stream, ws)
 
@@ -1292,13 +1301,15 @@ def chunk_attention(q, cache, page_table, row_start, kv_len, softmax_scale=0.0, 
                     causal: bool = True, window: int = 0, want_lse: bool = True, ws=None, stream=None):
     """Attention of a packed ragged batch q [rows][Hq][D] over a paged cache (spec_chunk_attention):
     cache = (k_cache, v_cache) or (kv_cache, kv_scale); row_start and kv_len as map_slots leaves
-    them. Returns (out bf16, lse fp32 or None); rows past row_start[-1] are 0 and -inf."""
+    them. Returns (out bf16, lse fp32 or None); rows past row_start[-1] are 0 and -inf. The status
+    (bad pages or lengths, a wait that ran out) is in ws: give one (new_chunk_attn_workspace) and
+    read it with read_device_status."""
     out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
     lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float32, device=q.device) if want_lse else None
     a = chunk_attn_args(q, cache, page_table, row_start, kv_len, out, lse, softmax_scale, path, causal,
                         window)
     if ws is None:
-        ws = new_workspace(chunk_attn_workspace_size(a), q.device)
+        ws = new_chunk_attn_workspace(a)
     chunk_attention_args(a, ws, stream)
     return out, lse
 
