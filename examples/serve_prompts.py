@@ -47,7 +47,8 @@ class Server:
         self.table = torch.full((batch, max_pages), -1, **i32)
         self.free, self.free_count = torch.arange(N, **i32), torch.tensor([N], **i32)
         self.shares, self.kv_len = torch.zeros(N, **i32), torch.zeros(batch, **i32)
-        self.status = b.new_workspace(256)
+        self.status = b.new_workspace(256)  # of cache writes and page copies
+        self.attn_ws, self.attn_rows = None, 0
         self.waiting = [[] for _ in range(batch)]  # tokens that a sequence has yet to bring
 
     def submit(self, prompts):
@@ -67,11 +68,32 @@ class Server:
         x = self.embed[torch.tensor(tokens, device="cuda")]
         where = b.map_slots(new, self.kv_len, self.table, self.P, self.shares.numel(), self.free, self.free_count,
                             len(tokens))
+        self._refused(where["flags"], "no pages for new tokens")
+        self._room(len(tokens))
         for layer in range(self.L):
             x = self._layer(layer, x, where)
+        self._check()
         ends = where["row_start"][1:].long() - 1
         logits = (x[ends.clamp_min(0)] @ self.head).float()
         return [logits[i] if n else None for i, n in enumerate(take)]
+
+    def _room(self, rows):
+        """The workspace of every layer's attention, which also holds its status, for steps of `rows` tokens."""
+        if rows > self.attn_rows:
+            q = torch.empty(rows, self.Hq, self.D, dtype=torch.bfloat16, device="cuda")
+            starts = torch.zeros(self.B + 1, dtype=torch.int32, device="cuda")
+            a = b.chunk_attn_args(q, self.caches[0], self.table, starts, self.kv_len, q)
+            self.attn_ws, self.attn_rows = b.new_chunk_attn_workspace(a), rows
+
+    def _refused(self, flags, what):
+        if bool(flags.any()):
+            raise RuntimeError(f"{what}: sequences {flags.nonzero().flatten().tolist()}")
+
+    def _check(self):
+        for ws, what in ((self.status, "cache writes or page copies"), (self.attn_ws, "attention")):
+            code, flags = b.read_device_status(ws) if ws is not None else (0, 0)
+            if code:
+                raise RuntimeError(f"{what}: status {code}, flags {flags}")
 
     def _layer(self, layer, x, where):
         q, k, v = (x @ self.wqkv[layer]).unflatten(-1, (-1, self.D)).split([self.Hq, self.H, self.H], 1)
@@ -82,7 +104,8 @@ class Server:
         else:
             q, _ = b.rope_kv(q, k, v, where["positions"], self.turns, where["slots"], *cache, factor=self.factor,
                              in_place=True, status_ws=self.status)
-        out, _ = b.chunk_attention(q, cache, self.table, where["row_start"], self.kv_len, window=self.window)
+        out, _ = b.chunk_attention(q, cache, self.table, where["row_start"], self.kv_len, window=self.window,
+                                   ws=self.attn_ws)
         return x + out.flatten(1) @ self.wo[layer]
 
     def fork(self, parent):
@@ -90,6 +113,8 @@ class Server:
         res = b.fork_sequences(torch.tensor(parent, dtype=torch.int32, device="cuda"), self.kv_len, self.table,
                                self.shares, self.free, self.free_count, self.P)
         b.copy_pages(res["copies"], [x for cache in self.caches for x in cache], self.status)
+        self._refused(res["flags"], "not forked")
+        self._check()
         self.waiting = [list(self.waiting[q]) if q >= 0 else [] for q in parent]
         return res
 
