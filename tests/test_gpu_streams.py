@@ -96,3 +96,26 @@ def test_map_slots():
         res = b.map_slots(new, t["kv_len"], t["table"], 16, 5000, t["free"], t["count"], 700, stream=stream)
         return [*t.values(), *res.values()]
     check(call)
+
+
+def test_a_captured_stream():
+    """Calls that are given the stream under capture, with what they make in the graph's own memory."""
+    from paper_2609_04010_gb300 import binding as b
+    c = make([300, 1, 5], [700, 9000, 41], seed=35)
+    starts, lens = i32(c["starts"]), i32(c["lens"])
+    positions, t = i32(np.arange(c["rows"])), b.rope_turns(b.rope_frequencies(128)[0])
+
+    def call(stream):
+        q, _ = b.rope_kv(c["q"], None, None, positions, t, stream=stream)
+        return b.chunk_attention(q, c["cache"], c["table"], starts, lens, stream=stream)
+    want = [x.clone() for x in call(None)]
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        got = call(s)
+    for _ in range(3):
+        for x in got:
+            x.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
