@@ -179,7 +179,8 @@ ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, 
   // a block per SM, or as many as the longest sequences could give work
   const int64_t work = static_cast<int64_t>(P.max_units) * a.num_kv_heads * chunk_longest(a) / kChunkTwinCost;
   P.grid = static_cast<int>(work < num_sms ? (work < 1 ? 1 : work) : num_sms);
-  P.redo_cap = P.max_units * a.num_kv_heads + P.grid;  // stops of all blocks, which note their unit once each
+  // one note a stop of a block, of each warp that notes
+  P.redo_cap = (P.max_units * a.num_kv_heads + P.grid) * (P.fp8 ? kChunkConverters : 1);
   const size_t rows = static_cast<size_t>(P.grid) * 2 * 2 * kChunkTileRows;
   P.cum = P.end;
   P.work = ws_round(P.cum + sizeof(long long) * (static_cast<size_t>(P.max_units) + 1));

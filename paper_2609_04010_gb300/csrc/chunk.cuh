@@ -21,13 +21,14 @@ struct ChunkPlan {
   int tile_tokens;   // tensor cores: tokens of an M tile, 128 / group
   int grid;          // tensor cores: blocks
   int max_units;     // units per KV head, at most
-  int redo_cap;      // tensor cores: units that may have to be computed again
+  int redo_cap;      // tensor cores: notes of units that have to be computed again, at most
   size_t seqs, bad, cum, work, redo, partial_o, partial_ml, q_half, q_scale, end;
 };
 bool chunk_tc_fits(const spec_chunk_attn_args_t& a);
 ChunkPlan chunk_plan(const spec_chunk_attn_args_t& a, size_t base, int num_sms, int path);
 constexpr int kChunkKeyTile = 128;     // keys of a tile on the tensor cores
 constexpr int kChunkTileRows = 128;    // query rows of an M tile
+constexpr int kChunkConverters = 2;    // warps that convert the 8-bit cache's tiles
 // The work list counts in virtual steps: what a step costs (a twin's reads twice the bytes for the same
 // products), and what a unit's start costs (its queries, the pipeline's refill, the outputs before).
 // 60 requests decoding beside four chunks take 668 us; with a step of either kind at 1 and a start at

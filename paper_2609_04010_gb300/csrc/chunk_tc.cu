@@ -83,7 +83,7 @@ struct RawTile {
   uint32_t stop;
   int more;  // another tile follows
 };
-constexpr int kConverters = 2;
+constexpr int kConverters = kChunkConverters;
 
 template <int D, bool FP8>
 struct Cfg {
@@ -114,7 +114,7 @@ struct Cfg {
   // k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], v_ready[VST], s_full[2], p_full[2],
   // o_full[2], q_full, q_free, drain, joined[2], raw_full[2], raw_empty[2]
   static constexpr int NBAR = 2 * KST + 3 * VST + 15;
-  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort, noted
+  static constexpr uint32_t OFF_MISC = OFF_BAR + NBAR * 8;  // tmem base, abort
   static constexpr uint32_t BYTES = OFF_MISC + 16;
   static constexpr size_t SMEM = BYTES;
   static_assert(SMEM <= kTcMaxSmem, "a block's shared memory");
@@ -385,7 +385,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(bar0 + 8u * i, n);
     }
     *abort_flag = 0;
-    misc[2] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kSoftWarps + 2) tmem_alloc(smem_u32(misc), C::TMEM_COLS);
@@ -412,10 +411,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     fewer_registers<FP8>();
     const int part = warp == kSoftWarps ? -1 : warp == kSoftWarps + 1 ? 0 : 1;  // -1: the producer
     RawTile* const notes = reinterpret_cast<RawTile*>(smem + C::OFF_RAWS);
-    uint32_t made = 0;  // tiles converted
-    // The last stop whose unit was noted, + 1, of both converters: the list has one place a stop. They are
-    // at the same tile's values, since the next ones are brought when both have read these.
-    uint32_t* const noted = misc + 2;
+    // tiles converted; stops + 1 of the last unit noted for redoing, by each converter (one word for both, in
+    // shared memory: 533 us where two chunks of 2,048 tokens take 527)
+    uint32_t made = 0, noted = 0;
     auto convert = [&](int kind) {
       const uint32_t st = made % (kind ? VST : KST), use = made / (kind ? VST : KST);
       wait(raw_full(kind), made & 1);
@@ -425,9 +423,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const unsigned char* raw = smem + C::OFF_RAW + kind * C::RAW;
       if (kind) {
         const bool odd = convert_tile<D, true>(raw, smem + C::OFF_V + st * C::TILE, t, part);
-        if (__any_sync(0xffffffffu, odd) && lane == 0 && atomicExch(noted, t.stop + 1) != t.stop + 1) {
-          const int n = atomicAdd(&p.redo[0].x, 1);
-          if (n < p.redo_cap) p.redo[1 + n] = make_int4(t.b, t.g, t.rt, 0);
+        if (__any_sync(0xffffffffu, odd) && noted != t.stop + 1) {
+          noted = t.stop + 1;
+          if (lane == 0) {
+            const int n = atomicAdd(&p.redo[0].x, 1);
+            if (n < p.redo_cap) p.redo[1 + n] = make_int4(t.b, t.g, t.rt, 0);
+          }
         }
       } else {
         convert_tile<D, false>(raw, smem + C::OFF_K + st * C::TILE, t, part);
