@@ -760,8 +760,8 @@ spec_status_t spec_rope_kv(const spec_rope_args_t* rope, spec_stream_t stream);
  *   sides, as in a drafter's pass over its block), and, with window > 0, k > t - window;
  *   out = sum_k softmax_k(scale * q.k_k) v_k, lse = log sum_k exp(scale * q.k_k) (natural log).
  *   - What a row's mask hides does not reach it, whatever the bytes there, and page ids that only
- *     hidden keys use are not looked at. A row whose visible scores are all -inf gets out = NaN
- *     and lse = -inf.
+ *     hidden keys use are not looked at. A NaN that it sees does, however small the weight. A row
+ *     whose visible scores are all -inf gets out = NaN and lse = -inf.
  *   - Rows past row_start[batch] are not written. A sequence whose rows do not lie in
  *     [0, rows) in order is left out; one with rows but kv_len[b] outside [n_b,
  *     max_pages_per_seq * page_size] gets out = 0 and lse = -inf (both SPEC_FLAG_BAD_KV_LEN), as

@@ -176,8 +176,8 @@ struct ChunkWalk {
     ns = u.step_at(off + take) - s0;
     left -= take;
   }
-  // A range has at least kChunkTwinCost virtual steps, so that it has a step of a unit that it lies
-  // within; the first stop of one that begins at the very end of a unit has none, and is passed.
+  // The first stop of a range that begins at the very end of a unit has no step, and is passed. A range may
+  // lie wholly within a unit's start: it has none at all, and the unit's steps are the next block's.
   __device__ __forceinline__ bool begin(const ChunkParams& p, int block) {
     const int4* at = reinterpret_cast<const int4*>(&p.work->starts[block]);
     const int4 x = at[0], y = at[1];

@@ -6,7 +6,9 @@
 // with P = 2^(c S - m), c = softmax scale * log2(e), a reference m per row that is raised only
 // when a weight would pass 2^8, and the output O / sum P. A block holds a unit: two M tiles of the
 // query rows (token, head of the group) of consecutive tokens and one KV head. Each tile of 128
-// keys is read once for both; while one M tile is at its softmax the tensor core works for the
+// keys is read once for both (weights are bf16, off by 2^-8 of themselves, because values are and a
+// product's operands have one type; l is the fp32 sum of the weights before that, so that nothing drifts);
+// while one M tile is at its softmax the tensor core works for the
 // other. A unit with no more rows than one M tile holds them twice and gives every second tile of
 // keys to each ("twin"), so that single tokens keep two tiles in flight too.
 //
@@ -29,18 +31,21 @@
 // units are joined by the finishing launch. Every wait is bounded: one that runs out sets
 // SPEC_FLAG_TIMEOUT, and the block drains its copies and products, frees TMEM and returns.
 //
-// What bounds it. Long chunks (4,096 tokens behind 28,672, 32 / 8 heads): 1,306 us, 1,578 TFLOP/s of
-// Q K^T and P V (1,893 measured peak); without the softmax's work the same code takes 1,150, the
-// products' own time and the turns between them. Whole prompts (4 x 4,093): 458 us, 1,200 TFLOP/s: a unit
-// of 64 tokens has 17 steps on average, and its outputs and first weights, about 4 steps of time, are
-// not hidden. Single tokens (32 requests to 16,384 tokens): 200 us, 5.5 TB/s, 0.81 of the copy rate: a
-// step's five tiles in flight. 8-bit, two chunks of 2,048 tokens: 522 us, 1,180 TFLOP/s:
+// What bounds it. Long chunks (4,096 tokens behind 28,672, 32 / 8 heads): 1,317 us by itself, 1,565 TFLOP/s of
+// Q K^T and P V (1,893 measured peak), 1,452 in a row under the power cap (1,420 of 1,717); without the
+// softmax's work the same code takes 1,150 by itself, the products' own time and the turns between them.
+// Whole prompts (4 x 4,093): 468 us, 1,173 TFLOP/s: a unit of 64 tokens has 17 steps on average, and its
+// outputs and first weights, about 4 steps of time, are not hidden. Single tokens (32 requests to 16,384
+// tokens): 195 us, 5.6 TB/s, 0.83 of the copy rate: a step's five tiles in flight. 8-bit, two chunks of 2,048
+// tokens: 527 us, 1,167 TFLOP/s:
 // two warps make 32,768 values fp16 a step, 2,570 of its 3,860 cycles, in shared memory that the products
 // read most of the time.
-// What was measured on the way (long chunk): one softmax thread per row 1,697 us (eight warps cannot
+// What was measured on the way (long chunk by itself): one softmax thread per row 1,697 us (eight warps cannot
 // hide each other's waits); two product warps in turns 1,446; products issued by "lane == 0" instead of
-// an elected lane 1,404; registers spilled in any role's loop 1,800 to 2,900, because next to 226 KB of
-// shared memory there is hardly any L1; outputs written after the next unit's first weights 1,626.
+// an elected lane 1,404; registers spilled throughout a role's loop 1,800 to 2,900, because next to 226 KB of
+// shared memory there is hardly any L1; outputs written after the next unit's first weights 1,626. What
+// the compiler still spills, 16 bytes a thread (8-bit cache: 48), a block's warps load 82 times (16,400) in
+// the 200 steps of a chunk of 2,048 tokens behind 14,336: at a unit's ends (five times a softmax warp's tile).
 
 #include <cuda.h>  // CUtensorMap
 #include <cuda_bf16.h>
@@ -239,7 +244,7 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_low, u
 }
 
 // One lane of a converged warp. (The compiler knows that it is one; with lane == 0 in its place the
-// products' operands cost more than the products hide: a long prompt took 1,404 us instead of 1,304.)
+// products' operands cost more than the products hide: a long prompt took 1,404 us instead of 1,306.)
 __device__ __forceinline__ bool elected() {
   uint32_t one;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));

@@ -67,9 +67,10 @@ __device__ __forceinline__ void for_entries(const int32_t* row, int n, F f) {
 // pages keep one order whatever the order of the blocks: a page goes to the last place that
 // held it, by a minimum over the places, and places are counted in order.
 //
-// What bounds it is latency: seven passes (who goes on, the scan, the rows, claims, counts, the list, the
-// lengths), each a round trip or two to L2 and a barrier of the blocks. 512 sequences of up to 8,192
-// tokens, a quarter of which fork or end: 29 us with up to 16 blocks, 41 with 8, 78 with a load at a time.
+// What bounds it is latency: a chain of passes (who goes on and the scan, the rows, claims, counts, the list),
+// each a round trip or two to L2, and four barriers of the cluster between them (five in place). 512 sequences
+// of up to 8,192 tokens, a quarter of which fork or end: 23.6 us; when up to 16 blocks were first taken 29,
+// where 8 took 41 and a load at a time 78.
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constant__ ForkParams p) {
   extern __shared__ int32_t smem[];
   const spec_fork_args_t& a = p.a;
